@@ -62,9 +62,9 @@ typedef enum fh_status {
     FH_ERR_ALIGNMENT = 8,
     FH_ERR_LAUNCH = 9,           /* the HIP runtime refused the launch */
     FH_ERR_BAD_COUNT = 10,       /* negative item count */
-    FH_ERR_BAD_SHAPE = 11,       /* outer / channels / inner / raw_channels out of range */
-    FH_ERR_BAD_PARAM = 12,       /* k_sigma not positive, min_outliers < 1, a pooling window other than 2, 4, 8,
-                                    or a reserved field that is not 0 */
+    FH_ERR_BAD_SHAPE = 11,       /* outer / channels / inner / raw_channels, or rows / cols / a row stride out of range */
+    FH_ERR_BAD_PARAM = 12,       /* k_sigma not positive, min_outliers < 1, a pooling window other than 2, 4, 8, a negative eps
+                                    of a norm, or a reserved field that is not 0 */
     FH_ERR_SCRATCH_LIMIT = 13    /* the tensor needs more scratch than the library's static buffer holds */
 } fh_status;
 
@@ -480,6 +480,97 @@ fh_status fh_mix_compress(const fh_mix_item *item, void *stream);
 fh_status fh_mix_decompress(const fh_mix_item *item, void *stream);
 fh_status fh_mix_compress_batch(const fh_mix_item *items, int32_t count, void *stream);
 fh_status fh_mix_decompress_batch(const fh_mix_item *items, int32_t count, void *stream);
+
+/* ---- microscaled 4-bit storage and its product -----------------------------------------
+ * Saved activations whose stored form is a matrix product's operand: a layer's input kept in
+ * this form needs no restore before the weight's gradient is computed.  A matrix of rows x
+ * cols is stored with 32 consecutive values of a row sharing a scale 2^(s-127) (s a byte):
+ *
+ *   - top = the largest magnitude of the block; s = max(floor(log2 top) - 2 + 127, 1), and 1
+ *     where top is below 2^-124; where the block holds a NaN or an infinity s = 255 and all
+ *     codes are 0: the whole block, and every sum it enters, is NaN;
+ *   - t = min(|v| * 2^(127-s), 6) becomes one of {0, 0.5, 1, 1.5, 2, 3, 4, 6}, codes 0 .. 7, by
+ *       nearest:    ties to the even code;
+ *       stochastic: up iff u < f, f the way from the lower value to the upper one, rounded to a
+ *                   multiple of 2^-22, u = h / 2^16, where h are 16 bits of Philox4x32-10: key =
+ *                   seed, counter = ((row / 8) * cols + column, tensor_id), half-word row mod 8
+ *                   of the four output words in little-endian order (row and column of the
+ *                   tensor as given, whichever way its blocks run);
+ *     bit 3 of the code is the value's sign (also of a zero);
+ *   - rows are padded with zeros to a multiple of 256 values; value c of a row is in byte c/2
+ *     of the row's codes, the even one in the low half; row r's codes begin at byte
+ *     r * 128 * ceil(cols/256);
+ *   - the scales follow at fh_mx_scales_offset(): block b of row r at byte
+ *     ((r/32) * ceil(cols/256) + b/8) * 256 + (b mod 8)/4 * 128 + (r mod 32) * 4 + b mod 4;
+ *     bytes of rows past the last are unspecified.
+ *
+ * fh_mx_quantize stores x (row r from element r * row_stride on, row_stride >= cols) with its
+ * blocks along the rows (by_rows), along the columns (by_columns: the stored form of the
+ * transposed matrix, cols x rows), or both; either pointer may be NULL.
+ * fh_mx_dequantize restores value = code * 2^(s-127) (s = 0 is 2^-127), rounded to out_dtype.
+ * fh_mx_matmul computes out[i][j] = sum_k a[i][k] * b[j][k] + bias[j] of the stored matrices a
+ * (m x k) and b (n x k) in binary32 and rounds once to out_dtype.  For y = x W^T: a = x by rows,
+ * b = W by rows; for dx = dy W: a = dy by rows, b = W by columns; for dW = dy^T x: a = dy by
+ * columns, b = x by columns.  bias may be NULL.  k = 0 gives the bias, or zeros.
+ *
+ * Stored matrices and workspaces are 16-byte aligned, plain matrices and vectors aligned to
+ * their elements.  rows, cols <= 2^31 - 256 (product: k <= 2^24); row_stride <= 2^31.  Nothing
+ * is launched where there is no output.  The sums' order depends on the shapes alone. */
+size_t    fh_mx_bytes(int64_t rows, int64_t cols);             /* of a stored matrix; 0 for a bad shape */
+size_t    fh_mx_scales_offset(int64_t rows, int64_t cols);
+fh_status fh_mx_quantize(const void *x, fh_dtype x_dtype, int64_t rows, int64_t cols, int64_t row_stride, int32_t rounding,
+                         uint64_t seed, uint64_t tensor_id, void *by_rows, size_t by_rows_cap,
+                         void *by_columns, size_t by_columns_cap, void *stream);
+fh_status fh_mx_dequantize(const void *stored, size_t stored_cap, int64_t rows, int64_t cols, fh_dtype out_dtype,
+                           void *out, int64_t row_stride, size_t out_cap, void *stream);
+typedef struct fh_mx_product {
+    const void *a;          size_t a_cap;       /* >= fh_mx_bytes(m, k) */
+    const void *b;          size_t b_cap;       /* >= fh_mx_bytes(n, k) */
+    int64_t     m, n, k;
+    const void *bias;                           /* NULL, or n values of bias_dtype */
+    int32_t     bias_dtype; int32_t out_dtype;  /* fh_dtype */
+    void       *out;        int64_t stride;     /* row i from element i * stride on, stride >= n */
+    size_t      out_cap;
+    void       *workspace;  size_t workspace_cap;   /* >= fh_mx_matmul_workspace_bytes(m, n, k), NULL if that is 0 */
+    int64_t     reserved;                       /* 0 */
+} fh_mx_product;
+size_t    fh_mx_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
+fh_status fh_mx_matmul(const fh_mx_product *product, void *stream);
+
+/* ---- layer norm ----------------------------------------------------------------------------
+ * Over the columns of every row, in binary32:  mean = sum x / cols,
+ * rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps),  y = fma((x - mean) * rstd, weight, bias),
+ * rounded to the dtype of x.  weight and bias (of p_dtype, cols values) may be NULL: 1 and 0.
+ * mean and rstd (float, a value per row) may be NULL in the forward call.
+ *
+ * fh_layer_norm_mx stores y in microscaled form instead, quantised from the binary32 value
+ * (fh_mx_quantize's rules and arguments); with by_columns or stochastic rounding mean and rstd
+ * are required.
+ * fh_layer_norm_backward: with h = (x - mean) * rstd and g = dy * weight
+ *   dx = rstd * (g - sum g / cols - h * sum (g * h) / cols),  dweight = sum_rows dy * h,
+ *   dbias = sum_rows dy;  dx in the dtype of x and dy, the sums in p_dtype.  dx, dweight and dbias may be
+ *   NULL.  With a sum wanted and rows > 0 the workspace is required.  The sums' order depends on
+ *   the shape alone.  rows = 0 writes zeros to dweight and dbias.
+ * cols >= 1; pointers aligned to their elements (workspace: 16 bytes); row strides in elements,
+ * >= cols, <= 2^31.  y and dx may be x and dy themselves (same stride), no other overlap is allowed. */
+fh_status fh_layer_norm(const void *x, fh_dtype dtype, int64_t rows, int64_t cols, int64_t x_stride, const void *weight,
+                        const void *bias, fh_dtype p_dtype, float eps, void *y, int64_t y_stride, size_t y_cap,
+                        void *mean, void *rstd, void *stream);
+fh_status fh_layer_norm_mx(const void *x, fh_dtype x_dtype, int64_t rows, int64_t cols, int64_t row_stride,
+                           const void *weight, const void *bias, fh_dtype p_dtype, float eps, int32_t rounding,
+                           uint64_t seed, uint64_t tensor_id, void *by_rows, size_t by_rows_cap,
+                           void *by_columns, size_t by_columns_cap, void *mean, void *rstd, void *stream);
+typedef struct fh_norm_backward {
+    const void *dy, *x;     int64_t dy_stride, x_stride;
+    const void *mean, *rstd, *weight;
+    int64_t     rows, cols;
+    int32_t     dtype, p_dtype;                 /* fh_dtype: of dy, x, dx; of weight, dweight, dbias */
+    void       *dx;         int64_t dx_stride;  size_t dx_cap;
+    void       *dweight, *dbias;
+    void       *workspace;  size_t workspace_cap;   /* >= fh_layer_norm_backward_workspace_bytes(rows, cols) */
+} fh_norm_backward;
+size_t    fh_layer_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
+fh_status fh_layer_norm_backward(const fh_norm_backward *norm, void *stream);
 
 const char *fh_status_string(fh_status s);
 

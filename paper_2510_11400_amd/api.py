@@ -40,6 +40,8 @@ EXPORTS = ("fh_packed_bytes", "fh_meta_bytes", "fh_compress", "fh_decompress", "
            "fh_huffman_stream_bytes", "fh_huffman_workspace_bytes", "fh_huffman_encode", "fh_huffman_decode",
            "fh_huffman_encode_batch", "fh_huffman_decode_batch", "fh_huffman_batch_capacity",
            "fh_mix_layout", "fh_mix_compress", "fh_mix_decompress", "fh_mix_compress_batch", "fh_mix_decompress_batch",
+           "fh_mx_bytes", "fh_mx_scales_offset", "fh_mx_quantize", "fh_mx_dequantize", "fh_mx_matmul_workspace_bytes", "fh_mx_matmul",
+           "fh_layer_norm", "fh_layer_norm_mx", "fh_layer_norm_backward_workspace_bytes", "fh_layer_norm_backward",
            "fh_status_string")
 
 
@@ -250,6 +252,50 @@ for _name in ("fh_mix_compress", "fh_mix_decompress"):
 for _name in ("fh_mix_compress_batch", "fh_mix_decompress_batch"):
     getattr(_lib, _name).argtypes = [_P(fh_mix_item), ctypes.c_int32, ctypes.c_void_p]
     getattr(_lib, _name).restype = ctypes.c_int
+
+
+class fh_mx_product(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_void_p), ("a_cap", ctypes.c_size_t), ("b", ctypes.c_void_p), ("b_cap", ctypes.c_size_t),
+                ("m", ctypes.c_int64), ("n", ctypes.c_int64), ("k", ctypes.c_int64),
+                ("bias", ctypes.c_void_p), ("bias_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("out", ctypes.c_void_p), ("stride", ctypes.c_int64), ("out_cap", ctypes.c_size_t),
+                ("workspace", ctypes.c_void_p), ("workspace_cap", ctypes.c_size_t), ("reserved", ctypes.c_int64)]
+
+
+class fh_norm_backward(ctypes.Structure):
+    _fields_ = [("dy", ctypes.c_void_p), ("x", ctypes.c_void_p), ("dy_stride", ctypes.c_int64), ("x_stride", ctypes.c_int64),
+                ("mean", ctypes.c_void_p), ("rstd", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("dtype", ctypes.c_int32), ("p_dtype", ctypes.c_int32),
+                ("dx", ctypes.c_void_p), ("dx_stride", ctypes.c_int64), ("dx_cap", ctypes.c_size_t),
+                ("dweight", ctypes.c_void_p), ("dbias", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_cap", ctypes.c_size_t)]
+
+
+for _name in ("fh_mx_bytes", "fh_mx_scales_offset", "fh_layer_norm_backward_workspace_bytes"):
+    getattr(_lib, _name).argtypes = [ctypes.c_int64, ctypes.c_int64]
+    getattr(_lib, _name).restype = ctypes.c_size_t
+_lib.fh_mx_matmul_workspace_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64]
+_lib.fh_mx_matmul_workspace_bytes.restype = ctypes.c_size_t
+_lib.fh_mx_quantize.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32,
+                                ctypes.c_uint64, ctypes.c_uint64, ctypes.c_void_p, ctypes.c_size_t,
+                                ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+_lib.fh_mx_quantize.restype = ctypes.c_int
+_lib.fh_mx_dequantize.argtypes = [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64, ctypes.c_int64, ctypes.c_int, ctypes.c_void_p,
+                                  ctypes.c_int64, ctypes.c_size_t, ctypes.c_void_p]
+_lib.fh_mx_dequantize.restype = ctypes.c_int
+_lib.fh_mx_matmul.argtypes = [_P(fh_mx_product), ctypes.c_void_p]
+_lib.fh_mx_matmul.restype = ctypes.c_int
+_lib.fh_layer_norm.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p,
+                               ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_void_p, ctypes.c_int64, ctypes.c_size_t,
+                               ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
+_lib.fh_layer_norm.restype = ctypes.c_int
+_lib.fh_layer_norm_mx.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p,
+                                  ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_int32, ctypes.c_uint64, ctypes.c_uint64,
+                                  ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_size_t,
+                                  ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
+_lib.fh_layer_norm_mx.restype = ctypes.c_int
+_lib.fh_layer_norm_backward.argtypes = [_P(fh_norm_backward), ctypes.c_void_p]
+_lib.fh_layer_norm_backward.restype = ctypes.c_int
 
 
 class FedHybridError(RuntimeError):
@@ -1237,3 +1283,228 @@ def fh_mix_compress_batch(batch: MixBatch, stream=None) -> None:
 
 def fh_mix_decompress_batch(batch: MixBatch, stream=None) -> None:
     batch._call(_lib.fh_mix_decompress_batch, stream)
+
+
+# ---- microscaled 4-bit storage, its product, layer norm ---------------------------------------------------
+def mx_bytes(rows: int, cols: int) -> int:
+    """Bytes of a stored matrix of rows x cols: a byte for two values (rows padded to multiples of 256) and one for 32."""
+    return int(_lib.fh_mx_bytes(rows, cols))
+
+
+def mx_scales_offset(rows: int, cols: int) -> int:
+    """Where the scales begin in a stored matrix."""
+    return int(_lib.fh_mx_scales_offset(rows, cols))
+
+
+class MxMatrix:
+    """A matrix of rows x cols in microscaled 4-bit form: `data` holds the codes and, behind them, the scales."""
+    __slots__ = ("data", "rows", "cols")
+
+    def __init__(self, data: torch.Tensor, rows: int, cols: int):
+        self.data, self.rows, self.cols = data, rows, cols
+
+    @property
+    def nbytes(self) -> int:
+        return self.data.numel()
+
+
+def _same_device(*tensors) -> None:
+    device = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"tensors of one call live on {device} and {t.device}")
+
+
+def _matrix(t: torch.Tensor, what: str):
+    """(rows, cols, row stride) of a device matrix whose rows are contiguous."""
+    if not t.is_cuda:
+        raise ValueError(f"{what} must live in device memory (got a {t.device} tensor)")
+    if t.dim() != 2:
+        raise ValueError(f"{what} must have two dimensions (got {t.dim()})")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"the rows of {what} must be contiguous")
+    stride = t.stride(0) if rows > 1 else cols
+    if stride < cols:
+        raise ValueError(f"the rows of {what} overlap")
+    return rows, cols, stride
+
+
+def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
+    if t is None:
+        return None
+    _device_tensor(t, what)
+    if t.dim() != 1 or t.shape[0] != n:
+        raise ValueError(f"{what} must be a vector of {n} values")
+    return t.data_ptr()
+
+
+def _parameters(weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], cols: int):
+    """(weight's pointer, bias's pointer, their dtype code)"""
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise TypeError(f"weight and bias have different dtypes ({weight.dtype}, {bias.dtype})")
+    w, b = _vector(weight, cols, "weight"), _vector(bias, cols, "bias")
+    return w, b, _dtype_code(weight if weight is not None else bias) if weight is not None or bias is not None else FH_F32
+
+
+_FORMS = ("rows", "columns", "both")
+
+
+def _stores(forms: str, rows: int, cols: int, device):
+    """Buffers of the forms that are asked for: (by rows, by columns), None for one that is not."""
+    if forms not in _FORMS:
+        raise ValueError(f"forms must be one of {_FORMS} (got {forms!r})")
+    by_rows = by_columns = None
+    if forms != "columns":
+        by_rows = MxMatrix(torch.empty(mx_bytes(rows, cols), dtype=torch.uint8, device=device), rows, cols)
+    if forms != "rows":
+        by_columns = MxMatrix(torch.empty(mx_bytes(cols, rows), dtype=torch.uint8, device=device), cols, rows)
+    return by_rows, by_columns
+
+
+def _store_args(m: Optional[MxMatrix]):
+    return (None, 0) if m is None else (m.data.data_ptr(), m.data.numel())
+
+
+def _asked(forms: str, by_rows, by_columns):
+    return by_rows if forms == "rows" else by_columns if forms == "columns" else (by_rows, by_columns)
+
+
+def _u64(v: int) -> int:
+    return int(v) & 0xFFFFFFFFFFFFFFFF
+
+
+def fh_mx_quantize(x: torch.Tensor, forms: str = "rows", rounding="nearest", seed: int = 0, tensor_id: int = 0, stream=None):
+    """Enqueue the quantisation of the matrix x (rows contiguous, any row stride).  forms "rows" returns an MxMatrix of x
+    with blocks of 32 values along its rows, "columns" one of x transposed (blocks along x's columns), "both" the two."""
+    rows, cols, stride = _matrix(x, "x")
+    by_rows, by_columns = _stores(forms, rows, cols, x.device)
+    with _on(x.device):
+        _check(_lib.fh_mx_quantize(x.data_ptr(), _dtype_code(x), rows, cols, stride, _ROUND[rounding], _u64(seed), _u64(tensor_id),
+                                   *_store_args(by_rows), *_store_args(by_columns), _stream_ptr(stream)))
+    return _asked(forms, by_rows, by_columns)
+
+
+def _stored(m: MxMatrix, what: str) -> torch.Tensor:
+    t = _device_tensor(m.data, what)
+    if t.dtype != torch.uint8 or t.numel() < mx_bytes(m.rows, m.cols):
+        raise FedHybridError(7)
+    return t
+
+
+def fh_mx_dequantize(m: MxMatrix, out_dtype=torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Enqueue the restoration of a stored matrix; returns it as [rows, cols]."""
+    data = _stored(m, "the stored matrix")
+    if out is None:
+        out = torch.empty((m.rows, m.cols), dtype=out_dtype, device=data.device)
+    rows, cols, stride = _matrix(out, "out")
+    if (rows, cols) != (m.rows, m.cols):
+        raise ValueError(f"out is {rows} x {cols}, the matrix {m.rows} x {m.cols}")
+    _same_device(data, out)
+    code = _dtype_code(out)
+    nbytes = ((rows - 1) * stride + cols) * out.element_size() if rows and cols else 0
+    with _on(data.device):
+        _check(_lib.fh_mx_dequantize(data.data_ptr(), data.numel(), rows, cols, code, out.data_ptr(), stride, nbytes,
+                                     _stream_ptr(stream)))
+    return out
+
+
+def mx_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
+    return int(_lib.fh_mx_matmul_workspace_bytes(m, n, k))
+
+
+def fh_mx_matmul(a: MxMatrix, b: MxMatrix, bias: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
+                 out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Enqueue out = a b^T + bias of two stored matrices whose blocks run along the summed dimension."""
+    da, db = _stored(a, "a"), _stored(b, "b")
+    if a.cols != b.cols:
+        raise ValueError(f"a has {a.cols} columns, b {b.cols}")
+    m, n, k = a.rows, b.rows, a.cols
+    if out is None:
+        out = torch.empty((m, n), dtype=out_dtype, device=da.device)
+    rows, cols, stride = _matrix(out, "out")
+    if (rows, cols) != (m, n):
+        raise ValueError(f"out is {rows} x {cols}, the product {m} x {n}")
+    need = _lib.fh_mx_matmul_workspace_bytes(m, n, k)
+    if workspace is None and need:
+        workspace = _scratch(need, da.device, stream)
+    _same_device(da, db, bias, out, workspace)
+    p = fh_mx_product(da.data_ptr(), da.numel(), db.data_ptr(), db.numel(), m, n, k, _vector(bias, n, "bias"),
+                      FH_F32 if bias is None else _dtype_code(bias), _dtype_code(out), out.data_ptr(), stride,
+                      ((m - 1) * stride + n) * out.element_size() if m and n else 0,
+                      None if workspace is None else _device_tensor(workspace, "workspace").data_ptr(),
+                      0 if workspace is None else workspace.numel() * workspace.element_size(), 0)
+    with _on(da.device):
+        _check(_lib.fh_mx_matmul(ctypes.byref(p), _stream_ptr(stream)))
+    return out
+
+
+def fh_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                  out: Optional[torch.Tensor] = None, stream=None):
+    """Enqueue the layer norm of the matrix x over its rows; returns (y, mean, rstd), y in x's dtype, the statistics in fp32."""
+    rows, cols, stride = _matrix(x, "x")
+    w, b, p_dtype = _parameters(weight, bias, cols)
+    if out is None:
+        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    out_rows, out_cols, out_stride = _matrix(out, "out")
+    if (out_rows, out_cols) != (rows, cols) or out.dtype != x.dtype:
+        raise ValueError("out must have the shape and the dtype of x")
+    _same_device(x, weight, bias, out)
+    stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+    mean, rstd = stats.unbind(0)
+    with _on(x.device):
+        _check(_lib.fh_layer_norm(x.data_ptr(), _dtype_code(x), rows, cols, stride, w, b, p_dtype, eps, out.data_ptr(), out_stride,
+                                  ((rows - 1) * out_stride + cols) * out.element_size() if rows else 0,
+                                  mean.data_ptr(), rstd.data_ptr(), _stream_ptr(stream)))
+    return out, mean, rstd
+
+
+def fh_layer_norm_mx(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                     forms: str = "rows", rounding="nearest", seed: int = 0, tensor_id: int = 0, stream=None):
+    """Enqueue the layer norm of x with its result stored in microscaled form, as fh_mx_quantize stores it; returns
+    (what fh_mx_quantize would return, mean, rstd)."""
+    rows, cols, stride = _matrix(x, "x")
+    w, b, p_dtype = _parameters(weight, bias, cols)
+    _same_device(x, weight, bias)
+    by_rows, by_columns = _stores(forms, rows, cols, x.device)
+    stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+    mean, rstd = stats.unbind(0)
+    with _on(x.device):
+        _check(_lib.fh_layer_norm_mx(x.data_ptr(), _dtype_code(x), rows, cols, stride, w, b, p_dtype, eps, _ROUND[rounding],
+                                     _u64(seed), _u64(tensor_id), *_store_args(by_rows), *_store_args(by_columns),
+                                     mean.data_ptr(), rstd.data_ptr(), _stream_ptr(stream)))
+    return _asked(forms, by_rows, by_columns), mean, rstd
+
+
+def fh_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                           weight: Optional[torch.Tensor] = None, sums: bool = True, dx: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None, stream=None):
+    """Enqueue the backward pass of fh_layer_norm; returns (dx, dweight, dbias), the last two (None unless `sums`) in the
+    weight's dtype, in x's where there is no weight."""
+    rows, cols, x_stride = _matrix(x, "x")
+    dy_rows, dy_cols, dy_stride = _matrix(dy, "dy")
+    if (dy_rows, dy_cols) != (rows, cols) or dy.dtype != x.dtype:
+        raise ValueError("dy must have the shape and the dtype of x")
+    if mean.dtype != torch.float32 or rstd.dtype != torch.float32:
+        raise TypeError("mean and rstd must be float32")
+    if dx is None:
+        dx = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    dx_rows, dx_cols, dx_stride = _matrix(dx, "dx")
+    if (dx_rows, dx_cols) != (rows, cols) or dx.dtype != x.dtype:
+        raise ValueError("dx must have the shape and the dtype of x")
+    p_dtype = x.dtype if weight is None else weight.dtype
+    dweight = dbias = None
+    if sums:
+        dweight, dbias = torch.empty((2, cols), dtype=p_dtype, device=x.device).unbind(0)
+        if workspace is None:
+            workspace = _scratch(_lib.fh_layer_norm_backward_workspace_bytes(rows, cols), x.device, stream)
+    _same_device(x, dy, mean, rstd, weight, dx, workspace)
+    p = fh_norm_backward(dy.data_ptr(), x.data_ptr(), dy_stride, x_stride, _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"),
+                         _vector(weight, cols, "weight"), rows, cols, _dtype_code(x), _dtype_code(x if weight is None else weight),
+                         dx.data_ptr(), dx_stride, ((rows - 1) * dx_stride + cols) * dx.element_size() if rows else 0,
+                         None if dweight is None else dweight.data_ptr(), None if dbias is None else dbias.data_ptr(),
+                         None if workspace is None else _device_tensor(workspace, "workspace").data_ptr(),
+                         0 if workspace is None else workspace.numel() * workspace.element_size())
+    with _on(x.device):
+        _check(_lib.fh_layer_norm_backward(ctypes.byref(p), _stream_ptr(stream)))
+    return dx, dweight, dbias

@@ -1,0 +1,412 @@
+// Layer norm, its backward pass, and the form that writes 4-bit codes.
+#include "fh_norm.hpp"
+
+namespace fh {
+namespace {
+
+// Columns up to which a row is held in registers: by a wave, and by a workgroup of 1024.
+constexpr int64_t kWaveCols = 2048, kGroupCols = 16384;
+
+// The sum of v over the T threads that share a row; `s_sums` holds a value per wave and is used by every call in turn.
+template <int T>
+__device__ __forceinline__ float row_sum(float v, float* s_sums)
+{
+    v = wave_sum(v);
+    if constexpr (T > 64) {
+        __syncthreads();                                         // the sums of the call before have been read
+        if ((threadIdx.x & 63) == 0) s_sums[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.0f;
+        for (int w = 0; w < T / 64; ++w) v += s_sums[w];
+    }
+    return v;
+}
+
+// ---- forward: a row in the registers of T threads, NV runs of eight values each ------------
+template <typename T, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_rows_kernel(const T* x, int64_t rows, int64_t cols, int64_t x_stride,
+                                                                                  NormArgs n, T* y, int64_t y_stride, MxStore to)
+{
+    __shared__ float s_sums[16];
+    const int t = threadIdx.x % THREADS;
+    const int64_t row = (int64_t)blockIdx.x * (THREADS < 256 ? 256 / THREADS : 1) + threadIdx.x / THREADS;
+    const bool write = row < rows;
+    const T* p = x + (write ? row : rows - 1) * x_stride;
+    float v[NV][8];
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int64_t first = ((int64_t)k * THREADS + t) * 8;
+        load8(p + first, cols - first, v[k]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += v[k][i];
+    }
+    const float mean = row_sum<THREADS>(sum, s_sums) / (float)cols;
+    // the squares of what is left, so that a mean far from zero costs no digits
+    float squares = 0.0f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int64_t first = ((int64_t)k * THREADS + t) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float d = first + i < cols ? v[k][i] - mean : 0.0f;
+            squares = __builtin_fmaf(d, d, squares);
+        }
+    }
+    const float rstd = 1.0f / __builtin_sqrtf(row_sum<THREADS>(squares, s_sums) / (float)cols + n.eps);
+    if (write && t == 0) {
+        if (n.mean) n.mean[row] = mean;
+        if (n.rstd) n.rstd[row] = rstd;
+    }
+    if (!y && !to.codes) return;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int64_t first = ((int64_t)k * THREADS + t) * 8;
+        float w[8], b[8];
+        if (n.p_dtype == FH_F32) {
+            if (n.weight) load8(static_cast<const float*>(n.weight) + first, cols - first, w);
+            if (n.bias) load8(static_cast<const float*>(n.bias) + first, cols - first, b);
+        } else {
+            if (n.weight) load8(static_cast<const Bf16*>(n.weight) + first, cols - first, w);
+            if (n.bias) load8(static_cast<const Bf16*>(n.bias) + first, cols - first, b);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[k][i] = norm_value(v[k][i], mean, rstd, n.weight ? w[i] : 1.0f, n.bias ? b[i] : 0.0f);
+        if (y) {
+            if (write) store8(y + row * y_stride + first, cols - first, v[k]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[k][i] = first + i < cols ? v[k][i] : 0.0f;
+            mx_write8(to, row, first, v[k], write && first < to.chunks * kMxChunk);
+        }
+    }
+}
+
+// Rows that do not fit: the row is read three times, from the caches after the first.
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_long_rows_kernel(const T* x, int64_t cols, int64_t x_stride, NormArgs n, T* y,
+                                                              int64_t y_stride, MxStore to)
+{
+    __shared__ float s_sums[16];
+    const int64_t row = blockIdx.x;
+    const T* p = x + row * x_stride;
+    const int64_t end = mx_chunks(cols) * kMxChunk;             // whole waves have the same number of turns
+    float sum = 0.0f, v[8];
+    for (int64_t first = threadIdx.x * 8; first < cols; first += 8192) {
+        load8(p + first, cols - first, v);
+        for (int i = 0; i < 8; ++i) sum += v[i];
+    }
+    const float mean = row_sum<1024>(sum, s_sums) / (float)cols;
+    float squares = 0.0f;
+    for (int64_t first = threadIdx.x * 8; first < cols; first += 8192) {
+        load8(p + first, cols - first, v);
+        for (int i = 0; i < 8; ++i) {
+            const float d = first + i < cols ? v[i] - mean : 0.0f;
+            squares = __builtin_fmaf(d, d, squares);
+        }
+    }
+    const float rstd = 1.0f / __builtin_sqrtf(row_sum<1024>(squares, s_sums) / (float)cols + n.eps);
+    if (threadIdx.x == 0) {
+        if (n.mean) n.mean[row] = mean;
+        if (n.rstd) n.rstd[row] = rstd;
+    }
+    if (!y && !to.codes) return;
+    for (int64_t start = 0; start < end; start += 8192) {       // every lane takes every turn: quads work together
+        const int64_t first = start + threadIdx.x * 8;
+        load8(p + first, cols - first, v);
+        for (int i = 0; i < 8; ++i) {
+            const int64_t c = first + i;
+            v[i] = c < cols ? norm_value(v[i], mean, rstd, parameter(n.weight, n.p_dtype, c, 1.0f), parameter(n.bias, n.p_dtype, c, 0.0f)) : 0.0f;
+        }
+        if (y) store8(y + row * y_stride + first, cols - first, v);
+        else mx_write8(to, row, first, v, first < end);
+    }
+}
+
+// ---- backward ------------------------------------------------------------------------------
+struct NormBackwardArgs {
+    const void*  dy;
+    const void*  x;
+    const float* mean;
+    const float* rstd;
+    const void*  weight;
+    void*        dx;                   // may be null
+    float*       partial;              // [workgroups][2][cols]: sums of dy * x^ and of dy; may be null
+    int64_t      dy_stride, x_stride, dx_stride, rows, cols;
+    int32_t      p_dtype;
+};
+
+// Each workgroup takes rows a grid apart, keeps the sums of its columns in registers and leaves one row of partial sums.
+template <typename T, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_backward_kernel(NormBackwardArgs a)
+{
+    constexpr int kRows = THREADS < 256 ? 256 / THREADS : 1;     // rows of a workgroup at a time
+    __shared__ float s_sums[16];
+    const int t = threadIdx.x % THREADS, part = threadIdx.x / THREADS;
+    float w[NV][8], dw[NV][8], db[NV][8];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int64_t first = ((int64_t)k * THREADS + t) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { w[k][i] = 1.0f; dw[k][i] = 0.0f; db[k][i] = 0.0f; }
+        if (a.weight) {
+            if (a.p_dtype == FH_F32) load8(static_cast<const float*>(a.weight) + first, a.cols - first, w[k]);
+            else load8(static_cast<const Bf16*>(a.weight) + first, a.cols - first, w[k]);
+        }
+    }
+    const float share = 1.0f / (float)a.cols;
+    for (int64_t start = (int64_t)blockIdx.x * kRows; start < a.rows; start += (int64_t)gridDim.x * kRows) {
+        const int64_t row = start + part;
+        const bool here = row < a.rows;
+        float x[NV][8], g[NV][8];
+        const int64_t at = here ? row : a.rows - 1;
+        const float mean = a.mean[at], rstd = a.rstd[at];
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int64_t first = ((int64_t)k * THREADS + t) * 8;
+            load8(static_cast<const T*>(a.x) + at * a.x_stride + first, here ? a.cols - first : 0, x[k]);
+            load8(static_cast<const T*>(a.dy) + at * a.dy_stride + first, here ? a.cols - first : 0, g[k]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[k][i] = first + i < a.cols && here ? (x[k][i] - mean) * rstd : 0.0f;
+                dw[k][i] = __builtin_fmaf(g[k][i], x[k][i], dw[k][i]);
+                db[k][i] += g[k][i];
+                g[k][i] *= w[k][i];
+                s1 += g[k][i];
+                s2 = __builtin_fmaf(g[k][i], x[k][i], s2);
+            }
+        }
+        if (a.dx) {
+            s1 = row_sum<THREADS>(s1, s_sums) * share;
+            s2 = row_sum<THREADS>(s2, s_sums) * share;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                const int64_t first = ((int64_t)k * THREADS + t) * 8;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[k][i] = rstd * (g[k][i] - s1 - x[k][i] * s2);
+                if (here) store8(static_cast<T*>(a.dx) + row * a.dx_stride + first, a.cols - first, g[k]);
+            }
+        }
+    }
+    if (!a.partial) return;
+    float* to = a.partial + ((int64_t)blockIdx.x * kRows + part) * 2 * a.cols;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int64_t first = ((int64_t)k * THREADS + t) * 8;
+        store8(to + first, a.cols - first, dw[k]);
+        store8(to + a.cols + first, a.cols - first, db[k]);
+    }
+}
+
+// Rows that do not fit: dx by a workgroup a row, which reads the row twice; the columns' sums by a kernel of their own.
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_backward_long_rows_kernel(NormBackwardArgs a)
+{
+    __shared__ float s_sums[16];
+    const int64_t row = blockIdx.x;
+    const T *px = static_cast<const T*>(a.x) + row * a.x_stride, *pg = static_cast<const T*>(a.dy) + row * a.dy_stride;
+    const float mean = a.mean[row], rstd = a.rstd[row], share = 1.0f / (float)a.cols;
+    float x[8], g[8], s1 = 0.0f, s2 = 0.0f;
+    for (int64_t first = threadIdx.x * 8; first < a.cols; first += 8192) {
+        load8(px + first, a.cols - first, x);
+        load8(pg + first, a.cols - first, g);
+        for (int i = 0; i < 8; ++i) {
+            const float gw = first + i < a.cols ? g[i] * parameter(a.weight, a.p_dtype, first + i, 1.0f) : 0.0f;
+            s1 += gw;
+            s2 = __builtin_fmaf(gw, (x[i] - mean) * rstd, s2);
+        }
+    }
+    s1 = row_sum<1024>(s1, s_sums) * share;
+    s2 = row_sum<1024>(s2, s_sums) * share;
+    for (int64_t first = threadIdx.x * 8; first < a.cols; first += 8192) {
+        load8(px + first, a.cols - first, x);
+        load8(pg + first, a.cols - first, g);
+        for (int i = 0; i < 8; ++i) {
+            const float gw = first + i < a.cols ? g[i] * parameter(a.weight, a.p_dtype, first + i, 1.0f) : 0.0f;
+            g[i] = rstd * (gw - s1 - (x[i] - mean) * rstd * s2);
+        }
+        store8(static_cast<T*>(a.dx) + row * a.dx_stride + first, a.cols - first, g);
+    }
+}
+template <typename T>
+__global__ __launch_bounds__(256) void norm_column_sums_kernel(NormBackwardArgs a, int64_t rows_each, uint32_t col_groups)
+{
+    const int64_t first = ((int64_t)(blockIdx.x % col_groups) * 256 + threadIdx.x) * 8, part = blockIdx.x / col_groups;
+    if (first >= a.cols) return;
+    float x[8], g[8], dw[8] = {}, db[8] = {};
+    const int64_t end = part * rows_each + rows_each < a.rows ? part * rows_each + rows_each : a.rows;
+    for (int64_t row = part * rows_each; row < end; ++row) {
+        load8(static_cast<const T*>(a.x) + row * a.x_stride + first, a.cols - first, x);
+        load8(static_cast<const T*>(a.dy) + row * a.dy_stride + first, a.cols - first, g);
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        for (int i = 0; i < 8; ++i) {
+            dw[i] = __builtin_fmaf(g[i], (x[i] - mean) * rstd, dw[i]);
+            db[i] += g[i];
+        }
+    }
+    float* to = a.partial + part * 2 * a.cols;
+    store8(to + first, a.cols - first, dw);
+    store8(to + a.cols + first, a.cols - first, db);
+}
+
+// The partial rows added up, in their order whatever the launch: 64 columns of one of the two sums a workgroup, a quarter of the
+// rows a wave.
+template <typename P>
+__global__ __launch_bounds__(256) void norm_join_kernel(const float* partial, int64_t parts, int64_t cols, P* dweight, P* dbias)
+{
+    __shared__ float s_part[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = (int64_t)(blockIdx.x >> 1) * 64 + lane, which = blockIdx.x & 1;
+    float sum = 0.0f;
+    if (c < cols)
+        for (int64_t r = wave; r < parts; r += 4) sum += partial[(r * 2 + which) * cols + c];
+    s_part[wave][lane] = sum;
+    __syncthreads();
+    P* to = which ? dbias : dweight;
+    if (wave == 0 && c < cols && to) store1(to + c, (s_part[0][lane] + s_part[1][lane]) + (s_part[2][lane] + s_part[3][lane]));
+}
+
+// ---- launches ------------------------------------------------------------------------------
+template <typename T, int THREADS, int NV>
+hipError_t norm_of(const void* x, int64_t rows, int64_t cols, int64_t xs, const NormArgs& n, void* y, int64_t ys, const MxStore& to, hipStream_t s)
+{
+    constexpr int kRows = THREADS < 256 ? 256 / THREADS : 1;
+    const int64_t groups = (rows + kRows - 1) / kRows;
+    hipLaunchKernelGGL((norm_rows_kernel<T, THREADS, NV>), dim3((uint32_t)groups), dim3(THREADS < 256 ? 256 : THREADS), 0, s,
+                       static_cast<const T*>(x), rows, cols, xs, n, static_cast<T*>(y), ys, to);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t norm_any(const void* x, int64_t rows, int64_t cols, int64_t xs, const NormArgs& n, void* y, int64_t ys, const MxStore& to, hipStream_t s)
+{
+    if (cols <= 512) return norm_of<T, 64, 1>(x, rows, cols, xs, n, y, ys, to, s);
+    if (cols <= 1024) return norm_of<T, 64, 2>(x, rows, cols, xs, n, y, ys, to, s);
+    if (cols <= kWaveCols) return norm_of<T, 64, 4>(x, rows, cols, xs, n, y, ys, to, s);
+    if (cols <= 4096) return norm_of<T, 256, 2>(x, rows, cols, xs, n, y, ys, to, s);
+    if (cols <= 8192) return norm_of<T, 1024, 1>(x, rows, cols, xs, n, y, ys, to, s);
+    if (cols <= kGroupCols) return norm_of<T, 1024, 2>(x, rows, cols, xs, n, y, ys, to, s);
+    hipLaunchKernelGGL((norm_long_rows_kernel<T>), dim3((uint32_t)rows), dim3(1024), 0, s, static_cast<const T*>(x), cols, xs, n,
+                       static_cast<T*>(y), ys, to);
+    return hipGetLastError();
+}
+
+// Workgroups of the backward pass, and the rows of partial sums that they leave.
+struct BackwardShape { int64_t groups, parts; };
+inline BackwardShape backward_shape(int64_t rows, int64_t cols)
+{
+    const int64_t at_once = cols <= kWaveCols ? 4 : 1;
+    const int64_t most = cols <= kWaveCols ? 256 : 256;
+    const int64_t groups = (rows + at_once - 1) / at_once < most ? (rows + at_once - 1) / at_once : most;
+    return BackwardShape{groups, groups * at_once};
+}
+
+template <typename T, int THREADS, int NV>
+hipError_t backward_of(const NormBackwardArgs& a, int64_t groups, hipStream_t s)
+{
+    hipLaunchKernelGGL((norm_backward_kernel<T, THREADS, NV>), dim3((uint32_t)groups), dim3(THREADS < 256 ? 256 : THREADS), 0, s, a);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t backward_any(const NormBackwardArgs& a, int64_t* parts, hipStream_t s)
+{
+    const BackwardShape b = backward_shape(a.rows, a.cols);
+    *parts = b.parts;
+    if (a.cols <= 512) return backward_of<T, 64, 1>(a, b.groups, s);
+    if (a.cols <= 1024) return backward_of<T, 64, 2>(a, b.groups, s);
+    if (a.cols <= kWaveCols) return backward_of<T, 64, 4>(a, b.groups, s);
+    if (a.cols <= 4096) return backward_of<T, 256, 2>(a, b.groups, s);
+    if (a.cols <= 8192) return backward_of<T, 1024, 1>(a, b.groups, s);
+    if (a.cols <= kGroupCols) return backward_of<T, 1024, 2>(a, b.groups, s);
+    if (a.partial) {                                             // first: dx may be dy itself
+        const int64_t each = (a.rows + b.parts - 1) / b.parts, col_groups = (a.cols + 2047) / 2048;
+        *parts = (a.rows + each - 1) / each;
+        hipLaunchKernelGGL((norm_column_sums_kernel<T>), dim3((uint32_t)(col_groups * *parts)), dim3(256), 0, s, a, each, (uint32_t)col_groups);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (a.dx) hipLaunchKernelGGL((norm_backward_long_rows_kernel<T>), dim3((uint32_t)a.rows), dim3(1024), 0, s, a);
+    return hipGetLastError();
+}
+template <typename P>
+hipError_t join_of(const float* partial, int64_t parts, int64_t cols, void* dweight, void* dbias, hipStream_t s)
+{
+    hipLaunchKernelGGL((norm_join_kernel<P>), dim3((uint32_t)((cols + 63) / 64 * 2)), dim3(256), 0, s, partial, parts, cols,
+                       static_cast<P*>(dweight), static_cast<P*>(dbias));
+    return hipGetLastError();
+}
+
+bool norm_shape_ok(int64_t rows, int64_t cols) { return mx_shape_ok(rows, cols) && cols >= 1; }
+
+}  // namespace
+
+hipError_t launch_layer_norm(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t xs, const NormArgs& n, void* y, int64_t ys,
+                             const MxStore& to, hipStream_t s)
+{
+    return dtype == FH_F32 ? norm_any<float>(x, rows, cols, xs, n, y, ys, to, s) : norm_any<Bf16>(x, rows, cols, xs, n, y, ys, to, s);
+}
+
+}  // namespace fh
+
+extern "C" {
+
+fh_status fh_layer_norm(const void* x, fh_dtype dtype, int64_t rows, int64_t cols, int64_t x_stride, const void* weight, const void* bias,
+                        fh_dtype p_dtype, float eps, void* y, int64_t y_stride, size_t y_cap, void* mean, void* rstd, void* stream)
+{
+    using namespace fh;
+    if (!is_dtype(dtype) || !is_dtype(p_dtype)) return FH_ERR_BAD_DTYPE;
+    if (!norm_shape_ok(rows, cols) || x_stride < cols || y_stride < cols || x_stride > kMostStride || y_stride > kMostStride)
+        return FH_ERR_BAD_SHAPE;
+    if (!(eps >= 0.0f)) return FH_ERR_BAD_PARAM;
+    if (rows == 0) return FH_OK;
+    if (!x || !y) return FH_ERR_NULL;
+    if (!is_aligned(x, dtype_size(dtype)) || !is_aligned(y, dtype_size(dtype)) || !is_aligned(weight, dtype_size(p_dtype)) ||
+        !is_aligned(bias, dtype_size(p_dtype)) || !is_aligned(mean, 4) || !is_aligned(rstd, 4)) return FH_ERR_ALIGNMENT;
+    if (y_cap < strided_elements(rows, cols, y_stride) * dtype_size(dtype)) return FH_ERR_BUFFER_TOO_SMALL;
+    const NormArgs n = {weight, bias, p_dtype, eps, static_cast<float*>(mean), static_cast<float*>(rstd)};
+    const MxStore none = {};
+    return launch_layer_norm(x, dtype, rows, cols, x_stride, n, y, y_stride, none, static_cast<hipStream_t>(stream)) == hipSuccess
+               ? FH_OK : FH_ERR_LAUNCH;
+}
+
+size_t fh_layer_norm_backward_workspace_bytes(int64_t rows, int64_t cols)
+{
+    if (!fh::norm_shape_ok(rows, cols)) return 0;
+    return (size_t)fh::backward_shape(rows, cols).parts * 2u * (size_t)cols * 4u;
+}
+
+fh_status fh_layer_norm_backward(const fh_norm_backward* b, void* stream)
+{
+    using namespace fh;
+    if (!b) return FH_ERR_NULL;
+    if (!is_dtype(b->dtype) || !is_dtype(b->p_dtype)) return FH_ERR_BAD_DTYPE;
+    if (!norm_shape_ok(b->rows, b->cols) || b->dy_stride < b->cols || b->x_stride < b->cols || b->dx_stride < b->cols ||
+        b->dy_stride > kMostStride || b->x_stride > kMostStride || b->dx_stride > kMostStride) return FH_ERR_BAD_SHAPE;
+    const bool sums = b->dweight || b->dbias;
+    if (b->rows > 0 && (!b->dy || !b->x || !b->mean || !b->rstd)) return FH_ERR_NULL;
+    const size_t size = dtype_size(b->dtype), p_size = dtype_size(b->p_dtype);
+    if (!is_aligned(b->dy, size) || !is_aligned(b->x, size) || !is_aligned(b->dx, size) || !is_aligned(b->weight, p_size) ||
+        !is_aligned(b->dweight, p_size) || !is_aligned(b->dbias, p_size) || !is_aligned(b->mean, 4) || !is_aligned(b->rstd, 4) ||
+        !is_aligned(b->workspace, 16)) return FH_ERR_ALIGNMENT;
+    if (b->dx && b->dx_cap < strided_elements(b->rows, b->cols, b->dx_stride) * size) return FH_ERR_BUFFER_TOO_SMALL;
+    if (sums && b->rows > 0) {
+        if (!b->workspace) return FH_ERR_NULL;
+        if (b->workspace_cap < fh_layer_norm_backward_workspace_bytes(b->rows, b->cols)) return FH_ERR_BUFFER_TOO_SMALL;
+    }
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    float* partial = sums ? static_cast<float*>(b->workspace) : nullptr;
+    int64_t parts = 0;
+    if (b->rows > 0 && (b->dx || sums)) {
+        const NormBackwardArgs a = {b->dy, b->x, static_cast<const float*>(b->mean), static_cast<const float*>(b->rstd), b->weight, b->dx, partial,
+                                    b->dy_stride, b->x_stride, b->dx_stride, b->rows, b->cols, b->p_dtype};
+        const hipError_t e = b->dtype == FH_F32 ? backward_any<float>(a, &parts, s) : backward_any<Bf16>(a, &parts, s);
+        if (e != hipSuccess) return FH_ERR_LAUNCH;
+    }
+    if (!sums) return FH_OK;                                     // no rows: sums of nothing, which are written all the same
+    const hipError_t e = b->p_dtype == FH_F32 ? join_of<float>(partial, parts, b->cols, b->dweight, b->dbias, s)
+                                              : join_of<Bf16>(partial, parts, b->cols, b->dweight, b->dbias, s);
+    return e == hipSuccess ? FH_OK : FH_ERR_LAUNCH;
+}
+
+}  // extern "C"
