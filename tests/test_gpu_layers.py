@@ -1,0 +1,193 @@
+"""The layers on the GPU: values and gradients against the formulas in binary64 on the quantised operands, as they are used
+in training, in serving, under saved-tensor compression and captured in a graph."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+import mx_reference as R
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def layers():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a visible MI355X")
+    from paper_2510_11400_amd import layers as _layers
+    return _layers
+
+
+def _blocks(v, halves=None):
+    """v's values on the grid of its rows' blocks."""
+    data, _ = R.stored(v.astype(np.float32), halves)
+    return R.restored(data, *v.shape)
+
+
+def _rel(got, want):
+    want = torch.as_tensor(want)
+    return float((got.double().cpu() - want).norm() / want.norm())
+
+
+def _case(tokens, features, out, dtype, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(2, tokens // 2, features, generator=g).to(dtype)
+    w = (torch.randn(out, features, generator=g) / features ** 0.5).to(dtype)
+    b = torch.randn(out, generator=g).to(dtype)
+    dy = torch.randn(2, tokens // 2, out, generator=g).to(dtype)
+    nw, nb = (1 + 0.2 * torch.randn(features, generator=g)).to(dtype), (0.1 * torch.randn(features, generator=g)).to(dtype)
+    return x, nw, nb, w, b, dy
+
+
+def _leaf(v):
+    return v.cuda().requires_grad_()
+
+
+@pytest.mark.parametrize("rounding", ["nearest", "stochastic"])
+@pytest.mark.parametrize("tokens, features, out", [(2, 40, 33), (66, 300, 130), (512, 768, 260)])
+def test_linear(layers, tokens, features, out, rounding):
+    """fp32 throughout: the quantised operands are exact, so the products are off by their sums' rounding alone."""
+    x, _, _, w, b, dy = _case(tokens, features, out, torch.float32)
+    xc, wc, bc = _leaf(x), _leaf(w), _leaf(b)
+    y = layers.mx_linear(xc, wc, bc, rounding, 9, 4)
+    dx, dw, db = torch.autograd.grad(y, (xc, wc, bc), dy.cuda())
+    xm, wm, gm = x.reshape(-1, features).numpy(), w.numpy(), dy.reshape(-1, out).numpy()
+    h = R.philox_halves(*gm.shape, 9, 4) if rounding == "stochastic" else None
+    for got, want in ((y, R.product(_blocks(xm), _blocks(wm), b.double().numpy())),
+                      (dx, R.product(_blocks(gm, h), _blocks(wm.T))),
+                      (dw, R.product(_blocks(gm.T, None if h is None else h.T), _blocks(xm.T)))):
+        far = np.abs(got.detach().double().cpu().numpy().reshape(want[0].shape) - want[0])
+        assert (far <= want[1] + R.U32 * np.abs(want[0])).all()
+    assert _rel(db, gm.astype(float).sum(0)) < 1e-5
+
+
+@pytest.mark.parametrize("tokens, features, out", [(2, 40, 33), (130, 300, 130), (512, 768, 260)])
+def test_norm_and_linear(layers, tokens, features, out):
+    """In bf16: outputs are rounded once (2^-9 of a value on average at most), dx and the norm's gradients carry the data
+    gradient's rounding as well, and a norm's output next to a border may take the other code: 0.01 of the norm covers all."""
+    x, nw, nb, w, b, dy = _case(tokens, features, out, torch.bfloat16)
+    leaves = [_leaf(v) for v in (x, nw, nb, w, b)]
+    y = layers.layer_norm_mx_linear(*leaves)
+    grads = torch.autograd.grad(y, leaves, dy.cuda())
+    xm, wm, gm = x.reshape(-1, features).double().numpy(), w.float().numpy(), dy.reshape(-1, out).float().numpy()
+    h, mean, rstd, _, _, _ = R.layer_norm(xm, nw.double().numpy(), nb.double().numpy(), 1e-5)
+    dh = _blocks(gm) @ _blocks(wm.T).T
+    dx, dnw, dnb, _, _, _ = R.layer_norm_backward(dh, xm, mean, rstd, nw.double().numpy())
+    want = [_blocks(h) @ _blocks(wm).T + b.double().numpy(), dx, dnw, dnb, _blocks(gm.T) @ _blocks(h.T).T, gm.astype(float).sum(0)]
+    for name, got, ref in zip(("y", "dx", "d norm weight", "d norm bias", "dw", "db"), (y, *grads), want):
+        assert got.shape == (y.shape if name == "y" else leaves[("dx", "d norm weight", "d norm bias", "dw", "db").index(name)].shape)
+        assert _rel(got.detach().reshape(ref.shape), ref) < 0.01, name
+
+
+def test_norm_layer_is_the_norm(layers):
+    x, nw, nb, _, _, _ = _case(64, 300, 8, torch.float32)
+    leaves = [_leaf(v) for v in (x, nw, nb)]
+    dy = torch.randn(x.shape, generator=torch.Generator().manual_seed(3))
+    y = layers.layer_norm(*leaves)
+    grads = torch.autograd.grad(y, leaves, dy.cuda())
+    ref = [v.double().requires_grad_() for v in (x, nw, nb)]
+    d = ref[0] - ref[0].mean(-1, keepdim=True)
+    want = d / (d.square().mean(-1, keepdim=True) + 1e-5).sqrt() * ref[1] + ref[2]
+    for got, r in zip((y, *grads), (want, *torch.autograd.grad(want, ref, dy.double()))):
+        assert got.shape == r.shape and _rel(got.detach(), r.detach()) < 1e-5
+
+
+def test_gradients_that_nobody_needs_are_not_made(layers):
+    x, nw, nb, w, b, dy = (v.cuda() for v in _case(66, 100, 40, torch.float32))
+    full = [v.clone().requires_grad_() for v in (x, nw, nb, w, b)]
+    want = torch.autograd.grad(layers.layer_norm_mx_linear(*full), full, dy)
+    for needed in ((0,), (3,), (1, 2), (4,), (0, 4), (2, 3)):
+        leaves = [v.clone().requires_grad_(i in needed) for i, v in enumerate((x, nw, nb, w, b))]
+        got = torch.autograd.grad(layers.layer_norm_mx_linear(*leaves), [leaves[i] for i in needed], dy)
+        for i, g in zip(needed, got):
+            assert torch.equal(g, want[i]), (needed, i)
+    lin = [v.clone().requires_grad_() for v in (x, w)]
+    want = torch.autograd.grad(layers.mx_linear(*lin), lin, dy)
+    for i in (0, 1):
+        leaves = [v.clone().requires_grad_(i == k) for k, v in enumerate((x, w))]
+        assert torch.equal(torch.autograd.grad(layers.mx_linear(*leaves), leaves[i], dy)[0], want[i])
+    assert not layers.mx_linear(x, w).requires_grad
+
+
+def test_views_and_expanded_gradients(layers):
+    """Inputs whose rows are not next to each other, and the gradient of a sum, which is one value seen everywhere."""
+    x, _, _, w, _, _ = _case(64, 100, 40, torch.float32)
+    wide = torch.randn(2, 32, 130, device="cuda")
+    wide[..., 7:107] = x.cuda()
+    got, want = [], []
+    for src, keep in ((wide[..., 7:107], got), (x.cuda(), want)):
+        leaf = src.detach().requires_grad_() if src.is_contiguous() else src
+        wc = _leaf(w)
+        y = layers.mx_linear(leaf, wc)
+        keep += [y.detach(), *torch.autograd.grad(y.sum(), wc)]
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    t = x.transpose(0, 1).cuda()
+    assert torch.equal(layers.mx_linear(t, w.cuda()), layers.mx_linear(x.cuda(), w.cuda()).transpose(0, 1))
+
+
+def test_a_frozen_layer_answers_as_the_trained_one(layers):
+    torch.manual_seed(1)
+    layer = layers.LayerNormMxLinear(300, 130, device="cuda", dtype=torch.bfloat16)
+    for tokens in (1, 2, 17, 100):
+        x = torch.randn(tokens, 300, device="cuda", dtype=torch.bfloat16)
+        want = layer(x).detach()
+        assert torch.equal(layer.freeze()(x), want)
+        one = layer(x[-1:])
+        # the same sums of one token alone, in another order: an fp32 sum's rounding may fall to the other side of a bf16 border
+        assert float((one.float() - want[-1:].float()).abs().max()) <= 2.0 ** -7 * float(want[-1:].float().abs().max())
+        assert layer.thaw()(x).requires_grad
+
+
+def test_training_reduces_the_loss(layers):
+    """A few steps of a two-layer model with stochastically rounded gradients under saved-tensor compression."""
+    from paper_2510_11400_amd import hooks
+    torch.manual_seed(2)
+    model = torch.nn.Sequential(layers.LayerNormMxLinear(256, 512, rounding="stochastic", tensor_id=0, device="cuda", dtype=torch.bfloat16),
+                                torch.nn.GELU(),
+                                layers.LayerNormMxLinear(512, 64, rounding="stochastic", tensor_id=1, device="cuda", dtype=torch.bfloat16))
+    x = torch.randn(1024, 256, device="cuda", dtype=torch.bfloat16)
+    target = torch.randn(1024, 64, device="cuda", dtype=torch.bfloat16).float()
+    opt = torch.optim.SGD(model.parameters(), lr=0.5)
+    losses = []
+    for step in range(12):
+        with hooks.SavedActivations(64, 8, exclude=model.parameters(), first_tensor_id=10 * step):
+            loss = (model(x).float() - target).square().mean()
+        opt.zero_grad()
+        loss.backward()
+        opt.step()
+        losses.append(float(loss))
+    assert model[0].steps == 12
+    assert losses[-1] < losses[0] and all(np.isfinite(losses)), losses
+
+
+def test_captured_in_a_graph(layers):
+    """Forward and backward of the layer recorded once, replayed on new inputs between eager work, each replay against the
+    eager result.  The leaves of the graph are its own."""
+    x, nw, nb, w, _, dy = (v.cuda() for v in _case(200, 300, 130, torch.bfloat16))
+
+    def step(x, dy, leaves):
+        xl = x.detach().requires_grad_()
+        y = layers.layer_norm_mx_linear(xl, *leaves)
+        return [y.detach(), *torch.autograd.grad(y, [xl, *leaves], dy)]
+
+    static_x, static_dy = x.clone(), dy.clone()
+    static = [v.clone().requires_grad_() for v in (nw, nb, w)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(static_x, static_dy, static)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(static_x, static_dy, static)
+    for k in range(4):
+        g = torch.Generator(device="cuda").manual_seed(k)
+        nx, ndy = (torch.randn(v.shape, generator=g, device="cuda").to(v.dtype) for v in (x, dy))
+        static_x.copy_(nx)
+        static_dy.copy_(ndy)
+        graph.replay()
+        got = [v.clone() for v in out]
+        want = step(nx, ndy, [v.clone().requires_grad_() for v in (nw, nb, w)])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), k
