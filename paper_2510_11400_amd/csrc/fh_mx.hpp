@@ -169,6 +169,13 @@ __device__ __forceinline__ void store8(Bf16* p, int64_t n, const float (&v)[8])
     }
 }
 
+__device__ __forceinline__ void store_run(float* p, int64_t n, const float (&v)[4])
+{
+    if (n >= 4) *reinterpret_cast<f32x4_a4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+    else for (int i = 0; i < 4; ++i) if (i < n) p[i] = v[i];
+}
+__device__ __forceinline__ void store_run(Bf16* p, int64_t n, const float (&v)[8]) { store8(p, n, v); }
+
 // ---- eight values of a lane, 32 of a quad, to the stored form of their row ----------------
 // All 64 lanes are active; `first` is a multiple of 8, the quad's 32 values are one block.  Columns past the row's end hold
 // 0 (the caller's loads see to that), so that the padding becomes what a block of zeros becomes.

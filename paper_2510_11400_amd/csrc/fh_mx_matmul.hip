@@ -7,13 +7,16 @@ namespace {
 constexpr int64_t kMostSummed = (int64_t)1 << 24;   // a row's codes are addressed with 32 bits
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct ProductArgs {
     MxStore      a, b;                 // m and n rows, the same number of chunks
     int64_t      m, n, chunks;
     const void*  bias;                 // may be null
     int32_t      bias_dtype;
-    void*        out;
+    int32_t      parts;                // workgroups that share a tile's sum, each a run of chunks_each chunks
+    int64_t      chunks_each;
+    void*        out;                  // parts > 1: float [parts][m][n]
     int64_t      stride;
 };
 
@@ -27,9 +30,6 @@ __device__ __forceinline__ f32x4 mx_mfma(u32x4 a, u32x4 b, uint32_t sa, uint32_t
     const i32x8 x = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0}, y = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, BYTE, (int)sa, BYTE, (int)sb);
 }
-
-template <typename T>
-__device__ __forceinline__ float bias_of(const ProductArgs& p, int64_t j) { return parameter(p.bias, p.bias_dtype, j, 0.0f); }
 
 // 16 x 16 outputs a workgroup, its waves taking chunks in turn: their sums are joined in LDS in the waves' order.
 template <typename T, int WAVES>
@@ -57,16 +57,257 @@ __global__ __launch_bounds__(WAVES * 64) void mx_few_rows_kernel(ProductArgs p, 
         float sum = 0.0f;
         for (int w = 0; w < WAVES; ++w) sum += s_part[w][threadIdx.x];
         const int64_t row = i0 + (threadIdx.x >> 4), col = j0 + (threadIdx.x & 15);
-        if (row < p.m && col < p.n) store1(static_cast<T*>(p.out) + row * p.stride + col, sum + bias_of<T>(p, col));
+        if (row < p.m && col < p.n) store1(static_cast<T*>(p.out) + row * p.stride + col, sum + parameter(p.bias, p.bias_dtype, col, 0.0f));
     }
 }
 
+// ---- large products: tiles through LDS ----------------------------------------------------------
+// v_mfma_scale_f32_32x32x64_f8f6f4: lane (r = lane % 32, h = lane / 32) brings 32 values of row r of each operand, and gets
+// the outputs [8 (i/4) + 4 h + i % 4][r].  It measured 7.0 PFLOP/s from registers, the 16 x 16 form 4.3.  Of a chunk's
+// eight blocks a lane takes 4h .. 4h+3, in four instructions, whose scales are the bytes of one word.
+template <int BYTE>
+__device__ __forceinline__ f32x16 mx_mfma32(u32x4 a, u32x4 b, uint32_t sa, uint32_t sb, f32x16 c)
+{
+    const i32x8 x = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0}, y = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, BYTE, (int)sa, BYTE, (int)sb);
+}
+
+// 16 bytes a lane from a buffer straight into LDS, at `lds` + 16 * lane.  Written out because the compiler would wait for all
+// of them before every later read of LDS, the other stage's too.  No register is written; the caller waits by
+// s_waitcnt vmcnt before the barrier that hands the stage over.
+__device__ __forceinline__ void to_lds(uint32_t lds, u32x4 from, uint32_t offset, uint32_t moved)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :: "s"(lds), "v"(offset), "s"(from), "s"(moved) : "memory");
+}
+__device__ __forceinline__ u32x4 buffer_of(const uint8_t* p, uint32_t bytes)
+{
+    const uint64_t at = (uint64_t)p;
+    return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, bytes, 0x00020000u};
+}
+
+// BM x BN outputs a workgroup of WM x WN waves, a chunk of 256 summed values at a time.  Two stages of LDS: while one is
+// multiplied the next is on its way, and a stage is handed over before its last quarter, which is in registers by then, so
+// that the matrix unit works across the barrier.  A row's eight pieces of 16 bytes are turned by the row (the loads take
+// them from turned addresses), so that eight lanes reading the same piece of eight rows meet all banks.
+// The sum is bound by the matrix unit and, in the small tile, by LDS: a wave reads (BM/WM + BN/WN) * 128 bytes a chunk for
+// (BM/WM) * (BN/WN) * 256 products.
+template <typename T, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64, BM * BN > 16384 ? 1 : 2) void mx_tile_kernel(ProductArgs p, uint32_t m_tiles, uint32_t n_tiles)
+{
+    constexpr int kWaves = WM * WN, MT = BM / WM / 32, NT = BN / WN / 32;
+    constexpr uint32_t kCodes = (BM + BN) * 128, kStage = kCodes + (BM + BN) * 8;
+    constexpr int kLoadsA = BM / 8 / kWaves, kLoadsB = BN / 8 / kWaves;
+    constexpr uint32_t kRow = NT * 32 * 4 + 16;                  // of the outputs on their way through LDS
+    static_assert(BM % 128 == 0 && BN % 128 == 0 && (BM + BN) / 128 <= kWaves, "a wave loads the scales of 128 rows");
+    static_assert(kWaves * 32 * kRow <= 2 * kStage, "the outputs go through the stages' memory");
+    __shared__ __attribute__((aligned(16))) uint8_t s_stage[2 * kStage];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+
+    // Tiles go to the XCDs in runs (workgroups go to them in turn), a run in columns of up to eight tiles, so that what an
+    // XCD works on at a time shares rows of both operands in its L2.
+    const uint32_t tiles = m_tiles * n_tiles, part = blockIdx.x / tiles, at = blockIdx.x % tiles;
+    const uint32_t xcd = at & 7, share = tiles >> 3, rest = tiles & 7;
+    const uint32_t tile = xcd * share + (xcd < rest ? xcd : rest) + (at >> 3);
+    const uint32_t band = tile / (8 * n_tiles), first = band * 8, high = m_tiles - first < 8 ? m_tiles - first : 8;
+    const int64_t i0 = (int64_t)(first + (tile - band * 8 * n_tiles) % high) * BM;
+    const int64_t j0 = (int64_t)((tile - band * 8 * n_tiles) / high) * BN;
+
+    // rows past the last are the last one, so that every address is inside
+    const int rows_a = (int)(p.m - i0 < BM ? p.m - i0 : BM), rows_b = (int)(p.n - j0 < BN ? p.n - j0 : BN);
+    const uint32_t pitch = (uint32_t)p.chunks * 128, scale_pitch = (uint32_t)p.chunks * 256;
+    const u32x4 from_a = buffer_of(p.a.codes + i0 * pitch, rows_a * pitch), from_b = buffer_of(p.b.codes + j0 * pitch, rows_b * pitch);
+    const uint32_t piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    uint32_t at_a[kLoadsA], at_b[kLoadsB];
+#pragma unroll
+    for (int t = 0; t < kLoadsA; ++t) {
+        const int r = (t * kWaves + wave) * 8 + (lane >> 3);
+        at_a[t] = (r < rows_a ? r : rows_a - 1) * pitch + piece;
+    }
+#pragma unroll
+    for (int t = 0; t < kLoadsB; ++t) {
+        const int r = (t * kWaves + wave) * 8 + (lane >> 3);
+        at_b[t] = (r < rows_b ? r : rows_b - 1) * pitch + piece;
+    }
+    const bool scales_of_a = wave < BM / 128, loads_scales = wave < (BM + BN) / 128;
+    const uint32_t groups = ((scales_of_a ? rows_a : rows_b) + 31) / 32;
+    const u32x4 from_scales = buffer_of(scales_of_a ? p.a.scales + (i0 >> 5) * scale_pitch : p.b.scales + (j0 >> 5) * scale_pitch, groups * scale_pitch);
+    const uint32_t group = (scales_of_a ? wave : wave - BM / 128) * 4 + (lane >> 4);
+    const uint32_t at_scales = (group < groups ? group : groups - 1) * scale_pitch + (lane & 15) * 16;
+
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_stage;
+    auto load = [&](uint32_t stage, uint32_t chunk) {
+        if (loads_scales) to_lds(lds + stage + kCodes + wave * 1024, from_scales, at_scales, chunk * 256);
+#pragma unroll
+        for (int t = 0; t < kLoadsA; ++t) to_lds(lds + stage + (t * kWaves + wave) * 1024, from_a, at_a[t], chunk * 128);
+#pragma unroll
+        for (int t = 0; t < kLoadsB; ++t) to_lds(lds + stage + BM * 128 + (t * kWaves + wave) * 1024, from_b, at_b[t], chunk * 128);
+    };
+
+    const int h = lane >> 5, r = lane & 31, turned = (h * 4) ^ (lane & 7);
+    const uint32_t read_a = (wm * MT * 32 + r) * 128, read_b = BM * 128 + (wn * NT * 32 + r) * 128;
+    const uint32_t read_sa = kCodes + wm * MT * 256 + h * 128 + r * 4, read_sb = kCodes + BM * 8 + wn * NT * 256 + h * 128 + r * 4;
+    u32x4 fa[2][MT], fb[2][NT];
+    uint32_t sa[MT], sb[NT], next_sa[MT], next_sb[NT];
+    f32x16 c[MT][NT] = {};
+    auto read = [&](uint32_t stage, int quarter, int to) {
+        const uint8_t* from = s_stage + stage + (uint32_t)(turned ^ quarter) * 16;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) fa[to][t] = *reinterpret_cast<const u32x4*>(from + read_a + t * 4096);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) fb[to][t] = *reinterpret_cast<const u32x4*>(from + read_b + t * 4096);
+    };
+    auto read_scales = [&](uint32_t stage, uint32_t (&ua)[MT], uint32_t (&ub)[NT]) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t) ua[t] = *reinterpret_cast<const uint32_t*>(s_stage + stage + read_sa + t * 256);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) ub[t] = *reinterpret_cast<const uint32_t*>(s_stage + stage + read_sb + t * 256);
+    };
+    // Outputs run along b's rows within a lane.  A read of LDS goes with every two matrix instructions.
+#define FH_QUARTER(Q, WHICH)                                                                                      \
+    _Pragma("unroll") for (int x = 0; x < MT; ++x) _Pragma("unroll") for (int y = 0; y < NT; ++y)                 \
+        c[x][y] = mx_mfma32<Q>(fb[WHICH][y], fa[WHICH][x], sb[y], sa[x], c[x][y]);                                \
+    _Pragma("unroll") for (int z = 0; z < MT + NT; ++z) {                                                         \
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                                                        \
+        __builtin_amdgcn_sched_group_barrier(0x008, MT * NT / (MT + NT), 0);                                      \
+    }
+    const uint32_t begin = (uint32_t)(part * p.chunks_each), end = (uint32_t)(begin + p.chunks_each < p.chunks ? begin + p.chunks_each : p.chunks);
+    load(0, begin);
+    if (begin + 1 < end) {
+        load(kStage, begin + 1);
+        asm volatile("s_waitcnt vmcnt(%0)" :: "n"(kLoadsA + kLoadsB) : "memory");   // the first stage's are older
+    } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    uint32_t stage = 0;
+    read(stage, 0, 0);
+    read_scales(stage, sa, sb);
+    for (uint32_t k = begin; k < end; ++k) {
+        read(stage, 1, 1);
+        FH_QUARTER(0, 0)
+        read(stage, 2, 0);
+        FH_QUARTER(1, 1)
+        read(stage, 3, 1);
+        FH_QUARTER(2, 0)
+        // this wave has read all of this stage, and its part of the next has arrived
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (k + 2 < end) load(stage, k + 2);
+        stage = kStage - stage;
+        read(stage, 0, 0);                                       // after the last chunk: of no use, and inside
+        read_scales(stage, next_sa, next_sb);
+        FH_QUARTER(3, 1)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) sa[t] = next_sa[t];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sb[t] = next_sb[t];
+    }
+#undef FH_QUARTER
+    __syncthreads();
+
+    // Out by rows: 32 rows of the wave's columns at a time through LDS, then whole runs of 16 bytes a lane.
+    float* s_out = reinterpret_cast<float*>(s_stage + wave * 32 * kRow);
+    T* out = static_cast<T*>(p.out) + (p.parts > 1 ? (int64_t)part * p.m * p.n : 0);
+    constexpr int kRun = 16 / sizeof(T), kLanes = NT * 32 / kRun, kRows = 64 / kLanes;
+    const int64_t col = j0 + wn * NT * 32 + (lane % kLanes) * kRun;
+    float bias[kRun];
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) bias[i] = col + i < p.n && p.bias ? parameter(p.bias, p.bias_dtype, col + i, 0.0f) : 0.0f;
+#pragma unroll
+    for (int x = 0; x < MT; ++x) {
+#pragma unroll
+        for (int y = 0; y < NT; ++y)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<f32x4*>(s_out + r * (kRow / 4) + y * 32 + 2 * i + 4 * h) = f32x4{c[x][y][i], c[x][y][i + 1], c[x][y][i + 2], c[x][y][i + 3]};
+        asm volatile("" ::: "memory");                           // a wave's own LDS accesses are in order
+#pragma unroll
+        for (int t = 0; t < 32 / kRows; ++t) {
+            const int mine = t * kRows + lane / kLanes;
+            const int64_t row = i0 + (wm * MT + x) * 32 + mine;
+            const float* from = s_out + mine * (kRow / 4) + (lane % kLanes) * kRun;
+            float v[kRun];
+#pragma unroll
+            for (int i = 0; i < kRun; i += 4) {
+                const f32x4 w = *reinterpret_cast<const f32x4*>(from + i);
+                v[i] = w.x + bias[i]; v[i + 1] = w.y + bias[i + 1]; v[i + 2] = w.z + bias[i + 2]; v[i + 3] = w.w + bias[i + 3];
+            }
+            if (row < p.m) store_run(out + row * p.stride + col, p.n - col, v);
+        }
+        asm volatile("" ::: "memory");
+    }
+}
+
+// The parts of a split sum added up in their order.
 template <typename T>
-hipError_t product_of(const ProductArgs& p, hipStream_t s)
+__global__ __launch_bounds__(256) void mx_join_kernel(const float* parts, int64_t m, int64_t n, int32_t count, const void* bias, int32_t bias_dtype,
+                                                      T* out, int64_t stride, uint32_t runs)
+{
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / runs, col = (at - row * runs) * 4;
+    if (row >= m) return;
+    float v[4] = {};
+    for (int32_t k = 0; k < count; ++k) {
+        const float* from = parts + ((int64_t)k * m + row) * n + col;
+        if (col + 4 <= n) {
+            const f32x4 w = *reinterpret_cast<const f32x4_a4*>(from);
+            for (int i = 0; i < 4; ++i) v[i] += w[i];
+        } else {
+            for (int i = 0; i < 4; ++i) if (col + i < n) v[i] += from[i];
+        }
+    }
+    for (int i = 0; i < 4; ++i)
+        if (col + i < n) store1(out + row * stride + col + i, v[i] + parameter(bias, bias_dtype, col + i, 0.0f));
+}
+
+// ---- which kernel -------------------------------------------------------------------------------
+struct Plan { int32_t tile; int32_t parts; int64_t chunks_each; };      // tile: 0 few rows, else BM = BN
+Plan plan_of(int64_t m, int64_t n, int64_t k)
+{
+    const int64_t chunks = mx_chunks(k);
+    if (m <= 32 || n <= 32 || chunks == 0) return Plan{0, 1, chunks};
+    const int64_t large = ((m + 255) / 256) * ((n + 255) / 256);
+    if (large >= 256) return Plan{256, 1, chunks};
+    const int64_t tiles = ((m + 127) / 128) * ((n + 127) / 128);
+    int64_t parts = 512 / tiles;
+    if (parts > chunks / 2) parts = chunks / 2;
+    if (parts < 1) parts = 1;
+    const int64_t each = (chunks + parts - 1) / parts;
+    return Plan{128, (int32_t)((chunks + each - 1) / each), each};
+}
+
+template <typename T>
+hipError_t few_rows_of(const ProductArgs& p, hipStream_t s)
 {
     const int64_t n_tiles = (p.n + 15) / 16, tiles = n_tiles * ((p.m + 15) / 16);
     if (tiles > INT32_MAX) return hipErrorInvalidValue;
     hipLaunchKernelGGL((mx_few_rows_kernel<T, 4>), dim3((uint32_t)tiles), dim3(256), 0, s, p, (uint32_t)n_tiles);
+    return hipGetLastError();
+}
+template <typename T, int B>
+hipError_t tiles_of(const ProductArgs& p, hipStream_t s)
+{
+    const int64_t m_tiles = (p.m + B - 1) / B, n_tiles = (p.n + B - 1) / B, groups = m_tiles * n_tiles * p.parts;
+    if (groups > INT32_MAX || m_tiles * n_tiles * 8 > INT32_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((mx_tile_kernel<T, B, B, 2, 2>), dim3((uint32_t)groups), dim3(256), 0, s, p, (uint32_t)m_tiles, (uint32_t)n_tiles);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t product_of(ProductArgs p, const Plan& plan, float* workspace, hipStream_t s)
+{
+    if (plan.tile == 0) return few_rows_of<T>(p, s);
+    p.parts = plan.parts;
+    p.chunks_each = plan.chunks_each;
+    if (plan.parts == 1) return plan.tile == 256 ? tiles_of<T, 256>(p, s) : tiles_of<T, 128>(p, s);
+    ProductArgs q = p;
+    q.out = workspace;
+    q.stride = p.n;
+    q.bias = nullptr;
+    const hipError_t e = plan.tile == 256 ? tiles_of<float, 256>(q, s) : tiles_of<float, 128>(q, s);
+    if (e != hipSuccess) return e;
+    const int64_t runs = (p.n + 3) / 4, groups = (p.m * runs + 255) / 256;
+    hipLaunchKernelGGL((mx_join_kernel<T>), dim3((uint32_t)groups), dim3(256), 0, s, workspace, p.m, p.n, p.parts, p.bias, p.bias_dtype,
+                       static_cast<T*>(p.out), p.stride, (uint32_t)runs);
     return hipGetLastError();
 }
 
@@ -75,7 +316,12 @@ hipError_t product_of(const ProductArgs& p, hipStream_t s)
 
 extern "C" {
 
-size_t fh_mx_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k) { return 0; }
+size_t fh_mx_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k)
+{
+    if (!fh::mx_shape_ok(m, k) || !fh::mx_shape_ok(n, k) || k > fh::kMostSummed || m == 0 || n == 0) return 0;
+    const fh::Plan plan = fh::plan_of(m, n, k);
+    return plan.parts > 1 ? (size_t)plan.parts * (size_t)m * (size_t)n * 4u : 0;
+}
 
 fh_status fh_mx_matmul(const fh_mx_product* q, void* stream)
 {
@@ -95,9 +341,11 @@ fh_status fh_mx_matmul(const fh_mx_product* q, void* stream)
     if (workspace && !q->workspace) return FH_ERR_NULL;
     if (q->workspace_cap < workspace) return FH_ERR_BUFFER_TOO_SMALL;
     const ProductArgs p = {mx_store(const_cast<void*>(q->a), q->m, q->k), mx_store(const_cast<void*>(q->b), q->n, q->k), q->m, q->n,
-                           mx_chunks(q->k), q->bias, q->bias_dtype, q->out, q->stride};
+                           mx_chunks(q->k), q->bias, q->bias_dtype, 1, mx_chunks(q->k), q->out, q->stride};
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const hipError_t e = q->out_dtype == FH_F32 ? product_of<float>(p, s) : product_of<Bf16>(p, s);
+    const Plan plan = plan_of(q->m, q->n, q->k);
+    float* w = static_cast<float*>(q->workspace);
+    const hipError_t e = q->out_dtype == FH_F32 ? product_of<float>(p, plan, w, s) : product_of<Bf16>(p, plan, w, s);
     return e == hipSuccess ? FH_OK : FH_ERR_LAUNCH;
 }
 
