@@ -7,7 +7,8 @@ namespace {
 // Columns up to which a row is held in registers: by a wave, and by a workgroup of 1024.
 constexpr int64_t kWaveCols = 2048, kGroupCols = 16384;
 
-// The sum of v over the T threads that share a row; `s_sums` holds a value per wave and is used by every call in turn.
+// The sum of v over the T threads that share a row (the workgroup's rows are T threads each); `s_sums` holds a value per
+// wave and is used by every call in turn.
 template <int T>
 __device__ __forceinline__ float row_sum(float v, float* s_sums)
 {
@@ -16,8 +17,9 @@ __device__ __forceinline__ float row_sum(float v, float* s_sums)
         __syncthreads();                                         // the sums of the call before have been read
         if ((threadIdx.x & 63) == 0) s_sums[threadIdx.x >> 6] = v;
         __syncthreads();
+        const float* mine = s_sums + threadIdx.x / T * (T / 64);
         v = 0.0f;
-        for (int w = 0; w < T / 64; ++w) v += s_sums[w];
+        for (int w = 0; w < T / 64; ++w) v += mine[w];
     }
     return v;
 }
@@ -137,12 +139,14 @@ struct NormBackwardArgs {
     int32_t      p_dtype;
 };
 
-// Each workgroup takes rows a grid apart, keeps the sums of its columns in registers and leaves one row of partial sums.
-template <typename T, int THREADS, int NV>
-__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_backward_kernel(NormBackwardArgs a)
+// A workgroup takes ROWS rows at a time, a grid apart, THREADS threads each.  Every thread keeps the sums of its columns in
+// registers; at the end the rows' sums are added up in LDS, a run of columns at a time, and the workgroup leaves one row of
+// partial sums, for norm_join_kernel.
+template <typename T, int THREADS, int NV, int ROWS>
+__global__ __launch_bounds__(THREADS * ROWS) void norm_backward_kernel(NormBackwardArgs a)
 {
-    constexpr int kRows = THREADS < 256 ? 256 / THREADS : 1;     // rows of a workgroup at a time
     __shared__ float s_sums[16];
+    __shared__ __attribute__((aligned(16))) float s_join[ROWS > 1 ? ROWS * THREADS * 8 : 4];
     const int t = threadIdx.x % THREADS, part = threadIdx.x / THREADS;
     float w[NV][8], dw[NV][8], db[NV][8];
 #pragma unroll
@@ -156,7 +160,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_backward_k
         }
     }
     const float share = 1.0f / (float)a.cols;
-    for (int64_t start = (int64_t)blockIdx.x * kRows; start < a.rows; start += (int64_t)gridDim.x * kRows) {
+    for (int64_t start = (int64_t)blockIdx.x * ROWS; start < a.rows; start += (int64_t)gridDim.x * ROWS) {
         const int64_t row = start + part;
         const bool here = row < a.rows;
         float x[NV][8], g[NV][8];
@@ -168,6 +172,10 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_backward_k
             const int64_t first = ((int64_t)k * THREADS + t) * 8;
             load8(static_cast<const T*>(a.x) + at * a.x_stride + first, here ? a.cols - first : 0, x[k]);
             load8(static_cast<const T*>(a.dy) + at * a.dy_stride + first, here ? a.cols - first : 0, g[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int64_t first = ((int64_t)k * THREADS + t) * 8;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 x[k][i] = first + i < a.cols && here ? (x[k][i] - mean) * rstd : 0.0f;
@@ -191,13 +199,29 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_backward_k
         }
     }
     if (!a.partial) return;
-    float* to = a.partial + ((int64_t)blockIdx.x * kRows + part) * 2 * a.cols;
+    float* to = a.partial + (int64_t)blockIdx.x * 2 * a.cols;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int64_t first = ((int64_t)k * THREADS + t) * 8;
-        store8(to + first, a.cols - first, dw[k]);
-        store8(to + a.cols + first, a.cols - first, db[k]);
-    }
+    for (int which = 0; which < 2; ++which)
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int64_t first = ((int64_t)k * THREADS + t) * 8;
+            if constexpr (ROWS == 1) {
+                store8(to + which * a.cols + first, a.cols - first, which ? db[k] : dw[k]);
+            } else {
+                if ((int64_t)k * THREADS * 8 >= a.cols) continue;    // uniform
+                const float (&v)[8] = which ? db[k] : dw[k];
+                __syncthreads();
+                *reinterpret_cast<f32x4*>(s_join + (part * THREADS + t) * 8) = f32x4{v[0], v[1], v[2], v[3]};
+                *reinterpret_cast<f32x4*>(s_join + (part * THREADS + t) * 8 + 4) = f32x4{v[4], v[5], v[6], v[7]};
+                __syncthreads();
+                for (int c = threadIdx.x; c < THREADS * 8; c += THREADS * ROWS) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int r = 0; r < ROWS; ++r) sum += s_join[r * THREADS * 8 + c];
+                    if ((int64_t)k * THREADS * 8 + c < a.cols) to[which * a.cols + (int64_t)k * THREADS * 8 + c] = sum;
+                }
+            }
+        }
 }
 
 // Rows that do not fit: dx by a workgroup a row, which reads the row twice; the columns' sums by a kernel of their own.
@@ -251,21 +275,32 @@ __global__ __launch_bounds__(256) void norm_column_sums_kernel(NormBackwardArgs 
     store8(to + a.cols + first, a.cols - first, db);
 }
 
-// The partial rows added up, in their order whatever the launch: 64 columns of one of the two sums a workgroup, a quarter of the
-// rows a wave.
+// The partial rows added up in an order of their number alone: 64 columns of one of the two sums a workgroup, a sixteenth of the
+// rows a wave, four running sums each so that as many loads are on their way.
 template <typename P>
-__global__ __launch_bounds__(256) void norm_join_kernel(const float* partial, int64_t parts, int64_t cols, P* dweight, P* dbias)
+__global__ __launch_bounds__(1024) void norm_join_kernel(const float* partial, int64_t parts, int64_t cols, P* dweight, P* dbias)
 {
-    __shared__ float s_part[4][64];
+    __shared__ float s_part[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t c = (int64_t)(blockIdx.x >> 1) * 64 + lane, which = blockIdx.x & 1;
-    float sum = 0.0f;
-    if (c < cols)
-        for (int64_t r = wave; r < parts; r += 4) sum += partial[(r * 2 + which) * cols + c];
-    s_part[wave][lane] = sum;
+    float sum[4] = {};
+    if (c < cols) {
+        const float* from = partial + which * cols + c;
+        int64_t r = wave;
+        for (; r + 48 < parts; r += 64)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] += from[(r + 16 * i) * 2 * cols];
+        for (int i = 0; r < parts; r += 16, ++i) sum[i] += from[r * 2 * cols];
+    }
+    s_part[wave][lane] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
     __syncthreads();
     P* to = which ? dbias : dweight;
-    if (wave == 0 && c < cols && to) store1(to + c, (s_part[0][lane] + s_part[1][lane]) + (s_part[2][lane] + s_part[3][lane]));
+    if (wave == 0 && c < cols && to) {
+        float all = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) all += s_part[w][lane];
+        store1(to + c, all);
+    }
 }
 
 // ---- launches ------------------------------------------------------------------------------
@@ -285,42 +320,40 @@ hipError_t norm_any(const void* x, int64_t rows, int64_t cols, int64_t xs, const
     if (cols <= 1024) return norm_of<T, 64, 2>(x, rows, cols, xs, n, y, ys, to, s);
     if (cols <= kWaveCols) return norm_of<T, 64, 4>(x, rows, cols, xs, n, y, ys, to, s);
     if (cols <= 4096) return norm_of<T, 256, 2>(x, rows, cols, xs, n, y, ys, to, s);
-    if (cols <= 8192) return norm_of<T, 1024, 1>(x, rows, cols, xs, n, y, ys, to, s);
-    if (cols <= kGroupCols) return norm_of<T, 1024, 2>(x, rows, cols, xs, n, y, ys, to, s);
+    if (cols <= 8192) return rows >= 512 ? norm_of<T, 256, 4>(x, rows, cols, xs, n, y, ys, to, s) : norm_of<T, 1024, 1>(x, rows, cols, xs, n, y, ys, to, s);
+    if (cols <= kGroupCols) return rows >= 512 ? norm_of<T, 256, 8>(x, rows, cols, xs, n, y, ys, to, s) : norm_of<T, 1024, 2>(x, rows, cols, xs, n, y, ys, to, s);
     hipLaunchKernelGGL((norm_long_rows_kernel<T>), dim3((uint32_t)rows), dim3(1024), 0, s, static_cast<const T*>(x), cols, xs, n,
                        static_cast<T*>(y), ys, to);
     return hipGetLastError();
 }
 
-// Workgroups of the backward pass, and the rows of partial sums that they leave.
-struct BackwardShape { int64_t groups, parts; };
-inline BackwardShape backward_shape(int64_t rows, int64_t cols)
+// Rows that a workgroup of the backward pass takes at a time, workgroups, each of which leaves a row of partial sums.
+inline int64_t backward_rows(int64_t cols) { return cols <= 1024 ? 16 : cols <= kWaveCols ? 8 : cols <= 4096 ? 4 : 1; }
+inline int64_t backward_groups(int64_t rows, int64_t cols)
 {
-    const int64_t at_once = cols <= kWaveCols ? 4 : 1;
-    const int64_t most = cols <= kWaveCols ? 256 : 256;
-    const int64_t groups = (rows + at_once - 1) / at_once < most ? (rows + at_once - 1) / at_once : most;
-    return BackwardShape{groups, groups * at_once};
+    const int64_t each = backward_rows(cols), groups = (rows + each - 1) / each;
+    return groups < 256 ? groups : 256;
 }
 
-template <typename T, int THREADS, int NV>
+template <typename T, int THREADS, int NV, int ROWS>
 hipError_t backward_of(const NormBackwardArgs& a, int64_t groups, hipStream_t s)
 {
-    hipLaunchKernelGGL((norm_backward_kernel<T, THREADS, NV>), dim3((uint32_t)groups), dim3(THREADS < 256 ? 256 : THREADS), 0, s, a);
+    hipLaunchKernelGGL((norm_backward_kernel<T, THREADS, NV, ROWS>), dim3((uint32_t)groups), dim3(THREADS * ROWS), 0, s, a);
     return hipGetLastError();
 }
 template <typename T>
 hipError_t backward_any(const NormBackwardArgs& a, int64_t* parts, hipStream_t s)
 {
-    const BackwardShape b = backward_shape(a.rows, a.cols);
-    *parts = b.parts;
-    if (a.cols <= 512) return backward_of<T, 64, 1>(a, b.groups, s);
-    if (a.cols <= 1024) return backward_of<T, 64, 2>(a, b.groups, s);
-    if (a.cols <= kWaveCols) return backward_of<T, 64, 4>(a, b.groups, s);
-    if (a.cols <= 4096) return backward_of<T, 256, 2>(a, b.groups, s);
-    if (a.cols <= 8192) return backward_of<T, 1024, 1>(a, b.groups, s);
-    if (a.cols <= kGroupCols) return backward_of<T, 1024, 2>(a, b.groups, s);
+    const int64_t groups = backward_groups(a.rows, a.cols);
+    *parts = groups;
+    if (a.cols <= 512) return backward_of<T, 64, 1, 16>(a, groups, s);
+    if (a.cols <= 1024) return backward_of<T, 64, 2, 16>(a, groups, s);
+    if (a.cols <= kWaveCols) return backward_of<T, 64, 4, 8>(a, groups, s);
+    if (a.cols <= 4096) return backward_of<T, 256, 2, 4>(a, groups, s);
+    if (a.cols <= 8192) return backward_of<T, 1024, 1, 1>(a, groups, s);
+    if (a.cols <= kGroupCols) return backward_of<T, 1024, 2, 1>(a, groups, s);
     if (a.partial) {                                             // first: dx may be dy itself
-        const int64_t each = (a.rows + b.parts - 1) / b.parts, col_groups = (a.cols + 2047) / 2048;
+        const int64_t each = (a.rows + groups - 1) / groups, col_groups = (a.cols + 2047) / 2048;
         *parts = (a.rows + each - 1) / each;
         hipLaunchKernelGGL((norm_column_sums_kernel<T>), dim3((uint32_t)(col_groups * *parts)), dim3(256), 0, s, a, each, (uint32_t)col_groups);
         const hipError_t e = hipGetLastError();
@@ -332,7 +365,7 @@ hipError_t backward_any(const NormBackwardArgs& a, int64_t* parts, hipStream_t s
 template <typename P>
 hipError_t join_of(const float* partial, int64_t parts, int64_t cols, void* dweight, void* dbias, hipStream_t s)
 {
-    hipLaunchKernelGGL((norm_join_kernel<P>), dim3((uint32_t)((cols + 63) / 64 * 2)), dim3(256), 0, s, partial, parts, cols,
+    hipLaunchKernelGGL((norm_join_kernel<P>), dim3((uint32_t)((cols + 63) / 64 * 2)), dim3(1024), 0, s, partial, parts, cols,
                        static_cast<P*>(dweight), static_cast<P*>(dbias));
     return hipGetLastError();
 }
@@ -373,7 +406,7 @@ fh_status fh_layer_norm(const void* x, fh_dtype dtype, int64_t rows, int64_t col
 size_t fh_layer_norm_backward_workspace_bytes(int64_t rows, int64_t cols)
 {
     if (!fh::norm_shape_ok(rows, cols)) return 0;
-    return (size_t)fh::backward_shape(rows, cols).parts * 2u * (size_t)cols * 4u;
+    return (size_t)fh::backward_groups(rows, cols) * 2u * (size_t)cols * 4u;
 }
 
 fh_status fh_layer_norm_backward(const fh_norm_backward* b, void* stream)

@@ -20,163 +20,211 @@ __global__ __launch_bounds__(kThreads) void mx_rows_kernel(const T* x, int64_t r
     mx_write8(to, row, first, v, write);
 }
 
-// ---- tiles: blocks along the columns, along the rows, or both ------------------------------
-// A wave holds 32 rows x 128 columns, a lane two columns of all 32 rows: a column's block is the lane's own registers, a
-// row's block the 16 lanes of a DPP row.  Eight waves make 256 rows, so that the codes of a column, gathered in LDS, leave
-// as whole lines of 128 bytes.  The random bits of eight rows of a column are one Philox block, which the lane computes for
-// itself whatever the tensor's width.
 __device__ __forceinline__ float lane_value(float v, int lane)
 {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
 }
 
-constexpr int kTileRows = 256, kTileCols = 128, kTileThreads = 512;
+// ---- tiles: blocks along the columns, along the rows, or both ------------------------------
+// A wave holds 32 rows x 256 bytes.  It reads them by 16 bytes a lane, eight values of a row each, whose blocks are quads
+// of lanes, and passes them through LDS to have the 32 values of a column in one lane (two columns in bf16), whose block is
+// the lane's own registers: with columns in the lanes from the start a row's block would be 16 lanes wide, which took four
+// times the instructions.  Eight waves make 256 rows, so that the codes of a column, gathered in LDS, leave as whole lines
+// of 128 bytes.  The random bits of eight rows of a column are one Philox block, computed where the column is and handed to
+// the rows through LDS as well.
+constexpr int kTileRows = 256, kTileThreads = 512;
+constexpr int kWaveBytes = 32 * 256 + 16;          // the 16 turn the waves' areas, so that a gather of all eight meets all banks
+template <typename T> constexpr int kTileCols = 256 / (int)sizeof(T);
+
+// Eight values in words as they lie in memory.
+template <typename T>
+struct Run {
+    static constexpr int kWords = 2 * (int)sizeof(T);
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T* p, int64_t n)
+    {
+        if (n >= 8) {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4) {
+                const u32x4 v = *reinterpret_cast<const u32x4_a2*>(reinterpret_cast<const uint32_t*>(p) + i);
+                w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if constexpr (sizeof(T) == 4) w[i] = i < n ? __builtin_bit_cast(uint32_t, p[i]) : 0u;
+                else w[i / 2] = (i & 1 ? w[i / 2] : 0u) | (i < n ? (uint32_t)p[i].bits : 0u) << (16 * (i & 1));
+            }
+        }
+    }
+    __device__ __forceinline__ float at(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, w[i]);
+        else return i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
+    }
+};
 
 template <typename T, bool NORM, bool STOCHASTIC>
-__global__ __launch_bounds__(kTileThreads) void mx_tiles_kernel(const T* x, int64_t rows, int64_t cols, int64_t stride, NormArgs n,
-                                                                uint32_t k0, uint32_t k1, uint32_t id0, uint32_t id1,
-                                                                MxStore by_rows, MxStore by_columns, uint32_t col_tiles)
+__global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4) void mx_tiles_kernel(const T* x, int64_t rows, int64_t cols, int64_t stride, NormArgs n,
+                                                                   uint32_t k0, uint32_t k1, uint32_t id0, uint32_t id1,
+                                                                   MxStore by_rows, MxStore by_columns, uint32_t col_tiles)
 {
-    __shared__ u32x4 s_codes[kTileCols * 8];
-    __shared__ uint32_t s_scales[kTileCols * 2];
+    constexpr int kCols = kTileCols<T>, kLanes = kCols / 8, kAtOnce = 64 / kLanes, kGroups = 32 / kAtOnce, kEach = kCols / 64;
+    __shared__ __attribute__((aligned(16))) uint8_t s_area[8 * kWaveBytes];
+    __shared__ uint32_t s_scales[kCols * 2];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t col_tile = blockIdx.x % col_tiles, row_tile = blockIdx.x / col_tiles;
-    const int64_t r0 = row_tile * kTileRows + wave * 32;
-    const int64_t c0 = col_tile * kTileCols + lane * 2;
-    const bool in0 = c0 < cols, in1 = c0 + 1 < cols;
+    const int64_t r0 = row_tile * kTileRows + wave * 32, c0 = col_tile * kCols;
+    uint8_t* area = s_area + wave * kWaveBytes;
 
-    float v0[32], v1[32];
+    // as rows: lane (row % kAtOnce, column / 8)
+    const int64_t row_c = c0 + (lane % kLanes) * 8;
+    Run<T> run[kGroups];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        v0[i] = v1[i] = 0.0f;
-        if (r0 + i < rows) {                                     // uniform
-            const T* p = x + (r0 + i) * stride + c0;
-            if (in1) {
-                if constexpr (sizeof(T) == 4) {
-                    const f32x2 w = *reinterpret_cast<const f32x2_a4*>(p);
-                    v0[i] = w.x; v1[i] = w.y;
-                } else {
-                    const uint32_t w = *reinterpret_cast<const u32_a2*>(p);
-                    v0[i] = bf16_lo(w); v1[i] = bf16_hi(w);
-                }
-            } else if (in0) v0[i] = value(*p);
-        }
+    for (int g = 0; g < kGroups; ++g) {
+        const int64_t row = r0 + g * kAtOnce + lane / kLanes;
+        run[g].load(x + (row < rows ? row : 0) * stride + row_c, row < rows ? cols - row_c : 0);
     }
-    if constexpr (NORM) {
-        const float w0 = in0 ? parameter(n.weight, n.p_dtype, c0, 1.0f) : 0.0f, b0 = in0 ? parameter(n.bias, n.p_dtype, c0, 0.0f) : 0.0f;
-        const float w1 = in1 ? parameter(n.weight, n.p_dtype, c0 + 1, 1.0f) : 0.0f, b1 = in1 ? parameter(n.bias, n.p_dtype, c0 + 1, 0.0f) : 0.0f;
-        // lane i of the wave fetches row i's statistics; rows past the last stay zeros, whatever the bias
-        const int64_t mine = r0 + (lane & 31);
-        const float means = mine < rows ? n.mean[mine] : 0.0f, rstds = mine < rows ? n.rstd[mine] : 0.0f;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const float mean = lane_value(means, i), rstd = lane_value(rstds, i);
-            const bool row_in = r0 + i < rows;
-            v0[i] = row_in && in0 ? norm_value(v0[i], mean, rstd, w0, b0) : 0.0f;
-            v1[i] = row_in && in1 ? norm_value(v1[i], mean, rstd, w1, b1) : 0.0f;
-        }
-    }
-    // 65535 - h of row 8g + i: half-word i of not_h[.][g]
-    u32x4 not_h0[4], not_h1[4];
+    // 65535 - h of the lane's columns: half-word i of a block is row 8g + i's
+    u32x4 not_h[kEach][4];
     if constexpr (STOCHASTIC) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const uint64_t at = (uint64_t)((r0 >> 3) + g) * (uint64_t)cols + (uint64_t)c0;
-            not_h0[g] = philox4x32_10_complement((uint32_t)at, (uint32_t)(at >> 32), id0, id1, k0, k1);
-            const uint64_t bt = at + 1;
-            not_h1[g] = philox4x32_10_complement((uint32_t)bt, (uint32_t)(bt >> 32), id0, id1, k0, k1);
-        }
+        for (int e = 0; e < kEach; ++e)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const uint64_t at = (uint64_t)((r0 >> 3) + g) * (uint64_t)cols + (uint64_t)(c0 + lane * kEach + e);
+                not_h[e][g] = philox4x32_10_complement((uint32_t)at, (uint32_t)(at >> 32), id0, id1, k0, k1);
+            }
     }
-    auto half = [](const u32x4 (&w)[4], int i) -> uint32_t {
-        const uint32_t word = w[i >> 3][(i & 7) >> 1];
+    auto half = [&](int e, int i) -> uint32_t {
+        const uint32_t word = not_h[e][i >> 3][(i & 7) >> 1];
         return i & 1 ? word >> 16 : word & 0xFFFFu;
     };
 
     if (by_columns.codes) {
-        uint32_t t0 = 0, t1 = 0;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) { t0 = umax(t0, abs_bits(v0[i])); t1 = umax(t1, abs_bits(v1[i])); }
-        const uint32_t s0 = mx_scale_byte(t0), s1 = mx_scale_byte(t1);
-        u32x4 q0, q1;
+        for (int g = 0; g < kGroups; ++g)
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            uint32_t a = 0, b = 0;
-            if constexpr (STOCHASTIC) {
+            for (int i = 0; i < Run<T>::kWords; i += 4)
+                *reinterpret_cast<u32x4*>(area + (g * kAtOnce + lane / kLanes) * 256 + (lane % kLanes) * (8 * sizeof(T)) + i * 4) =
+                    u32x4{run[g].w[i], run[g].w[i + 1], run[g].w[i + 2], run[g].w[i + 3]};
+    }
+    // the rows' form, from the registers
+    auto write_rows = [&]() {
+        if constexpr (STOCHASTIC) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    a |= mx_stochastic(v0[8 * w + i], s0, half(not_h0, 8 * w + i)) << (4 * i);
-                    b |= mx_stochastic(v1[8 * w + i], s1, half(not_h1, 8 * w + i)) << (4 * i);
-                }
-            } else {
-                a = mx_nearest<0>(a, v0[8 * w], v0[8 * w + 1], s0);
-                a = mx_nearest<1>(a, v0[8 * w + 2], v0[8 * w + 3], s0);
-                a = mx_nearest<2>(a, v0[8 * w + 4], v0[8 * w + 5], s0);
-                a = mx_nearest<3>(a, v0[8 * w + 6], v0[8 * w + 7], s0);
-                b = mx_nearest<0>(b, v1[8 * w], v1[8 * w + 1], s1);
-                b = mx_nearest<1>(b, v1[8 * w + 2], v1[8 * w + 3], s1);
-                b = mx_nearest<2>(b, v1[8 * w + 4], v1[8 * w + 5], s1);
-                b = mx_nearest<3>(b, v1[8 * w + 6], v1[8 * w + 7], s1);
+            for (int i = 0; i < 32; ++i) {
+                if constexpr (kEach == 2) *reinterpret_cast<uint32_t*>(area + i * 256 + lane * 4) = half(0, i) | half(1, i) << 16;
+                else *reinterpret_cast<uint16_t*>(area + i * 128 + lane * 2) = (uint16_t)half(0, i);
             }
-            q0[w] = s0 == 255u ? 0u : a;
-            q1[w] = s1 == 255u ? 0u : b;
+            asm volatile("" ::: "memory");
         }
-        // a column's eight pieces are turned by the column pair, so that the lanes' writes meet all banks
-        const int turned = wave ^ (lane & 7);
-        s_codes[(2 * lane) * 8 + turned] = q0;
-        s_codes[(2 * lane + 1) * 8 + turned] = q1;
-        // [column/32][wave/4][column%32][wave%4], as the stored form has it
-        uint8_t* bytes = reinterpret_cast<uint8_t*>(s_scales);
-        const int at = (lane >> 4) * 256 + (wave >> 2) * 128 + (wave & 3);
-        bytes[at + ((2 * lane) & 31) * 4] = (uint8_t)s0;
-        bytes[at + ((2 * lane + 1) & 31) * 4] = (uint8_t)s1;
-        __syncthreads();
-        const int64_t first = col_tile * kTileCols;
+        float w[8], b[8];
+        if constexpr (NORM) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int id = threadIdx.x + i * kTileThreads, c = id >> 3, piece = id & 7;
-            if (first + c < by_columns.rows)
-                *reinterpret_cast<u32x4*>(by_columns.codes + (first + c) * (by_columns.chunks * 128) + row_tile * 128 + piece * 16) =
-                    s_codes[c * 8 + (piece ^ ((c >> 1) & 7))];
+            for (int i = 0; i < 8; ++i) {
+                w[i] = row_c + i < cols ? parameter(n.weight, n.p_dtype, row_c + i, 1.0f) : 0.0f;
+                b[i] = row_c + i < cols ? parameter(n.bias, n.p_dtype, row_c + i, 0.0f) : 0.0f;
+            }
         }
-        if (threadIdx.x < 256) {
-            const int64_t group = (first >> 5) + (threadIdx.x >> 6);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const int in_area = g * kAtOnce + lane / kLanes;
+            const int64_t row = r0 + in_area;
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = run[g].at(i);
+            if constexpr (NORM) {
+                const float mean = row < rows ? n.mean[row] : 0.0f, rstd = row < rows ? n.rstd[row] : 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = row_c + i < cols ? norm_value(v[i], mean, rstd, w[i], b[i]) : 0.0f;
+            }
+            if constexpr (STOCHASTIC) {
+                const u32x4 u = *reinterpret_cast<const u32x4*>(area + in_area * (kCols * 2) + (lane % kLanes) * 16);
+                uint32_t top = 0, codes = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = umax(top, abs_bits(v[i]));
+                const uint32_t s = mx_scale_byte(quad_max(top));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) codes |= mx_stochastic(v[i], s, i & 1 ? u[i / 2] >> 16 : u[i / 2] & 0xFFFFu) << (4 * i);
+                mx_put8(by_rows, row, row_c, codes, s, row < rows && row_c < by_rows.chunks * kMxChunk);
+            } else {
+                mx_write8(by_rows, row, row_c, v, row < rows && row_c < by_rows.chunks * kMxChunk);
+            }
+        }
+    };
+    // Random bits are made where the columns are, and reach the rows through the area that the columns leave; without them
+    // the rows come first, which frees their registers.
+    if (!STOCHASTIC && by_rows.codes) write_rows();
+    if (by_columns.codes) {
+        asm volatile("" ::: "memory");                           // a wave's own LDS accesses are in order
+        // lane i of the wave fetches row i's statistics; rows and columns past the last stay zeros, whatever the bias
+        float means = 0.0f, rstds = 0.0f;
+        if constexpr (NORM) {
+            const int64_t mine = r0 + (lane & 31);
+            if (mine < rows) { means = n.mean[mine]; rstds = n.rstd[mine]; }
+        }
+        u32x4 q[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {                        // one column at a time: both at once do not fit 128 registers
+            __builtin_amdgcn_sched_barrier(0);
+            const int c = lane * kEach + e;
+            float v[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(area + i * 256 + lane * 4);
+                if constexpr (sizeof(T) == 4) v[i] = __builtin_bit_cast(float, w);
+                else v[i] = e ? bf16_hi(w) : bf16_lo(w);
+            }
+            asm volatile("" ::: "memory");
+            if constexpr (NORM) {
+                const bool in = c0 + c < cols;
+                const float w = in ? parameter(n.weight, n.p_dtype, c0 + c, 1.0f) : 0.0f, b = in ? parameter(n.bias, n.p_dtype, c0 + c, 0.0f) : 0.0f;
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    v[i] = in && r0 + i < rows ? norm_value(v[i], lane_value(means, i), lane_value(rstds, i), w, b) : 0.0f;
+            }
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) top = umax(top, abs_bits(v[i]));
+            const uint32_t s = mx_scale_byte(top);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                uint32_t a = 0;
+                if constexpr (STOCHASTIC) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) a |= mx_stochastic(v[8 * w + i], s, half(e, 8 * w + i)) << (4 * i);
+                } else {
+                    a = mx_nearest<0>(a, v[8 * w], v[8 * w + 1], s);
+                    a = mx_nearest<1>(a, v[8 * w + 2], v[8 * w + 3], s);
+                    a = mx_nearest<2>(a, v[8 * w + 4], v[8 * w + 5], s);
+                    a = mx_nearest<3>(a, v[8 * w + 6], v[8 * w + 7], s);
+                }
+                q[e][w] = s == 255u ? 0u : a;
+            }
+            // [column/32][wave/4][column%32][wave%4], as the stored form has it
+            reinterpret_cast<uint8_t*>(s_scales)[(c >> 5) * 256 + (wave >> 2) * 128 + (c & 31) * 4 + (wave & 3)] = (uint8_t)s;
+        }
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) *reinterpret_cast<u32x4*>(area + (lane * kEach + e) * 16) = q[e];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kCols * 8 / kTileThreads; ++i) {
+            const int id = threadIdx.x + i * kTileThreads, c = id >> 3, piece = id & 7;
+            if (c0 + c < by_columns.rows)
+                *reinterpret_cast<u32x4*>(by_columns.codes + (c0 + c) * (by_columns.chunks * 128) + row_tile * 128 + piece * 16) =
+                    *reinterpret_cast<const u32x4*>(s_area + piece * kWaveBytes + c * 16);
+        }
+        if (threadIdx.x < kCols * 2) {
+            const int64_t group = (c0 >> 5) + (threadIdx.x >> 6);
             if (group * 32 < by_columns.rows)
                 *reinterpret_cast<uint32_t*>(by_columns.scales + ((group * by_columns.chunks + row_tile) << 8) + (threadIdx.x & 63) * 4) =
                     s_scales[threadIdx.x];
         }
+        if (STOCHASTIC && by_rows.codes) __syncthreads();        // the random bits go where the codes were
     }
 
-    if (by_rows.codes) {
-        const int quad = lane & 3;
-        const uint32_t pick1 = lane & 1 ? 0x03070105u : 0x06020400u;      // {b1,a1,b3,a3} : {a0,b0,a2,b2}, b the neighbour's
-        const uint32_t pick2 = lane & 2 ? 0x03020706u : 0x05040100u;
-        uint32_t kept0 = 1, kept1 = 1;                                    // scales of rows lane%16 and 16 + lane%16
-#pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-            uint32_t word = 0;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t s = mx_scale_byte(row_max(umax(abs_bits(v0[i + k]), abs_bits(v1[i + k]))));
-                uint32_t byte;
-                if constexpr (STOCHASTIC)
-                    byte = mx_stochastic(v0[i + k], s, half(not_h0, i + k)) | mx_stochastic(v1[i + k], s, half(not_h1, i + k)) << 4;
-                else
-                    byte = mx_nearest<0>(0, v0[i + k], v1[i + k], s) & 0xFFu;
-                word |= (s == 255u ? 0u : byte) << (8 * k);
-                if (i + k < 16) kept0 = (lane & 15) == i + k ? s : kept0;
-                else kept1 = (lane & 15) == i + k - 16 ? s : kept1;
-            }
-            // four rows' bytes of a column pair to a row's bytes of four column pairs, within each quad of lanes
-            word = __builtin_amdgcn_perm(dpp<kQuadXor1>(word), word, pick1);
-            word = __builtin_amdgcn_perm(dpp<kQuadXor2>(word), word, pick2);
-            const int64_t row = r0 + i + quad;
-            if (row < rows)
-                *reinterpret_cast<uint32_t*>(by_rows.codes + row * (by_rows.chunks * 128) + col_tile * (kTileCols / 2) + (lane >> 2) * 4) = word;
-        }
-        const int64_t block = col_tile * 4 + (lane >> 4), row = r0 + (lane & 15);
-        if (row < rows) by_rows.scales[mx_scale_at(row, block, by_rows.chunks)] = (uint8_t)kept0;
-        if (row + 16 < rows) by_rows.scales[mx_scale_at(row + 16, block, by_rows.chunks)] = (uint8_t)kept1;
-    }
+    if (STOCHASTIC && by_rows.codes) write_rows();
 }
 
 // ---- back ---------------------------------------------------------------------------------
@@ -214,7 +262,7 @@ hipError_t tiles_of(const void* x, int64_t rows, int64_t cols, int64_t stride, c
                     const MxStore& by_rows, const MxStore& by_columns, hipStream_t s)
 {
     // columns up to a whole chunk where rows are stored, rows up to a whole chunk where columns are
-    const int64_t col_tiles = by_rows.codes ? 2 * by_rows.chunks : (cols + kTileCols - 1) / kTileCols;
+    const int64_t width = by_rows.codes ? by_rows.chunks * kMxChunk : cols, col_tiles = (width + kTileCols<T> - 1) / kTileCols<T>;
     const int64_t row_tiles = (rows + kTileRows - 1) / kTileRows;
     if (col_tiles * row_tiles > INT32_MAX) return hipErrorInvalidValue;
     hipLaunchKernelGGL((mx_tiles_kernel<T, NORM, STOCHASTIC>), dim3((uint32_t)(col_tiles * row_tiles)), dim3(kTileThreads), 0, s,

@@ -34,7 +34,7 @@ __device__ __forceinline__ float parameter(const void* p, int32_t dtype, int64_t
 // Layer norm of rows: y (dense, may be null), or `to` (codes by rows, codes null: none), and the statistics where given.
 hipError_t launch_layer_norm(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t x_stride, const NormArgs& n,
                              void* y, int64_t y_stride, const MxStore& to, hipStream_t s);
-// The quantiser over tiles of 256 rows x 128 columns, with or without a norm whose statistics are known.
+// The quantiser over tiles of 256 rows, with or without a norm whose statistics are known.
 hipError_t launch_mx_tiles(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t x_stride, const NormArgs* n,
                            bool stochastic, uint64_t seed, uint64_t tensor_id, const MxStore& by_rows,
                            const MxStore& by_columns, hipStream_t s);
