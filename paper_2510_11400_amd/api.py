@@ -1286,14 +1286,19 @@ def fh_mix_decompress_batch(batch: MixBatch, stream=None) -> None:
 
 
 # ---- microscaled 4-bit storage, its product, layer norm ---------------------------------------------------
-def mx_bytes(rows: int, cols: int) -> int:
-    """Bytes of a stored matrix of rows x cols: a byte for two values (rows padded to multiples of 256) and one for 32."""
-    return int(_lib.fh_mx_bytes(rows, cols))
+# A launch takes the host about 3 us, a small product or norm the device as long: these functions ask a tensor for nothing
+# twice, and not the library for what a line of arithmetic gives.
+_MOST = 2 ** 31 - 256
 
 
 def mx_scales_offset(rows: int, cols: int) -> int:
     """Where the scales begin in a stored matrix."""
-    return int(_lib.fh_mx_scales_offset(rows, cols))
+    return (cols + 255) // 256 * 128 * rows if 0 <= rows <= _MOST and 0 <= cols <= _MOST else 0
+
+
+def mx_bytes(rows: int, cols: int) -> int:
+    """Bytes of a stored matrix of rows x cols: a byte for two values (rows padded to multiples of 256) and one for 32."""
+    return (cols + 255) // 256 * (128 * rows + (rows + 31) // 32 * 256) if 0 <= rows <= _MOST and 0 <= cols <= _MOST else 0
 
 
 class MxMatrix:
@@ -1308,11 +1313,21 @@ class MxMatrix:
         return self.data.numel()
 
 
-def _same_device(*tensors) -> None:
-    device = tensors[0].device
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"tensors of one call live on {device} and {t.device}")
+def _enqueue(device, stream: Optional[torch.cuda.Stream], call, *args) -> None:
+    """call(*args, stream's handle) with `device` the current one."""
+    index = torch._C._cuda_getDevice()
+    if device.index == index:
+        status = call(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            status = call(*args, _stream_ptr(stream))
+    if status:
+        raise FedHybridError(status)
+
+
+def _on_device(t: torch.Tensor, device, what: str) -> None:
+    if t.device != device:
+        raise ValueError(f"{what} lives on {t.device}, other tensors of the call on {device}")
 
 
 def _matrix(t: torch.Tensor, what: str):
@@ -1322,29 +1337,33 @@ def _matrix(t: torch.Tensor, what: str):
     if t.dim() != 2:
         raise ValueError(f"{what} must have two dimensions (got {t.dim()})")
     rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    stride, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError(f"the rows of {what} must be contiguous")
-    stride = t.stride(0) if rows > 1 else cols
+    if rows <= 1:
+        stride = cols
     if stride < cols:
         raise ValueError(f"the rows of {what} overlap")
     return rows, cols, stride
 
 
-def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
+def _vector(t: Optional[torch.Tensor], n: int, device, what: str) -> Optional[int]:
     if t is None:
         return None
-    _device_tensor(t, what)
+    _on_device(_device_tensor(t, what), device, what)
     if t.dim() != 1 or t.shape[0] != n:
         raise ValueError(f"{what} must be a vector of {n} values")
     return t.data_ptr()
 
 
-def _parameters(weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], cols: int):
+def _parameters(weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], cols: int, device):
     """(weight's pointer, bias's pointer, their dtype code)"""
+    if weight is None and bias is None:
+        return None, None, FH_F32
     if weight is not None and bias is not None and weight.dtype != bias.dtype:
         raise TypeError(f"weight and bias have different dtypes ({weight.dtype}, {bias.dtype})")
-    w, b = _vector(weight, cols, "weight"), _vector(bias, cols, "bias")
-    return w, b, _dtype_code(weight if weight is not None else bias) if weight is not None or bias is not None else FH_F32
+    return (_vector(weight, cols, device, "weight"), _vector(bias, cols, device, "bias"),
+            _dtype_code(weight if weight is not None else bias))
 
 
 _FORMS = ("rows", "columns", "both")
@@ -1378,34 +1397,34 @@ def fh_mx_quantize(x: torch.Tensor, forms: str = "rows", rounding="nearest", see
     """Enqueue the quantisation of the matrix x (rows contiguous, any row stride).  forms "rows" returns an MxMatrix of x
     with blocks of 32 values along its rows, "columns" one of x transposed (blocks along x's columns), "both" the two."""
     rows, cols, stride = _matrix(x, "x")
-    by_rows, by_columns = _stores(forms, rows, cols, x.device)
-    with _on(x.device):
-        _check(_lib.fh_mx_quantize(x.data_ptr(), _dtype_code(x), rows, cols, stride, _ROUND[rounding], _u64(seed), _u64(tensor_id),
-                                   *_store_args(by_rows), *_store_args(by_columns), _stream_ptr(stream)))
+    device = x.device
+    by_rows, by_columns = _stores(forms, rows, cols, device)
+    _enqueue(device, stream, _lib.fh_mx_quantize, x.data_ptr(), _dtype_code(x), rows, cols, stride, _ROUND[rounding], _u64(seed),
+             _u64(tensor_id), *_store_args(by_rows), *_store_args(by_columns))
     return _asked(forms, by_rows, by_columns)
 
 
 def _stored(m: MxMatrix, what: str) -> torch.Tensor:
     t = _device_tensor(m.data, what)
-    if t.dtype != torch.uint8 or t.numel() < mx_bytes(m.rows, m.cols):
-        raise FedHybridError(7)
+    if t.dtype != torch.uint8:
+        raise TypeError(f"{what} holds {t.dtype}, a stored matrix bytes")
     return t
 
 
 def fh_mx_dequantize(m: MxMatrix, out_dtype=torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Enqueue the restoration of a stored matrix; returns it as [rows, cols]."""
     data = _stored(m, "the stored matrix")
+    device, rows, cols, stride = data.device, m.rows, m.cols, m.cols
     if out is None:
-        out = torch.empty((m.rows, m.cols), dtype=out_dtype, device=data.device)
-    rows, cols, stride = _matrix(out, "out")
-    if (rows, cols) != (m.rows, m.cols):
-        raise ValueError(f"out is {rows} x {cols}, the matrix {m.rows} x {m.cols}")
-    _same_device(data, out)
+        out = torch.empty((rows, cols), dtype=out_dtype, device=device)
+    else:
+        out_rows, out_cols, stride = _matrix(out, "out")
+        if (out_rows, out_cols) != (rows, cols):
+            raise ValueError(f"out is {out_rows} x {out_cols}, the matrix {rows} x {cols}")
+        _on_device(out, device, "out")
     code = _dtype_code(out)
     nbytes = ((rows - 1) * stride + cols) * out.element_size() if rows and cols else 0
-    with _on(data.device):
-        _check(_lib.fh_mx_dequantize(data.data_ptr(), data.numel(), rows, cols, code, out.data_ptr(), stride, nbytes,
-                                     _stream_ptr(stream)))
+    _enqueue(device, stream, _lib.fh_mx_dequantize, data.data_ptr(), data.numel(), rows, cols, code, out.data_ptr(), stride, nbytes)
     return out
 
 
@@ -1417,45 +1436,55 @@ def fh_mx_matmul(a: MxMatrix, b: MxMatrix, bias: Optional[torch.Tensor] = None, 
                  out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Enqueue out = a b^T + bias of two stored matrices whose blocks run along the summed dimension."""
     da, db = _stored(a, "a"), _stored(b, "b")
-    if a.cols != b.cols:
-        raise ValueError(f"a has {a.cols} columns, b {b.cols}")
     m, n, k = a.rows, b.rows, a.cols
+    if b.cols != k:
+        raise ValueError(f"a has {k} columns, b {b.cols}")
+    device, stride = da.device, n
+    _on_device(db, device, "b")
     if out is None:
-        out = torch.empty((m, n), dtype=out_dtype, device=da.device)
-    rows, cols, stride = _matrix(out, "out")
-    if (rows, cols) != (m, n):
-        raise ValueError(f"out is {rows} x {cols}, the product {m} x {n}")
-    need = _lib.fh_mx_matmul_workspace_bytes(m, n, k)
-    if workspace is None and need:
-        workspace = _scratch(need, da.device, stream)
-    _same_device(da, db, bias, out, workspace)
-    p = fh_mx_product(da.data_ptr(), da.numel(), db.data_ptr(), db.numel(), m, n, k, _vector(bias, n, "bias"),
+        out = torch.empty((m, n), dtype=out_dtype, device=device)
+    else:
+        rows, cols, stride = _matrix(out, "out")
+        if (rows, cols) != (m, n):
+            raise ValueError(f"out is {rows} x {cols}, the product {m} x {n}")
+        _on_device(out, device, "out")
+    work, work_bytes = None, 0
+    if workspace is not None:
+        _on_device(_device_tensor(workspace, "workspace"), device, "workspace")
+    elif need := _lib.fh_mx_matmul_workspace_bytes(m, n, k):
+        workspace = _scratch(need, device, stream)
+    if workspace is not None:
+        work, work_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    p = fh_mx_product(da.data_ptr(), da.numel(), db.data_ptr(), db.numel(), m, n, k, _vector(bias, n, device, "bias"),
                       FH_F32 if bias is None else _dtype_code(bias), _dtype_code(out), out.data_ptr(), stride,
-                      ((m - 1) * stride + n) * out.element_size() if m and n else 0,
-                      None if workspace is None else _device_tensor(workspace, "workspace").data_ptr(),
-                      0 if workspace is None else workspace.numel() * workspace.element_size(), 0)
-    with _on(da.device):
-        _check(_lib.fh_mx_matmul(ctypes.byref(p), _stream_ptr(stream)))
+                      ((m - 1) * stride + n) * out.element_size() if m and n else 0, work, work_bytes, 0)
+    _enqueue(device, stream, _lib.fh_mx_matmul, ctypes.byref(p))
     return out
+
+
+def _like(t: Optional[torch.Tensor], x: torch.Tensor, rows: int, cols: int, what: str):
+    """(t, its row stride), or a new matrix like x."""
+    if t is None:
+        return torch.empty((rows, cols), dtype=x.dtype, device=x.device), cols
+    t_rows, t_cols, stride = _matrix(t, what)
+    if (t_rows, t_cols) != (rows, cols) or t.dtype != x.dtype:
+        raise ValueError(f"{what} must have the shape and the dtype of x")
+    _on_device(t, x.device, what)
+    return t, stride
 
 
 def fh_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
                   out: Optional[torch.Tensor] = None, stream=None):
     """Enqueue the layer norm of the matrix x over its rows; returns (y, mean, rstd), y in x's dtype, the statistics in fp32."""
     rows, cols, stride = _matrix(x, "x")
-    w, b, p_dtype = _parameters(weight, bias, cols)
-    if out is None:
-        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    out_rows, out_cols, out_stride = _matrix(out, "out")
-    if (out_rows, out_cols) != (rows, cols) or out.dtype != x.dtype:
-        raise ValueError("out must have the shape and the dtype of x")
-    _same_device(x, weight, bias, out)
-    stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
-    mean, rstd = stats.unbind(0)
-    with _on(x.device):
-        _check(_lib.fh_layer_norm(x.data_ptr(), _dtype_code(x), rows, cols, stride, w, b, p_dtype, eps, out.data_ptr(), out_stride,
-                                  ((rows - 1) * out_stride + cols) * out.element_size() if rows else 0,
-                                  mean.data_ptr(), rstd.data_ptr(), _stream_ptr(stream)))
+    device = x.device
+    w, b, p_dtype = _parameters(weight, bias, cols, device)
+    out, out_stride = _like(out, x, rows, cols, "out")
+    mean = torch.empty(rows, dtype=torch.float32, device=device)
+    rstd = torch.empty(rows, dtype=torch.float32, device=device)
+    _enqueue(device, stream, _lib.fh_layer_norm, x.data_ptr(), _dtype_code(x), rows, cols, stride, w, b, p_dtype, eps,
+             out.data_ptr(), out_stride, ((rows - 1) * out_stride + cols) * out.element_size() if rows else 0,
+             mean.data_ptr(), rstd.data_ptr())
     return out, mean, rstd
 
 
@@ -1464,15 +1493,14 @@ def fh_layer_norm_mx(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bia
     """Enqueue the layer norm of x with its result stored in microscaled form, as fh_mx_quantize stores it; returns
     (what fh_mx_quantize would return, mean, rstd)."""
     rows, cols, stride = _matrix(x, "x")
-    w, b, p_dtype = _parameters(weight, bias, cols)
-    _same_device(x, weight, bias)
-    by_rows, by_columns = _stores(forms, rows, cols, x.device)
-    stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
-    mean, rstd = stats.unbind(0)
-    with _on(x.device):
-        _check(_lib.fh_layer_norm_mx(x.data_ptr(), _dtype_code(x), rows, cols, stride, w, b, p_dtype, eps, _ROUND[rounding],
-                                     _u64(seed), _u64(tensor_id), *_store_args(by_rows), *_store_args(by_columns),
-                                     mean.data_ptr(), rstd.data_ptr(), _stream_ptr(stream)))
+    device = x.device
+    w, b, p_dtype = _parameters(weight, bias, cols, device)
+    by_rows, by_columns = _stores(forms, rows, cols, device)
+    mean = torch.empty(rows, dtype=torch.float32, device=device)
+    rstd = torch.empty(rows, dtype=torch.float32, device=device)
+    _enqueue(device, stream, _lib.fh_layer_norm_mx, x.data_ptr(), _dtype_code(x), rows, cols, stride, w, b, p_dtype, eps,
+             _ROUND[rounding], _u64(seed), _u64(tensor_id), *_store_args(by_rows), *_store_args(by_columns),
+             mean.data_ptr(), rstd.data_ptr())
     return _asked(forms, by_rows, by_columns), mean, rstd
 
 
@@ -1482,29 +1510,30 @@ def fh_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor
     """Enqueue the backward pass of fh_layer_norm; returns (dx, dweight, dbias), the last two (None unless `sums`) in the
     weight's dtype, in x's where there is no weight."""
     rows, cols, x_stride = _matrix(x, "x")
+    device = x.device
     dy_rows, dy_cols, dy_stride = _matrix(dy, "dy")
-    if (dy_rows, dy_cols) != (rows, cols) or dy.dtype != x.dtype:
+    if dy_rows != rows or dy_cols != cols or dy.dtype != x.dtype:
         raise ValueError("dy must have the shape and the dtype of x")
+    _on_device(dy, device, "dy")
     if mean.dtype != torch.float32 or rstd.dtype != torch.float32:
         raise TypeError("mean and rstd must be float32")
-    if dx is None:
-        dx = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    dx_rows, dx_cols, dx_stride = _matrix(dx, "dx")
-    if (dx_rows, dx_cols) != (rows, cols) or dx.dtype != x.dtype:
-        raise ValueError("dx must have the shape and the dtype of x")
-    p_dtype = x.dtype if weight is None else weight.dtype
-    dweight = dbias = None
+    dx, dx_stride = _like(dx, x, rows, cols, "dx")
+    like = x if weight is None else weight
+    dweight = dbias = work = dweight_ptr = dbias_ptr = None
+    work_bytes = 0
+    if workspace is not None:
+        _on_device(_device_tensor(workspace, "workspace"), device, "workspace")
     if sums:
-        dweight, dbias = torch.empty((2, cols), dtype=p_dtype, device=x.device).unbind(0)
+        dweight = torch.empty(cols, dtype=like.dtype, device=device)
+        dbias = torch.empty(cols, dtype=like.dtype, device=device)
+        dweight_ptr, dbias_ptr = dweight.data_ptr(), dbias.data_ptr()
         if workspace is None:
-            workspace = _scratch(_lib.fh_layer_norm_backward_workspace_bytes(rows, cols), x.device, stream)
-    _same_device(x, dy, mean, rstd, weight, dx, workspace)
-    p = fh_norm_backward(dy.data_ptr(), x.data_ptr(), dy_stride, x_stride, _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"),
-                         _vector(weight, cols, "weight"), rows, cols, _dtype_code(x), _dtype_code(x if weight is None else weight),
-                         dx.data_ptr(), dx_stride, ((rows - 1) * dx_stride + cols) * dx.element_size() if rows else 0,
-                         None if dweight is None else dweight.data_ptr(), None if dbias is None else dbias.data_ptr(),
-                         None if workspace is None else _device_tensor(workspace, "workspace").data_ptr(),
-                         0 if workspace is None else workspace.numel() * workspace.element_size())
-    with _on(x.device):
-        _check(_lib.fh_layer_norm_backward(ctypes.byref(p), _stream_ptr(stream)))
+            workspace = _scratch(_lib.fh_layer_norm_backward_workspace_bytes(rows, cols), device, stream)
+        work, work_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    p = fh_norm_backward(dy.data_ptr(), x.data_ptr(), dy_stride, x_stride, _vector(mean, rows, device, "mean"),
+                         _vector(rstd, rows, device, "rstd"), _vector(weight, cols, device, "weight"), rows, cols, _dtype_code(x),
+                         _dtype_code(like), dx.data_ptr(), dx_stride,
+                         ((rows - 1) * dx_stride + cols) * dx.element_size() if rows else 0,
+                         dweight_ptr, dbias_ptr, work, work_bytes)
+    _enqueue(device, stream, _lib.fh_layer_norm_backward, ctypes.byref(p))
     return dx, dweight, dbias

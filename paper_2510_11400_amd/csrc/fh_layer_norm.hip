@@ -25,9 +25,12 @@ __device__ __forceinline__ float row_sum(float v, float* s_sums)
 }
 
 // ---- forward: a row in the registers of T threads, NV runs of eight values each ------------
-template <typename T, int THREADS, int NV>
+// Where the rows go: dense (MX false: y and its row stride), or as codes.
+struct NormOut { void* y; uint8_t* scales; int64_t stride_or_chunks; };
+
+template <typename T, int THREADS, int NV, bool MX>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_rows_kernel(const T* x, int64_t rows, int64_t cols, int64_t x_stride,
-                                                                                  NormArgs n, T* y, int64_t y_stride, MxStore to)
+                                                                                  NormArgs n, NormOut to)
 {
     __shared__ float s_sums[16];
     const int t = threadIdx.x % THREADS;
@@ -60,7 +63,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_rows_kerne
         if (n.mean) n.mean[row] = mean;
         if (n.rstd) n.rstd[row] = rstd;
     }
-    if (!y && !to.codes) return;
+    if (!to.y) return;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         const int64_t first = ((int64_t)k * THREADS + t) * 8;
@@ -75,20 +78,20 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_rows_kerne
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             v[k][i] = norm_value(v[k][i], mean, rstd, n.weight ? w[i] : 1.0f, n.bias ? b[i] : 0.0f);
-        if (y) {
-            if (write) store8(y + row * y_stride + first, cols - first, v[k]);
+        if constexpr (!MX) {
+            if (write) store8(static_cast<T*>(to.y) + row * to.stride_or_chunks + first, cols - first, v[k]);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[k][i] = first + i < cols ? v[k][i] : 0.0f;
-            mx_write8(to, row, first, v[k], write && first < to.chunks * kMxChunk);
+            mx_write8(MxStore{static_cast<uint8_t*>(to.y), to.scales, to.stride_or_chunks}, row, first, v[k],
+                      write && first < to.stride_or_chunks * kMxChunk);
         }
     }
 }
 
 // Rows that do not fit: the row is read three times, from the caches after the first.
-template <typename T>
-__global__ __launch_bounds__(1024) void norm_long_rows_kernel(const T* x, int64_t cols, int64_t x_stride, NormArgs n, T* y,
-                                                              int64_t y_stride, MxStore to)
+template <typename T, bool MX>
+__global__ __launch_bounds__(1024) void norm_long_rows_kernel(const T* x, int64_t cols, int64_t x_stride, NormArgs n, NormOut to)
 {
     __shared__ float s_sums[16];
     const int64_t row = blockIdx.x;
@@ -113,7 +116,7 @@ __global__ __launch_bounds__(1024) void norm_long_rows_kernel(const T* x, int64_
         if (n.mean) n.mean[row] = mean;
         if (n.rstd) n.rstd[row] = rstd;
     }
-    if (!y && !to.codes) return;
+    if (!to.y) return;
     for (int64_t start = 0; start < end; start += 8192) {       // every lane takes every turn: quads work together
         const int64_t first = start + threadIdx.x * 8;
         load8(p + first, cols - first, v);
@@ -121,8 +124,8 @@ __global__ __launch_bounds__(1024) void norm_long_rows_kernel(const T* x, int64_
             const int64_t c = first + i;
             v[i] = c < cols ? norm_value(v[i], mean, rstd, parameter(n.weight, n.p_dtype, c, 1.0f), parameter(n.bias, n.p_dtype, c, 0.0f)) : 0.0f;
         }
-        if (y) store8(y + row * y_stride + first, cols - first, v);
-        else mx_write8(to, row, first, v, first < end);
+        if constexpr (!MX) store8(static_cast<T*>(to.y) + row * to.stride_or_chunks + first, cols - first, v);
+        else mx_write8(MxStore{static_cast<uint8_t*>(to.y), to.scales, to.stride_or_chunks}, row, first, v, first < end);
     }
 }
 
@@ -137,6 +140,7 @@ struct NormBackwardArgs {
     float*       partial;              // [workgroups][2][cols]: sums of dy * x^ and of dy; may be null
     int64_t      dy_stride, x_stride, dx_stride, rows, cols;
     int32_t      p_dtype;
+    int32_t      groups;               // workgroups
 };
 
 // A workgroup takes ROWS rows at a time, a grid apart, THREADS threads each.  Every thread keeps the sums of its columns in
@@ -160,7 +164,7 @@ __global__ __launch_bounds__(THREADS * ROWS) void norm_backward_kernel(NormBackw
         }
     }
     const float share = 1.0f / (float)a.cols;
-    for (int64_t start = (int64_t)blockIdx.x * ROWS; start < a.rows; start += (int64_t)gridDim.x * ROWS) {
+    for (int64_t start = (int64_t)blockIdx.x * ROWS; start < a.rows; start += (int64_t)a.groups * ROWS) {
         const int64_t row = start + part;
         const bool here = row < a.rows;
         float x[NV][8], g[NV][8];
@@ -304,26 +308,25 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const float* partial, i
 }
 
 // ---- launches ------------------------------------------------------------------------------
-template <typename T, int THREADS, int NV>
-hipError_t norm_of(const void* x, int64_t rows, int64_t cols, int64_t xs, const NormArgs& n, void* y, int64_t ys, const MxStore& to, hipStream_t s)
+template <typename T, int THREADS, int NV, bool MX>
+hipError_t norm_of(const void* x, int64_t rows, int64_t cols, int64_t xs, const NormArgs& n, const NormOut& to, hipStream_t s)
 {
     constexpr int kRows = THREADS < 256 ? 256 / THREADS : 1;
     const int64_t groups = (rows + kRows - 1) / kRows;
-    hipLaunchKernelGGL((norm_rows_kernel<T, THREADS, NV>), dim3((uint32_t)groups), dim3(THREADS < 256 ? 256 : THREADS), 0, s,
-                       static_cast<const T*>(x), rows, cols, xs, n, static_cast<T*>(y), ys, to);
+    hipLaunchKernelGGL((norm_rows_kernel<T, THREADS, NV, MX>), dim3((uint32_t)groups), dim3(THREADS < 256 ? 256 : THREADS), 0, s,
+                       static_cast<const T*>(x), rows, cols, xs, n, to);
     return hipGetLastError();
 }
-template <typename T>
-hipError_t norm_any(const void* x, int64_t rows, int64_t cols, int64_t xs, const NormArgs& n, void* y, int64_t ys, const MxStore& to, hipStream_t s)
+template <typename T, bool MX>
+hipError_t norm_any(const void* x, int64_t rows, int64_t cols, int64_t xs, const NormArgs& n, const NormOut& to, hipStream_t s)
 {
-    if (cols <= 512) return norm_of<T, 64, 1>(x, rows, cols, xs, n, y, ys, to, s);
-    if (cols <= 1024) return norm_of<T, 64, 2>(x, rows, cols, xs, n, y, ys, to, s);
-    if (cols <= kWaveCols) return norm_of<T, 64, 4>(x, rows, cols, xs, n, y, ys, to, s);
-    if (cols <= 4096) return norm_of<T, 256, 2>(x, rows, cols, xs, n, y, ys, to, s);
-    if (cols <= 8192) return rows >= 512 ? norm_of<T, 256, 4>(x, rows, cols, xs, n, y, ys, to, s) : norm_of<T, 1024, 1>(x, rows, cols, xs, n, y, ys, to, s);
-    if (cols <= kGroupCols) return rows >= 512 ? norm_of<T, 256, 8>(x, rows, cols, xs, n, y, ys, to, s) : norm_of<T, 1024, 2>(x, rows, cols, xs, n, y, ys, to, s);
-    hipLaunchKernelGGL((norm_long_rows_kernel<T>), dim3((uint32_t)rows), dim3(1024), 0, s, static_cast<const T*>(x), cols, xs, n,
-                       static_cast<T*>(y), ys, to);
+    if (cols <= 512) return norm_of<T, 64, 1, MX>(x, rows, cols, xs, n, to, s);
+    if (cols <= 1024) return norm_of<T, 64, 2, MX>(x, rows, cols, xs, n, to, s);
+    if (cols <= kWaveCols) return norm_of<T, 64, 4, MX>(x, rows, cols, xs, n, to, s);
+    if (cols <= 4096) return norm_of<T, 256, 2, MX>(x, rows, cols, xs, n, to, s);
+    if (cols <= 8192) return norm_of<T, 1024, 1, MX>(x, rows, cols, xs, n, to, s);
+    if (cols <= kGroupCols) return norm_of<T, 1024, 2, MX>(x, rows, cols, xs, n, to, s);
+    hipLaunchKernelGGL((norm_long_rows_kernel<T, MX>), dim3((uint32_t)rows), dim3(1024), 0, s, static_cast<const T*>(x), cols, xs, n, to);
     return hipGetLastError();
 }
 
@@ -344,7 +347,7 @@ hipError_t backward_of(const NormBackwardArgs& a, int64_t groups, hipStream_t s)
 template <typename T>
 hipError_t backward_any(const NormBackwardArgs& a, int64_t* parts, hipStream_t s)
 {
-    const int64_t groups = backward_groups(a.rows, a.cols);
+    const int64_t groups = a.groups;
     *parts = groups;
     if (a.cols <= 512) return backward_of<T, 64, 1, 16>(a, groups, s);
     if (a.cols <= 1024) return backward_of<T, 64, 2, 16>(a, groups, s);
@@ -375,9 +378,15 @@ bool norm_shape_ok(int64_t rows, int64_t cols) { return mx_shape_ok(rows, cols) 
 }  // namespace
 
 hipError_t launch_layer_norm(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t xs, const NormArgs& n, void* y, int64_t ys,
-                             const MxStore& to, hipStream_t s)
+                             void* codes, hipStream_t s)
 {
-    return dtype == FH_F32 ? norm_any<float>(x, rows, cols, xs, n, y, ys, to, s) : norm_any<Bf16>(x, rows, cols, xs, n, y, ys, to, s);
+    if (codes) {
+        const MxStore m = mx_store(codes, rows, cols);
+        const NormOut to = {m.codes, m.scales, m.chunks};
+        return dtype == FH_F32 ? norm_any<float, true>(x, rows, cols, xs, n, to, s) : norm_any<Bf16, true>(x, rows, cols, xs, n, to, s);
+    }
+    const NormOut to = {y, nullptr, ys};
+    return dtype == FH_F32 ? norm_any<float, false>(x, rows, cols, xs, n, to, s) : norm_any<Bf16, false>(x, rows, cols, xs, n, to, s);
 }
 
 }  // namespace fh
@@ -398,8 +407,7 @@ fh_status fh_layer_norm(const void* x, fh_dtype dtype, int64_t rows, int64_t col
         !is_aligned(bias, dtype_size(p_dtype)) || !is_aligned(mean, 4) || !is_aligned(rstd, 4)) return FH_ERR_ALIGNMENT;
     if (y_cap < strided_elements(rows, cols, y_stride) * dtype_size(dtype)) return FH_ERR_BUFFER_TOO_SMALL;
     const NormArgs n = {weight, bias, p_dtype, eps, static_cast<float*>(mean), static_cast<float*>(rstd)};
-    const MxStore none = {};
-    return launch_layer_norm(x, dtype, rows, cols, x_stride, n, y, y_stride, none, static_cast<hipStream_t>(stream)) == hipSuccess
+    return launch_layer_norm(x, dtype, rows, cols, x_stride, n, y, y_stride, nullptr, static_cast<hipStream_t>(stream)) == hipSuccess
                ? FH_OK : FH_ERR_LAUNCH;
 }
 
@@ -432,7 +440,8 @@ fh_status fh_layer_norm_backward(const fh_norm_backward* b, void* stream)
     int64_t parts = 0;
     if (b->rows > 0 && (b->dx || sums)) {
         const NormBackwardArgs a = {b->dy, b->x, static_cast<const float*>(b->mean), static_cast<const float*>(b->rstd), b->weight, b->dx, partial,
-                                    b->dy_stride, b->x_stride, b->dx_stride, b->rows, b->cols, b->p_dtype};
+                                    b->dy_stride, b->x_stride, b->dx_stride, b->rows, b->cols, b->p_dtype,
+                                    (int32_t)backward_groups(b->rows, b->cols)};
         const hipError_t e = b->dtype == FH_F32 ? backward_any<float>(a, &parts, s) : backward_any<Bf16>(a, &parts, s);
         if (e != hipSuccess) return FH_ERR_LAUNCH;
     }

@@ -29,16 +29,17 @@ inline uint64_t mx_bytes(int64_t rows, int64_t cols)
     return mx_codes_bytes(rows, cols) + (uint64_t)((rows + 31) / 32) * (uint64_t)mx_chunks(cols) * 256u;
 }
 
-// A stored matrix: for the kernels' arguments.
+// A stored matrix for the kernels.  Their arguments hold as few of these as possible: a launch of up to 112 bytes of
+// arguments is enqueued a microsecond sooner than a longer one, and the small calls wait for nothing else.
 struct MxStore {
     uint8_t* codes;
     uint8_t* scales;
-    int64_t  rows, chunks;
+    int64_t  chunks;
 };
-inline MxStore mx_store(void* p, int64_t rows, int64_t cols)
+inline __host__ __device__ MxStore mx_store(void* p, int64_t rows, int64_t cols)
 {
     uint8_t* b = static_cast<uint8_t*>(p);
-    return MxStore{b, b ? b + mx_codes_bytes(rows, cols) : nullptr, rows, mx_chunks(cols)};
+    return MxStore{b, b + rows * mx_pitch(cols), mx_chunks(cols)};
 }
 // Where the scale of row r's block b is.
 __device__ __forceinline__ int64_t mx_scale_at(int64_t r, int64_t b, int64_t chunks)

@@ -10,15 +10,19 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct ProductArgs {
-    MxStore      a, b;                 // m and n rows, the same number of chunks
-    int64_t      m, n, chunks;
-    const void*  bias;                 // may be null
-    int32_t      bias_dtype;
-    int32_t      parts;                // workgroups that share a tile's sum, each a run of chunks_each chunks
-    int64_t      chunks_each;
-    void*        out;                  // parts > 1: float [parts][m][n]
-    int64_t      stride;
+    const uint8_t *a, *a_scales;       // m rows
+    const uint8_t *b, *b_scales;       // n rows
+    int64_t        m, n;
+    const void*    bias;               // may be null
+    void*          out;                // parts > 1: float [parts][m][n]
+    int64_t        stride;
+    int32_t        chunks;             // of the rows of both
+    int32_t        chunks_each;        // of a workgroup's part of the sum
+    int32_t        parts;              // workgroups that share a tile's sum
+    int32_t        bias_dtype;
+    uint32_t       m_tiles, n_tiles;
 };
+static_assert(sizeof(ProductArgs) <= 112, "longer arguments are enqueued a microsecond later");
 
 // v_mfma_scale_f32_16x16x128_f8f6f4 with 4-bit operands: lane (r = lane % 16, g = lane / 16) brings 32 values of row r of
 // each operand with their scale, and gets the outputs [4g .. 4g+3][r].  Any 32 values of the sum may go to any g, the same
@@ -33,14 +37,14 @@ __device__ __forceinline__ f32x4 mx_mfma(u32x4 a, u32x4 b, uint32_t sa, uint32_t
 
 // 16 x 16 outputs a workgroup, its waves taking chunks in turn: their sums are joined in LDS in the waves' order.
 template <typename T, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void mx_few_rows_kernel(ProductArgs p, uint32_t n_tiles)
+__global__ __launch_bounds__(WAVES * 64) void mx_few_rows_kernel(ProductArgs p)
 {
     __shared__ float s_part[WAVES][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    const int64_t j0 = (int64_t)(blockIdx.x % n_tiles) * 16, i0 = (int64_t)(blockIdx.x / n_tiles) * 16;
+    const int64_t j0 = (int64_t)(blockIdx.x % p.n_tiles) * 16, i0 = (int64_t)(blockIdx.x / p.n_tiles) * 16;
     const int64_t j = j0 + r < p.n ? j0 + r : p.n - 1, i = i0 + r < p.m ? i0 + r : p.m - 1;
-    const uint8_t *cb = p.b.codes + j * (p.chunks * 128) + g * 32, *ca = p.a.codes + i * (p.chunks * 128) + g * 32;
-    const uint8_t *sb = p.b.scales + mx_scale_at(j, (g >> 1) * 4, p.chunks), *sa = p.a.scales + mx_scale_at(i, (g >> 1) * 4, p.chunks);
+    const uint8_t *cb = p.b + j * (p.chunks * 128) + g * 32, *ca = p.a + i * (p.chunks * 128) + g * 32;
+    const uint8_t *sb = p.b_scales + mx_scale_at(j, (g >> 1) * 4, p.chunks), *sa = p.a_scales + mx_scale_at(i, (g >> 1) * 4, p.chunks);
     f32x4 c = {0, 0, 0, 0};
     for (int64_t k = wave; k < p.chunks; k += WAVES) {
         const u32x4 b0 = *reinterpret_cast<const u32x4*>(cb + k * 128), b1 = *reinterpret_cast<const u32x4*>(cb + k * 128 + 16);
@@ -93,7 +97,7 @@ __device__ __forceinline__ u32x4 buffer_of(const uint8_t* p, uint32_t bytes)
 // The sum is bound by the matrix unit and, in the small tile, by LDS: a wave reads (BM/WM + BN/WN) * 128 bytes a chunk for
 // (BM/WM) * (BN/WN) * 256 products.
 template <typename T, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * 64, BM * BN > 16384 ? 1 : 2) void mx_tile_kernel(ProductArgs p, uint32_t m_tiles, uint32_t n_tiles)
+__global__ __launch_bounds__(WM * WN * 64, BM * BN > 16384 ? 1 : 2) void mx_tile_kernel(ProductArgs p)
 {
     constexpr int kWaves = WM * WN, MT = BM / WM / 32, NT = BN / WN / 32;
     constexpr uint32_t kCodes = (BM + BN) * 128, kStage = kCodes + (BM + BN) * 8;
@@ -107,7 +111,7 @@ __global__ __launch_bounds__(WM * WN * 64, BM * BN > 16384 ? 1 : 2) void mx_tile
 
     // Tiles go to the XCDs in runs (workgroups go to them in turn), a run in columns of up to eight tiles, so that what an
     // XCD works on at a time shares rows of both operands in its L2.
-    const uint32_t tiles = m_tiles * n_tiles, part = blockIdx.x / tiles, at = blockIdx.x % tiles;
+    const uint32_t m_tiles = p.m_tiles, n_tiles = p.n_tiles, tiles = m_tiles * n_tiles, part = blockIdx.x / tiles, at = blockIdx.x % tiles;
     const uint32_t xcd = at & 7, share = tiles >> 3, rest = tiles & 7;
     const uint32_t tile = xcd * share + (xcd < rest ? xcd : rest) + (at >> 3);
     const uint32_t band = tile / (8 * n_tiles), first = band * 8, high = m_tiles - first < 8 ? m_tiles - first : 8;
@@ -117,7 +121,7 @@ __global__ __launch_bounds__(WM * WN * 64, BM * BN > 16384 ? 1 : 2) void mx_tile
     // rows past the last are the last one, so that every address is inside
     const int rows_a = (int)(p.m - i0 < BM ? p.m - i0 : BM), rows_b = (int)(p.n - j0 < BN ? p.n - j0 : BN);
     const uint32_t pitch = (uint32_t)p.chunks * 128, scale_pitch = (uint32_t)p.chunks * 256;
-    const u32x4 from_a = buffer_of(p.a.codes + i0 * pitch, rows_a * pitch), from_b = buffer_of(p.b.codes + j0 * pitch, rows_b * pitch);
+    const u32x4 from_a = buffer_of(p.a + i0 * pitch, rows_a * pitch), from_b = buffer_of(p.b + j0 * pitch, rows_b * pitch);
     const uint32_t piece = ((lane & 7) ^ (lane >> 3)) * 16;
     uint32_t at_a[kLoadsA], at_b[kLoadsB];
 #pragma unroll
@@ -132,7 +136,7 @@ __global__ __launch_bounds__(WM * WN * 64, BM * BN > 16384 ? 1 : 2) void mx_tile
     }
     const bool scales_of_a = wave < BM / 128, loads_scales = wave < (BM + BN) / 128;
     const uint32_t groups = ((scales_of_a ? rows_a : rows_b) + 31) / 32;
-    const u32x4 from_scales = buffer_of(scales_of_a ? p.a.scales + (i0 >> 5) * scale_pitch : p.b.scales + (j0 >> 5) * scale_pitch, groups * scale_pitch);
+    const u32x4 from_scales = buffer_of(scales_of_a ? p.a_scales + (i0 >> 5) * scale_pitch : p.b_scales + (j0 >> 5) * scale_pitch, groups * scale_pitch);
     const uint32_t group = (scales_of_a ? wave : wave - BM / 128) * 4 + (lane >> 4);
     const uint32_t at_scales = (group < groups ? group : groups - 1) * scale_pitch + (lane & 15) * 16;
 
@@ -172,7 +176,8 @@ __global__ __launch_bounds__(WM * WN * 64, BM * BN > 16384 ? 1 : 2) void mx_tile
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                                                        \
         __builtin_amdgcn_sched_group_barrier(0x008, MT * NT / (MT + NT), 0);                                      \
     }
-    const uint32_t begin = (uint32_t)(part * p.chunks_each), end = (uint32_t)(begin + p.chunks_each < p.chunks ? begin + p.chunks_each : p.chunks);
+    const uint32_t chunks = (uint32_t)p.chunks, begin = part * (uint32_t)p.chunks_each;
+    const uint32_t end = begin + (uint32_t)p.chunks_each < chunks ? begin + (uint32_t)p.chunks_each : chunks;
     load(0, begin);
     if (begin + 1 < end) {
         load(kStage, begin + 1);
@@ -277,27 +282,28 @@ Plan plan_of(int64_t m, int64_t n, int64_t k)
 }
 
 template <typename T>
-hipError_t few_rows_of(const ProductArgs& p, hipStream_t s)
+hipError_t few_rows_of(ProductArgs p, hipStream_t s)
 {
     const int64_t n_tiles = (p.n + 15) / 16, tiles = n_tiles * ((p.m + 15) / 16);
     if (tiles > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((mx_few_rows_kernel<T, 4>), dim3((uint32_t)tiles), dim3(256), 0, s, p, (uint32_t)n_tiles);
+    p.n_tiles = (uint32_t)n_tiles;
+    hipLaunchKernelGGL((mx_few_rows_kernel<T, 4>), dim3((uint32_t)tiles), dim3(256), 0, s, p);
     return hipGetLastError();
 }
 template <typename T, int B>
-hipError_t tiles_of(const ProductArgs& p, hipStream_t s)
+hipError_t tiles_of(ProductArgs p, hipStream_t s)
 {
     const int64_t m_tiles = (p.m + B - 1) / B, n_tiles = (p.n + B - 1) / B, groups = m_tiles * n_tiles * p.parts;
     if (groups > INT32_MAX || m_tiles * n_tiles * 8 > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((mx_tile_kernel<T, B, B, 2, 2>), dim3((uint32_t)groups), dim3(256), 0, s, p, (uint32_t)m_tiles, (uint32_t)n_tiles);
+    p.m_tiles = (uint32_t)m_tiles;
+    p.n_tiles = (uint32_t)n_tiles;
+    hipLaunchKernelGGL((mx_tile_kernel<T, B, B, 2, 2>), dim3((uint32_t)groups), dim3(256), 0, s, p);
     return hipGetLastError();
 }
 template <typename T>
-hipError_t product_of(ProductArgs p, const Plan& plan, float* workspace, hipStream_t s)
+hipError_t product_of(const ProductArgs& p, const Plan& plan, float* workspace, hipStream_t s)
 {
     if (plan.tile == 0) return few_rows_of<T>(p, s);
-    p.parts = plan.parts;
-    p.chunks_each = plan.chunks_each;
     if (plan.parts == 1) return plan.tile == 256 ? tiles_of<T, 256>(p, s) : tiles_of<T, 128>(p, s);
     ProductArgs q = p;
     q.out = workspace;
@@ -340,10 +346,11 @@ fh_status fh_mx_matmul(const fh_mx_product* q, void* stream)
     const size_t workspace = fh_mx_matmul_workspace_bytes(q->m, q->n, q->k);
     if (workspace && !q->workspace) return FH_ERR_NULL;
     if (q->workspace_cap < workspace) return FH_ERR_BUFFER_TOO_SMALL;
-    const ProductArgs p = {mx_store(const_cast<void*>(q->a), q->m, q->k), mx_store(const_cast<void*>(q->b), q->n, q->k), q->m, q->n,
-                           mx_chunks(q->k), q->bias, q->bias_dtype, 1, mx_chunks(q->k), q->out, q->stride};
-    const hipStream_t s = static_cast<hipStream_t>(stream);
     const Plan plan = plan_of(q->m, q->n, q->k);
+    const MxStore a = mx_store(const_cast<void*>(q->a), q->m, q->k), b = mx_store(const_cast<void*>(q->b), q->n, q->k);
+    const ProductArgs p = {a.codes, a.scales, b.codes, b.scales, q->m, q->n, q->bias, q->out, q->stride, (int32_t)a.chunks,
+                           (int32_t)plan.chunks_each, plan.parts, q->bias_dtype, 0, 0};
+    const hipStream_t s = static_cast<hipStream_t>(stream);
     float* w = static_cast<float*>(q->workspace);
     const hipError_t e = q->out_dtype == FH_F32 ? product_of<float>(p, plan, w, s) : product_of<Bf16>(p, plan, w, s);
     return e == hipSuccess ? FH_OK : FH_ERR_LAUNCH;

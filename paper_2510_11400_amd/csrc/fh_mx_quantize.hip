@@ -67,8 +67,9 @@ struct Run {
 template <typename T, bool NORM, bool STOCHASTIC>
 __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4) void mx_tiles_kernel(const T* x, int64_t rows, int64_t cols, int64_t stride, NormArgs n,
                                                                    uint32_t k0, uint32_t k1, uint32_t id0, uint32_t id1,
-                                                                   MxStore by_rows, MxStore by_columns, uint32_t col_tiles)
+                                                                   uint8_t* rows_form, uint8_t* columns_form, uint32_t col_tiles)
 {
+    const MxStore by_rows = mx_store(rows_form, rows, cols), by_columns = mx_store(columns_form, cols, rows);
     constexpr int kCols = kTileCols<T>, kLanes = kCols / 8, kAtOnce = 64 / kLanes, kGroups = 32 / kAtOnce, kEach = kCols / 64;
     __shared__ __attribute__((aligned(16))) uint8_t s_area[8 * kWaveBytes];
     __shared__ uint32_t s_scales[kCols * 2];
@@ -101,7 +102,7 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
         return i & 1 ? word >> 16 : word & 0xFFFFu;
     };
 
-    if (by_columns.codes) {
+    if (columns_form) {
 #pragma unroll
         for (int g = 0; g < kGroups; ++g)
 #pragma unroll
@@ -155,8 +156,8 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
     };
     // Random bits are made where the columns are, and reach the rows through the area that the columns leave; without them
     // the rows come first, which frees their registers.
-    if (!STOCHASTIC && by_rows.codes) write_rows();
-    if (by_columns.codes) {
+    if (!STOCHASTIC && rows_form) write_rows();
+    if (columns_form) {
         asm volatile("" ::: "memory");                           // a wave's own LDS accesses are in order
         // lane i of the wave fetches row i's statistics; rows and columns past the last stay zeros, whatever the bias
         float means = 0.0f, rstds = 0.0f;
@@ -211,20 +212,20 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
 #pragma unroll
         for (int i = 0; i < kCols * 8 / kTileThreads; ++i) {
             const int id = threadIdx.x + i * kTileThreads, c = id >> 3, piece = id & 7;
-            if (c0 + c < by_columns.rows)
+            if (c0 + c < cols)
                 *reinterpret_cast<u32x4*>(by_columns.codes + (c0 + c) * (by_columns.chunks * 128) + row_tile * 128 + piece * 16) =
                     *reinterpret_cast<const u32x4*>(s_area + piece * kWaveBytes + c * 16);
         }
         if (threadIdx.x < kCols * 2) {
             const int64_t group = (c0 >> 5) + (threadIdx.x >> 6);
-            if (group * 32 < by_columns.rows)
+            if (group * 32 < cols)
                 *reinterpret_cast<uint32_t*>(by_columns.scales + ((group * by_columns.chunks + row_tile) << 8) + (threadIdx.x & 63) * 4) =
                     s_scales[threadIdx.x];
         }
-        if (STOCHASTIC && by_rows.codes) __syncthreads();        // the random bits go where the codes were
+        if (STOCHASTIC && rows_form) __syncthreads();        // the random bits go where the codes were
     }
 
-    if (STOCHASTIC && by_rows.codes) write_rows();
+    if (STOCHASTIC && rows_form) write_rows();
 }
 
 // ---- back ---------------------------------------------------------------------------------
@@ -259,15 +260,15 @@ hipError_t rows_of(const void* x, int64_t rows, int64_t cols, int64_t stride, co
 
 template <typename T, bool NORM, bool STOCHASTIC>
 hipError_t tiles_of(const void* x, int64_t rows, int64_t cols, int64_t stride, const NormArgs& n, uint64_t seed, uint64_t id,
-                    const MxStore& by_rows, const MxStore& by_columns, hipStream_t s)
+                    void* by_rows, void* by_columns, hipStream_t s)
 {
     // columns up to a whole chunk where rows are stored, rows up to a whole chunk where columns are
-    const int64_t width = by_rows.codes ? by_rows.chunks * kMxChunk : cols, col_tiles = (width + kTileCols<T> - 1) / kTileCols<T>;
+    const int64_t width = by_rows ? mx_chunks(cols) * kMxChunk : cols, col_tiles = (width + kTileCols<T> - 1) / kTileCols<T>;
     const int64_t row_tiles = (rows + kTileRows - 1) / kTileRows;
     if (col_tiles * row_tiles > INT32_MAX) return hipErrorInvalidValue;
     hipLaunchKernelGGL((mx_tiles_kernel<T, NORM, STOCHASTIC>), dim3((uint32_t)(col_tiles * row_tiles)), dim3(kTileThreads), 0, s,
                        static_cast<const T*>(x), rows, cols, stride, n, (uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)id,
-                       (uint32_t)(id >> 32), by_rows, by_columns, (uint32_t)col_tiles);
+                       (uint32_t)(id >> 32), static_cast<uint8_t*>(by_rows), static_cast<uint8_t*>(by_columns), (uint32_t)col_tiles);
     return hipGetLastError();
 }
 
@@ -305,7 +306,7 @@ fh_status check_input(const void* x, int x_dtype, int64_t rows, int64_t cols, in
 }  // namespace
 
 hipError_t launch_mx_tiles(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, const NormArgs* n, bool stochastic,
-                           uint64_t seed, uint64_t id, const MxStore& by_rows, const MxStore& by_columns, hipStream_t s)
+                           uint64_t seed, uint64_t id, void* by_rows, void* by_columns, hipStream_t s)
 {
     const NormArgs none = {};
     if (dtype == FH_F32) {
@@ -336,12 +337,12 @@ fh_status fh_mx_quantize(const void* x, fh_dtype x_dtype, int64_t rows, int64_t 
     const fh_status st = check_input(x, x_dtype, rows, cols, row_stride, rounding, by_rows, by_rows_cap, by_columns, by_columns_cap);
     if (st != FH_OK || rows == 0 || cols == 0) return st;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const MxStore to = mx_store(by_rows, rows, cols), turned = mx_store(by_columns, cols, rows);
     hipError_t e;
     if (by_columns || rounding == FH_ROUND_STOCHASTIC)
-        e = launch_mx_tiles(x, x_dtype, rows, cols, row_stride, nullptr, rounding == FH_ROUND_STOCHASTIC, seed, tensor_id, to, turned, s);
+        e = launch_mx_tiles(x, x_dtype, rows, cols, row_stride, nullptr, rounding == FH_ROUND_STOCHASTIC, seed, tensor_id, by_rows, by_columns, s);
     else
-        e = x_dtype == FH_F32 ? rows_of<float>(x, rows, cols, row_stride, to, s) : rows_of<Bf16>(x, rows, cols, row_stride, to, s);
+        e = x_dtype == FH_F32 ? rows_of<float>(x, rows, cols, row_stride, mx_store(by_rows, rows, cols), s)
+                                : rows_of<Bf16>(x, rows, cols, row_stride, mx_store(by_rows, rows, cols), s);
     return e == hipSuccess ? FH_OK : FH_ERR_LAUNCH;
 }
 
@@ -378,11 +379,10 @@ fh_status fh_layer_norm_mx(const void* x, fh_dtype x_dtype, int64_t rows, int64_
     if (!is_aligned(mean, 4) || !is_aligned(rstd, 4) || (weight && !is_aligned(weight, dtype_size(p_dtype))) ||
         (bias && !is_aligned(bias, dtype_size(p_dtype)))) return FH_ERR_ALIGNMENT;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const MxStore to = mx_store(by_rows, rows, cols), turned = mx_store(by_columns, cols, rows), none = {};
     const NormArgs n = {weight, bias, p_dtype, eps, static_cast<float*>(mean), static_cast<float*>(rstd)};
-    if (launch_layer_norm(x, x_dtype, rows, cols, row_stride, n, nullptr, 0, tiles ? none : to, s) != hipSuccess) return FH_ERR_LAUNCH;
+    if (launch_layer_norm(x, x_dtype, rows, cols, row_stride, n, nullptr, 0, tiles ? nullptr : by_rows, s) != hipSuccess) return FH_ERR_LAUNCH;
     if (!tiles) return FH_OK;
-    return launch_mx_tiles(x, x_dtype, rows, cols, row_stride, &n, rounding == FH_ROUND_STOCHASTIC, seed, tensor_id, to, turned, s) == hipSuccess
+    return launch_mx_tiles(x, x_dtype, rows, cols, row_stride, &n, rounding == FH_ROUND_STOCHASTIC, seed, tensor_id, by_rows, by_columns, s) == hipSuccess
                ? FH_OK : FH_ERR_LAUNCH;
 }
 

@@ -31,13 +31,12 @@ __device__ __forceinline__ float parameter(const void* p, int32_t dtype, int64_t
     return dtype == FH_F32 ? static_cast<const float*>(p)[i] : value(static_cast<const Bf16*>(p)[i]);
 }
 
-// Layer norm of rows: y (dense, may be null), or `to` (codes by rows, codes null: none), and the statistics where given.
+// Layer norm of rows to y (dense), to `codes` (by rows), or the statistics alone where both are null.
 hipError_t launch_layer_norm(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t x_stride, const NormArgs& n,
-                             void* y, int64_t y_stride, const MxStore& to, hipStream_t s);
-// The quantiser over tiles of 256 rows, with or without a norm whose statistics are known.
+                             void* y, int64_t y_stride, void* codes, hipStream_t s);
+// The quantiser over tiles of 256 rows, with or without a norm whose statistics are known; either form may be null.
 hipError_t launch_mx_tiles(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t x_stride, const NormArgs* n,
-                           bool stochastic, uint64_t seed, uint64_t tensor_id, const MxStore& by_rows,
-                           const MxStore& by_columns, hipStream_t s);
+                           bool stochastic, uint64_t seed, uint64_t tensor_id, void* by_rows, void* by_columns, hipStream_t s);
 
 // The host's checks of a matrix in rows: `elements` from its pointer on are read or written.
 inline bool is_aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }

@@ -187,3 +187,10 @@ def test_the_binding_refuses_host_tensors_and_shapes():
             call()
     with pytest.raises(ValueError, match="forms"):
         api._stores("diagonal", 4, 40, "cpu")
+
+
+@pytest.mark.parametrize("rows, cols", [(0, 0), (0, 5), (5, 0), (1, 1), (33, 255), (8192, 768), (2 ** 31 - 256, 257), (3, 2 ** 31 - 256), (-1, 5), (5, -1),
+                                        (2 ** 31 - 255, 1), (1, 2 ** 31)])
+def test_the_binding_and_the_library_agree_on_sizes(rows, cols):
+    assert api.mx_bytes(rows, cols) == LIB.fh_mx_bytes(rows, cols)
+    assert api.mx_scales_offset(rows, cols) == LIB.fh_mx_scales_offset(rows, cols)
