@@ -176,6 +176,13 @@ __device__ __forceinline__ void store_run(float* p, int64_t n, const float (&v)[
     else for (int i = 0; i < 4; ++i) if (i < n) p[i] = v[i];
 }
 __device__ __forceinline__ void store_run(Bf16* p, int64_t n, const float (&v)[8]) { store8(p, n, v); }
+typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
+__device__ __forceinline__ void store4(float* p, int64_t n, const float (&v)[4]) { store_run(p, n, v); }
+__device__ __forceinline__ void store4(Bf16* p, int64_t n, const float (&v)[4])
+{
+    if (n >= 4) *reinterpret_cast<u32x2_a2*>(p) = u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+    else for (int i = 0; i < 4; ++i) if (i < n) store1(p + i, v[i]);
+}
 
 // ---- eight values of a lane, 32 of a quad, to the stored form of their row ----------------
 // All 64 lanes are active; `first` is a multiple of 8, the quad's 32 values are one block.  Columns past the row's end hold

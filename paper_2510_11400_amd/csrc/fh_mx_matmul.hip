@@ -24,48 +24,6 @@ struct ProductArgs {
 };
 static_assert(sizeof(ProductArgs) <= 112, "longer arguments are enqueued a microsecond later");
 
-// v_mfma_scale_f32_16x16x128_f8f6f4 with 4-bit operands: lane (r = lane % 16, g = lane / 16) brings 32 values of row r of
-// each operand with their scale, and gets the outputs [4g .. 4g+3][r].  Any 32 values of the sum may go to any g, the same
-// for both operands: of a chunk's eight blocks a lane takes 2g and 2g+1, for one instruction each, whose codes are 32
-// contiguous bytes and whose scales lie in one word.
-template <int BYTE>
-__device__ __forceinline__ f32x4 mx_mfma(u32x4 a, u32x4 b, uint32_t sa, uint32_t sb, f32x4 c)
-{
-    const i32x8 x = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0}, y = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, BYTE, (int)sa, BYTE, (int)sb);
-}
-
-// 16 x 16 outputs a workgroup, its waves taking chunks in turn: their sums are joined in LDS in the waves' order.
-template <typename T, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void mx_few_rows_kernel(ProductArgs p)
-{
-    __shared__ float s_part[WAVES][256];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    const int64_t j0 = (int64_t)(blockIdx.x % p.n_tiles) * 16, i0 = (int64_t)(blockIdx.x / p.n_tiles) * 16;
-    const int64_t j = j0 + r < p.n ? j0 + r : p.n - 1, i = i0 + r < p.m ? i0 + r : p.m - 1;
-    const uint8_t *cb = p.b + j * (p.chunks * 128) + g * 32, *ca = p.a + i * (p.chunks * 128) + g * 32;
-    const uint8_t *sb = p.b_scales + mx_scale_at(j, (g >> 1) * 4, p.chunks), *sa = p.a_scales + mx_scale_at(i, (g >> 1) * 4, p.chunks);
-    f32x4 c = {0, 0, 0, 0};
-    for (int64_t k = wave; k < p.chunks; k += WAVES) {
-        const u32x4 b0 = *reinterpret_cast<const u32x4*>(cb + k * 128), b1 = *reinterpret_cast<const u32x4*>(cb + k * 128 + 16);
-        const u32x4 a0 = *reinterpret_cast<const u32x4*>(ca + k * 128), a1 = *reinterpret_cast<const u32x4*>(ca + k * 128 + 16);
-        const uint32_t tb = *reinterpret_cast<const uint32_t*>(sb + k * 256) >> ((g & 1) * 16);
-        const uint32_t ta = *reinterpret_cast<const uint32_t*>(sa + k * 256) >> ((g & 1) * 16);
-        c = mx_mfma<0>(b0, a0, tb, ta, c);
-        c = mx_mfma<1>(b1, a1, tb, ta, c);
-    }
-    // outputs [i = r][j = 4g ..]
-    *reinterpret_cast<f32x4*>(&s_part[wave][r * 16 + g * 4]) = c;
-    __syncthreads();
-    if (threadIdx.x < 256) {
-        float sum = 0.0f;
-        for (int w = 0; w < WAVES; ++w) sum += s_part[w][threadIdx.x];
-        const int64_t row = i0 + (threadIdx.x >> 4), col = j0 + (threadIdx.x & 15);
-        if (row < p.m && col < p.n) store1(static_cast<T*>(p.out) + row * p.stride + col, sum + parameter(p.bias, p.bias_dtype, col, 0.0f));
-    }
-}
-
-// ---- large products: tiles through LDS ----------------------------------------------------------
 // v_mfma_scale_f32_32x32x64_f8f6f4: lane (r = lane % 32, h = lane / 32) brings 32 values of row r of each operand, and gets
 // the outputs [8 (i/4) + 4 h + i % 4][r].  It measured 7.0 PFLOP/s from registers, the 16 x 16 form 4.3.  Of a chunk's
 // eight blocks a lane takes 4h .. 4h+3, in four instructions, whose scales are the bytes of one word.
@@ -82,7 +40,7 @@ __device__ __forceinline__ f32x16 mx_mfma32(u32x4 a, u32x4 b, uint32_t sa, uint3
 __device__ __forceinline__ void to_lds(uint32_t lds, u32x4 from, uint32_t offset, uint32_t moved)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 :: "s"(lds), "v"(offset), "s"(from), "s"(moved) : "memory");
+                 :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(from), "s"(__builtin_amdgcn_readfirstlane(moved)) : "memory");
 }
 __device__ __forceinline__ u32x4 buffer_of(const uint8_t* p, uint32_t bytes)
 {
@@ -90,12 +48,112 @@ __device__ __forceinline__ u32x4 buffer_of(const uint8_t* p, uint32_t bytes)
     return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, bytes, 0x00020000u};
 }
 
+// ---- few tiles: the sum split over a workgroup's waves, through LDS --------------------------------
+// (32 MT) x (32 NT) outputs a workgroup; each wave multiplies a run of chunks by itself, with an area of LDS of its own and no barrier:
+// a chunk's rows come as whole lines into the area, from there to registers, and while those are multiplied the next chunk's
+// come.  The waves' sums are joined in LDS in the waves' order.
+template <typename T, int MT, int NT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void mx_waves_kernel(ProductArgs p)
+{
+    constexpr int kRowsA = MT * 32, kRowsB = NT * 32, kPad = kRowsB + 4;
+    constexpr uint32_t kCodes = (kRowsA + kRowsB) * 128, kScales = (kRowsA + kRowsB) * 8;
+    constexpr uint32_t kSums = kRowsA * kPad * 4, kArea = kCodes + kScales > kSums ? kCodes + kScales : kSums;
+    static_assert(kScales <= 1024, "one load brings the scales");
+    __shared__ __attribute__((aligned(16))) uint8_t s_area[WAVES * kArea];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t tiles = p.m_tiles * p.n_tiles, part = blockIdx.x / tiles, tile = blockIdx.x - part * tiles;
+    const int64_t j0 = (int64_t)(tile % p.n_tiles) * kRowsB, i0 = (int64_t)(tile / p.n_tiles) * kRowsA;
+    const uint32_t pitch = (uint32_t)p.chunks * 128, scale_pitch = (uint32_t)p.chunks * 256;
+    // rows past the last are the last one, so that every address is inside
+    const int rows_a = (int)(p.m - i0 < kRowsA ? p.m - i0 : kRowsA), rows_b = (int)(p.n - j0 < kRowsB ? p.n - j0 : kRowsB);
+    const u32x4 from_a = buffer_of(p.a + i0 * pitch, rows_a * pitch), from_b = buffer_of(p.b + j0 * pitch, rows_b * pitch);
+    const uint32_t piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    uint32_t at_a[MT * 4], at_b[NT * 4];
+#pragma unroll
+    for (int t = 0; t < MT * 4; ++t) {
+        const int r = t * 8 + (lane >> 3);
+        at_a[t] = (r < rows_a ? r : rows_a - 1) * pitch + piece;
+    }
+#pragma unroll
+    for (int t = 0; t < NT * 4; ++t) {
+        const int r = t * 8 + (lane >> 3);
+        at_b[t] = (r < rows_b ? r : rows_b - 1) * pitch + piece;
+    }
+    const uint32_t groups_a = (rows_a + 31) / 32, groups_b = (rows_b + 31) / 32;
+    const u32x4 from_sa = buffer_of(p.a_scales + (i0 >> 5) * scale_pitch, groups_a * scale_pitch);
+    const u32x4 from_sb = buffer_of(p.b_scales + (j0 >> 5) * scale_pitch, groups_b * scale_pitch);
+    const uint32_t group = lane >> 4, group_b = group - MT;
+    const bool of_a = group < MT, of_b = !of_a && group_b < NT;
+    const uint32_t at_scales = (of_a ? (group < groups_a ? group : groups_a - 1) : (group_b < groups_b ? group_b : groups_b - 1)) * scale_pitch + (lane & 15) * 16;
+    uint8_t* area = s_area + wave * kArea;
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_area + wave * kArea;
+    auto load = [&](uint32_t chunk) {
+        if (of_a) to_lds(lds + kCodes, from_sa, at_scales, chunk * 256);
+        if (of_b) to_lds(lds + kCodes, from_sb, at_scales, chunk * 256);
+#pragma unroll
+        for (int t = 0; t < MT * 4; ++t) to_lds(lds + t * 1024, from_a, at_a[t], chunk * 128);
+#pragma unroll
+        for (int t = 0; t < NT * 4; ++t) to_lds(lds + kRowsA * 128 + t * 1024, from_b, at_b[t], chunk * 128);
+    };
+    const int h = lane >> 5, r = lane & 31, turned = (h * 4) ^ (lane & 7);
+    const uint32_t chunks = (uint32_t)p.chunks, begin = part * (uint32_t)p.chunks_each;
+    const uint32_t end = begin + (uint32_t)p.chunks_each < chunks ? begin + (uint32_t)p.chunks_each : chunks;
+    f32x16 c[MT][NT] = {};
+    uint32_t k = begin + wave;
+    if (k < end) load(k);
+    while (k < end) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        u32x4 fa[4][MT], fb[4][NT];
+        uint32_t sa[MT], sb[NT];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) sa[t] = *reinterpret_cast<const uint32_t*>(area + kCodes + t * 256 + h * 128 + r * 4);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sb[t] = *reinterpret_cast<const uint32_t*>(area + kCodes + (MT + t) * 256 + h * 128 + r * 4);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint8_t* from = area + (uint32_t)(turned ^ q) * 16 + r * 128;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) fb[q][t] = *reinterpret_cast<const u32x4*>(from + kRowsA * 128 + t * 4096);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) fa[q][t] = *reinterpret_cast<const u32x4*>(from + t * 4096);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the area may be written again
+        k += WAVES;
+        if (k < end) load(k);
+#define FH_QUARTER(Q)                                                                                             \
+        _Pragma("unroll") for (int x = 0; x < MT; ++x) _Pragma("unroll") for (int y = 0; y < NT; ++y)             \
+            c[x][y] = mx_mfma32<Q>(fb[Q][y], fa[Q][x], sb[y], sa[x], c[x][y]);
+        FH_QUARTER(0) FH_QUARTER(1) FH_QUARTER(2) FH_QUARTER(3)
+#undef FH_QUARTER
+    }
+    // this wave's area is its own still
+#pragma unroll
+    for (int x = 0; x < MT; ++x)
+#pragma unroll
+        for (int y = 0; y < NT; ++y)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<f32x4*>(area + ((x * 32 + r) * kPad + y * 32 + 2 * i + 4 * h) * 4) = f32x4{c[x][y][i], c[x][y][i + 1], c[x][y][i + 2], c[x][y][i + 3]};
+    __syncthreads();
+    for (int at = threadIdx.x; at < kRowsA * kRowsB / 4; at += WAVES * 64) {
+        const int row = at / (kRowsB / 4), col = at % (kRowsB / 4) * 4;
+        f32x4 sum = *reinterpret_cast<const f32x4*>(s_area + (row * kPad + col) * 4);
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) sum += *reinterpret_cast<const f32x4*>(s_area + w * kArea + (row * kPad + col) * 4);
+        const int64_t i = i0 + row, j = j0 + col;
+        if (i >= p.m) continue;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = sum[e] + (j + e < p.n ? parameter(p.bias, p.bias_dtype, j + e, 0.0f) : 0.0f);
+        store4(static_cast<T*>(p.out) + (int64_t)part * p.m * p.n + i * p.stride + j, p.n - j, v);
+    }
+}
+
+// ---- large products: tiles through LDS ----------------------------------------------------------
 // BM x BN outputs a workgroup of WM x WN waves, a chunk of 256 summed values at a time.  Two stages of LDS: while one is
 // multiplied the next is on its way, and a stage is handed over before its last quarter, which is in registers by then, so
 // that the matrix unit works across the barrier.  A row's eight pieces of 16 bytes are turned by the row (the loads take
 // them from turned addresses), so that eight lanes reading the same piece of eight rows meet all banks.
-// The sum is bound by the matrix unit and, in the small tile, by LDS: a wave reads (BM/WM + BN/WN) * 128 bytes a chunk for
-// (BM/WM) * (BN/WN) * 256 products.
 template <typename T, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * 64, BM * BN > 16384 ? 1 : 2) void mx_tile_kernel(ProductArgs p)
 {
@@ -111,12 +169,12 @@ __global__ __launch_bounds__(WM * WN * 64, BM * BN > 16384 ? 1 : 2) void mx_tile
 
     // Tiles go to the XCDs in runs (workgroups go to them in turn), a run in columns of up to eight tiles, so that what an
     // XCD works on at a time shares rows of both operands in its L2.
-    const uint32_t m_tiles = p.m_tiles, n_tiles = p.n_tiles, tiles = m_tiles * n_tiles, part = blockIdx.x / tiles, at = blockIdx.x % tiles;
+    const uint32_t m_tiles = p.m_tiles, n_tiles = p.n_tiles, tiles = m_tiles * n_tiles, at = blockIdx.x;
     const uint32_t xcd = at & 7, share = tiles >> 3, rest = tiles & 7;
     const uint32_t tile = xcd * share + (xcd < rest ? xcd : rest) + (at >> 3);
-    const uint32_t band = tile / (8 * n_tiles), first = band * 8, high = m_tiles - first < 8 ? m_tiles - first : 8;
-    const int64_t i0 = (int64_t)(first + (tile - band * 8 * n_tiles) % high) * BM;
-    const int64_t j0 = (int64_t)((tile - band * 8 * n_tiles) / high) * BN;
+    const uint32_t band = tile / (8 * m_tiles), first = band * 8, wide = n_tiles - first < 8 ? n_tiles - first : 8;
+    const int64_t i0 = (int64_t)((tile - band * 8 * m_tiles) / wide) * BM;
+    const int64_t j0 = (int64_t)(first + (tile - band * 8 * m_tiles) % wide) * BN;
 
     // rows past the last are the last one, so that every address is inside
     const int rows_a = (int)(p.m - i0 < BM ? p.m - i0 : BM), rows_b = (int)(p.n - j0 < BN ? p.n - j0 : BN);
@@ -176,18 +234,17 @@ __global__ __launch_bounds__(WM * WN * 64, BM * BN > 16384 ? 1 : 2) void mx_tile
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                                                        \
         __builtin_amdgcn_sched_group_barrier(0x008, MT * NT / (MT + NT), 0);                                      \
     }
-    const uint32_t chunks = (uint32_t)p.chunks, begin = part * (uint32_t)p.chunks_each;
-    const uint32_t end = begin + (uint32_t)p.chunks_each < chunks ? begin + (uint32_t)p.chunks_each : chunks;
-    load(0, begin);
-    if (begin + 1 < end) {
-        load(kStage, begin + 1);
+    const uint32_t end = (uint32_t)p.chunks;
+    load(0, 0);
+    if (end > 1) {
+        load(kStage, 1);
         asm volatile("s_waitcnt vmcnt(%0)" :: "n"(kLoadsA + kLoadsB) : "memory");   // the first stage's are older
     } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     uint32_t stage = 0;
     read(stage, 0, 0);
     read_scales(stage, sa, sb);
-    for (uint32_t k = begin; k < end; ++k) {
+    for (uint32_t k = 0; k < end; ++k) {
         read(stage, 1, 1);
         FH_QUARTER(0, 0)
         read(stage, 2, 0);
@@ -213,7 +270,7 @@ __global__ __launch_bounds__(WM * WN * 64, BM * BN > 16384 ? 1 : 2) void mx_tile
 
     // Out by rows: 32 rows of the wave's columns at a time through LDS, then whole runs of 16 bytes a lane.
     float* s_out = reinterpret_cast<float*>(s_stage + wave * 32 * kRow);
-    T* out = static_cast<T*>(p.out) + (p.parts > 1 ? (int64_t)part * p.m * p.n : 0);
+    T* out = static_cast<T*>(p.out);
     constexpr int kRun = 16 / sizeof(T), kLanes = NT * 32 / kRun, kRows = 64 / kLanes;
     const int64_t col = j0 + wn * NT * 32 + (lane % kLanes) * kRun;
     float bias[kRun];
@@ -266,50 +323,71 @@ __global__ __launch_bounds__(256) void mx_join_kernel(const float* parts, int64_
 }
 
 // ---- which kernel -------------------------------------------------------------------------------
-struct Plan { int32_t tile; int32_t parts; int64_t chunks_each; };      // tile: 0 few rows, else BM = BN
+enum class Tile : int32_t { waves32, waves32_wide, waves64, square128, square256 };
+struct Plan { Tile tile; int32_t parts; int64_t chunks_each; };
+
+// Times in us (m x n x k, bf16 out), each kernel's against the next best:
+//   32 x 32 outputs a workgroup: up to three workgroups a compute unit.  1024 x 768 x 768 3.7 (64 x 64: 4.6), 700 x 700 x 8192 9.1 (11.5);
+//       1024^3 4.5 (4.8), 2048 x 768 x 768 5.9 (5.3).  Eight waves each while there is at most one a compute unit and every
+//       wave has a chunk: 300 x 300 x 8192 5.8 (four waves: 7.1), 700 x 700 x 8192 10.1 (9.1).
+//   64 x 64, four waves: up to about two a compute unit.  512 x 4096 x 4096 11.3 (128: 15.0), 2304 x 768 x 8192 19.5 (24.9),
+//       1500 x 1500 x 8192 24.0 (25.7); 4096 x 768 x 768 9.5 (7.1).
+//   256 against 128: a round of 256 workgroups takes about 10.4 + 1.82 us a chunk with the one, of 512 (two a compute unit) 5.6 + 0.99 with
+//       the other.  8192 x 8192 x 4096 156 (183), 4096 x 4096 x 1024 17.7 (19.2); 8192 x 2304 x 768 26.1 (20.2).
+// A sum is split over workgroups where its outputs leave compute units idle, in parts of sixteen chunks at least.
 Plan plan_of(int64_t m, int64_t n, int64_t k)
 {
-    const int64_t chunks = mx_chunks(k);
-    if (m <= 32 || n <= 32 || chunks == 0) return Plan{0, 1, chunks};
-    const int64_t large = ((m + 255) / 256) * ((n + 255) / 256);
-    if (large >= 256) return Plan{256, 1, chunks};
-    const int64_t tiles = ((m + 127) / 128) * ((n + 127) / 128);
-    int64_t parts = 512 / tiles;
-    if (parts > chunks / 2) parts = chunks / 2;
-    if (parts < 1) parts = 1;
-    const int64_t each = (chunks + parts - 1) / parts;
-    return Plan{128, (int32_t)((chunks + each - 1) / each), each};
+    const auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
+    const int64_t chunks = mx_chunks(k), small = tiles(32);
+    if (small <= 128 && chunks >= 32) {
+        int64_t parts = 256 / small;
+        if (parts > chunks / 16) parts = chunks / 16;
+        const int64_t each = (chunks + parts - 1) / parts;
+        return Plan{Tile::waves32_wide, (int32_t)((chunks + each - 1) / each), each};
+    }
+    if (small <= 256 && chunks >= 8) return Plan{Tile::waves32_wide, 1, chunks};
+    if (small <= 768) return Plan{Tile::waves32, 1, chunks};
+    if (tiles(64) <= 576) return Plan{Tile::waves64, 1, chunks};
+    const int64_t large = 2 * ((tiles(256) + 255) / 256) * (104 + 18 * chunks), middle = (tiles(128) + 255) / 256 * (56 + 10 * chunks);
+    return Plan{large < middle ? Tile::square256 : Tile::square128, 1, chunks};
 }
 
-template <typename T>
-hipError_t few_rows_of(ProductArgs p, hipStream_t s)
+template <typename T, int MT, int NT, int WAVES>
+hipError_t waves_of(ProductArgs p, hipStream_t s)
 {
-    const int64_t n_tiles = (p.n + 15) / 16, tiles = n_tiles * ((p.m + 15) / 16);
-    if (tiles > INT32_MAX) return hipErrorInvalidValue;
-    p.n_tiles = (uint32_t)n_tiles;
-    hipLaunchKernelGGL((mx_few_rows_kernel<T, 4>), dim3((uint32_t)tiles), dim3(256), 0, s, p);
-    return hipGetLastError();
-}
-template <typename T, int B>
-hipError_t tiles_of(ProductArgs p, hipStream_t s)
-{
-    const int64_t m_tiles = (p.m + B - 1) / B, n_tiles = (p.n + B - 1) / B, groups = m_tiles * n_tiles * p.parts;
-    if (groups > INT32_MAX || m_tiles * n_tiles * 8 > INT32_MAX) return hipErrorInvalidValue;
+    const int64_t m_tiles = (p.m + MT * 32 - 1) / (MT * 32), n_tiles = (p.n + NT * 32 - 1) / (NT * 32), groups = m_tiles * n_tiles * p.parts;
+    if (groups > INT32_MAX) return hipErrorInvalidValue;
     p.m_tiles = (uint32_t)m_tiles;
     p.n_tiles = (uint32_t)n_tiles;
-    hipLaunchKernelGGL((mx_tile_kernel<T, B, B, 2, 2>), dim3((uint32_t)groups), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((mx_waves_kernel<T, MT, NT, WAVES>), dim3((uint32_t)groups), dim3(WAVES * 64), 0, s, p);
+    return hipGetLastError();
+}
+template <typename T, int B, int WN>
+hipError_t squares_of(ProductArgs p, hipStream_t s)
+{
+    const int64_t m_tiles = (p.m + B - 1) / B, n_tiles = (p.n + B - 1) / B;
+    if (m_tiles * n_tiles * 8 > INT32_MAX) return hipErrorInvalidValue;
+    p.m_tiles = (uint32_t)m_tiles;
+    p.n_tiles = (uint32_t)n_tiles;
+    hipLaunchKernelGGL((mx_tile_kernel<T, B, B, 2, WN>), dim3((uint32_t)(m_tiles * n_tiles)), dim3(2 * WN * 64), 0, s, p);
     return hipGetLastError();
 }
 template <typename T>
 hipError_t product_of(const ProductArgs& p, const Plan& plan, float* workspace, hipStream_t s)
 {
-    if (plan.tile == 0) return few_rows_of<T>(p, s);
-    if (plan.parts == 1) return plan.tile == 256 ? tiles_of<T, 256>(p, s) : tiles_of<T, 128>(p, s);
+    switch (plan.tile) {
+        case Tile::square256: return squares_of<T, 256, 4>(p, s);
+        case Tile::square128: return squares_of<T, 128, 2>(p, s);
+        case Tile::waves64: return waves_of<T, 2, 2, 4>(p, s);
+        case Tile::waves32: return waves_of<T, 1, 1, 4>(p, s);
+        case Tile::waves32_wide: break;
+    }
+    if (plan.parts == 1) return waves_of<T, 1, 1, 8>(p, s);
     ProductArgs q = p;
     q.out = workspace;
     q.stride = p.n;
     q.bias = nullptr;
-    const hipError_t e = plan.tile == 256 ? tiles_of<float, 256>(q, s) : tiles_of<float, 128>(q, s);
+    const hipError_t e = waves_of<float, 1, 1, 8>(q, s);
     if (e != hipSuccess) return e;
     const int64_t runs = (p.n + 3) / 4, groups = (p.m * runs + 255) / 256;
     hipLaunchKernelGGL((mx_join_kernel<T>), dim3((uint32_t)groups), dim3(256), 0, s, workspace, p.m, p.n, p.parts, p.bias, p.bias_dtype,
