@@ -572,6 +572,48 @@ typedef struct fh_norm_backward {
 size_t    fh_layer_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
 fh_status fh_layer_norm_backward(const fh_norm_backward *norm, void *stream);
 
+/* ---- a linear layer's training step, each half by one call -------------------------------------
+ * y = x W^T + bias, or norm(x) W^T + bias, with fh_mx_matmul's products, and its gradients: the
+ * calls above in this order, and the same results:
+ *   forward   fh_layer_norm_mx (norm = 1) or fh_mx_quantize of x, by rows and (NEEDS_WEIGHT) by columns;
+ *             fh_mx_quantize of weight, by rows and (NEEDS_INPUT) by columns; fh_mx_matmul: y;
+ *   backward  fh_mx_quantize of dy (rounding, seed, tensor_id) by rows (NEEDS_INPUT) and by columns
+ *             (NEEDS_WEIGHT); fh_mx_matmul: dweight = dy^T x; fh_mx_matmul: dx = dy W, rounded to
+ *             dtype; with a norm fh_layer_norm_backward of that in place (dnorm_weight, dnorm_bias
+ *             may be NULL).
+ * x is tokens x features and weight out_features x features, rows contiguous with row strides; dy
+ * tokens x out_features with a row stride; y, dx and dweight are dense.  x, y, dy and dx are of dtype, the
+ * norm's parameters, weight, bias and their gradients of p_dtype; norm_weight, norm_bias and bias may
+ * be NULL.  `kept` (fh_mx_layer_kept_bytes) carries the statistics and the operands by columns from
+ * the forward to the backward call and may be NULL where there is neither a norm nor a need; `scratch`
+ * (fh_mx_layer_scratch_bytes) is free again once a call's work has run.  Both 16-byte aligned.
+ * The backward call takes the same needs as the forward one had, or fewer.  1 <= features,
+ * out_features <= 2^24, tokens <= 2^24; tokens = 0 writes zeros to the gradients of the parameters.
+ * Everything is checked before the first launch. */
+#define FH_MX_NEEDS_INPUT  1                    /* the gradients of x and of the norm's parameters */
+#define FH_MX_NEEDS_WEIGHT 2                    /* the gradient of weight */
+typedef struct fh_mx_layer {
+    int64_t     tokens, features, out_features;
+    int32_t     dtype, p_dtype;                 /* fh_dtype */
+    int32_t     norm, needs;                    /* 0 | 1; FH_MX_NEEDS_* */
+    int32_t     rounding;   float eps;          /* fh_round, of dy; the norm's */
+    uint64_t    seed, tensor_id;
+    const void *x;          int64_t x_stride;
+    const void *norm_weight, *norm_bias;
+    const void *weight;     int64_t weight_stride;
+    const void *bias;
+    void       *y;                              /* forward */
+    const void *dy;         int64_t dy_stride;  /* backward, as all that follow (dy_stride: >= out_features in both) */
+    void       *dx, *dweight, *dnorm_weight, *dnorm_bias;
+    void       *kept;       size_t kept_cap;
+    void       *scratch;    size_t scratch_cap;
+    int64_t     reserved;                       /* 0 */
+} fh_mx_layer;
+size_t    fh_mx_layer_kept_bytes(int64_t tokens, int64_t features, int64_t out_features);
+size_t    fh_mx_layer_scratch_bytes(int64_t tokens, int64_t features, int64_t out_features);
+fh_status fh_mx_layer_forward(const fh_mx_layer *layer, void *stream);
+fh_status fh_mx_layer_backward(const fh_mx_layer *layer, void *stream);
+
 const char *fh_status_string(fh_status s);
 
 #ifdef __cplusplus

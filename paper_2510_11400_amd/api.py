@@ -42,6 +42,7 @@ EXPORTS = ("fh_packed_bytes", "fh_meta_bytes", "fh_compress", "fh_decompress", "
            "fh_mix_layout", "fh_mix_compress", "fh_mix_decompress", "fh_mix_compress_batch", "fh_mix_decompress_batch",
            "fh_mx_bytes", "fh_mx_scales_offset", "fh_mx_quantize", "fh_mx_dequantize", "fh_mx_matmul_workspace_bytes", "fh_mx_matmul",
            "fh_layer_norm", "fh_layer_norm_mx", "fh_layer_norm_backward_workspace_bytes", "fh_layer_norm_backward",
+           "fh_mx_layer_kept_bytes", "fh_mx_layer_scratch_bytes", "fh_mx_layer_forward", "fh_mx_layer_backward",
            "fh_status_string")
 
 
@@ -271,6 +272,24 @@ class fh_norm_backward(ctypes.Structure):
                 ("workspace", ctypes.c_void_p), ("workspace_cap", ctypes.c_size_t)]
 
 
+class fh_mx_layer(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("features", ctypes.c_int64), ("out_features", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("p_dtype", ctypes.c_int32), ("norm", ctypes.c_int32), ("needs", ctypes.c_int32),
+                ("rounding", ctypes.c_int32), ("eps", ctypes.c_float), ("seed", ctypes.c_uint64), ("tensor_id", ctypes.c_uint64),
+                ("x", ctypes.c_void_p), ("x_stride", ctypes.c_int64), ("norm_weight", ctypes.c_void_p), ("norm_bias", ctypes.c_void_p),
+                ("weight", ctypes.c_void_p), ("weight_stride", ctypes.c_int64), ("bias", ctypes.c_void_p), ("y", ctypes.c_void_p),
+                ("dy", ctypes.c_void_p), ("dy_stride", ctypes.c_int64), ("dx", ctypes.c_void_p), ("dweight", ctypes.c_void_p),
+                ("dnorm_weight", ctypes.c_void_p), ("dnorm_bias", ctypes.c_void_p),
+                ("kept", ctypes.c_void_p), ("kept_cap", ctypes.c_size_t), ("scratch", ctypes.c_void_p), ("scratch_cap", ctypes.c_size_t),
+                ("reserved", ctypes.c_int64)]
+
+
+for _name in ("fh_mx_layer_kept_bytes", "fh_mx_layer_scratch_bytes"):
+    getattr(_lib, _name).argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64]
+    getattr(_lib, _name).restype = ctypes.c_size_t
+for _name in ("fh_mx_layer_forward", "fh_mx_layer_backward"):
+    getattr(_lib, _name).argtypes = [_P(fh_mx_layer), ctypes.c_void_p]
+    getattr(_lib, _name).restype = ctypes.c_int
 for _name in ("fh_mx_bytes", "fh_mx_scales_offset", "fh_layer_norm_backward_workspace_bytes"):
     getattr(_lib, _name).argtypes = [ctypes.c_int64, ctypes.c_int64]
     getattr(_lib, _name).restype = ctypes.c_size_t
@@ -1313,11 +1332,16 @@ class MxMatrix:
         return self.data.numel()
 
 
+_current_device = torch._C._cuda_getDevice
+_current_stream = torch._C._cuda_getCurrentRawStream
+_MASK64 = 0xFFFFFFFFFFFFFFFF
+
+
 def _enqueue(device, stream: Optional[torch.cuda.Stream], call, *args) -> None:
     """call(*args, stream's handle) with `device` the current one."""
-    index = torch._C._cuda_getDevice()
+    index = _current_device()
     if device.index == index:
-        status = call(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream)
+        status = call(*args, _current_stream(index) if stream is None else stream.cuda_stream)
     else:
         with torch.cuda.device(device):
             status = call(*args, _stream_ptr(stream))
@@ -1348,49 +1372,40 @@ def _matrix(t: torch.Tensor, what: str):
 
 
 def _vector(t: Optional[torch.Tensor], n: int, device, what: str) -> Optional[int]:
+    """The address of a vector of n values, None for none."""
     if t is None:
         return None
-    _on_device(_device_tensor(t, what), device, what)
-    if t.dim() != 1 or t.shape[0] != n:
+    if t.device != device or t.shape != (n,) or not t.is_contiguous():
+        _on_device(_device_tensor(t, what), device, what)
         raise ValueError(f"{what} must be a vector of {n} values")
     return t.data_ptr()
 
 
 def _parameters(weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], cols: int, device):
     """(weight's pointer, bias's pointer, their dtype code)"""
-    if weight is None and bias is None:
-        return None, None, FH_F32
-    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+    if weight is None:
+        return (None, None, FH_F32) if bias is None else (None, _vector(bias, cols, device, "bias"), _dtype_code(bias))
+    if bias is not None and weight.dtype != bias.dtype:
         raise TypeError(f"weight and bias have different dtypes ({weight.dtype}, {bias.dtype})")
-    return (_vector(weight, cols, device, "weight"), _vector(bias, cols, device, "bias"),
-            _dtype_code(weight if weight is not None else bias))
+    return _vector(weight, cols, device, "weight"), _vector(bias, cols, device, "bias"), _dtype_code(weight)
 
 
-_FORMS = ("rows", "columns", "both")
+def _new_store(rows: int, cols: int, device) -> MxMatrix:
+    return MxMatrix(torch.empty(mx_bytes(rows, cols), dtype=torch.uint8, device=device), rows, cols)
 
 
 def _stores(forms: str, rows: int, cols: int, device):
-    """Buffers of the forms that are asked for: (by rows, by columns), None for one that is not."""
-    if forms not in _FORMS:
-        raise ValueError(f"forms must be one of {_FORMS} (got {forms!r})")
-    by_rows = by_columns = None
-    if forms != "columns":
-        by_rows = MxMatrix(torch.empty(mx_bytes(rows, cols), dtype=torch.uint8, device=device), rows, cols)
-    if forms != "rows":
-        by_columns = MxMatrix(torch.empty(mx_bytes(cols, rows), dtype=torch.uint8, device=device), cols, rows)
-    return by_rows, by_columns
-
-
-def _store_args(m: Optional[MxMatrix]):
-    return (None, 0) if m is None else (m.data.data_ptr(), m.data.numel())
-
-
-def _asked(forms: str, by_rows, by_columns):
-    return by_rows if forms == "rows" else by_columns if forms == "columns" else (by_rows, by_columns)
-
-
-def _u64(v: int) -> int:
-    return int(v) & 0xFFFFFFFFFFFFFFFF
+    """(what a call returns, by rows: address, bytes, by columns: address, bytes) with new buffers for the forms asked for."""
+    if forms == "rows":
+        m = _new_store(rows, cols, device)
+        return m, m.data.data_ptr(), m.data.numel(), None, 0
+    if forms == "columns":
+        m = _new_store(cols, rows, device)
+        return m, None, 0, m.data.data_ptr(), m.data.numel()
+    if forms == "both":
+        m, t = _new_store(rows, cols, device), _new_store(cols, rows, device)
+        return (m, t), m.data.data_ptr(), m.data.numel(), t.data.data_ptr(), t.data.numel()
+    raise ValueError(f"forms must be 'rows', 'columns' or 'both' (got {forms!r})")
 
 
 def fh_mx_quantize(x: torch.Tensor, forms: str = "rows", rounding="nearest", seed: int = 0, tensor_id: int = 0, stream=None):
@@ -1398,25 +1413,30 @@ def fh_mx_quantize(x: torch.Tensor, forms: str = "rows", rounding="nearest", see
     with blocks of 32 values along its rows, "columns" one of x transposed (blocks along x's columns), "both" the two."""
     rows, cols, stride = _matrix(x, "x")
     device = x.device
-    by_rows, by_columns = _stores(forms, rows, cols, device)
-    _enqueue(device, stream, _lib.fh_mx_quantize, x.data_ptr(), _dtype_code(x), rows, cols, stride, _ROUND[rounding], _u64(seed),
-             _u64(tensor_id), *_store_args(by_rows), *_store_args(by_columns))
-    return _asked(forms, by_rows, by_columns)
+    kept, a, a_bytes, b, b_bytes = _stores(forms, rows, cols, device)
+    _enqueue(device, stream, _lib.fh_mx_quantize, x.data_ptr(), _dtype_code(x), rows, cols, stride, _ROUND[rounding],
+             seed & _MASK64, tensor_id & _MASK64, a, a_bytes, b, b_bytes)
+    return kept
 
 
 def _stored(m: MxMatrix, what: str) -> torch.Tensor:
-    t = _device_tensor(m.data, what)
-    if t.dtype != torch.uint8:
+    t = m.data
+    if not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous():
+        _device_tensor(t, what)
         raise TypeError(f"{what} holds {t.dtype}, a stored matrix bytes")
     return t
+
+
+def _new(rows: int, cols: int, dtype, device) -> torch.Tensor:
+    return torch.empty((rows, cols), dtype=dtype, device=device)
 
 
 def fh_mx_dequantize(m: MxMatrix, out_dtype=torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Enqueue the restoration of a stored matrix; returns it as [rows, cols]."""
     data = _stored(m, "the stored matrix")
-    device, rows, cols, stride = data.device, m.rows, m.cols, m.cols
+    device, rows, cols = data.device, m.rows, m.cols
     if out is None:
-        out = torch.empty((rows, cols), dtype=out_dtype, device=device)
+        out, stride = _new(rows, cols, out_dtype, device), cols
     else:
         out_rows, out_cols, stride = _matrix(out, "out")
         if (out_rows, out_cols) != (rows, cols):
@@ -1429,7 +1449,7 @@ def fh_mx_dequantize(m: MxMatrix, out_dtype=torch.float32, out: Optional[torch.T
 
 
 def mx_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
-    return int(_lib.fh_mx_matmul_workspace_bytes(m, n, k))
+    return _lib.fh_mx_matmul_workspace_bytes(m, n, k)
 
 
 def fh_mx_matmul(a: MxMatrix, b: MxMatrix, bias: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
@@ -1439,10 +1459,10 @@ def fh_mx_matmul(a: MxMatrix, b: MxMatrix, bias: Optional[torch.Tensor] = None, 
     m, n, k = a.rows, b.rows, a.cols
     if b.cols != k:
         raise ValueError(f"a has {k} columns, b {b.cols}")
-    device, stride = da.device, n
+    device = da.device
     _on_device(db, device, "b")
     if out is None:
-        out = torch.empty((m, n), dtype=out_dtype, device=device)
+        out, stride = _new(m, n, out_dtype, device), n
     else:
         rows, cols, stride = _matrix(out, "out")
         if (rows, cols) != (m, n):
@@ -1465,7 +1485,7 @@ def fh_mx_matmul(a: MxMatrix, b: MxMatrix, bias: Optional[torch.Tensor] = None, 
 def _like(t: Optional[torch.Tensor], x: torch.Tensor, rows: int, cols: int, what: str):
     """(t, its row stride), or a new matrix like x."""
     if t is None:
-        return torch.empty((rows, cols), dtype=x.dtype, device=x.device), cols
+        return _new(rows, cols, x.dtype, x.device), cols
     t_rows, t_cols, stride = _matrix(t, what)
     if (t_rows, t_cols) != (rows, cols) or t.dtype != x.dtype:
         raise ValueError(f"{what} must have the shape and the dtype of x")
@@ -1481,7 +1501,7 @@ def fh_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: 
     w, b, p_dtype = _parameters(weight, bias, cols, device)
     out, out_stride = _like(out, x, rows, cols, "out")
     mean = torch.empty(rows, dtype=torch.float32, device=device)
-    rstd = torch.empty(rows, dtype=torch.float32, device=device)
+    rstd = torch.empty_like(mean)
     _enqueue(device, stream, _lib.fh_layer_norm, x.data_ptr(), _dtype_code(x), rows, cols, stride, w, b, p_dtype, eps,
              out.data_ptr(), out_stride, ((rows - 1) * out_stride + cols) * out.element_size() if rows else 0,
              mean.data_ptr(), rstd.data_ptr())
@@ -1495,13 +1515,13 @@ def fh_layer_norm_mx(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bia
     rows, cols, stride = _matrix(x, "x")
     device = x.device
     w, b, p_dtype = _parameters(weight, bias, cols, device)
-    by_rows, by_columns = _stores(forms, rows, cols, device)
+    kept, by_rows, rows_bytes, by_columns, columns_bytes = _stores(forms, rows, cols, device)
     mean = torch.empty(rows, dtype=torch.float32, device=device)
-    rstd = torch.empty(rows, dtype=torch.float32, device=device)
+    rstd = torch.empty_like(mean)
     _enqueue(device, stream, _lib.fh_layer_norm_mx, x.data_ptr(), _dtype_code(x), rows, cols, stride, w, b, p_dtype, eps,
-             _ROUND[rounding], _u64(seed), _u64(tensor_id), *_store_args(by_rows), *_store_args(by_columns),
+             _ROUND[rounding], seed & _MASK64, tensor_id & _MASK64, by_rows, rows_bytes, by_columns, columns_bytes,
              mean.data_ptr(), rstd.data_ptr())
-    return _asked(forms, by_rows, by_columns), mean, rstd
+    return kept, mean, rstd
 
 
 def fh_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
@@ -1510,9 +1530,9 @@ def fh_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor
     """Enqueue the backward pass of fh_layer_norm; returns (dx, dweight, dbias), the last two (None unless `sums`) in the
     weight's dtype, in x's where there is no weight."""
     rows, cols, x_stride = _matrix(x, "x")
-    device = x.device
+    device, dtype = x.device, x.dtype
     dy_rows, dy_cols, dy_stride = _matrix(dy, "dy")
-    if dy_rows != rows or dy_cols != cols or dy.dtype != x.dtype:
+    if dy_rows != rows or dy_cols != cols or dy.dtype != dtype:
         raise ValueError("dy must have the shape and the dtype of x")
     _on_device(dy, device, "dy")
     if mean.dtype != torch.float32 or rstd.dtype != torch.float32:
@@ -1525,7 +1545,7 @@ def fh_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor
         _on_device(_device_tensor(workspace, "workspace"), device, "workspace")
     if sums:
         dweight = torch.empty(cols, dtype=like.dtype, device=device)
-        dbias = torch.empty(cols, dtype=like.dtype, device=device)
+        dbias = torch.empty_like(dweight)
         dweight_ptr, dbias_ptr = dweight.data_ptr(), dbias.data_ptr()
         if workspace is None:
             workspace = _scratch(_lib.fh_layer_norm_backward_workspace_bytes(rows, cols), device, stream)
@@ -1537,3 +1557,83 @@ def fh_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor
                          dweight_ptr, dbias_ptr, work, work_bytes)
     _enqueue(device, stream, _lib.fh_layer_norm_backward, ctypes.byref(p))
     return dx, dweight, dbias
+
+
+FH_MX_NEEDS_INPUT, FH_MX_NEEDS_WEIGHT = 1, 2
+
+
+class MxLayer:
+    """One pass through a linear layer in microscaled form: what its forward call keeps for its backward call.  x: [tokens,
+    features], weight: [out, features]; `norm`: a layer norm ahead, with norm_weight and norm_bias (either may be None).  Parameters
+    are of one dtype, and so are x, y and the gradients of both."""
+    __slots__ = ("args", "kept", "device", "dtype", "p_dtype")
+
+    def __init__(self, x: torch.Tensor, weight: torch.Tensor, bias=None, norm: bool = False, norm_weight=None, norm_bias=None,
+                 eps: float = 1e-5, needs_input: bool = True, needs_weight: bool = True, rounding="nearest", seed: int = 0,
+                 tensor_id: int = 0):
+        tokens, features, x_stride = _matrix(x, "x")
+        out, w_features, w_stride = _matrix(weight, "weight")
+        if w_features != features:
+            raise ValueError(f"x has {features} features, weight takes {w_features}")
+        device = self.device = x.device
+        _on_device(weight, device, "weight")
+        self.dtype, self.p_dtype = x.dtype, weight.dtype
+        for t, what in ((bias, "bias"), (norm_weight, "norm_weight"), (norm_bias, "norm_bias")):
+            if t is not None and t.dtype != weight.dtype:
+                raise TypeError(f"{what} is of {t.dtype}, weight of {weight.dtype}")
+        self.kept = None
+        self.args = fh_mx_layer(tokens, features, out, _dtype_code(x), _dtype_code(weight), 1 if norm else 0,
+                                (FH_MX_NEEDS_INPUT if needs_input else 0) | (FH_MX_NEEDS_WEIGHT if needs_weight else 0),
+                                _ROUND[rounding], eps, seed & _MASK64, tensor_id & _MASK64, x.data_ptr(), x_stride,
+                                _vector(norm_weight, features, device, "norm_weight"), _vector(norm_bias, features, device, "norm_bias"),
+                                weight.data_ptr(), w_stride, _vector(bias, out, device, "bias"), None, None, out)
+
+    def _work(self, stream) -> torch.Tensor:
+        a = self.args
+        scratch = _scratch(_lib.fh_mx_layer_scratch_bytes(a.tokens, a.features, a.out_features), self.device, stream)
+        a.scratch, a.scratch_cap = scratch.data_ptr(), scratch.numel()
+        return scratch
+
+    def forward(self, stream=None) -> torch.Tensor:
+        """Enqueue the forward half; returns y."""
+        a = self.args
+        y = _new(a.tokens, a.out_features, self.dtype, self.device)
+        if a.norm or a.needs:
+            self.kept = torch.empty(_lib.fh_mx_layer_kept_bytes(a.tokens, a.features, a.out_features), dtype=torch.uint8, device=self.device)
+            a.kept, a.kept_cap = self.kept.data_ptr(), self.kept.numel()
+        scratch = self._work(stream)  # noqa: F841  (held until the call has been enqueued)
+        a.y = y.data_ptr()
+        _enqueue(self.device, stream, _lib.fh_mx_layer_forward, ctypes.byref(a))
+        return y
+
+    def backward(self, dy: torch.Tensor, x: Optional[torch.Tensor] = None, norm_weight: Optional[torch.Tensor] = None, stream=None):
+        """Enqueue the backward half; returns (dx, dweight, dnorm_weight, dnorm_bias), None for what is not needed.  With a norm x
+        and norm_weight are the forward call's (x may have moved, as a saved tensor that was restored has)."""
+        a = self.args
+        tokens, out, a.dy_stride = _matrix(dy, "dy")
+        device, p_dtype, features = self.device, self.p_dtype, a.features
+        if (tokens, out) != (a.tokens, a.out_features) or dy.dtype != self.dtype:
+            raise ValueError("dy must have the shape and the dtype of y")
+        _on_device(dy, device, "dy")
+        dx = dweight = dnorm_weight = dnorm_bias = None
+        if a.needs & FH_MX_NEEDS_WEIGHT:
+            dweight = _new(out, features, p_dtype, device)
+            a.dweight = dweight.data_ptr()
+        if a.needs & FH_MX_NEEDS_INPUT:
+            dx = _new(tokens, features, self.dtype, device)
+            a.dx = dx.data_ptr()
+            if a.norm:
+                if x is None:
+                    raise ValueError("with a norm the backward call takes x again")
+                x_rows, x_cols, a.x_stride = _matrix(x, "x")
+                if (x_rows, x_cols) != (tokens, features) or x.dtype != self.dtype:
+                    raise ValueError("x must have the shape and the dtype of the forward call's")
+                _on_device(x, device, "x")
+                dnorm_weight = torch.empty(features, dtype=p_dtype, device=device)
+                dnorm_bias = torch.empty_like(dnorm_weight)
+                a.x, a.norm_weight = x.data_ptr(), _vector(norm_weight, features, device, "norm_weight")
+                a.dnorm_weight, a.dnorm_bias = dnorm_weight.data_ptr(), dnorm_bias.data_ptr()
+        scratch = self._work(stream)  # noqa: F841
+        a.dy = dy.data_ptr()
+        _enqueue(device, stream, _lib.fh_mx_layer_backward, ctypes.byref(a))
+        return dx, dweight, dnorm_weight, dnorm_bias

@@ -16,7 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libfedhybrid.so")
 SOURCES = ("fh_abi.hip", "fh_compress.hip", "fh_decompress.hip", "fh_classify.hip", "fh_mixed.hip", "fh_sparse.hip",
-           "fh_huffman.hip", "fh_chain.hip", "fh_mx_quantize.hip", "fh_mx_matmul.hip", "fh_layer_norm.hip")
+           "fh_huffman.hip", "fh_chain.hip", "fh_mx_quantize.hip", "fh_mx_matmul.hip", "fh_layer_norm.hip",
+           "fh_mx_layer.hip")
 
 # Strict binary32 semantics on the device: no contraction (the one fused multiply-add
 # of the method is written explicitly), IEEE division, denormals kept.  Packed-fp32

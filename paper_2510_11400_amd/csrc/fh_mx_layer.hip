@@ -1,0 +1,149 @@
+// A linear layer's training step in microscaled form, each half by one call: an optional layer norm, the operands' storage and the
+// products, with everything in between in two buffers of the caller's.
+#include "fh_norm.hpp"
+
+namespace fh {
+namespace {
+
+inline size_t whole(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+inline size_t larger(size_t a, size_t b) { return a > b ? a : b; }
+
+// Offsets into the two buffers.  kept: from the forward call until the backward one; scratch: within a call.
+struct Parts {
+    size_t mean, rstd, x_columns, w_columns, kept;
+    size_t x_rows, w_rows, forward_work, forward;
+    size_t dy_rows, dy_columns, backward_work, backward;
+};
+Parts parts_of(int64_t tokens, int64_t features, int64_t out)
+{
+    Parts p;
+    p.mean = 0;
+    p.rstd = whole((size_t)tokens * 4);
+    p.x_columns = p.rstd + whole((size_t)tokens * 4);
+    p.w_columns = p.x_columns + whole(mx_bytes(features, tokens));
+    p.kept = p.w_columns + whole(mx_bytes(features, out));
+    p.x_rows = 0;
+    p.w_rows = whole(mx_bytes(tokens, features));
+    p.forward_work = p.w_rows + whole(mx_bytes(out, features));
+    p.forward = p.forward_work + whole(fh_mx_matmul_workspace_bytes(tokens, out, features));
+    p.dy_rows = 0;
+    p.dy_columns = whole(mx_bytes(tokens, out));
+    p.backward_work = p.dy_columns + whole(mx_bytes(out, tokens));
+    p.backward = p.backward_work + whole(larger(larger(fh_mx_matmul_workspace_bytes(tokens, features, out), fh_mx_matmul_workspace_bytes(out, features, tokens)),
+                                                fh_layer_norm_backward_workspace_bytes(tokens, features)));
+    return p;
+}
+
+bool shape_ok(int64_t tokens, int64_t features, int64_t out)
+{
+    constexpr int64_t kMostSummed = (int64_t)1 << 24;             // each of the three is summed over by one of the products
+    return tokens >= 0 && features >= 1 && out >= 1 && tokens <= kMostSummed && features <= kMostSummed && out <= kMostSummed;
+}
+
+fh_status check(const fh_mx_layer* l)
+{
+    if (!l) return FH_ERR_NULL;
+    if (!is_dtype(l->dtype) || !is_dtype(l->p_dtype)) return FH_ERR_BAD_DTYPE;
+    if (l->rounding != FH_ROUND_NEAREST && l->rounding != FH_ROUND_STOCHASTIC) return FH_ERR_BAD_ROUND;
+    if (!shape_ok(l->tokens, l->features, l->out_features) || l->x_stride < l->features || l->weight_stride < l->features ||
+        l->dy_stride < l->out_features || l->x_stride > kMostStride || l->weight_stride > kMostStride || l->dy_stride > kMostStride)
+        return FH_ERR_BAD_SHAPE;
+    if (l->norm != 0 && l->norm != 1) return FH_ERR_BAD_PARAM;
+    if ((l->needs & ~(FH_MX_NEEDS_INPUT | FH_MX_NEEDS_WEIGHT)) != 0 || l->reserved != 0 || (l->norm && !(l->eps >= 0.0f))) return FH_ERR_BAD_PARAM;
+    return FH_OK;
+}
+
+uint8_t* at(void* p, size_t offset) { return static_cast<uint8_t*>(p) + offset; }
+
+}  // namespace
+}  // namespace fh
+
+extern "C" {
+
+size_t fh_mx_layer_kept_bytes(int64_t tokens, int64_t features, int64_t out_features)
+{
+    return fh::shape_ok(tokens, features, out_features) ? fh::parts_of(tokens, features, out_features).kept : 0;
+}
+
+size_t fh_mx_layer_scratch_bytes(int64_t tokens, int64_t features, int64_t out_features)
+{
+    if (!fh::shape_ok(tokens, features, out_features)) return 0;
+    const fh::Parts p = fh::parts_of(tokens, features, out_features);
+    return fh::larger(p.forward, p.backward);
+}
+
+fh_status fh_mx_layer_forward(const fh_mx_layer* l, void* stream)
+{
+    using namespace fh;
+    const fh_status ok = check(l);
+    if (ok != FH_OK || l->tokens == 0) return ok;
+    const Parts p = parts_of(l->tokens, l->features, l->out_features);
+    const size_t size = dtype_size(l->dtype), p_size = dtype_size(l->p_dtype);
+    const bool keeps = l->norm || l->needs;
+    if (!l->x || !l->weight || !l->y || !l->scratch || (keeps && !l->kept)) return FH_ERR_NULL;
+    if (!is_aligned(l->x, size) || !is_aligned(l->y, size) || !is_aligned(l->weight, p_size) || !is_aligned(l->bias, p_size) ||
+        !is_aligned(l->norm_weight, p_size) || !is_aligned(l->norm_bias, p_size) || !is_aligned(l->kept, 16) || !is_aligned(l->scratch, 16))
+        return FH_ERR_ALIGNMENT;
+    if (l->scratch_cap < p.forward || (keeps && l->kept_cap < p.kept)) return FH_ERR_BUFFER_TOO_SMALL;
+
+    const fh_dtype dtype = (fh_dtype)l->dtype, p_dtype = (fh_dtype)l->p_dtype;
+    uint8_t *x_rows = at(l->scratch, p.x_rows), *w_rows = at(l->scratch, p.w_rows);
+    uint8_t* x_columns = l->needs & FH_MX_NEEDS_WEIGHT ? at(l->kept, p.x_columns) : nullptr;
+    uint8_t* w_columns = l->needs & FH_MX_NEEDS_INPUT ? at(l->kept, p.w_columns) : nullptr;
+    const size_t x_bytes = mx_bytes(l->tokens, l->features), w_bytes = mx_bytes(l->out_features, l->features);
+    fh_status s;
+    if (l->norm)
+        s = fh_layer_norm_mx(l->x, dtype, l->tokens, l->features, l->x_stride, l->norm_weight, l->norm_bias, p_dtype, l->eps, FH_ROUND_NEAREST, 0, 0,
+                             x_rows, x_bytes, x_columns, mx_bytes(l->features, l->tokens), at(l->kept, p.mean), at(l->kept, p.rstd), stream);
+    else
+        s = fh_mx_quantize(l->x, dtype, l->tokens, l->features, l->x_stride, FH_ROUND_NEAREST, 0, 0, x_rows, x_bytes, x_columns,
+                           mx_bytes(l->features, l->tokens), stream);
+    if (s != FH_OK) return s;
+    s = fh_mx_quantize(l->weight, p_dtype, l->out_features, l->features, l->weight_stride, FH_ROUND_NEAREST, 0, 0, w_rows, w_bytes, w_columns,
+                       mx_bytes(l->features, l->out_features), stream);
+    if (s != FH_OK) return s;
+    const fh_mx_product y = {x_rows, x_bytes, w_rows, w_bytes, l->tokens, l->out_features, l->features, l->bias, l->p_dtype, l->dtype, l->y,
+                             l->out_features, (size_t)l->tokens * (size_t)l->out_features * size, at(l->scratch, p.forward_work),
+                             l->scratch_cap - p.forward_work, 0};
+    return fh_mx_matmul(&y, stream);
+}
+
+fh_status fh_mx_layer_backward(const fh_mx_layer* l, void* stream)
+{
+    using namespace fh;
+    const fh_status ok = check(l);
+    if (ok != FH_OK || !l->needs) return ok;
+    const Parts p = parts_of(l->tokens, l->features, l->out_features);
+    const size_t size = dtype_size(l->dtype), p_size = dtype_size(l->p_dtype);
+    const bool input = l->needs & FH_MX_NEEDS_INPUT, weight = l->needs & FH_MX_NEEDS_WEIGHT;
+    if (!l->kept || !l->scratch || (weight && !l->dweight)) return FH_ERR_NULL;
+    if (l->tokens > 0 && (!l->dy || (input && !l->dx) || (input && l->norm && !l->x))) return FH_ERR_NULL;
+    if (!is_aligned(l->x, size) || !is_aligned(l->dy, size) || !is_aligned(l->dx, size) || !is_aligned(l->dweight, p_size) ||
+        !is_aligned(l->norm_weight, p_size) || !is_aligned(l->dnorm_weight, p_size) || !is_aligned(l->dnorm_bias, p_size) ||
+        !is_aligned(l->kept, 16) || !is_aligned(l->scratch, 16)) return FH_ERR_ALIGNMENT;
+    if (l->scratch_cap < p.backward || l->kept_cap < p.kept) return FH_ERR_BUFFER_TOO_SMALL;
+
+    uint8_t *dy_rows = input ? at(l->scratch, p.dy_rows) : nullptr, *dy_columns = weight ? at(l->scratch, p.dy_columns) : nullptr;
+    const size_t rows_bytes = mx_bytes(l->tokens, l->out_features), columns_bytes = mx_bytes(l->out_features, l->tokens);
+    void* work = at(l->scratch, p.backward_work);
+    const size_t work_bytes = l->scratch_cap - p.backward_work;
+    fh_status s = fh_mx_quantize(l->dy, (fh_dtype)l->dtype, l->tokens, l->out_features, l->dy_stride, l->rounding, l->seed, l->tensor_id,
+                                 dy_rows, rows_bytes, dy_columns, columns_bytes, stream);
+    if (s != FH_OK) return s;
+    if (weight) {
+        const fh_mx_product dw = {dy_columns, columns_bytes, at(l->kept, p.x_columns), mx_bytes(l->features, l->tokens), l->out_features, l->features,
+                                  l->tokens, nullptr, l->p_dtype, l->p_dtype, l->dweight, l->features,
+                                  (size_t)l->out_features * (size_t)l->features * p_size, work, work_bytes, 0};
+        if ((s = fh_mx_matmul(&dw, stream)) != FH_OK) return s;
+    }
+    if (!input) return FH_OK;
+    const size_t dx_bytes = (size_t)l->tokens * (size_t)l->features * size;
+    const fh_mx_product dx = {dy_rows, rows_bytes, at(l->kept, p.w_columns), mx_bytes(l->features, l->out_features), l->tokens, l->features,
+                              l->out_features, nullptr, l->p_dtype, l->dtype, l->dx, l->features, dx_bytes, work, work_bytes, 0};
+    if ((s = fh_mx_matmul(&dx, stream)) != FH_OK || !l->norm) return s;
+    const fh_norm_backward n = {l->dx, l->x, l->features, l->x_stride, at(l->kept, p.mean), at(l->kept, p.rstd), l->norm_weight, l->tokens, l->features,
+                                l->dtype, l->p_dtype, l->dx, l->features, dx_bytes, l->dnorm_weight, l->dnorm_bias, work, work_bytes};
+    return fh_layer_norm_backward(&n, stream);
+}
+
+}  // extern "C"

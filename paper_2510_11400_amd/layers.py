@@ -21,58 +21,10 @@ from . import api
 
 
 def _rows(x: torch.Tensor) -> torch.Tensor:
-    """x as a matrix of its last dimension, its rows contiguous."""
-    m = x.reshape(-1, x.shape[-1])
-    return m if m.stride(1) == 1 or m.shape[1] <= 1 else m.contiguous()
-
-
-def _weight_gradients(dy, x_columns, weight_dtype, need_weight, need_bias, bias_dtype, dy_columns):
-    dw = api.fh_mx_matmul(dy_columns, x_columns, out_dtype=weight_dtype) if need_weight else None
-    db = dy.float().sum(0).to(bias_dtype) if need_bias else None
-    return dw, db
-
-
-class _Rounding:
-    """How a layer's gradients are quantised; a step's random numbers are those of its seed."""
-    __slots__ = ("mode", "seed", "tensor_id")
-
-    def __init__(self, mode, seed, tensor_id):
-        self.mode, self.seed, self.tensor_id = mode, seed, tensor_id
-
-
-def _quantised_gradient(dy, rounding: _Rounding, need_input: bool, need_weight: bool):
-    """(dy by rows, dy by columns), None for one that is not needed."""
-    if need_input and need_weight:
-        return api.fh_mx_quantize(dy, "both", rounding.mode, rounding.seed, rounding.tensor_id)
-    if need_input:
-        return api.fh_mx_quantize(dy, "rows", rounding.mode, rounding.seed, rounding.tensor_id), None
-    if need_weight:
-        return None, api.fh_mx_quantize(dy, "columns", rounding.mode, rounding.seed, rounding.tensor_id)
-    return None, None
-
-
-class _MxLinear(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, x, weight, bias, rounding):
-        m = _rows(x)
-        need_x, need_w = ctx.needs_input_grad[0], ctx.needs_input_grad[1]
-        x_rows, x_columns = api.fh_mx_quantize(m, "both") if need_w else (api.fh_mx_quantize(m, "rows"), None)
-        w_rows, w_columns = api.fh_mx_quantize(weight, "both") if need_x else (api.fh_mx_quantize(weight, "rows"), None)
-        y = api.fh_mx_matmul(x_rows, w_rows, bias, x.dtype)
-        ctx.kept, ctx.rounding = (x_columns, w_columns), rounding
-        ctx.shape, ctx.dtypes = x.shape, (weight.dtype, None if bias is None else bias.dtype)
-        return y.view(*x.shape[:-1], weight.shape[0])
-
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, dy):
-        need_x, need_w, need_b = ctx.needs_input_grad[:3]
-        x_columns, w_columns = ctx.kept
-        g = _rows(dy)
-        g_rows, g_columns = _quantised_gradient(g, ctx.rounding, need_x, need_w)
-        dx = api.fh_mx_matmul(g_rows, w_columns, out_dtype=dy.dtype).view(ctx.shape) if need_x else None
-        dw, db = _weight_gradients(g, x_columns, ctx.dtypes[0], need_w, need_b, ctx.dtypes[1], g_columns)
-        return dx, dw, db, None
+    """x as a matrix of its last dimension, its rows contiguous and apart (an expanded gradient's are not)."""
+    m = x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
+    stride, step = m.stride()
+    return m if step == 1 and stride >= m.shape[1] else m.contiguous()
 
 
 class _LayerNorm(torch.autograd.Function):
@@ -81,7 +33,6 @@ class _LayerNorm(torch.autograd.Function):
         m = _rows(x)
         y, mean, rstd = api.fh_layer_norm(m, weight, bias, eps)
         ctx.save_for_backward(m, mean, rstd, weight)
-        ctx.has_bias = bias is not None
         return y.view(x.shape)
 
     @staticmethod
@@ -93,37 +44,32 @@ class _LayerNorm(torch.autograd.Function):
                 db if ctx.needs_input_grad[2] else None, None)
 
 
-class _LayerNormMxLinear(torch.autograd.Function):
+class _MxLinear(torch.autograd.Function):
+    """norm(x) W^T + b, the norm left out where `norm` is None, else its eps."""
+
     @staticmethod
-    def forward(ctx, x, norm_weight, norm_bias, weight, bias, eps, rounding):
-        m = _rows(x)
-        need_norm, need_w = any(ctx.needs_input_grad[:3]), ctx.needs_input_grad[3]
-        h, mean, rstd = api.fh_layer_norm_mx(m, norm_weight, norm_bias, eps, "both" if need_w else "rows")
-        h_rows, h_columns = h if need_w else (h, None)
-        w_rows, w_columns = api.fh_mx_quantize(weight, "both") if need_norm else (api.fh_mx_quantize(weight, "rows"), None)
-        y = api.fh_mx_matmul(h_rows, w_rows, bias, x.dtype)
-        ctx.kept, ctx.rounding, ctx.shape = (h_columns, w_columns), rounding, x.shape
-        ctx.dtypes = weight.dtype, None if bias is None else bias.dtype
-        if need_norm:
-            ctx.save_for_backward(m, mean, rstd, norm_weight)
-        return y.view(*x.shape[:-1], weight.shape[0])
+    def forward(ctx, x, norm_weight, norm_bias, weight, bias, norm, rounding, seed, tensor_id):
+        m, needs = _rows(x), ctx.needs_input_grad
+        needs_input = needs[0] or needs[1] or needs[2]
+        layer = api.MxLayer(m, weight, bias, norm is not None, norm_weight, norm_bias, 0.0 if norm is None else norm, needs_input, needs[3],
+                            rounding, seed, tensor_id)
+        y = layer.forward()
+        ctx.layer, ctx.shape, ctx.bias_dtype = layer, x.shape, None if bias is None else bias.dtype
+        if norm is not None and needs_input:
+            ctx.save_for_backward(m, norm_weight)
+        return y if x.dim() == 2 else y.view(*x.shape[:-1], weight.shape[0])
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        need_norm, (need_w, need_b) = any(ctx.needs_input_grad[:3]), ctx.needs_input_grad[3:5]
-        h_columns, w_columns = ctx.kept
-        g = _rows(dy)
-        g_rows, g_columns = _quantised_gradient(g, ctx.rounding, need_norm, need_w)
-        dw, db = _weight_gradients(g, h_columns, ctx.dtypes[0], need_w, need_b, ctx.dtypes[1], g_columns)
-        dx = d_norm_weight = d_norm_bias = None
-        if need_norm:
-            m, mean, rstd, norm_weight = ctx.saved_tensors
-            dh = api.fh_mx_matmul(g_rows, w_columns, out_dtype=dy.dtype)
-            dx, d_norm_weight, d_norm_bias = api.fh_layer_norm_backward(dh, m, mean, rstd, norm_weight, dx=dh,
-                                                                        sums=any(ctx.needs_input_grad[1:3]))
-            dx = dx.view(ctx.shape) if ctx.needs_input_grad[0] else None
-        return (dx, d_norm_weight if ctx.needs_input_grad[1] else None, d_norm_bias if ctx.needs_input_grad[2] else None, dw, db, None, None)
+        needs, layer, g = ctx.needs_input_grad, ctx.layer, _rows(dy)
+        x, norm_weight = ctx.saved_tensors if layer.args.norm and layer.args.needs & api.FH_MX_NEEDS_INPUT else (None, None)
+        dx = dw = d_norm_weight = d_norm_bias = None
+        if layer.args.needs:
+            dx, dw, d_norm_weight, d_norm_bias = layer.backward(g, x, norm_weight)
+        db = g.float().sum(0).to(ctx.bias_dtype) if needs[4] else None
+        return (dx.view(ctx.shape) if needs[0] else None, d_norm_weight if needs[1] else None, d_norm_bias if needs[2] else None, dw, db,
+                None, None, None, None)
 
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5) -> torch.Tensor:
@@ -136,14 +82,15 @@ def mx_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor
               tensor_id: int = 0) -> torch.Tensor:
     """x W^T + bias with all three products of a training step in microscaled 4-bit form.  rounding, seed and tensor_id
     are those of the gradient's quantisation; activations and weights are rounded to the nearest."""
-    return _MxLinear.apply(x, weight, bias, _Rounding(rounding, seed, tensor_id))
+    return _MxLinear.apply(x, None, None, weight, bias, None, rounding, seed, tensor_id)
 
 
 def layer_norm_mx_linear(x: torch.Tensor, norm_weight: Optional[torch.Tensor], norm_bias: Optional[torch.Tensor], weight: torch.Tensor,
                          bias: Optional[torch.Tensor] = None, eps: float = 1e-5, rounding="nearest", seed: int = 0,
                          tensor_id: int = 0) -> torch.Tensor:
-    """mx_linear(layer_norm(x)) without the norm's output ever being written but as codes."""
-    return _LayerNormMxLinear.apply(x, norm_weight, norm_bias, weight, bias, eps, _Rounding(rounding, seed, tensor_id))
+    """mx_linear(layer_norm(x)) without the norm's output ever being written but as codes.  x is saved as autograd saves it
+    (hooks.SavedActivations compresses it); the product's operands are kept in 4-bit form.  The parameters are of one dtype."""
+    return _MxLinear.apply(x, norm_weight, norm_bias, weight, bias, eps, rounding, seed, tensor_id)
 
 
 class LayerNorm(torch.nn.Module):

@@ -191,3 +191,64 @@ def test_captured_in_a_graph(layers):
         want = step(nx, ndy, [v.clone().requires_grad_() for v in (nw, nb, w)])
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), k
+
+
+@pytest.mark.parametrize("dtype, params", [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float32, torch.float32)])
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("tokens, features, out", [(1, 40, 7), (33, 100, 300), (300, 768, 64), (70, 2100, 33)])
+def test_the_layer_calls_are_their_parts(layers, tokens, features, out, norm, dtype, params):
+    """MxLayer's two calls against the calls that they stand for, bit for bit, from rows that are not next to each other."""
+    from paper_2510_11400_amd import api
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    wide = torch.randn(tokens, features + 9, generator=g, device="cuda").to(dtype)
+    x, w = wide[:, 5:5 + features], torch.randn(out, features + 3, generator=g, device="cuda").to(params)[:, :features]
+    b, nw, nb = (torch.randn(n, generator=g, device="cuda").to(params) for n in (out, features, features))
+    dy = torch.randn(tokens, out + 1, generator=g, device="cuda").to(dtype)[:, 1:]
+    if norm:
+        (xr, xc), mean, rstd = api.fh_layer_norm_mx(x, nw, nb, 1e-4, "both")
+    else:
+        xr, xc = api.fh_mx_quantize(x, "both")
+    wr, wc = api.fh_mx_quantize(w, "both")
+    want = api.fh_mx_matmul(xr, wr, b, dtype)
+    gr, gc = api.fh_mx_quantize(dy, "both", "stochastic", 3, 8)
+    want_dw = api.fh_mx_matmul(gc, xc, out_dtype=params)
+    want_dx = api.fh_mx_matmul(gr, wc, out_dtype=dtype)
+    want_nw = want_nb = None
+    if norm:
+        want_dx, want_nw, want_nb = api.fh_layer_norm_backward(want_dx, x, mean, rstd, nw)
+        if params != dtype:
+            want_nw, want_nb = want_nw.to(params), want_nb.to(params)
+    layer = api.MxLayer(x, w, b, norm, nw if norm else None, nb if norm else None, 1e-4, rounding="stochastic", seed=3, tensor_id=8)
+    assert torch.equal(layer.forward(), want)
+    for _ in range(2):
+        got = layer.backward(dy, x, nw if norm else None)
+        assert torch.equal(got[0], want_dx) and torch.equal(got[1], want_dw)
+        assert (got[2] is None and got[3] is None) if not norm else torch.equal(got[2], want_nw) and torch.equal(got[3], want_nb)
+    alone = api.MxLayer(x, w, b, norm, nw if norm else None, nb if norm else None, 1e-4, needs_input=False, needs_weight=False)
+    assert torch.equal(alone.forward(), want)
+
+
+def test_no_tokens(layers):
+    x = torch.empty(0, 40, device="cuda", requires_grad=True)
+    w = torch.randn(7, 40, device="cuda", requires_grad=True)
+    nw = torch.ones(40, device="cuda", requires_grad=True)
+    y = layers.layer_norm_mx_linear(x, nw, None, w)
+    assert y.shape == (0, 7)
+    dx, dnw, dw = torch.autograd.grad(y, (x, nw, w), torch.empty(0, 7, device="cuda"))
+    assert dx.shape == (0, 40) and not dnw.any() and not dw.any()
+
+
+def test_gradients_that_are_one_row_everywhere(layers):
+    """The gradient of a sum over tokens reaches the layer as one row expanded over all of them."""
+    x, nw, nb, w, _, _ = (v.cuda() for v in _case(64, 100, 40, torch.float32))
+    leaves = [v.clone().requires_grad_() for v in (x, nw, nb, w)]
+    scale = torch.randn(40, device="cuda")
+    y = layers.layer_norm_mx_linear(*leaves)
+    got = torch.autograd.grad((y.sum((0, 1)) * scale).sum(), leaves, retain_graph=True)
+    want = torch.autograd.grad(y, leaves, scale.expand(y.shape).contiguous())
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    z = [v.clone().requires_grad_() for v in (x.view(64, 100), nw, nb)]
+    y = layers.layer_norm(*z)
+    got = torch.autograd.grad((y.sum(0) * scale[0]).sum(), z, retain_graph=True)
+    want = torch.autograd.grad(y, z, scale[0].expand(y.shape).contiguous())
+    assert all(torch.equal(a, b) for a, b in zip(got, want))

@@ -194,3 +194,40 @@ def test_the_binding_refuses_host_tensors_and_shapes():
 def test_the_binding_and_the_library_agree_on_sizes(rows, cols):
     assert api.mx_bytes(rows, cols) == LIB.fh_mx_bytes(rows, cols)
     assert api.mx_scales_offset(rows, cols) == LIB.fh_mx_scales_offset(rows, cols)
+
+
+def _layer(backward=False, **change):
+    a = api.fh_mx_layer(5, 40, 7, 0, 0, 1, 3, 0, 1e-5, 0, 0, FAKE, 40, FAKE, FAKE, FAKE, 40, FAKE, FAKE, FAKE, 7, FAKE, FAKE, FAKE, FAKE,
+                        FAKE, BIG, FAKE, BIG, 0)
+    for name, v in change.items():
+        setattr(a, name, v)
+    return (LIB.fh_mx_layer_backward if backward else LIB.fh_mx_layer_forward)(ctypes.byref(a), None)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_layer_refusals(backward):
+    assert (LIB.fh_mx_layer_backward if backward else LIB.fh_mx_layer_forward)(None, None) == 1
+    assert _layer(backward, dtype=2) == 2 and _layer(backward, p_dtype=-1) == 2 and _layer(backward, rounding=2) == 5
+    for bad in (dict(tokens=-1), dict(features=0), dict(out_features=0), dict(tokens=2 ** 24 + 1), dict(features=2 ** 24 + 1), dict(x_stride=39),
+                dict(weight_stride=39), dict(dy_stride=6), dict(x_stride=2 ** 31 + 1)):
+        assert _layer(backward, **bad) == 11, bad
+    for bad in (dict(norm=2), dict(needs=4), dict(needs=-1), dict(reserved=1), dict(eps=-1.0), dict(eps=float("nan"))):
+        assert _layer(backward, **bad) == 12, bad
+    needed = ("kept", "scratch", "dweight", "dy", "dx", "x") if backward else ("kept", "scratch", "x", "weight", "y")
+    for name in needed:
+        assert _layer(backward, **{name: None}) == 1, name
+    aligned = ("x", "dy", "dx", "dweight", "norm_weight", "dnorm_weight", "dnorm_bias") if backward else ("x", "y", "weight", "bias", "norm_weight", "norm_bias")
+    for name in aligned:
+        assert _layer(backward, **{name: FAKE + 2}) == 8, name
+    assert _layer(backward, kept=FAKE + 8) == 8 and _layer(backward, scratch=FAKE + 4) == 8
+    assert _layer(backward, kept_cap=LIB.fh_mx_layer_kept_bytes(5, 40, 7) - 1) == 7 and _layer(backward, scratch_cap=100) == 7
+    assert (_layer(True, needs=0, kept=None, scratch=None) if backward else _layer(tokens=0, x=None, y=None, kept=None)) == 0
+
+
+def test_layer_sizes():
+    assert LIB.fh_mx_layer_kept_bytes(0, 1, 1) >= 0
+    for bad in ((-1, 4, 4), (4, 0, 4), (4, 4, 0), (2 ** 24 + 1, 4, 4)):
+        assert LIB.fh_mx_layer_kept_bytes(*bad) == 0 and LIB.fh_mx_layer_scratch_bytes(*bad) == 0
+    kept = LIB.fh_mx_layer_kept_bytes(100, 300, 70)
+    assert kept >= 2 * 400 + api.mx_bytes(300, 100) + api.mx_bytes(300, 70)
+    assert LIB.fh_mx_layer_scratch_bytes(100, 300, 70) >= max(api.mx_bytes(100, 300) + api.mx_bytes(70, 300), api.mx_bytes(100, 70) + api.mx_bytes(70, 100))
