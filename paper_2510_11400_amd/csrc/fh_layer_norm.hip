@@ -7,21 +7,37 @@ namespace {
 // Columns up to which a row is held in registers: by a wave, and by a workgroup of 1024.
 constexpr int64_t kWaveCols = 2048, kGroupCols = 16384;
 
-// The sum of v over the T threads that share a row (the workgroup's rows are T threads each); `s_sums` holds a value per
-// wave and is used by every call in turn.
+// The sum of v over the T threads that share a row (a workgroup's rows are T threads each).  `s_sums` holds a value per wave; the
+// calls of a workgroup take its two halves in turn, so that one barrier a call is enough: a wave writes a half again only
+// after the barrier of the call between, which every wave enters when it has read that half.
 template <int T>
-__device__ __forceinline__ float row_sum(float v, float* s_sums)
+__device__ __forceinline__ float row_sum(float v, float (&s_sums)[2][16], int turn)
 {
-    v = wave_sum(v);
-    if constexpr (T > 64) {
-        __syncthreads();                                         // the sums of the call before have been read
-        if ((threadIdx.x & 63) == 0) s_sums[threadIdx.x >> 6] = v;
-        __syncthreads();
-        const float* mine = s_sums + threadIdx.x / T * (T / 64);
-        v = 0.0f;
-        for (int w = 0; w < T / 64; ++w) v += mine[w];
-    }
+    if constexpr (T <= 64) return lane_sum<T>(v);
+    v = lane_sum<64>(v);
+    float* sums = s_sums[turn & 1];
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = v;
+    __syncthreads();
+    const float* mine = sums + threadIdx.x / T * (T / 64);
+    v = 0.0f;
+    for (int w = 0; w < T / 64; ++w) v += mine[w];
     return v;
+}
+// The same for two values.
+template <int T>
+__device__ __forceinline__ void row_sums(float& v, float& u, f32x2 (&s_pairs)[2][16], int turn)
+{
+    constexpr int kLanes = T < 64 ? T : 64;
+    v = lane_sum<kLanes>(v);
+    u = lane_sum<kLanes>(u);
+    if constexpr (T > 64) {
+        f32x2* sums = s_pairs[turn & 1];
+        if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = f32x2{v, u};
+        __syncthreads();
+        const f32x2* mine = sums + threadIdx.x / T * (T / 64);
+        v = u = 0.0f;
+        for (int w = 0; w < T / 64; ++w) { v += mine[w].x; u += mine[w].y; }
+    }
 }
 
 // ---- forward: a row in the registers of T threads, NV runs of eight values each ------------
@@ -32,7 +48,7 @@ template <typename T, int THREADS, int NV, bool MX>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_rows_kernel(const T* x, int64_t rows, int64_t cols, int64_t x_stride,
                                                                                   NormArgs n, NormOut to)
 {
-    __shared__ float s_sums[16];
+    __shared__ float s_sums[2][16];
     const int t = threadIdx.x % THREADS;
     const int64_t row = (int64_t)blockIdx.x * (THREADS < 256 ? 256 / THREADS : 1) + threadIdx.x / THREADS;
     const bool write = row < rows;
@@ -46,7 +62,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_rows_kerne
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum += v[k][i];
     }
-    const float mean = row_sum<THREADS>(sum, s_sums) / (float)cols;
+    const float mean = row_sum<THREADS>(sum, s_sums, 0) / (float)cols;
     // the squares of what is left, so that a mean far from zero costs no digits
     float squares = 0.0f;
 #pragma unroll
@@ -58,7 +74,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_rows_kerne
             squares = __builtin_fmaf(d, d, squares);
         }
     }
-    const float rstd = 1.0f / __builtin_sqrtf(row_sum<THREADS>(squares, s_sums) / (float)cols + n.eps);
+    const float rstd = 1.0f / __builtin_sqrtf(row_sum<THREADS>(squares, s_sums, 1) / (float)cols + n.eps);
     if (write && t == 0) {
         if (n.mean) n.mean[row] = mean;
         if (n.rstd) n.rstd[row] = rstd;
@@ -93,7 +109,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_rows_kerne
 template <typename T, bool MX>
 __global__ __launch_bounds__(1024) void norm_long_rows_kernel(const T* x, int64_t cols, int64_t x_stride, NormArgs n, NormOut to)
 {
-    __shared__ float s_sums[16];
+    __shared__ float s_sums[2][16];
     const int64_t row = blockIdx.x;
     const T* p = x + row * x_stride;
     const int64_t end = mx_chunks(cols) * kMxChunk;             // whole waves have the same number of turns
@@ -102,7 +118,7 @@ __global__ __launch_bounds__(1024) void norm_long_rows_kernel(const T* x, int64_
         load8(p + first, cols - first, v);
         for (int i = 0; i < 8; ++i) sum += v[i];
     }
-    const float mean = row_sum<1024>(sum, s_sums) / (float)cols;
+    const float mean = row_sum<1024>(sum, s_sums, 0) / (float)cols;
     float squares = 0.0f;
     for (int64_t first = threadIdx.x * 8; first < cols; first += 8192) {
         load8(p + first, cols - first, v);
@@ -111,7 +127,7 @@ __global__ __launch_bounds__(1024) void norm_long_rows_kernel(const T* x, int64_
             squares = __builtin_fmaf(d, d, squares);
         }
     }
-    const float rstd = 1.0f / __builtin_sqrtf(row_sum<1024>(squares, s_sums) / (float)cols + n.eps);
+    const float rstd = 1.0f / __builtin_sqrtf(row_sum<1024>(squares, s_sums, 1) / (float)cols + n.eps);
     if (threadIdx.x == 0) {
         if (n.mean) n.mean[row] = mean;
         if (n.rstd) n.rstd[row] = rstd;
@@ -143,62 +159,80 @@ struct NormBackwardArgs {
     int32_t      groups;               // workgroups
 };
 
-// A workgroup takes ROWS rows at a time, a grid apart, THREADS threads each.  Every thread keeps the sums of its columns in
-// registers; at the end the rows' sums are added up in LDS, a run of columns at a time, and the workgroup leaves one row of
-// partial sums, for norm_join_kernel.
+// A workgroup takes ROWS rows at a time, a grid apart, THREADS threads each, NV runs of four columns a thread (with eight, a row of 768
+// left a quarter of the lanes idle, and the arithmetic of some 17 instructions a value is what binds rows of bf16).  Every
+// thread keeps the sums of its columns in registers; at the end the rows' sums are added up in LDS, a run of columns at a time,
+// and the workgroup leaves one row of partial sums, for norm_join_kernel.
 template <typename T, int THREADS, int NV, int ROWS>
 __global__ __launch_bounds__(THREADS * ROWS) void norm_backward_kernel(NormBackwardArgs a)
 {
-    __shared__ float s_sums[16];
-    __shared__ __attribute__((aligned(16))) float s_join[ROWS > 1 ? ROWS * THREADS * 8 : 4];
+    constexpr bool kAhead = sizeof(T) == 2 || NV < (THREADS < 1024 ? 8 : 4);   // the next row's loads before this row's sums: as registers allow
+    constexpr int kWidth = THREADS * 4;
+    __shared__ f32x2 s_pairs[2][16];
+    __shared__ __attribute__((aligned(16))) float s_join[ROWS > 1 ? ROWS * kWidth : 4];
+    // the weight, read again for every row: in registers it would push the next row's loads out of them
+    __shared__ __attribute__((aligned(16))) float s_weight[NV * kWidth];
     const int t = threadIdx.x % THREADS, part = threadIdx.x / THREADS;
-    float w[NV][8], dw[NV][8], db[NV][8];
+    Run<T, 4> next_x[NV], next_g[NV];
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    auto load = [&](int64_t row) {                               // nothing of a row past the last
+        const bool here = row < a.rows;
+        const int64_t at = here ? row : 0;
+        next_mean = here ? a.mean[at] : 0.0f;
+        next_rstd = here ? a.rstd[at] : 0.0f;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int64_t first = ((int64_t)k * THREADS + t) * 8;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) { w[k][i] = 1.0f; dw[k][i] = 0.0f; db[k][i] = 0.0f; }
-        if (a.weight) {
-            if (a.p_dtype == FH_F32) load8(static_cast<const float*>(a.weight) + first, a.cols - first, w[k]);
-            else load8(static_cast<const Bf16*>(a.weight) + first, a.cols - first, w[k]);
+        for (int k = 0; k < NV; ++k) {
+            const int64_t first = (int64_t)k * kWidth + t * 4;
+            next_x[k].load(static_cast<const T*>(a.x) + at * a.x_stride + first, here ? a.cols - first : 0);
+            next_g[k].load(static_cast<const T*>(a.dy) + at * a.dy_stride + first, here ? a.cols - first : 0);
         }
-    }
+    };
+    if constexpr (kAhead) load((int64_t)blockIdx.x * ROWS + part);
+    for (int c = threadIdx.x; c < NV * kWidth; c += THREADS * ROWS)
+        s_weight[c] = c < a.cols ? parameter(a.weight, a.p_dtype, c, 1.0f) : 0.0f;
+    __syncthreads();
+    f32x4 dw[NV] = {}, db[NV] = {};
     const float share = 1.0f / (float)a.cols;
-    for (int64_t start = (int64_t)blockIdx.x * ROWS; start < a.rows; start += (int64_t)a.groups * ROWS) {
+    const int64_t step = (int64_t)a.groups * ROWS;
+    int turn = 0;
+    for (int64_t start = (int64_t)blockIdx.x * ROWS; start < a.rows; start += step, ++turn) {
         const int64_t row = start + part;
         const bool here = row < a.rows;
-        float x[NV][8], g[NV][8];
-        const int64_t at = here ? row : a.rows - 1;
-        const float mean = a.mean[at], rstd = a.rstd[at];
+        if constexpr (!kAhead) load(row);
+        f32x4 h[NV], g[NV];
+        const float mean = next_mean, rstd = next_rstd;
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int64_t first = ((int64_t)k * THREADS + t) * 8;
-            load8(static_cast<const T*>(a.x) + at * a.x_stride + first, here ? a.cols - first : 0, x[k]);
-            load8(static_cast<const T*>(a.dy) + at * a.dy_stride + first, here ? a.cols - first : 0, g[k]);
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { h[k][i] = next_x[k].at(i); g[k][i] = next_g[k].at(i); }
+        if constexpr (kAhead) {
+            if (start + step < a.rows) load(row + step);
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int64_t first = ((int64_t)k * THREADS + t) * 8;
+            const f32x4 w = *reinterpret_cast<const f32x4*>(s_weight + k * kWidth + t * 4);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[k][i] = first + i < a.cols && here ? (x[k][i] - mean) * rstd : 0.0f;
-                dw[k][i] = __builtin_fmaf(g[k][i], x[k][i], dw[k][i]);
+            for (int i = 0; i < 4; ++i) {                        // where there is no column or row: g is 0, and rstd without a row
+                h[k][i] = (h[k][i] - mean) * rstd;
+                dw[k][i] = __builtin_fmaf(g[k][i], h[k][i], dw[k][i]);
                 db[k][i] += g[k][i];
-                g[k][i] *= w[k][i];
+                g[k][i] *= w[i];
                 s1 += g[k][i];
-                s2 = __builtin_fmaf(g[k][i], x[k][i], s2);
+                s2 = __builtin_fmaf(g[k][i], h[k][i], s2);
             }
         }
         if (a.dx) {
-            s1 = row_sum<THREADS>(s1, s_sums) * share;
-            s2 = row_sum<THREADS>(s2, s_sums) * share;
+            row_sums<THREADS>(s1, s2, s_pairs, turn);
+            s1 *= share * rstd;
+            s2 *= share * rstd;
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                const int64_t first = ((int64_t)k * THREADS + t) * 8;
+                const int64_t first = (int64_t)k * kWidth + t * 4;
+                float v[4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[k][i] = rstd * (g[k][i] - s1 - x[k][i] * s2);
-                if (here) store8(static_cast<T*>(a.dx) + row * a.dx_stride + first, a.cols - first, g[k]);
+                for (int i = 0; i < 4; ++i) v[i] = __builtin_fmaf(g[k][i], rstd, -__builtin_fmaf(h[k][i], s2, s1));
+                if (here) store4(static_cast<T*>(a.dx) + row * a.dx_stride + first, a.cols - first, v);
             }
         }
     }
@@ -208,21 +242,21 @@ __global__ __launch_bounds__(THREADS * ROWS) void norm_backward_kernel(NormBackw
     for (int which = 0; which < 2; ++which)
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int64_t first = ((int64_t)k * THREADS + t) * 8;
+            const int64_t first = (int64_t)k * kWidth + t * 4;
+            const f32x4 v = which ? db[k] : dw[k];
             if constexpr (ROWS == 1) {
-                store8(to + which * a.cols + first, a.cols - first, which ? db[k] : dw[k]);
+                const float u[4] = {v.x, v.y, v.z, v.w};
+                store4(to + which * a.cols + first, a.cols - first, u);
             } else {
-                if ((int64_t)k * THREADS * 8 >= a.cols) continue;    // uniform
-                const float (&v)[8] = which ? db[k] : dw[k];
+                if ((int64_t)k * kWidth >= a.cols) continue;     // uniform
                 __syncthreads();
-                *reinterpret_cast<f32x4*>(s_join + (part * THREADS + t) * 8) = f32x4{v[0], v[1], v[2], v[3]};
-                *reinterpret_cast<f32x4*>(s_join + (part * THREADS + t) * 8 + 4) = f32x4{v[4], v[5], v[6], v[7]};
+                *reinterpret_cast<f32x4*>(s_join + (part * THREADS + t) * 4) = v;
                 __syncthreads();
-                for (int c = threadIdx.x; c < THREADS * 8; c += THREADS * ROWS) {
+                for (int c = threadIdx.x; c < kWidth; c += THREADS * ROWS) {
                     float sum = 0.0f;
-#pragma unroll
-                    for (int r = 0; r < ROWS; ++r) sum += s_join[r * THREADS * 8 + c];
-                    if ((int64_t)k * THREADS * 8 + c < a.cols) to[which * a.cols + (int64_t)k * THREADS * 8 + c] = sum;
+#pragma unroll 8
+                    for (int r = 0; r < ROWS; ++r) sum += s_join[r * kWidth + c];
+                    if ((int64_t)k * kWidth + c < a.cols) to[which * a.cols + (int64_t)k * kWidth + c] = sum;
                 }
             }
         }
@@ -232,7 +266,7 @@ __global__ __launch_bounds__(THREADS * ROWS) void norm_backward_kernel(NormBackw
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_backward_long_rows_kernel(NormBackwardArgs a)
 {
-    __shared__ float s_sums[16];
+    __shared__ f32x2 s_pairs[2][16];
     const int64_t row = blockIdx.x;
     const T *px = static_cast<const T*>(a.x) + row * a.x_stride, *pg = static_cast<const T*>(a.dy) + row * a.dy_stride;
     const float mean = a.mean[row], rstd = a.rstd[row], share = 1.0f / (float)a.cols;
@@ -246,8 +280,9 @@ __global__ __launch_bounds__(1024) void norm_backward_long_rows_kernel(NormBackw
             s2 = __builtin_fmaf(gw, (x[i] - mean) * rstd, s2);
         }
     }
-    s1 = row_sum<1024>(s1, s_sums) * share;
-    s2 = row_sum<1024>(s2, s_sums) * share;
+    row_sums<1024>(s1, s2, s_pairs, 0);
+    s1 *= share;
+    s2 *= share;
     for (int64_t first = threadIdx.x * 8; first < a.cols; first += 8192) {
         load8(px + first, a.cols - first, x);
         load8(pg + first, a.cols - first, g);
@@ -279,24 +314,29 @@ __global__ __launch_bounds__(256) void norm_column_sums_kernel(NormBackwardArgs 
     store8(to + a.cols + first, a.cols - first, db);
 }
 
-// The partial rows added up in an order of their number alone: 64 columns of one of the two sums a workgroup, a sixteenth of the
-// rows a wave, four running sums each so that as many loads are on their way.
+// The partial rows (kMostParts at most) added up in an order of their number alone: 64 columns of one of the two sums a workgroup,
+// a sixteenth of the rows a wave, whose loads are all on their way at once: the kernel takes little more than one of them.
+constexpr int kMostParts = 256;
 template <typename P>
 __global__ __launch_bounds__(1024) void norm_join_kernel(const float* partial, int64_t parts, int64_t cols, P* dweight, P* dbias)
 {
+    constexpr int kEach = kMostParts / 16;
     __shared__ float s_part[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t c = (int64_t)(blockIdx.x >> 1) * 64 + lane, which = blockIdx.x & 1;
-    float sum[4] = {};
-    if (c < cols) {
-        const float* from = partial + which * cols + c;
-        int64_t r = wave;
-        for (; r + 48 < parts; r += 64)
+    const float* from = partial + which * cols + (c < cols ? c : 0);
+    float v[kEach] = {};
+    if (parts > 0) {                                             // rows past the last: the first one, for nothing
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] += from[(r + 16 * i) * 2 * cols];
-        for (int i = 0; r < parts; r += 16, ++i) sum[i] += from[r * 2 * cols];
+        for (int i = 0; i < kEach; ++i) v[i] = from[(int64_t)(wave + 16 * i < parts ? wave + 16 * i : 0) * 2 * cols];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) v[i] = wave + 16 * i < parts ? v[i] : 0.0f;
     }
-    s_part[wave][lane] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+    for (int half = kEach / 2; half > 0; half /= 2)
+#pragma unroll
+        for (int i = 0; i < half; ++i) v[i] += v[i + half];
+    s_part[wave][lane] = v[0];
     __syncthreads();
     P* to = which ? dbias : dweight;
     if (wave == 0 && c < cols && to) {
@@ -320,22 +360,40 @@ hipError_t norm_of(const void* x, int64_t rows, int64_t cols, int64_t xs, const 
 template <typename T, bool MX>
 hipError_t norm_any(const void* x, int64_t rows, int64_t cols, int64_t xs, const NormArgs& n, const NormOut& to, hipStream_t s)
 {
+    // narrow rows share a wave; codes are written for 256 columns at least, which takes 32 lanes
+    if constexpr (!MX) {
+        if (cols <= 64) return norm_of<T, 8, 1, MX>(x, rows, cols, xs, n, to, s);
+        if (cols <= 128) return norm_of<T, 16, 1, MX>(x, rows, cols, xs, n, to, s);
+    }
+    if (cols <= 256) return norm_of<T, 32, 1, MX>(x, rows, cols, xs, n, to, s);
     if (cols <= 512) return norm_of<T, 64, 1, MX>(x, rows, cols, xs, n, to, s);
     if (cols <= 1024) return norm_of<T, 64, 2, MX>(x, rows, cols, xs, n, to, s);
     if (cols <= kWaveCols) return norm_of<T, 64, 4, MX>(x, rows, cols, xs, n, to, s);
     if (cols <= 4096) return norm_of<T, 256, 2, MX>(x, rows, cols, xs, n, to, s);
     if (cols <= 8192) return norm_of<T, 1024, 1, MX>(x, rows, cols, xs, n, to, s);
-    if (cols <= kGroupCols) return norm_of<T, 1024, 2, MX>(x, rows, cols, xs, n, to, s);
+    if (cols <= kGroupCols) return rows >= 512 ? norm_of<T, 512, 4, MX>(x, rows, cols, xs, n, to, s) : norm_of<T, 1024, 2, MX>(x, rows, cols, xs, n, to, s);
     hipLaunchKernelGGL((norm_long_rows_kernel<T, MX>), dim3((uint32_t)rows), dim3(1024), 0, s, static_cast<const T*>(x), cols, xs, n, to);
     return hipGetLastError();
 }
 
-// Rows that a workgroup of the backward pass takes at a time, workgroups, each of which leaves a row of partial sums.
-inline int64_t backward_rows(int64_t cols) { return cols <= 1024 ? 16 : cols <= kWaveCols ? 8 : cols <= 4096 ? 4 : 1; }
+// Threads that share a row of the backward pass, runs of four columns a thread, rows that a workgroup takes at a time (as many as
+// their registers allow; with few rows the workgroups are smaller, so that there are more of them), workgroups, each of which
+// leaves a row of partial sums.
+struct BackwardShape { int32_t threads, runs, rows; };
+inline BackwardShape backward_shape(int64_t rows, int64_t cols)
+{
+    int32_t threads = cols <= 64 ? 16 : cols <= 128 ? 32 : cols <= kWaveCols ? 64 : cols <= 4096 ? 256 : 1024;
+    int32_t runs = (int32_t)((cols + threads * 4 - 1) / (threads * 4));
+    if (threads == 64 && runs > 4) runs = runs > 6 ? 8 : 6;
+    else if (threads == 256) runs = 4;
+    const int32_t most = threads == 64 && runs > 4 ? 512 : runs == 4 ? 768 : 1024;
+    const bool few = rows * threads <= 128 * 1024 && threads <= 256;
+    return BackwardShape{threads, runs, threads == 1024 ? 1 : (few ? 256 : most) / threads};
+}
 inline int64_t backward_groups(int64_t rows, int64_t cols)
 {
-    const int64_t each = backward_rows(cols), groups = (rows + each - 1) / each;
-    return groups < 256 ? groups : 256;
+    const int64_t each = backward_shape(rows, cols).rows, groups = (rows + each - 1) / each;
+    return groups < kMostParts ? groups : kMostParts;
 }
 
 template <typename T, int THREADS, int NV, int ROWS>
@@ -349,12 +407,24 @@ hipError_t backward_any(const NormBackwardArgs& a, int64_t* parts, hipStream_t s
 {
     const int64_t groups = a.groups;
     *parts = groups;
-    if (a.cols <= 512) return backward_of<T, 64, 1, 16>(a, groups, s);
-    if (a.cols <= 1024) return backward_of<T, 64, 2, 16>(a, groups, s);
-    if (a.cols <= kWaveCols) return backward_of<T, 64, 4, 8>(a, groups, s);
-    if (a.cols <= 4096) return backward_of<T, 256, 2, 4>(a, groups, s);
-    if (a.cols <= 8192) return backward_of<T, 1024, 1, 1>(a, groups, s);
-    if (a.cols <= kGroupCols) return backward_of<T, 1024, 2, 1>(a, groups, s);
+    if (a.cols <= kGroupCols) {
+        const BackwardShape b = backward_shape(a.rows, a.cols);
+        const bool few = b.threads * b.rows == 256;
+        switch (b.threads * 16 + b.runs) {
+            case 16 * 16 + 1: return few ? backward_of<T, 16, 1, 16>(a, groups, s) : backward_of<T, 16, 1, 64>(a, groups, s);
+            case 32 * 16 + 1: return few ? backward_of<T, 32, 1, 8>(a, groups, s) : backward_of<T, 32, 1, 32>(a, groups, s);
+            case 64 * 16 + 1: return few ? backward_of<T, 64, 1, 4>(a, groups, s) : backward_of<T, 64, 1, 16>(a, groups, s);
+            case 64 * 16 + 2: return few ? backward_of<T, 64, 2, 4>(a, groups, s) : backward_of<T, 64, 2, 16>(a, groups, s);
+            case 64 * 16 + 3: return few ? backward_of<T, 64, 3, 4>(a, groups, s) : backward_of<T, 64, 3, 16>(a, groups, s);
+            case 64 * 16 + 4: return few ? backward_of<T, 64, 4, 4>(a, groups, s) : backward_of<T, 64, 4, 12>(a, groups, s);
+            case 64 * 16 + 6: return few ? backward_of<T, 64, 6, 4>(a, groups, s) : backward_of<T, 64, 6, 8>(a, groups, s);
+            case 64 * 16 + 8: return few ? backward_of<T, 64, 8, 4>(a, groups, s) : backward_of<T, 64, 8, 8>(a, groups, s);
+            case 256 * 16 + 4: return few ? backward_of<T, 256, 4, 1>(a, groups, s) : backward_of<T, 256, 4, 3>(a, groups, s);
+            case 1024 * 16 + 2: return backward_of<T, 1024, 2, 1>(a, groups, s);
+            case 1024 * 16 + 3: return backward_of<T, 1024, 3, 1>(a, groups, s);
+            default: return backward_of<T, 1024, 4, 1>(a, groups, s);
+        }
+    }
     if (a.partial) {                                             // first: dx may be dy itself
         const int64_t each = (a.rows + groups - 1) / groups, col_groups = (a.cols + 2047) / 2048;
         *parts = (a.rows + each - 1) / each;

@@ -98,17 +98,25 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v)      // over 16 lanes
     v = umax(v, dpp<kHalfMirror>(v));
     return umax(v, dpp<kRowMirror>(v));
 }
-__device__ __forceinline__ float wave_sum(float v)
+template <int LANES>
+__device__ __forceinline__ float lane_sum(float v)           // over aligned runs of 8, 16, 32 or 64 lanes
 {
+    static_assert(LANES == 8 || LANES == 16 || LANES == 32 || LANES == 64, "run length");
     v += dpp<kQuadXor1>(v);
     v += dpp<kQuadXor2>(v);
     v += dpp<kHalfMirror>(v);
-    v += dpp<kRowMirror>(v);
-    float a, b;
-    self_swap<16>(v, a, b);
-    v = a + b;
-    self_swap<32>(v, a, b);
-    return a + b;
+    if constexpr (LANES >= 16) v += dpp<kRowMirror>(v);
+    if constexpr (LANES >= 32) {
+        float a, b;
+        self_swap<16>(v, a, b);
+        v = a + b;
+    }
+    if constexpr (LANES >= 64) {
+        float a, b;
+        self_swap<32>(v, a, b);
+        v = a + b;
+    }
+    return v;
 }
 
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu; }
@@ -118,11 +126,45 @@ __device__ __forceinline__ uint32_t abs_bits(float v) { return __builtin_bit_cas
 typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
 typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
 typedef uint32_t u32_a2 __attribute__((aligned(2)));
+typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
 typedef f32x2 f32x2_a4 __attribute__((aligned(4)));
 
 struct Bf16 { uint16_t bits; };
 __device__ __forceinline__ float value(float v) { return v; }
 __device__ __forceinline__ float value(Bf16 v) { return __builtin_bit_cast(float, (uint32_t)v.bits << 16); }
+
+// N values in words as they lie in memory.
+template <typename T, int N = 8>
+struct Run {
+    static constexpr int kWords = N * (int)sizeof(T) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T* p, int64_t n)
+    {
+        if (n >= N) {
+            if constexpr (kWords == 2) {
+                const u32x2 v = *reinterpret_cast<const u32x2_a2*>(p);
+                w[0] = v.x; w[1] = v.y;
+            } else {
+#pragma unroll
+                for (int i = 0; i < kWords; i += 4) {
+                    const u32x4 v = *reinterpret_cast<const u32x4_a2*>(reinterpret_cast<const uint32_t*>(p) + i);
+                    w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if constexpr (sizeof(T) == 4) w[i] = i < n ? __builtin_bit_cast(uint32_t, p[i]) : 0u;
+                else w[i / 2] = (i & 1 ? w[i / 2] : 0u) | (i < n ? (uint32_t)p[i].bits : 0u) << (16 * (i & 1));
+            }
+        }
+    }
+    __device__ __forceinline__ float at(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, w[i]);
+        else return i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
+    }
+};
 
 // Eight values from p on, of which the first `n` exist (the others are 0).
 __device__ __forceinline__ void load8(const float* p, int64_t n, float (&v)[8])
@@ -176,7 +218,6 @@ __device__ __forceinline__ void store_run(float* p, int64_t n, const float (&v)[
     else for (int i = 0; i < 4; ++i) if (i < n) p[i] = v[i];
 }
 __device__ __forceinline__ void store_run(Bf16* p, int64_t n, const float (&v)[8]) { store8(p, n, v); }
-typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
 __device__ __forceinline__ void store4(float* p, int64_t n, const float (&v)[4]) { store_run(p, n, v); }
 __device__ __forceinline__ void store4(Bf16* p, int64_t n, const float (&v)[4])
 {

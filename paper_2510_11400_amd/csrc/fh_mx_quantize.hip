@@ -6,17 +6,28 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// ---- by rows, nearest: 8 values a lane, one row's chunk of 256 for half a wave ------------
-// Bound by the read: 2 or 4 bytes in, 17/32 out a value.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void mx_rows_kernel(const T* x, int64_t rows, int64_t cols, int64_t stride, MxStore to, int64_t units)
+// ---- by rows, nearest, and back: a chunk of a row is half a wave's, 8 values a lane --------------
+// A workgroup takes one chunk of eight rows, the grid is (chunks, rows / 8, and a third dimension where that passes the second's
+// limit): no thread divides.  With a division of 64 bits in every thread the kernels, which have little else to do, took a third longer.
+// Bound by memory: 2 or 4 bytes a value on the plain side, 17/32 on the stored one.
+constexpr int kRowsAtOnce = kThreads / 32;
+constexpr int64_t kMostGridY = 65535;
+__device__ __forceinline__ int64_t row_of_thread() { return ((int64_t)blockIdx.z * kMostGridY + blockIdx.y) * kRowsAtOnce + threadIdx.x / 32; }
+inline bool grid_of(int64_t rows, int64_t chunks, dim3& grid)
 {
-    const int64_t unit = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
-    const bool write = unit < units;
-    const int64_t row = write ? unit / to.chunks : 0, chunk = write ? unit - row * to.chunks : 0;
-    const int64_t first = chunk * kMxChunk + (threadIdx.x & 31) * 8;
+    const int64_t groups = (rows + kRowsAtOnce - 1) / kRowsAtOnce, z = (groups + kMostGridY - 1) / kMostGridY;
+    if (z > kMostGridY || chunks > INT32_MAX) return false;
+    grid = dim3((uint32_t)chunks, (uint32_t)(z > 1 ? kMostGridY : groups), (uint32_t)z);
+    return true;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void mx_rows_kernel(const T* x, int64_t rows, int64_t cols, int64_t stride, MxStore to)
+{
+    const int64_t row = row_of_thread(), first = (int64_t)blockIdx.x * kMxChunk + (threadIdx.x & 31) * 8;
+    const bool write = row < rows;
     float v[8];
-    load8(x + row * stride + first, cols - first, v);
+    load8(x + (write ? row : 0) * stride + first, write ? cols - first : 0, v);
     mx_write8(to, row, first, v, write);
 }
 
@@ -35,34 +46,6 @@ __device__ __forceinline__ float lane_value(float v, int lane)
 constexpr int kTileRows = 256, kTileThreads = 512;
 constexpr int kWaveBytes = 32 * 256 + 16;          // the 16 turn the waves' areas, so that a gather of all eight meets all banks
 template <typename T> constexpr int kTileCols = 256 / (int)sizeof(T);
-
-// Eight values in words as they lie in memory.
-template <typename T>
-struct Run {
-    static constexpr int kWords = 2 * (int)sizeof(T);
-    uint32_t w[kWords];
-    __device__ __forceinline__ void load(const T* p, int64_t n)
-    {
-        if (n >= 8) {
-#pragma unroll
-            for (int i = 0; i < kWords; i += 4) {
-                const u32x4 v = *reinterpret_cast<const u32x4_a2*>(reinterpret_cast<const uint32_t*>(p) + i);
-                w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if constexpr (sizeof(T) == 4) w[i] = i < n ? __builtin_bit_cast(uint32_t, p[i]) : 0u;
-                else w[i / 2] = (i & 1 ? w[i / 2] : 0u) | (i < n ? (uint32_t)p[i].bits : 0u) << (16 * (i & 1));
-            }
-        }
-    }
-    __device__ __forceinline__ float at(int i) const
-    {
-        if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, w[i]);
-        else return i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
-    }
-};
 
 template <typename T, bool NORM, bool STOCHASTIC>
 __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4) void mx_tiles_kernel(const T* x, int64_t rows, int64_t cols, int64_t stride, NormArgs n,
@@ -228,15 +211,11 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
     if (STOCHASTIC && rows_form) write_rows();
 }
 
-// ---- back ---------------------------------------------------------------------------------
 template <typename T>
-__global__ __launch_bounds__(kThreads) void mx_restore_kernel(MxStore from, int64_t cols, T* out, int64_t stride, int64_t units)
+__global__ __launch_bounds__(kThreads) void mx_restore_kernel(MxStore from, int64_t rows, int64_t cols, T* out, int64_t stride)
 {
-    const int64_t unit = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
-    if (unit >= units) return;
-    const int64_t row = unit / from.chunks, chunk = unit - row * from.chunks;
-    const int64_t first = chunk * kMxChunk + (threadIdx.x & 31) * 8;
-    if (first >= cols) return;
+    const int64_t row = row_of_thread(), first = (int64_t)blockIdx.x * kMxChunk + (threadIdx.x & 31) * 8;
+    if (row >= rows || first >= cols) return;
     const uint32_t codes = *reinterpret_cast<const uint32_t*>(from.codes + row * (from.chunks * 128) + (first >> 1));
     const uint32_t s = from.scales[mx_scale_at(row, first >> 5, from.chunks)];
     // byte 0 is 2^-127, byte 255 no number; the product is exact but for numbers over the largest
@@ -252,9 +231,9 @@ __global__ __launch_bounds__(kThreads) void mx_restore_kernel(MxStore from, int6
 template <typename T>
 hipError_t rows_of(const void* x, int64_t rows, int64_t cols, int64_t stride, const MxStore& to, hipStream_t s)
 {
-    const int64_t units = rows * to.chunks, groups = (units + kThreads / 32 - 1) / (kThreads / 32);
-    if (groups > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((mx_rows_kernel<T>), dim3((uint32_t)groups), dim3(kThreads), 0, s, static_cast<const T*>(x), rows, cols, stride, to, units);
+    dim3 grid;
+    if (!grid_of(rows, to.chunks, grid)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((mx_rows_kernel<T>), grid, dim3(kThreads), 0, s, static_cast<const T*>(x), rows, cols, stride, to);
     return hipGetLastError();
 }
 
@@ -275,9 +254,9 @@ hipError_t tiles_of(const void* x, int64_t rows, int64_t cols, int64_t stride, c
 template <typename T>
 hipError_t restore_of(const MxStore& from, int64_t rows, int64_t cols, void* out, int64_t stride, hipStream_t s)
 {
-    const int64_t units = rows * from.chunks, groups = (units + kThreads / 32 - 1) / (kThreads / 32);
-    if (groups > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((mx_restore_kernel<T>), dim3((uint32_t)groups), dim3(kThreads), 0, s, from, cols, static_cast<T*>(out), stride, units);
+    dim3 grid;
+    if (!grid_of(rows, from.chunks, grid)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((mx_restore_kernel<T>), grid, dim3(kThreads), 0, s, from, rows, cols, static_cast<T*>(out), stride);
     return hipGetLastError();
 }
 
