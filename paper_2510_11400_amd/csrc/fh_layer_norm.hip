@@ -7,23 +7,9 @@ namespace {
 // Columns up to which a row is held in registers: by a wave, and by a workgroup of 1024.
 constexpr int64_t kWaveCols = 2048, kGroupCols = 16384;
 
-// The sum of v over the T threads that share a row (a workgroup's rows are T threads each).  `s_sums` holds a value per wave; the
-// calls of a workgroup take its two halves in turn, so that one barrier a call is enough: a wave writes a half again only
-// after the barrier of the call between, which every wave enters when it has read that half.
-template <int T>
-__device__ __forceinline__ float row_sum(float v, float (&s_sums)[2][16], int turn)
-{
-    if constexpr (T <= 64) return lane_sum<T>(v);
-    v = lane_sum<64>(v);
-    float* sums = s_sums[turn & 1];
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = v;
-    __syncthreads();
-    const float* mine = sums + threadIdx.x / T * (T / 64);
-    v = 0.0f;
-    for (int w = 0; w < T / 64; ++w) v += mine[w];
-    return v;
-}
-// The same for two values.
+// The sums of v and of u over the T threads that share a row (a workgroup's rows are T threads each).  `s_pairs` holds two
+// values per wave; the calls of a workgroup take its two halves in turn, so that one barrier a call is enough: a wave writes a half
+// again only after the barrier of the call between, which every wave enters when it has read that half.
 template <int T>
 __device__ __forceinline__ void row_sums(float& v, float& u, f32x2 (&s_pairs)[2][16], int turn)
 {
@@ -40,67 +26,135 @@ __device__ __forceinline__ void row_sums(float& v, float& u, f32x2 (&s_pairs)[2]
     }
 }
 
+// Mean and sum of squares about it of a row whose T threads hold `sum` of its values, and whose squares about any mean
+// `about(mean)` gives.  Each wave takes the squares about its own mean, and one barrier brings the waves' sums and squares
+// together: with n_w values of mean m_w in wave w the squares about the row's mean m are sum_w (squares_w + n_w (m_w - m)^2), which
+// costs no digits either.  `s_counts`: n_w.
+template <int T, typename About>
+__device__ __forceinline__ void row_moments(float sum, float columns, float& mean, float& squares, About about, f32x2 (&s_pairs)[2][16],
+                                            const float (&s_counts)[16], int turn)
+{
+    if constexpr (T <= 64) {
+        mean = lane_sum<T>(sum) / columns;
+        squares = lane_sum<T>(about(mean));
+    } else {
+        const int wave = threadIdx.x >> 6;
+        const float all = lane_sum<64>(sum), count = s_counts[wave % (T / 64)];
+        const float inside = lane_sum<64>(about(count > 0.0f ? all / count : 0.0f));
+        f32x2* pairs = s_pairs[turn & 1];
+        if ((threadIdx.x & 63) == 0) pairs[wave] = f32x2{all, inside};
+        __syncthreads();
+        const f32x2* mine = pairs + threadIdx.x / T * (T / 64);
+        float total = 0.0f;
+#pragma unroll 4
+        for (int w = 0; w < T / 64; ++w) total += mine[w].x;
+        mean = total / columns;
+        squares = 0.0f;
+#pragma unroll 4
+        for (int w = 0; w < T / 64; ++w) {
+            const float n = s_counts[w], d = n > 0.0f ? mine[w].x / n - mean : 0.0f;
+            squares += __builtin_fmaf(n * d, d, mine[w].y);
+        }
+    }
+}
+
 // ---- forward: a row in the registers of T threads, NV runs of eight values each ------------
 // Where the rows go: dense (MX false: y and its row stride), or as codes.
 struct NormOut { void* y; uint8_t* scales; int64_t stride_or_chunks; };
 
+// A workgroup stays, with the parameters of its threads' columns in registers, and takes rows a grid apart, the next one on its way
+// while one is worked on: with a workgroup a row the parameters came from L2 for every row, up to four times the bytes of a
+// bf16 row (8192 x 768 bf16: 9.6 us).  The rows have columns in every run, so that only the last runs can end early.
+template <int THREADS> constexpr int kNormGroup = THREADS <= 64 ? 256 : THREADS;     // threads of a workgroup
 template <typename T, int THREADS, int NV, bool MX>
-__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_rows_kernel(const T* x, int64_t rows, int64_t cols, int64_t x_stride,
-                                                                                  NormArgs n, NormOut to)
+__global__ __launch_bounds__(kNormGroup<THREADS>) void norm_rows_kernel(const T* x, int64_t rows, int64_t cols, int64_t x_stride,
+                                                                                  NormArgs n, NormOut to, int32_t groups)
 {
-    __shared__ float s_sums[2][16];
-    const int t = threadIdx.x % THREADS;
-    const int64_t row = (int64_t)blockIdx.x * (THREADS < 256 ? 256 / THREADS : 1) + threadIdx.x / THREADS;
-    const bool write = row < rows;
-    const T* p = x + (write ? row : rows - 1) * x_stride;
-    float v[NV][8];
-    float sum = 0.0f;
+    constexpr int kRows = kNormGroup<THREADS> / THREADS, kWhole = NV - 1;
+    __shared__ f32x2 s_pairs[2][16];
+    __shared__ float s_counts[16];                               // columns of a row's waves
+    const int t = threadIdx.x % THREADS, part = threadIdx.x / THREADS;
+    Run<T> next[NV];
+    auto load = [&](int64_t row) {
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int64_t first = ((int64_t)k * THREADS + t) * 8;
-        load8(p + first, cols - first, v[k]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum += v[k][i];
-    }
-    const float mean = row_sum<THREADS>(sum, s_sums, 0) / (float)cols;
-    // the squares of what is left, so that a mean far from zero costs no digits
-    float squares = 0.0f;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const int64_t first = ((int64_t)k * THREADS + t) * 8;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float d = first + i < cols ? v[k][i] - mean : 0.0f;
-            squares = __builtin_fmaf(d, d, squares);
+        for (int k = 0; k < NV; ++k) {
+            const int64_t first = ((int64_t)k * THREADS + t) * 8;
+            next[k].load(x + (row < rows ? row : 0) * x_stride + first, row < rows ? cols - first : 0);
         }
+    };
+    load((int64_t)blockIdx.x * kRows + part);
+    if constexpr (THREADS > 64) {
+        if (threadIdx.x < THREADS / 64) {
+            const int64_t end = cols - (int64_t)kWhole * THREADS * 8 - threadIdx.x * 512;      // of the last run
+            s_counts[threadIdx.x] = (float)(kWhole * 512 + (end < 0 ? 0 : end < 512 ? end : 512));
+        }
+        __syncthreads();
     }
-    const float rstd = 1.0f / __builtin_sqrtf(row_sum<THREADS>(squares, s_sums, 1) / (float)cols + n.eps);
-    if (write && t == 0) {
-        if (n.mean) n.mean[row] = mean;
-        if (n.rstd) n.rstd[row] = rstd;
-    }
-    if (!to.y) return;
+    float w[NV][8], b[NV][8];
+    int left[NV];                                                // columns of a run
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         const int64_t first = ((int64_t)k * THREADS + t) * 8;
-        float w[8], b[8];
+        left[k] = (int)(cols - first < 0 ? 0 : cols - first < 8 ? cols - first : 8);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { w[k][i] = 1.0f; b[k][i] = 0.0f; }
         if (n.p_dtype == FH_F32) {
-            if (n.weight) load8(static_cast<const float*>(n.weight) + first, cols - first, w);
-            if (n.bias) load8(static_cast<const float*>(n.bias) + first, cols - first, b);
+            if (n.weight) load8(static_cast<const float*>(n.weight) + first, left[k], w[k]);
+            if (n.bias) load8(static_cast<const float*>(n.bias) + first, left[k], b[k]);
         } else {
-            if (n.weight) load8(static_cast<const Bf16*>(n.weight) + first, cols - first, w);
-            if (n.bias) load8(static_cast<const Bf16*>(n.bias) + first, cols - first, b);
+            if (n.weight) load8(static_cast<const Bf16*>(n.weight) + first, left[k], w[k]);
+            if (n.bias) load8(static_cast<const Bf16*>(n.bias) + first, left[k], b[k]);
         }
+    }
+    const int64_t step = (int64_t)groups * kRows;
+    const float columns = (float)cols;
+    int turn = 0;
+    for (int64_t start = (int64_t)blockIdx.x * kRows; start < rows; start += step, ++turn) {
+        const int64_t row = start + part;
+        const bool write = row < rows;
+        float v[NV][8];
+        float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            v[k][i] = norm_value(v[k][i], mean, rstd, n.weight ? w[i] : 1.0f, n.bias ? b[i] : 0.0f);
-        if constexpr (!MX) {
-            if (write) store8(static_cast<T*>(to.y) + row * to.stride_or_chunks + first, cols - first, v[k]);
-        } else {
+        for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[k][i] = first + i < cols ? v[k][i] : 0.0f;
-            mx_write8(MxStore{static_cast<uint8_t*>(to.y), to.scales, to.stride_or_chunks}, row, first, v[k],
-                      write && first < to.stride_or_chunks * kMxChunk);
+            for (int i = 0; i < 8; ++i) {
+                v[k][i] = next[k].at(i);
+                sum += v[k][i];
+            }
+        if (start + step < rows) load(row + step);
+        // the squares of what is left, so that a mean far from zero costs no digits
+        const auto about = [&](float m) {
+            float squares = 0.0f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float d = k < kWhole || i < left[k] ? v[k][i] - m : 0.0f;
+                    squares = __builtin_fmaf(d, d, squares);
+                }
+            return squares;
+        };
+        float mean, squares;
+        row_moments<THREADS>(sum, columns, mean, squares, about, s_pairs, s_counts, turn);
+        const float rstd = 1.0f / __builtin_sqrtf(squares / columns + n.eps);
+        if (write && t == 0) {
+            if (n.mean) n.mean[row] = mean;
+            if (n.rstd) n.rstd[row] = rstd;
+        }
+        if (!to.y) continue;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int64_t first = ((int64_t)k * THREADS + t) * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[k][i] = norm_value(v[k][i] - mean, rstd, w[k][i], b[k][i]);
+            if constexpr (!MX) {
+                if (write) store8(static_cast<T*>(to.y) + row * to.stride_or_chunks + first, left[k], v[k]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[k][i] = k < kWhole || i < left[k] ? v[k][i] : 0.0f;
+                mx_write8(MxStore{static_cast<uint8_t*>(to.y), to.scales, to.stride_or_chunks}, row, first, v[k],
+                          write && first < to.stride_or_chunks * kMxChunk);
+            }
         }
     }
 }
@@ -109,7 +163,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void norm_rows_kerne
 template <typename T, bool MX>
 __global__ __launch_bounds__(1024) void norm_long_rows_kernel(const T* x, int64_t cols, int64_t x_stride, NormArgs n, NormOut to)
 {
-    __shared__ float s_sums[2][16];
+    __shared__ f32x2 s_pairs[2][16];
     const int64_t row = blockIdx.x;
     const T* p = x + row * x_stride;
     const int64_t end = mx_chunks(cols) * kMxChunk;             // whole waves have the same number of turns
@@ -118,7 +172,9 @@ __global__ __launch_bounds__(1024) void norm_long_rows_kernel(const T* x, int64_
         load8(p + first, cols - first, v);
         for (int i = 0; i < 8; ++i) sum += v[i];
     }
-    const float mean = row_sum<1024>(sum, s_sums, 0) / (float)cols;
+    float none = 0.0f;
+    row_sums<1024>(sum, none, s_pairs, 0);
+    const float mean = sum / (float)cols;
     float squares = 0.0f;
     for (int64_t first = threadIdx.x * 8; first < cols; first += 8192) {
         load8(p + first, cols - first, v);
@@ -127,7 +183,8 @@ __global__ __launch_bounds__(1024) void norm_long_rows_kernel(const T* x, int64_
             squares = __builtin_fmaf(d, d, squares);
         }
     }
-    const float rstd = 1.0f / __builtin_sqrtf(row_sum<1024>(squares, s_sums, 1) / (float)cols + n.eps);
+    row_sums<1024>(squares, none, s_pairs, 1);
+    const float rstd = 1.0f / __builtin_sqrtf(squares / (float)cols + n.eps);
     if (threadIdx.x == 0) {
         if (n.mean) n.mean[row] = mean;
         if (n.rstd) n.rstd[row] = rstd;
@@ -138,7 +195,7 @@ __global__ __launch_bounds__(1024) void norm_long_rows_kernel(const T* x, int64_
         load8(p + first, cols - first, v);
         for (int i = 0; i < 8; ++i) {
             const int64_t c = first + i;
-            v[i] = c < cols ? norm_value(v[i], mean, rstd, parameter(n.weight, n.p_dtype, c, 1.0f), parameter(n.bias, n.p_dtype, c, 0.0f)) : 0.0f;
+            v[i] = c < cols ? norm_value(v[i] - mean, rstd, parameter(n.weight, n.p_dtype, c, 1.0f), parameter(n.bias, n.p_dtype, c, 0.0f)) : 0.0f;
         }
         if constexpr (!MX) store8(static_cast<T*>(to.y) + row * to.stride_or_chunks + first, cols - first, v);
         else mx_write8(MxStore{static_cast<uint8_t*>(to.y), to.scales, to.stride_or_chunks}, row, first, v, first < end);
@@ -351,10 +408,13 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const float* partial, i
 template <typename T, int THREADS, int NV, bool MX>
 hipError_t norm_of(const void* x, int64_t rows, int64_t cols, int64_t xs, const NormArgs& n, const NormOut& to, hipStream_t s)
 {
-    constexpr int kRows = THREADS < 256 ? 256 / THREADS : 1;
-    const int64_t groups = (rows + kRows - 1) / kRows;
-    hipLaunchKernelGGL((norm_rows_kernel<T, THREADS, NV, MX>), dim3((uint32_t)groups), dim3(THREADS < 256 ? 256 : THREADS), 0, s,
-                       static_cast<const T*>(x), rows, cols, xs, n, to);
+    // workgroups that stay: what 256 compute units hold, by the threads that NV runs' registers allow on one
+    constexpr int kThreads = kNormGroup<THREADS>, kRows = kThreads / THREADS, kHeld = NV == 1 ? 2048 : NV == 2 ? 1280 : NV == 3 ? 1024 : 768;
+    constexpr int64_t kStay = kHeld < kThreads ? 256 : 256 * (kHeld / kThreads);
+    int64_t groups = (rows + kRows - 1) / kRows;
+    if (groups > kStay) groups = kStay;
+    hipLaunchKernelGGL((norm_rows_kernel<T, THREADS, NV, MX>), dim3((uint32_t)groups), dim3(kThreads), 0, s, static_cast<const T*>(x), rows, cols,
+                       xs, n, to, (int32_t)groups);
     return hipGetLastError();
 }
 template <typename T, bool MX>
@@ -368,10 +428,20 @@ hipError_t norm_any(const void* x, int64_t rows, int64_t cols, int64_t xs, const
     if (cols <= 256) return norm_of<T, 32, 1, MX>(x, rows, cols, xs, n, to, s);
     if (cols <= 512) return norm_of<T, 64, 1, MX>(x, rows, cols, xs, n, to, s);
     if (cols <= 1024) return norm_of<T, 64, 2, MX>(x, rows, cols, xs, n, to, s);
+    if (cols <= 1536) return norm_of<T, 64, 3, MX>(x, rows, cols, xs, n, to, s);
     if (cols <= kWaveCols) return norm_of<T, 64, 4, MX>(x, rows, cols, xs, n, to, s);
-    if (cols <= 4096) return norm_of<T, 256, 2, MX>(x, rows, cols, xs, n, to, s);
-    if (cols <= 8192) return norm_of<T, 1024, 1, MX>(x, rows, cols, xs, n, to, s);
-    if (cols <= kGroupCols) return rows >= 512 ? norm_of<T, 512, 4, MX>(x, rows, cols, xs, n, to, s) : norm_of<T, 1024, 2, MX>(x, rows, cols, xs, n, to, s);
+    if (rows <= 256) {                                           // no more than a row a compute unit: all the threads it can use
+        if (cols <= 4096) return norm_of<T, 512, 1, MX>(x, rows, cols, xs, n, to, s);
+        if (cols <= 8192) return norm_of<T, 1024, 1, MX>(x, rows, cols, xs, n, to, s);
+        if (cols <= kGroupCols) return norm_of<T, 1024, 2, MX>(x, rows, cols, xs, n, to, s);
+    } else {
+        if (cols <= 3072) return norm_of<T, 128, 3, MX>(x, rows, cols, xs, n, to, s);
+        if (cols <= 4096) return norm_of<T, 128, 4, MX>(x, rows, cols, xs, n, to, s);
+        if (cols <= 6144) return norm_of<T, 256, 3, MX>(x, rows, cols, xs, n, to, s);
+        if (cols <= 8192) return norm_of<T, 256, 4, MX>(x, rows, cols, xs, n, to, s);
+        if (cols <= 12288) return norm_of<T, 512, 3, MX>(x, rows, cols, xs, n, to, s);
+        if (cols <= kGroupCols) return norm_of<T, 512, 4, MX>(x, rows, cols, xs, n, to, s);
+    }
     hipLaunchKernelGGL((norm_long_rows_kernel<T, MX>), dim3((uint32_t)rows), dim3(1024), 0, s, static_cast<const T*>(x), cols, xs, n, to);
     return hipGetLastError();
 }

@@ -31,11 +31,6 @@ __global__ __launch_bounds__(kThreads) void mx_rows_kernel(const T* x, int64_t r
     mx_write8(to, row, first, v, write);
 }
 
-__device__ __forceinline__ float lane_value(float v, int lane)
-{
-    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
-}
-
 // ---- tiles: blocks along the columns, along the rows, or both ------------------------------
 // A wave holds 32 rows x 256 bytes.  It reads them by 16 bytes a lane, eight values of a row each, whose blocks are quads
 // of lanes, and passes them through LDS to have the 32 values of a column in one lane (two columns in bf16), whose block is
@@ -56,9 +51,11 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
     constexpr int kCols = kTileCols<T>, kLanes = kCols / 8, kAtOnce = 64 / kLanes, kGroups = 32 / kAtOnce, kEach = kCols / 64;
     __shared__ __attribute__((aligned(16))) uint8_t s_area[8 * kWaveBytes];
     __shared__ uint32_t s_scales[kCols * 2];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ __attribute__((aligned(16))) f32x2 s_stats[NORM ? 8 : 1][32];   // mean and 1 / deviation of a wave's rows
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t col_tile = blockIdx.x % col_tiles, row_tile = blockIdx.x / col_tiles;
     const int64_t r0 = row_tile * kTileRows + wave * 32, c0 = col_tile * kCols;
+    const bool whole = r0 + 32 <= rows && c0 + kCols <= cols;
     uint8_t* area = s_area + wave * kWaveBytes;
 
     // as rows: lane (row % kAtOnce, column / 8)
@@ -68,6 +65,11 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
     for (int g = 0; g < kGroups; ++g) {
         const int64_t row = r0 + g * kAtOnce + lane / kLanes;
         run[g].load(x + (row < rows ? row : 0) * stride + row_c, row < rows ? cols - row_c : 0);
+    }
+    if constexpr (NORM) {
+        const int64_t row = r0 + (lane & 31) < rows ? r0 + (lane & 31) : rows - 1;
+        s_stats[wave][lane & 31] = f32x2{n.mean[row], n.rstd[row]};
+        asm volatile("" ::: "memory");
     }
     // 65535 - h of the lane's columns: half-word i of a block is row 8g + i's
     u32x4 not_h[kEach][4];
@@ -106,9 +108,13 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
         float w[8], b[8];
         if constexpr (NORM) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                w[i] = row_c + i < cols ? parameter(n.weight, n.p_dtype, row_c + i, 1.0f) : 0.0f;
-                b[i] = row_c + i < cols ? parameter(n.bias, n.p_dtype, row_c + i, 0.0f) : 0.0f;
+            for (int i = 0; i < 8; ++i) { w[i] = 1.0f; b[i] = 0.0f; }
+            if (n.p_dtype == FH_F32) {
+                if (n.weight) load8(static_cast<const float*>(n.weight) + row_c, cols - row_c, w);
+                if (n.bias) load8(static_cast<const float*>(n.bias) + row_c, cols - row_c, b);
+            } else {
+                if (n.weight) load8(static_cast<const Bf16*>(n.weight) + row_c, cols - row_c, w);
+                if (n.bias) load8(static_cast<const Bf16*>(n.bias) + row_c, cols - row_c, b);
             }
         }
 #pragma unroll
@@ -119,9 +125,13 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = run[g].at(i);
             if constexpr (NORM) {
-                const float mean = row < rows ? n.mean[row] : 0.0f, rstd = row < rows ? n.rstd[row] : 0.0f;
+                const f32x2 st = s_stats[wave][in_area];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = row_c + i < cols ? norm_value(v[i], mean, rstd, w[i], b[i]) : 0.0f;
+                for (int i = 0; i < 8; ++i) v[i] = norm_value(v[i] - st.x, st.y, w[i], b[i]);
+                if (!whole) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = row_c + i < cols ? v[i] : 0.0f;
+                }
             }
             if constexpr (STOCHASTIC) {
                 const u32x4 u = *reinterpret_cast<const u32x4*>(area + in_area * (kCols * 2) + (lane % kLanes) * 16);
@@ -142,12 +152,6 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
     if (!STOCHASTIC && rows_form) write_rows();
     if (columns_form) {
         asm volatile("" ::: "memory");                           // a wave's own LDS accesses are in order
-        // lane i of the wave fetches row i's statistics; rows and columns past the last stay zeros, whatever the bias
-        float means = 0.0f, rstds = 0.0f;
-        if constexpr (NORM) {
-            const int64_t mine = r0 + (lane & 31);
-            if (mine < rows) { means = n.mean[mine]; rstds = n.rstd[mine]; }
-        }
         u32x4 q[kEach];
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {                        // one column at a time: both at once do not fit 128 registers
@@ -165,8 +169,15 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
                 const bool in = c0 + c < cols;
                 const float w = in ? parameter(n.weight, n.p_dtype, c0 + c, 1.0f) : 0.0f, b = in ? parameter(n.bias, n.p_dtype, c0 + c, 0.0f) : 0.0f;
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    v[i] = in && r0 + i < rows ? norm_value(v[i], lane_value(means, i), lane_value(rstds, i), w, b) : 0.0f;
+                for (int i = 0; i < 32; i += 2) {                // two rows' statistics by one read, the same for all lanes
+                    const f32x4 st = *reinterpret_cast<const f32x4*>(&s_stats[wave][i]);
+                    v[i] = norm_value(v[i] - st.x, st.y, w, b);
+                    v[i + 1] = norm_value(v[i + 1] - st.z, st.w, w, b);
+                }
+                if (!whole) {                                    // zeros stay zeros, whatever the bias
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = in && r0 + i < rows ? v[i] : 0.0f;
+                }
             }
             uint32_t top = 0;
 #pragma unroll

@@ -9,12 +9,9 @@
 
 namespace fh {
 
-// y of one value, in this order everywhere, so that a row's and a column's stored form of a norm's output come from the
-// same bits.
-__device__ __forceinline__ float norm_value(float x, float mean, float rstd, float w, float b)
-{
-    return __builtin_fmaf((x - mean) * rstd, w, b);
-}
+// y of one value, x less the mean, in this order everywhere, so that a row's and a column's stored form of a norm's output come
+// from the same bits.
+__device__ __forceinline__ float norm_value(float d, float rstd, float w, float b) { return __builtin_fmaf(d * rstd, w, b); }
 
 // A norm ahead of the quantiser; weight and bias may be null (1 and 0).
 struct NormArgs {
