@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
@@ -1562,11 +1563,17 @@ def fh_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor
 FH_MX_NEEDS_INPUT, FH_MX_NEEDS_WEIGHT = 1, 2
 
 
+@functools.lru_cache(maxsize=256)
+def _layer_sizes(tokens: int, features: int, out: int):
+    """Bytes that a layer keeps between its halves, and bytes of scratch."""
+    return _lib.fh_mx_layer_kept_bytes(tokens, features, out), _lib.fh_mx_layer_scratch_bytes(tokens, features, out)
+
+
 class MxLayer:
     """One pass through a linear layer in microscaled form: what its forward call keeps for its backward call.  x: [tokens,
     features], weight: [out, features]; `norm`: a layer norm ahead, with norm_weight and norm_bias (either may be None).  Parameters
     are of one dtype, and so are x, y and the gradients of both."""
-    __slots__ = ("args", "kept", "device", "dtype", "p_dtype")
+    __slots__ = ("args", "kept", "sizes", "device", "dtype", "p_dtype", "needs_input", "needs_weight", "norm")
 
     def __init__(self, x: torch.Tensor, weight: torch.Tensor, bias=None, norm: bool = False, norm_weight=None, norm_bias=None,
                  eps: float = 1e-5, needs_input: bool = True, needs_weight: bool = True, rounding="nearest", seed: int = 0,
@@ -1575,65 +1582,61 @@ class MxLayer:
         out, w_features, w_stride = _matrix(weight, "weight")
         if w_features != features:
             raise ValueError(f"x has {features} features, weight takes {w_features}")
-        device = self.device = x.device
+        device, p_dtype = x.device, weight.dtype
         _on_device(weight, device, "weight")
-        self.dtype, self.p_dtype = x.dtype, weight.dtype
-        for t, what in ((bias, "bias"), (norm_weight, "norm_weight"), (norm_bias, "norm_bias")):
-            if t is not None and t.dtype != weight.dtype:
-                raise TypeError(f"{what} is of {t.dtype}, weight of {weight.dtype}")
-        self.kept = None
+        if (bias is not None and bias.dtype != p_dtype) or (norm_weight is not None and norm_weight.dtype != p_dtype) or \
+                (norm_bias is not None and norm_bias.dtype != p_dtype):
+            raise TypeError(f"the parameters of one layer are of one dtype, as its weight: {p_dtype}")
+        self.device, self.dtype, self.p_dtype, self.kept = device, x.dtype, p_dtype, None
+        self.norm, self.needs_input, self.needs_weight = norm, needs_input, needs_weight
+        self.sizes = _layer_sizes(tokens, features, out)
         self.args = fh_mx_layer(tokens, features, out, _dtype_code(x), _dtype_code(weight), 1 if norm else 0,
                                 (FH_MX_NEEDS_INPUT if needs_input else 0) | (FH_MX_NEEDS_WEIGHT if needs_weight else 0),
                                 _ROUND[rounding], eps, seed & _MASK64, tensor_id & _MASK64, x.data_ptr(), x_stride,
                                 _vector(norm_weight, features, device, "norm_weight"), _vector(norm_bias, features, device, "norm_bias"),
                                 weight.data_ptr(), w_stride, _vector(bias, out, device, "bias"), None, None, out)
 
-    def _work(self, stream) -> torch.Tensor:
-        a = self.args
-        scratch = _scratch(_lib.fh_mx_layer_scratch_bytes(a.tokens, a.features, a.out_features), self.device, stream)
-        a.scratch, a.scratch_cap = scratch.data_ptr(), scratch.numel()
-        return scratch
-
     def forward(self, stream=None) -> torch.Tensor:
         """Enqueue the forward half; returns y."""
-        a = self.args
-        y = _new(a.tokens, a.out_features, self.dtype, self.device)
-        if a.norm or a.needs:
-            self.kept = torch.empty(_lib.fh_mx_layer_kept_bytes(a.tokens, a.features, a.out_features), dtype=torch.uint8, device=self.device)
-            a.kept, a.kept_cap = self.kept.data_ptr(), self.kept.numel()
-        scratch = self._work(stream)  # noqa: F841  (held until the call has been enqueued)
-        a.y = y.data_ptr()
-        _enqueue(self.device, stream, _lib.fh_mx_layer_forward, ctypes.byref(a))
+        a, device = self.args, self.device
+        kept_bytes, scratch_bytes = self.sizes
+        y = _new(a.tokens, a.out_features, self.dtype, device)
+        if self.norm or self.needs_input or self.needs_weight:
+            self.kept = torch.empty(kept_bytes, dtype=torch.uint8, device=device)
+            a.kept, a.kept_cap = self.kept.data_ptr(), kept_bytes
+        scratch = _scratch(scratch_bytes, device, stream)
+        a.y, a.scratch, a.scratch_cap = y.data_ptr(), scratch.data_ptr(), scratch_bytes
+        _enqueue(device, stream, _lib.fh_mx_layer_forward, ctypes.byref(a))
         return y
 
     def backward(self, dy: torch.Tensor, x: Optional[torch.Tensor] = None, norm_weight: Optional[torch.Tensor] = None, stream=None):
         """Enqueue the backward half; returns (dx, dweight, dnorm_weight, dnorm_bias), None for what is not needed.  With a norm x
         and norm_weight are the forward call's (x may have moved, as a saved tensor that was restored has)."""
-        a = self.args
-        tokens, out, a.dy_stride = _matrix(dy, "dy")
-        device, p_dtype, features = self.device, self.p_dtype, a.features
-        if (tokens, out) != (a.tokens, a.out_features) or dy.dtype != self.dtype:
+        a, device, p_dtype = self.args, self.device, self.p_dtype
+        tokens, out, dy_stride = _matrix(dy, "dy")
+        features = a.features
+        if tokens != a.tokens or out != a.out_features or dy.dtype != self.dtype:
             raise ValueError("dy must have the shape and the dtype of y")
         _on_device(dy, device, "dy")
         dx = dweight = dnorm_weight = dnorm_bias = None
-        if a.needs & FH_MX_NEEDS_WEIGHT:
+        if self.needs_weight:
             dweight = _new(out, features, p_dtype, device)
             a.dweight = dweight.data_ptr()
-        if a.needs & FH_MX_NEEDS_INPUT:
+        if self.needs_input:
             dx = _new(tokens, features, self.dtype, device)
             a.dx = dx.data_ptr()
-            if a.norm:
+            if self.norm:
                 if x is None:
                     raise ValueError("with a norm the backward call takes x again")
                 x_rows, x_cols, a.x_stride = _matrix(x, "x")
-                if (x_rows, x_cols) != (tokens, features) or x.dtype != self.dtype:
+                if x_rows != tokens or x_cols != features or x.dtype != self.dtype:
                     raise ValueError("x must have the shape and the dtype of the forward call's")
                 _on_device(x, device, "x")
                 dnorm_weight = torch.empty(features, dtype=p_dtype, device=device)
                 dnorm_bias = torch.empty_like(dnorm_weight)
                 a.x, a.norm_weight = x.data_ptr(), _vector(norm_weight, features, device, "norm_weight")
                 a.dnorm_weight, a.dnorm_bias = dnorm_weight.data_ptr(), dnorm_bias.data_ptr()
-        scratch = self._work(stream)  # noqa: F841
-        a.dy = dy.data_ptr()
+        scratch = _scratch(self.sizes[1], device, stream)
+        a.dy, a.dy_stride, a.scratch, a.scratch_cap = dy.data_ptr(), dy_stride, scratch.data_ptr(), self.sizes[1]
         _enqueue(device, stream, _lib.fh_mx_layer_backward, ctypes.byref(a))
         return dx, dweight, dnorm_weight, dnorm_bias

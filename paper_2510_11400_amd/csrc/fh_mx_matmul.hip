@@ -326,18 +326,19 @@ __global__ __launch_bounds__(256) void mx_join_kernel(const float* parts, int64_
 enum class Tile : int32_t { waves32, waves32_wide, waves64, square128, square256 };
 struct Plan { Tile tile; int32_t parts; int64_t chunks_each; };
 
-// Times in us (m x n x k, bf16 out), each kernel's against the next best:
-//   32 x 32 outputs a workgroup: up to three workgroups a compute unit.  1024 x 768 x 768 3.7 (64 x 64: 4.6), 700 x 700 x 8192 9.1 (11.5);
-//       1024^3 4.5 (4.8), 2048 x 768 x 768 5.9 (5.3).  Eight waves each while there is at most one a compute unit and every
-//       wave has a chunk: 300 x 300 x 8192 5.8 (four waves: 7.1), 700 x 700 x 8192 10.1 (9.1).
-//   64 x 64, four waves: up to about two a compute unit.  512 x 4096 x 4096 11.3 (128: 15.0), 2304 x 768 x 8192 19.5 (24.9),
-//       1500 x 1500 x 8192 24.0 (25.7); 4096 x 768 x 768 9.5 (7.1).
-//   256 against 128: a round of 256 workgroups takes about 10.4 + 1.82 us a chunk with the one, of 512 (two a compute unit) 5.6 + 0.99 with
-//       the other.  8192 x 8192 x 4096 156 (183), 4096 x 4096 x 1024 17.7 (19.2); 8192 x 2304 x 768 26.1 (20.2).
-// A sum is split over workgroups where its outputs leave compute units idle, in parts of sixteen chunks at least.
+// A sum is split over workgroups where its outputs leave compute units idle, in parts of sixteen chunks at least.  Otherwise the kernel
+// with the shortest time, in hundredths of a microsecond with c chunks, by lines through what they measured (bf16 out; us,
+// in the order 32 (four waves), 64, 128, 256):
+//     1024 x 768 x 768    3.7  4.6  6.6 11.9     700 x 700 x 8192    9.1 11.5 25.1 56.6     768 x 768 x 8192   12.3 10.9 25.5 57.4
+//     4096 x 768 x 768    9.4  9.5  7.1 12.4     512 x 4096 x 4096  15.3 11.3 15.0 32.3     2304 x 768 x 8192  25.0 19.5 24.9 55.5
+//     8192 x 2304 x 768  44.6 35.9 20.2 26.1     2048^3             17.7 14.0 10.9 20.5     3000^3             46.9 44.5 27.9 29.0
+//     4096 x 4096 x 1024 41.6 35.5 19.2 17.7     4096^3            100.4 67.3 43.0 39.5     8192 x 8192 x 4096  422  282  183  156
+// Workgroups of a kernel run in rounds of 256 (32: up to four a compute unit share it; 128: two, which one round of 512 makes).
+// Up to one tile of 32 a compute unit, eight waves share its sum where each has a chunk (300 x 300 x 8192 7.1 -> 5.8).
 Plan plan_of(int64_t m, int64_t n, int64_t k)
 {
     const auto tiles = [&](int64_t side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
+    const auto rounds = [&](int64_t side) { return (tiles(side) + 255) / 256; };
     const int64_t chunks = mx_chunks(k), small = tiles(32);
     if (small <= 128 && chunks >= 32) {
         int64_t parts = 256 / small;
@@ -346,10 +347,13 @@ Plan plan_of(int64_t m, int64_t n, int64_t k)
         return Plan{Tile::waves32_wide, (int32_t)((chunks + each - 1) / each), each};
     }
     if (small <= 256 && chunks >= 8) return Plan{Tile::waves32_wide, 1, chunks};
-    if (small <= 768) return Plan{Tile::waves32, 1, chunks};
-    if (tiles(64) <= 576) return Plan{Tile::waves64, 1, chunks};
-    const int64_t large = 2 * ((tiles(256) + 255) / 256) * (104 + 18 * chunks), middle = (tiles(128) + 255) / 256 * (56 + 10 * chunks);
-    return Plan{large < middle ? Tile::square256 : Tile::square128, 1, chunks};
+    const int64_t times[4] = {290 + rounds(32) * 10 * chunks, 340 + rounds(64) * (90 + 22 * chunks),
+                              tiles(128) <= 256 ? 490 + 65 * chunks : (560 + 99 * chunks) * tiles(128) / 512, rounds(256) * (1040 + 182 * chunks)};
+    const Tile kernels[4] = {Tile::waves32, Tile::waves64, Tile::square128, Tile::square256};
+    int best = 0;
+    for (int i = 1; i < 4; ++i)
+        if (times[i] < times[best]) best = i;
+    return Plan{kernels[best], 1, chunks};
 }
 
 template <typename T, int MT, int NT, int WAVES>

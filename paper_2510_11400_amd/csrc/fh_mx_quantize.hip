@@ -7,15 +7,15 @@ namespace {
 constexpr int kThreads = 256;
 
 // ---- by rows, nearest, and back: a chunk of a row is half a wave's, 8 values a lane --------------
-// A workgroup takes one chunk of eight rows, the grid is (chunks, rows / 8, and a third dimension where that passes the second's
+// A workgroup takes one chunk of eight (four) rows, the grid is (chunks, rows / 8, and a third dimension where that passes the second's
 // limit): no thread divides.  With a division of 64 bits in every thread the kernels, which have little else to do, took a third longer.
 // Bound by memory: 2 or 4 bytes a value on the plain side, 17/32 on the stored one.
-constexpr int kRowsAtOnce = kThreads / 32;
 constexpr int64_t kMostGridY = 65535;
-__device__ __forceinline__ int64_t row_of_thread() { return ((int64_t)blockIdx.z * kMostGridY + blockIdx.y) * kRowsAtOnce + threadIdx.x / 32; }
-inline bool grid_of(int64_t rows, int64_t chunks, dim3& grid)
+template <int LANES>
+__device__ __forceinline__ int64_t row_of_thread() { return ((int64_t)blockIdx.z * kMostGridY + blockIdx.y) * (kThreads / LANES) + threadIdx.x / LANES; }
+inline bool grid_of(int64_t rows, int64_t chunks, int lanes, dim3& grid)
 {
-    const int64_t groups = (rows + kRowsAtOnce - 1) / kRowsAtOnce, z = (groups + kMostGridY - 1) / kMostGridY;
+    const int64_t at_once = kThreads / lanes, groups = (rows + at_once - 1) / at_once, z = (groups + kMostGridY - 1) / kMostGridY;
     if (z > kMostGridY || chunks > INT32_MAX) return false;
     grid = dim3((uint32_t)chunks, (uint32_t)(z > 1 ? kMostGridY : groups), (uint32_t)z);
     return true;
@@ -24,7 +24,7 @@ inline bool grid_of(int64_t rows, int64_t chunks, dim3& grid)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void mx_rows_kernel(const T* x, int64_t rows, int64_t cols, int64_t stride, MxStore to)
 {
-    const int64_t row = row_of_thread(), first = (int64_t)blockIdx.x * kMxChunk + (threadIdx.x & 31) * 8;
+    const int64_t row = row_of_thread<32>(), first = (int64_t)blockIdx.x * kMxChunk + (threadIdx.x & 31) * 8;
     const bool write = row < rows;
     float v[8];
     load8(x + (write ? row : 0) * stride + first, write ? cols - first : 0, v);
@@ -222,28 +222,36 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
     if (STOCHASTIC && rows_form) write_rows();
 }
 
+// 16 bytes of output a lane: 4 values in fp32, 8 in bf16.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void mx_restore_kernel(MxStore from, int64_t rows, int64_t cols, T* out, int64_t stride)
 {
-    const int64_t row = row_of_thread(), first = (int64_t)blockIdx.x * kMxChunk + (threadIdx.x & 31) * 8;
+    constexpr int kEach = 16 / (int)sizeof(T), kLanes = kMxChunk / kEach;
+    const int64_t row = row_of_thread<kLanes>(), first = (int64_t)blockIdx.x * kMxChunk + (threadIdx.x % kLanes) * kEach;
     if (row >= rows || first >= cols) return;
-    const uint32_t codes = *reinterpret_cast<const uint32_t*>(from.codes + row * (from.chunks * 128) + (first >> 1));
+    const uint8_t* at = from.codes + row * (from.chunks * 128) + (first >> 1);
+    uint32_t codes;
+    if constexpr (kEach == 8) codes = *reinterpret_cast<const uint32_t*>(at);
+    else codes = *reinterpret_cast<const uint16_t*>(at);
     const uint32_t s = from.scales[mx_scale_at(row, first >> 5, from.chunks)];
     // byte 0 is 2^-127, byte 255 no number; the product is exact but for numbers over the largest
     const float scale = __builtin_bit_cast(float, s == 0u ? 0x00400000u : s == 255u ? 0x7FC00000u : s << 23);
-    float v[8];
-    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 1),
-                c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 3);
-    v[0] = a.x * scale; v[1] = a.y * scale; v[2] = b.x * scale; v[3] = b.y * scale;
-    v[4] = c.x * scale; v[5] = c.y * scale; v[6] = d.x * scale; v[7] = d.y * scale;
-    store8(out + row * stride + first, cols - first, v);
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 1);
+    if constexpr (kEach == 8) {
+        const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, 3);
+        const float v[8] = {a.x * scale, a.y * scale, b.x * scale, b.y * scale, c.x * scale, c.y * scale, d.x * scale, d.y * scale};
+        store8(out + row * stride + first, cols - first, v);
+    } else {
+        const float v[4] = {a.x * scale, a.y * scale, b.x * scale, b.y * scale};
+        store4(out + row * stride + first, cols - first, v);
+    }
 }
 
 template <typename T>
 hipError_t rows_of(const void* x, int64_t rows, int64_t cols, int64_t stride, const MxStore& to, hipStream_t s)
 {
     dim3 grid;
-    if (!grid_of(rows, to.chunks, grid)) return hipErrorInvalidValue;
+    if (!grid_of(rows, to.chunks, 32, grid)) return hipErrorInvalidValue;
     hipLaunchKernelGGL((mx_rows_kernel<T>), grid, dim3(kThreads), 0, s, static_cast<const T*>(x), rows, cols, stride, to);
     return hipGetLastError();
 }
@@ -266,7 +274,7 @@ template <typename T>
 hipError_t restore_of(const MxStore& from, int64_t rows, int64_t cols, void* out, int64_t stride, hipStream_t s)
 {
     dim3 grid;
-    if (!grid_of(rows, from.chunks, grid)) return hipErrorInvalidValue;
+    if (!grid_of(rows, from.chunks, sizeof(T) == 4 ? 64 : 32, grid)) return hipErrorInvalidValue;
     hipLaunchKernelGGL((mx_restore_kernel<T>), grid, dim3(kThreads), 0, s, from, rows, cols, static_cast<T*>(out), stride);
     return hipGetLastError();
 }

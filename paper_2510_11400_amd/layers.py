@@ -63,9 +63,9 @@ class _MxLinear(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         needs, layer, g = ctx.needs_input_grad, ctx.layer, _rows(dy)
-        x, norm_weight = ctx.saved_tensors if layer.args.norm and layer.args.needs & api.FH_MX_NEEDS_INPUT else (None, None)
+        x, norm_weight = ctx.saved_tensors if layer.norm and layer.needs_input else (None, None)
         dx = dw = d_norm_weight = d_norm_bias = None
-        if layer.args.needs:
+        if layer.needs_input or layer.needs_weight:
             dx, dw, d_norm_weight, d_norm_bias = layer.backward(g, x, norm_weight)
         db = g.float().sum(0).to(ctx.bias_dtype) if needs[4] else None
         return (dx.view(ctx.shape) if needs[0] else None, d_norm_weight if needs[1] else None, d_norm_bias if needs[2] else None, dw, db,
