@@ -1,4 +1,5 @@
-"""Thin ctypes binding over libfedhybrid.so: argument marshalling only.
+"""Thin binding over libfedhybrid.so (ctypes, and compiled for the calls whose kernels take no longer than that): argument
+marshalling only.
 
 Every step of the method runs in the HIP kernels behind the C ABI declared in
 include/fedhybrid.h (FedHybrid Section 3: compress in the forward pass, decompress in
@@ -10,7 +11,6 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
-import functools
 import os
 from dataclasses import dataclass
 from typing import List, Optional, Sequence
@@ -20,12 +20,15 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libfedhybrid.so")
 
-if not os.path.exists(_LIB_PATH):
-    raise ImportError(
-        f"{_LIB_PATH} is missing: build it with `python -m paper_2510_11400_amd.build` "
-        "(hipcc, gfx950). There is no fallback implementation.")
+for _path in (_LIB_PATH, os.path.join(_HERE, "_fh_binding.so")):
+    if not os.path.exists(_path):
+        raise ImportError(
+            f"{_path} is missing: build it with `python -m paper_2510_11400_amd.build` "
+            "(hipcc, gfx950). There is no fallback implementation.")
 
 _lib = ctypes.CDLL(_LIB_PATH)
+
+from . import _fh_binding as _binding  # noqa: E402  (finds the library loaded)
 
 FH_F32, FH_BF16 = 0, 1
 FH_ROUND_NEAREST, FH_ROUND_STOCHASTIC = 0, 1
@@ -1306,8 +1309,7 @@ def fh_mix_decompress_batch(batch: MixBatch, stream=None) -> None:
 
 
 # ---- microscaled 4-bit storage, its product, layer norm ---------------------------------------------------
-# A launch takes the host about 3 us, a small product or norm the device as long: these functions ask a tensor for nothing
-# twice, and not the library for what a line of arithmetic gives.
+# These kernels take a few us for small inputs, as long as Python takes to marshal a call: _fh_binding does it compiled.
 _MOST = 2 ** 31 - 256
 
 
@@ -1333,120 +1335,18 @@ class MxMatrix:
         return self.data.numel()
 
 
-_current_device = torch._C._cuda_getDevice
-_current_stream = torch._C._cuda_getCurrentRawStream
-_MASK64 = 0xFFFFFFFFFFFFFFFF
-
-
-def _enqueue(device, stream: Optional[torch.cuda.Stream], call, *args) -> None:
-    """call(*args, stream's handle) with `device` the current one."""
-    index = _current_device()
-    if device.index == index:
-        status = call(*args, _current_stream(index) if stream is None else stream.cuda_stream)
-    else:
-        with torch.cuda.device(device):
-            status = call(*args, _stream_ptr(stream))
-    if status:
-        raise FedHybridError(status)
-
-
-def _on_device(t: torch.Tensor, device, what: str) -> None:
-    if t.device != device:
-        raise ValueError(f"{what} lives on {t.device}, other tensors of the call on {device}")
-
-
-def _matrix(t: torch.Tensor, what: str):
-    """(rows, cols, row stride) of a device matrix whose rows are contiguous."""
-    if not t.is_cuda:
-        raise ValueError(f"{what} must live in device memory (got a {t.device} tensor)")
-    if t.dim() != 2:
-        raise ValueError(f"{what} must have two dimensions (got {t.dim()})")
-    rows, cols = t.shape
-    stride, step = t.stride()
-    if step != 1 and cols > 1:
-        raise ValueError(f"the rows of {what} must be contiguous")
-    if rows <= 1:
-        stride = cols
-    if stride < cols:
-        raise ValueError(f"the rows of {what} overlap")
-    return rows, cols, stride
-
-
-def _vector(t: Optional[torch.Tensor], n: int, device, what: str) -> Optional[int]:
-    """The address of a vector of n values, None for none."""
-    if t is None:
-        return None
-    if t.device != device or t.shape != (n,) or not t.is_contiguous():
-        _on_device(_device_tensor(t, what), device, what)
-        raise ValueError(f"{what} must be a vector of {n} values")
-    return t.data_ptr()
-
-
-def _parameters(weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], cols: int, device):
-    """(weight's pointer, bias's pointer, their dtype code)"""
-    if weight is None:
-        return (None, None, FH_F32) if bias is None else (None, _vector(bias, cols, device, "bias"), _dtype_code(bias))
-    if bias is not None and weight.dtype != bias.dtype:
-        raise TypeError(f"weight and bias have different dtypes ({weight.dtype}, {bias.dtype})")
-    return _vector(weight, cols, device, "weight"), _vector(bias, cols, device, "bias"), _dtype_code(weight)
-
-
-def _new_store(rows: int, cols: int, device) -> MxMatrix:
-    return MxMatrix(torch.empty(mx_bytes(rows, cols), dtype=torch.uint8, device=device), rows, cols)
-
-
-def _stores(forms: str, rows: int, cols: int, device):
-    """(what a call returns, by rows: address, bytes, by columns: address, bytes) with new buffers for the forms asked for."""
-    if forms == "rows":
-        m = _new_store(rows, cols, device)
-        return m, m.data.data_ptr(), m.data.numel(), None, 0
-    if forms == "columns":
-        m = _new_store(cols, rows, device)
-        return m, None, 0, m.data.data_ptr(), m.data.numel()
-    if forms == "both":
-        m, t = _new_store(rows, cols, device), _new_store(cols, rows, device)
-        return (m, t), m.data.data_ptr(), m.data.numel(), t.data.data_ptr(), t.data.numel()
-    raise ValueError(f"forms must be 'rows', 'columns' or 'both' (got {forms!r})")
+_binding.use(FedHybridError, MxMatrix)
 
 
 def fh_mx_quantize(x: torch.Tensor, forms: str = "rows", rounding="nearest", seed: int = 0, tensor_id: int = 0, stream=None):
     """Enqueue the quantisation of the matrix x (rows contiguous, any row stride).  forms "rows" returns an MxMatrix of x
     with blocks of 32 values along its rows, "columns" one of x transposed (blocks along x's columns), "both" the two."""
-    rows, cols, stride = _matrix(x, "x")
-    device = x.device
-    kept, a, a_bytes, b, b_bytes = _stores(forms, rows, cols, device)
-    _enqueue(device, stream, _lib.fh_mx_quantize, x.data_ptr(), _dtype_code(x), rows, cols, stride, _ROUND[rounding],
-             seed & _MASK64, tensor_id & _MASK64, a, a_bytes, b, b_bytes)
-    return kept
-
-
-def _stored(m: MxMatrix, what: str) -> torch.Tensor:
-    t = m.data
-    if not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous():
-        _device_tensor(t, what)
-        raise TypeError(f"{what} holds {t.dtype}, a stored matrix bytes")
-    return t
-
-
-def _new(rows: int, cols: int, dtype, device) -> torch.Tensor:
-    return torch.empty((rows, cols), dtype=dtype, device=device)
+    return _binding.mx_quantize(x, forms, rounding, seed, tensor_id, stream)
 
 
 def fh_mx_dequantize(m: MxMatrix, out_dtype=torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Enqueue the restoration of a stored matrix; returns it as [rows, cols]."""
-    data = _stored(m, "the stored matrix")
-    device, rows, cols = data.device, m.rows, m.cols
-    if out is None:
-        out, stride = _new(rows, cols, out_dtype, device), cols
-    else:
-        out_rows, out_cols, stride = _matrix(out, "out")
-        if (out_rows, out_cols) != (rows, cols):
-            raise ValueError(f"out is {out_rows} x {out_cols}, the matrix {rows} x {cols}")
-        _on_device(out, device, "out")
-    code = _dtype_code(out)
-    nbytes = ((rows - 1) * stride + cols) * out.element_size() if rows and cols else 0
-    _enqueue(device, stream, _lib.fh_mx_dequantize, data.data_ptr(), data.numel(), rows, cols, code, out.data_ptr(), stride, nbytes)
-    return out
+    return _binding.mx_dequantize(m, out_dtype, out, stream)
 
 
 def mx_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
@@ -1456,73 +1356,20 @@ def mx_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
 def fh_mx_matmul(a: MxMatrix, b: MxMatrix, bias: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
                  out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Enqueue out = a b^T + bias of two stored matrices whose blocks run along the summed dimension."""
-    da, db = _stored(a, "a"), _stored(b, "b")
-    m, n, k = a.rows, b.rows, a.cols
-    if b.cols != k:
-        raise ValueError(f"a has {k} columns, b {b.cols}")
-    device = da.device
-    _on_device(db, device, "b")
-    if out is None:
-        out, stride = _new(m, n, out_dtype, device), n
-    else:
-        rows, cols, stride = _matrix(out, "out")
-        if (rows, cols) != (m, n):
-            raise ValueError(f"out is {rows} x {cols}, the product {m} x {n}")
-        _on_device(out, device, "out")
-    work, work_bytes = None, 0
-    if workspace is not None:
-        _on_device(_device_tensor(workspace, "workspace"), device, "workspace")
-    elif need := _lib.fh_mx_matmul_workspace_bytes(m, n, k):
-        workspace = _scratch(need, device, stream)
-    if workspace is not None:
-        work, work_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    p = fh_mx_product(da.data_ptr(), da.numel(), db.data_ptr(), db.numel(), m, n, k, _vector(bias, n, device, "bias"),
-                      FH_F32 if bias is None else _dtype_code(bias), _dtype_code(out), out.data_ptr(), stride,
-                      ((m - 1) * stride + n) * out.element_size() if m and n else 0, work, work_bytes, 0)
-    _enqueue(device, stream, _lib.fh_mx_matmul, ctypes.byref(p))
-    return out
-
-
-def _like(t: Optional[torch.Tensor], x: torch.Tensor, rows: int, cols: int, what: str):
-    """(t, its row stride), or a new matrix like x."""
-    if t is None:
-        return _new(rows, cols, x.dtype, x.device), cols
-    t_rows, t_cols, stride = _matrix(t, what)
-    if (t_rows, t_cols) != (rows, cols) or t.dtype != x.dtype:
-        raise ValueError(f"{what} must have the shape and the dtype of x")
-    _on_device(t, x.device, what)
-    return t, stride
+    return _binding.mx_matmul(a, b, bias, out_dtype, out, workspace, stream)
 
 
 def fh_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
                   out: Optional[torch.Tensor] = None, stream=None):
     """Enqueue the layer norm of the matrix x over its rows; returns (y, mean, rstd), y in x's dtype, the statistics in fp32."""
-    rows, cols, stride = _matrix(x, "x")
-    device = x.device
-    w, b, p_dtype = _parameters(weight, bias, cols, device)
-    out, out_stride = _like(out, x, rows, cols, "out")
-    mean = torch.empty(rows, dtype=torch.float32, device=device)
-    rstd = torch.empty_like(mean)
-    _enqueue(device, stream, _lib.fh_layer_norm, x.data_ptr(), _dtype_code(x), rows, cols, stride, w, b, p_dtype, eps,
-             out.data_ptr(), out_stride, ((rows - 1) * out_stride + cols) * out.element_size() if rows else 0,
-             mean.data_ptr(), rstd.data_ptr())
-    return out, mean, rstd
+    return _binding.layer_norm(x, weight, bias, eps, out, stream)
 
 
 def fh_layer_norm_mx(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
                      forms: str = "rows", rounding="nearest", seed: int = 0, tensor_id: int = 0, stream=None):
     """Enqueue the layer norm of x with its result stored in microscaled form, as fh_mx_quantize stores it; returns
     (what fh_mx_quantize would return, mean, rstd)."""
-    rows, cols, stride = _matrix(x, "x")
-    device = x.device
-    w, b, p_dtype = _parameters(weight, bias, cols, device)
-    kept, by_rows, rows_bytes, by_columns, columns_bytes = _stores(forms, rows, cols, device)
-    mean = torch.empty(rows, dtype=torch.float32, device=device)
-    rstd = torch.empty_like(mean)
-    _enqueue(device, stream, _lib.fh_layer_norm_mx, x.data_ptr(), _dtype_code(x), rows, cols, stride, w, b, p_dtype, eps,
-             _ROUND[rounding], seed & _MASK64, tensor_id & _MASK64, by_rows, rows_bytes, by_columns, columns_bytes,
-             mean.data_ptr(), rstd.data_ptr())
-    return kept, mean, rstd
+    return _binding.layer_norm_mx(x, weight, bias, eps, forms, rounding, seed, tensor_id, stream)
 
 
 def fh_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
@@ -1530,113 +1377,38 @@ def fh_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor
                            workspace: Optional[torch.Tensor] = None, stream=None):
     """Enqueue the backward pass of fh_layer_norm; returns (dx, dweight, dbias), the last two (None unless `sums`) in the
     weight's dtype, in x's where there is no weight."""
-    rows, cols, x_stride = _matrix(x, "x")
-    device, dtype = x.device, x.dtype
-    dy_rows, dy_cols, dy_stride = _matrix(dy, "dy")
-    if dy_rows != rows or dy_cols != cols or dy.dtype != dtype:
-        raise ValueError("dy must have the shape and the dtype of x")
-    _on_device(dy, device, "dy")
-    if mean.dtype != torch.float32 or rstd.dtype != torch.float32:
-        raise TypeError("mean and rstd must be float32")
-    dx, dx_stride = _like(dx, x, rows, cols, "dx")
-    like = x if weight is None else weight
-    dweight = dbias = work = dweight_ptr = dbias_ptr = None
-    work_bytes = 0
-    if workspace is not None:
-        _on_device(_device_tensor(workspace, "workspace"), device, "workspace")
-    if sums:
-        dweight = torch.empty(cols, dtype=like.dtype, device=device)
-        dbias = torch.empty_like(dweight)
-        dweight_ptr, dbias_ptr = dweight.data_ptr(), dbias.data_ptr()
-        if workspace is None:
-            workspace = _scratch(_lib.fh_layer_norm_backward_workspace_bytes(rows, cols), device, stream)
-        work, work_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    p = fh_norm_backward(dy.data_ptr(), x.data_ptr(), dy_stride, x_stride, _vector(mean, rows, device, "mean"),
-                         _vector(rstd, rows, device, "rstd"), _vector(weight, cols, device, "weight"), rows, cols, _dtype_code(x),
-                         _dtype_code(like), dx.data_ptr(), dx_stride,
-                         ((rows - 1) * dx_stride + cols) * dx.element_size() if rows else 0,
-                         dweight_ptr, dbias_ptr, work, work_bytes)
-    _enqueue(device, stream, _lib.fh_layer_norm_backward, ctypes.byref(p))
-    return dx, dweight, dbias
+    return _binding.layer_norm_backward(dy, x, mean, rstd, weight, sums, dx, workspace, stream)
 
 
 FH_MX_NEEDS_INPUT, FH_MX_NEEDS_WEIGHT = 1, 2
-
-
-@functools.lru_cache(maxsize=256)
-def _layer_sizes(tokens: int, features: int, out: int):
-    """Bytes that a layer keeps between its halves, and bytes of scratch."""
-    return _lib.fh_mx_layer_kept_bytes(tokens, features, out), _lib.fh_mx_layer_scratch_bytes(tokens, features, out)
 
 
 class MxLayer:
     """One pass through a linear layer in microscaled form: what its forward call keeps for its backward call.  x: [tokens,
     features], weight: [out, features]; `norm`: a layer norm ahead, with norm_weight and norm_bias (either may be None).  Parameters
     are of one dtype, and so are x, y and the gradients of both."""
-    __slots__ = ("args", "kept", "sizes", "device", "dtype", "p_dtype", "needs_input", "needs_weight", "norm")
+    __slots__ = ("inputs", "kept", "shape", "dtype", "p_dtype", "features", "norm", "eps", "needs_input", "needs_weight", "rounding")
 
     def __init__(self, x: torch.Tensor, weight: torch.Tensor, bias=None, norm: bool = False, norm_weight=None, norm_bias=None,
                  eps: float = 1e-5, needs_input: bool = True, needs_weight: bool = True, rounding="nearest", seed: int = 0,
                  tensor_id: int = 0):
-        tokens, features, x_stride = _matrix(x, "x")
-        out, w_features, w_stride = _matrix(weight, "weight")
-        if w_features != features:
-            raise ValueError(f"x has {features} features, weight takes {w_features}")
-        device, p_dtype = x.device, weight.dtype
-        _on_device(weight, device, "weight")
-        if (bias is not None and bias.dtype != p_dtype) or (norm_weight is not None and norm_weight.dtype != p_dtype) or \
-                (norm_bias is not None and norm_bias.dtype != p_dtype):
-            raise TypeError(f"the parameters of one layer are of one dtype, as its weight: {p_dtype}")
-        self.device, self.dtype, self.p_dtype, self.kept = device, x.dtype, p_dtype, None
-        self.norm, self.needs_input, self.needs_weight = norm, needs_input, needs_weight
-        self.sizes = _layer_sizes(tokens, features, out)
-        self.args = fh_mx_layer(tokens, features, out, _dtype_code(x), _dtype_code(weight), 1 if norm else 0,
-                                (FH_MX_NEEDS_INPUT if needs_input else 0) | (FH_MX_NEEDS_WEIGHT if needs_weight else 0),
-                                _ROUND[rounding], eps, seed & _MASK64, tensor_id & _MASK64, x.data_ptr(), x_stride,
-                                _vector(norm_weight, features, device, "norm_weight"), _vector(norm_bias, features, device, "norm_bias"),
-                                weight.data_ptr(), w_stride, _vector(bias, out, device, "bias"), None, None, out)
+        self.inputs, self.kept = (x, weight, bias, norm, norm_weight, norm_bias, eps, needs_input, needs_weight), None
+        self.norm, self.eps, self.needs_input, self.needs_weight = norm, eps, needs_input, needs_weight
+        self.rounding = (rounding, seed, tensor_id)
+        if rounding not in _ROUND:
+            raise KeyError(rounding)
 
     def forward(self, stream=None) -> torch.Tensor:
         """Enqueue the forward half; returns y."""
-        a, device = self.args, self.device
-        kept_bytes, scratch_bytes = self.sizes
-        y = _new(a.tokens, a.out_features, self.dtype, device)
-        if self.norm or self.needs_input or self.needs_weight:
-            self.kept = torch.empty(kept_bytes, dtype=torch.uint8, device=device)
-            a.kept, a.kept_cap = self.kept.data_ptr(), kept_bytes
-        scratch = _scratch(scratch_bytes, device, stream)
-        a.y, a.scratch, a.scratch_cap = y.data_ptr(), scratch.data_ptr(), scratch_bytes
-        _enqueue(device, stream, _lib.fh_mx_layer_forward, ctypes.byref(a))
+        x, weight = self.inputs[:2]
+        y, self.kept = _binding.layer_forward(*self.inputs, stream)
+        self.inputs, self.shape, self.dtype, self.p_dtype, self.features = None, y.shape, x.dtype, weight.dtype, x.shape[1]
         return y
 
     def backward(self, dy: torch.Tensor, x: Optional[torch.Tensor] = None, norm_weight: Optional[torch.Tensor] = None, stream=None):
         """Enqueue the backward half; returns (dx, dweight, dnorm_weight, dnorm_bias), None for what is not needed.  With a norm x
         and norm_weight are the forward call's (x may have moved, as a saved tensor that was restored has)."""
-        a, device, p_dtype = self.args, self.device, self.p_dtype
-        tokens, out, dy_stride = _matrix(dy, "dy")
-        features = a.features
-        if tokens != a.tokens or out != a.out_features or dy.dtype != self.dtype:
+        if dy.shape != self.shape or dy.dtype != self.dtype:
             raise ValueError("dy must have the shape and the dtype of y")
-        _on_device(dy, device, "dy")
-        dx = dweight = dnorm_weight = dnorm_bias = None
-        if self.needs_weight:
-            dweight = _new(out, features, p_dtype, device)
-            a.dweight = dweight.data_ptr()
-        if self.needs_input:
-            dx = _new(tokens, features, self.dtype, device)
-            a.dx = dx.data_ptr()
-            if self.norm:
-                if x is None:
-                    raise ValueError("with a norm the backward call takes x again")
-                x_rows, x_cols, a.x_stride = _matrix(x, "x")
-                if x_rows != tokens or x_cols != features or x.dtype != self.dtype:
-                    raise ValueError("x must have the shape and the dtype of the forward call's")
-                _on_device(x, device, "x")
-                dnorm_weight = torch.empty(features, dtype=p_dtype, device=device)
-                dnorm_bias = torch.empty_like(dnorm_weight)
-                a.x, a.norm_weight = x.data_ptr(), _vector(norm_weight, features, device, "norm_weight")
-                a.dnorm_weight, a.dnorm_bias = dnorm_weight.data_ptr(), dnorm_bias.data_ptr()
-        scratch = _scratch(self.sizes[1], device, stream)
-        a.dy, a.dy_stride, a.scratch, a.scratch_cap = dy.data_ptr(), dy_stride, scratch.data_ptr(), self.sizes[1]
-        _enqueue(device, stream, _lib.fh_mx_layer_backward, ctypes.byref(a))
-        return dx, dweight, dnorm_weight, dnorm_bias
+        return _binding.layer_backward(dy, x, norm_weight, self.kept, self.features, self.p_dtype, self.norm, self.eps, self.needs_input,
+                                       self.needs_weight, *self.rounding, stream)

@@ -1,4 +1,4 @@
-"""Build libfedhybrid.so (HIP kernels + C ABI) in-tree for gfx950 with hipcc.
+"""Build libfedhybrid.so (HIP kernels + C ABI) in-tree for gfx950 with hipcc, and _fh_binding.so (host code only) beside it.
 
 Cross-compiles without a GPU.  Run as `python -m paper_2510_11400_amd.build`.
 Every call compiles every source (one hipcc process per file, side by side) and links.
@@ -9,12 +9,14 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libfedhybrid.so")
+BINDING = os.path.join(HERE, "_fh_binding.so")
 SOURCES = ("fh_abi.hip", "fh_compress.hip", "fh_decompress.hip", "fh_classify.hip", "fh_mixed.hip", "fh_sparse.hip",
            "fh_huffman.hip", "fh_chain.hip", "fh_mx_quantize.hip", "fh_mx_matmul.hip", "fh_layer_norm.hip",
            "fh_mx_layer.hip")
@@ -45,7 +47,7 @@ def _run(cmd, verbose: bool) -> None:
     res = subprocess.run(cmd, cwd=CSRC, capture_output=True, text=True)
     err = "\n".join(l for l in res.stderr.splitlines() if _NOISE not in l)
     if res.returncode != 0:
-        raise RuntimeError(f"hipcc failed ({res.returncode}): {' '.join(cmd)}\n{err}")
+        raise RuntimeError(f"{os.path.basename(cmd[0])} failed ({res.returncode}): {' '.join(cmd)}\n{err}")
     if verbose and err.strip():
         print(err, file=sys.stderr)
 
@@ -66,5 +68,20 @@ def build_library(verbose: bool = False, extra_flags=(), out: str = LIB, only=No
     return out
 
 
+def build_binding(verbose: bool = False) -> str:
+    """Compile the Python functions over the built library: a C++ file against PyTorch's headers, no device code."""
+    import torch
+
+    home, rocm = os.path.dirname(torch.__file__), os.path.dirname(os.path.dirname(os.path.realpath(hipcc())))
+    headers = [os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"),
+               os.path.join(rocm, "include"), sysconfig.get_paths()["include"]]
+    _run([shutil.which("g++") or "c++", "-std=c++17", "-O2", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+          *[f"-isystem{h}" for h in headers], os.path.join(CSRC, "fh_binding.cpp"), "-o", BINDING, f"-L{HERE}", "-lfedhybrid",
+          f"-L{os.path.join(home, 'lib')}", "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python", "-Wl,-rpath,$ORIGIN"], verbose)
+    return BINDING
+
+
 if __name__ == "__main__":
     print(build_library(verbose=True, only=sys.argv[1:] or None))
+    print(build_binding(verbose=True))

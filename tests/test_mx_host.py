@@ -186,7 +186,7 @@ def test_the_binding_refuses_host_tensors_and_shapes():
         with pytest.raises(ValueError, match="device memory"):
             call()
     with pytest.raises(ValueError, match="forms"):
-        api._stores("diagonal", 4, 40, "cpu")
+        api.fh_mx_quantize(x, "diagonal")
 
 
 @pytest.mark.parametrize("rows, cols", [(0, 0), (0, 5), (5, 0), (1, 1), (33, 255), (8192, 768), (2 ** 31 - 256, 257), (3, 2 ** 31 - 256), (-1, 5), (5, -1),
