@@ -21,6 +21,7 @@ struct ProductArgs {
     int32_t        parts;              // workgroups that share a tile's sum
     int32_t        bias_dtype;
     uint32_t       m_tiles, n_tiles;
+    uint32_t       step;               // from a workgroup's tile to its next one
 };
 static_assert(sizeof(ProductArgs) <= 112, "longer arguments are enqueued a microsecond later");
 
@@ -67,17 +68,17 @@ __global__ __launch_bounds__(WAVES * 64) void mx_waves_kernel(ProductArgs p)
     // rows past the last are the last one, so that every address is inside
     const int rows_a = (int)(p.m - i0 < kRowsA ? p.m - i0 : kRowsA), rows_b = (int)(p.n - j0 < kRowsB ? p.n - j0 : kRowsB);
     const u32x4 from_a = buffer_of(p.a + i0 * pitch, rows_a * pitch), from_b = buffer_of(p.b + j0 * pitch, rows_b * pitch);
-    const uint32_t piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    const uint32_t piece = ((lane & 7) ^ (lane >> 4)) * 16;      // turned by half the row's number, 4 more for every other eight rows
     uint32_t at_a[MT * 4], at_b[NT * 4];
 #pragma unroll
     for (int t = 0; t < MT * 4; ++t) {
         const int r = t * 8 + (lane >> 3);
-        at_a[t] = (r < rows_a ? r : rows_a - 1) * pitch + piece;
+        at_a[t] = (r < rows_a ? r : rows_a - 1) * pitch + (piece ^ (t & 1) * 64);
     }
 #pragma unroll
     for (int t = 0; t < NT * 4; ++t) {
         const int r = t * 8 + (lane >> 3);
-        at_b[t] = (r < rows_b ? r : rows_b - 1) * pitch + piece;
+        at_b[t] = (r < rows_b ? r : rows_b - 1) * pitch + (piece ^ (t & 1) * 64);
     }
     const uint32_t groups_a = (rows_a + 31) / 32, groups_b = (rows_b + 31) / 32;
     const u32x4 from_sa = buffer_of(p.a_scales + (i0 >> 5) * scale_pitch, groups_a * scale_pitch);
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(WAVES * 64) void mx_waves_kernel(ProductArgs p)
 #pragma unroll
         for (int t = 0; t < NT * 4; ++t) to_lds(lds + kRowsA * 128 + t * 1024, from_b, at_b[t], chunk * 128);
     };
-    const int h = lane >> 5, r = lane & 31, turned = (h * 4) ^ (lane & 7);
+    const int h = lane >> 5, r = lane & 31, turned = (h * 4) ^ (lane >> 1 & 7);
     const uint32_t chunks = (uint32_t)p.chunks, begin = part * (uint32_t)p.chunks_each;
     const uint32_t end = begin + (uint32_t)p.chunks_each < chunks ? begin + (uint32_t)p.chunks_each : chunks;
     f32x16 c[MT][NT] = {};
@@ -149,78 +150,97 @@ __global__ __launch_bounds__(WAVES * 64) void mx_waves_kernel(ProductArgs p)
     }
 }
 
-// ---- large products: tiles through LDS ----------------------------------------------------------
-// BM x BN outputs a workgroup of WM x WN waves, a chunk of 256 summed values at a time.  Two stages of LDS: while one is
-// multiplied the next is on its way, and a stage is handed over before its last quarter, which is in registers by then, so
-// that the matrix unit works across the barrier.  A row's eight pieces of 16 bytes are turned by the row (the loads take
-// them from turned addresses), so that eight lanes reading the same piece of eight rows meet all banks.
-template <typename T, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * 64, BM * BN > 16384 ? 1 : 2) void mx_tile_kernel(ProductArgs p)
+// Of 16 bytes of outputs those that are before a row's end.
+template <typename T>
+__device__ __forceinline__ void store_packed(T* p, int n, u32x4 v)
 {
-    constexpr int kWaves = WM * WN, MT = BM / WM / 32, NT = BN / WN / 32;
-    constexpr uint32_t kCodes = (BM + BN) * 128, kStage = kCodes + (BM + BN) * 8;
-    constexpr int kLoadsA = BM / 8 / kWaves, kLoadsB = BN / 8 / kWaves;
-    constexpr uint32_t kRow = NT * 32 * 4 + 16;                  // of the outputs on their way through LDS
-    static_assert(BM % 128 == 0 && BN % 128 == 0 && (BM + BN) / 128 <= kWaves, "a wave loads the scales of 128 rows");
-    static_assert(kWaves * 32 * kRow <= 2 * kStage, "the outputs go through the stages' memory");
+    constexpr int kRun = 16 / sizeof(T);
+    if (n >= kRun) *reinterpret_cast<u32x4_a2*>(p) = v;
+    else {
+#pragma unroll
+        for (int i = 0; i < kRun; ++i)
+            if (i < n) {
+                if constexpr (sizeof(T) == 4) p[i] = __builtin_bit_cast(float, v[i]);
+                else p[i].bits = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
+            }
+    }
+}
+
+// ---- large products: tiles through LDS ----------------------------------------------------------
+// B x B outputs of a tile, a chunk of 256 summed values at a time; a workgroup of 2 x WN waves, each with B/2 x 64 outputs, takes one
+// tile after another.  Two stages of LDS: while one is multiplied the next is on its way, and a stage is handed over before its last
+// quarter, which is in registers by then, so that the matrix unit works across the barrier.  A row's eight pieces of 16 bytes
+// are turned by half the row's number (the loads take them from turned addresses), so that sixteen lanes reading the same
+// piece of sixteen rows meet all 64 banks.
+// The chunks of the next tile follow those of the last without a gap.  A wave's outputs are turned into rows in the part of the free stage that
+// the wave itself loads, so it needs no barrier before it loads there again; that load is sent before the outputs are, because
+// memory operations are counted in their order and the next wait is for the load alone.
+template <typename T, int B, int WN>
+__global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void mx_tile_kernel(ProductArgs p)
+{
+    constexpr int kWaves = 2 * WN, kHalf = kWaves / 2, MT = B / 64, NT = 2;
+    constexpr uint32_t kCodes = 2 * B * 128, kStage = kCodes + 2 * B * 8;
+    constexpr int kRun = 16 / sizeof(T), kLanes = 64 / kRun, kRows = 64 / kLanes, kStores = MT * 32 / kRows;
+    static_assert(kHalf * 64 == B && WN * 64 == B, "a wave loads 64 rows of one operand, and has 64 columns");
     __shared__ __attribute__((aligned(16))) uint8_t s_stage[2 * kStage];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
 
     // Tiles go to the XCDs in runs (workgroups go to them in turn), a run in columns of up to eight tiles, so that what an
     // XCD works on at a time shares rows of both operands in its L2.
-    const uint32_t m_tiles = p.m_tiles, n_tiles = p.n_tiles, tiles = m_tiles * n_tiles, at = blockIdx.x;
-    const uint32_t xcd = at & 7, share = tiles >> 3, rest = tiles & 7;
-    const uint32_t tile = xcd * share + (xcd < rest ? xcd : rest) + (at >> 3);
-    const uint32_t band = tile / (8 * m_tiles), first = band * 8, wide = n_tiles - first < 8 ? n_tiles - first : 8;
-    const int64_t i0 = (int64_t)((tile - band * 8 * m_tiles) / wide) * BM;
-    const int64_t j0 = (int64_t)(first + (tile - band * 8 * m_tiles) % wide) * BN;
-
-    // rows past the last are the last one, so that every address is inside
-    const int rows_a = (int)(p.m - i0 < BM ? p.m - i0 : BM), rows_b = (int)(p.n - j0 < BN ? p.n - j0 : BN);
-    const uint32_t pitch = (uint32_t)p.chunks * 128, scale_pitch = (uint32_t)p.chunks * 256;
-    const u32x4 from_a = buffer_of(p.a + i0 * pitch, rows_a * pitch), from_b = buffer_of(p.b + j0 * pitch, rows_b * pitch);
-    const uint32_t piece = ((lane & 7) ^ (lane >> 3)) * 16;
-    uint32_t at_a[kLoadsA], at_b[kLoadsB];
-#pragma unroll
-    for (int t = 0; t < kLoadsA; ++t) {
-        const int r = (t * kWaves + wave) * 8 + (lane >> 3);
-        at_a[t] = (r < rows_a ? r : rows_a - 1) * pitch + piece;
-    }
-#pragma unroll
-    for (int t = 0; t < kLoadsB; ++t) {
-        const int r = (t * kWaves + wave) * 8 + (lane >> 3);
-        at_b[t] = (r < rows_b ? r : rows_b - 1) * pitch + piece;
-    }
-    const bool scales_of_a = wave < BM / 128, loads_scales = wave < (BM + BN) / 128;
-    const uint32_t groups = ((scales_of_a ? rows_a : rows_b) + 31) / 32;
-    const u32x4 from_scales = buffer_of(scales_of_a ? p.a_scales + (i0 >> 5) * scale_pitch : p.b_scales + (j0 >> 5) * scale_pitch, groups * scale_pitch);
-    const uint32_t group = (scales_of_a ? wave : wave - BM / 128) * 4 + (lane >> 4);
-    const uint32_t at_scales = (group < groups ? group : groups - 1) * scale_pitch + (lane & 15) * 16;
-
-    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_stage;
-    auto load = [&](uint32_t stage, uint32_t chunk) {
-        if (loads_scales) to_lds(lds + stage + kCodes + wave * 1024, from_scales, at_scales, chunk * 256);
-#pragma unroll
-        for (int t = 0; t < kLoadsA; ++t) to_lds(lds + stage + (t * kWaves + wave) * 1024, from_a, at_a[t], chunk * 128);
-#pragma unroll
-        for (int t = 0; t < kLoadsB; ++t) to_lds(lds + stage + BM * 128 + (t * kWaves + wave) * 1024, from_b, at_b[t], chunk * 128);
+    const uint32_t m_tiles = p.m_tiles, n_tiles = p.n_tiles, tiles = m_tiles * n_tiles, xcd = blockIdx.x & 7, share = tiles >> 3, rest = tiles & 7;
+    const uint32_t first_tile = xcd * share + (xcd < rest ? xcd : rest), end_tile = first_tile + share + (xcd < rest ? 1 : 0);
+    const auto corner = [&](uint32_t tile, int64_t& i0, int64_t& j0) {
+        const uint32_t band = tile / (8 * m_tiles), first = band * 8, wide = n_tiles - first < 8 ? n_tiles - first : 8, in_band = tile - band * 8 * m_tiles;
+        i0 = (int64_t)(in_band / wide) * B;
+        j0 = (int64_t)(first + in_band % wide) * B;
     };
 
-    const int h = lane >> 5, r = lane & 31, turned = (h * 4) ^ (lane & 7);
-    const uint32_t read_a = (wm * MT * 32 + r) * 128, read_b = BM * 128 + (wn * NT * 32 + r) * 128;
-    const uint32_t read_sa = kCodes + wm * MT * 256 + h * 128 + r * 4, read_sb = kCodes + BM * 8 + wn * NT * 256 + h * 128 + r * 4;
+    // what is loaded next: a chunk of a tile, in this wave 64 rows of one operand and with it maybe the scales of 128
+    const bool of_b = wave >= kHalf, loads_scales = wave % kHalf < kHalf / 2;
+    const int part = wave % kHalf;
+    const uint32_t pitch = (uint32_t)p.chunks * 128, scale_pitch = (uint32_t)p.chunks * 256, end = (uint32_t)p.chunks;
+    uint32_t next_tile = first_tile + (blockIdx.x >> 3), next_chunk = 0;
+    u32x4 from, from_scales;
+    const uint32_t at = (part * 64 + (lane >> 3)) * pitch + ((lane & 7) ^ (lane >> 4)) * 16, at_scales = (part * 4 + (lane >> 4)) * scale_pitch + (lane & 15) * 16;
+    const auto aim = [&]() {
+        int64_t i0, j0;
+        corner(next_tile, i0, j0);
+        const int64_t row0 = of_b ? j0 : i0, left = (of_b ? p.n : p.m) - row0;
+        const int rows = left < B ? (int)left : B, groups = (rows + 31) / 32;
+        // rows past the last are past the buffer's end: nothing is read for them, and nothing of theirs is stored
+        from = buffer_of((of_b ? p.b : p.a) + row0 * pitch, (uint32_t)rows * pitch);
+        from_scales = buffer_of((of_b ? p.b_scales : p.a_scales) + (row0 >> 5) * scale_pitch, (uint32_t)groups * scale_pitch);
+    };
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_stage;
+    const uint32_t lds_scales = kCodes + (of_b ? B * 8 : 0) + part * 1024;
+    const auto load = [&](uint32_t stage) {
+        if (next_tile >= end_tile) return;
+        if (loads_scales) to_lds(lds + stage + lds_scales, from_scales, at_scales, next_chunk * 256);
+        uint32_t row_at = at;
+        asm("" : "+v"(row_at));                                  // seven sums made here, not seven registers kept
+#pragma unroll
+        for (int t = 0; t < 8; ++t) to_lds(lds + stage + wave * 8192 + t * 1024, from, (row_at ^ (t & 1) * 64) + t * 8 * pitch, next_chunk * 128);
+        if (++next_chunk == end) {
+            next_chunk = 0;
+            next_tile += p.step;
+            if (next_tile < end_tile) aim();
+        }
+    };
+
+    const int h = lane >> 5, r = lane & 31, turned = (h * 4) ^ (lane >> 1 & 7);
+    const uint32_t read_a = (wm * MT * 32 + r) * 128, read_b = B * 128 + (wn * NT * 32 + r) * 128;
+    const uint32_t read_sa = kCodes + wm * MT * 256 + h * 128 + r * 4, read_sb = kCodes + B * 8 + wn * NT * 256 + h * 128 + r * 4;
     u32x4 fa[2][MT], fb[2][NT];
     uint32_t sa[MT], sb[NT], next_sa[MT], next_sb[NT];
-    f32x16 c[MT][NT] = {};
-    auto read = [&](uint32_t stage, int quarter, int to) {
-        const uint8_t* from = s_stage + stage + (uint32_t)(turned ^ quarter) * 16;
+    const auto read = [&](uint32_t stage, int quarter, int to) {
+        const uint8_t* at_piece = s_stage + stage + (uint32_t)(turned ^ quarter) * 16;
 #pragma unroll
-        for (int t = 0; t < MT; ++t) fa[to][t] = *reinterpret_cast<const u32x4*>(from + read_a + t * 4096);
+        for (int t = 0; t < MT; ++t) fa[to][t] = *reinterpret_cast<const u32x4*>(at_piece + read_a + t * 4096);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) fb[to][t] = *reinterpret_cast<const u32x4*>(from + read_b + t * 4096);
+        for (int t = 0; t < NT; ++t) fb[to][t] = *reinterpret_cast<const u32x4*>(at_piece + read_b + t * 4096);
     };
-    auto read_scales = [&](uint32_t stage, uint32_t (&ua)[MT], uint32_t (&ub)[NT]) {
+    const auto read_scales = [&](uint32_t stage, uint32_t (&ua)[MT], uint32_t (&ub)[NT]) {
 #pragma unroll
         for (int t = 0; t < MT; ++t) ua[t] = *reinterpret_cast<const uint32_t*>(s_stage + stage + read_sa + t * 256);
 #pragma unroll
@@ -234,71 +254,113 @@ __global__ __launch_bounds__(WM * WN * 64, BM * BN > 16384 ? 1 : 2) void mx_tile
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                                                        \
         __builtin_amdgcn_sched_group_barrier(0x008, MT * NT / (MT + NT), 0);                                      \
     }
-    const uint32_t end = (uint32_t)p.chunks;
-    load(0, 0);
-    if (end > 1) {
-        load(kStage, 1);
-        asm volatile("s_waitcnt vmcnt(%0)" :: "n"(kLoadsA + kLoadsB) : "memory");   // the first stage's are older
+    uint32_t tile = next_tile, stage = 0;
+    bool behind = false;                                         // outputs were sent after the load that is waited for
+    aim();
+    load(0);
+    if (next_tile < end_tile) {
+        load(kStage);
+        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");         // the first stage's are older
     } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    uint32_t stage = 0;
     read(stage, 0, 0);
     read_scales(stage, sa, sb);
-    for (uint32_t k = 0; k < end; ++k) {
-        read(stage, 1, 1);
-        FH_QUARTER(0, 0)
-        read(stage, 2, 0);
-        FH_QUARTER(1, 1)
-        read(stage, 3, 1);
-        FH_QUARTER(2, 0)
-        // this wave has read all of this stage, and its part of the next has arrived
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (k + 2 < end) load(stage, k + 2);
-        stage = kStage - stage;
-        read(stage, 0, 0);                                       // after the last chunk: of no use, and inside
-        read_scales(stage, next_sa, next_sb);
-        FH_QUARTER(3, 1)
+    T* out = static_cast<T*>(p.out);
+#pragma clang loop unroll(disable)
+    for (; tile < end_tile; tile += p.step) {
+        int64_t i0, j0;
+        corner(tile, i0, j0);
+        float bias_here = 0.0f;
+        f32x16 c[MT][NT] = {};
+#pragma clang loop unroll(disable)
+        for (uint32_t k = 0; k < end; ++k) {
+            if (k + 1 == end && p.bias) {
+                const int64_t j = j0 + wn * 64 + lane;
+                bias_here = parameter(p.bias, p.bias_dtype, j < p.n ? j : p.n - 1, 0.0f);
+            }
+            read(stage, 1, 1);
+            FH_QUARTER(0, 0)
+            read(stage, 2, 0);
+            FH_QUARTER(1, 1)
+            read(stage, 3, 1);
+            FH_QUARTER(2, 0)
+            // this wave has read all of this stage, and its part of the next has arrived
+            if (behind) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(kStores) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            behind = false;
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (k + 1 < end) load(stage);
+            stage = kStage - stage;
+            read(stage, 0, 0);                                   // after the last chunk: of no use, and inside
+            read_scales(stage, next_sa, next_sb);
+            FH_QUARTER(3, 1)
 #pragma unroll
-        for (int t = 0; t < MT; ++t) sa[t] = next_sa[t];
+            for (int t = 0; t < MT; ++t) sa[t] = next_sa[t];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) sb[t] = next_sb[t];
+            for (int t = 0; t < NT; ++t) sb[t] = next_sb[t];
+        }
+
+        // 32 rows at a time through this wave's 8 KiB of the stage that is free, to runs of 16 bytes a lane
+        int l = lane;
+        asm("" : "+v"(l));                                       // what is worked out from it is not kept in registers meanwhile
+        const int mine = l / kLanes, piece = l % kLanes, row32 = l & 31, half = l >> 5;
+        uint8_t* s_out = s_stage + (kStage - stage) + wave * 8192;
+        if (p.bias) {
+#pragma unroll
+            for (int y = 0; y < NT; ++y)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float b = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute((y * 32 + i / 4 * 8 + half * 4 + i % 4) * 4, __builtin_bit_cast(int, bias_here)));
+#pragma unroll
+                    for (int x = 0; x < MT; ++x) c[x][y][i] += b;
+                }
+        }
+        u32x4 v[kStores];
+#pragma unroll
+        for (int x = 0; x < MT; ++x) {
+#pragma unroll
+            for (int y = 0; y < NT; ++y)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x16& o = c[x][y];
+                    if constexpr (sizeof(T) == 2) {              // rows of 128 bytes; the upper sixteen have the halves of a piece exchanged
+                        const uint32_t at_piece = (uint32_t)((y * 4 + i) ^ (row32 >> 1 & 7)) * 16 + (uint32_t)(half ^ row32 >> 4) * 8;
+                        *reinterpret_cast<u32x2*>(s_out + row32 * 128 + at_piece) = u32x2{bf16_pair(o[4 * i], o[4 * i + 1]), bf16_pair(o[4 * i + 2], o[4 * i + 3])};
+                    } else {
+                        const uint32_t at_piece = (uint32_t)((y * 8 + 2 * i + half) ^ (row32 & 15)) * 16;
+                        *reinterpret_cast<f32x4*>(s_out + row32 * 256 + at_piece) = f32x4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
+                    }
+                }
+            asm volatile("" ::: "memory");                       // a wave's own LDS accesses are in order
+#pragma unroll
+            for (int t = 0; t < 32 / kRows; ++t) {
+                const int from_row = t * kRows + mine;
+                const uint32_t turn = sizeof(T) == 2 ? from_row >> 1 & 7 : from_row & 15;
+                const u32x4 w = *reinterpret_cast<const u32x4*>(s_out + from_row * (kLanes * 16) + (piece ^ turn) * 16);
+                v[x * (32 / kRows) + t] = sizeof(T) == 2 && t * kRows >= 16 ? u32x4{w.z, w.w, w.x, w.y} : w;
+            }
+            asm volatile("" ::: "memory");
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        load(kStage - stage);
+        const int64_t row = i0 + wm * MT * 32 + mine, col = j0 + wn * 64 + piece * kRun;
+        T* to = out + row * p.stride + col;
+        if (i0 + B <= p.m && j0 + B <= p.n) {
+#pragma unroll
+            for (int t = 0; t < kStores; ++t) *reinterpret_cast<u32x4_a2*>(to + (int64_t)(t * kRows) * p.stride) = v[t];
+            behind = true;
+        } else {
+            const int rows = p.m - row < B ? (int)(p.m - row) : B, cols = p.n - col < kRun ? (int)(p.n - col) : kRun;
+#pragma unroll
+            for (int t = 0; t < kStores; ++t) {
+                int some = t * kRows < rows ? cols : 0;
+                asm("" : "+v"(some));                            // its masks are not kept in registers either
+                store_packed(to + (int64_t)(t * kRows) * p.stride, some, v[t]);
+            }
+        }
     }
 #undef FH_QUARTER
-    __syncthreads();
-
-    // Out by rows: 32 rows of the wave's columns at a time through LDS, then whole runs of 16 bytes a lane.
-    float* s_out = reinterpret_cast<float*>(s_stage + wave * 32 * kRow);
-    T* out = static_cast<T*>(p.out);
-    constexpr int kRun = 16 / sizeof(T), kLanes = NT * 32 / kRun, kRows = 64 / kLanes;
-    const int64_t col = j0 + wn * NT * 32 + (lane % kLanes) * kRun;
-    float bias[kRun];
-#pragma unroll
-    for (int i = 0; i < kRun; ++i) bias[i] = col + i < p.n && p.bias ? parameter(p.bias, p.bias_dtype, col + i, 0.0f) : 0.0f;
-#pragma unroll
-    for (int x = 0; x < MT; ++x) {
-#pragma unroll
-        for (int y = 0; y < NT; ++y)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                *reinterpret_cast<f32x4*>(s_out + r * (kRow / 4) + y * 32 + 2 * i + 4 * h) = f32x4{c[x][y][i], c[x][y][i + 1], c[x][y][i + 2], c[x][y][i + 3]};
-        asm volatile("" ::: "memory");                           // a wave's own LDS accesses are in order
-#pragma unroll
-        for (int t = 0; t < 32 / kRows; ++t) {
-            const int mine = t * kRows + lane / kLanes;
-            const int64_t row = i0 + (wm * MT + x) * 32 + mine;
-            const float* from = s_out + mine * (kRow / 4) + (lane % kLanes) * kRun;
-            float v[kRun];
-#pragma unroll
-            for (int i = 0; i < kRun; i += 4) {
-                const f32x4 w = *reinterpret_cast<const f32x4*>(from + i);
-                v[i] = w.x + bias[i]; v[i + 1] = w.y + bias[i + 1]; v[i + 2] = w.z + bias[i + 2]; v[i + 3] = w.w + bias[i + 3];
-            }
-            if (row < p.m) store_run(out + row * p.stride + col, p.n - col, v);
-        }
-        asm volatile("" ::: "memory");
-    }
 }
 
 // The parts of a split sum added up in their order.
@@ -351,7 +413,7 @@ Plan plan_of(int64_t m, int64_t n, int64_t k)
                               tiles(128) <= 256 ? 490 + 65 * chunks : (560 + 99 * chunks) * tiles(128) / 512, rounds(256) * (1040 + 182 * chunks)};
     const Tile kernels[4] = {Tile::waves32, Tile::waves64, Tile::square128, Tile::square256};
     int best = 0;
-    for (int i = 1; i < 4; ++i)
+    for (int i = 1; i < 4 && chunks > 0; ++i)
         if (times[i] < times[best]) best = i;
     return Plan{kernels[best], 1, chunks};
 }
@@ -371,9 +433,12 @@ hipError_t squares_of(ProductArgs p, hipStream_t s)
 {
     const int64_t m_tiles = (p.m + B - 1) / B, n_tiles = (p.n + B - 1) / B;
     if (m_tiles * n_tiles * 8 > INT32_MAX) return hipErrorInvalidValue;
+    const int64_t groups = B > 128 ? 256 : 512;                  // what the card holds at a time
     p.m_tiles = (uint32_t)m_tiles;
     p.n_tiles = (uint32_t)n_tiles;
-    hipLaunchKernelGGL((mx_tile_kernel<T, B, B, 2, WN>), dim3((uint32_t)(m_tiles * n_tiles)), dim3(2 * WN * 64), 0, s, p);
+    const uint32_t grid = (uint32_t)(m_tiles * n_tiles < groups ? m_tiles * n_tiles : groups);
+    p.step = (grid + 7) / 8;
+    hipLaunchKernelGGL((mx_tile_kernel<T, B, WN>), dim3(grid), dim3(2 * WN * 64), 0, s, p);
     return hipGetLastError();
 }
 template <typename T>
@@ -431,7 +496,7 @@ fh_status fh_mx_matmul(const fh_mx_product* q, void* stream)
     const Plan plan = plan_of(q->m, q->n, q->k);
     const MxStore a = mx_store(const_cast<void*>(q->a), q->m, q->k), b = mx_store(const_cast<void*>(q->b), q->n, q->k);
     const ProductArgs p = {a.codes, a.scales, b.codes, b.scales, q->m, q->n, q->bias, q->out, q->stride, (int32_t)a.chunks,
-                           (int32_t)plan.chunks_each, plan.parts, q->bias_dtype, 0, 0};
+                           (int32_t)plan.chunks_each, plan.parts, q->bias_dtype, 0, 0, 0};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     float* w = static_cast<float*>(q->workspace);
     const hipError_t e = q->out_dtype == FH_F32 ? product_of<float>(p, plan, w, s) : product_of<Bf16>(p, plan, w, s);
