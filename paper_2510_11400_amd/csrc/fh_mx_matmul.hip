@@ -391,10 +391,10 @@ struct Plan { Tile tile; int32_t parts; int64_t chunks_each; };
 // A sum is split over workgroups where its outputs leave compute units idle, in parts of sixteen chunks at least.  Otherwise the kernel
 // with the shortest time, in hundredths of a microsecond with c chunks, by lines through what they measured (bf16 out; us,
 // in the order 32 (four waves), 64, 128, 256):
-//     1024 x 768 x 768    3.7  4.6  6.6 11.9     700 x 700 x 8192    9.1 11.5 25.1 56.6     768 x 768 x 8192   12.3 10.9 25.5 57.4
-//     4096 x 768 x 768    9.4  9.5  7.1 12.4     512 x 4096 x 4096  15.3 11.3 15.0 32.3     2304 x 768 x 8192  25.0 19.5 24.9 55.5
-//     8192 x 2304 x 768  44.6 35.9 20.2 26.1     2048^3             17.7 14.0 10.9 20.5     3000^3             46.9 44.5 27.9 29.0
-//     4096 x 4096 x 1024 41.6 35.5 19.2 17.7     4096^3            100.4 67.3 43.0 39.5     8192 x 8192 x 4096  422  282  183  156
+//     1024 x 768 x 768    3.8  4.7  4.9  8.8     700 x 700 x 8192    9.3 11.7 23.9 51.3     4096 x 4096 x 4096  99   66 39.2 36.7
+//     4096 x 768 x 768    9.6  9.6  5.7  9.4     512 x 4096 x 4096  16.1 11.7 14.0 27.2     2304 x 768 x 8192  25.6 20.2 24.0 49.1
+//     8192 x 2304 x 768  44.3 36.3 15.5 20.5     2048^3             17.6 13.9  9.6 16.9     3000^3             47.1 44.7 25.2 26.7
+//     4096 x 4096 x 1024 40.9 35.3 15.9 15.7     8192 x 8192 x 1024  176  143   68   54     8192 x 8192 x 4096  422  278  172  139
 // Workgroups of a kernel run in rounds of 256 (32: up to four a compute unit share it; 128: two, which one round of 512 makes).
 // Up to one tile of 32 a compute unit, eight waves share its sum where each has a chunk (300 x 300 x 8192 7.1 -> 5.8).
 Plan plan_of(int64_t m, int64_t n, int64_t k)
@@ -409,8 +409,9 @@ Plan plan_of(int64_t m, int64_t n, int64_t k)
         return Plan{Tile::waves32_wide, (int32_t)((chunks + each - 1) / each), each};
     }
     if (small <= 256 && chunks >= 8) return Plan{Tile::waves32_wide, 1, chunks};
-    const int64_t times[4] = {290 + rounds(32) * 10 * chunks, 340 + rounds(64) * (90 + 22 * chunks),
-                              tiles(128) <= 256 ? 490 + 65 * chunks : (560 + 99 * chunks) * tiles(128) / 512, rounds(256) * (1040 + 182 * chunks)};
+    const int64_t times[4] = {230 + rounds(32) * (30 + 9 * chunks), 340 + rounds(64) * (90 + 22 * chunks),
+                              tiles(128) <= 256 ? 310 + tiles(128) / 3 + 66 * chunks : 250 + (360 + 102 * chunks) * tiles(128) / 512,
+                              500 + rounds(256) * (480 + (tiles(256) <= 128 ? 125 : 179) * chunks)};
     const Tile kernels[4] = {Tile::waves32, Tile::waves64, Tile::square128, Tile::square256};
     int best = 0;
     for (int i = 1; i < 4 && chunks > 0; ++i)
