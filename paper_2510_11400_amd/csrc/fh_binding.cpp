@@ -110,6 +110,17 @@ at::Tensor bytes(size_t n, c10::Device device)
     return at::Tensor(at::detail::empty_cuda({(int64_t)n}, at::kByte, device, std::nullopt));
 }
 at::Tensor values(int64_t n, at::ScalarType type, c10::Device device) { return at::Tensor(at::detail::empty_cuda({n}, type, device, std::nullopt)); }
+// Two vectors of n values in one allocation.
+struct Pair { at::Tensor first, second; };
+Pair pair(int64_t n, at::ScalarType type, c10::Device device)
+{
+    Pair p{values(2 * n, type, device), at::Tensor()};
+    p.second = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(p.first.storage()), p.first.key_set(), p.first.dtype());
+    const int64_t step = 1;
+    p.second.unsafeGetTensorImpl()->set_sizes_and_strides(at::IntArrayRef(n), at::IntArrayRef(step), n);
+    p.first.unsafeGetTensorImpl()->set_sizes_contiguous(at::IntArrayRef(n));
+    return p;
+}
 Matrix new_matrix(int64_t rows, int64_t cols, at::ScalarType type, c10::Device device)
 {
     const int code = dtype_code(type);
@@ -361,12 +372,12 @@ FH_ENTRY(layer_norm, 6)
     const Parameters p(a[1], a[2], x.cols, x.device());
     const float eps = (float)f64(a[3]);
     const Matrix y = matrix_like(a[4], x, "out");
-    const at::Tensor mean = values(x.rows, at::kFloat, x.device()), rstd = values(x.rows, at::kFloat, x.device());
+    const Pair stats = pair(x.rows, at::kFloat, x.device());
     enqueue(x.device(), a[5], [&](void* stream) {
         return fh_layer_norm(x.data(), (fh_dtype)x.dtype, x.rows, x.cols, x.stride, p.w, p.b, (fh_dtype)p.dtype, eps, y.data(), y.stride, y.bytes(),
-                             mean.data_ptr(), rstd.data_ptr(), stream);
+                             stats.first.data_ptr(), stats.second.data_ptr(), stream);
     });
-    return tuple(Ref(wrap(y.t)), Ref(wrap(mean)), Ref(wrap(rstd)));
+    return tuple(Ref(wrap(y.t)), Ref(wrap(stats.first)), Ref(wrap(stats.second)));
 FH_EXIT
 
 // (x, weight, bias, eps, forms, rounding, seed, tensor_id, stream)
@@ -378,12 +389,12 @@ FH_ENTRY(layer_norm_mx, 9)
     const int rounding = rounding_of(a[5]);
     const uint64_t seed = u64(a[6]), id = u64(a[7]);
     const Stores s(f, x.rows, x.cols, x.device());
-    const at::Tensor mean = values(x.rows, at::kFloat, x.device()), rstd = values(x.rows, at::kFloat, x.device());
+    const Pair stats = pair(x.rows, at::kFloat, x.device());
     enqueue(x.device(), a[8], [&](void* stream) {
         return fh_layer_norm_mx(x.data(), (fh_dtype)x.dtype, x.rows, x.cols, x.stride, p.w, p.b, (fh_dtype)p.dtype, eps, rounding, seed, id,
-                                s.data(s.by_rows), s.size(s.by_rows), s.data(s.by_columns), s.size(s.by_columns), mean.data_ptr(), rstd.data_ptr(), stream);
+                                s.data(s.by_rows), s.size(s.by_rows), s.data(s.by_columns), s.size(s.by_columns), stats.first.data_ptr(), stats.second.data_ptr(), stream);
     });
-    return tuple(s.wrapped(), Ref(wrap(mean)), Ref(wrap(rstd)));
+    return tuple(s.wrapped(), Ref(wrap(stats.first)), Ref(wrap(stats.second)));
 FH_EXIT
 
 // (dy, x, mean, rstd, weight, sums, dx, workspace, stream)
@@ -399,17 +410,16 @@ FH_ENTRY(layer_norm_backward, 9)
     const Matrix dx = matrix_like(a[6], x, "dx");
     const at::ScalarType type = weight.defined() ? weight.scalar_type() : x.t.scalar_type();
     const int p_dtype = dtype_code(type);
-    at::Tensor dweight, dbias;
+    Pair sum;
     Work w;
     if (sums) {
-        dweight = values(x.cols, type, device);
-        dbias = values(x.cols, type, device);
+        sum = pair(x.cols, type, device);
         w = work(a[7], fh_layer_norm_backward_workspace_bytes(x.rows, x.cols), device, a[8]);
     }
     const fh_norm_backward b = {dy.data(), x.data(), dy.stride, x.stride, mean_at, rstd_at, weight_at, x.rows, x.cols, x.dtype, p_dtype, dx.data(), dx.stride,
-                                dx.bytes(), sums ? dweight.data_ptr() : nullptr, sums ? dbias.data_ptr() : nullptr, w.p, w.n};
+                                dx.bytes(), sums ? sum.first.data_ptr() : nullptr, sums ? sum.second.data_ptr() : nullptr, w.p, w.n};
     enqueue(device, a[8], [&](void* stream) { return fh_layer_norm_backward(&b, stream); });
-    return tuple(Ref(wrap(dx.t)), Ref(wrap(dweight)), Ref(wrap(dbias)));
+    return tuple(Ref(wrap(dx.t)), Ref(wrap(sum.first)), Ref(wrap(sum.second)));
 FH_EXIT
 
 // (x, weight, bias, norm, norm_weight, norm_bias, eps, needs_input, needs_weight, stream) -> (y, kept)
@@ -462,7 +472,8 @@ FH_ENTRY(layer_backward, 14)
     l.rounding = rounding_of(a[10]); l.seed = u64(a[11]); l.tensor_id = u64(a[12]);
     l.dy = dy.data(); l.dy_stride = dy.stride; l.x_stride = l.weight_stride = l.features;
     l.kept = kept.data_ptr(); l.kept_cap = kept.nbytes();
-    at::Tensor dx, dweight, dnorm_weight, dnorm_bias;
+    at::Tensor dx, dweight;
+    Pair dnorm;
     Matrix x{};
     if (needs_weight) {
         dweight = new_matrix(l.out_features, l.features, p_type, device).t;
@@ -478,15 +489,14 @@ FH_ENTRY(layer_backward, 14)
             on_device(x.t, device, "x");
             l.x = x.data(); l.x_stride = x.stride;
             l.norm_weight = vector(norm_weight, l.features, device, "norm_weight");
-            dnorm_weight = values(l.features, p_type, device);
-            dnorm_bias = values(l.features, p_type, device);
-            l.dnorm_weight = dnorm_weight.data_ptr(); l.dnorm_bias = dnorm_bias.data_ptr();
+            dnorm = pair(l.features, p_type, device);
+            l.dnorm_weight = dnorm.first.data_ptr(); l.dnorm_bias = dnorm.second.data_ptr();
         }
     }
     const Work w = work(Py_None, fh_mx_layer_scratch_bytes(l.tokens, l.features, l.out_features), device, a[13]);
     l.scratch = w.p; l.scratch_cap = w.n;
     enqueue(device, a[13], [&](void* stream) { return fh_mx_layer_backward(&l, stream); });
-    return tuple(Ref(wrap(dx)), Ref(wrap(dweight)), Ref(wrap(dnorm_weight)), Ref(wrap(dnorm_bias)));
+    return tuple(Ref(wrap(dx)), Ref(wrap(dweight)), Ref(wrap(dnorm.first)), Ref(wrap(dnorm.second)));
 FH_EXIT
 
 // (FedHybridError, MxMatrix): the classes that results and errors are of.

@@ -413,9 +413,8 @@ hipError_t norm_of(const void* x, int64_t rows, int64_t cols, int64_t xs, const 
     constexpr int64_t kStay = kHeld < kThreads ? 256 : 256 * (kHeld / kThreads);
     int64_t groups = (rows + kRows - 1) / kRows;
     if (groups > kStay) groups = kStay;
-    hipLaunchKernelGGL((norm_rows_kernel<T, THREADS, NV, MX>), dim3((uint32_t)groups), dim3(kThreads), 0, s, static_cast<const T*>(x), rows, cols,
+    return launch(norm_rows_kernel<T, THREADS, NV, MX>, dim3((uint32_t)groups), dim3(kThreads), s, static_cast<const T*>(x), rows, cols,
                        xs, n, to, (int32_t)groups);
-    return hipGetLastError();
 }
 template <typename T, bool MX>
 hipError_t norm_any(const void* x, int64_t rows, int64_t cols, int64_t xs, const NormArgs& n, const NormOut& to, hipStream_t s)
@@ -442,8 +441,7 @@ hipError_t norm_any(const void* x, int64_t rows, int64_t cols, int64_t xs, const
         if (cols <= 12288) return norm_of<T, 512, 3, MX>(x, rows, cols, xs, n, to, s);
         if (cols <= kGroupCols) return norm_of<T, 512, 4, MX>(x, rows, cols, xs, n, to, s);
     }
-    hipLaunchKernelGGL((norm_long_rows_kernel<T, MX>), dim3((uint32_t)rows), dim3(1024), 0, s, static_cast<const T*>(x), cols, xs, n, to);
-    return hipGetLastError();
+    return launch(norm_long_rows_kernel<T, MX>, dim3((uint32_t)rows), dim3(1024), s, static_cast<const T*>(x), cols, xs, n, to);
 }
 
 // Threads that share a row of the backward pass, runs of four columns a thread, rows that a workgroup takes at a time (as many as
@@ -469,8 +467,7 @@ inline int64_t backward_groups(int64_t rows, int64_t cols)
 template <typename T, int THREADS, int NV, int ROWS>
 hipError_t backward_of(const NormBackwardArgs& a, int64_t groups, hipStream_t s)
 {
-    hipLaunchKernelGGL((norm_backward_kernel<T, THREADS, NV, ROWS>), dim3((uint32_t)groups), dim3(THREADS * ROWS), 0, s, a);
-    return hipGetLastError();
+    return launch(norm_backward_kernel<T, THREADS, NV, ROWS>, dim3((uint32_t)groups), dim3(THREADS * ROWS), s, a);
 }
 template <typename T>
 hipError_t backward_any(const NormBackwardArgs& a, int64_t* parts, hipStream_t s)
@@ -498,19 +495,16 @@ hipError_t backward_any(const NormBackwardArgs& a, int64_t* parts, hipStream_t s
     if (a.partial) {                                             // first: dx may be dy itself
         const int64_t each = (a.rows + groups - 1) / groups, col_groups = (a.cols + 2047) / 2048;
         *parts = (a.rows + each - 1) / each;
-        hipLaunchKernelGGL((norm_column_sums_kernel<T>), dim3((uint32_t)(col_groups * *parts)), dim3(256), 0, s, a, each, (uint32_t)col_groups);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = launch(norm_column_sums_kernel<T>, dim3((uint32_t)(col_groups * *parts)), dim3(256), s, a, each, (uint32_t)col_groups);
         if (e != hipSuccess) return e;
     }
-    if (a.dx) hipLaunchKernelGGL((norm_backward_long_rows_kernel<T>), dim3((uint32_t)a.rows), dim3(1024), 0, s, a);
-    return hipGetLastError();
+    return a.dx ? launch(norm_backward_long_rows_kernel<T>, dim3((uint32_t)a.rows), dim3(1024), s, a) : hipSuccess;
 }
 template <typename P>
 hipError_t join_of(const float* partial, int64_t parts, int64_t cols, void* dweight, void* dbias, hipStream_t s)
 {
-    hipLaunchKernelGGL((norm_join_kernel<P>), dim3((uint32_t)((cols + 63) / 64 * 2)), dim3(1024), 0, s, partial, parts, cols,
+    return launch(norm_join_kernel<P>, dim3((uint32_t)((cols + 63) / 64 * 2)), dim3(1024), s, partial, parts, cols,
                        static_cast<P*>(dweight), static_cast<P*>(dbias));
-    return hipGetLastError();
 }
 
 bool norm_shape_ok(int64_t rows, int64_t cols) { return mx_shape_ok(rows, cols) && cols >= 1; }

@@ -133,6 +133,16 @@ struct Bf16 { uint16_t bits; };
 __device__ __forceinline__ float value(float v) { return v; }
 __device__ __forceinline__ float value(Bf16 v) { return __builtin_bit_cast(float, (uint32_t)v.bits << 16); }
 
+// A launch as the runtime takes it; <<< >>> lays its shape aside on the way, which is 0.2 us of the host's 2.4.
+template <typename... P, typename... A>
+hipError_t launch(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t s, const A&... given)
+{
+    return [&](P... args) {
+        void* list[] = {static_cast<void*>(&args)...};
+        return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, list, 0, s);
+    }(given...);
+}
+
 // N values in words as they lie in memory.
 template <typename T, int N = 8>
 struct Run {

@@ -426,8 +426,7 @@ hipError_t waves_of(ProductArgs p, hipStream_t s)
     if (groups > INT32_MAX) return hipErrorInvalidValue;
     p.m_tiles = (uint32_t)m_tiles;
     p.n_tiles = (uint32_t)n_tiles;
-    hipLaunchKernelGGL((mx_waves_kernel<T, MT, NT, WAVES>), dim3((uint32_t)groups), dim3(WAVES * 64), 0, s, p);
-    return hipGetLastError();
+    return launch(mx_waves_kernel<T, MT, NT, WAVES>, dim3((uint32_t)groups), dim3(WAVES * 64), s, p);
 }
 template <typename T, int B, int WN>
 hipError_t squares_of(ProductArgs p, hipStream_t s)
@@ -439,8 +438,7 @@ hipError_t squares_of(ProductArgs p, hipStream_t s)
     p.n_tiles = (uint32_t)n_tiles;
     const uint32_t grid = (uint32_t)(m_tiles * n_tiles < groups ? m_tiles * n_tiles : groups);
     p.step = (grid + 7) / 8;
-    hipLaunchKernelGGL((mx_tile_kernel<T, B, WN>), dim3(grid), dim3(2 * WN * 64), 0, s, p);
-    return hipGetLastError();
+    return launch(mx_tile_kernel<T, B, WN>, dim3(grid), dim3(2 * WN * 64), s, p);
 }
 template <typename T>
 hipError_t product_of(const ProductArgs& p, const Plan& plan, float* workspace, hipStream_t s)
@@ -460,9 +458,8 @@ hipError_t product_of(const ProductArgs& p, const Plan& plan, float* workspace, 
     const hipError_t e = waves_of<float, 1, 1, 8>(q, s);
     if (e != hipSuccess) return e;
     const int64_t runs = (p.n + 3) / 4, groups = (p.m * runs + 255) / 256;
-    hipLaunchKernelGGL((mx_join_kernel<T>), dim3((uint32_t)groups), dim3(256), 0, s, workspace, p.m, p.n, p.parts, p.bias, p.bias_dtype,
+    return launch(mx_join_kernel<T>, dim3((uint32_t)groups), dim3(256), s, workspace, p.m, p.n, p.parts, p.bias, p.bias_dtype,
                        static_cast<T*>(p.out), p.stride, (uint32_t)runs);
-    return hipGetLastError();
 }
 
 }  // namespace

@@ -252,8 +252,7 @@ hipError_t rows_of(const void* x, int64_t rows, int64_t cols, int64_t stride, co
 {
     dim3 grid;
     if (!grid_of(rows, to.chunks, 32, grid)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((mx_rows_kernel<T>), grid, dim3(kThreads), 0, s, static_cast<const T*>(x), rows, cols, stride, to);
-    return hipGetLastError();
+    return launch(mx_rows_kernel<T>, grid, dim3(kThreads), s, static_cast<const T*>(x), rows, cols, stride, to);
 }
 
 template <typename T, bool NORM, bool STOCHASTIC>
@@ -264,10 +263,9 @@ hipError_t tiles_of(const void* x, int64_t rows, int64_t cols, int64_t stride, c
     const int64_t width = by_rows ? mx_chunks(cols) * kMxChunk : cols, col_tiles = (width + kTileCols<T> - 1) / kTileCols<T>;
     const int64_t row_tiles = (rows + kTileRows - 1) / kTileRows;
     if (col_tiles * row_tiles > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((mx_tiles_kernel<T, NORM, STOCHASTIC>), dim3((uint32_t)(col_tiles * row_tiles)), dim3(kTileThreads), 0, s,
+    return launch(mx_tiles_kernel<T, NORM, STOCHASTIC>, dim3((uint32_t)(col_tiles * row_tiles)), dim3(kTileThreads), s,
                        static_cast<const T*>(x), rows, cols, stride, n, (uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)id,
                        (uint32_t)(id >> 32), static_cast<uint8_t*>(by_rows), static_cast<uint8_t*>(by_columns), (uint32_t)col_tiles);
-    return hipGetLastError();
 }
 
 template <typename T>
@@ -275,8 +273,7 @@ hipError_t restore_of(const MxStore& from, int64_t rows, int64_t cols, void* out
 {
     dim3 grid;
     if (!grid_of(rows, from.chunks, sizeof(T) == 4 ? 64 : 32, grid)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((mx_restore_kernel<T>), grid, dim3(kThreads), 0, s, from, rows, cols, static_cast<T*>(out), stride);
-    return hipGetLastError();
+    return launch(mx_restore_kernel<T>, grid, dim3(kThreads), s, from, rows, cols, static_cast<T*>(out), stride);
 }
 
 // Where a stored form is wanted: its buffer's checks.
