@@ -6,6 +6,8 @@
 // 4.2, a norm 10.4 and 5.1, its backward pass (two launches) 16.3 and 8.8; a training step of a layer of 8192 x 768 tokens 162 and 119 us.
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/hip/EmptyTensor.h>
@@ -20,11 +22,19 @@ PyObject* g_error;                       // FedHybridError(status)
 PyObject* g_matrix;                      // MxMatrix(data, rows, cols)
 PyObject *g_data, *g_rows, *g_cols, *g_cuda_stream, *g_nearest, *g_stochastic;     // interned names
 
+// The interpreter's lock; autograd's threads come without it.
+struct Inside {
+    PyGILState_STATE state = PyGILState_Ensure();
+    ~Inside() { PyGILState_Release(state); }
+};
 template <typename... A>
 [[noreturn]] void raise(PyObject* type, const char* format, A... a)
 {
+    const Inside inside;
     PyErr_Format(type, format, a...);
-    throw python_error();
+    python_error e;
+    e.persist();
+    throw e;
 }
 
 // An owned reference.
@@ -235,11 +245,11 @@ struct Outside {
     {
         if (before != index) c10::hip::set_device(index);
         else before = -1;
-        gil = PyEval_SaveThread();
+        gil = PyGILState_Check() ? PyEval_SaveThread() : nullptr;
     }
     ~Outside()
     {
-        PyEval_RestoreThread(gil);
+        if (gil) PyEval_RestoreThread(gil);
         if (before >= 0) c10::hip::set_device(before);
     }
 };
@@ -255,9 +265,12 @@ void enqueue(c10::Device device, PyObject* stream, F call)
         status = call(handle);
     }
     if (status == FH_OK) return;
-    Ref e(PyObject_CallFunction(g_error, "i", (int)status));
-    PyErr_SetObject(g_error, e.p);
-    throw python_error();
+    const Inside inside;
+    Ref value(PyObject_CallFunction(g_error, "i", (int)status));
+    PyErr_SetObject(g_error, value.p);
+    python_error e;
+    e.persist();
+    throw e;
 }
 
 // What the forms of a stored matrix are asked for by.
@@ -422,81 +435,188 @@ FH_ENTRY(layer_norm_backward, 9)
     return tuple(Ref(wrap(dx.t)), Ref(wrap(sum.first)), Ref(wrap(sum.second)));
 FH_EXIT
 
-// (x, weight, bias, norm, norm_weight, norm_bias, eps, needs_input, needs_weight, stream) -> (y, kept)
-FH_ENTRY(layer_forward, 10)
-    const Matrix x = matrix(a[0], "x"), weight = matrix(a[1], "weight");
-    const at::Tensor bias = tensor_or_none(a[2], "bias"), norm_weight = tensor_or_none(a[4], "norm_weight"), norm_bias = tensor_or_none(a[5], "norm_bias");
+// ---- a linear layer's two halves ----------------------------------------------------------------
+struct Layer { bool norm; float eps; bool input, weight; int rounding; uint64_t seed, id; };    // input, weight: what gradients are wanted of
+
+struct Forward { at::Tensor y, kept; };
+Forward forward_of(const Layer& layer, const Matrix& x, const Matrix& weight, const at::Tensor& bias, const at::Tensor& norm_weight, const at::Tensor& norm_bias,
+                   PyObject* stream)
+{
     const c10::Device device = x.device();
     if (weight.cols != x.cols) raise(PyExc_ValueError, "x has %lld features, weight takes %lld", (long long)x.cols, (long long)weight.cols);
     on_device(weight.t, device, "weight");
     for (const at::Tensor* t : {&bias, &norm_weight, &norm_bias})
         if (t->defined() && t->scalar_type() != weight.t.scalar_type())
             raise(PyExc_TypeError, "the parameters of one layer are of one dtype, as its weight: %s", c10::toString(weight.t.scalar_type()));
-    const int32_t norm = truth(a[3]), needs = (truth(a[7]) ? FH_MX_NEEDS_INPUT : 0) | (truth(a[8]) ? FH_MX_NEEDS_WEIGHT : 0);
     fh_mx_layer l = {};
     l.tokens = x.rows; l.features = x.cols; l.out_features = weight.rows;
-    l.dtype = x.dtype; l.p_dtype = weight.dtype; l.norm = norm; l.needs = needs;
-    l.eps = (float)f64(a[6]);
+    l.dtype = x.dtype; l.p_dtype = weight.dtype; l.norm = layer.norm;
+    l.needs = (layer.input ? FH_MX_NEEDS_INPUT : 0) | (layer.weight ? FH_MX_NEEDS_WEIGHT : 0);
+    l.eps = layer.eps;
     l.x = x.data(); l.x_stride = x.stride; l.weight = weight.data(); l.weight_stride = weight.stride; l.dy_stride = weight.rows;
     l.norm_weight = vector(norm_weight, x.cols, device, "norm_weight");
     l.norm_bias = vector(norm_bias, x.cols, device, "norm_bias");
     l.bias = vector(bias, weight.rows, device, "bias");
-    const Matrix y = new_matrix(x.rows, weight.rows, x.t.scalar_type(), device);
-    l.y = y.data();
-    at::Tensor kept;
-    if (norm || needs) {
-        kept = bytes(fh_mx_layer_kept_bytes(l.tokens, l.features, l.out_features), device);
-        l.kept = kept.data_ptr(); l.kept_cap = (size_t)kept.numel();
+    Forward f;
+    f.y = new_matrix(x.rows, weight.rows, x.t.scalar_type(), device).t;
+    l.y = f.y.data_ptr();
+    if (layer.norm || l.needs) {
+        f.kept = bytes(fh_mx_layer_kept_bytes(l.tokens, l.features, l.out_features), device);
+        l.kept = f.kept.data_ptr(); l.kept_cap = (size_t)f.kept.numel();
     }
-    const Work w = work(Py_None, fh_mx_layer_scratch_bytes(l.tokens, l.features, l.out_features), device, a[9]);
+    const Work w = work(Py_None, fh_mx_layer_scratch_bytes(l.tokens, l.features, l.out_features), device, stream);
     l.scratch = w.p; l.scratch_cap = w.n;
-    enqueue(device, a[9], [&](void* stream) { return fh_mx_layer_forward(&l, stream); });
-    return tuple(Ref(wrap(y.t)), Ref(wrap(kept)));
+    enqueue(device, stream, [&](void* s) { return fh_mx_layer_forward(&l, s); });
+    return f;
+}
+
+struct Backward { at::Tensor dx, dweight; Pair dnorm; };
+Backward backward_of(const Layer& layer, const Matrix& dy, const at::Tensor& x_again, const at::Tensor& norm_weight, const at::Tensor& kept, int64_t features,
+                     at::ScalarType p_type, PyObject* stream)
+{
+    const c10::Device device = dy.device();
+    in_device_memory(kept, "kept");
+    on_device(kept, device, "kept");
+    const at::ScalarType type = dy.t.scalar_type();
+    fh_mx_layer l = {};
+    l.tokens = dy.rows; l.features = features; l.out_features = dy.cols;
+    l.dtype = dy.dtype; l.p_dtype = dtype_code(p_type); l.norm = layer.norm;
+    l.needs = (layer.input ? FH_MX_NEEDS_INPUT : 0) | (layer.weight ? FH_MX_NEEDS_WEIGHT : 0);
+    l.eps = layer.eps;
+    l.rounding = layer.rounding; l.seed = layer.seed; l.tensor_id = layer.id;
+    l.dy = dy.data(); l.dy_stride = dy.stride; l.x_stride = l.weight_stride = features;
+    l.kept = kept.data_ptr(); l.kept_cap = kept.nbytes();
+    Backward b;
+    Matrix x{};
+    if (layer.weight) {
+        b.dweight = new_matrix(l.out_features, features, p_type, device).t;
+        l.dweight = b.dweight.data_ptr();
+    }
+    if (layer.input) {
+        b.dx = new_matrix(l.tokens, features, type, device).t;
+        l.dx = b.dx.data_ptr();
+        if (layer.norm) {
+            if (!x_again.defined()) raise(PyExc_ValueError, "with a norm the backward call takes x again");
+            x = matrix(x_again, "x");
+            if (x.rows != l.tokens || x.cols != features || x.dtype != l.dtype) raise(PyExc_ValueError, "x must have the shape and the dtype of the forward call's");
+            on_device(x.t, device, "x");
+            l.x = x.data(); l.x_stride = x.stride;
+            l.norm_weight = vector(norm_weight, features, device, "norm_weight");
+            b.dnorm = pair(features, p_type, device);
+            l.dnorm_weight = b.dnorm.first.data_ptr(); l.dnorm_bias = b.dnorm.second.data_ptr();
+        }
+    }
+    const Work w = work(Py_None, fh_mx_layer_scratch_bytes(l.tokens, features, l.out_features), device, stream);
+    l.scratch = w.p; l.scratch_cap = w.n;
+    enqueue(device, stream, [&](void* s) { return fh_mx_layer_backward(&l, s); });
+    return b;
+}
+
+// (x, weight, bias, norm, norm_weight, norm_bias, eps, needs_input, needs_weight, stream) -> (y, kept)
+FH_ENTRY(layer_forward, 10)
+    const Layer layer = {truth(a[3]), (float)f64(a[6]), truth(a[7]), truth(a[8]), FH_ROUND_NEAREST, 0, 0};
+    const Forward f = forward_of(layer, matrix(a[0], "x"), matrix(a[1], "weight"), tensor_or_none(a[2], "bias"), tensor_or_none(a[4], "norm_weight"),
+                                 tensor_or_none(a[5], "norm_bias"), a[9]);
+    return tuple(Ref(wrap(f.y)), Ref(wrap(f.kept)));
 FH_EXIT
 
 // (dy, x, norm_weight, kept, features, p_dtype, norm, eps, needs_input, needs_weight, rounding, seed, tensor_id, stream)
 //   -> (dx, dweight, dnorm_weight, dnorm_bias)
 FH_ENTRY(layer_backward, 14)
-    const Matrix dy = matrix(a[0], "dy");
-    const c10::Device device = dy.device();
-    const at::Tensor norm_weight = tensor_or_none(a[2], "norm_weight"), kept = tensor(a[3], "kept");
-    in_device_memory(kept, "kept");
-    on_device(kept, device, "kept");
-    const at::ScalarType type = dy.t.scalar_type(), p_type = scalar_type(a[5]);
-    const bool norm = truth(a[6]), input = truth(a[8]), needs_weight = truth(a[9]);
-    fh_mx_layer l = {};
-    l.tokens = dy.rows; l.features = i64(a[4]); l.out_features = dy.cols;
-    l.dtype = dy.dtype; l.p_dtype = dtype_code(p_type); l.norm = norm;
-    l.needs = (input ? FH_MX_NEEDS_INPUT : 0) | (needs_weight ? FH_MX_NEEDS_WEIGHT : 0);
-    l.eps = (float)f64(a[7]);
-    l.rounding = rounding_of(a[10]); l.seed = u64(a[11]); l.tensor_id = u64(a[12]);
-    l.dy = dy.data(); l.dy_stride = dy.stride; l.x_stride = l.weight_stride = l.features;
-    l.kept = kept.data_ptr(); l.kept_cap = kept.nbytes();
-    at::Tensor dx, dweight;
-    Pair dnorm;
-    Matrix x{};
-    if (needs_weight) {
-        dweight = new_matrix(l.out_features, l.features, p_type, device).t;
-        l.dweight = dweight.data_ptr();
+    const Layer layer = {truth(a[6]), (float)f64(a[7]), truth(a[8]), truth(a[9]), rounding_of(a[10]), u64(a[11]), u64(a[12])};
+    const Backward b = backward_of(layer, matrix(a[0], "dy"), tensor_or_none(a[1], "x"), tensor_or_none(a[2], "norm_weight"), tensor(a[3], "kept"), i64(a[4]),
+                                   scalar_type(a[5]), a[13]);
+    return tuple(Ref(wrap(b.dx)), Ref(wrap(b.dweight)), Ref(wrap(b.dnorm.first)), Ref(wrap(b.dnorm.second)));
+FH_EXIT
+
+// ---- the same as a step of autograd -------------------------------------------------------------
+// x as a matrix of its last dimension, its rows contiguous and apart (an expanded gradient's are not).
+at::Tensor rows_of(const at::Tensor& x)
+{
+    const at::Tensor m = x.dim() == 2 ? x : x.reshape({-1, x.size(-1)});
+    return m.stride(1) == 1 && m.stride(0) >= m.size(1) ? m : m.contiguous();
+}
+
+// y's rows in the order of x's.
+at::Tensor shaped(const at::Tensor& y, const at::Tensor& x)
+{
+    if (x.dim() == 2) return y;
+    std::vector<int64_t> shape = x.sizes().vec();
+    shape.back() = y.size(1);
+    return y.view(shape);
+}
+
+struct Pass : torch::CustomClassHolder {                                  // from one half to the other, but for what is saved as a variable
+    Layer layer;
+    bool x, norm_weight, norm_bias, bias;                                 // whose gradients are wanted
+    at::Tensor kept;
+    std::vector<int64_t> shape;
+    int64_t features;
+    at::ScalarType p_type, bias_type;
+};
+
+struct Linear : torch::autograd::Function<Linear> {
+    using Context = torch::autograd::AutogradContext;
+    static at::Tensor forward(Context* ctx, const at::Tensor& x, const std::optional<at::Tensor>& norm_weight, const std::optional<at::Tensor>& norm_bias,
+                              const at::Tensor& weight, const std::optional<at::Tensor>& bias, const c10::intrusive_ptr<Pass>& pass)
+    {
+        const at::Tensor m = rows_of(x);
+        Forward f = forward_of(pass->layer, matrix(m, "x"), matrix(weight, "weight"), bias.value_or(at::Tensor()), norm_weight.value_or(at::Tensor()),
+                               norm_bias.value_or(at::Tensor()), Py_None);
+        pass->kept = std::move(f.kept);
+        pass->features = m.size(1);
+        if (pass->layer.norm && pass->layer.input) ctx->save_for_backward({m, norm_weight.value_or(at::Tensor())});
+        ctx->saved_data.emplace("pass", c10::IValue::make_capsule(pass));
+        return shaped(f.y, x);
     }
-    if (input) {
-        dx = new_matrix(l.tokens, l.features, type, device).t;
-        l.dx = dx.data_ptr();
-        if (norm) {
-            if (a[1] == Py_None) raise(PyExc_ValueError, "with a norm the backward call takes x again");
-            x = matrix(a[1], "x");
-            if (x.rows != l.tokens || x.cols != l.features || x.dtype != l.dtype) raise(PyExc_ValueError, "x must have the shape and the dtype of the forward call's");
-            on_device(x.t, device, "x");
-            l.x = x.data(); l.x_stride = x.stride;
-            l.norm_weight = vector(norm_weight, l.features, device, "norm_weight");
-            dnorm = pair(l.features, p_type, device);
-            l.dnorm_weight = dnorm.first.data_ptr(); l.dnorm_bias = dnorm.second.data_ptr();
+    static torch::autograd::variable_list backward(Context* ctx, const torch::autograd::variable_list& given)
+    {
+        const auto pass = c10::static_intrusive_pointer_cast<Pass>(ctx->saved_data.at("pass").toCapsule());
+        const bool again = at::GradMode::is_enabled() && given[0].requires_grad();
+        torch::autograd::variable_list grads(6);
+        {
+            const at::AutoGradMode off(false);
+            const at::Tensor dy = rows_of(given[0]);
+            if (pass->layer.input || pass->layer.weight) {
+                const auto saved = ctx->get_saved_variables();
+                const Backward b = backward_of(pass->layer, matrix(dy, "dy"), saved.empty() ? at::Tensor() : saved[0], saved.empty() ? at::Tensor() : saved[1],
+                                               pass->kept, pass->features, pass->p_type, Py_None);
+                if (pass->x) grads[0] = b.dx.view(pass->shape);
+                if (pass->norm_weight) grads[1] = b.dnorm.first;
+                if (pass->norm_bias) grads[2] = b.dnorm.second;
+                grads[3] = b.dweight;
+            }
+            if (pass->bias) grads[4] = dy.to(at::kFloat).sum(0).to(pass->bias_type);
         }
+        if (!again) return grads;
+        for (at::Tensor& g : grads)                                       // leaves of a graph that ends in an error
+            if (g.defined()) g = g.detach().set_requires_grad(true);
+        return torch::autograd::DelayedError("a linear layer in microscaled form is differentiated once", (int64_t)grads.size()).apply(std::move(grads));
     }
-    const Work w = work(Py_None, fh_mx_layer_scratch_bytes(l.tokens, l.features, l.out_features), device, a[13]);
-    l.scratch = w.p; l.scratch_cap = w.n;
-    enqueue(device, a[13], [&](void* stream) { return fh_mx_layer_backward(&l, stream); });
-    return tuple(Ref(wrap(dx)), Ref(wrap(dweight)), Ref(wrap(dnorm.first)), Ref(wrap(dnorm.second)));
+};
+
+// (x, norm_weight, norm_bias, weight, bias, eps or None where there is no norm, rounding, seed, tensor_id) -> y
+FH_ENTRY(mx_linear, 9)
+    const at::Tensor x = tensor(a[0], "x"), norm_weight = tensor_or_none(a[1], "norm_weight"), norm_bias = tensor_or_none(a[2], "norm_bias"),
+                     weight = tensor(a[3], "weight"), bias = tensor_or_none(a[4], "bias");
+    in_device_memory(x, "x");
+    if (x.dim() == 0) raise(PyExc_ValueError, "x must have a dimension");
+    const auto pass = c10::make_intrusive<Pass>();
+    const bool norm = a[5] != Py_None, grad = at::GradMode::is_enabled();
+    const auto wanted = [&](const at::Tensor& t) { return grad && t.defined() && t.requires_grad(); };
+    pass->x = wanted(x); pass->norm_weight = wanted(norm_weight); pass->norm_bias = wanted(norm_bias); pass->bias = wanted(bias);
+    pass->layer = {norm, norm ? (float)f64(a[5]) : 0.0f, pass->x || pass->norm_weight || pass->norm_bias, wanted(weight), rounding_of(a[6]), u64(a[7]), u64(a[8])};
+    pass->p_type = weight.scalar_type();
+    pass->bias_type = bias.defined() ? bias.scalar_type() : at::kFloat;
+    pass->shape = x.sizes().vec();
+    at::Tensor y;
+    if (pass->layer.input || pass->layer.weight || pass->bias) {
+        const auto some = [](const at::Tensor& t) { return t.defined() ? std::optional<at::Tensor>(t) : std::nullopt; };
+        y = Linear::apply(x, some(norm_weight), some(norm_bias), weight, some(bias), pass);
+    } else {
+        y = shaped(forward_of(pass->layer, matrix(rows_of(x), "x"), matrix(weight, "weight"), bias, norm_weight, norm_bias, Py_None).y, x);
+    }
+    return wrap(y);
 FH_EXIT
 
 // (FedHybridError, MxMatrix): the classes that results and errors are of.
@@ -508,7 +628,8 @@ FH_EXIT
 
 #define FH_METHOD(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {FH_METHOD(mx_quantize), FH_METHOD(mx_dequantize), FH_METHOD(mx_matmul), FH_METHOD(layer_norm), FH_METHOD(layer_norm_mx),
-                           FH_METHOD(layer_norm_backward), FH_METHOD(layer_forward), FH_METHOD(layer_backward), FH_METHOD(use), {}};
+                           FH_METHOD(layer_norm_backward), FH_METHOD(layer_forward), FH_METHOD(layer_backward), FH_METHOD(mx_linear),
+                           FH_METHOD(use), {}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_fh_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

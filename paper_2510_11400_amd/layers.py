@@ -17,7 +17,7 @@ from typing import Optional
 
 import torch
 
-from . import api
+from . import _fh_binding as _binding, api
 
 
 def _rows(x: torch.Tensor) -> torch.Tensor:
@@ -44,34 +44,6 @@ class _LayerNorm(torch.autograd.Function):
                 db if ctx.needs_input_grad[2] else None, None)
 
 
-class _MxLinear(torch.autograd.Function):
-    """norm(x) W^T + b, the norm left out where `norm` is None, else its eps."""
-
-    @staticmethod
-    def forward(ctx, x, norm_weight, norm_bias, weight, bias, norm, rounding, seed, tensor_id):
-        m, needs = _rows(x), ctx.needs_input_grad
-        needs_input = needs[0] or needs[1] or needs[2]
-        layer = api.MxLayer(m, weight, bias, norm is not None, norm_weight, norm_bias, 0.0 if norm is None else norm, needs_input, needs[3],
-                            rounding, seed, tensor_id)
-        y = layer.forward()
-        ctx.layer, ctx.shape, ctx.bias_dtype = layer, x.shape, None if bias is None else bias.dtype
-        if norm is not None and needs_input:
-            ctx.save_for_backward(m, norm_weight)
-        return y if x.dim() == 2 else y.view(*x.shape[:-1], weight.shape[0])
-
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, dy):
-        needs, layer, g = ctx.needs_input_grad, ctx.layer, _rows(dy)
-        x, norm_weight = ctx.saved_tensors if layer.norm and layer.needs_input else (None, None)
-        dx = dw = d_norm_weight = d_norm_bias = None
-        if layer.needs_input or layer.needs_weight:
-            dx, dw, d_norm_weight, d_norm_bias = layer.backward(g, x, norm_weight)
-        db = g.float().sum(0).to(ctx.bias_dtype) if needs[4] else None
-        return (dx.view(ctx.shape) if needs[0] else None, d_norm_weight if needs[1] else None, d_norm_bias if needs[2] else None, dw, db,
-                None, None, None, None)
-
-
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5) -> torch.Tensor:
     """Layer norm over the last dimension, differentiable.  x is saved as it is: under hooks.SavedActivations it is stored
     compressed, like any activation that autograd saves."""
@@ -82,7 +54,7 @@ def mx_linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor
               tensor_id: int = 0) -> torch.Tensor:
     """x W^T + bias with all three products of a training step in microscaled 4-bit form.  rounding, seed and tensor_id
     are those of the gradient's quantisation; activations and weights are rounded to the nearest."""
-    return _MxLinear.apply(x, None, None, weight, bias, None, rounding, seed, tensor_id)
+    return _binding.mx_linear(x, None, None, weight, bias, None, rounding, seed, tensor_id)
 
 
 def layer_norm_mx_linear(x: torch.Tensor, norm_weight: Optional[torch.Tensor], norm_bias: Optional[torch.Tensor], weight: torch.Tensor,
@@ -90,7 +62,7 @@ def layer_norm_mx_linear(x: torch.Tensor, norm_weight: Optional[torch.Tensor], n
                          tensor_id: int = 0) -> torch.Tensor:
     """mx_linear(layer_norm(x)) without the norm's output ever being written but as codes.  x is saved as autograd saves it
     (hooks.SavedActivations compresses it); the product's operands are kept in 4-bit form.  The parameters are of one dtype."""
-    return _MxLinear.apply(x, norm_weight, norm_bias, weight, bias, eps, rounding, seed, tensor_id)
+    return _binding.mx_linear(x, norm_weight, norm_bias, weight, bias, eps, rounding, seed, tensor_id)
 
 
 class LayerNorm(torch.nn.Module):

@@ -252,3 +252,45 @@ def test_gradients_that_are_one_row_everywhere(layers):
     got = torch.autograd.grad((y.sum(0) * scale[0]).sum(), z, retain_graph=True)
     want = torch.autograd.grad(y, z, scale[0].expand(y.shape).contiguous())
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_differentiated_once(layers):
+    """A second derivative is refused when it is asked for, also where the first one was asked for with a graph."""
+    x, w = torch.randn(64, 96, device="cuda").requires_grad_(), torch.randn(40, 96, device="cuda").requires_grad_()
+    dy = torch.randn(64, 40, device="cuda").requires_grad_()
+    dx, dw = torch.autograd.grad(layers.mx_linear(x, w), (x, w), dy, create_graph=True)
+    want = torch.autograd.grad(layers.mx_linear(x, w), (x, w), dy.detach())
+    assert torch.equal(dx, want[0]) and torch.equal(dw, want[1])
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(dx.sum() + dw.sum(), dy, retain_graph=True)
+    with pytest.raises(RuntimeError, match="once"):
+        (dx.sum() + dw.sum()).backward()
+
+
+def test_one_row_as_a_vector_and_no_gradients_without_a_graph(layers):
+    x, w, b = torch.randn(96, device="cuda"), torch.randn(40, 96, device="cuda").requires_grad_(), torch.randn(40, device="cuda")
+    y = layers.mx_linear(x, w, b)
+    assert y.shape == (40,) and y.requires_grad
+    with torch.no_grad():
+        z = layers.mx_linear(x, w, b)
+    assert not z.requires_grad and torch.equal(z, y)
+    with torch.inference_mode():
+        z = layers.layer_norm_mx_linear(x[None], None, None, w)
+    assert z.shape == (1, 40) and torch.equal(z, layers.layer_norm_mx_linear(x[None], None, None, w))
+
+
+def test_faults_of_a_backward_pass_reach_the_caller(layers):
+    """What a saved-tensor hook gives back is checked on autograd's own thread."""
+    x, w = torch.randn(64, 96, device="cuda").requires_grad_(), torch.randn(40, 96, device="cuda")
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: t[:, :-1]):
+        y = layers.layer_norm_mx_linear(x, None, None, w)
+    with pytest.raises(ValueError, match="shape"):
+        y.sum().backward()
+    with pytest.raises(KeyError):
+        layers.mx_linear(x, w, rounding="up")
+    with pytest.raises(ValueError):
+        layers.mx_linear(x.cpu(), w)
+    with pytest.raises(ValueError):
+        layers.mx_linear(x, w[:, :-1].contiguous())
+    with pytest.raises(TypeError):
+        layers.mx_linear(x, w, torch.zeros(40, device="cuda", dtype=torch.bfloat16))
