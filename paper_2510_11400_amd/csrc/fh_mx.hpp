@@ -238,24 +238,24 @@ __device__ __forceinline__ void store4(Bf16* p, int64_t n, const float (&v)[4])
 // ---- eight values of a lane, 32 of a quad, to the stored form of their row ----------------
 // All 64 lanes are active; `first` is a multiple of 8, the quad's 32 values are one block.  Columns past the row's end hold
 // 0 (the caller's loads see to that), so that the padding becomes what a block of zeros becomes.
-__device__ __forceinline__ void mx_put8(const MxStore& to, int64_t row, int64_t first, uint32_t codes, uint32_t s, bool write)
-{
-    if (!write) return;
-    *reinterpret_cast<uint32_t*>(to.codes + row * (to.chunks * 128) + (first >> 1)) = s == 255u ? 0u : codes;
-    if ((first & 31) == 0) to.scales[mx_scale_at(row, first >> 5, to.chunks)] = (uint8_t)s;
-}
-__device__ __forceinline__ void mx_write8(const MxStore& to, int64_t row, int64_t first, const float (&v)[8], bool write)
+__device__ __forceinline__ uint32_t mx_codes8(const float (&v)[8], uint32_t& s)
 {
     uint32_t top = abs_bits(v[0]);
     for (int i = 1; i < 8; ++i) top = umax(top, abs_bits(v[i]));
-    top = quad_max(top);
-    const uint32_t s = mx_scale_byte(top);
+    s = mx_scale_byte(quad_max(top));
     uint32_t codes = 0;
     codes = mx_nearest<0>(codes, v[0], v[1], s);
     codes = mx_nearest<1>(codes, v[2], v[3], s);
     codes = mx_nearest<2>(codes, v[4], v[5], s);
-    codes = mx_nearest<3>(codes, v[6], v[7], s);
-    mx_put8(to, row, first, codes, s, write);
+    return mx_nearest<3>(codes, v[6], v[7], s);
+}
+__device__ __forceinline__ void mx_write8(const MxStore& to, int64_t row, int64_t first, const float (&v)[8], bool write)
+{
+    uint32_t s;
+    const uint32_t codes = mx_codes8(v, s);
+    if (!write) return;
+    *reinterpret_cast<uint32_t*>(to.codes + row * (to.chunks * 128) + (first >> 1)) = s == 255u ? 0u : codes;
+    if ((first & 31) == 0) to.scales[mx_scale_at(row, first >> 5, to.chunks)] = (uint8_t)s;
 }
 
 }  // namespace fh

@@ -45,15 +45,23 @@ template <typename T> constexpr int kTileCols = 256 / (int)sizeof(T);
 template <typename T, bool NORM, bool STOCHASTIC>
 __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4) void mx_tiles_kernel(const T* x, int64_t rows, int64_t cols, int64_t stride, NormArgs n,
                                                                    uint32_t k0, uint32_t k1, uint32_t id0, uint32_t id1,
-                                                                   uint8_t* rows_form, uint8_t* columns_form, uint32_t col_tiles)
+                                                                   uint8_t* rows_form, uint8_t* columns_form, uint32_t col_tiles, uint32_t tiles)
 {
     const MxStore by_rows = mx_store(rows_form, rows, cols), by_columns = mx_store(columns_form, cols, rows);
     constexpr int kCols = kTileCols<T>, kLanes = kCols / 8, kAtOnce = 64 / kLanes, kGroups = 32 / kAtOnce, kEach = kCols / 64;
     __shared__ __attribute__((aligned(16))) uint8_t s_area[8 * kWaveBytes];
     __shared__ uint32_t s_scales[kCols * 2];
+    __shared__ __attribute__((aligned(16))) uint8_t s_row_scales[8][kCols];                   // a wave's: [row][block]
     __shared__ __attribute__((aligned(16))) f32x2 s_stats[NORM ? 8 : 1][32];   // mean and 1 / deviation of a wave's rows
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t col_tile = blockIdx.x % col_tiles, row_tile = blockIdx.x / col_tiles;
+    // Workgroups go to the XCDs in turn.  In fp32 a row's codes leave by 32 bytes a tile, so an XCD takes a run of neighbours, whose
+    // parts of a line meet in its L2 (8192 x 8192, both forms: 86 -> 71 us); the halves of bf16 lose by it (48 -> 50).
+    uint32_t at = blockIdx.x;
+    if constexpr (sizeof(T) == 4) {
+        const uint32_t xcd = at & 7, share = tiles >> 3, rest = tiles & 7;
+        at = xcd * share + (xcd < rest ? xcd : rest) + (at >> 3);
+    }
+    const int64_t col_tile = at % col_tiles, row_tile = at / col_tiles;
     const int64_t r0 = row_tile * kTileRows + wave * 32, c0 = col_tile * kCols;
     const bool whole = r0 + 32 <= rows && c0 + kCols <= cols;
     uint8_t* area = s_area + wave * kWaveBytes;
@@ -95,6 +103,11 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
                 *reinterpret_cast<u32x4*>(area + (g * kAtOnce + lane / kLanes) * 256 + (lane % kLanes) * (8 * sizeof(T)) + i * 4) =
                     u32x4{run[g].w[i], run[g].w[i + 1], run[g].w[i + 2], run[g].w[i + 3]};
     }
+    const auto put = [&](int64_t row, int in_area, uint32_t codes, uint32_t s) {
+        if (row < rows && row_c < by_rows.chunks * kMxChunk)
+            *reinterpret_cast<uint32_t*>(by_rows.codes + row * (by_rows.chunks * 128) + (row_c >> 1)) = s == 255u ? 0u : codes;
+        if ((lane & 3) == 0) s_row_scales[wave][in_area * (kCols / 32) + (lane % kLanes) / 4] = (uint8_t)s;
+    };
     // the rows' form, from the registers
     auto write_rows = [&]() {
         if constexpr (STOCHASTIC) {
@@ -141,10 +154,18 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
                 const uint32_t s = mx_scale_byte(quad_max(top));
 #pragma unroll
                 for (int i = 0; i < 8; ++i) codes |= mx_stochastic(v[i], s, i & 1 ? u[i / 2] >> 16 : u[i / 2] & 0xFFFFu) << (4 * i);
-                mx_put8(by_rows, row, row_c, codes, s, row < rows && row_c < by_rows.chunks * kMxChunk);
+                put(row, in_area, codes, s);
             } else {
-                mx_write8(by_rows, row, row_c, v, row < rows && row_c < by_rows.chunks * kMxChunk);
+                uint32_t s;
+                const uint32_t codes = mx_codes8(v, s);
+                put(row, in_area, codes, s);
             }
+        }
+        asm volatile("" ::: "memory");                           // the scales of 32 rows are next to each other in the stored form
+        if (lane < 32 && r0 + lane < rows && c0 < by_rows.chunks * kMxChunk) {
+            uint8_t* to = by_rows.scales + mx_scale_at(r0 + lane, c0 >> 5, by_rows.chunks);
+            if constexpr (kCols == 128) *reinterpret_cast<uint32_t*>(to) = reinterpret_cast<const uint32_t*>(s_row_scales[wave])[lane];
+            else *reinterpret_cast<uint16_t*>(to) = reinterpret_cast<const uint16_t*>(s_row_scales[wave])[lane];
         }
     };
     // Random bits are made where the columns are, and reach the rows through the area that the columns leave; without them
@@ -265,7 +286,7 @@ hipError_t tiles_of(const void* x, int64_t rows, int64_t cols, int64_t stride, c
     if (col_tiles * row_tiles > INT32_MAX) return hipErrorInvalidValue;
     return launch(mx_tiles_kernel<T, NORM, STOCHASTIC>, dim3((uint32_t)(col_tiles * row_tiles)), dim3(kTileThreads), s,
                        static_cast<const T*>(x), rows, cols, stride, n, (uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)id,
-                       (uint32_t)(id >> 32), static_cast<uint8_t*>(by_rows), static_cast<uint8_t*>(by_columns), (uint32_t)col_tiles);
+                       (uint32_t)(id >> 32), static_cast<uint8_t*>(by_rows), static_cast<uint8_t*>(by_columns), (uint32_t)col_tiles, (uint32_t)(col_tiles * row_tiles));
 }
 
 template <typename T>
