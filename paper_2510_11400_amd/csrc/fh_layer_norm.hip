@@ -429,6 +429,10 @@ hipError_t norm_any(const void* x, int64_t rows, int64_t cols, int64_t xs, const
     if (cols <= 1024) return norm_of<T, 64, 2, MX>(x, rows, cols, xs, n, to, s);
     if (cols <= 1536) return norm_of<T, 64, 3, MX>(x, rows, cols, xs, n, to, s);
     if (cols <= kWaveCols) return norm_of<T, 64, 4, MX>(x, rows, cols, xs, n, to, s);
+    if constexpr (MX) {                                          // a wave each for somewhat longer rows: 8192 x 2304 bf16 22.6 -> 17.9 us (dense 18.2, 19.2)
+        if (rows > 256 && cols <= 2560) return norm_of<T, 64, 5, MX>(x, rows, cols, xs, n, to, s);
+        if (rows > 256 && cols <= 3072) return norm_of<T, 64, 6, MX>(x, rows, cols, xs, n, to, s);
+    }
     if (rows <= 256) {                                           // no more than a row a compute unit: all the threads it can use
         if (cols <= 4096) return norm_of<T, 512, 1, MX>(x, rows, cols, xs, n, to, s);
         if (cols <= 8192) return norm_of<T, 1024, 1, MX>(x, rows, cols, xs, n, to, s);
