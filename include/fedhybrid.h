@@ -580,12 +580,12 @@ fh_status fh_layer_norm_backward(const fh_norm_backward *norm, void *stream);
  *   backward  fh_mx_quantize of dy (rounding, seed, tensor_id) by rows (NEEDS_INPUT) and by columns
  *             (NEEDS_WEIGHT); fh_mx_matmul: dweight = dy^T x; fh_mx_matmul: dx = dy W, rounded to
  *             dtype; with a norm fh_layer_norm_backward of that in place (dnorm_weight, dnorm_bias
- *             may be NULL).
+ *             may be NULL); dbias (or NULL): the sum of dy's rows in binary32, in an order of the shape alone.
  * x is tokens x features and weight out_features x features, rows contiguous with row strides; dy
  * tokens x out_features with a row stride; y, dx and dweight are dense.  x, y, dy and dx are of dtype, the
  * norm's parameters, weight, bias and their gradients of p_dtype; norm_weight, norm_bias and bias may
  * be NULL.  `kept` (fh_mx_layer_kept_bytes) carries the statistics and the operands by columns from
- * the forward to the backward call and may be NULL where there is neither a norm nor a need; `scratch`
+ * the forward to the backward call and may be NULL where there is neither a norm nor a need (in the backward call: no need); `scratch`
  * (fh_mx_layer_scratch_bytes) is free again once a call's work has run.  Both 16-byte aligned.
  * The backward call takes the same needs as the forward one had, or fewer.  1 <= features,
  * out_features <= 2^24, tokens <= 2^24; tokens = 0 writes zeros to the gradients of the parameters.
@@ -608,6 +608,7 @@ typedef struct fh_mx_layer {
     void       *kept;       size_t kept_cap;
     void       *scratch;    size_t scratch_cap;
     int64_t     reserved;                       /* 0 */
+    void       *dbias;                          /* backward */
 } fh_mx_layer;
 size_t    fh_mx_layer_kept_bytes(int64_t tokens, int64_t features, int64_t out_features);
 size_t    fh_mx_layer_scratch_bytes(int64_t tokens, int64_t features, int64_t out_features);

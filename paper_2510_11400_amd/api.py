@@ -285,7 +285,7 @@ class fh_mx_layer(ctypes.Structure):
                 ("dy", ctypes.c_void_p), ("dy_stride", ctypes.c_int64), ("dx", ctypes.c_void_p), ("dweight", ctypes.c_void_p),
                 ("dnorm_weight", ctypes.c_void_p), ("dnorm_bias", ctypes.c_void_p),
                 ("kept", ctypes.c_void_p), ("kept_cap", ctypes.c_size_t), ("scratch", ctypes.c_void_p), ("scratch_cap", ctypes.c_size_t),
-                ("reserved", ctypes.c_int64)]
+                ("reserved", ctypes.c_int64), ("dbias", ctypes.c_void_p)]
 
 
 for _name in ("fh_mx_layer_kept_bytes", "fh_mx_layer_scratch_bytes"):
@@ -1405,10 +1405,13 @@ class MxLayer:
         self.inputs, self.shape, self.dtype, self.p_dtype, self.features = None, y.shape, x.dtype, weight.dtype, x.shape[1]
         return y
 
-    def backward(self, dy: torch.Tensor, x: Optional[torch.Tensor] = None, norm_weight: Optional[torch.Tensor] = None, stream=None):
-        """Enqueue the backward half; returns (dx, dweight, dnorm_weight, dnorm_bias), None for what is not needed.  With a norm x
-        and norm_weight are the forward call's (x may have moved, as a saved tensor that was restored has)."""
+    def backward(self, dy: torch.Tensor, x: Optional[torch.Tensor] = None, norm_weight: Optional[torch.Tensor] = None, stream=None,
+                 bias: bool = False):
+        """Enqueue the backward half; returns (dx, dweight, dnorm_weight, dnorm_bias), None for what is not needed, and with `bias`
+        a fifth, the bias's gradient.  With a norm x and norm_weight are the forward call's (x may have moved, as a saved tensor that
+        was restored has)."""
         if dy.shape != self.shape or dy.dtype != self.dtype:
             raise ValueError("dy must have the shape and the dtype of y")
-        return _binding.layer_backward(dy, x, norm_weight, self.kept, self.features, self.p_dtype, self.norm, self.eps, self.needs_input,
-                                       self.needs_weight, *self.rounding, stream)
+        grads = _binding.layer_backward(dy, x, norm_weight, self.kept, self.features, self.p_dtype, self.norm, self.eps, self.needs_input,
+                                        self.needs_weight, bias, *self.rounding, stream)
+        return grads if bias else grads[:4]

@@ -436,7 +436,7 @@ FH_ENTRY(layer_norm_backward, 9)
 FH_EXIT
 
 // ---- a linear layer's two halves ----------------------------------------------------------------
-struct Layer { bool norm; float eps; bool input, weight; int rounding; uint64_t seed, id; };    // input, weight: what gradients are wanted of
+struct Layer { bool norm; float eps; bool input, weight, bias; int rounding; uint64_t seed, id; };    // input, weight, bias: what gradients are wanted of
 
 struct Forward { at::Tensor y, kept; };
 Forward forward_of(const Layer& layer, const Matrix& x, const Matrix& weight, const at::Tensor& bias, const at::Tensor& norm_weight, const at::Tensor& norm_bias,
@@ -470,13 +470,15 @@ Forward forward_of(const Layer& layer, const Matrix& x, const Matrix& weight, co
     return f;
 }
 
-struct Backward { at::Tensor dx, dweight; Pair dnorm; };
+struct Backward { at::Tensor dx, dweight, dbias; Pair dnorm; };
 Backward backward_of(const Layer& layer, const Matrix& dy, const at::Tensor& x_again, const at::Tensor& norm_weight, const at::Tensor& kept, int64_t features,
                      at::ScalarType p_type, PyObject* stream)
 {
     const c10::Device device = dy.device();
-    in_device_memory(kept, "kept");
-    on_device(kept, device, "kept");
+    if (kept.defined()) {
+        in_device_memory(kept, "kept");
+        on_device(kept, device, "kept");
+    }
     const at::ScalarType type = dy.t.scalar_type();
     fh_mx_layer l = {};
     l.tokens = dy.rows; l.features = features; l.out_features = dy.cols;
@@ -485,12 +487,16 @@ Backward backward_of(const Layer& layer, const Matrix& dy, const at::Tensor& x_a
     l.eps = layer.eps;
     l.rounding = layer.rounding; l.seed = layer.seed; l.tensor_id = layer.id;
     l.dy = dy.data(); l.dy_stride = dy.stride; l.x_stride = l.weight_stride = features;
-    l.kept = kept.data_ptr(); l.kept_cap = kept.nbytes();
+    if (kept.defined()) { l.kept = kept.data_ptr(); l.kept_cap = kept.nbytes(); }
     Backward b;
     Matrix x{};
     if (layer.weight) {
         b.dweight = new_matrix(l.out_features, features, p_type, device).t;
         l.dweight = b.dweight.data_ptr();
+    }
+    if (layer.bias) {
+        b.dbias = values(l.out_features, p_type, device);
+        l.dbias = b.dbias.data_ptr();
     }
     if (layer.input) {
         b.dx = new_matrix(l.tokens, features, type, device).t;
@@ -514,19 +520,19 @@ Backward backward_of(const Layer& layer, const Matrix& dy, const at::Tensor& x_a
 
 // (x, weight, bias, norm, norm_weight, norm_bias, eps, needs_input, needs_weight, stream) -> (y, kept)
 FH_ENTRY(layer_forward, 10)
-    const Layer layer = {truth(a[3]), (float)f64(a[6]), truth(a[7]), truth(a[8]), FH_ROUND_NEAREST, 0, 0};
+    const Layer layer = {truth(a[3]), (float)f64(a[6]), truth(a[7]), truth(a[8]), false, FH_ROUND_NEAREST, 0, 0};
     const Forward f = forward_of(layer, matrix(a[0], "x"), matrix(a[1], "weight"), tensor_or_none(a[2], "bias"), tensor_or_none(a[4], "norm_weight"),
                                  tensor_or_none(a[5], "norm_bias"), a[9]);
     return tuple(Ref(wrap(f.y)), Ref(wrap(f.kept)));
 FH_EXIT
 
-// (dy, x, norm_weight, kept, features, p_dtype, norm, eps, needs_input, needs_weight, rounding, seed, tensor_id, stream)
-//   -> (dx, dweight, dnorm_weight, dnorm_bias)
-FH_ENTRY(layer_backward, 14)
-    const Layer layer = {truth(a[6]), (float)f64(a[7]), truth(a[8]), truth(a[9]), rounding_of(a[10]), u64(a[11]), u64(a[12])};
-    const Backward b = backward_of(layer, matrix(a[0], "dy"), tensor_or_none(a[1], "x"), tensor_or_none(a[2], "norm_weight"), tensor(a[3], "kept"), i64(a[4]),
-                                   scalar_type(a[5]), a[13]);
-    return tuple(Ref(wrap(b.dx)), Ref(wrap(b.dweight)), Ref(wrap(b.dnorm.first)), Ref(wrap(b.dnorm.second)));
+// (dy, x, norm_weight, kept, features, p_dtype, norm, eps, needs_input, needs_weight, needs_bias, rounding, seed, tensor_id, stream)
+//   -> (dx, dweight, dnorm_weight, dnorm_bias, dbias)
+FH_ENTRY(layer_backward, 15)
+    const Layer layer = {truth(a[6]), (float)f64(a[7]), truth(a[8]), truth(a[9]), truth(a[10]), rounding_of(a[11]), u64(a[12]), u64(a[13])};
+    const Backward b = backward_of(layer, matrix(a[0], "dy"), tensor_or_none(a[1], "x"), tensor_or_none(a[2], "norm_weight"), tensor_or_none(a[3], "kept"), i64(a[4]),
+                                   scalar_type(a[5]), a[14]);
+    return tuple(Ref(wrap(b.dx)), Ref(wrap(b.dweight)), Ref(wrap(b.dnorm.first)), Ref(wrap(b.dnorm.second)), Ref(wrap(b.dbias)));
 FH_EXIT
 
 // ---- the same as a step of autograd -------------------------------------------------------------
@@ -548,11 +554,11 @@ at::Tensor shaped(const at::Tensor& y, const at::Tensor& x)
 
 struct Pass : torch::CustomClassHolder {                                  // from one half to the other, but for what is saved as a variable
     Layer layer;
-    bool x, norm_weight, norm_bias, bias;                                 // whose gradients are wanted
+    bool x, norm_weight, norm_bias;                                       // whose gradients are wanted, beside the layer's
     at::Tensor kept;
     std::vector<int64_t> shape;
     int64_t features;
-    at::ScalarType p_type, bias_type;
+    at::ScalarType p_type;
 };
 
 struct Linear : torch::autograd::Function<Linear> {
@@ -577,16 +583,14 @@ struct Linear : torch::autograd::Function<Linear> {
         {
             const at::AutoGradMode off(false);
             const at::Tensor dy = rows_of(given[0]);
-            if (pass->layer.input || pass->layer.weight) {
-                const auto saved = ctx->get_saved_variables();
-                const Backward b = backward_of(pass->layer, matrix(dy, "dy"), saved.empty() ? at::Tensor() : saved[0], saved.empty() ? at::Tensor() : saved[1],
-                                               pass->kept, pass->features, pass->p_type, Py_None);
-                if (pass->x) grads[0] = b.dx.view(pass->shape);
-                if (pass->norm_weight) grads[1] = b.dnorm.first;
-                if (pass->norm_bias) grads[2] = b.dnorm.second;
-                grads[3] = b.dweight;
-            }
-            if (pass->bias) grads[4] = dy.to(at::kFloat).sum(0).to(pass->bias_type);
+            const auto saved = ctx->get_saved_variables();
+            const Backward b = backward_of(pass->layer, matrix(dy, "dy"), saved.empty() ? at::Tensor() : saved[0], saved.empty() ? at::Tensor() : saved[1],
+                                           pass->kept, pass->features, pass->p_type, Py_None);
+            if (pass->x) grads[0] = b.dx.view(pass->shape);
+            if (pass->norm_weight) grads[1] = b.dnorm.first;
+            if (pass->norm_bias) grads[2] = b.dnorm.second;
+            grads[3] = b.dweight;
+            grads[4] = b.dbias;
         }
         if (!again) return grads;
         for (at::Tensor& g : grads)                                       // leaves of a graph that ends in an error
@@ -604,13 +608,13 @@ FH_ENTRY(mx_linear, 9)
     const auto pass = c10::make_intrusive<Pass>();
     const bool norm = a[5] != Py_None, grad = at::GradMode::is_enabled();
     const auto wanted = [&](const at::Tensor& t) { return grad && t.defined() && t.requires_grad(); };
-    pass->x = wanted(x); pass->norm_weight = wanted(norm_weight); pass->norm_bias = wanted(norm_bias); pass->bias = wanted(bias);
-    pass->layer = {norm, norm ? (float)f64(a[5]) : 0.0f, pass->x || pass->norm_weight || pass->norm_bias, wanted(weight), rounding_of(a[6]), u64(a[7]), u64(a[8])};
+    pass->x = wanted(x); pass->norm_weight = wanted(norm_weight); pass->norm_bias = wanted(norm_bias);
+    pass->layer = {norm, norm ? (float)f64(a[5]) : 0.0f, pass->x || pass->norm_weight || pass->norm_bias, wanted(weight), wanted(bias),
+                   rounding_of(a[6]), u64(a[7]), u64(a[8])};
     pass->p_type = weight.scalar_type();
-    pass->bias_type = bias.defined() ? bias.scalar_type() : at::kFloat;
     pass->shape = x.sizes().vec();
     at::Tensor y;
-    if (pass->layer.input || pass->layer.weight || pass->bias) {
+    if (pass->layer.input || pass->layer.weight || pass->layer.bias) {
         const auto some = [](const at::Tensor& t) { return t.defined() ? std::optional<at::Tensor>(t) : std::nullopt; };
         y = Linear::apply(x, some(norm_weight), some(norm_bias), weight, some(bias), pass);
     } else {

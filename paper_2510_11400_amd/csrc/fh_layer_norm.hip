@@ -371,31 +371,37 @@ __global__ __launch_bounds__(256) void norm_column_sums_kernel(NormBackwardArgs 
     store8(to + a.cols + first, a.cols - first, db);
 }
 
-// The partial rows (kMostParts at most) added up in an order of their number alone: 64 columns of one of the two sums a workgroup,
-// a sixteenth of the rows a wave, whose loads are all on their way at once: the kernel takes little more than one of them.
+// Rows of partial sums added up in an order of their number alone: 64 columns of one of the `count` sums a workgroup, a sixteenth of
+// 256 rows at a time a wave, whose loads are all on their way at once: up to 256 rows the kernel takes little more than one of them.
 constexpr int kMostParts = 256;
 template <typename P>
-__global__ __launch_bounds__(1024) void norm_join_kernel(const float* partial, int64_t parts, int64_t cols, P* dweight, P* dbias)
+__global__ __launch_bounds__(1024) void norm_join_kernel(const float* partial, int64_t parts, int64_t cols, int32_t count, P* first, P* second)
 {
     constexpr int kEach = kMostParts / 16;
     __shared__ float s_part[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)(blockIdx.x >> 1) * 64 + lane, which = blockIdx.x & 1;
+    const int32_t which = count == 2 ? blockIdx.x & 1 : 0;
+    const int64_t c = (int64_t)(count == 2 ? blockIdx.x >> 1 : blockIdx.x) * 64 + lane;
     const float* from = partial + which * cols + (c < cols ? c : 0);
-    float v[kEach] = {};
-    if (parts > 0) {                                             // rows past the last: the first one, for nothing
+    float sum = 0.0f;
+    for (int64_t start = 0; start < parts; start += kMostParts) {
+        float v[kEach];
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) v[i] = from[(int64_t)(wave + 16 * i < parts ? wave + 16 * i : 0) * 2 * cols];
+        for (int i = 0; i < kEach; ++i) {                        // rows past the last: the run's first, for nothing
+            const int64_t row = start + wave + 16 * i;
+            v[i] = from[(row < parts ? row : start) * count * cols];
+        }
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) v[i] = wave + 16 * i < parts ? v[i] : 0.0f;
+        for (int i = 0; i < kEach; ++i) v[i] = start + wave + 16 * i < parts ? v[i] : 0.0f;
+#pragma unroll
+        for (int half = kEach / 2; half > 0; half /= 2)
+#pragma unroll
+            for (int i = 0; i < half; ++i) v[i] += v[i + half];
+        sum += v[0];
     }
-#pragma unroll
-    for (int half = kEach / 2; half > 0; half /= 2)
-#pragma unroll
-        for (int i = 0; i < half; ++i) v[i] += v[i + half];
-    s_part[wave][lane] = v[0];
+    s_part[wave][lane] = sum;
     __syncthreads();
-    P* to = which ? dbias : dweight;
+    P* to = which ? second : first;
     if (wave == 0 && c < cols && to) {
         float all = 0.0f;
 #pragma unroll
@@ -504,16 +510,16 @@ hipError_t backward_any(const NormBackwardArgs& a, int64_t* parts, hipStream_t s
     }
     return a.dx ? launch(norm_backward_long_rows_kernel<T>, dim3((uint32_t)a.rows), dim3(1024), s, a) : hipSuccess;
 }
-template <typename P>
-hipError_t join_of(const float* partial, int64_t parts, int64_t cols, void* dweight, void* dbias, hipStream_t s)
-{
-    return launch(norm_join_kernel<P>, dim3((uint32_t)((cols + 63) / 64 * 2)), dim3(1024), s, partial, parts, cols,
-                       static_cast<P*>(dweight), static_cast<P*>(dbias));
-}
-
 bool norm_shape_ok(int64_t rows, int64_t cols) { return mx_shape_ok(rows, cols) && cols >= 1; }
 
 }  // namespace
+
+hipError_t launch_join(const float* partial, int64_t parts, int64_t cols, int32_t count, int32_t p_dtype, void* first, void* second, hipStream_t s)
+{
+    const dim3 grid((uint32_t)((cols + 63) / 64 * count)), block(1024);
+    if (p_dtype == FH_F32) return launch(norm_join_kernel<float>, grid, block, s, partial, parts, cols, count, static_cast<float*>(first), static_cast<float*>(second));
+    return launch(norm_join_kernel<Bf16>, grid, block, s, partial, parts, cols, count, static_cast<Bf16*>(first), static_cast<Bf16*>(second));
+}
 
 hipError_t launch_layer_norm(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t xs, const NormArgs& n, void* y, int64_t ys,
                              void* codes, hipStream_t s)
@@ -584,9 +590,7 @@ fh_status fh_layer_norm_backward(const fh_norm_backward* b, void* stream)
         if (e != hipSuccess) return FH_ERR_LAUNCH;
     }
     if (!sums) return FH_OK;                                     // no rows: sums of nothing, which are written all the same
-    const hipError_t e = b->p_dtype == FH_F32 ? join_of<float>(partial, parts, b->cols, b->dweight, b->dbias, s)
-                                              : join_of<Bf16>(partial, parts, b->cols, b->dweight, b->dbias, s);
-    return e == hipSuccess ? FH_OK : FH_ERR_LAUNCH;
+    return launch_join(partial, parts, b->cols, 2, b->p_dtype, b->dweight, b->dbias, s) == hipSuccess ? FH_OK : FH_ERR_LAUNCH;
 }
 
 }  // extern "C"

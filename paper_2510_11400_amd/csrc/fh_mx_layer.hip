@@ -30,7 +30,7 @@ Parts parts_of(int64_t tokens, int64_t features, int64_t out)
     p.dy_columns = whole(mx_bytes(tokens, out));
     p.backward_work = p.dy_columns + whole(mx_bytes(out, tokens));
     p.backward = p.backward_work + whole(larger(larger(fh_mx_matmul_workspace_bytes(tokens, features, out), fh_mx_matmul_workspace_bytes(out, features, tokens)),
-                                                fh_layer_norm_backward_workspace_bytes(tokens, features)));
+                                                larger(fh_layer_norm_backward_workspace_bytes(tokens, features), (size_t)mx_tile_rows(tokens) * (size_t)out * 4)));
     return p;
 }
 
@@ -112,24 +112,34 @@ fh_status fh_mx_layer_backward(const fh_mx_layer* l, void* stream)
 {
     using namespace fh;
     const fh_status ok = check(l);
-    if (ok != FH_OK || !l->needs) return ok;
+    if (ok != FH_OK || (!l->needs && !l->dbias)) return ok;
     const Parts p = parts_of(l->tokens, l->features, l->out_features);
     const size_t size = dtype_size(l->dtype), p_size = dtype_size(l->p_dtype);
     const bool input = l->needs & FH_MX_NEEDS_INPUT, weight = l->needs & FH_MX_NEEDS_WEIGHT;
-    if (!l->kept || !l->scratch || (weight && !l->dweight)) return FH_ERR_NULL;
+    if ((l->needs && !l->kept) || !l->scratch || (weight && !l->dweight)) return FH_ERR_NULL;
     if (l->tokens > 0 && (!l->dy || (input && !l->dx) || (input && l->norm && !l->x))) return FH_ERR_NULL;
     if (!is_aligned(l->x, size) || !is_aligned(l->dy, size) || !is_aligned(l->dx, size) || !is_aligned(l->dweight, p_size) ||
         !is_aligned(l->norm_weight, p_size) || !is_aligned(l->dnorm_weight, p_size) || !is_aligned(l->dnorm_bias, p_size) ||
-        !is_aligned(l->kept, 16) || !is_aligned(l->scratch, 16)) return FH_ERR_ALIGNMENT;
-    if (l->scratch_cap < p.backward || l->kept_cap < p.kept) return FH_ERR_BUFFER_TOO_SMALL;
+        !is_aligned(l->dbias, p_size) || !is_aligned(l->kept, 16) || !is_aligned(l->scratch, 16)) return FH_ERR_ALIGNMENT;
+    if (l->scratch_cap < p.backward || (l->needs && l->kept_cap < p.kept)) return FH_ERR_BUFFER_TOO_SMALL;
 
     uint8_t *dy_rows = input ? at(l->scratch, p.dy_rows) : nullptr, *dy_columns = weight ? at(l->scratch, p.dy_columns) : nullptr;
     const size_t rows_bytes = mx_bytes(l->tokens, l->out_features), columns_bytes = mx_bytes(l->out_features, l->tokens);
     void* work = at(l->scratch, p.backward_work);
     const size_t work_bytes = l->scratch_cap - p.backward_work;
-    fh_status s = fh_mx_quantize(l->dy, (fh_dtype)l->dtype, l->tokens, l->out_features, l->dy_stride, l->rounding, l->seed, l->tensor_id,
-                                 dy_rows, rows_bytes, dy_columns, columns_bytes, stream);
-    if (s != FH_OK) return s;
+    fh_status s;
+    if (l->dbias) {                                              // in the workspace until the sums are joined, ahead of the products
+        const hipStream_t hs = static_cast<hipStream_t>(stream);
+        float* sums = static_cast<float*>(work);
+        if (l->tokens > 0 && launch_mx_tiles(l->dy, l->dtype, l->tokens, l->out_features, l->dy_stride, nullptr, sums, l->rounding == FH_ROUND_STOCHASTIC, l->seed,
+                                             l->tensor_id, dy_rows, dy_columns, hs) != hipSuccess) return FH_ERR_LAUNCH;
+        if (launch_join(sums, mx_tile_rows(l->tokens), l->out_features, 1, l->p_dtype, l->dbias, nullptr, hs) != hipSuccess) return FH_ERR_LAUNCH;
+        if (!l->needs) return FH_OK;
+    } else {
+        s = fh_mx_quantize(l->dy, (fh_dtype)l->dtype, l->tokens, l->out_features, l->dy_stride, l->rounding, l->seed, l->tensor_id,
+                           dy_rows, rows_bytes, dy_columns, columns_bytes, stream);
+        if (s != FH_OK) return s;
+    }
     if (weight) {
         const fh_mx_product dw = {dy_columns, columns_bytes, at(l->kept, p.x_columns), mx_bytes(l->features, l->tokens), l->out_features, l->features,
                                   l->tokens, nullptr, l->p_dtype, l->p_dtype, l->dweight, l->features,

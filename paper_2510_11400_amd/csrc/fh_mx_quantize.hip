@@ -1,4 +1,6 @@
 // Microscaled 4-bit storage: quantisation by rows, by columns or both, and its inverse.
+#include <type_traits>
+
 #include "fh_norm.hpp"
 
 namespace fh {
@@ -38,12 +40,16 @@ __global__ __launch_bounds__(kThreads) void mx_rows_kernel(const T* x, int64_t r
 // times the instructions.  Eight waves make 256 rows, so that the codes of a column, gathered in LDS, leave as whole lines
 // of 128 bytes.  The random bits of eight rows of a column are one Philox block, computed where the column is and handed to
 // the rows through LDS as well.
-constexpr int kTileRows = 256, kTileThreads = 512;
+constexpr int kTileRows = 256 /* mx_tile_rows */, kTileThreads = 512;
 constexpr int kWaveBytes = 32 * 256 + 16;          // the 16 turn the waves' areas, so that a gather of all eight meets all banks
 template <typename T> constexpr int kTileCols = 256 / (int)sizeof(T);
 
+// A linear layer's bias has the sums of its output gradient's columns for gradient: they come with that gradient's codes, from the lanes
+// that hold the columns, a row of partial sums a tile, where a pass of their own read 8192 x 2304 once more.
+struct SumArgs { float* sums; };
 template <typename T, bool NORM, bool STOCHASTIC>
-__global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4) void mx_tiles_kernel(const T* x, int64_t rows, int64_t cols, int64_t stride, NormArgs n,
+__global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4) void mx_tiles_kernel(const T* x, int64_t rows, int64_t cols, int64_t stride,
+                                                                   std::conditional_t<NORM, NormArgs, SumArgs> n,
                                                                    uint32_t k0, uint32_t k1, uint32_t id0, uint32_t id1,
                                                                    uint8_t* rows_form, uint8_t* columns_form, uint32_t col_tiles, uint32_t tiles)
 {
@@ -53,6 +59,7 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
     __shared__ uint32_t s_scales[kCols * 2];
     __shared__ __attribute__((aligned(16))) uint8_t s_row_scales[8][kCols];                   // a wave's: [row][block]
     __shared__ __attribute__((aligned(16))) f32x2 s_stats[NORM ? 8 : 1][32];   // mean and 1 / deviation of a wave's rows
+    __shared__ float s_sums[NORM ? 1 : 8][NORM ? 1 : kCols];                   // of a wave's rows
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // Workgroups go to the XCDs in turn.  In fp32 a row's codes leave by 32 bytes a tile, so an XCD takes a run of neighbours, whose
     // parts of a line meet in its L2 (8192 x 8192, both forms: 86 -> 71 us); the halves of bf16 lose by it (48 -> 50).
@@ -95,7 +102,9 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
         return i & 1 ? word >> 16 : word & 0xFFFFu;
     };
 
-    if (columns_form) {
+    bool by_lane = columns_form != nullptr;                      // the columns are wanted in the lanes
+    if constexpr (!NORM) by_lane = by_lane || n.sums;
+    if (by_lane) {
 #pragma unroll
         for (int g = 0; g < kGroups; ++g)
 #pragma unroll
@@ -171,7 +180,7 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
     // Random bits are made where the columns are, and reach the rows through the area that the columns leave; without them
     // the rows come first, which frees their registers.
     if (!STOCHASTIC && rows_form) write_rows();
-    if (columns_form) {
+    if (by_lane) {
         asm volatile("" ::: "memory");                           // a wave's own LDS accesses are in order
         u32x4 q[kEach];
 #pragma unroll
@@ -198,6 +207,14 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
                 if (!whole) {                                    // zeros stay zeros, whatever the bias
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = in && r0 + i < rows ? v[i] : 0.0f;
+                }
+            }
+            if constexpr (!NORM) {
+                if (n.sums) {
+                    float sum[4] = {};
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) sum[i & 3] += v[i];
+                    s_sums[wave][c] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
                 }
             }
             uint32_t top = 0;
@@ -227,11 +244,19 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
 #pragma unroll
         for (int i = 0; i < kCols * 8 / kTileThreads; ++i) {
             const int id = threadIdx.x + i * kTileThreads, c = id >> 3, piece = id & 7;
-            if (c0 + c < cols)
+            if (columns_form && c0 + c < cols)
                 *reinterpret_cast<u32x4*>(by_columns.codes + (c0 + c) * (by_columns.chunks * 128) + row_tile * 128 + piece * 16) =
                     *reinterpret_cast<const u32x4*>(s_area + piece * kWaveBytes + c * 16);
         }
-        if (threadIdx.x < kCols * 2) {
+        if constexpr (!NORM) {
+            if (n.sums && threadIdx.x < kCols && c0 + threadIdx.x < cols) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int w = 0; w < 8; ++w) sum += s_sums[w][threadIdx.x];
+                n.sums[row_tile * cols + c0 + threadIdx.x] = sum;
+            }
+        }
+        if (columns_form && threadIdx.x < kCols * 2) {
             const int64_t group = (c0 >> 5) + (threadIdx.x >> 6);
             if (group * 32 < cols)
                 *reinterpret_cast<uint32_t*>(by_columns.scales + ((group * by_columns.chunks + row_tile) << 8) + (threadIdx.x & 63) * 4) =
@@ -277,12 +302,12 @@ hipError_t rows_of(const void* x, int64_t rows, int64_t cols, int64_t stride, co
 }
 
 template <typename T, bool NORM, bool STOCHASTIC>
-hipError_t tiles_of(const void* x, int64_t rows, int64_t cols, int64_t stride, const NormArgs& n, uint64_t seed, uint64_t id,
+hipError_t tiles_of(const void* x, int64_t rows, int64_t cols, int64_t stride, const std::conditional_t<NORM, NormArgs, SumArgs>& n, uint64_t seed, uint64_t id,
                     void* by_rows, void* by_columns, hipStream_t s)
 {
     // columns up to a whole chunk where rows are stored, rows up to a whole chunk where columns are
     const int64_t width = by_rows ? mx_chunks(cols) * kMxChunk : cols, col_tiles = (width + kTileCols<T> - 1) / kTileCols<T>;
-    const int64_t row_tiles = (rows + kTileRows - 1) / kTileRows;
+    const int64_t row_tiles = mx_tile_rows(rows);
     if (col_tiles * row_tiles > INT32_MAX) return hipErrorInvalidValue;
     return launch(mx_tiles_kernel<T, NORM, STOCHASTIC>, dim3((uint32_t)(col_tiles * row_tiles)), dim3(kTileThreads), s,
                        static_cast<const T*>(x), rows, cols, stride, n, (uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)id,
@@ -321,10 +346,10 @@ fh_status check_input(const void* x, int x_dtype, int64_t rows, int64_t cols, in
 
 }  // namespace
 
-hipError_t launch_mx_tiles(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, const NormArgs* n, bool stochastic,
-                           uint64_t seed, uint64_t id, void* by_rows, void* by_columns, hipStream_t s)
+hipError_t launch_mx_tiles(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, const NormArgs* n, float* sums,
+                           bool stochastic, uint64_t seed, uint64_t id, void* by_rows, void* by_columns, hipStream_t s)
 {
-    const NormArgs none = {};
+    const SumArgs none = {sums};
     if (dtype == FH_F32) {
         if (n) return stochastic ? tiles_of<float, true, true>(x, rows, cols, stride, *n, seed, id, by_rows, by_columns, s)
                                  : tiles_of<float, true, false>(x, rows, cols, stride, *n, seed, id, by_rows, by_columns, s);
@@ -355,7 +380,7 @@ fh_status fh_mx_quantize(const void* x, fh_dtype x_dtype, int64_t rows, int64_t 
     const hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e;
     if (by_columns || rounding == FH_ROUND_STOCHASTIC)
-        e = launch_mx_tiles(x, x_dtype, rows, cols, row_stride, nullptr, rounding == FH_ROUND_STOCHASTIC, seed, tensor_id, by_rows, by_columns, s);
+        e = launch_mx_tiles(x, x_dtype, rows, cols, row_stride, nullptr, nullptr, rounding == FH_ROUND_STOCHASTIC, seed, tensor_id, by_rows, by_columns, s);
     else
         e = x_dtype == FH_F32 ? rows_of<float>(x, rows, cols, row_stride, mx_store(by_rows, rows, cols), s)
                                 : rows_of<Bf16>(x, rows, cols, row_stride, mx_store(by_rows, rows, cols), s);
@@ -398,7 +423,7 @@ fh_status fh_layer_norm_mx(const void* x, fh_dtype x_dtype, int64_t rows, int64_
     const NormArgs n = {weight, bias, p_dtype, eps, static_cast<float*>(mean), static_cast<float*>(rstd)};
     if (launch_layer_norm(x, x_dtype, rows, cols, row_stride, n, nullptr, 0, tiles ? nullptr : by_rows, s) != hipSuccess) return FH_ERR_LAUNCH;
     if (!tiles) return FH_OK;
-    return launch_mx_tiles(x, x_dtype, rows, cols, row_stride, &n, rounding == FH_ROUND_STOCHASTIC, seed, tensor_id, by_rows, by_columns, s) == hipSuccess
+    return launch_mx_tiles(x, x_dtype, rows, cols, row_stride, &n, nullptr, rounding == FH_ROUND_STOCHASTIC, seed, tensor_id, by_rows, by_columns, s) == hipSuccess
                ? FH_OK : FH_ERR_LAUNCH;
 }
 

@@ -31,9 +31,14 @@ __device__ __forceinline__ float parameter(const void* p, int32_t dtype, int64_t
 // Layer norm of rows to y (dense), to `codes` (by rows), or the statistics alone where both are null.
 hipError_t launch_layer_norm(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t x_stride, const NormArgs& n,
                              void* y, int64_t y_stride, void* codes, hipStream_t s);
-// The quantiser over tiles of 256 rows, with or without a norm whose statistics are known; either form may be null.
-hipError_t launch_mx_tiles(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t x_stride, const NormArgs* n,
+// The quantiser over tiles of 256 rows, with or without a norm whose statistics are known; either form may be null.  `sums` (without a
+// norm): mx_tile_rows(rows) rows of partial sums of x's columns, or null.
+inline int64_t mx_tile_rows(int64_t rows) { return (rows + 255) / 256; }
+hipError_t launch_mx_tiles(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t x_stride, const NormArgs* n, float* sums,
                            bool stochastic, uint64_t seed, uint64_t tensor_id, void* by_rows, void* by_columns, hipStream_t s);
+// Rows of partial sums added up: row i's k-th of `count` vectors begins at partial + (i * count + k) * cols, their sums go to
+// first (k = 0) and second (k = 1), of p_dtype; either may be null.
+hipError_t launch_join(const float* partial, int64_t parts, int64_t cols, int32_t count, int32_t p_dtype, void* first, void* second, hipStream_t s);
 
 // The host's checks of a matrix in rows: `elements` from its pointer on are read or written.
 inline bool is_aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }

@@ -294,3 +294,70 @@ def test_faults_of_a_backward_pass_reach_the_caller(layers):
         layers.mx_linear(x, w[:, :-1].contiguous())
     with pytest.raises(TypeError):
         layers.mx_linear(x, w, torch.zeros(40, device="cuda", dtype=torch.bfloat16))
+
+
+@pytest.mark.parametrize("rounding", ["nearest", "stochastic"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens, out", [(1, 7), (33, 300), (257, 64), (1030, 129), (70000, 40)])
+def test_the_sum_of_the_gradients_rows(layers, tokens, out, dtype, rounding):
+    """The bias's gradient beside every choice of the others, against binary64: a value passes 8 + 2 additions in its
+    lane, 8 over the waves, 4 + 2 in the join (two runs of 256 tiles at most) and 16 over its waves: 40, each off by 2^-24 of sums that
+    the magnitudes' sum bounds; then one rounding to the dtype."""
+    from paper_2510_11400_amd import api
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    x, w, b = torch.randn(tokens, 40, generator=g, device="cuda").to(dtype), torch.randn(out, 40, generator=g, device="cuda").to(dtype), torch.zeros(out, device="cuda", dtype=dtype)
+    dy = torch.randn(tokens, out + 3, generator=g, device="cuda").to(dtype)[:, 1:out + 1]
+    exact, size = dy.double().sum(0), dy.double().abs().sum(0)
+    limit = 40 * 2.0 ** -24 * size + torch.finfo(dtype).eps / 2 * exact.abs() + 1e-30
+    seen = []
+    for needs in ((True, True), (True, False), (False, True), (False, False)):
+        layer = api.MxLayer(x, w, b, needs_input=needs[0], needs_weight=needs[1], rounding=rounding, seed=1, tensor_id=2)
+        layer.forward()
+        without = layer.backward(dy)
+        *rest, db = layer.backward(dy, bias=True)
+        for p, q in zip(rest, without):
+            assert (p is None) == (q is None) and (p is None or torch.equal(p, q))
+        assert db.dtype == dtype and bool(((db.double() - exact).abs() <= limit).all())
+        seen.append(db)
+    assert all(torch.equal(seen[0], v) for v in seen[1:])
+
+
+def test_the_sum_of_no_rows_and_of_broken_ones(layers):
+    x, w, b = torch.empty(0, 40, device="cuda"), torch.randn(7, 40, device="cuda"), torch.zeros(7, device="cuda", requires_grad=True)
+    db, = torch.autograd.grad(layers.mx_linear(x, w, b), b, torch.empty(0, 7, device="cuda"))
+    assert db.shape == (7,) and not db.any()
+    x, dy = torch.randn(300, 40, device="cuda"), torch.randn(300, 7, device="cuda")
+    dy[299, 2], dy[5, 4] = float("nan"), float("inf")
+    db, = torch.autograd.grad(layers.mx_linear(x, w, b), b, dy)
+    assert torch.isnan(db[2]) and torch.isinf(db[4]) and torch.isfinite(db[[0, 1, 3, 5, 6]]).all()
+
+
+def test_a_layer_with_a_bias_captured_in_a_graph(layers):
+    """As test_captured_in_a_graph, with the gradient of the linear layer's bias, over more rows than a tile has."""
+    x, nw, nb, w, b, dy = (v.cuda() for v in _case(2100, 300, 130, torch.bfloat16))
+
+    def step(x, dy, leaves):
+        xl = x.detach().requires_grad_()
+        y = layers.layer_norm_mx_linear(xl, *leaves, rounding="stochastic", seed=5)
+        return [y.detach(), *torch.autograd.grad(y, [xl, *leaves], dy)]
+
+    static_x, static_dy = x.clone(), dy.clone()
+    static = [v.clone().requires_grad_() for v in (nw, nb, w, b)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(static_x, static_dy, static)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(static_x, static_dy, static)
+    for k in range(4):
+        g = torch.Generator(device="cuda").manual_seed(k)
+        nx, ndy = (torch.randn(v.shape, generator=g, device="cuda").to(v.dtype) for v in (x, dy))
+        static_x.copy_(nx)
+        static_dy.copy_(ndy)
+        graph.replay()
+        got = [v.clone() for v in out]
+        want = step(nx, ndy, [v.clone().requires_grad_() for v in (nw, nb, w, b)])
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, want)), k

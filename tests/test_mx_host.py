@@ -231,3 +231,11 @@ def test_layer_sizes():
     kept = LIB.fh_mx_layer_kept_bytes(100, 300, 70)
     assert kept >= 2 * 400 + api.mx_bytes(300, 100) + api.mx_bytes(300, 70)
     assert LIB.fh_mx_layer_scratch_bytes(100, 300, 70) >= max(api.mx_bytes(100, 300) + api.mx_bytes(70, 300), api.mx_bytes(100, 70) + api.mx_bytes(70, 100))
+
+
+def test_layer_bias_gradient_refusals():
+    assert _layer(True, dbias=FAKE + 2) == 8
+    assert _layer(True, dbias=FAKE, needs=0, kept=None, scratch=None) == 1 and _layer(True, dbias=FAKE, needs=0, kept=None, dy=None) == 1
+    assert _layer(True, dbias=FAKE, needs=0, kept=None, scratch_cap=LIB.fh_mx_layer_scratch_bytes(5, 40, 7) // 2) == 7
+    # the partial sums of a long, wide gradient fit
+    assert LIB.fh_mx_layer_scratch_bytes(2 ** 20, 1, 4096) >= api.mx_bytes(2 ** 20, 4096) + api.mx_bytes(4096, 2 ** 20) + 4096 * 4096 * 4
