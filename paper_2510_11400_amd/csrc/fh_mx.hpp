@@ -176,6 +176,13 @@ struct Run {
     }
 };
 
+// Workgroups go to the eight XCDs in turn.  A run of neighbours for each: the at-th of `all`.
+__device__ __forceinline__ uint32_t run_of(uint32_t at, uint32_t all)
+{
+    const uint32_t xcd = at & 7, share = all >> 3, rest = all & 7;
+    return xcd * share + (xcd < rest ? xcd : rest) + (at >> 3);
+}
+
 // Eight values from p on, of which the first `n` exist (the others are 0).
 __device__ __forceinline__ void load8(const float* p, int64_t n, float (&v)[8])
 {
@@ -248,6 +255,20 @@ __device__ __forceinline__ uint32_t mx_codes8(const float (&v)[8], uint32_t& s)
     codes = mx_nearest<1>(codes, v[2], v[3], s);
     codes = mx_nearest<2>(codes, v[4], v[5], s);
     return mx_nearest<3>(codes, v[6], v[7], s);
+}
+// 32 values of a lane: a block's 16 bytes of codes, to the nearest.
+__device__ __forceinline__ u32x4 mx_codes32(const float (&v)[32], uint32_t s)
+{
+    u32x4 q;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        uint32_t a = 0;
+        a = mx_nearest<0>(a, v[8 * w], v[8 * w + 1], s);
+        a = mx_nearest<1>(a, v[8 * w + 2], v[8 * w + 3], s);
+        a = mx_nearest<2>(a, v[8 * w + 4], v[8 * w + 5], s);
+        q[w] = s == 255u ? 0u : mx_nearest<3>(a, v[8 * w + 6], v[8 * w + 7], s);
+    }
+    return q;
 }
 __device__ __forceinline__ void mx_write8(const MxStore& to, int64_t row, int64_t first, const float (&v)[8], bool write)
 {

@@ -49,12 +49,6 @@ __device__ __forceinline__ u32x4 buffer_of(const uint8_t* p, uint32_t bytes)
     return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, bytes, 0x00020000u};
 }
 
-// Workgroups go to the eight XCDs in turn.  A run of neighbours for each: the at-th of `all`.
-__device__ __forceinline__ uint32_t run_of(uint32_t at, uint32_t all)
-{
-    const uint32_t xcd = at & 7, share = all >> 3, rest = all & 7;
-    return xcd * share + (xcd < rest ? xcd : rest) + (at >> 3);
-}
 // Tiles in bands of eight columns, so that what an XCD works on at a time shares rows of both operands in its L2.
 __device__ __forceinline__ void in_bands(uint32_t tile, uint32_t m_tiles, uint32_t n_tiles, uint32_t& i, uint32_t& j)
 {

@@ -61,13 +61,9 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
     __shared__ __attribute__((aligned(16))) f32x2 s_stats[NORM ? 8 : 1][32];   // mean and 1 / deviation of a wave's rows
     __shared__ float s_sums[NORM ? 1 : 8][NORM ? 1 : kCols];                   // of a wave's rows
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // Workgroups go to the XCDs in turn.  In fp32 a row's codes leave by 32 bytes a tile, so an XCD takes a run of neighbours, whose
-    // parts of a line meet in its L2 (8192 x 8192, both forms: 86 -> 71 us); the halves of bf16 lose by it (48 -> 50).
-    uint32_t at = blockIdx.x;
-    if constexpr (sizeof(T) == 4) {
-        const uint32_t xcd = at & 7, share = tiles >> 3, rest = tiles & 7;
-        at = xcd * share + (xcd < rest ? xcd : rest) + (at >> 3);
-    }
+    // In fp32 a row's codes leave by 32 bytes a tile, so an XCD takes a run of neighbours, whose parts of a line meet in its L2
+    // (8192 x 8192, both forms: 86 -> 71 us); the halves of bf16 lose by it (48 -> 50).
+    const uint32_t at = sizeof(T) == 4 ? run_of(blockIdx.x, tiles) : blockIdx.x;
     const int64_t col_tile = at % col_tiles, row_tile = at / col_tiles;
     const int64_t r0 = row_tile * kTileRows + wave * 32, c0 = col_tile * kCols;
     const bool whole = r0 + 32 <= rows && c0 + kCols <= cols;
@@ -221,19 +217,16 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
 #pragma unroll
             for (int i = 0; i < 32; ++i) top = umax(top, abs_bits(v[i]));
             const uint32_t s = mx_scale_byte(top);
+            if constexpr (STOCHASTIC) {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                uint32_t a = 0;
-                if constexpr (STOCHASTIC) {
+                for (int w = 0; w < 4; ++w) {
+                    uint32_t a = 0;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) a |= mx_stochastic(v[8 * w + i], s, half(e, 8 * w + i)) << (4 * i);
-                } else {
-                    a = mx_nearest<0>(a, v[8 * w], v[8 * w + 1], s);
-                    a = mx_nearest<1>(a, v[8 * w + 2], v[8 * w + 3], s);
-                    a = mx_nearest<2>(a, v[8 * w + 4], v[8 * w + 5], s);
-                    a = mx_nearest<3>(a, v[8 * w + 6], v[8 * w + 7], s);
+                    q[e][w] = s == 255u ? 0u : a;
                 }
-                q[e][w] = s == 255u ? 0u : a;
+            } else {
+                q[e] = mx_codes32(v, s);
             }
             // [column/32][wave/4][column%32][wave%4], as the stored form has it
             reinterpret_cast<uint8_t*>(s_scales)[(c >> 5) * 256 + (wave >> 2) * 128 + (c & 31) * 4 + (wave & 3)] = (uint8_t)s;
@@ -421,6 +414,8 @@ fh_status fh_layer_norm_mx(const void* x, fh_dtype x_dtype, int64_t rows, int64_
         (bias && !is_aligned(bias, dtype_size(p_dtype)))) return FH_ERR_ALIGNMENT;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const NormArgs n = {weight, bias, p_dtype, eps, static_cast<float*>(mean), static_cast<float*>(rstd)};
+    if (by_columns && rounding == FH_ROUND_NEAREST && norm_blocks_fit(x_dtype, rows, cols))
+        return launch_norm_blocks(x, x_dtype, rows, cols, row_stride, n, by_rows, by_columns, s) == hipSuccess ? FH_OK : FH_ERR_LAUNCH;
     if (launch_layer_norm(x, x_dtype, rows, cols, row_stride, n, nullptr, 0, tiles ? nullptr : by_rows, s) != hipSuccess) return FH_ERR_LAUNCH;
     if (!tiles) return FH_OK;
     return launch_mx_tiles(x, x_dtype, rows, cols, row_stride, &n, nullptr, rounding == FH_ROUND_STOCHASTIC, seed, tensor_id, by_rows, by_columns, s) == hipSuccess

@@ -31,6 +31,10 @@ __device__ __forceinline__ float parameter(const void* p, int32_t dtype, int64_t
 // Layer norm of rows to y (dense), to `codes` (by rows), or the statistics alone where both are null.
 hipError_t launch_layer_norm(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t x_stride, const NormArgs& n,
                              void* y, int64_t y_stride, void* codes, hipStream_t s);
+// Layer norm to codes by columns, and by rows too where by_rows is not null, in one pass over rows that fit.
+bool norm_blocks_fit(int32_t dtype, int64_t rows, int64_t cols);
+hipError_t launch_norm_blocks(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t x_stride, const NormArgs& n, void* by_rows,
+                              void* by_columns, hipStream_t s);
 // The quantiser over tiles of 256 rows, with or without a norm whose statistics are known; either form may be null.  `sums` (without a
 // norm): mx_tile_rows(rows) rows of partial sums of x's columns, or null.
 inline int64_t mx_tile_rows(int64_t rows) { return (rows + 255) / 256; }

@@ -233,3 +233,31 @@ def test_codes_without_parameters_from_views(api):
     for forms in ("rows", "columns"):
         got, _, _ = api.fh_layer_norm_mx(x, forms=forms)
         assert torch.equal(api.fh_mx_dequantize(got), api.fh_mx_dequantize(api.fh_mx_quantize(y, forms)))
+
+
+@pytest.mark.parametrize("params", ["f32", "bf16"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_codes_by_columns_of_every_width(api, dtype, params):
+    """Around every limit on the columns and the rows, from rows that are not next to each other: both forms are those of the fp32
+    output's, whichever kernels made them, and the form by rows is the one that is made alone."""
+    for i, (rows, cols) in enumerate([(1, 1), (31, 255), (32, 256), (33, 257), (64, 512), (65, 513), (257, 767), (520, 1023), (290, 1024), (40, 1025), (300, 1536),
+                                      (96, 1537), (513, 2047), (255, 2048), (34, 2049)]):
+        t, _, w, b = _inputs(rows, cols + 5, dtype, params, i)
+        x, w, b = t.cuda()[:, 2:2 + cols], w[:cols].cuda(), b[:cols].cuda()
+        y, mean, rstd = api.fh_layer_norm(x.float(), w, b)
+        (r, c), mean2, rstd2 = api.fh_layer_norm_mx(x, w, b, forms="both")
+        alone = api.fh_layer_norm_mx(x, w, b, forms="columns")[0], api.fh_layer_norm_mx(x, w, b, forms="rows")[0]
+        assert torch.equal(mean, mean2) and torch.equal(rstd, rstd2), (rows, cols)
+        for m, want in zip((r, c, *alone), (*api.fh_mx_quantize(y, "both"), api.fh_mx_quantize(y, "columns"), api.fh_mx_quantize(y, "rows"))):
+            known = torch.from_numpy(R.stored(np.zeros((m.rows, m.cols), np.float32))[1]).cuda()
+            assert torch.equal(m.data[known], want.data[known]), (rows, cols)
+
+
+def test_codes_of_broken_rows(api):
+    """A row with a NaN or an infinity is NaN everywhere, and so is the block of every column that it is in, and nothing else."""
+    x = torch.randn(100, 300, device="cuda")
+    x[40, 7], x[97, 299] = float("nan"), float("inf")
+    (r, c), _, _ = api.fh_layer_norm_mx(x, forms="both")
+    by_rows, by_columns = torch.isnan(api.fh_mx_dequantize(r)), torch.isnan(api.fh_mx_dequantize(c))
+    assert by_rows[[40, 97]].all() and int(by_rows.sum()) == 600
+    assert by_columns[:, 32:64].all() and by_columns[:, 96:].all() and int(by_columns.sum()) == 300 * 36
