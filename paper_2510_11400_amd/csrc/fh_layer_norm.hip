@@ -205,7 +205,8 @@ __global__ __launch_bounds__(1024) void norm_long_rows_kernel(const T* x, int64_
 // ---- forward to codes by columns: blocks of 32 rows -----------------------------------------
 // A block of a column is 32 rows, so a workgroup that has all of 32 rows writes both forms from one pass over x: it takes a row's
 // statistics and codes from registers as above, leaves the row in LDS, and then has its columns in the lanes.  With a kernel for the
-// statistics and the tiles behind it x was read twice and a launch more was waited for (8192 x 768 bf16 17.4 us, this 12.4).
+// statistics and the tiles behind it x was read twice and a launch more was waited for: bf16 64 x 768 12.6 -> 8.6 us, 8192 x 768 16.3 -> 11.5,
+// 8192 x 2048 26.7 -> 20.5, 32768 x 256 17.4 -> 18.8, fp32 8192 x 1024 18.5 -> 13.5.  Bound by arithmetic, some fifteen instructions a value and form.
 // A column's 16 bytes of a block are an eighth of a line: neighbours run on one XCD, in whose L2 the line is put together.
 template <typename T, int LANES, int NV>
 __global__ __launch_bounds__(1024) void norm_blocks_kernel(const T* x, int64_t rows, int64_t cols, int64_t x_stride, NormArgs n, uint8_t* rows_form,

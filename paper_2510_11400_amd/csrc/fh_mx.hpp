@@ -163,9 +163,12 @@ struct Run {
             }
         } else {
 #pragma unroll
+            for (int i = 0; i < kWords; ++i) w[i] = 0u;
+            if (n <= 0) return;                                  // not by way of the run's end, which waits for the loads before it
+#pragma unroll
             for (int i = 0; i < N; ++i) {
                 if constexpr (sizeof(T) == 4) w[i] = i < n ? __builtin_bit_cast(uint32_t, p[i]) : 0u;
-                else w[i / 2] = (i & 1 ? w[i / 2] : 0u) | (i < n ? (uint32_t)p[i].bits : 0u) << (16 * (i & 1));
+                else w[i / 2] |= (i < n ? (uint32_t)p[i].bits : 0u) << (16 * (i & 1));
             }
         }
     }
@@ -190,6 +193,8 @@ __device__ __forceinline__ void load8(const float* p, int64_t n, float (&v)[8])
         const f32x4 a = *reinterpret_cast<const f32x4_a4*>(p), b = *reinterpret_cast<const f32x4_a4*>(p + 4);
         for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
     } else {
+        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        if (n <= 0) return;
         for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
     }
 }
@@ -199,6 +204,8 @@ __device__ __forceinline__ void load8(const Bf16* p, int64_t n, float (&v)[8])
         const u32x4 a = *reinterpret_cast<const u32x4_a2*>(p);
         for (int i = 0; i < 4; ++i) { const uint32_t w = a[i]; v[2 * i] = bf16_lo(w); v[2 * i + 1] = bf16_hi(w); }
     } else {
+        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        if (n <= 0) return;
         for (int i = 0; i < 8; ++i) v[i] = i < n ? value(p[i]) : 0.0f;
     }
 }
