@@ -630,8 +630,8 @@ hipError_t launch_join(const float* partial, int64_t parts, int64_t cols, int32_
     return launch(norm_join_kernel<Bf16>, grid, block, s, partial, parts, cols, count, static_cast<Bf16*>(first), static_cast<Bf16*>(second));
 }
 
-// Rows whose 32 fit in LDS, beside a second workgroup's up to half of that.
-bool norm_blocks_fit(int32_t dtype, int64_t rows, int64_t cols) { return cols <= (dtype == FH_F32 ? 1024 : 2048) && mx_chunks(rows) <= INT32_MAX / 8; }
+// Rows of which 32 fit in LDS, and no more threads than a launch may have (2^32).
+bool norm_blocks_fit(int32_t dtype, int64_t rows, int64_t cols) { return cols <= (dtype == FH_F32 ? 1024 : 2048) && mx_chunks(rows) < (1 << 19); }
 
 hipError_t launch_norm_blocks(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t x_stride, const NormArgs& n, void* by_rows,
                               void* by_columns, hipStream_t s)

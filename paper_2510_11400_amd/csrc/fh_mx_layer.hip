@@ -147,6 +147,8 @@ fh_status fh_mx_layer_backward(const fh_mx_layer* l, void* stream)
         if ((s = fh_mx_matmul(&dw, stream)) != FH_OK) return s;
     }
     if (!input) return FH_OK;
+    // With a norm its output's gradient is rounded to dtype on the way, as between two layers of their own: in bf16 dx is then 0.0024 of its
+    // norm from the exact one instead of 0.0017, and 8192 x 768 values go through memory as 25 MB instead of 50.
     const size_t dx_bytes = (size_t)l->tokens * (size_t)l->features * size;
     const fh_mx_product dx = {dy_rows, rows_bytes, at(l->kept, p.w_columns), mx_bytes(l->features, l->out_features), l->tokens, l->features,
                               l->out_features, nullptr, l->p_dtype, l->dtype, l->dx, l->features, dx_bytes, work, work_bytes, 0};
