@@ -301,3 +301,15 @@ def test_the_binding_refuses(api):
         api.fh_mx_dequantize(api.MxMatrix(m.data[:-1], 8, 64))
     with pytest.raises(ValueError):
         api.fh_mx_dequantize(m, out=torch.zeros(8, 63, device="cuda"))
+
+
+@pytest.mark.parametrize("rows, cols", [(65536, 200), (65537, 200), (65539, 33), (32771, 300)])
+def test_restored_values_of_many_rows(api, rows, cols):
+    """Around the number of rows from which a lane takes several, the last ones fewer, into a view: exact products of codes and scales."""
+    t, x = _values(rows, cols, rows)
+    m = api.fh_mx_quantize(t.cuda())
+    want = torch.from_numpy(R.restored(m.data.cpu().numpy(), rows, cols))
+    for dtype in (torch.float32, torch.bfloat16):
+        wide = torch.full((rows, cols + 3), 7.0, dtype=dtype, device="cuda")
+        api.fh_mx_dequantize(m, out=wide[:, 1:1 + cols])
+        assert torch.equal(wide[:, 1:1 + cols].cpu(), want.to(dtype)) and (wide[:, 0] == 7).all() and (wide[:, 1 + cols:] == 7).all()
