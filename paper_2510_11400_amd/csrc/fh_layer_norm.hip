@@ -1,4 +1,6 @@
 // Layer norm, its backward pass, and the form that writes 4-bit codes.
+#include <type_traits>
+
 #include "fh_norm.hpp"
 
 namespace fh {
@@ -29,9 +31,9 @@ __device__ __forceinline__ void row_sums(float& v, float& u, f32x2 (&s_pairs)[2]
 // Mean and sum of squares about it of a row whose T threads hold `sum` of its values, and whose squares about any mean
 // `about(mean)` gives.  Each wave takes the squares about its own mean, and one barrier brings the waves' sums and squares
 // together: with n_w values of mean m_w in wave w the squares about the row's mean m are sum_w (squares_w + n_w (m_w - m)^2), which
-// costs no digits either.  `s_counts`: n_w.
+// costs no digits either.  `s_counts`: n_w; `s_waves`: each wave's sum, squares and mean.
 template <int T, typename About>
-__device__ __forceinline__ void row_moments(float sum, float columns, float& mean, float& squares, About about, f32x2 (&s_pairs)[2][16],
+__device__ __forceinline__ void row_moments(float sum, float columns, float& mean, float& squares, About about, f32x4 (&s_waves)[2][16],
                                             const float (&s_counts)[16], int turn)
 {
     if constexpr (T <= 64) {
@@ -40,11 +42,18 @@ __device__ __forceinline__ void row_moments(float sum, float columns, float& mea
     } else {
         const int wave = threadIdx.x >> 6;
         const float all = lane_sum<64>(sum), count = s_counts[wave % (T / 64)];
-        const float inside = lane_sum<64>(about(count > 0.0f ? all / count : 0.0f));
-        f32x2* pairs = s_pairs[turn & 1];
-        if ((threadIdx.x & 63) == 0) pairs[wave] = f32x2{all, inside};
+        const float own = count > 0.0f ? all / count : 0.0f;
+        const float inside = lane_sum<64>(about(own));
+        // With two waves a row the divisions are made again: a mean more in registers costs their kernels a wave a SIMD (4096 x 4096 bf16
+        // 14.6 -> 17.7 us); with more it is one more value of the wave's (64 x 8192 5.6 -> 4.5, 2047 x 8193 fp32 30.8 -> 28.5).
+        using Sums = std::conditional_t<T == 128, f32x2, f32x4>;
+        Sums* waves = reinterpret_cast<Sums*>(s_waves[turn & 1]);
+        if ((threadIdx.x & 63) == 0) {
+            if constexpr (T == 128) waves[wave] = f32x2{all, inside};
+            else waves[wave] = f32x4{all, inside, own, count};
+        }
         __syncthreads();
-        const f32x2* mine = pairs + threadIdx.x / T * (T / 64);
+        const Sums* mine = waves + threadIdx.x / T * (T / 64);
         float total = 0.0f;
 #pragma unroll 4
         for (int w = 0; w < T / 64; ++w) total += mine[w].x;
@@ -52,7 +61,15 @@ __device__ __forceinline__ void row_moments(float sum, float columns, float& mea
         squares = 0.0f;
 #pragma unroll 4
         for (int w = 0; w < T / 64; ++w) {
-            const float n = s_counts[w], d = n > 0.0f ? mine[w].x / n - mean : 0.0f;
+            float n, m;
+            if constexpr (T == 128) {
+                n = s_counts[w];
+                m = n > 0.0f ? mine[w].x / n : mean;
+            } else {
+                n = mine[w].w;
+                m = n > 0.0f ? mine[w].z : mean;
+            }
+            const float d = m - mean;
             squares += __builtin_fmaf(n * d, d, mine[w].y);
         }
     }
@@ -71,7 +88,7 @@ __global__ __launch_bounds__(kNormGroup<THREADS>) void norm_rows_kernel(const T*
                                                                                   NormArgs n, NormOut to, int32_t groups)
 {
     constexpr int kRows = kNormGroup<THREADS> / THREADS, kWhole = NV - 1;
-    __shared__ f32x2 s_pairs[2][16];
+    __shared__ __attribute__((aligned(16))) f32x4 s_waves[2][16];
     __shared__ float s_counts[16];                               // columns of a row's waves
     const int t = threadIdx.x % THREADS, part = threadIdx.x / THREADS;
     Run<T> next[NV];
@@ -135,7 +152,7 @@ __global__ __launch_bounds__(kNormGroup<THREADS>) void norm_rows_kernel(const T*
             return squares;
         };
         float mean, squares;
-        row_moments<THREADS>(sum, columns, mean, squares, about, s_pairs, s_counts, turn);
+        row_moments<THREADS>(sum, columns, mean, squares, about, s_waves, s_counts, turn);
         const float rstd = 1.0f / __builtin_sqrtf(squares / columns + n.eps);
         if (write && t == 0) {
             if (n.mean) n.mean[row] = mean;
