@@ -371,8 +371,25 @@ __global__ __launch_bounds__(THREADS * ROWS) void norm_backward_kernel(NormBackw
         }
     };
     if constexpr (kAhead) load((int64_t)blockIdx.x * ROWS + part);
-    for (int c = threadIdx.x; c < NV * kWidth; c += THREADS * ROWS)
-        s_weight[c] = c < a.cols ? parameter(a.weight, a.p_dtype, c, 1.0f) : 0.0f;
+    const auto stage_weight = [&](const auto* p) {               // all loads ahead of the first store (one value at a time: 3 x 14488 fp32 11.8 us, now 9.8)
+        using P = std::remove_cv_t<std::remove_reference_t<decltype(*p)>>;
+        constexpr int kRuns = NV * THREADS, kTimes = (kRuns + THREADS * ROWS - 1) / (THREADS * ROWS);
+        Run<P, 4> run[kTimes];
+#pragma unroll
+        for (int i = 0; i < kTimes; ++i) {
+            const int at = (threadIdx.x + i * THREADS * ROWS) * 4;
+            run[i].load(p + at, at < kRuns * 4 ? a.cols - at : 0);
+        }
+#pragma unroll
+        for (int i = 0; i < kTimes; ++i) {
+            const int at = (threadIdx.x + i * THREADS * ROWS) * 4;
+            if (at < kRuns * 4) *reinterpret_cast<f32x4*>(s_weight + at) = f32x4{run[i].at(0), run[i].at(1), run[i].at(2), run[i].at(3)};
+        }
+    };
+    if (!a.weight) {
+        for (int c = threadIdx.x; c < NV * kWidth; c += THREADS * ROWS) s_weight[c] = c < a.cols ? 1.0f : 0.0f;
+    } else if (a.p_dtype == FH_F32) stage_weight(static_cast<const float*>(a.weight));
+    else stage_weight(static_cast<const Bf16*>(a.weight));
     __syncthreads();
     f32x4 dw[NV] = {}, db[NV] = {};
     const float share = 1.0f / (float)a.cols;
