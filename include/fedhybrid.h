@@ -581,12 +581,16 @@ fh_status fh_layer_norm_backward(const fh_norm_backward *norm, void *stream);
  *             (NEEDS_WEIGHT); fh_mx_matmul: dweight = dy^T x; fh_mx_matmul: dx = dy W, rounded to
  *             dtype; with a norm fh_layer_norm_backward of that in place (dnorm_weight, dnorm_bias
  *             may be NULL); dbias (or NULL): the sum of dy's rows in binary32, in an order of the shape alone.
+ *             With wide_gradient dy W is not rounded ahead of the norm's backward pass, which takes it
+ *             in binary32; dx is rounded to dtype once.
  * x is tokens x features and weight out_features x features, rows contiguous with row strides; dy
  * tokens x out_features with a row stride; y, dx and dweight are dense.  x, y, dy and dx are of dtype, the
  * norm's parameters, weight, bias and their gradients of p_dtype; norm_weight, norm_bias and bias may
  * be NULL.  `kept` (fh_mx_layer_kept_bytes) carries the statistics and the operands by columns from
  * the forward to the backward call and may be NULL where there is neither a norm nor a need (in the backward call: no need); `scratch`
- * (fh_mx_layer_scratch_bytes) is free again once a call's work has run.  Both 16-byte aligned.
+ * (fh_mx_layer_scratch_bytes, which is enough for either call without wide_gradient) is free again
+ * once a call's work has run.  Both 16-byte aligned.  fh_mx_layer_sizes gives the bytes that the calls with this layer ask for (no
+ * pointer of it is looked at).
  * The backward call takes the same needs as the forward one had, or fewer.  1 <= features,
  * out_features <= 2^24, tokens <= 2^24; tokens = 0 writes zeros to the gradients of the parameters.
  * Everything is checked before the first launch. */
@@ -609,9 +613,11 @@ typedef struct fh_mx_layer {
     void       *scratch;    size_t scratch_cap;
     int64_t     reserved;                       /* 0 */
     void       *dbias;                          /* backward */
+    int32_t     wide_gradient;                  /* backward: 0 | 1 */
 } fh_mx_layer;
 size_t    fh_mx_layer_kept_bytes(int64_t tokens, int64_t features, int64_t out_features);
 size_t    fh_mx_layer_scratch_bytes(int64_t tokens, int64_t features, int64_t out_features);
+fh_status fh_mx_layer_sizes(const fh_mx_layer *layer, size_t *kept, size_t *forward_scratch, size_t *backward_scratch);
 fh_status fh_mx_layer_forward(const fh_mx_layer *layer, void *stream);
 fh_status fh_mx_layer_backward(const fh_mx_layer *layer, void *stream);
 

@@ -46,7 +46,7 @@ EXPORTS = ("fh_packed_bytes", "fh_meta_bytes", "fh_compress", "fh_decompress", "
            "fh_mix_layout", "fh_mix_compress", "fh_mix_decompress", "fh_mix_compress_batch", "fh_mix_decompress_batch",
            "fh_mx_bytes", "fh_mx_scales_offset", "fh_mx_quantize", "fh_mx_dequantize", "fh_mx_matmul_workspace_bytes", "fh_mx_matmul",
            "fh_layer_norm", "fh_layer_norm_mx", "fh_layer_norm_backward_workspace_bytes", "fh_layer_norm_backward",
-           "fh_mx_layer_kept_bytes", "fh_mx_layer_scratch_bytes", "fh_mx_layer_forward", "fh_mx_layer_backward",
+           "fh_mx_layer_kept_bytes", "fh_mx_layer_scratch_bytes", "fh_mx_layer_sizes", "fh_mx_layer_forward", "fh_mx_layer_backward",
            "fh_status_string")
 
 
@@ -285,12 +285,14 @@ class fh_mx_layer(ctypes.Structure):
                 ("dy", ctypes.c_void_p), ("dy_stride", ctypes.c_int64), ("dx", ctypes.c_void_p), ("dweight", ctypes.c_void_p),
                 ("dnorm_weight", ctypes.c_void_p), ("dnorm_bias", ctypes.c_void_p),
                 ("kept", ctypes.c_void_p), ("kept_cap", ctypes.c_size_t), ("scratch", ctypes.c_void_p), ("scratch_cap", ctypes.c_size_t),
-                ("reserved", ctypes.c_int64), ("dbias", ctypes.c_void_p)]
+                ("reserved", ctypes.c_int64), ("dbias", ctypes.c_void_p), ("wide_gradient", ctypes.c_int32)]
 
 
 for _name in ("fh_mx_layer_kept_bytes", "fh_mx_layer_scratch_bytes"):
     getattr(_lib, _name).argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64]
     getattr(_lib, _name).restype = ctypes.c_size_t
+_lib.fh_mx_layer_sizes.argtypes = [_P(fh_mx_layer), _P(ctypes.c_size_t), _P(ctypes.c_size_t), _P(ctypes.c_size_t)]
+_lib.fh_mx_layer_sizes.restype = ctypes.c_int
 for _name in ("fh_mx_layer_forward", "fh_mx_layer_backward"):
     getattr(_lib, _name).argtypes = [_P(fh_mx_layer), ctypes.c_void_p]
     getattr(_lib, _name).restype = ctypes.c_int
@@ -1386,15 +1388,17 @@ FH_MX_NEEDS_INPUT, FH_MX_NEEDS_WEIGHT = 1, 2
 class MxLayer:
     """One pass through a linear layer in microscaled form: what its forward call keeps for its backward call.  x: [tokens,
     features], weight: [out, features]; `norm`: a layer norm ahead, with norm_weight and norm_bias (either may be None).  Parameters
-    are of one dtype, and so are x, y and the gradients of both."""
-    __slots__ = ("inputs", "kept", "shape", "dtype", "p_dtype", "features", "norm", "eps", "needs_input", "needs_weight", "rounding")
+    are of one dtype, and so are x, y and the gradients of both.  The norm's backward pass takes its output's gradient rounded to
+    that dtype, as from a layer of its own, with `wide_gradient` in fp32."""
+    __slots__ = ("inputs", "kept", "shape", "dtype", "p_dtype", "features", "norm", "eps", "needs_input", "needs_weight", "rounding",
+                 "wide_gradient")
 
     def __init__(self, x: torch.Tensor, weight: torch.Tensor, bias=None, norm: bool = False, norm_weight=None, norm_bias=None,
                  eps: float = 1e-5, needs_input: bool = True, needs_weight: bool = True, rounding="nearest", seed: int = 0,
-                 tensor_id: int = 0):
+                 tensor_id: int = 0, wide_gradient: bool = False):
         self.inputs, self.kept = (x, weight, bias, norm, norm_weight, norm_bias, eps, needs_input, needs_weight), None
         self.norm, self.eps, self.needs_input, self.needs_weight = norm, eps, needs_input, needs_weight
-        self.rounding = (rounding, seed, tensor_id)
+        self.rounding, self.wide_gradient = (rounding, seed, tensor_id), wide_gradient
         if rounding not in _ROUND:
             raise KeyError(rounding)
 
@@ -1413,5 +1417,5 @@ class MxLayer:
         if dy.shape != self.shape or dy.dtype != self.dtype:
             raise ValueError("dy must have the shape and the dtype of y")
         grads = _binding.layer_backward(dy, x, norm_weight, self.kept, self.features, self.p_dtype, self.norm, self.eps, self.needs_input,
-                                        self.needs_weight, bias, *self.rounding, stream)
+                                        self.needs_weight, bias, *self.rounding, self.wide_gradient, stream)
         return grads if bias else grads[:4]

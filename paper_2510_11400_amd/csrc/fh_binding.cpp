@@ -438,7 +438,21 @@ FH_ENTRY(layer_norm_backward, 9)
 FH_EXIT
 
 // ---- a linear layer's two halves ----------------------------------------------------------------
-struct Layer { bool norm; float eps; bool input, weight, bias; int rounding; uint64_t seed, id; };    // input, weight, bias: what gradients are wanted of
+struct Layer {
+    bool norm;
+    float eps;
+    bool input, weight, bias;                                             // what gradients are wanted of
+    int rounding;
+    uint64_t seed, id;
+    bool wide;                                                            // the gradient of a norm's output in fp32
+};
+struct Sizes { size_t kept, forward, backward; };
+Sizes sizes_of(const fh_mx_layer& l)                                      // of a layer that the call itself will refuse: nothing
+{
+    Sizes s = {};
+    if (fh_mx_layer_sizes(&l, &s.kept, &s.forward, &s.backward) != FH_OK) return {};
+    return s;
+}
 
 struct Forward { at::Tensor y, kept; };
 Forward forward_of(const Layer& layer, const Matrix& x, const Matrix& weight, const at::Tensor& bias, const at::Tensor& norm_weight, const at::Tensor& norm_bias,
@@ -459,14 +473,15 @@ Forward forward_of(const Layer& layer, const Matrix& x, const Matrix& weight, co
     l.norm_weight = vector(norm_weight, x.cols, device, "norm_weight");
     l.norm_bias = vector(norm_bias, x.cols, device, "norm_bias");
     l.bias = vector(bias, weight.rows, device, "bias");
+    const Sizes sizes = sizes_of(l);
     Forward f;
     f.y = new_matrix(x.rows, weight.rows, x.t.scalar_type(), device).t;
     l.y = f.y.data_ptr();
     if (layer.norm || l.needs) {
-        f.kept = bytes(fh_mx_layer_kept_bytes(l.tokens, l.features, l.out_features), device);
+        f.kept = bytes(sizes.kept, device);
         l.kept = f.kept.data_ptr(); l.kept_cap = (size_t)f.kept.numel();
     }
-    const Work w = work(Py_None, fh_mx_layer_scratch_bytes(l.tokens, l.features, l.out_features), device, stream);
+    const Work w = work(Py_None, sizes.forward, device, stream);
     l.scratch = w.p; l.scratch_cap = w.n;
     enqueue(device, stream, [&](void* s) { return fh_mx_layer_forward(&l, s); });
     return f;
@@ -487,7 +502,7 @@ Backward backward_of(const Layer& layer, const Matrix& dy, const at::Tensor& x_a
     l.dtype = dy.dtype; l.p_dtype = dtype_code(p_type); l.norm = layer.norm;
     l.needs = (layer.input ? FH_MX_NEEDS_INPUT : 0) | (layer.weight ? FH_MX_NEEDS_WEIGHT : 0);
     l.eps = layer.eps;
-    l.rounding = layer.rounding; l.seed = layer.seed; l.tensor_id = layer.id;
+    l.rounding = layer.rounding; l.seed = layer.seed; l.tensor_id = layer.id; l.wide_gradient = layer.wide;
     l.dy = dy.data(); l.dy_stride = dy.stride; l.x_stride = l.weight_stride = features;
     if (kept.defined()) { l.kept = kept.data_ptr(); l.kept_cap = kept.nbytes(); }
     Backward b;
@@ -514,7 +529,7 @@ Backward backward_of(const Layer& layer, const Matrix& dy, const at::Tensor& x_a
             l.dnorm_weight = b.dnorm.first.data_ptr(); l.dnorm_bias = b.dnorm.second.data_ptr();
         }
     }
-    const Work w = work(Py_None, fh_mx_layer_scratch_bytes(l.tokens, features, l.out_features), device, stream);
+    const Work w = work(Py_None, sizes_of(l).backward, device, stream);
     l.scratch = w.p; l.scratch_cap = w.n;
     enqueue(device, stream, [&](void* s) { return fh_mx_layer_backward(&l, s); });
     return b;
@@ -522,18 +537,18 @@ Backward backward_of(const Layer& layer, const Matrix& dy, const at::Tensor& x_a
 
 // (x, weight, bias, norm, norm_weight, norm_bias, eps, needs_input, needs_weight, stream) -> (y, kept)
 FH_ENTRY(layer_forward, 10)
-    const Layer layer = {truth(a[3]), (float)f64(a[6]), truth(a[7]), truth(a[8]), false, FH_ROUND_NEAREST, 0, 0};
+    const Layer layer = {truth(a[3]), (float)f64(a[6]), truth(a[7]), truth(a[8]), false, FH_ROUND_NEAREST, 0, 0, false};
     const Forward f = forward_of(layer, matrix(a[0], "x"), matrix(a[1], "weight"), tensor_or_none(a[2], "bias"), tensor_or_none(a[4], "norm_weight"),
                                  tensor_or_none(a[5], "norm_bias"), a[9]);
     return tuple(Ref(wrap(f.y)), Ref(wrap(f.kept)));
 FH_EXIT
 
-// (dy, x, norm_weight, kept, features, p_dtype, norm, eps, needs_input, needs_weight, needs_bias, rounding, seed, tensor_id, stream)
-//   -> (dx, dweight, dnorm_weight, dnorm_bias, dbias)
-FH_ENTRY(layer_backward, 15)
-    const Layer layer = {truth(a[6]), (float)f64(a[7]), truth(a[8]), truth(a[9]), truth(a[10]), rounding_of(a[11]), u64(a[12]), u64(a[13])};
+// (dy, x, norm_weight, kept, features, p_dtype, norm, eps, needs_input, needs_weight, needs_bias, rounding, seed, tensor_id, wide_gradient,
+//  stream) -> (dx, dweight, dnorm_weight, dnorm_bias, dbias)
+FH_ENTRY(layer_backward, 16)
+    const Layer layer = {truth(a[6]), (float)f64(a[7]), truth(a[8]), truth(a[9]), truth(a[10]), rounding_of(a[11]), u64(a[12]), u64(a[13]), truth(a[14])};
     const Backward b = backward_of(layer, matrix(a[0], "dy"), tensor_or_none(a[1], "x"), tensor_or_none(a[2], "norm_weight"), tensor_or_none(a[3], "kept"), i64(a[4]),
-                                   scalar_type(a[5]), a[14]);
+                                   scalar_type(a[5]), a[15]);
     return tuple(Ref(wrap(b.dx)), Ref(wrap(b.dweight)), Ref(wrap(b.dnorm.first)), Ref(wrap(b.dnorm.second)), Ref(wrap(b.dbias)));
 FH_EXIT
 
@@ -612,7 +627,7 @@ FH_ENTRY(mx_linear, 9)
     const auto wanted = [&](const at::Tensor& t) { return grad && t.defined() && t.requires_grad(); };
     pass->x = wanted(x); pass->norm_weight = wanted(norm_weight); pass->norm_bias = wanted(norm_bias);
     pass->layer = {norm, norm ? (float)f64(a[5]) : 0.0f, pass->x || pass->norm_weight || pass->norm_bias, wanted(weight), wanted(bias),
-                   rounding_of(a[6]), u64(a[7]), u64(a[8])};
+                   rounding_of(a[6]), u64(a[7]), u64(a[8]), true};
     pass->p_type = weight.scalar_type();
     pass->shape = x.sizes().vec();
     at::Tensor y;

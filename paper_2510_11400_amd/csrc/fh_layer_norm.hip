@@ -346,17 +346,19 @@ struct NormBackwardArgs {
 // left a quarter of the lanes idle, and the arithmetic of some 17 instructions a value is what binds rows of bf16).  Every
 // thread keeps the sums of its columns in registers; at the end the rows' sums are added up in LDS, all at once (by runs of
 // columns it took two barriers a run and sum: 8192 x 768 bf16 13.7 -> 12.4 us), and the workgroup leaves one row of partial sums, for norm_join_kernel.
-template <typename T, int THREADS, int NV, int ROWS>
+// dy is of type G: T, or float where it is a product that has not been rounded to T.
+template <typename T, typename G, int THREADS, int NV, int ROWS>
 __global__ __launch_bounds__(THREADS * ROWS) void norm_backward_kernel(NormBackwardArgs a)
 {
-    constexpr bool kAhead = sizeof(T) == 2 || NV < (THREADS < 1024 ? 8 : 4);   // the next row's loads before this row's sums: as registers allow
+    constexpr bool kAhead = sizeof(G) == 2 || NV < (THREADS < 1024 ? 8 : 4);   // the next row's loads before this row's sums: as registers allow
     constexpr int kWidth = THREADS * 4;
     __shared__ f32x2 s_pairs[2][16];
     __shared__ __attribute__((aligned(16))) float s_join[ROWS > 1 ? ROWS * 2 * NV * kWidth : 4];
     // the weight, read again for every row: in registers it would push the next row's loads out of them
     __shared__ __attribute__((aligned(16))) float s_weight[NV * kWidth];
     const int t = threadIdx.x % THREADS, part = threadIdx.x / THREADS;
-    Run<T, 4> next_x[NV], next_g[NV];
+    Run<T, 4> next_x[NV];
+    Run<G, 4> next_g[NV];
     float next_mean = 0.0f, next_rstd = 0.0f;
     auto load = [&](int64_t row) {                               // nothing of a row past the last
         const bool here = row < a.rows;
@@ -367,7 +369,7 @@ __global__ __launch_bounds__(THREADS * ROWS) void norm_backward_kernel(NormBackw
         for (int k = 0; k < NV; ++k) {
             const int64_t first = (int64_t)k * kWidth + t * 4;
             next_x[k].load(static_cast<const T*>(a.x) + at * a.x_stride + first, here ? a.cols - first : 0);
-            next_g[k].load(static_cast<const T*>(a.dy) + at * a.dy_stride + first, here ? a.cols - first : 0);
+            next_g[k].load(static_cast<const G*>(a.dy) + at * a.dy_stride + first, here ? a.cols - first : 0);
         }
     };
     if constexpr (kAhead) load((int64_t)blockIdx.x * ROWS + part);
@@ -465,12 +467,13 @@ __global__ __launch_bounds__(THREADS * ROWS) void norm_backward_kernel(NormBackw
 }
 
 // Rows that do not fit: dx by a workgroup a row, which reads the row twice; the columns' sums by a kernel of their own.
-template <typename T>
+template <typename T, typename G>
 __global__ __launch_bounds__(1024) void norm_backward_long_rows_kernel(NormBackwardArgs a)
 {
     __shared__ f32x2 s_pairs[2][16];
     const int64_t row = blockIdx.x;
-    const T *px = static_cast<const T*>(a.x) + row * a.x_stride, *pg = static_cast<const T*>(a.dy) + row * a.dy_stride;
+    const T* px = static_cast<const T*>(a.x) + row * a.x_stride;
+    const G* pg = static_cast<const G*>(a.dy) + row * a.dy_stride;
     const float mean = a.mean[row], rstd = a.rstd[row], share = 1.0f / (float)a.cols;
     float x[8], g[8], s1 = 0.0f, s2 = 0.0f;
     for (int64_t first = threadIdx.x * 8; first < a.cols; first += 8192) {
@@ -495,7 +498,7 @@ __global__ __launch_bounds__(1024) void norm_backward_long_rows_kernel(NormBackw
         store8(static_cast<T*>(a.dx) + row * a.dx_stride + first, a.cols - first, g);
     }
 }
-template <typename T>
+template <typename T, typename G>
 __global__ __launch_bounds__(256) void norm_column_sums_kernel(NormBackwardArgs a, int64_t rows_each, uint32_t col_groups)
 {
     const int64_t first = ((int64_t)(blockIdx.x % col_groups) * 256 + threadIdx.x) * 8, part = blockIdx.x / col_groups;
@@ -504,7 +507,7 @@ __global__ __launch_bounds__(256) void norm_column_sums_kernel(NormBackwardArgs 
     const int64_t end = part * rows_each + rows_each < a.rows ? part * rows_each + rows_each : a.rows;
     for (int64_t row = part * rows_each; row < end; ++row) {
         load8(static_cast<const T*>(a.x) + row * a.x_stride + first, a.cols - first, x);
-        load8(static_cast<const T*>(a.dy) + row * a.dy_stride + first, a.cols - first, g);
+        load8(static_cast<const G*>(a.dy) + row * a.dy_stride + first, a.cols - first, g);
         const float mean = a.mean[row], rstd = a.rstd[row];
         for (int i = 0; i < 8; ++i) {
             dw[i] = __builtin_fmaf(g[i], (x[i] - mean) * rstd, dw[i]);
@@ -619,12 +622,12 @@ inline int64_t backward_groups(int64_t rows, int64_t cols)
     return groups < kMostParts ? groups : kMostParts;
 }
 
-template <typename T, int THREADS, int NV, int ROWS>
+template <typename T, typename G, int THREADS, int NV, int ROWS>
 hipError_t backward_of(const NormBackwardArgs& a, int64_t groups, hipStream_t s)
 {
-    return launch(norm_backward_kernel<T, THREADS, NV, ROWS>, dim3((uint32_t)groups), dim3(THREADS * ROWS), s, a);
+    return launch(norm_backward_kernel<T, G, THREADS, NV, ROWS>, dim3((uint32_t)groups), dim3(THREADS * ROWS), s, a);
 }
-template <typename T>
+template <typename T, typename G>
 hipError_t backward_any(const NormBackwardArgs& a, int64_t* parts, hipStream_t s)
 {
     const int64_t groups = a.groups;
@@ -633,27 +636,27 @@ hipError_t backward_any(const NormBackwardArgs& a, int64_t* parts, hipStream_t s
         const BackwardShape b = backward_shape(a.rows, a.cols);
         const bool few = b.threads * b.rows == 256;
         switch (b.threads * 16 + b.runs) {
-            case 16 * 16 + 1: return few ? backward_of<T, 16, 1, 16>(a, groups, s) : backward_of<T, 16, 1, 64>(a, groups, s);
-            case 32 * 16 + 1: return few ? backward_of<T, 32, 1, 8>(a, groups, s) : backward_of<T, 32, 1, 32>(a, groups, s);
-            case 64 * 16 + 1: return few ? backward_of<T, 64, 1, 4>(a, groups, s) : backward_of<T, 64, 1, 16>(a, groups, s);
-            case 64 * 16 + 2: return few ? backward_of<T, 64, 2, 4>(a, groups, s) : backward_of<T, 64, 2, 16>(a, groups, s);
-            case 64 * 16 + 3: return few ? backward_of<T, 64, 3, 4>(a, groups, s) : backward_of<T, 64, 3, 16>(a, groups, s);
-            case 64 * 16 + 4: return few ? backward_of<T, 64, 4, 4>(a, groups, s) : backward_of<T, 64, 4, 12>(a, groups, s);
-            case 64 * 16 + 6: return few ? backward_of<T, 64, 6, 4>(a, groups, s) : backward_of<T, 64, 6, 8>(a, groups, s);
-            case 64 * 16 + 8: return few ? backward_of<T, 64, 8, 4>(a, groups, s) : backward_of<T, 64, 8, 8>(a, groups, s);
-            case 256 * 16 + 4: return few ? backward_of<T, 256, 4, 1>(a, groups, s) : backward_of<T, 256, 4, 3>(a, groups, s);
-            case 1024 * 16 + 2: return backward_of<T, 1024, 2, 1>(a, groups, s);
-            case 1024 * 16 + 3: return backward_of<T, 1024, 3, 1>(a, groups, s);
-            default: return backward_of<T, 1024, 4, 1>(a, groups, s);
+            case 16 * 16 + 1: return few ? backward_of<T, G, 16, 1, 16>(a, groups, s) : backward_of<T, G, 16, 1, 64>(a, groups, s);
+            case 32 * 16 + 1: return few ? backward_of<T, G, 32, 1, 8>(a, groups, s) : backward_of<T, G, 32, 1, 32>(a, groups, s);
+            case 64 * 16 + 1: return few ? backward_of<T, G, 64, 1, 4>(a, groups, s) : backward_of<T, G, 64, 1, 16>(a, groups, s);
+            case 64 * 16 + 2: return few ? backward_of<T, G, 64, 2, 4>(a, groups, s) : backward_of<T, G, 64, 2, 16>(a, groups, s);
+            case 64 * 16 + 3: return few ? backward_of<T, G, 64, 3, 4>(a, groups, s) : backward_of<T, G, 64, 3, 16>(a, groups, s);
+            case 64 * 16 + 4: return few ? backward_of<T, G, 64, 4, 4>(a, groups, s) : backward_of<T, G, 64, 4, 12>(a, groups, s);
+            case 64 * 16 + 6: return few ? backward_of<T, G, 64, 6, 4>(a, groups, s) : backward_of<T, G, 64, 6, 8>(a, groups, s);
+            case 64 * 16 + 8: return few ? backward_of<T, G, 64, 8, 4>(a, groups, s) : backward_of<T, G, 64, 8, 8>(a, groups, s);
+            case 256 * 16 + 4: return few ? backward_of<T, G, 256, 4, 1>(a, groups, s) : backward_of<T, G, 256, 4, 3>(a, groups, s);
+            case 1024 * 16 + 2: return backward_of<T, G, 1024, 2, 1>(a, groups, s);
+            case 1024 * 16 + 3: return backward_of<T, G, 1024, 3, 1>(a, groups, s);
+            default: return backward_of<T, G, 1024, 4, 1>(a, groups, s);
         }
     }
     if (a.partial) {                                             // first: dx may be dy itself
         const int64_t each = (a.rows + groups - 1) / groups, col_groups = (a.cols + 2047) / 2048;
         *parts = (a.rows + each - 1) / each;
-        const hipError_t e = launch(norm_column_sums_kernel<T>, dim3((uint32_t)(col_groups * *parts)), dim3(256), s, a, each, (uint32_t)col_groups);
+        const hipError_t e = launch(norm_column_sums_kernel<T, G>, dim3((uint32_t)(col_groups * *parts)), dim3(256), s, a, each, (uint32_t)col_groups);
         if (e != hipSuccess) return e;
     }
-    return a.dx ? launch(norm_backward_long_rows_kernel<T>, dim3((uint32_t)a.rows), dim3(1024), s, a) : hipSuccess;
+    return a.dx ? launch(norm_backward_long_rows_kernel<T, G>, dim3((uint32_t)a.rows), dim3(1024), s, a) : hipSuccess;
 }
 bool norm_shape_ok(int64_t rows, int64_t cols) { return mx_shape_ok(rows, cols) && cols >= 1; }
 
@@ -697,6 +700,36 @@ hipError_t launch_layer_norm(const void* x, int32_t dtype, int64_t rows, int64_t
     return dtype == FH_F32 ? norm_any<float, false>(x, rows, cols, xs, n, to, s) : norm_any<Bf16, false>(x, rows, cols, xs, n, to, s);
 }
 
+fh_status norm_backward(const fh_norm_backward& b, int32_t dy_dtype, hipStream_t s)
+{
+    if (!is_dtype(b.dtype) || !is_dtype(b.p_dtype) || (dy_dtype != b.dtype && dy_dtype != FH_F32)) return FH_ERR_BAD_DTYPE;
+    if (!norm_shape_ok(b.rows, b.cols) || b.dy_stride < b.cols || b.x_stride < b.cols || b.dx_stride < b.cols ||
+        b.dy_stride > kMostStride || b.x_stride > kMostStride || b.dx_stride > kMostStride) return FH_ERR_BAD_SHAPE;
+    const bool sums = b.dweight || b.dbias;
+    if (b.rows > 0 && (!b.dy || !b.x || !b.mean || !b.rstd)) return FH_ERR_NULL;
+    const size_t size = dtype_size(b.dtype), p_size = dtype_size(b.p_dtype);
+    if (!is_aligned(b.dy, dtype_size(dy_dtype)) || !is_aligned(b.x, size) || !is_aligned(b.dx, size) || !is_aligned(b.weight, p_size) ||
+        !is_aligned(b.dweight, p_size) || !is_aligned(b.dbias, p_size) || !is_aligned(b.mean, 4) || !is_aligned(b.rstd, 4) ||
+        !is_aligned(b.workspace, 16)) return FH_ERR_ALIGNMENT;
+    if (b.dx && b.dx_cap < strided_elements(b.rows, b.cols, b.dx_stride) * size) return FH_ERR_BUFFER_TOO_SMALL;
+    if (sums && b.rows > 0) {
+        if (!b.workspace) return FH_ERR_NULL;
+        if (b.workspace_cap < fh_layer_norm_backward_workspace_bytes(b.rows, b.cols)) return FH_ERR_BUFFER_TOO_SMALL;
+    }
+    float* partial = sums ? static_cast<float*>(b.workspace) : nullptr;
+    int64_t parts = 0;
+    if (b.rows > 0 && (b.dx || sums)) {
+        const NormBackwardArgs a = {b.dy, b.x, static_cast<const float*>(b.mean), static_cast<const float*>(b.rstd), b.weight, b.dx, partial,
+                                    b.dy_stride, b.x_stride, b.dx_stride, b.rows, b.cols, b.p_dtype,
+                                    (int32_t)backward_groups(b.rows, b.cols)};
+        const hipError_t e = b.dtype == FH_F32 ? backward_any<float, float>(a, &parts, s)
+                           : dy_dtype == FH_F32 ? backward_any<Bf16, float>(a, &parts, s) : backward_any<Bf16, Bf16>(a, &parts, s);
+        if (e != hipSuccess) return FH_ERR_LAUNCH;
+    }
+    if (!sums) return FH_OK;                                     // no rows: sums of nothing, which are written all the same
+    return launch_join(partial, parts, b.cols, 2, b.p_dtype, b.dweight, b.dbias, s) == hipSuccess ? FH_OK : FH_ERR_LAUNCH;
+}
+
 }  // namespace fh
 
 extern "C" {
@@ -727,34 +760,7 @@ size_t fh_layer_norm_backward_workspace_bytes(int64_t rows, int64_t cols)
 
 fh_status fh_layer_norm_backward(const fh_norm_backward* b, void* stream)
 {
-    using namespace fh;
-    if (!b) return FH_ERR_NULL;
-    if (!is_dtype(b->dtype) || !is_dtype(b->p_dtype)) return FH_ERR_BAD_DTYPE;
-    if (!norm_shape_ok(b->rows, b->cols) || b->dy_stride < b->cols || b->x_stride < b->cols || b->dx_stride < b->cols ||
-        b->dy_stride > kMostStride || b->x_stride > kMostStride || b->dx_stride > kMostStride) return FH_ERR_BAD_SHAPE;
-    const bool sums = b->dweight || b->dbias;
-    if (b->rows > 0 && (!b->dy || !b->x || !b->mean || !b->rstd)) return FH_ERR_NULL;
-    const size_t size = dtype_size(b->dtype), p_size = dtype_size(b->p_dtype);
-    if (!is_aligned(b->dy, size) || !is_aligned(b->x, size) || !is_aligned(b->dx, size) || !is_aligned(b->weight, p_size) ||
-        !is_aligned(b->dweight, p_size) || !is_aligned(b->dbias, p_size) || !is_aligned(b->mean, 4) || !is_aligned(b->rstd, 4) ||
-        !is_aligned(b->workspace, 16)) return FH_ERR_ALIGNMENT;
-    if (b->dx && b->dx_cap < strided_elements(b->rows, b->cols, b->dx_stride) * size) return FH_ERR_BUFFER_TOO_SMALL;
-    if (sums && b->rows > 0) {
-        if (!b->workspace) return FH_ERR_NULL;
-        if (b->workspace_cap < fh_layer_norm_backward_workspace_bytes(b->rows, b->cols)) return FH_ERR_BUFFER_TOO_SMALL;
-    }
-    const hipStream_t s = static_cast<hipStream_t>(stream);
-    float* partial = sums ? static_cast<float*>(b->workspace) : nullptr;
-    int64_t parts = 0;
-    if (b->rows > 0 && (b->dx || sums)) {
-        const NormBackwardArgs a = {b->dy, b->x, static_cast<const float*>(b->mean), static_cast<const float*>(b->rstd), b->weight, b->dx, partial,
-                                    b->dy_stride, b->x_stride, b->dx_stride, b->rows, b->cols, b->p_dtype,
-                                    (int32_t)backward_groups(b->rows, b->cols)};
-        const hipError_t e = b->dtype == FH_F32 ? backward_any<float>(a, &parts, s) : backward_any<Bf16>(a, &parts, s);
-        if (e != hipSuccess) return FH_ERR_LAUNCH;
-    }
-    if (!sums) return FH_OK;                                     // no rows: sums of nothing, which are written all the same
-    return launch_join(partial, parts, b->cols, 2, b->p_dtype, b->dweight, b->dbias, s) == hipSuccess ? FH_OK : FH_ERR_LAUNCH;
+    return b ? fh::norm_backward(*b, b->dtype, static_cast<hipStream_t>(stream)) : FH_ERR_NULL;
 }
 
 }  // extern "C"

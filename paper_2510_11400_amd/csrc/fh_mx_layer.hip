@@ -12,9 +12,10 @@ inline size_t larger(size_t a, size_t b) { return a > b ? a : b; }
 struct Parts {
     size_t mean, rstd, x_columns, w_columns, kept;
     size_t x_rows, w_rows, forward_work, forward;
-    size_t dy_rows, dy_columns, backward_work, backward;
+    size_t dy_rows, dy_columns, dh, backward_work, backward;
 };
-Parts parts_of(int64_t tokens, int64_t features, int64_t out)
+// `wide`: with the gradient of a norm's output in binary32, in the place of dy's columns, which only the product before it reads.
+Parts parts_of(int64_t tokens, int64_t features, int64_t out, bool wide)
 {
     Parts p;
     p.mean = 0;
@@ -28,7 +29,8 @@ Parts parts_of(int64_t tokens, int64_t features, int64_t out)
     p.forward = p.forward_work + whole(fh_mx_matmul_workspace_bytes(tokens, out, features));
     p.dy_rows = 0;
     p.dy_columns = whole(mx_bytes(tokens, out));
-    p.backward_work = p.dy_columns + whole(mx_bytes(out, tokens));
+    p.dh = p.dy_columns;
+    p.backward_work = p.dy_columns + larger(whole(mx_bytes(out, tokens)), wide ? whole((size_t)tokens * (size_t)features * 4) : 0);
     p.backward = p.backward_work + whole(larger(larger(fh_mx_matmul_workspace_bytes(tokens, features, out), fh_mx_matmul_workspace_bytes(out, features, tokens)),
                                                 larger(fh_layer_norm_backward_workspace_bytes(tokens, features), (size_t)mx_tile_rows(tokens) * (size_t)out * 4)));
     return p;
@@ -48,10 +50,13 @@ fh_status check(const fh_mx_layer* l)
     if (!shape_ok(l->tokens, l->features, l->out_features) || l->x_stride < l->features || l->weight_stride < l->features ||
         l->dy_stride < l->out_features || l->x_stride > kMostStride || l->weight_stride > kMostStride || l->dy_stride > kMostStride)
         return FH_ERR_BAD_SHAPE;
-    if (l->norm != 0 && l->norm != 1) return FH_ERR_BAD_PARAM;
+    if ((l->norm != 0 && l->norm != 1) || (l->wide_gradient != 0 && l->wide_gradient != 1)) return FH_ERR_BAD_PARAM;
     if ((l->needs & ~(FH_MX_NEEDS_INPUT | FH_MX_NEEDS_WEIGHT)) != 0 || l->reserved != 0 || (l->norm && !(l->eps >= 0.0f))) return FH_ERR_BAD_PARAM;
     return FH_OK;
 }
+
+bool is_wide(const fh_mx_layer& l) { return l.wide_gradient && l.norm && (l.needs & FH_MX_NEEDS_INPUT) && l.dtype != FH_F32; }
+Parts parts_of(const fh_mx_layer& l) { return parts_of(l.tokens, l.features, l.out_features, is_wide(l)); }
 
 uint8_t* at(void* p, size_t offset) { return static_cast<uint8_t*>(p) + offset; }
 
@@ -62,14 +67,27 @@ extern "C" {
 
 size_t fh_mx_layer_kept_bytes(int64_t tokens, int64_t features, int64_t out_features)
 {
-    return fh::shape_ok(tokens, features, out_features) ? fh::parts_of(tokens, features, out_features).kept : 0;
+    return fh::shape_ok(tokens, features, out_features) ? fh::parts_of(tokens, features, out_features, false).kept : 0;
 }
 
 size_t fh_mx_layer_scratch_bytes(int64_t tokens, int64_t features, int64_t out_features)
 {
     if (!fh::shape_ok(tokens, features, out_features)) return 0;
-    const fh::Parts p = fh::parts_of(tokens, features, out_features);
+    const fh::Parts p = fh::parts_of(tokens, features, out_features, false);
     return fh::larger(p.forward, p.backward);
+}
+
+fh_status fh_mx_layer_sizes(const fh_mx_layer* l, size_t* kept, size_t* forward_scratch, size_t* backward_scratch)
+{
+    using namespace fh;
+    if (!kept || !forward_scratch || !backward_scratch) return FH_ERR_NULL;
+    const fh_status ok = check(l);
+    if (ok != FH_OK) return ok;
+    const Parts p = parts_of(*l);
+    *kept = p.kept;
+    *forward_scratch = p.forward;
+    *backward_scratch = p.backward;
+    return FH_OK;
 }
 
 fh_status fh_mx_layer_forward(const fh_mx_layer* l, void* stream)
@@ -77,7 +95,7 @@ fh_status fh_mx_layer_forward(const fh_mx_layer* l, void* stream)
     using namespace fh;
     const fh_status ok = check(l);
     if (ok != FH_OK || l->tokens == 0) return ok;
-    const Parts p = parts_of(l->tokens, l->features, l->out_features);
+    const Parts p = parts_of(*l);
     const size_t size = dtype_size(l->dtype), p_size = dtype_size(l->p_dtype);
     const bool keeps = l->norm || l->needs;
     if (!l->x || !l->weight || !l->y || !l->scratch || (keeps && !l->kept)) return FH_ERR_NULL;
@@ -113,10 +131,10 @@ fh_status fh_mx_layer_backward(const fh_mx_layer* l, void* stream)
     using namespace fh;
     const fh_status ok = check(l);
     if (ok != FH_OK || (!l->needs && !l->dbias)) return ok;
-    const Parts p = parts_of(l->tokens, l->features, l->out_features);
+    const Parts p = parts_of(*l);
     const size_t size = dtype_size(l->dtype), p_size = dtype_size(l->p_dtype);
     const bool input = l->needs & FH_MX_NEEDS_INPUT, weight = l->needs & FH_MX_NEEDS_WEIGHT;
-    if ((l->needs && !l->kept) || !l->scratch || (weight && !l->dweight)) return FH_ERR_NULL;
+    if ((l->needs && !l->kept) || (p.backward && !l->scratch) || (weight && !l->dweight)) return FH_ERR_NULL;
     if (l->tokens > 0 && (!l->dy || (input && !l->dx) || (input && l->norm && !l->x))) return FH_ERR_NULL;
     if (!is_aligned(l->x, size) || !is_aligned(l->dy, size) || !is_aligned(l->dx, size) || !is_aligned(l->dweight, p_size) ||
         !is_aligned(l->norm_weight, p_size) || !is_aligned(l->dnorm_weight, p_size) || !is_aligned(l->dnorm_bias, p_size) ||
@@ -147,15 +165,19 @@ fh_status fh_mx_layer_backward(const fh_mx_layer* l, void* stream)
         if ((s = fh_mx_matmul(&dw, stream)) != FH_OK) return s;
     }
     if (!input) return FH_OK;
-    // With a norm its output's gradient is rounded to dtype on the way, as between two layers of their own: in bf16 dx is then 0.0024 of its
-    // norm from the exact one instead of 0.0017, and 8192 x 768 values go through memory as 25 MB instead of 50.
-    const size_t dx_bytes = (size_t)l->tokens * (size_t)l->features * size;
+    // With a norm its output's gradient stays in binary32 on the way, or is rounded to dtype as between two layers of their own: in bf16 dx is then
+    // 0.0024 of its norm from the exact one instead of 0.0017, the norm's parameters have sums of rounded values for gradients, and 8192 x 768 values
+    // go through memory as 25 MB instead of 50 (a step of 8192 x 768 tokens to 2304: 97.5 and 102.3 us).
+    const bool wide = is_wide(*l);
+    const int32_t dh_dtype = wide ? FH_F32 : l->dtype;
+    void* dh = wide ? at(l->scratch, p.dh) : l->dx;
+    const size_t values = (size_t)l->tokens * (size_t)l->features;
     const fh_mx_product dx = {dy_rows, rows_bytes, at(l->kept, p.w_columns), mx_bytes(l->features, l->out_features), l->tokens, l->features,
-                              l->out_features, nullptr, l->p_dtype, l->dtype, l->dx, l->features, dx_bytes, work, work_bytes, 0};
+                              l->out_features, nullptr, l->p_dtype, dh_dtype, dh, l->features, values * dtype_size(dh_dtype), work, work_bytes, 0};
     if ((s = fh_mx_matmul(&dx, stream)) != FH_OK || !l->norm) return s;
-    const fh_norm_backward n = {l->dx, l->x, l->features, l->x_stride, at(l->kept, p.mean), at(l->kept, p.rstd), l->norm_weight, l->tokens, l->features,
-                                l->dtype, l->p_dtype, l->dx, l->features, dx_bytes, l->dnorm_weight, l->dnorm_bias, work, work_bytes};
-    return fh_layer_norm_backward(&n, stream);
+    const fh_norm_backward n = {dh, l->x, l->features, l->x_stride, at(l->kept, p.mean), at(l->kept, p.rstd), l->norm_weight, l->tokens, l->features,
+                                l->dtype, l->p_dtype, l->dx, l->features, values * size, l->dnorm_weight, l->dnorm_bias, work, work_bytes};
+    return norm_backward(n, dh_dtype, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

@@ -44,6 +44,9 @@ hipError_t launch_mx_tiles(const void* x, int32_t dtype, int64_t rows, int64_t c
 // first (k = 0) and second (k = 1), of p_dtype; either may be null.
 hipError_t launch_join(const float* partial, int64_t parts, int64_t cols, int32_t count, int32_t p_dtype, void* first, void* second, hipStream_t s);
 
+// fh_layer_norm_backward with a dy of its own type: b.dtype or FH_F32.
+fh_status norm_backward(const fh_norm_backward& b, int32_t dy_dtype, hipStream_t s);
+
 // The host's checks of a matrix in rows: `elements` from its pointer on are read or written.
 inline bool is_aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline bool is_dtype(int d) { return d == FH_F32 || d == FH_BF16; }

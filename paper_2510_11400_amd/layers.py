@@ -61,7 +61,8 @@ def layer_norm_mx_linear(x: torch.Tensor, norm_weight: Optional[torch.Tensor], n
                          bias: Optional[torch.Tensor] = None, eps: float = 1e-5, rounding="nearest", seed: int = 0,
                          tensor_id: int = 0) -> torch.Tensor:
     """mx_linear(layer_norm(x)) without the norm's output ever being written but as codes.  x is saved as autograd saves it
-    (hooks.SavedActivations compresses it); the product's operands are kept in 4-bit form.  The parameters are of one dtype."""
+    (hooks.SavedActivations compresses it); the product's operands are kept in 4-bit form.  The parameters are of one dtype.
+    Backward, the norm takes its output's gradient in fp32."""
     return _binding.mx_linear(x, norm_weight, norm_bias, weight, bias, eps, rounding, seed, tensor_id)
 
 

@@ -1,0 +1,70 @@
+"""Steps of the layers on the GPU: what precision, memory, streams and derivatives they keep to beside their values."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+import mx_reference as R
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def layers():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a visible MI355X")
+    from paper_2510_11400_amd import layers as _layers
+    return _layers
+
+
+@pytest.fixture(scope="module")
+def api(layers):
+    return layers.api
+
+
+def _randn(g, *shape, dtype=torch.bfloat16):
+    return torch.randn(*shape, generator=g, device="cuda").to(dtype)
+
+
+# ---- the gradient of a norm's output stays in fp32 -------------------------------------------------
+@pytest.mark.parametrize("tokens, features, out", [(1, 40, 7), (33, 100, 300), (300, 768, 64), (70, 2100, 33), (600, 1500, 40), (20, 5000, 40), (9, 17000, 40)])
+@pytest.mark.parametrize("params", [torch.bfloat16, torch.float32])
+def test_a_wide_gradient_is_not_rounded_ahead_of_the_norm(api, tokens, features, out, params):
+    """The backward half in bf16 with wide_gradient is the product in fp32 and the norm's backward pass of that in fp32, whose dx is
+    rounded at the end, bit for bit; where rows are whole and where a norm's kernels of every kind take them."""
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    x, dy = _randn(g, tokens, features + 3)[:, 1:1 + features], _randn(g, tokens, out)
+    w, b, nw, nb = (_randn(g, *s, dtype=params) for s in ((out, features), (out,), (features,), (features,)))
+    _, mean, rstd = api.fh_layer_norm_mx(x, nw, nb, 1e-4, "both")
+    dh = api.fh_mx_matmul(api.fh_mx_quantize(dy), api.fh_mx_quantize(w, "columns"), out_dtype=torch.float32)
+    dx, dnw, dnb = api.fh_layer_norm_backward(dh, x.float(), mean, rstd, nw.float())
+    narrow, layer = api.MxLayer(x, w, b, True, nw, nb, 1e-4), api.MxLayer(x, w, b, True, nw, nb, 1e-4, wide_gradient=True)
+    assert torch.equal(layer.forward(), narrow.forward())
+    got = layer.backward(dy, x, nw)
+    assert torch.equal(got[1], narrow.backward(dy, x, nw)[1])
+    layer.needs_weight = False
+    for got in (got, layer.backward(dy, x, nw)):
+        assert torch.equal(got[0], dx.bfloat16()) and torch.equal(got[2], dnw.to(params)) and torch.equal(got[3], dnb.to(params))
+
+
+@pytest.mark.parametrize("tokens, features, out", [(130, 300, 130), (512, 768, 260)])
+def test_the_steps_input_gradient_is_rounded_once(layers, tokens, features, out):
+    """dx of a bf16 step, value by value: the operands' codes are exact, the product is off by its sums' rounding (R.product's bound p), the norm's
+    backward pass by R.layer_norm_backward's with the kernel's own statistics; p passes through it as dx itself does, linear in its three terms.
+    Then one rounding to bf16, half a step of the value.  (A gradient rounded in between would add 2^-9 of itself on average, which where
+    the terms cancel is many steps of dx.)"""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x, dy, w, nw, nb = _randn(g, tokens, features), _randn(g, tokens, out), _randn(g, out, features), 1 + 0.2 * _randn(g, features), _randn(g, features)
+    leaf = x.clone().requires_grad_()
+    dx, = torch.autograd.grad(layers.layer_norm_mx_linear(leaf, nw, nb, w), leaf, dy)
+    _, mean, rstd = layers.api.fh_layer_norm_mx(x, nw, nb)
+    xm, gm, wm, weight, mean, rstd = (v.double().cpu().numpy() for v in (x, dy, w, nw, mean, rstd))
+    blocks = lambda v: R.restored(R.stored(v.astype(np.float32))[0], *v.shape)  # noqa: E731
+    dh, p = R.product(blocks(gm), blocks(wm.T))
+    want, _, _, bound, _, _ = R.layer_norm_backward(dh, xm, mean, rstd, weight)
+    h, pw = (xm - mean[:, None]) * rstd[:, None], p * np.abs(weight)
+    bound = bound + np.abs(rstd[:, None]) * (pw + pw.mean(1, keepdims=True) + np.abs(h) * (pw * np.abs(h)).mean(1, keepdims=True))
+    far = np.abs(dx.double().cpu().numpy() - want)
+    bad = np.argwhere(~(far <= bound + R.HALF_STEP["bf16"] * (np.abs(want) + bound)))
+    assert bad.size == 0, f"{len(bad)} of {want.size} off, first at {bad[0]}: {far[tuple(bad[0])]:.3g}"

@@ -1,0 +1,54 @@
+"""The linear layer's calls without a GPU: what they ask for and refuse ahead of any launch."""
+from __future__ import annotations
+
+import ctypes
+
+import pytest
+
+from paper_2510_11400_amd import api
+
+FAKE = 0x10000  # an aligned non-NULL address; never dereferenced because validation fails first
+LIB = api.raw_library()
+BF16 = 1
+
+
+def _layer(**change):
+    a = api.fh_mx_layer(tokens=100, features=300, out_features=70, dtype=BF16, p_dtype=0, norm=1, needs=3, rounding=0, eps=1e-5, x=FAKE, x_stride=300,
+                        norm_weight=FAKE, norm_bias=FAKE, weight=FAKE, weight_stride=300, bias=FAKE, y=FAKE, dy=FAKE, dy_stride=70, dx=FAKE, dweight=FAKE,
+                        dnorm_weight=FAKE, dnorm_bias=FAKE, kept=FAKE, kept_cap=1 << 40, scratch=FAKE, scratch_cap=1 << 40)
+    for name, v in change.items():
+        assert hasattr(a, name)
+        setattr(a, name, v)
+    return a
+
+
+def _sizes(**change):
+    """(status, kept, forward scratch, backward scratch)"""
+    out = [ctypes.c_size_t(0) for _ in range(3)]
+    a = _layer(**change)
+    return (LIB.fh_mx_layer_sizes(ctypes.byref(a), *(ctypes.byref(v) for v in out)), *(v.value for v in out))
+
+
+def test_a_wide_gradient_asks_for_room():
+    """The fp32 gradient lies in the scratch of the backward call, where there is one that would be rounded otherwise."""
+    status, kept, forward, backward = _sizes()
+    assert status == 0 and kept == LIB.fh_mx_layer_kept_bytes(100, 300, 70) and max(forward, backward) == LIB.fh_mx_layer_scratch_bytes(100, 300, 70)
+    status, kept2, forward2, wide = _sizes(wide_gradient=1)
+    assert (status, kept2, forward2) == (0, kept, forward) and wide >= api.mx_bytes(100, 70) + 4 * 100 * 300 and wide > backward
+    for change in (dict(norm=0), dict(needs=2), dict(dtype=0)):
+        assert _sizes(wide_gradient=1, **change)[3] == _sizes(**change)[3]
+    assert LIB.fh_mx_layer_backward(ctypes.byref(_layer(wide_gradient=1, scratch_cap=wide - 1)), None) == 7
+
+
+@pytest.mark.parametrize("change, status", [(dict(wide_gradient=2), 12), (dict(wide_gradient=-1), 12), (dict(tokens=-1), 11), (dict(dtype=7), 2), (dict(norm=3), 12)])
+def test_sizes_of_a_layer_that_is_refused(change, status):
+    assert _sizes(**change) == (status, 0, 0, 0)
+    for call in (LIB.fh_mx_layer_forward, LIB.fh_mx_layer_backward):
+        assert call(ctypes.byref(_layer(**change)), None) == status
+
+
+def test_sizes_want_somewhere_to_go():
+    one = ctypes.byref(ctypes.c_size_t(0))
+    a = ctypes.byref(_layer())
+    assert LIB.fh_mx_layer_sizes(None, one, one, one) == 1
+    assert LIB.fh_mx_layer_sizes(a, None, one, one) == 1 and LIB.fh_mx_layer_sizes(a, one, None, one) == 1 and LIB.fh_mx_layer_sizes(a, one, one, None) == 1
