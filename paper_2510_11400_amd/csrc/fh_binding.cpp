@@ -524,6 +524,8 @@ Backward backward_of(const Layer& layer, const Matrix& dy, const at::Tensor& x_a
             if (x.rows != l.tokens || x.cols != features || x.dtype != l.dtype) raise(PyExc_ValueError, "x must have the shape and the dtype of the forward call's");
             on_device(x.t, device, "x");
             l.x = x.data(); l.x_stride = x.stride;
+            if (norm_weight.defined() && norm_weight.scalar_type() != p_type)      // it is read as the parameters' type
+                raise(PyExc_TypeError, "norm_weight is of %s, the layer's parameters of %s", c10::toString(norm_weight.scalar_type()), c10::toString(p_type));
             l.norm_weight = vector(norm_weight, features, device, "norm_weight");
             b.dnorm = pair(features, p_type, device);
             l.dnorm_weight = b.dnorm.first.data_ptr(); l.dnorm_bias = b.dnorm.second.data_ptr();

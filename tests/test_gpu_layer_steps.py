@@ -68,3 +68,22 @@ def test_the_steps_input_gradient_is_rounded_once(layers, tokens, features, out)
     far = np.abs(dx.double().cpu().numpy() - want)
     bad = np.argwhere(~(far <= bound + R.HALF_STEP["bf16"] * (np.abs(want) + bound)))
     assert bad.size == 0, f"{len(bad)} of {want.size} off, first at {bad[0]}: {far[tuple(bad[0])]:.3g}"
+
+
+# ---- what the backward half is given again ------------------------------------------------------------
+@pytest.mark.parametrize("params, other", [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)])
+def test_the_norms_weight_has_to_be_of_the_parameters_dtype(layers, api, params, other):
+    """The kernel reads it by that dtype: twice its bytes where it is the narrower one, other numbers where it is the wider."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, dy = _randn(g, 64, 300), _randn(g, 64, 40)
+    w, nw = _randn(g, 40, 300, dtype=params), _randn(g, 300, dtype=params)
+    layer = api.MxLayer(x, w, norm=True, norm_weight=nw)
+    layer.forward()
+    with pytest.raises(TypeError, match="norm_weight"):
+        layer.backward(dy, x, nw.to(other))
+    assert layer.backward(dy, x, nw)[0].shape == x.shape
+    leaf = x.clone().requires_grad_()                                     # and where a saved-tensor hook gives it back
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: t.to(other) if t.shape == nw.shape else t):
+        y = layers.layer_norm_mx_linear(leaf, nw, None, w)
+    with pytest.raises(TypeError, match="norm_weight"):
+        y.sum().backward()
