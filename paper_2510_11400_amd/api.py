@@ -1391,14 +1391,14 @@ class MxLayer:
     are of one dtype, and so are x, y and the gradients of both.  The norm's backward pass takes its output's gradient rounded to
     that dtype, as from a layer of its own, with `wide_gradient` in fp32."""
     __slots__ = ("inputs", "kept", "shape", "dtype", "p_dtype", "features", "norm", "eps", "needs_input", "needs_weight", "rounding",
-                 "wide_gradient")
+                 "wide_gradient", "weighted")
 
     def __init__(self, x: torch.Tensor, weight: torch.Tensor, bias=None, norm: bool = False, norm_weight=None, norm_bias=None,
                  eps: float = 1e-5, needs_input: bool = True, needs_weight: bool = True, rounding="nearest", seed: int = 0,
                  tensor_id: int = 0, wide_gradient: bool = False):
         self.inputs, self.kept = (x, weight, bias, norm, norm_weight, norm_bias, eps, needs_input, needs_weight), None
         self.norm, self.eps, self.needs_input, self.needs_weight = norm, eps, needs_input, needs_weight
-        self.rounding, self.wide_gradient = (rounding, seed, tensor_id), wide_gradient
+        self.rounding, self.wide_gradient, self.weighted = (rounding, seed, tensor_id), wide_gradient, norm_weight is not None
         if rounding not in _ROUND:
             raise KeyError(rounding)
 
@@ -1416,6 +1416,8 @@ class MxLayer:
         was restored has)."""
         if dy.shape != self.shape or dy.dtype != self.dtype:
             raise ValueError("dy must have the shape and the dtype of y")
+        if self.norm and self.needs_input and (norm_weight is not None) != self.weighted:
+            raise ValueError("norm_weight must be given again" if self.weighted else "the forward call had no norm_weight")
         grads = _binding.layer_backward(dy, x, norm_weight, self.kept, self.features, self.p_dtype, self.norm, self.eps, self.needs_input,
                                         self.needs_weight, bias, *self.rounding, self.wide_gradient, stream)
         return grads if bias else grads[:4]

@@ -4,6 +4,7 @@ from __future__ import annotations
 import ctypes
 
 import pytest
+import torch
 
 from paper_2510_11400_amd import api
 
@@ -52,3 +53,16 @@ def test_sizes_want_somewhere_to_go():
     a = ctypes.byref(_layer())
     assert LIB.fh_mx_layer_sizes(None, one, one, one) == 1
     assert LIB.fh_mx_layer_sizes(a, None, one, one) == 1 and LIB.fh_mx_layer_sizes(a, one, None, one) == 1 and LIB.fh_mx_layer_sizes(a, one, one, None) == 1
+
+
+@pytest.mark.parametrize("before, again", [(True, False), (False, True)])
+def test_the_norms_weight_is_given_again(before, again):
+    """Left out, the gradients would be those of a weight of ones."""
+    x, w, nw = torch.zeros(4, 40), torch.zeros(7, 40), torch.ones(40)
+    layer = api.MxLayer(x, w, norm=True, norm_weight=nw if before else None)
+    layer.shape, layer.dtype = torch.Size((4, 7)), torch.float32                # as a forward call leaves them
+    layer.kept, layer.features, layer.p_dtype = None, 40, torch.float32
+    with pytest.raises(ValueError, match="norm_weight"):
+        layer.backward(torch.zeros(4, 7), x, nw if again else None)
+    with pytest.raises(ValueError, match="device memory"):                      # alike: on to the call itself, which wants device tensors
+        layer.backward(torch.zeros(4, 7), x, nw if before else None)
