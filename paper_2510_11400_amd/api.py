@@ -1312,6 +1312,8 @@ def fh_mix_decompress_batch(batch: MixBatch, stream=None) -> None:
 
 # ---- microscaled 4-bit storage, its product, layer norm ---------------------------------------------------
 # These kernels take a few us for small inputs, as long as Python takes to marshal a call: _fh_binding does it compiled.
+# With `stream` a call allocates as if that stream were the current one, so that results come from the memory that the stream itself has let go;
+# they are marked as in use on the current stream too.  Waiting for the inputs and for the results is the caller's part.
 _MOST = 2 ** 31 - 256
 
 

@@ -145,10 +145,9 @@ Matrix matrix_like(PyObject* o, const Matrix& x, const char* what)
     on_device(m.t, x.device(), what);
     return m;
 }
-// A caller's scratch buffer, or a new one of `need` bytes.  The allocator hands a freed block to the next allocation on the stream that it was
-// allocated on (the current one), so a buffer for a call on another stream is marked as in use there before it is dropped.
+// A caller's scratch buffer, or a new one of `need` bytes.
 struct Work { at::Tensor t; void* p = nullptr; size_t n = 0; };
-Work work(PyObject* given, size_t need, c10::Device device, PyObject* stream)
+Work work(PyObject* given, size_t need, c10::Device device)
 {
     Work w;
     w.t = tensor_or_none(given, "workspace");
@@ -158,7 +157,6 @@ Work work(PyObject* given, size_t need, c10::Device device, PyObject* stream)
         on_device(w.t, device, "workspace");
     } else if (need) {
         w.t = bytes(need, device);
-        if (stream != Py_None) Ref(PyObject_CallMethod(Ref(wrap(w.t)).p, "record_stream", "O", stream));
     } else {
         return w;
     }
@@ -206,6 +204,26 @@ bool truth(PyObject* o)
     if (v < 0) throw python_error();
     return v != 0;
 }
+
+// The stream of a call as the current one, for the time of the call: what is allocated belongs to that stream, is written after all that
+// the stream did with it before, and goes back to that stream's allocations, whether it is a workspace, what a layer keeps or
+// a result.  Results are read on the stream that was current as well, as a rule: they are marked as in use there (lent()).
+struct On {
+    std::optional<c10::hip::HIPStream> before;
+    On(PyObject* stream, c10::Device device)
+    {
+        if (stream == Py_None) return;
+        const hipStream_t given = reinterpret_cast<hipStream_t>(u64(attribute(stream, g_cuda_stream).p));
+        const c10::hip::HIPStream current = c10::hip::getCurrentHIPStream(device.index());
+        if (current.stream() == given) return;
+        c10::hip::setCurrentHIPStream(c10::hip::getStreamFromExternal(given, device.index()));
+        before = current;
+    }
+    On(const On&) = delete;
+    ~On() { if (before) c10::hip::setCurrentHIPStream(*before); }
+    void lent(const at::Tensor& t) const { if (before && t.defined()) t.record_stream(as_recorded(*before)); }
+    static c10::Stream as_recorded(const c10::hip::HIPStream& s) { return c10::Stream::unpack3(s.id(), s.device_index(), c10::DeviceType::CUDA); }
+};
 
 Ref wrapped_matrix(const at::Tensor& data, int64_t rows, int64_t cols)
 {
@@ -256,11 +274,9 @@ struct Outside {
     }
 };
 template <typename F>
-void enqueue(c10::Device device, PyObject* stream, F call)
+void enqueue(c10::Device device, F call)
 {
-    void* handle;
-    if (stream == Py_None) handle = c10::hip::getCurrentHIPStream(device.index()).stream();
-    else handle = reinterpret_cast<void*>(u64(attribute(stream, g_cuda_stream).p));
+    void* handle = c10::hip::getCurrentHIPStream(device.index()).stream();
     fh_status status;
     {
         const Outside outside(device.index());
@@ -296,6 +312,11 @@ struct Stores {
         if (f.rows) by_rows = bytes(fh_mx_bytes(r, c), device);
         if (f.columns) by_columns = bytes(fh_mx_bytes(c, r), device);
     }
+    void lent(const On& on) const
+    {
+        on.lent(by_rows);
+        on.lent(by_columns);
+    }
     static void* data(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
     static size_t size(const at::Tensor& t) { return t.defined() ? (size_t)t.numel() : 0; }
     Ref wrapped() const
@@ -325,8 +346,10 @@ FH_ENTRY(mx_quantize, 6)
     const Matrix x = matrix(a[0], "x");
     const int rounding = rounding_of(a[2]);
     const uint64_t seed = u64(a[3]), id = u64(a[4]);
+    const On on(a[5], x.device());
     const Stores s(f, x.rows, x.cols, x.device());
-    enqueue(x.device(), a[5], [&](void* stream) {
+    s.lent(on);
+    enqueue(x.device(), [&](void* stream) {
         return fh_mx_quantize(x.data(), (fh_dtype)x.dtype, x.rows, x.cols, x.stride, rounding, seed, id, s.data(s.by_rows), s.size(s.by_rows),
                               s.data(s.by_columns), s.size(s.by_columns), stream);
     });
@@ -337,11 +360,13 @@ FH_EXIT
 FH_ENTRY(mx_dequantize, 4)
     const Stored m = stored(a[0], "the stored matrix");
     const c10::Device device = m.data.device();
+    const On on(a[3], device);
     const Matrix out = a[2] == Py_None ? new_matrix(m.rows, m.cols, scalar_type(a[1]), device) : matrix(a[2], "out");
     if (out.rows != m.rows || out.cols != m.cols)
         raise(PyExc_ValueError, "out is %lld x %lld, the matrix %lld x %lld", (long long)out.rows, (long long)out.cols, (long long)m.rows, (long long)m.cols);
     on_device(out.t, device, "out");
-    enqueue(device, a[3], [&](void* stream) {
+    if (a[2] == Py_None) on.lent(out.t);
+    enqueue(device, [&](void* stream) {
         return fh_mx_dequantize(m.data.data_ptr(), (size_t)m.data.numel(), m.rows, m.cols, (fh_dtype)out.dtype, out.data(), out.stride, out.bytes(), stream);
     });
     return wrap(out.t);
@@ -354,15 +379,17 @@ FH_ENTRY(mx_matmul, 7)
     const c10::Device device = x.data.device();
     if (x.cols != y.cols) raise(PyExc_ValueError, "a has %lld columns, b %lld", (long long)x.cols, (long long)y.cols);
     on_device(y.data, device, "b");
+    const On on(a[6], device);
     const Matrix out = a[4] == Py_None ? new_matrix(x.rows, y.rows, scalar_type(a[3]), device) : matrix(a[4], "out");
     if (out.rows != x.rows || out.cols != y.rows)
         raise(PyExc_ValueError, "out is %lld x %lld, the product %lld x %lld", (long long)out.rows, (long long)out.cols, (long long)x.rows, (long long)y.rows);
     on_device(out.t, device, "out");
-    const Work w = work(a[5], fh_mx_matmul_workspace_bytes(x.rows, y.rows, x.cols), device, a[6]);
+    if (a[4] == Py_None) on.lent(out.t);
+    const Work w = work(a[5], fh_mx_matmul_workspace_bytes(x.rows, y.rows, x.cols), device);
     const fh_mx_product p = {x.data.data_ptr(), (size_t)x.data.numel(), y.data.data_ptr(), (size_t)y.data.numel(), x.rows, y.rows, x.cols,
                              vector(bias, y.rows, device, "bias"), bias.defined() ? dtype_code(bias.scalar_type()) : FH_F32, out.dtype, out.data(),
                              out.stride, out.bytes(), w.p, w.n, 0};
-    enqueue(device, a[6], [&](void* stream) { return fh_mx_matmul(&p, stream); });
+    enqueue(device, [&](void* stream) { return fh_mx_matmul(&p, stream); });
     return wrap(out.t);
 FH_EXIT
 
@@ -386,9 +413,12 @@ FH_ENTRY(layer_norm, 6)
     const Matrix x = matrix(a[0], "x");
     const Parameters p(a[1], a[2], x.cols, x.device());
     const float eps = (float)f64(a[3]);
+    const On on(a[5], x.device());
     const Matrix y = matrix_like(a[4], x, "out");
     const Pair stats = pair(x.rows, at::kFloat, x.device());
-    enqueue(x.device(), a[5], [&](void* stream) {
+    if (a[4] == Py_None) on.lent(y.t);
+    on.lent(stats.first);
+    enqueue(x.device(), [&](void* stream) {
         return fh_layer_norm(x.data(), (fh_dtype)x.dtype, x.rows, x.cols, x.stride, p.w, p.b, (fh_dtype)p.dtype, eps, y.data(), y.stride, y.bytes(),
                              stats.first.data_ptr(), stats.second.data_ptr(), stream);
     });
@@ -403,9 +433,12 @@ FH_ENTRY(layer_norm_mx, 9)
     const Forms f = forms_of(a[4]);
     const int rounding = rounding_of(a[5]);
     const uint64_t seed = u64(a[6]), id = u64(a[7]);
+    const On on(a[8], x.device());
     const Stores s(f, x.rows, x.cols, x.device());
     const Pair stats = pair(x.rows, at::kFloat, x.device());
-    enqueue(x.device(), a[8], [&](void* stream) {
+    s.lent(on);
+    on.lent(stats.first);
+    enqueue(x.device(), [&](void* stream) {
         return fh_layer_norm_mx(x.data(), (fh_dtype)x.dtype, x.rows, x.cols, x.stride, p.w, p.b, (fh_dtype)p.dtype, eps, rounding, seed, id,
                                 s.data(s.by_rows), s.size(s.by_rows), s.data(s.by_columns), s.size(s.by_columns), stats.first.data_ptr(), stats.second.data_ptr(), stream);
     });
@@ -422,18 +455,21 @@ FH_ENTRY(layer_norm_backward, 9)
     if (mean.scalar_type() != at::kFloat || rstd.scalar_type() != at::kFloat) raise(PyExc_TypeError, "mean and rstd must be float32");
     void *mean_at = vector(mean, x.rows, device, "mean"), *rstd_at = vector(rstd, x.rows, device, "rstd"), *weight_at = vector(weight, x.cols, device, "weight");
     const bool sums = truth(a[5]);
+    const On on(a[8], device);
     const Matrix dx = matrix_like(a[6], x, "dx");
+    if (a[6] == Py_None) on.lent(dx.t);
     const at::ScalarType type = weight.defined() ? weight.scalar_type() : x.t.scalar_type();
     const int p_dtype = dtype_code(type);
     Pair sum;
     Work w;
     if (sums) {
         sum = pair(x.cols, type, device);
-        w = work(a[7], fh_layer_norm_backward_workspace_bytes(x.rows, x.cols), device, a[8]);
+        on.lent(sum.first);
+        w = work(a[7], fh_layer_norm_backward_workspace_bytes(x.rows, x.cols), device);
     }
     const fh_norm_backward b = {dy.data(), x.data(), dy.stride, x.stride, mean_at, rstd_at, weight_at, x.rows, x.cols, x.dtype, p_dtype, dx.data(), dx.stride,
                                 dx.bytes(), sums ? sum.first.data_ptr() : nullptr, sums ? sum.second.data_ptr() : nullptr, w.p, w.n};
-    enqueue(device, a[8], [&](void* stream) { return fh_layer_norm_backward(&b, stream); });
+    enqueue(device, [&](void* stream) { return fh_layer_norm_backward(&b, stream); });
     return tuple(Ref(wrap(dx.t)), Ref(wrap(sum.first)), Ref(wrap(sum.second)));
 FH_EXIT
 
@@ -455,8 +491,7 @@ Sizes sizes_of(const fh_mx_layer& l)                                      // of 
 }
 
 struct Forward { at::Tensor y, kept; };
-Forward forward_of(const Layer& layer, const Matrix& x, const Matrix& weight, const at::Tensor& bias, const at::Tensor& norm_weight, const at::Tensor& norm_bias,
-                   PyObject* stream)
+Forward forward_of(const Layer& layer, const Matrix& x, const Matrix& weight, const at::Tensor& bias, const at::Tensor& norm_weight, const at::Tensor& norm_bias)
 {
     const c10::Device device = x.device();
     if (weight.cols != x.cols) raise(PyExc_ValueError, "x has %lld features, weight takes %lld", (long long)x.cols, (long long)weight.cols);
@@ -481,15 +516,15 @@ Forward forward_of(const Layer& layer, const Matrix& x, const Matrix& weight, co
         f.kept = bytes(sizes.kept, device);
         l.kept = f.kept.data_ptr(); l.kept_cap = (size_t)f.kept.numel();
     }
-    const Work w = work(Py_None, sizes.forward, device, stream);
+    const Work w = work(Py_None, sizes.forward, device);
     l.scratch = w.p; l.scratch_cap = w.n;
-    enqueue(device, stream, [&](void* s) { return fh_mx_layer_forward(&l, s); });
+    enqueue(device, [&](void* s) { return fh_mx_layer_forward(&l, s); });
     return f;
 }
 
 struct Backward { at::Tensor dx, dweight, dbias; Pair dnorm; };
 Backward backward_of(const Layer& layer, const Matrix& dy, const at::Tensor& x_again, const at::Tensor& norm_weight, const at::Tensor& kept, int64_t features,
-                     at::ScalarType p_type, PyObject* stream)
+                     at::ScalarType p_type)
 {
     const c10::Device device = dy.device();
     if (kept.defined()) {
@@ -531,17 +566,19 @@ Backward backward_of(const Layer& layer, const Matrix& dy, const at::Tensor& x_a
             l.dnorm_weight = b.dnorm.first.data_ptr(); l.dnorm_bias = b.dnorm.second.data_ptr();
         }
     }
-    const Work w = work(Py_None, sizes_of(l).backward, device, stream);
+    const Work w = work(Py_None, sizes_of(l).backward, device);
     l.scratch = w.p; l.scratch_cap = w.n;
-    enqueue(device, stream, [&](void* s) { return fh_mx_layer_backward(&l, s); });
+    enqueue(device, [&](void* s) { return fh_mx_layer_backward(&l, s); });
     return b;
 }
 
 // (x, weight, bias, norm, norm_weight, norm_bias, eps, needs_input, needs_weight, stream) -> (y, kept)
 FH_ENTRY(layer_forward, 10)
     const Layer layer = {truth(a[3]), (float)f64(a[6]), truth(a[7]), truth(a[8]), false, FH_ROUND_NEAREST, 0, 0, false};
-    const Forward f = forward_of(layer, matrix(a[0], "x"), matrix(a[1], "weight"), tensor_or_none(a[2], "bias"), tensor_or_none(a[4], "norm_weight"),
-                                 tensor_or_none(a[5], "norm_bias"), a[9]);
+    const Matrix x = matrix(a[0], "x");
+    const On on(a[9], x.device());
+    const Forward f = forward_of(layer, x, matrix(a[1], "weight"), tensor_or_none(a[2], "bias"), tensor_or_none(a[4], "norm_weight"), tensor_or_none(a[5], "norm_bias"));
+    on.lent(f.y);
     return tuple(Ref(wrap(f.y)), Ref(wrap(f.kept)));
 FH_EXIT
 
@@ -549,8 +586,13 @@ FH_EXIT
 //  stream) -> (dx, dweight, dnorm_weight, dnorm_bias, dbias)
 FH_ENTRY(layer_backward, 16)
     const Layer layer = {truth(a[6]), (float)f64(a[7]), truth(a[8]), truth(a[9]), truth(a[10]), rounding_of(a[11]), u64(a[12]), u64(a[13]), truth(a[14])};
-    const Backward b = backward_of(layer, matrix(a[0], "dy"), tensor_or_none(a[1], "x"), tensor_or_none(a[2], "norm_weight"), tensor_or_none(a[3], "kept"), i64(a[4]),
-                                   scalar_type(a[5]), a[15]);
+    const Matrix dy = matrix(a[0], "dy");
+    const at::Tensor kept = tensor_or_none(a[3], "kept");
+    const On on(a[15], dy.device());
+    const Backward b = backward_of(layer, dy, tensor_or_none(a[1], "x"), tensor_or_none(a[2], "norm_weight"), kept, i64(a[4]), scalar_type(a[5]));
+    // it is of the stream that the forward call went through, and may be dropped before this one is through with it
+    if (kept.defined()) kept.record_stream(On::as_recorded(c10::hip::getCurrentHIPStream(dy.device().index())));
+    for (const at::Tensor* t : {&b.dx, &b.dweight, &b.dnorm.first, &b.dbias}) on.lent(*t);
     return tuple(Ref(wrap(b.dx)), Ref(wrap(b.dweight)), Ref(wrap(b.dnorm.first)), Ref(wrap(b.dnorm.second)), Ref(wrap(b.dbias)));
 FH_EXIT
 
@@ -587,7 +629,7 @@ struct Linear : torch::autograd::Function<Linear> {
     {
         const at::Tensor m = rows_of(x);
         Forward f = forward_of(pass->layer, matrix(m, "x"), matrix(weight, "weight"), bias.value_or(at::Tensor()), norm_weight.value_or(at::Tensor()),
-                               norm_bias.value_or(at::Tensor()), Py_None);
+                               norm_bias.value_or(at::Tensor()));
         pass->kept = std::move(f.kept);
         pass->features = m.size(1);
         if (pass->layer.norm && pass->layer.input) ctx->save_for_backward({m, norm_weight.value_or(at::Tensor())});
@@ -604,7 +646,7 @@ struct Linear : torch::autograd::Function<Linear> {
             const at::Tensor dy = rows_of(given[0]);
             const auto saved = ctx->get_saved_variables();
             const Backward b = backward_of(pass->layer, matrix(dy, "dy"), saved.empty() ? at::Tensor() : saved[0], saved.empty() ? at::Tensor() : saved[1],
-                                           pass->kept, pass->features, pass->p_type, Py_None);
+                                           pass->kept, pass->features, pass->p_type);
             if (pass->x) grads[0] = b.dx.view(pass->shape);
             if (pass->norm_weight) grads[1] = b.dnorm.first;
             if (pass->norm_bias) grads[2] = b.dnorm.second;
@@ -637,7 +679,7 @@ FH_ENTRY(mx_linear, 9)
         const auto some = [](const at::Tensor& t) { return t.defined() ? std::optional<at::Tensor>(t) : std::nullopt; };
         y = Linear::apply(x, some(norm_weight), some(norm_bias), weight, some(bias), pass);
     } else {
-        y = shaped(forward_of(pass->layer, matrix(rows_of(x), "x"), matrix(weight, "weight"), bias, norm_weight, norm_bias, Py_None).y, x);
+        y = shaped(forward_of(pass->layer, matrix(rows_of(x), "x"), matrix(weight, "weight"), bias, norm_weight, norm_bias).y, x);
     }
     return wrap(y);
 FH_EXIT

@@ -87,3 +87,140 @@ def test_the_norms_weight_has_to_be_of_the_parameters_dtype(layers, api, params,
         y = layers.layer_norm_mx_linear(leaf, nw, None, w)
     with pytest.raises(TypeError, match="norm_weight"):
         y.sum().backward()
+
+
+# ---- streams: whose memory a call takes, shown by addresses, never by what a race would leave -----------
+def _busy(stream):
+    """Some ten milliseconds of nothing on `stream`."""
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(20_000_000)
+
+
+def _calls(api, g):
+    """{name: call(stream) -> its results}, of inputs that every stream may read"""
+    x, dy, nw = _randn(g, 608, 704), _randn(g, 608, 704), _randn(g, 704)
+    long_a = api.fh_mx_quantize(_randn(g, 96, 40000))
+    m = api.fh_mx_quantize(x)
+    y, mean, rstd = api.fh_layer_norm(x, nw)
+    assert api.mx_matmul_workspace_bytes(96, 96, 40000) > 0
+    return {
+        "quantize": lambda s: [q.data for q in api.fh_mx_quantize(x, "both", stream=s)],
+        "dequantize": lambda s: [api.fh_mx_dequantize(m, stream=s)],
+        "matmul": lambda s: [api.fh_mx_matmul(long_a, long_a, stream=s)],
+        "layer_norm": lambda s: list(api.fh_layer_norm(x, nw, stream=s)),
+        "layer_norm_mx": lambda s: [(r := api.fh_layer_norm_mx(x, nw, stream=s))[0].data, *r[1:]],
+        "layer_norm_backward": lambda s: list(api.fh_layer_norm_backward(dy, x, mean, rstd, nw, stream=s)),
+    }
+
+
+def _spans(tensors):
+    return [(t.untyped_storage().data_ptr(), t.untyped_storage().data_ptr() + t.untyped_storage().nbytes()) for t in tensors]
+
+
+def _apart(a, b):
+    return all(p[1] <= q[0] or q[1] <= p[0] for p in a for q in b)
+
+
+def _blocks_like(tensors):
+    """Blocks of the same sizes, from the current stream's memory."""
+    return [torch.empty(t.untyped_storage().nbytes(), dtype=torch.uint8, device="cuda") for t in tensors]
+
+
+CALLS = ["quantize", "dequantize", "matmul", "layer_norm", "layer_norm_mx", "layer_norm_backward"]
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_results_on_another_stream_take_its_memory(api, name):
+    """Not blocks that the current stream has just let go and may still read; nor does the current stream get blocks of theirs while the other
+    one works; and they stay where they are while the current stream still reads them."""
+    call = _calls(api, torch.Generator(device="cuda").manual_seed(2))[name]
+    want = [t.clone() for t in call(None)]
+    torch.cuda.synchronize()
+    here, side = torch.cuda.current_stream(), torch.cuda.Stream()
+    freed = _blocks_like(want)
+    spans = _spans(freed)
+    del freed
+    got = call(side)
+    assert _apart(_spans(got), spans)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+    _busy(side)
+    got = call(side)
+    theirs = _spans(got)
+    del got
+    mine = _blocks_like(want)
+    assert _apart(_spans(mine), theirs)
+    torch.cuda.synchronize()
+    del mine
+
+    got = call(side)
+    side.synchronize()
+    _busy(here)
+    read = [t.clone() for t in got]                              # behind the current stream's other work
+    theirs = _spans(got)
+    del got
+    again = call(side)
+    assert _apart(_spans(again), theirs)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(read, want))
+
+
+def test_a_workspace_on_another_stream(api):
+    """A product whose sum is split, with the current stream's allocations behind it."""
+    call = _calls(api, torch.Generator(device="cuda").manual_seed(3))["matmul"]
+    want = call(None)[0].clone()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = call(side)[0]
+        for k in range(4):
+            torch.empty(api.mx_matmul_workspace_bytes(96, 96, 40000), dtype=torch.uint8, device="cuda").fill_(k)
+        side.synchronize()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+
+
+def test_what_a_layer_keeps_stays_until_its_stream_is_through(api):
+    """A layer dropped behind its backward half on another stream than its forward half's, or on the same: its operands' memory is nobody's
+    until that half has run."""
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x, dy, w = _randn(g, 600, 700), _randn(g, 600, 96), _randn(g, 96, 700)
+    first = api.MxLayer(x, w)
+    first.forward()
+    want = first.backward(dy)[:2]
+    torch.cuda.synchronize()
+    here, one, two = torch.cuda.current_stream(), torch.cuda.Stream(), torch.cuda.Stream()
+    for forward, backward in ((None, one), (one, one), (one, two), (one, None)):
+        layer = api.MxLayer(x, w)
+        layer.forward(stream=forward)
+        torch.cuda.synchronize()
+        _busy(backward or here)
+        got = layer.backward(dy, stream=backward)[:2]
+        kept = [layer.kept]
+        size, theirs = kept[0].numel(), _spans(kept)
+        del layer, kept
+        blocks = []
+        for stream in (here, one, two):
+            if stream is (backward or here) and stream is (forward or here):
+                continue                                         # its own next allocation comes behind that half anyway
+            with torch.cuda.stream(stream):
+                blocks.append(torch.empty(size, dtype=torch.uint8, device="cuda"))
+        assert _apart(_spans(blocks), theirs), (forward, backward)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_stream_that_is_the_current_one_changes_nothing(api):
+    call = _calls(api, torch.Generator(device="cuda").manual_seed(2))["quantize"]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        got, want = call(side), call(None)
+    assert torch.cuda.current_stream() != side
+    with pytest.raises(ValueError):
+        api.fh_mx_matmul(api.fh_mx_quantize(torch.zeros(4, 40, device="cuda")), api.fh_mx_quantize(torch.zeros(4, 40, device="cuda")),
+                         bias=torch.zeros(3, device="cuda"), stream=side)
+    assert torch.cuda.current_stream() == torch.cuda.default_stream()     # also behind a refusal
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
