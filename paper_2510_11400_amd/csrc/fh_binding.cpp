@@ -660,10 +660,26 @@ struct Linear : torch::autograd::Function<Linear> {
     }
 };
 
+// Forward-mode derivatives: a tangent that went no further would be read as a derivative of zero.
+void no_tangent(const at::Tensor& t, const char* what)
+{
+    if (t.defined() && t._fw_grad(/*level=*/0).defined()) raise(PyExc_NotImplementedError, "%s carries a tangent; the microscaled layers have no forward-mode derivative", what);
+}
+
+// (tensors): refused where one carries a tangent
+PyObject* refuse_tangents(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    for (Py_ssize_t i = 0; i < n; ++i) no_tangent(tensor_or_none(a[i], "x"), "an input");
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
 // (x, norm_weight, norm_bias, weight, bias, eps or None where there is no norm, rounding, seed, tensor_id) -> y
 FH_ENTRY(mx_linear, 9)
     const at::Tensor x = tensor(a[0], "x"), norm_weight = tensor_or_none(a[1], "norm_weight"), norm_bias = tensor_or_none(a[2], "norm_bias"),
                      weight = tensor(a[3], "weight"), bias = tensor_or_none(a[4], "bias");
+    no_tangent(x, "x"); no_tangent(norm_weight, "norm_weight"); no_tangent(norm_bias, "norm_bias"); no_tangent(weight, "weight"); no_tangent(bias, "bias");
     in_device_memory(x, "x");
     if (x.dim() == 0) raise(PyExc_ValueError, "x must have a dimension");
     const auto pass = c10::make_intrusive<Pass>();
@@ -693,7 +709,7 @@ FH_EXIT
 
 #define FH_METHOD(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {FH_METHOD(mx_quantize), FH_METHOD(mx_dequantize), FH_METHOD(mx_matmul), FH_METHOD(layer_norm), FH_METHOD(layer_norm_mx),
-                           FH_METHOD(layer_norm_backward), FH_METHOD(layer_forward), FH_METHOD(layer_backward), FH_METHOD(mx_linear),
+                           FH_METHOD(layer_norm_backward), FH_METHOD(layer_forward), FH_METHOD(layer_backward), FH_METHOD(mx_linear), FH_METHOD(refuse_tangents),
                            FH_METHOD(use), {}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_fh_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -94,7 +94,7 @@ class LayerNormMxLinear(torch.nn.Module):
         self._stored: Optional[api.MxMatrix] = None
 
     def freeze(self) -> "LayerNormMxLinear":
-        """Store the weights in 4-bit blocks; from here on forward() uses these and gives no gradients.  Call it again after
+        """Store the weights in 4-bit blocks; from here on forward() uses these and gives no gradients (tangents are refused).  Call it again after
         the weights have changed, `thaw()` to train on."""
         self._stored = api.fh_mx_quantize(self.linear.weight.detach(), "rows")
         return self
@@ -108,7 +108,9 @@ class LayerNormMxLinear(torch.nn.Module):
             seed, self.steps = self.seed + self.steps, self.steps + 1
             return layer_norm_mx_linear(x, self.norm.weight, self.norm.bias, self.linear.weight, self.linear.bias, self.norm.eps,
                                         self.rounding, seed, self.tensor_id)
+        norm_weight, norm_bias, bias = self.norm.weight, self.norm.bias, self.linear.bias
+        _binding.refuse_tangents(x, norm_weight, norm_bias, bias)
         with torch.no_grad():
-            h, _, _ = api.fh_layer_norm_mx(_rows(x), self.norm.weight, self.norm.bias, self.norm.eps, "rows")
-            y = api.fh_mx_matmul(h, self._stored, self.linear.bias, x.dtype)
+            h, _, _ = api.fh_layer_norm_mx(_rows(x), norm_weight, norm_bias, self.norm.eps, "rows")
+            y = api.fh_mx_matmul(h, self._stored, bias, x.dtype)
         return y.view(*x.shape[:-1], self._stored.rows)

@@ -6,7 +6,7 @@ import ctypes
 import pytest
 import torch
 
-from paper_2510_11400_amd import api
+from paper_2510_11400_amd import api, layers
 
 FAKE = 0x10000  # an aligned non-NULL address; never dereferenced because validation fails first
 LIB = api.raw_library()
@@ -66,3 +66,25 @@ def test_the_norms_weight_is_given_again(before, again):
         layer.backward(torch.zeros(4, 7), x, nw if again else None)
     with pytest.raises(ValueError, match="device memory"):                      # alike: on to the call itself, which wants device tensors
         layer.backward(torch.zeros(4, 7), x, nw if before else None)
+
+
+@pytest.mark.parametrize("which", range(5))
+def test_tangents_are_refused(which):
+    """A tensor with a tangent requires no gradient, and the kernels know nothing of it: y without one would be a derivative of zero."""
+    tensors = [torch.randn(s) for s in ((6, 40), (40,), (40,), (7, 40), (7,))]
+    with torch.autograd.forward_ad.dual_level():
+        dual = [torch.autograd.forward_ad.make_dual(t, torch.ones_like(t)) if i == which else t for i, t in enumerate(tensors)]
+        with pytest.raises(NotImplementedError, match="tangent"):
+            layers.layer_norm_mx_linear(*dual)
+        if which in (0, 3, 4):
+            with pytest.raises(NotImplementedError, match="tangent"):
+                layers.mx_linear(dual[0], dual[3], dual[4])
+        frozen = layers.LayerNormMxLinear(40, 7)
+        frozen._stored = api.MxMatrix(torch.zeros(api.mx_bytes(7, 40), dtype=torch.uint8), 7, 40)
+        if which == 0:
+            with pytest.raises(NotImplementedError, match="tangent"):
+                frozen(dual[0])
+    with pytest.raises(ValueError, match="device memory"):       # without one: on to the call itself, which wants device tensors
+        layers.layer_norm_mx_linear(*tensors)
+    with pytest.raises(ValueError, match="device memory"):
+        frozen(tensors[0])
