@@ -530,6 +530,7 @@ Backward backward_of(const Layer& layer, const Matrix& dy, const at::Tensor& x_a
     if (kept.defined()) {
         in_device_memory(kept, "kept");
         on_device(kept, device, "kept");
+        if (kept.scalar_type() != at::kByte || !kept.is_contiguous()) raise(PyExc_ValueError, "what the forward call kept has changed");
     }
     const at::ScalarType type = dy.t.scalar_type();
     fh_mx_layer l = {};
@@ -616,7 +617,6 @@ at::Tensor shaped(const at::Tensor& y, const at::Tensor& x)
 struct Pass : torch::CustomClassHolder {                                  // from one half to the other, but for what is saved as a variable
     Layer layer;
     bool x, norm_weight, norm_bias;                                       // whose gradients are wanted, beside the layer's
-    at::Tensor kept;
     std::vector<int64_t> shape;
     int64_t features;
     at::ScalarType p_type;
@@ -628,11 +628,13 @@ struct Linear : torch::autograd::Function<Linear> {
                               const at::Tensor& weight, const std::optional<at::Tensor>& bias, const c10::intrusive_ptr<Pass>& pass)
     {
         const at::Tensor m = rows_of(x);
-        Forward f = forward_of(pass->layer, matrix(m, "x"), matrix(weight, "weight"), bias.value_or(at::Tensor()), norm_weight.value_or(at::Tensor()),
+        const Forward f = forward_of(pass->layer, matrix(m, "x"), matrix(weight, "weight"), bias.value_or(at::Tensor()), norm_weight.value_or(at::Tensor()),
                                norm_bias.value_or(at::Tensor()));
-        pass->kept = std::move(f.kept);
         pass->features = m.size(1);
-        if (pass->layer.norm && pass->layer.input) ctx->save_for_backward({m, norm_weight.value_or(at::Tensor())});
+        // Saved as variables are, so that the backward pass frees what was kept and checkpointing drops it; one row of bytes, which hooks for
+        // activations leave as it is.
+        if (f.kept.defined() && pass->layer.norm && pass->layer.input) ctx->save_for_backward({f.kept.unsqueeze(0), m, norm_weight.value_or(at::Tensor())});
+        else if (f.kept.defined()) ctx->save_for_backward({f.kept.unsqueeze(0)});
         ctx->saved_data.emplace("pass", c10::IValue::make_capsule(pass));
         return shaped(f.y, x);
     }
@@ -645,8 +647,8 @@ struct Linear : torch::autograd::Function<Linear> {
             const at::AutoGradMode off(false);
             const at::Tensor dy = rows_of(given[0]);
             const auto saved = ctx->get_saved_variables();
-            const Backward b = backward_of(pass->layer, matrix(dy, "dy"), saved.empty() ? at::Tensor() : saved[0], saved.empty() ? at::Tensor() : saved[1],
-                                           pass->kept, pass->features, pass->p_type);
+            const auto from = [&](size_t i) { return i < saved.size() ? saved[i] : at::Tensor(); };
+            const Backward b = backward_of(pass->layer, matrix(dy, "dy"), from(1), from(2), from(0), pass->features, pass->p_type);
             if (pass->x) grads[0] = b.dx.view(pass->shape);
             if (pass->norm_weight) grads[1] = b.dnorm.first;
             if (pass->norm_bias) grads[2] = b.dnorm.second;

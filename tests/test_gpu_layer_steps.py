@@ -224,3 +224,63 @@ def test_a_stream_that_is_the_current_one_changes_nothing(api):
     assert torch.cuda.current_stream() == torch.cuda.default_stream()     # also behind a refusal
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+# ---- what is kept for the backward pass goes with it ------------------------------------------------------
+def _held(then):
+    """Bytes that `then` leaves allocated, and its result."""
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    result = then()
+    return torch.cuda.memory_allocated() - before, result
+
+
+@pytest.mark.parametrize("norm", [False, True])
+def test_the_backward_pass_frees_what_was_kept(layers, api, norm):
+    """Also where the graph outlives it: the output is still there, as a loss is through the next step's forward pass.  Of the step only
+    the output and the gradients are left, each in blocks of 512 bytes."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, w, dy = _randn(g, 2048, 768).requires_grad_(), _randn(g, 768, 768).requires_grad_(), _randn(g, 2048, 768)
+    operands = api.mx_bytes(768, 2048) + api.mx_bytes(768, 768)
+    held, y = _held(lambda: layers.layer_norm_mx_linear(x, None, None, w) if norm else layers.mx_linear(x, w))
+    assert held >= y.nbytes + operands
+    left, grads = _held(lambda: torch.autograd.grad(y, (x, w), dy))
+    assert held + left < y.nbytes + sum(v.nbytes for v in grads) + 16384
+    with pytest.raises(RuntimeError, match="second time"):
+        torch.autograd.grad(y, (x, w), dy)
+
+
+def test_a_retained_graph_keeps_it(layers):
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, w, dy = _randn(g, 100, 300).requires_grad_(), _randn(g, 40, 300).requires_grad_(), _randn(g, 100, 40)
+    y = layers.layer_norm_mx_linear(x, None, None, w)
+    first = torch.autograd.grad(y, (x, w), dy, retain_graph=True)
+    assert all(torch.equal(a, b) for a, b in zip(first, torch.autograd.grad(y, (x, w), dy)))
+
+
+def test_checkpointing_keeps_nothing(layers, api):
+    """Recomputed in the backward pass, the operands are not held in between; the gradients are the same."""
+    from torch.utils.checkpoint import checkpoint
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, w, dy = _randn(g, 2048, 768).requires_grad_(), _randn(g, 768, 768).requires_grad_(), _randn(g, 2048, 768)
+    want = torch.autograd.grad(layers.layer_norm_mx_linear(x, None, None, w), (x, w), dy)
+    held, y = _held(lambda: checkpoint(layers.layer_norm_mx_linear, x, None, None, w, use_reentrant=False))
+    assert held < y.nbytes + api.mx_bytes(768, 2048)
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(y, (x, w), dy), want))
+
+
+def test_what_was_kept_goes_through_hooks_unchanged(layers):
+    """SavedActivations leaves it alone, a hook that moves it away and back may, and one that gives back something else is told so."""
+    from paper_2510_11400_amd import hooks
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, w, dy = _randn(g, 600, 300).requires_grad_(), _randn(g, 40, 300).requires_grad_(), _randn(g, 600, 40)
+    want = torch.autograd.grad(layers.mx_linear(x, w), (x, w), dy)
+    for context in (hooks.SavedActivations(64, 4, exclude=(w,)), torch.autograd.graph.save_on_cpu()):
+        with context:
+            y = layers.mx_linear(x, w)
+        assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(y, (x, w), dy), want))
+    for change, error in ((lambda t: t.float(), ValueError), (lambda t: t.cpu(), ValueError), (lambda t: t[:, :-1], layers.api.FedHybridError)):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, change):
+            y = layers.mx_linear(x, w)
+        with pytest.raises(error):
+            torch.autograd.grad(y, (x, w), dy)
