@@ -32,13 +32,16 @@ class _LayerNorm(torch.autograd.Function):
     def forward(ctx, x, weight, bias, eps):
         m = _rows(x)
         y, mean, rstd = api.fh_layer_norm(m, weight, bias, eps)
-        ctx.save_for_backward(m, mean, rstd, weight)
+        # the statistics as bytes: hooks.SavedActivations would quantise vectors of fp32 from 4096 rows on, and an rstd that is small beside its
+        # group's others would be off by any factor
+        ctx.save_for_backward(m, mean.view(torch.uint8), rstd.view(torch.uint8), weight)
         return y.view(x.shape)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         m, mean, rstd, weight = ctx.saved_tensors
+        mean, rstd = mean.view(torch.float32), rstd.view(torch.float32)
         dx, dw, db = api.fh_layer_norm_backward(_rows(dy), m, mean, rstd, weight, sums=any(ctx.needs_input_grad[1:3]))
         return (dx.view(dy.shape) if ctx.needs_input_grad[0] else None, dw if ctx.needs_input_grad[1] else None,
                 db if ctx.needs_input_grad[2] else None, None)
@@ -46,7 +49,7 @@ class _LayerNorm(torch.autograd.Function):
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5) -> torch.Tensor:
     """Layer norm over the last dimension, differentiable.  x is saved as it is: under hooks.SavedActivations it is stored
-    compressed, like any activation that autograd saves."""
+    compressed, like any activation that autograd saves; the rows' statistics stay exact."""
     return _LayerNorm.apply(x, weight, bias, eps)
 
 

@@ -284,3 +284,22 @@ def test_what_was_kept_goes_through_hooks_unchanged(layers):
             y = layers.mx_linear(x, w)
         with pytest.raises(error):
             torch.autograd.grad(y, (x, w), dy)
+
+
+# ---- a norm's statistics are not activations -----------------------------------------------------------------
+@pytest.mark.parametrize("rows", [100, 5000])
+def test_the_statistics_stay_exact_under_saved_activations(layers, rows):
+    """Rows whose widths differ by 2^24, x itself kept as it is: the gradients are those of an uncompressed step, bit for bit, however many
+    rows there are."""
+    from paper_2510_11400_amd import hooks
+    g = torch.Generator(device="cuda").manual_seed(1)
+    width = torch.exp2(torch.randint(-12, 13, (rows, 1), generator=g, device="cuda").float())
+    x = (torch.randn(rows, 40, generator=g, device="cuda") * width).requires_grad_()
+    w, b = torch.randn(40, generator=g, device="cuda").requires_grad_(), torch.randn(40, generator=g, device="cuda").requires_grad_()
+    dy = torch.randn(rows, 40, generator=g, device="cuda")
+    want = torch.autograd.grad(layers.layer_norm(x, w, b), (x, w, b), dy)
+    with hooks.SavedActivations(256, 4, exclude=(x, w, b)):
+        y = layers.layer_norm(x, w, b)
+    assert all(torch.equal(p, q) for p, q in zip(torch.autograd.grad(y, (x, w, b), dy), want))
+    empty = layers.layer_norm(x[:0], w, b)
+    assert not torch.autograd.grad(empty, w, dy[:0])[0].any()
