@@ -1378,10 +1378,10 @@ def fh_layer_norm_mx(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bia
 
 def fh_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
                            weight: Optional[torch.Tensor] = None, sums: bool = True, dx: Optional[torch.Tensor] = None,
-                           workspace: Optional[torch.Tensor] = None, stream=None):
+                           workspace: Optional[torch.Tensor] = None, stream=None, sums_dtype: Optional[torch.dtype] = None):
     """Enqueue the backward pass of fh_layer_norm; returns (dx, dweight, dbias), the last two (None unless `sums`) in the
-    weight's dtype, in x's where there is no weight."""
-    return _binding.layer_norm_backward(dy, x, mean, rstd, weight, sums, dx, workspace, stream)
+    weight's dtype; where there is no weight in `sums_dtype`, x's if that is left out."""
+    return _binding.layer_norm_backward(dy, x, mean, rstd, weight, sums, dx, workspace, stream, sums_dtype)
 
 
 FH_MX_NEEDS_INPUT, FH_MX_NEEDS_WEIGHT = 1, 2

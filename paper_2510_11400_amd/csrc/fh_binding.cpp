@@ -445,8 +445,8 @@ FH_ENTRY(layer_norm_mx, 9)
     return tuple(s.wrapped(), Ref(wrap(stats.first)), Ref(wrap(stats.second)));
 FH_EXIT
 
-// (dy, x, mean, rstd, weight, sums, dx, workspace, stream)
-FH_ENTRY(layer_norm_backward, 9)
+// (dy, x, mean, rstd, weight, sums, dx, workspace, stream, the sums' dtype or None)
+FH_ENTRY(layer_norm_backward, 10)
     const Matrix x = matrix(a[1], "x"), dy = matrix(a[0], "dy");
     const c10::Device device = x.device();
     if (dy.rows != x.rows || dy.cols != x.cols || dy.dtype != x.dtype) raise(PyExc_ValueError, "dy must have the shape and the dtype of x");
@@ -458,7 +458,9 @@ FH_ENTRY(layer_norm_backward, 9)
     const On on(a[8], device);
     const Matrix dx = matrix_like(a[6], x, "dx");
     if (a[6] == Py_None) on.lent(dx.t);
-    const at::ScalarType type = weight.defined() ? weight.scalar_type() : x.t.scalar_type();
+    const at::ScalarType type = a[9] != Py_None ? scalar_type(a[9]) : weight.defined() ? weight.scalar_type() : x.t.scalar_type();
+    if (weight.defined() && type != weight.scalar_type())
+        raise(PyExc_TypeError, "the sums are of the weight's dtype, %s, not of %s", c10::toString(weight.scalar_type()), c10::toString(type));
     const int p_dtype = dtype_code(type);
     Pair sum;
     Work w;

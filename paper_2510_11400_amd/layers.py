@@ -34,6 +34,7 @@ class _LayerNorm(torch.autograd.Function):
         y, mean, rstd = api.fh_layer_norm(m, weight, bias, eps)
         # the statistics as bytes: hooks.SavedActivations would quantise vectors of fp32 from 4096 rows on, and an rstd that is small beside its
         # group's others would be off by any factor
+        ctx.sums_dtype = None if weight is not None or bias is None else bias.dtype
         ctx.save_for_backward(m, mean.view(torch.uint8), rstd.view(torch.uint8), weight)
         return y.view(x.shape)
 
@@ -42,7 +43,8 @@ class _LayerNorm(torch.autograd.Function):
     def backward(ctx, dy):
         m, mean, rstd, weight = ctx.saved_tensors
         mean, rstd = mean.view(torch.float32), rstd.view(torch.float32)
-        dx, dw, db = api.fh_layer_norm_backward(_rows(dy), m, mean, rstd, weight, sums=any(ctx.needs_input_grad[1:3]))
+        dx, dw, db = api.fh_layer_norm_backward(_rows(dy), m, mean, rstd, weight, sums=any(ctx.needs_input_grad[1:3]),
+                                                sums_dtype=ctx.sums_dtype)
         return (dx.view(dy.shape) if ctx.needs_input_grad[0] else None, dw if ctx.needs_input_grad[1] else None,
                 db if ctx.needs_input_grad[2] else None, None)
 

@@ -303,3 +303,23 @@ def test_the_statistics_stay_exact_under_saved_activations(layers, rows):
     assert all(torch.equal(p, q) for p, q in zip(torch.autograd.grad(y, (x, w, b), dy), want))
     empty = layers.layer_norm(x[:0], w, b)
     assert not torch.autograd.grad(empty, w, dy[:0])[0].any()
+
+
+def test_the_gradient_of_a_norms_bias_without_a_weight(layers, api):
+    """It is of the bias's dtype, summed in fp32 and not rounded to x's on the way: equal to the sum that the call gives in fp32."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, dy, b = _randn(g, 300, 70), _randn(g, 300, 70), torch.zeros(70, device="cuda", requires_grad=True)
+    db, = torch.autograd.grad(layers.layer_norm(x, None, b), b, dy)
+    exact = dy.double().sum(0)
+    # 300 terms in a tree and one join: R.layer_norm_backward's depth
+    assert db.dtype == torch.float32 and bool(((db.double() - exact).abs() <= (300 / 256 + 300) * R.U32 * dy.double().abs().sum(0)).all())
+    assert bool((db.double() - db.bfloat16().double()).any())             # sums that bf16 does not hold
+    _, mean, rstd = api.fh_layer_norm(x)
+    for dtype in (torch.float32, torch.bfloat16):
+        got = api.fh_layer_norm_backward(dy, x, mean, rstd, sums_dtype=dtype)
+        assert got[1].dtype == got[2].dtype == dtype and torch.equal(got[2], db.to(dtype))
+    assert api.fh_layer_norm_backward(dy, x, mean, rstd)[2].dtype == x.dtype
+    with pytest.raises(TypeError, match="weight"):
+        api.fh_layer_norm_backward(dy, x, mean, rstd, torch.ones(70, device="cuda"), sums_dtype=torch.bfloat16)
+    with pytest.raises(TypeError):
+        api.fh_layer_norm_backward(dy, x, mean, rstd, sums_dtype=torch.float16)
