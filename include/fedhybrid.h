@@ -587,7 +587,8 @@ fh_status fh_layer_norm_backward(const fh_norm_backward *norm, void *stream);
  * tokens x out_features with a row stride; y, dx and dweight are dense.  x, y, dy and dx are of dtype, the
  * norm's parameters, weight, bias and their gradients of p_dtype; norm_weight, norm_bias and bias may
  * be NULL.  `kept` (fh_mx_layer_kept_bytes) carries the statistics and the operands by columns from
- * the forward to the backward call and may be NULL where there is neither a norm nor a need (in the backward call: no need); `scratch`
+ * the forward to the backward call and may be NULL where there is no need; with kept_for, the forward call's needs in both calls, it has
+ * room for what these ask for alone (fh_mx_layer_sizes), with 0 for everything.  `scratch`
  * (fh_mx_layer_scratch_bytes, which is enough for either call without wide_gradient) is free again
  * once a call's work has run.  Both 16-byte aligned.  fh_mx_layer_sizes gives the bytes that the calls with this layer ask for (no
  * pointer of it is looked at).
@@ -614,6 +615,7 @@ typedef struct fh_mx_layer {
     int64_t     reserved;                       /* 0 */
     void       *dbias;                          /* backward */
     int32_t     wide_gradient;                  /* backward: 0 | 1 */
+    int32_t     kept_for;                       /* 0, or FH_MX_NEEDS_*, the needs among them */
 } fh_mx_layer;
 size_t    fh_mx_layer_kept_bytes(int64_t tokens, int64_t features, int64_t out_features);
 size_t    fh_mx_layer_scratch_bytes(int64_t tokens, int64_t features, int64_t out_features);

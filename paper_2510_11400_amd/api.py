@@ -285,7 +285,7 @@ class fh_mx_layer(ctypes.Structure):
                 ("dy", ctypes.c_void_p), ("dy_stride", ctypes.c_int64), ("dx", ctypes.c_void_p), ("dweight", ctypes.c_void_p),
                 ("dnorm_weight", ctypes.c_void_p), ("dnorm_bias", ctypes.c_void_p),
                 ("kept", ctypes.c_void_p), ("kept_cap", ctypes.c_size_t), ("scratch", ctypes.c_void_p), ("scratch_cap", ctypes.c_size_t),
-                ("reserved", ctypes.c_int64), ("dbias", ctypes.c_void_p), ("wide_gradient", ctypes.c_int32)]
+                ("reserved", ctypes.c_int64), ("dbias", ctypes.c_void_p), ("wide_gradient", ctypes.c_int32), ("kept_for", ctypes.c_int32)]
 
 
 for _name in ("fh_mx_layer_kept_bytes", "fh_mx_layer_scratch_bytes"):
@@ -1393,7 +1393,7 @@ class MxLayer:
     are of one dtype, and so are x, y and the gradients of both.  The norm's backward pass takes its output's gradient rounded to
     that dtype, as from a layer of its own, with `wide_gradient` in fp32."""
     __slots__ = ("inputs", "kept", "shape", "dtype", "p_dtype", "features", "norm", "eps", "needs_input", "needs_weight", "rounding",
-                 "wide_gradient", "weighted")
+                 "wide_gradient", "weighted", "kept_for")
 
     def __init__(self, x: torch.Tensor, weight: torch.Tensor, bias=None, norm: bool = False, norm_weight=None, norm_bias=None,
                  eps: float = 1e-5, needs_input: bool = True, needs_weight: bool = True, rounding="nearest", seed: int = 0,
@@ -1407,6 +1407,7 @@ class MxLayer:
     def forward(self, stream=None) -> torch.Tensor:
         """Enqueue the forward half; returns y."""
         x, weight = self.inputs[:2]
+        self.kept_for = FH_MX_NEEDS_INPUT * bool(self.inputs[7]) | FH_MX_NEEDS_WEIGHT * bool(self.inputs[8])
         y, self.kept = _binding.layer_forward(*self.inputs, stream)
         self.inputs, self.shape, self.dtype, self.p_dtype, self.features = None, y.shape, x.dtype, weight.dtype, x.shape[1]
         return y
@@ -1421,5 +1422,5 @@ class MxLayer:
         if self.norm and self.needs_input and (norm_weight is not None) != self.weighted:
             raise ValueError("norm_weight must be given again" if self.weighted else "the forward call had no norm_weight")
         grads = _binding.layer_backward(dy, x, norm_weight, self.kept, self.features, self.p_dtype, self.norm, self.eps, self.needs_input,
-                                        self.needs_weight, bias, *self.rounding, self.wide_gradient, stream)
+                                        self.needs_weight, bias, *self.rounding, self.wide_gradient, self.kept_for, stream)
         return grads if bias else grads[:4]

@@ -483,6 +483,7 @@ struct Layer {
     int rounding;
     uint64_t seed, id;
     bool wide;                                                            // the gradient of a norm's output in fp32
+    int32_t needs() const { return (input ? FH_MX_NEEDS_INPUT : 0) | (weight ? FH_MX_NEEDS_WEIGHT : 0); }
 };
 struct Sizes { size_t kept, forward, backward; };
 Sizes sizes_of(const fh_mx_layer& l)                                      // of a layer that the call itself will refuse: nothing
@@ -504,7 +505,7 @@ Forward forward_of(const Layer& layer, const Matrix& x, const Matrix& weight, co
     fh_mx_layer l = {};
     l.tokens = x.rows; l.features = x.cols; l.out_features = weight.rows;
     l.dtype = x.dtype; l.p_dtype = weight.dtype; l.norm = layer.norm;
-    l.needs = (layer.input ? FH_MX_NEEDS_INPUT : 0) | (layer.weight ? FH_MX_NEEDS_WEIGHT : 0);
+    l.needs = l.kept_for = layer.needs();
     l.eps = layer.eps;
     l.x = x.data(); l.x_stride = x.stride; l.weight = weight.data(); l.weight_stride = weight.stride; l.dy_stride = weight.rows;
     l.norm_weight = vector(norm_weight, x.cols, device, "norm_weight");
@@ -514,7 +515,7 @@ Forward forward_of(const Layer& layer, const Matrix& x, const Matrix& weight, co
     Forward f;
     f.y = new_matrix(x.rows, weight.rows, x.t.scalar_type(), device).t;
     l.y = f.y.data_ptr();
-    if (layer.norm || l.needs) {
+    if (l.needs) {
         f.kept = bytes(sizes.kept, device);
         l.kept = f.kept.data_ptr(); l.kept_cap = (size_t)f.kept.numel();
     }
@@ -526,7 +527,7 @@ Forward forward_of(const Layer& layer, const Matrix& x, const Matrix& weight, co
 
 struct Backward { at::Tensor dx, dweight, dbias; Pair dnorm; };
 Backward backward_of(const Layer& layer, const Matrix& dy, const at::Tensor& x_again, const at::Tensor& norm_weight, const at::Tensor& kept, int64_t features,
-                     at::ScalarType p_type)
+                     at::ScalarType p_type, int32_t kept_for)
 {
     const c10::Device device = dy.device();
     if (kept.defined()) {
@@ -538,7 +539,8 @@ Backward backward_of(const Layer& layer, const Matrix& dy, const at::Tensor& x_a
     fh_mx_layer l = {};
     l.tokens = dy.rows; l.features = features; l.out_features = dy.cols;
     l.dtype = dy.dtype; l.p_dtype = dtype_code(p_type); l.norm = layer.norm;
-    l.needs = (layer.input ? FH_MX_NEEDS_INPUT : 0) | (layer.weight ? FH_MX_NEEDS_WEIGHT : 0);
+    l.needs = layer.needs();
+    l.kept_for = kept_for;
     l.eps = layer.eps;
     l.rounding = layer.rounding; l.seed = layer.seed; l.tensor_id = layer.id; l.wide_gradient = layer.wide;
     l.dy = dy.data(); l.dy_stride = dy.stride; l.x_stride = l.weight_stride = features;
@@ -586,13 +588,14 @@ FH_ENTRY(layer_forward, 10)
 FH_EXIT
 
 // (dy, x, norm_weight, kept, features, p_dtype, norm, eps, needs_input, needs_weight, needs_bias, rounding, seed, tensor_id, wide_gradient,
-//  stream) -> (dx, dweight, dnorm_weight, dnorm_bias, dbias)
-FH_ENTRY(layer_backward, 16)
+//  the forward call's needs, stream) -> (dx, dweight, dnorm_weight, dnorm_bias, dbias)
+FH_ENTRY(layer_backward, 17)
     const Layer layer = {truth(a[6]), (float)f64(a[7]), truth(a[8]), truth(a[9]), truth(a[10]), rounding_of(a[11]), u64(a[12]), u64(a[13]), truth(a[14])};
     const Matrix dy = matrix(a[0], "dy");
     const at::Tensor kept = tensor_or_none(a[3], "kept");
-    const On on(a[15], dy.device());
-    const Backward b = backward_of(layer, dy, tensor_or_none(a[1], "x"), tensor_or_none(a[2], "norm_weight"), kept, i64(a[4]), scalar_type(a[5]));
+    const On on(a[16], dy.device());
+    const Backward b = backward_of(layer, dy, tensor_or_none(a[1], "x"), tensor_or_none(a[2], "norm_weight"), kept, i64(a[4]), scalar_type(a[5]),
+                                   (int32_t)i64(a[15]));
     // it is of the stream that the forward call went through, and may be dropped before this one is through with it
     if (kept.defined()) kept.record_stream(On::as_recorded(c10::hip::getCurrentHIPStream(dy.device().index())));
     for (const at::Tensor* t : {&b.dx, &b.dweight, &b.dnorm.first, &b.dbias}) on.lent(*t);
@@ -650,7 +653,8 @@ struct Linear : torch::autograd::Function<Linear> {
             const at::Tensor dy = rows_of(given[0]);
             const auto saved = ctx->get_saved_variables();
             const auto from = [&](size_t i) { return i < saved.size() ? saved[i] : at::Tensor(); };
-            const Backward b = backward_of(pass->layer, matrix(dy, "dy"), from(1), from(2), from(0), pass->features, pass->p_type);
+            const Backward b = backward_of(pass->layer, matrix(dy, "dy"), from(1), from(2), from(0), pass->features, pass->p_type,
+                                           pass->layer.needs());
             if (pass->x) grads[0] = b.dx.view(pass->shape);
             if (pass->norm_weight) grads[1] = b.dnorm.first;
             if (pass->norm_bias) grads[2] = b.dnorm.second;

@@ -14,15 +14,17 @@ struct Parts {
     size_t x_rows, w_rows, forward_work, forward;
     size_t dy_rows, dy_columns, dh, backward_work, backward;
 };
+constexpr int32_t kNeeds = FH_MX_NEEDS_INPUT | FH_MX_NEEDS_WEIGHT;
 // `wide`: with the gradient of a norm's output in binary32, in the place of dy's columns, which only the product before it reads.
-Parts parts_of(int64_t tokens, int64_t features, int64_t out, bool wide)
+// `kept_for`, `stats`: what there is room for in `kept`.
+Parts parts_of(int64_t tokens, int64_t features, int64_t out, bool wide, int32_t kept_for, bool stats)
 {
     Parts p;
     p.mean = 0;
-    p.rstd = whole((size_t)tokens * 4);
-    p.x_columns = p.rstd + whole((size_t)tokens * 4);
-    p.w_columns = p.x_columns + whole(mx_bytes(features, tokens));
-    p.kept = p.w_columns + whole(mx_bytes(features, out));
+    p.rstd = stats ? whole((size_t)tokens * 4) : 0;
+    p.x_columns = p.rstd * 2;
+    p.w_columns = p.x_columns + (kept_for & FH_MX_NEEDS_WEIGHT ? whole(mx_bytes(features, tokens)) : 0);
+    p.kept = p.w_columns + (kept_for & FH_MX_NEEDS_INPUT ? whole(mx_bytes(features, out)) : 0);
     p.x_rows = 0;
     p.w_rows = whole(mx_bytes(tokens, features));
     p.forward_work = p.w_rows + whole(mx_bytes(out, features));
@@ -51,12 +53,16 @@ fh_status check(const fh_mx_layer* l)
         l->dy_stride < l->out_features || l->x_stride > kMostStride || l->weight_stride > kMostStride || l->dy_stride > kMostStride)
         return FH_ERR_BAD_SHAPE;
     if ((l->norm != 0 && l->norm != 1) || (l->wide_gradient != 0 && l->wide_gradient != 1)) return FH_ERR_BAD_PARAM;
-    if ((l->needs & ~(FH_MX_NEEDS_INPUT | FH_MX_NEEDS_WEIGHT)) != 0 || l->reserved != 0 || (l->norm && !(l->eps >= 0.0f))) return FH_ERR_BAD_PARAM;
+    if ((l->kept_for & ~kNeeds) != 0 || (l->kept_for && (l->needs & ~l->kept_for) != 0)) return FH_ERR_BAD_PARAM;
+    if ((l->needs & ~kNeeds) != 0 || l->reserved != 0 || (l->norm && !(l->eps >= 0.0f))) return FH_ERR_BAD_PARAM;
     return FH_OK;
 }
 
 bool is_wide(const fh_mx_layer& l) { return l.wide_gradient && l.norm && (l.needs & FH_MX_NEEDS_INPUT) && l.dtype != FH_F32; }
-Parts parts_of(const fh_mx_layer& l) { return parts_of(l.tokens, l.features, l.out_features, is_wide(l)); }
+Parts parts_of(const fh_mx_layer& l)
+{
+    return parts_of(l.tokens, l.features, l.out_features, is_wide(l), l.kept_for ? l.kept_for : kNeeds, l.norm || !l.kept_for);
+}
 
 uint8_t* at(void* p, size_t offset) { return static_cast<uint8_t*>(p) + offset; }
 
@@ -67,13 +73,13 @@ extern "C" {
 
 size_t fh_mx_layer_kept_bytes(int64_t tokens, int64_t features, int64_t out_features)
 {
-    return fh::shape_ok(tokens, features, out_features) ? fh::parts_of(tokens, features, out_features, false).kept : 0;
+    return fh::shape_ok(tokens, features, out_features) ? fh::parts_of(tokens, features, out_features, false, fh::kNeeds, true).kept : 0;
 }
 
 size_t fh_mx_layer_scratch_bytes(int64_t tokens, int64_t features, int64_t out_features)
 {
     if (!fh::shape_ok(tokens, features, out_features)) return 0;
-    const fh::Parts p = fh::parts_of(tokens, features, out_features, false);
+    const fh::Parts p = fh::parts_of(tokens, features, out_features, false, fh::kNeeds, true);
     return fh::larger(p.forward, p.backward);
 }
 
@@ -84,7 +90,7 @@ fh_status fh_mx_layer_sizes(const fh_mx_layer* l, size_t* kept, size_t* forward_
     const fh_status ok = check(l);
     if (ok != FH_OK) return ok;
     const Parts p = parts_of(*l);
-    *kept = p.kept;
+    *kept = l->needs ? p.kept : 0;
     *forward_scratch = p.forward;
     *backward_scratch = p.backward;
     return FH_OK;
@@ -97,7 +103,7 @@ fh_status fh_mx_layer_forward(const fh_mx_layer* l, void* stream)
     if (ok != FH_OK || l->tokens == 0) return ok;
     const Parts p = parts_of(*l);
     const size_t size = dtype_size(l->dtype), p_size = dtype_size(l->p_dtype);
-    const bool keeps = l->norm || l->needs;
+    const bool keeps = l->needs != 0;
     if (!l->x || !l->weight || !l->y || !l->scratch || (keeps && !l->kept)) return FH_ERR_NULL;
     if (!is_aligned(l->x, size) || !is_aligned(l->y, size) || !is_aligned(l->weight, p_size) || !is_aligned(l->bias, p_size) ||
         !is_aligned(l->norm_weight, p_size) || !is_aligned(l->norm_bias, p_size) || !is_aligned(l->kept, 16) || !is_aligned(l->scratch, 16))
@@ -112,7 +118,8 @@ fh_status fh_mx_layer_forward(const fh_mx_layer* l, void* stream)
     fh_status s;
     if (l->norm)
         s = fh_layer_norm_mx(l->x, dtype, l->tokens, l->features, l->x_stride, l->norm_weight, l->norm_bias, p_dtype, l->eps, FH_ROUND_NEAREST, 0, 0,
-                             x_rows, x_bytes, x_columns, mx_bytes(l->features, l->tokens), at(l->kept, p.mean), at(l->kept, p.rstd), stream);
+                             x_rows, x_bytes, x_columns, mx_bytes(l->features, l->tokens), keeps ? at(l->kept, p.mean) : nullptr, keeps ? at(l->kept, p.rstd) : nullptr,
+                             stream);
     else
         s = fh_mx_quantize(l->x, dtype, l->tokens, l->features, l->x_stride, FH_ROUND_NEAREST, 0, 0, x_rows, x_bytes, x_columns,
                            mx_bytes(l->features, l->tokens), stream);
@@ -134,7 +141,7 @@ fh_status fh_mx_layer_backward(const fh_mx_layer* l, void* stream)
     const Parts p = parts_of(*l);
     const size_t size = dtype_size(l->dtype), p_size = dtype_size(l->p_dtype);
     const bool input = l->needs & FH_MX_NEEDS_INPUT, weight = l->needs & FH_MX_NEEDS_WEIGHT;
-    if ((l->needs && !l->kept) || (p.backward && !l->scratch) || (weight && !l->dweight)) return FH_ERR_NULL;
+    if ((l->needs && p.kept && !l->kept) || (p.backward && !l->scratch) || (weight && !l->dweight)) return FH_ERR_NULL;
     if (l->tokens > 0 && (!l->dy || (input && !l->dx) || (input && l->norm && !l->x))) return FH_ERR_NULL;
     if (!is_aligned(l->x, size) || !is_aligned(l->dy, size) || !is_aligned(l->dx, size) || !is_aligned(l->dweight, p_size) ||
         !is_aligned(l->norm_weight, p_size) || !is_aligned(l->dnorm_weight, p_size) || !is_aligned(l->dnorm_bias, p_size) ||

@@ -323,3 +323,38 @@ def test_the_gradient_of_a_norms_bias_without_a_weight(layers, api):
         api.fh_layer_norm_backward(dy, x, mean, rstd, torch.ones(70, device="cuda"), sums_dtype=torch.bfloat16)
     with pytest.raises(TypeError):
         api.fh_layer_norm_backward(dy, x, mean, rstd, sums_dtype=torch.float16)
+
+
+@pytest.mark.parametrize("norm", [False, True])
+def test_a_layer_keeps_what_its_gradients_need(layers, api, norm):
+    """And gives the same ones: for the input alone, for the weight alone, for neither."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, dy, w, nw = _randn(g, 700, 300), _randn(g, 700, 130), _randn(g, 130, 300), _randn(g, 300)
+    given = dict(norm=norm, norm_weight=nw if norm else None)
+    again = (x, nw) if norm else ()
+    both = api.MxLayer(x, w, **given)
+    y = both.forward()
+    want = both.backward(dy, *again)
+    x_bytes, w_bytes = api.mx_bytes(300, 700), api.mx_bytes(300, 130)
+    slack = 2 * 700 * 4 + 1024
+    for needs_input, needs_weight, most in ((True, False, w_bytes), (False, True, x_bytes), (True, True, x_bytes + w_bytes)):
+        layer = api.MxLayer(x, w, needs_input=needs_input, needs_weight=needs_weight, **given)
+        assert torch.equal(layer.forward(), y) and most <= layer.kept.numel() < most + slack
+        got = layer.backward(dy, *again)
+        for needed, a, b in zip((needs_input, needs_weight, needs_input, needs_input), got, want):
+            assert (a is None) if not needed or b is None else torch.equal(a, b)
+        layer.needs_input = layer.needs_weight = True
+        if not (needs_input and needs_weight):
+            with pytest.raises(api.FedHybridError):
+                layer.backward(dy, *again)
+    none = api.MxLayer(x, w, needs_input=False, needs_weight=False, **given)
+    assert torch.equal(none.forward(), y) and none.kept is None
+
+
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("needed", [(True, False), (False, True), (True, True)])
+def test_no_tokens_for_some_gradients(layers, norm, needed):
+    x, w = torch.empty(0, 40, device="cuda", requires_grad=needed[0]), torch.randn(7, 40, device="cuda", requires_grad=needed[1])
+    y = layers.layer_norm_mx_linear(x, None, None, w) if norm else layers.mx_linear(x, w)
+    grads = torch.autograd.grad(y, [t for t, n in zip((x, w), needed) if n], torch.empty(0, 7, device="cuda"))
+    assert y.shape == (0, 7) and all(not v.any() for v in grads)

@@ -61,7 +61,7 @@ def test_the_norms_weight_is_given_again(before, again):
     x, w, nw = torch.zeros(4, 40), torch.zeros(7, 40), torch.ones(40)
     layer = api.MxLayer(x, w, norm=True, norm_weight=nw if before else None)
     layer.shape, layer.dtype = torch.Size((4, 7)), torch.float32                # as a forward call leaves them
-    layer.kept, layer.features, layer.p_dtype = None, 40, torch.float32
+    layer.kept, layer.features, layer.p_dtype, layer.kept_for = None, 40, torch.float32, 3
     with pytest.raises(ValueError, match="norm_weight"):
         layer.backward(torch.zeros(4, 7), x, nw if again else None)
     with pytest.raises(ValueError, match="device memory"):                      # alike: on to the call itself, which wants device tensors
@@ -88,3 +88,20 @@ def test_tangents_are_refused(which):
         layers.layer_norm_mx_linear(*tensors)
     with pytest.raises(ValueError, match="device memory"):
         frozen(tensors[0])
+
+
+def test_only_what_is_needed_is_kept():
+    """With kept_for: x by columns for the weight's gradient, W by columns for the input's, statistics with a norm; without, room for all."""
+    whole = lambda n: -(-n // 256) * 256  # noqa: E731
+    stats, x, w = 2 * whole(400), whole(api.mx_bytes(300, 100)), whole(api.mx_bytes(300, 70))
+    assert [_sizes(needs=n, kept_for=n)[1] for n in (1, 2, 3)] == [stats + w, stats + x, stats + x + w]
+    assert [_sizes(needs=n, kept_for=n, norm=0)[1] for n in (1, 2, 3)] == [w, x, x + w]
+    assert [_sizes(needs=n, kept_for=3)[1] for n in (1, 2)] == [stats + x + w] * 2
+    assert [_sizes(needs=n)[1] for n in (1, 2, 3)] == [LIB.fh_mx_layer_kept_bytes(100, 300, 70)] * 3 == [stats + x + w] * 3
+    assert _sizes(needs=0)[:2] == (0, 0) and _sizes(needs=0, norm=0)[:2] == (0, 0)
+    for n in (1, 2):
+        assert _sizes(needs=3, kept_for=n)[0] == 12 and _sizes(needs=3 - n, kept_for=n)[0] == 12
+        for call in (LIB.fh_mx_layer_forward, LIB.fh_mx_layer_backward):
+            assert call(ctypes.byref(_layer(needs=n, kept_for=n, kept_cap=_sizes(needs=n, kept_for=n)[1] - 1)), None) == 7
+            assert call(ctypes.byref(_layer(needs=n, kept_for=n, kept=None)), None) == 1
+    assert _sizes(kept_for=4)[0] == 12 and _sizes(kept_for=-1)[0] == 12
