@@ -523,13 +523,14 @@ __global__ __launch_bounds__(256) void norm_column_sums_kernel(NormBackwardArgs 
 // 256 rows at a time a wave, whose loads are all on their way at once: up to 256 rows the kernel takes little more than one of them.
 constexpr int kMostParts = 256;
 template <typename P>
-__global__ __launch_bounds__(1024) void norm_join_kernel(const float* partial, int64_t parts, int64_t cols, int32_t count, P* first, P* second)
+__global__ __launch_bounds__(1024) void norm_join_kernel(const float* partial, int64_t parts, int64_t cols, int32_t count, P* first, P* second, uint32_t first_group)
 {
     constexpr int kEach = kMostParts / 16;
     __shared__ float s_part[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int32_t which = count == 2 ? blockIdx.x & 1 : 0;
-    const int64_t c = (int64_t)(count == 2 ? blockIdx.x >> 1 : blockIdx.x) * 64 + lane;
+    const uint32_t group = first_group + blockIdx.x;
+    const int32_t which = count == 2 ? group & 1 : 0;
+    const int64_t c = (int64_t)(count == 2 ? group >> 1 : group) * 64 + lane;
     const float* from = partial + which * cols + (c < cols ? c : 0);
     float sum = 0.0f;
     for (int64_t start = 0; start < parts; start += kMostParts) {
@@ -599,7 +600,15 @@ hipError_t norm_any(const void* x, int64_t rows, int64_t cols, int64_t xs, const
         if (cols <= 12288) return norm_of<T, 512, 3, MX>(x, rows, cols, xs, n, to, s);
         if (cols <= kGroupCols) return norm_of<T, 512, 4, MX>(x, rows, cols, xs, n, to, s);
     }
-    return launch(norm_long_rows_kernel<T, MX>, dim3((uint32_t)rows), dim3(1024), s, static_cast<const T*>(x), cols, xs, n, to);
+    return in_parts(rows, 1024, [&](int64_t first, int64_t count) {        // parts of 2^21 rows: whole groups of 32 rows' scales
+        NormArgs of = n;
+        if (of.mean) of.mean += first;
+        if (of.rstd) of.rstd += first;
+        NormOut there = to;
+        if (to.y) there.y = static_cast<uint8_t*>(to.y) + (MX ? first * (to.stride_or_chunks * 128) : first * to.stride_or_chunks * (int64_t)sizeof(T));
+        if (MX && to.y) there.scales = to.scales + first / 32 * (to.stride_or_chunks * 256);
+        return launch(norm_long_rows_kernel<T, MX>, dim3((uint32_t)count), dim3(1024), s, static_cast<const T*>(x) + first * xs, cols, xs, of, there);
+    });
 }
 
 // Threads that share a row of the backward pass, runs of four columns a thread, rows that a workgroup takes at a time (as many as
@@ -656,7 +665,16 @@ hipError_t backward_any(const NormBackwardArgs& a, int64_t* parts, hipStream_t s
         const hipError_t e = launch(norm_column_sums_kernel<T, G>, dim3((uint32_t)(col_groups * *parts)), dim3(256), s, a, each, (uint32_t)col_groups);
         if (e != hipSuccess) return e;
     }
-    return a.dx ? launch(norm_backward_long_rows_kernel<T, G>, dim3((uint32_t)a.rows), dim3(1024), s, a) : hipSuccess;
+    if (!a.dx) return hipSuccess;
+    return in_parts(a.rows, 1024, [&](int64_t first, int64_t count) {
+        NormBackwardArgs of = a;
+        of.x = static_cast<const T*>(a.x) + first * a.x_stride;
+        of.dy = static_cast<const G*>(a.dy) + first * a.dy_stride;
+        of.dx = static_cast<T*>(a.dx) + first * a.dx_stride;
+        of.mean += first;
+        of.rstd += first;
+        return launch(norm_backward_long_rows_kernel<T, G>, dim3((uint32_t)count), dim3(1024), s, of);
+    });
 }
 bool norm_shape_ok(int64_t rows, int64_t cols) { return mx_shape_ok(rows, cols) && cols >= 1; }
 
@@ -664,9 +682,12 @@ bool norm_shape_ok(int64_t rows, int64_t cols) { return mx_shape_ok(rows, cols) 
 
 hipError_t launch_join(const float* partial, int64_t parts, int64_t cols, int32_t count, int32_t p_dtype, void* first, void* second, hipStream_t s)
 {
-    const dim3 grid((uint32_t)((cols + 63) / 64 * count)), block(1024);
-    if (p_dtype == FH_F32) return launch(norm_join_kernel<float>, grid, block, s, partial, parts, cols, count, static_cast<float*>(first), static_cast<float*>(second));
-    return launch(norm_join_kernel<Bf16>, grid, block, s, partial, parts, cols, count, static_cast<Bf16*>(first), static_cast<Bf16*>(second));
+    return in_parts((cols + 63) / 64 * count, 1024, [&](int64_t begin, int64_t groups) {
+        const dim3 grid((uint32_t)groups), block(1024);
+        const uint32_t b = (uint32_t)begin;
+        if (p_dtype == FH_F32) return launch(norm_join_kernel<float>, grid, block, s, partial, parts, cols, count, static_cast<float*>(first), static_cast<float*>(second), b);
+        return launch(norm_join_kernel<Bf16>, grid, block, s, partial, parts, cols, count, static_cast<Bf16*>(first), static_cast<Bf16*>(second), b);
+    });
 }
 
 // Rows of which 32 fit in LDS, and no more threads than a launch may have (2^32).

@@ -14,6 +14,7 @@
 #include <stdint.h>
 
 #include "fh_device.hpp"
+#include "fh_rules.hpp"
 
 namespace fh {
 
@@ -137,10 +138,23 @@ __device__ __forceinline__ float value(Bf16 v) { return __builtin_bit_cast(float
 template <typename... P, typename... A>
 hipError_t launch(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t s, const A&... given)
 {
+    if ((uint64_t)grid.x * block.x * grid.y * grid.z >> 32) return hipErrorInvalidConfiguration;
     return [&](P... args) {
         void* list[] = {static_cast<void*>(&args)...};
         return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, list, 0, s);
     }(given...);
+}
+
+// `groups` workgroups of `threads` by launches of as many as one may have: part(first, number).
+template <typename F>
+hipError_t in_parts(int64_t groups, int64_t threads, F part)
+{
+    const int64_t most = groups_at_once(threads);
+    for (int64_t first = 0; first < groups; first += most) {
+        const hipError_t e = part(first, groups - first < most ? groups - first : most);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 // N values in words as they lie in memory.

@@ -22,6 +22,7 @@ struct ProductArgs {
     int32_t        bias_dtype;
     uint32_t       m_tiles, n_tiles;
     uint32_t       step;               // from a workgroup's tile to its next one
+    uint32_t       first;              // workgroup of the launches before this one
 };
 static_assert(sizeof(ProductArgs) <= 112, "longer arguments are enqueued a microsecond later");
 
@@ -70,12 +71,12 @@ __global__ __launch_bounds__(WAVES * 64) void mx_waves_kernel(ProductArgs p)
     static_assert(kScales <= 1024, "one load brings the scales");
     __shared__ __attribute__((aligned(16))) uint8_t s_area[WAVES * kArea];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t tiles = p.m_tiles * p.n_tiles, part = RUNS ? 0 : blockIdx.x / tiles;
+    const uint32_t tiles = p.m_tiles * p.n_tiles, number = p.first + blockIdx.x, part = RUNS ? 0 : number / tiles;
     uint32_t i, j;
     if constexpr (RUNS) {                                        // 0.2 us of divisions in a row: where it pays
-        in_bands(run_of(blockIdx.x, tiles), p.m_tiles, p.n_tiles, i, j);
+        in_bands(run_of(number, tiles), p.m_tiles, p.n_tiles, i, j);
     } else {
-        const uint32_t tile = blockIdx.x - part * tiles;
+        const uint32_t tile = number - part * tiles;
         i = tile / p.n_tiles;
         j = tile % p.n_tiles;
     }
@@ -441,7 +442,10 @@ hipError_t waves_of(ProductArgs p, hipStream_t s)
     if (groups > INT32_MAX) return hipErrorInvalidValue;
     p.m_tiles = (uint32_t)m_tiles;
     p.n_tiles = (uint32_t)n_tiles;
-    return launch(mx_waves_kernel<T, MT, NT, WAVES, RUNS>, dim3((uint32_t)groups), dim3(WAVES * 64), s, p);
+    return in_parts(groups, WAVES * 64, [&](int64_t first, int64_t count) {
+        p.first = (uint32_t)first;
+        return launch(mx_waves_kernel<T, MT, NT, WAVES, RUNS>, dim3((uint32_t)count), dim3(WAVES * 64), s, p);
+    });
 }
 template <typename T, int B, int WN>
 hipError_t squares_of(ProductArgs p, hipStream_t s)
@@ -514,7 +518,7 @@ fh_status fh_mx_matmul(const fh_mx_product* q, void* stream)
     const Plan plan = plan_of(q->m, q->n, q->k);
     const MxStore a = mx_store(const_cast<void*>(q->a), q->m, q->k), b = mx_store(const_cast<void*>(q->b), q->n, q->k);
     const ProductArgs p = {a.codes, a.scales, b.codes, b.scales, q->m, q->n, q->bias, q->out, q->stride, (int32_t)a.chunks,
-                           (int32_t)plan.chunks_each, plan.parts, q->bias_dtype, 0, 0, 0};
+                           (int32_t)plan.chunks_each, plan.parts, q->bias_dtype, 0, 0, 0, 0};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     float* w = static_cast<float*>(q->workspace);
     const hipError_t e = q->out_dtype == FH_F32 ? product_of<float>(p, plan, w, s) : product_of<Bf16>(p, plan, w, s);

@@ -15,18 +15,21 @@ constexpr int kThreads = 256;
 constexpr int64_t kMostGridY = 65535;
 template <int LANES>
 __device__ __forceinline__ int64_t row_of_thread() { return ((int64_t)blockIdx.z * kMostGridY + blockIdx.y) * (kThreads / LANES) + threadIdx.x / LANES; }
-inline bool grid_of(int64_t rows, int64_t chunks, int lanes, dim3& grid)
+// part(first row, grid) for all rows, of which a workgroup takes kThreads / lanes.
+template <typename F>
+hipError_t by_rows_and_chunks(int64_t rows, int64_t chunks, int lanes, F part)
 {
-    const int64_t at_once = kThreads / lanes, groups = (rows + at_once - 1) / at_once, z = (groups + kMostGridY - 1) / kMostGridY;
-    if (z > kMostGridY || chunks > INT32_MAX) return false;
-    grid = dim3((uint32_t)chunks, (uint32_t)(z > 1 ? kMostGridY : groups), (uint32_t)z);
-    return true;
+    const int64_t each = kThreads / lanes;
+    return in_parts((rows + each - 1) / each, chunks * kThreads, [&](int64_t first, int64_t groups) {
+        const int64_t z = (groups + kMostGridY - 1) / kMostGridY;
+        return part(first * each, dim3((uint32_t)chunks, (uint32_t)(z > 1 ? kMostGridY : groups), (uint32_t)z));
+    });
 }
 
 template <typename T>
-__global__ __launch_bounds__(kThreads) void mx_rows_kernel(const T* x, int64_t rows, int64_t cols, int64_t stride, MxStore to)
+__global__ __launch_bounds__(kThreads) void mx_rows_kernel(const T* x, int64_t rows, int64_t cols, int64_t stride, MxStore to, int64_t first_row)
 {
-    const int64_t row = row_of_thread<32>(), first = (int64_t)blockIdx.x * kMxChunk + (threadIdx.x & 31) * 8;
+    const int64_t row = first_row + row_of_thread<32>(), first = (int64_t)blockIdx.x * kMxChunk + (threadIdx.x & 31) * 8;
     const bool write = row < rows;
     float v[8];
     load8(x + (write ? row : 0) * stride + first, write ? cols - first : 0, v);
@@ -46,10 +49,11 @@ template <typename T> constexpr int kTileCols = 256 / (int)sizeof(T);
 
 // A linear layer's bias has the sums of its output gradient's columns for gradient: they come with that gradient's codes, from the lanes
 // that hold the columns, a row of partial sums a tile, where a pass of their own read 8192 x 2304 once more.
-struct SumArgs { float* sums; };
+struct SumArgs { float* sums; uint32_t first_tile; };          // tiles of the launches before
+struct TileNormArgs { const void *weight, *bias; const float *mean, *rstd; int32_t p_dtype; uint32_t first_tile; };
 template <typename T, bool NORM, bool STOCHASTIC>
 __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4) void mx_tiles_kernel(const T* x, int64_t rows, int64_t cols, int64_t stride,
-                                                                   std::conditional_t<NORM, NormArgs, SumArgs> n,
+                                                                   std::conditional_t<NORM, TileNormArgs, SumArgs> n,
                                                                    uint32_t k0, uint32_t k1, uint32_t id0, uint32_t id1,
                                                                    uint8_t* rows_form, uint8_t* columns_form, uint32_t col_tiles, uint32_t tiles)
 {
@@ -63,7 +67,7 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // In fp32 a row's codes leave by 32 bytes a tile, so an XCD takes a run of neighbours, whose parts of a line meet in its L2
     // (8192 x 8192, both forms: 86 -> 71 us); the halves of bf16 lose by it (48 -> 50).
-    const uint32_t at = sizeof(T) == 4 ? run_of(blockIdx.x, tiles) : blockIdx.x;
+    const uint32_t at = n.first_tile + (sizeof(T) == 4 ? run_of(blockIdx.x, tiles) : blockIdx.x);
     const int64_t col_tile = at % col_tiles, row_tile = at / col_tiles;
     const int64_t r0 = row_tile * kTileRows + wave * 32, c0 = col_tile * kCols;
     const bool whole = r0 + 32 <= rows && c0 + kCols <= cols;
@@ -263,10 +267,10 @@ __global__ __launch_bounds__(kTileThreads, STOCHASTIC && sizeof(T) == 2 ? 2 : 4)
 
 // 16 bytes of output a lane and row: 4 values in fp32, 8 in bf16; ROWS neighbouring rows a lane (a power of two: their scales are in one group).
 template <typename T, int ROWS>
-__global__ __launch_bounds__(kThreads) void mx_restore_kernel(MxStore from, int64_t rows, int64_t cols, T* out, int64_t stride)
+__global__ __launch_bounds__(kThreads) void mx_restore_kernel(MxStore from, int64_t rows, int64_t cols, T* out, int64_t stride, int64_t first_row)
 {
     constexpr int kEach = 16 / (int)sizeof(T), kLanes = kMxChunk / kEach;
-    const int64_t row = row_of_thread<kLanes>() * ROWS, first = (int64_t)blockIdx.x * kMxChunk + (threadIdx.x % kLanes) * kEach;
+    const int64_t row = first_row + row_of_thread<kLanes>() * ROWS, first = (int64_t)blockIdx.x * kMxChunk + (threadIdx.x % kLanes) * kEach;
     if (row >= rows || first >= cols) return;
     const uint8_t* at = from.codes + row * (from.chunks * 128) + (first >> 1);
     const uint8_t* at_scale = from.scales + mx_scale_at(row, first >> 5, from.chunks);
@@ -300,30 +304,33 @@ __global__ __launch_bounds__(kThreads) void mx_restore_kernel(MxStore from, int6
 template <typename T>
 hipError_t rows_of(const void* x, int64_t rows, int64_t cols, int64_t stride, const MxStore& to, hipStream_t s)
 {
-    dim3 grid;
-    if (!grid_of(rows, to.chunks, 32, grid)) return hipErrorInvalidValue;
-    return launch(mx_rows_kernel<T>, grid, dim3(kThreads), s, static_cast<const T*>(x), rows, cols, stride, to);
+    return by_rows_and_chunks(rows, to.chunks, 32, [&](int64_t first, dim3 grid) {
+        return launch(mx_rows_kernel<T>, grid, dim3(kThreads), s, static_cast<const T*>(x), rows, cols, stride, to, first);
+    });
 }
 
 template <typename T, bool NORM, bool STOCHASTIC>
-hipError_t tiles_of(const void* x, int64_t rows, int64_t cols, int64_t stride, const std::conditional_t<NORM, NormArgs, SumArgs>& n, uint64_t seed, uint64_t id,
+hipError_t tiles_of(const void* x, int64_t rows, int64_t cols, int64_t stride, std::conditional_t<NORM, TileNormArgs, SumArgs> n, uint64_t seed, uint64_t id,
                     void* by_rows, void* by_columns, hipStream_t s)
 {
     // columns up to a whole chunk where rows are stored, rows up to a whole chunk where columns are
     const int64_t width = by_rows ? mx_chunks(cols) * kMxChunk : cols, col_tiles = (width + kTileCols<T> - 1) / kTileCols<T>;
     const int64_t row_tiles = mx_tile_rows(rows);
     if (col_tiles * row_tiles > INT32_MAX) return hipErrorInvalidValue;
-    return launch(mx_tiles_kernel<T, NORM, STOCHASTIC>, dim3((uint32_t)(col_tiles * row_tiles)), dim3(kTileThreads), s,
-                       static_cast<const T*>(x), rows, cols, stride, n, (uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)id,
-                       (uint32_t)(id >> 32), static_cast<uint8_t*>(by_rows), static_cast<uint8_t*>(by_columns), (uint32_t)col_tiles, (uint32_t)(col_tiles * row_tiles));
+    return in_parts(col_tiles * row_tiles, kTileThreads, [&](int64_t first, int64_t tiles) {
+        n.first_tile = (uint32_t)first;
+        return launch(mx_tiles_kernel<T, NORM, STOCHASTIC>, dim3((uint32_t)tiles), dim3(kTileThreads), s,
+                      static_cast<const T*>(x), rows, cols, stride, n, (uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)id,
+                      (uint32_t)(id >> 32), static_cast<uint8_t*>(by_rows), static_cast<uint8_t*>(by_columns), (uint32_t)col_tiles, (uint32_t)tiles);
+    });
 }
 
 template <typename T, int ROWS>
 hipError_t restore_by(const MxStore& from, int64_t rows, int64_t cols, void* out, int64_t stride, hipStream_t s)
 {
-    dim3 grid;
-    if (!grid_of((rows + ROWS - 1) / ROWS, from.chunks, sizeof(T) == 4 ? 64 : 32, grid)) return hipErrorInvalidValue;
-    return launch(mx_restore_kernel<T, ROWS>, grid, dim3(kThreads), s, from, rows, cols, static_cast<T*>(out), stride);
+    return by_rows_and_chunks((rows + ROWS - 1) / ROWS, from.chunks, sizeof(T) == 4 ? 64 : 32, [&](int64_t first, dim3 grid) {
+        return launch(mx_restore_kernel<T, ROWS>, grid, dim3(kThreads), s, from, rows, cols, static_cast<T*>(out), stride, first * ROWS);
+    });
 }
 // Four rows a lane once there are workgroups enough: addresses and bounds are worked out once for them (fp32, one row and four: 30000 x 2048
 // 61.3 and 55.4 us, 100000 x 64 14.1 and 9.8, but 8192 x 1024 7.2 and 7.5, 1000 x 4095 5.3 and 5.5; bf16 33.5 and 32.6, 8.2 and 6.8, 5.2 and 5.2, 3.8 and 4.1).
@@ -360,15 +367,16 @@ fh_status check_input(const void* x, int x_dtype, int64_t rows, int64_t cols, in
 hipError_t launch_mx_tiles(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, const NormArgs* n, float* sums,
                            bool stochastic, uint64_t seed, uint64_t id, void* by_rows, void* by_columns, hipStream_t s)
 {
-    const SumArgs none = {sums};
+    const SumArgs none = {sums, 0};
+    const TileNormArgs norm = n ? TileNormArgs{n->weight, n->bias, n->mean, n->rstd, n->p_dtype, 0} : TileNormArgs{};
     if (dtype == FH_F32) {
-        if (n) return stochastic ? tiles_of<float, true, true>(x, rows, cols, stride, *n, seed, id, by_rows, by_columns, s)
-                                 : tiles_of<float, true, false>(x, rows, cols, stride, *n, seed, id, by_rows, by_columns, s);
+        if (n) return stochastic ? tiles_of<float, true, true>(x, rows, cols, stride, norm, seed, id, by_rows, by_columns, s)
+                                 : tiles_of<float, true, false>(x, rows, cols, stride, norm, seed, id, by_rows, by_columns, s);
         return stochastic ? tiles_of<float, false, true>(x, rows, cols, stride, none, seed, id, by_rows, by_columns, s)
                           : tiles_of<float, false, false>(x, rows, cols, stride, none, seed, id, by_rows, by_columns, s);
     }
-    if (n) return stochastic ? tiles_of<Bf16, true, true>(x, rows, cols, stride, *n, seed, id, by_rows, by_columns, s)
-                             : tiles_of<Bf16, true, false>(x, rows, cols, stride, *n, seed, id, by_rows, by_columns, s);
+    if (n) return stochastic ? tiles_of<Bf16, true, true>(x, rows, cols, stride, norm, seed, id, by_rows, by_columns, s)
+                             : tiles_of<Bf16, true, false>(x, rows, cols, stride, norm, seed, id, by_rows, by_columns, s);
     return stochastic ? tiles_of<Bf16, false, true>(x, rows, cols, stride, none, seed, id, by_rows, by_columns, s)
                       : tiles_of<Bf16, false, false>(x, rows, cols, stride, none, seed, id, by_rows, by_columns, s);
 }

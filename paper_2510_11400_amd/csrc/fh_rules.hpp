@@ -27,6 +27,11 @@ inline int32_t marked_spans_per_wave(int64_t launch_spans, int64_t tensor_spans,
     return (int32_t)(spans < 1 ? 1 : spans > 8 ? 8 : spans);
 }
 
+// A launch has fewer than 2^32 threads: 2^22 workgroups of 1024 were refused, and of 2^22 + 4 the last ones never ran, with no error.  Work
+// of more than half of that, all dimensions multiplied, is launched in parts of whole workgroups; `threads` of one of them.
+constexpr uint64_t kLaunchThreads = (uint64_t)1 << 31;
+constexpr int64_t groups_at_once(int64_t threads) { return threads >= (int64_t)kLaunchThreads ? 1 : (int64_t)(kLaunchThreads / (uint64_t)threads); }
+
 // Tiles in runs.  Workgroups are dealt to the eight XCDs one by one.  Here a window of 8 * RUN of them takes as many tiles so that each XCD has RUN
 // consecutive ones, the windows following one another: what a launch has touched at any time is still one stretch of
 // memory, so that the codes written last are the ones that the restore begins with finds in the memory-side cache.
