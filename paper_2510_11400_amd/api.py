@@ -20,15 +20,30 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libfedhybrid.so")
 
-for _path in (_LIB_PATH, os.path.join(_HERE, "_fh_binding.so")):
-    if not os.path.exists(_path):
-        raise ImportError(
-            f"{_path} is missing: build it with `python -m paper_2510_11400_amd.build` "
-            "(hipcc, gfx950). There is no fallback implementation.")
+if not os.path.exists(_LIB_PATH):
+    raise ImportError(
+        f"{_LIB_PATH} is missing: build it with `python -m paper_2510_11400_amd.build` "
+        "(hipcc, gfx950). There is no fallback implementation.")
 
 _lib = ctypes.CDLL(_LIB_PATH)
 
-from . import _fh_binding as _binding  # noqa: E402  (finds the library loaded)
+
+class _NoBinding:
+    """In the place of the compiled binding where it cannot be loaded (it is built for one version of torch): the calls that go through it
+    raise, those that go through ctypes work."""
+
+    def __init__(self, why: BaseException):
+        self._why = why
+
+    def __getattr__(self, name: str):
+        raise ImportError(f"_fh_binding.so cannot be loaded ({self._why}): build it with `python -m paper_2510_11400_amd.build`. "
+                          "There is no fallback implementation.") from self._why
+
+
+try:
+    from . import _fh_binding as _binding  # finds the library loaded
+except ImportError as e:
+    _binding = _NoBinding(e)
 
 FH_F32, FH_BF16 = 0, 1
 FH_ROUND_NEAREST, FH_ROUND_STOCHASTIC = 0, 1
@@ -1339,7 +1354,8 @@ class MxMatrix:
         return self.data.numel()
 
 
-_binding.use(FedHybridError, MxMatrix)
+if not isinstance(_binding, _NoBinding):
+    _binding.use(FedHybridError, MxMatrix)
 
 
 def fh_mx_quantize(x: torch.Tensor, forms: str = "rows", rounding="nearest", seed: int = 0, tensor_id: int = 0, stream=None):

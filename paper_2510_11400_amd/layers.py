@@ -17,7 +17,8 @@ from typing import Optional
 
 import torch
 
-from . import _fh_binding as _binding, api
+from . import api
+from .api import _binding
 
 
 def _rows(x: torch.Tensor) -> torch.Tensor:
