@@ -42,7 +42,7 @@ __device__ __forceinline__ f32x16 mx_mfma32(u32x4 a, u32x4 b, uint32_t sa, uint3
 __device__ __forceinline__ void to_lds(uint32_t lds, u32x4 from, uint32_t offset, uint32_t moved)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(from), "s"(__builtin_amdgcn_readfirstlane(moved)) : "memory");
+                 :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(from), "s"(__builtin_amdgcn_readfirstlane(moved)) : "memory", "m0");
 }
 __device__ __forceinline__ u32x4 buffer_of(const uint8_t* p, uint32_t bytes)
 {
