@@ -93,12 +93,6 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v)
     v = umax(v, dpp<kQuadXor1>(v));
     return umax(v, dpp<kQuadXor2>(v));
 }
-__device__ __forceinline__ uint32_t row_max(uint32_t v)      // over 16 lanes
-{
-    v = quad_max(v);
-    v = umax(v, dpp<kHalfMirror>(v));
-    return umax(v, dpp<kRowMirror>(v));
-}
 template <int LANES>
 __device__ __forceinline__ float lane_sum(float v)           // over aligned runs of 8, 16, 32 or 64 lanes
 {
@@ -126,9 +120,7 @@ __device__ __forceinline__ uint32_t abs_bits(float v) { return __builtin_bit_cas
 // The hardware takes 16-byte accesses at any element's address; the types only say so to the compiler.
 typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
 typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
-typedef uint32_t u32_a2 __attribute__((aligned(2)));
 typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
-typedef f32x2 f32x2_a4 __attribute__((aligned(4)));
 
 struct Bf16 { uint16_t bits; };
 __device__ __forceinline__ float value(float v) { return v; }
@@ -250,13 +242,11 @@ __device__ __forceinline__ void store8(Bf16* p, int64_t n, const float (&v)[8])
     }
 }
 
-__device__ __forceinline__ void store_run(float* p, int64_t n, const float (&v)[4])
+__device__ __forceinline__ void store4(float* p, int64_t n, const float (&v)[4])
 {
     if (n >= 4) *reinterpret_cast<f32x4_a4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
     else for (int i = 0; i < 4; ++i) if (i < n) p[i] = v[i];
 }
-__device__ __forceinline__ void store_run(Bf16* p, int64_t n, const float (&v)[8]) { store8(p, n, v); }
-__device__ __forceinline__ void store4(float* p, int64_t n, const float (&v)[4]) { store_run(p, n, v); }
 __device__ __forceinline__ void store4(Bf16* p, int64_t n, const float (&v)[4])
 {
     if (n >= 4) *reinterpret_cast<u32x2_a2*>(p) = u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
