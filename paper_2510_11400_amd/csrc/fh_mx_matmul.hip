@@ -178,8 +178,9 @@ __device__ __forceinline__ void store_packed(T* p, int n, u32x4 v)
 #pragma unroll
         for (int i = 0; i < kRun; ++i)
             if (i < n) {
-                if constexpr (sizeof(T) == 4) p[i] = __builtin_bit_cast(float, v[i]);
-                else p[i].bits = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
+                const uint32_t w = v[i * (int)sizeof(T) / 4];    // a value of its own: bit_cast of a vector's element takes element 0 whichever is asked for
+                if constexpr (sizeof(T) == 4) p[i] = __builtin_bit_cast(float, w);
+                else p[i].bits = (uint16_t)(w >> (16 * (i & 1)));
             }
     }
 }
