@@ -584,9 +584,15 @@ hipError_t norm_any(const void* x, int64_t rows, int64_t cols, int64_t xs, const
     if (cols <= 1024) return norm_of<T, 64, 2, MX>(x, rows, cols, xs, n, to, s);
     if (cols <= 1536) return norm_of<T, 64, 3, MX>(x, rows, cols, xs, n, to, s);
     if (cols <= kWaveCols) return norm_of<T, 64, 4, MX>(x, rows, cols, xs, n, to, s);
-    if constexpr (MX) {                                          // a wave each for somewhat longer rows: 8192 x 2304 bf16 22.6 -> 17.9 us (dense 18.2, 19.2)
-        if (rows > 256 && cols <= 2560) return norm_of<T, 64, 5, MX>(x, rows, cols, xs, n, to, s);
-        if (rows > 256 && cols <= 3072) return norm_of<T, 64, 6, MX>(x, rows, cols, xs, n, to, s);
+    // Codes of somewhat longer rows by a wave each, where there are many.  By a wave and by two, us, for 1100, 1500, 1800, 3000, 8192, 20000 rows:
+    //   2100 columns bf16  6.9 6.7  7.1 6.8  7.2  9.7  12.3 12.5  22.0 26.3  41.8 51.6   fp32  6.0 5.8  6.7 6.1  6.7 8.4  11.3 12.1  19.9 22.8  47.8 50.6
+    //   2560               6.2 6.0  6.3 6.1  6.6  8.2  11.0 11.3  18.4 21.4  34.9 42.6         5.8 5.6  6.2 6.2  7.3 8.6  11.6 11.6  19.9 22.1  51.2 53.7
+    //   2600               7.1 6.2  7.2 6.4  7.5  8.8  12.7 11.9  21.2 22.2  38.6 44.2         6.4 5.8  7.1 6.6  7.8 9.0  12.7 12.3  21.3 23.0  54.6 55.2
+    //   3000               7.1 6.2  7.3 6.5  7.6  9.0  13.5 12.3  21.8 22.4  44.4 46.4         6.9 6.1  7.7 7.2  8.5 9.5  13.2 12.6  22.4 24.2  60.1 60.0
+    // (Dense rows gain nothing by it: 8192 x 2304 bf16 18.2 by two waves, 19.2 by one.)
+    if constexpr (MX) {
+        if (rows > 1536 && cols <= 2560) return norm_of<T, 64, 5, MX>(x, rows, cols, xs, n, to, s);
+        if (rows > 1536 && cols <= 3072) return norm_of<T, 64, 6, MX>(x, rows, cols, xs, n, to, s);
     }
     if (rows <= 256) {                                           // no more than a row a compute unit: all the threads it can use
         if (cols <= 4096) return norm_of<T, 512, 1, MX>(x, rows, cols, xs, n, to, s);

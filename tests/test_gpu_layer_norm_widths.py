@@ -79,7 +79,7 @@ def _values_of(x, mean, rstd, w, b):
 
 
 CODES = [(70001, 40), (9001, 250), (8301, 511), (5201, 1000), (4201, 1500), (3301, 2000), (4301, 2049), (4301, 2304), (4301, 2560), (4301, 2561), (4301, 3071), (1601, 3073),
-         (1601, 4096), (1101, 4097), (1101, 6145), (801, 8192), (521, 12289), (301, 16384)]
+         (1601, 4096), (1101, 4097), (1101, 6145), (801, 8192), (521, 12289), (301, 16384), (257, 2100), (1536, 2300), (1536, 2900)]
 
 
 @pytest.mark.parametrize("params", [False, True])
