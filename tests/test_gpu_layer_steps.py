@@ -1,6 +1,8 @@
 """Steps of the layers on the GPU: what precision, memory, streams and derivatives they keep to beside their values."""
 from __future__ import annotations
 
+import gc
+
 import numpy as np
 import pytest
 
@@ -228,7 +230,8 @@ def test_a_stream_that_is_the_current_one_changes_nothing(api):
 
 # ---- what is kept for the backward pass goes with it ------------------------------------------------------
 def _held(then):
-    """Bytes that `then` leaves allocated, and its result."""
+    """Bytes that `then` leaves allocated, and its result.  A block may be up to 1 MiB larger than what was asked for."""
+    gc.collect()
     torch.cuda.synchronize()
     before = torch.cuda.memory_allocated()
     result = then()
@@ -238,14 +241,14 @@ def _held(then):
 @pytest.mark.parametrize("norm", [False, True])
 def test_the_backward_pass_frees_what_was_kept(layers, api, norm):
     """Also where the graph outlives it: the output is still there, as a loss is through the next step's forward pass.  Of the step only
-    the output and the gradients are left, each in blocks of 512 bytes."""
+    the output and the two gradients are left."""
     g = torch.Generator(device="cuda").manual_seed(1)
-    x, w, dy = _randn(g, 2048, 768).requires_grad_(), _randn(g, 768, 768).requires_grad_(), _randn(g, 2048, 768)
-    operands = api.mx_bytes(768, 2048) + api.mx_bytes(768, 768)
+    x, w, dy = _randn(g, 16384, 768).requires_grad_(), _randn(g, 768, 768).requires_grad_(), _randn(g, 16384, 768)
+    operands = api.mx_bytes(768, 16384) + api.mx_bytes(768, 768)
     held, y = _held(lambda: layers.layer_norm_mx_linear(x, None, None, w) if norm else layers.mx_linear(x, w))
     assert held >= y.nbytes + operands
     left, grads = _held(lambda: torch.autograd.grad(y, (x, w), dy))
-    assert held + left < y.nbytes + sum(v.nbytes for v in grads) + 16384
+    assert held + left <= y.nbytes + sum(v.nbytes for v in grads) + 3 * 2 ** 20 < y.nbytes + sum(v.nbytes for v in grads) + operands
     with pytest.raises(RuntimeError, match="second time"):
         torch.autograd.grad(y, (x, w), dy)
 
@@ -262,10 +265,10 @@ def test_checkpointing_keeps_nothing(layers, api):
     """Recomputed in the backward pass, the operands are not held in between; the gradients are the same."""
     from torch.utils.checkpoint import checkpoint
     g = torch.Generator(device="cuda").manual_seed(1)
-    x, w, dy = _randn(g, 2048, 768).requires_grad_(), _randn(g, 768, 768).requires_grad_(), _randn(g, 2048, 768)
+    x, w, dy = _randn(g, 16384, 768).requires_grad_(), _randn(g, 768, 768).requires_grad_(), _randn(g, 16384, 768)
     want = torch.autograd.grad(layers.layer_norm_mx_linear(x, None, None, w), (x, w), dy)
     held, y = _held(lambda: checkpoint(layers.layer_norm_mx_linear, x, None, None, w, use_reentrant=False))
-    assert held < y.nbytes + api.mx_bytes(768, 2048)
+    assert held <= y.nbytes + 2 ** 20 < y.nbytes + api.mx_bytes(768, 16384)
     assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(y, (x, w), dy), want))
 
 

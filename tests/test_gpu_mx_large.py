@@ -106,3 +106,22 @@ def test_a_product_of_very_many_rows(api):
     want = api.fh_mx_matmul(last, w)
     right = torch.equal(out[-rows:], want[:rows]), not out[:-rows].any()
     assert right == (True, True)
+
+
+def test_codes_by_rows_of_very_many_rows(api):
+    """More rows than one dimension of the grid has workgroups for, and more than one launch has threads for: the values of the grid come back, and
+    the bytes are those that the kernel for both forms writes."""
+    _room(12)
+    print("[large] codes by rows", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x = torch.randn(600_001, 33, generator=g, device="cuda")
+    alone, both = api.fh_mx_quantize(x), api.fh_mx_quantize(x, "both")[0]
+    codes = api.mx_scales_offset(*x.shape)
+    right = torch.equal(alone.data[:codes + 600_001 // 32 * 256], both.data[:codes + 600_001 // 32 * 256])
+    assert right
+    del alone, both
+    rows = 2 ** 26 + 9
+    x = torch.ones((rows, 1), dtype=torch.bfloat16, device="cuda")
+    x[-7:, 0] = torch.tensor([0.0, -4.0, 6.0, 1.5, -0.5, 3.0, 2.0 ** 90], device="cuda")
+    right = torch.equal(api.fh_mx_dequantize(api.fh_mx_quantize(x), torch.bfloat16), x)
+    assert right

@@ -1,6 +1,7 @@
 """The rules by which the microscaled and layer norm calls shape their launches, looked at without a GPU."""
 from __future__ import annotations
 
+import ctypes
 import os
 import shutil
 import subprocess
@@ -67,3 +68,13 @@ def test_a_sums_parts_make_up_the_sum(tmp_path):
         assert api.mx_matmul_workspace_bytes(m, n, k) == (parts * m * n * 4 if parts > 1 else 0)
         split += parts > 1
     assert split > 20
+
+
+def test_a_split_product_is_refused_without_its_workspace():
+    m, n, k = 96, 97, 40000
+    need = api.mx_matmul_workspace_bytes(m, n, k)
+    fake, big = 0x10000, 1 << 40                                          # never dereferenced: the call is refused first
+    assert need > 0
+    for pointer, cap, status in ((None, big, 1), (fake, need - 1, 7), (fake + 4, big, 8)):
+        p = api.fh_mx_product(fake, big, fake, big, m, n, k, None, 0, 0, fake, n, big, pointer, cap, 0)
+        assert api.raw_library().fh_mx_matmul(ctypes.byref(p), None) == status
