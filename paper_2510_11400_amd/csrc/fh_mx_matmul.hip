@@ -28,8 +28,9 @@ struct ProductArgs {
 static_assert(sizeof(ProductArgs) <= 112, "longer arguments are enqueued a microsecond later");
 
 // v_mfma_scale_f32_32x32x64_f8f6f4: lane (r = lane % 32, h = lane / 32) brings 32 values of row r of each operand, and gets
-// the outputs [8 (i/4) + 4 h + i % 4][r].  It measured 7.0 PFLOP/s from registers, the 16 x 16 form 4.3.  Of a chunk's
-// eight blocks a lane takes 4h .. 4h+3, in four instructions, whose scales are the bytes of one word.
+// the outputs [8 (i/4) + 4 h + i % 4][r].  Of a chunk's
+// eight blocks a lane takes 4h .. 4h+3, in four instructions, whose scales are the bytes of one word.  From registers alone it measured 5.3 to 5.7 PFLOP/s on
+// operands of all kinds (7.2 on zeros), the 16 x 16 x 128 form 6.8 to 7.1 (8.8) with eight accumulators; the kernels have not been built on that one.
 template <int BYTE>
 __device__ __forceinline__ f32x16 mx_mfma32(u32x4 a, u32x4 b, uint32_t sa, uint32_t sb, f32x16 c)
 {

@@ -89,7 +89,7 @@ class LayerNormMxLinear(torch.nn.Module):
     """A layer norm and the linear layer behind it, trained in 4-bit blocks; `freeze()` stores the weights once for serving.
 
     With stochastic rounding of the gradients every step draws its own random numbers: the seed is `seed` plus the number
-    of forward passes so far, the tensor id `tensor_id`.  A frozen layer runs two kernels for any number of tokens."""
+    of forward passes so far, the tensor id `tensor_id` (a graph replays the numbers of its capture).  A frozen layer runs two kernels for any number of tokens."""
 
     def __init__(self, features: int, out_features: int, bias: bool = True, eps: float = 1e-5, rounding="nearest", seed: int = 0,
                  tensor_id: int = 0, device=None, dtype=None):
