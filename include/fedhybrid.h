@@ -64,7 +64,7 @@ typedef enum fh_status {
     FH_ERR_BAD_COUNT = 10,       /* negative item count */
     FH_ERR_BAD_SHAPE = 11,       /* outer / channels / inner / raw_channels, or rows / cols / a row stride out of range */
     FH_ERR_BAD_PARAM = 12,       /* k_sigma not positive, min_outliers < 1, a pooling window other than 2, 4, 8, a negative eps
-                                    of a norm, or a reserved field that is not 0 */
+                                    of a norm, a layer's flag that is none, or a reserved field that is not 0 */
     FH_ERR_SCRATCH_LIMIT = 13    /* the tensor needs more scratch than the library's static buffer holds */
 } fh_status;
 

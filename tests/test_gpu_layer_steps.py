@@ -361,3 +361,23 @@ def test_no_tokens_for_some_gradients(layers, norm, needed):
     y = layers.layer_norm_mx_linear(x, None, None, w) if norm else layers.mx_linear(x, w)
     grads = torch.autograd.grad(y, [t for t, n in zip((x, w), needed) if n], torch.empty(0, 7, device="cuda"))
     assert y.shape == (0, 7) and all(not v.any() for v in grads)
+
+
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("tokens, features, out", [(34, 100, 300), (300, 768, 64), (2600, 770, 777)])
+def test_the_step_of_autograd_is_the_layers_calls(layers, api, tokens, features, out, norm):
+    """Output and every gradient in bf16, bit for bit: with test_the_layer_calls_are_their_parts, and the parts' own bounds, no tolerance is left for what
+    lies between.  The last shape goes through the larger kernels of the product."""
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    x, dy = _randn(g, 2, tokens // 2, features), _randn(g, 2, tokens // 2, out)
+    w, b, nw, nb = (_randn(g, *s) for s in ((out, features), (out,), (features,), (features,)))
+    leaves = [v.clone().requires_grad_() for v in ((x, nw, nb, w, b) if norm else (x, w, b))]
+    how = dict(rounding="stochastic", seed=5, tensor_id=6)
+    y = layers.layer_norm_mx_linear(*leaves, **how) if norm else layers.mx_linear(*leaves, **how)
+    got = torch.autograd.grad(y, leaves, dy)
+    xm, gm = x.view(-1, features), dy.view(-1, out)
+    layer = api.MxLayer(xm, w, b, norm, nw if norm else None, nb if norm else None, wide_gradient=True, **how)
+    assert torch.equal(y.view(-1, out), layer.forward())
+    dx, dw, dnw, dnb, db = layer.backward(gm, xm if norm else None, nw if norm else None, bias=True)
+    want = (dx.view(x.shape), dnw, dnb, dw, db) if norm else (dx.view(x.shape), dw, db)
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
