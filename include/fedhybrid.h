@@ -64,7 +64,7 @@ typedef enum fh_status {
     FH_ERR_BAD_COUNT = 10,       /* negative item count */
     FH_ERR_BAD_SHAPE = 11,       /* outer / channels / inner / raw_channels, or rows / cols / a row stride out of range */
     FH_ERR_BAD_PARAM = 12,       /* k_sigma not positive, min_outliers < 1, a pooling window other than 2, 4, 8, a negative eps
-                                    of a norm, a layer's flag that is none, or a reserved field that is not 0 */
+                                    of a norm, a layer's flag or activation that is none, or a reserved field that is not 0 */
     FH_ERR_SCRATCH_LIMIT = 13    /* the tensor needs more scratch than the library's static buffer holds */
 } fh_status;
 
@@ -622,6 +622,103 @@ size_t    fh_mx_layer_scratch_bytes(int64_t tokens, int64_t features, int64_t ou
 fh_status fh_mx_layer_sizes(const fh_mx_layer *layer, size_t *kept, size_t *forward_scratch, size_t *backward_scratch);
 fh_status fh_mx_layer_forward(const fh_mx_layer *layer, void *stream);
 fh_status fh_mx_layer_backward(const fh_mx_layer *layer, void *stream);
+
+/* ---- 8-bit integer storage and its products ------------------------------------------------------
+ * A matrix of rows x cols with a scale for each row (a token of an activation, an output channel of a
+ * weight).  All arithmetic is binary32:
+ *
+ *   - top = the largest magnitude of the row; scale = top / 127, code = rint(v * (127 / top)), ties to
+ *     even; top below 2^-100: scale 0, codes 0; a row that holds a NaN or an infinity has the scale NaN
+ *     and codes 0: every sum that it enters is NaN;
+ *   - a code is a signed byte; rows are padded with zeros to a multiple of 128 of them; row r's begin at
+ *     byte r * 128 * ceil(cols/128);
+ *   - the scales (float, a value per row) follow at fh_q8_scales_offset().
+ *
+ * fh_q8_quantize stores x (row r from element r * row_stride on, row_stride >= cols).
+ * fh_q8_dequantize restores value = code * scale, rounded to out_dtype.
+ * fh_q8_matmul computes out[i][j] = (sum_k a[i][k] b[j][k]) * (a's scale i * b's scale j) + bias[j] of
+ * the stored matrices a (m x k) and b (n x k): the sum in integers, which is exact, then in binary32,
+ * rounded once to out_dtype.  bias may be NULL.
+ * fh_q8_gated computes out[i][j] = act(gate[i][j]) * up[i][j] of two such products (with their biases)
+ * of one x (m x k) and the weights gate and up (n x k each), in one pass.
+ *   act (fh_activation): FH_SILU g / (1 + e^-g); FH_GELU g times the normal distribution function at g;
+ *   FH_GELU_TANH (g / 2) (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))).
+ * k = 0: the products are their biases, or zeros.
+ *
+ * Stored matrices and workspaces are 16-byte aligned, plain matrices and vectors aligned to their
+ * elements.  rows, cols <= 2^31 - 256 (products: k <= 2^17 - 1, so that no sum overflows);
+ * row_stride <= 2^31.  Nothing is launched where there is no output. */
+typedef enum fh_activation { FH_SILU = 0, FH_GELU = 1, FH_GELU_TANH = 2 } fh_activation;
+size_t    fh_q8_bytes(int64_t rows, int64_t cols);             /* of a stored matrix; 0 for a bad shape */
+size_t    fh_q8_scales_offset(int64_t rows, int64_t cols);
+fh_status fh_q8_quantize(const void *x, fh_dtype x_dtype, int64_t rows, int64_t cols, int64_t row_stride, void *stored, size_t stored_cap,
+                         void *stream);
+fh_status fh_q8_dequantize(const void *stored, size_t stored_cap, int64_t rows, int64_t cols, fh_dtype out_dtype,
+                           void *out, int64_t row_stride, size_t out_cap, void *stream);
+typedef struct fh_q8_product {
+    const void *a;          size_t a_cap;       /* >= fh_q8_bytes(m, k) */
+    const void *b;          size_t b_cap;       /* >= fh_q8_bytes(n, k) */
+    int64_t     m, n, k;
+    const void *bias;                           /* NULL, or n values of bias_dtype */
+    int32_t     bias_dtype; int32_t out_dtype;  /* fh_dtype */
+    void       *out;        int64_t stride;     /* row i from element i * stride on, stride >= n */
+    size_t      out_cap;
+    void       *workspace;  size_t workspace_cap;   /* >= fh_q8_matmul_workspace_bytes(m, n, k), NULL if that is 0 */
+    int64_t     reserved;                       /* 0 */
+} fh_q8_product;
+typedef struct fh_q8_gated_product {
+    const void *x;          size_t x_cap;       /* >= fh_q8_bytes(m, k) */
+    const void *gate;       size_t gate_cap;    /* >= fh_q8_bytes(n, k) */
+    const void *up;         size_t up_cap;      /* >= fh_q8_bytes(n, k) */
+    int64_t     m, n, k;
+    const void *gate_bias, *up_bias;            /* NULL, or n values of bias_dtype */
+    int32_t     bias_dtype; int32_t out_dtype;  /* fh_dtype */
+    int32_t     activation; int32_t reserved;   /* fh_activation; 0 */
+    void       *out;        int64_t stride;
+    size_t      out_cap;
+    void       *workspace;  size_t workspace_cap;   /* >= fh_q8_gated_workspace_bytes(m, n, k), NULL if that is 0 */
+    int64_t     reserved2;                      /* 0 */
+} fh_q8_gated_product;
+size_t    fh_q8_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k);
+size_t    fh_q8_gated_workspace_bytes(int64_t m, int64_t n, int64_t k);
+fh_status fh_q8_matmul(const fh_q8_product *product, void *stream);
+fh_status fh_q8_gated(const fh_q8_gated_product *product, void *stream);
+
+/* ---- the gated projection of dense matrices, and its backward pass ----------------------------------
+ * gate = x Wg^T + bg,  up = x Wu^T + bu,  h = act(gate) * up, all in binary32, rounded once to dtype.
+ * fh_gated writes h.  fh_gated_backward computes from x, the weights, the biases and dh alone (gate and
+ * up are computed again; a forward call leaves nothing behind for it)
+ *   dgate = dh up act'(gate),  dup = dh act(gate), rounded to dtype for the products that follow:
+ *   dx = dgate Wg + dup Wu (with FH_GATED_NEEDS_INPUT),
+ *   dw_gate = dgate^T x,  dw_up = dup^T x (with FH_GATED_NEEDS_WEIGHT),
+ *   db_gate, db_up (each where it is not NULL): sums over the tokens, from before that rounding,
+ * with sums in binary32, each rounded once to dtype.
+ * x: tokens x features, w_gate and w_up: hidden x features, h and dh: tokens x hidden, rows contiguous with
+ * row strides; dx, dw_gate and dw_up are dense.  Everything is of dtype; b_gate and b_up may be NULL.
+ * tokens <= 2^21, 1 <= features, hidden <= 2^20, row strides <= 2^31.  tokens = 0 writes zeros to the
+ * gradients of the parameters that are asked for.  The sums' order depends on the shapes, the strides and
+ * the pointers' alignment alone.  No output may overlap another pointer's memory.
+ * fh_gated_workspace_bytes: of the forward (backward = 0) or the backward call with this layer; it looks at the
+ * shape, the strides, needs, at whether db_gate and db_up are NULL, and at the operands' addresses, not at what
+ * is there; 0 for a layer that the call refuses.  The workspace is 16-byte aligned and free again once the call's work has run. */
+#define FH_GATED_NEEDS_INPUT  1
+#define FH_GATED_NEEDS_WEIGHT 2
+typedef struct fh_gated_layer {
+    int64_t     tokens, features, hidden;
+    int32_t     dtype;      int32_t activation; /* fh_dtype; fh_activation */
+    int32_t     needs;      int32_t reserved;   /* backward: FH_GATED_NEEDS_*; 0 */
+    const void *x;          int64_t x_stride;
+    const void *w_gate;     int64_t w_gate_stride;
+    const void *w_up;       int64_t w_up_stride;
+    const void *b_gate, *b_up;
+    void       *h;          int64_t h_stride;   size_t h_cap;   /* forward */
+    const void *dh;         int64_t dh_stride;  /* backward, as all that follow but the workspace */
+    void       *dx, *dw_gate, *dw_up, *db_gate, *db_up;
+    void       *workspace;  size_t workspace_cap;
+} fh_gated_layer;
+size_t    fh_gated_workspace_bytes(const fh_gated_layer *layer, int32_t backward);
+fh_status fh_gated(const fh_gated_layer *layer, void *stream);
+fh_status fh_gated_backward(const fh_gated_layer *layer, void *stream);
 
 const char *fh_status_string(fh_status s);
 

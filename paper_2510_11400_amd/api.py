@@ -62,6 +62,8 @@ EXPORTS = ("fh_packed_bytes", "fh_meta_bytes", "fh_compress", "fh_decompress", "
            "fh_mx_bytes", "fh_mx_scales_offset", "fh_mx_quantize", "fh_mx_dequantize", "fh_mx_matmul_workspace_bytes", "fh_mx_matmul",
            "fh_layer_norm", "fh_layer_norm_mx", "fh_layer_norm_backward_workspace_bytes", "fh_layer_norm_backward",
            "fh_mx_layer_kept_bytes", "fh_mx_layer_scratch_bytes", "fh_mx_layer_sizes", "fh_mx_layer_forward", "fh_mx_layer_backward",
+           "fh_q8_bytes", "fh_q8_scales_offset", "fh_q8_quantize", "fh_q8_dequantize", "fh_q8_matmul_workspace_bytes", "fh_q8_gated_workspace_bytes",
+           "fh_q8_matmul", "fh_q8_gated", "fh_gated_workspace_bytes", "fh_gated", "fh_gated_backward",
            "fh_status_string")
 
 
@@ -303,6 +305,47 @@ class fh_mx_layer(ctypes.Structure):
                 ("reserved", ctypes.c_int64), ("dbias", ctypes.c_void_p), ("wide_gradient", ctypes.c_int32), ("kept_for", ctypes.c_int32)]
 
 
+class fh_q8_product(ctypes.Structure):
+    _fields_ = list(fh_mx_product._fields_)
+
+
+class fh_q8_gated_product(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("x_cap", ctypes.c_size_t), ("gate", ctypes.c_void_p), ("gate_cap", ctypes.c_size_t),
+                ("up", ctypes.c_void_p), ("up_cap", ctypes.c_size_t), ("m", ctypes.c_int64), ("n", ctypes.c_int64), ("k", ctypes.c_int64),
+                ("gate_bias", ctypes.c_void_p), ("up_bias", ctypes.c_void_p), ("bias_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("activation", ctypes.c_int32), ("reserved", ctypes.c_int32), ("out", ctypes.c_void_p), ("stride", ctypes.c_int64),
+                ("out_cap", ctypes.c_size_t), ("workspace", ctypes.c_void_p), ("workspace_cap", ctypes.c_size_t), ("reserved2", ctypes.c_int64)]
+
+
+class fh_gated_layer(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("features", ctypes.c_int64), ("hidden", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("needs", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("x", ctypes.c_void_p), ("x_stride", ctypes.c_int64), ("w_gate", ctypes.c_void_p), ("w_gate_stride", ctypes.c_int64),
+                ("w_up", ctypes.c_void_p), ("w_up_stride", ctypes.c_int64), ("b_gate", ctypes.c_void_p), ("b_up", ctypes.c_void_p),
+                ("h", ctypes.c_void_p), ("h_stride", ctypes.c_int64), ("h_cap", ctypes.c_size_t),
+                ("dh", ctypes.c_void_p), ("dh_stride", ctypes.c_int64), ("dx", ctypes.c_void_p), ("dw_gate", ctypes.c_void_p),
+                ("dw_up", ctypes.c_void_p), ("db_gate", ctypes.c_void_p), ("db_up", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_cap", ctypes.c_size_t)]
+
+
+for _name in ("fh_q8_bytes", "fh_q8_scales_offset"):
+    getattr(_lib, _name).argtypes = [ctypes.c_int64, ctypes.c_int64]
+    getattr(_lib, _name).restype = ctypes.c_size_t
+for _name in ("fh_q8_matmul_workspace_bytes", "fh_q8_gated_workspace_bytes"):
+    getattr(_lib, _name).argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64]
+    getattr(_lib, _name).restype = ctypes.c_size_t
+_lib.fh_q8_quantize.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t,
+                                ctypes.c_void_p]
+_lib.fh_q8_dequantize.argtypes = [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64, ctypes.c_int64, ctypes.c_int, ctypes.c_void_p,
+                                  ctypes.c_int64, ctypes.c_size_t, ctypes.c_void_p]
+_lib.fh_q8_matmul.argtypes = [_P(fh_q8_product), ctypes.c_void_p]
+_lib.fh_q8_gated.argtypes = [_P(fh_q8_gated_product), ctypes.c_void_p]
+_lib.fh_gated_workspace_bytes.argtypes = [_P(fh_gated_layer), ctypes.c_int32]
+_lib.fh_gated_workspace_bytes.restype = ctypes.c_size_t
+for _name in ("fh_gated", "fh_gated_backward"):
+    getattr(_lib, _name).argtypes = [_P(fh_gated_layer), ctypes.c_void_p]
+for _name in ("fh_q8_quantize", "fh_q8_dequantize", "fh_q8_matmul", "fh_q8_gated", "fh_gated", "fh_gated_backward"):
+    getattr(_lib, _name).restype = ctypes.c_int
 for _name in ("fh_mx_layer_kept_bytes", "fh_mx_layer_scratch_bytes"):
     getattr(_lib, _name).argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64]
     getattr(_lib, _name).restype = ctypes.c_size_t
@@ -1354,8 +1397,20 @@ class MxMatrix:
         return self.data.numel()
 
 
+class Q8Matrix:
+    """A matrix of rows x cols in 8-bit integers with a scale per row: `data` holds the codes and, behind them, the scales."""
+    __slots__ = ("data", "rows", "cols")
+
+    def __init__(self, data: torch.Tensor, rows: int, cols: int):
+        self.data, self.rows, self.cols = data, rows, cols
+
+    @property
+    def nbytes(self) -> int:
+        return self.data.numel()
+
+
 if not isinstance(_binding, _NoBinding):
-    _binding.use(FedHybridError, MxMatrix)
+    _binding.use(FedHybridError, MxMatrix, Q8Matrix)
 
 
 def fh_mx_quantize(x: torch.Tensor, forms: str = "rows", rounding="nearest", seed: int = 0, tensor_id: int = 0, stream=None):
@@ -1440,3 +1495,62 @@ class MxLayer:
         grads = _binding.layer_backward(dy, x, norm_weight, self.kept, self.features, self.p_dtype, self.norm, self.eps, self.needs_input,
                                         self.needs_weight, bias, *self.rounding, self.wide_gradient, self.kept_for, stream)
         return grads if bias else grads[:4]
+
+
+# ---- 8-bit integer storage, its products, the gated projection ----------------------------------------------
+def q8_scales_offset(rows: int, cols: int) -> int:
+    """Where the scales begin in a stored matrix."""
+    return (cols + 127) // 128 * 128 * rows if 0 <= rows <= _MOST and 0 <= cols <= _MOST else 0
+
+
+def q8_bytes(rows: int, cols: int) -> int:
+    """Bytes of a stored matrix of rows x cols: one for a value (rows padded to multiples of 128) and four for a row."""
+    return ((cols + 127) // 128 * 128 + 4) * rows if 0 <= rows <= _MOST and 0 < cols <= _MOST else 0
+
+
+def fh_q8_quantize(x: torch.Tensor, stream=None) -> Q8Matrix:
+    """Enqueue the quantisation of the matrix x (rows contiguous, any row stride) to 8-bit integers, a scale for each row."""
+    return _binding.q8_quantize(x, stream)
+
+
+def fh_q8_dequantize(m: Q8Matrix, out_dtype=torch.float32, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Enqueue the restoration of a stored matrix; returns it as [rows, cols]."""
+    return _binding.q8_dequantize(m, out_dtype, out, stream)
+
+
+def q8_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
+    return _lib.fh_q8_matmul_workspace_bytes(m, n, k)
+
+
+def fh_q8_matmul(a: Q8Matrix, b: Q8Matrix, bias: Optional[torch.Tensor] = None, out_dtype=torch.bfloat16,
+                 out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Enqueue out = a b^T + bias of two stored matrices: sums in integers, both rows' scales applied to each."""
+    return _binding.q8_matmul(a, b, bias, out_dtype, out, workspace, stream)
+
+
+def q8_gated_workspace_bytes(tokens: int, hidden: int, features: int) -> int:
+    return _lib.fh_q8_gated_workspace_bytes(tokens, hidden, features)
+
+
+def fh_q8_gated(x: Q8Matrix, w_gate: Q8Matrix, w_up: Q8Matrix, b_gate: Optional[torch.Tensor] = None, b_up: Optional[torch.Tensor] = None,
+                activation: str = "silu", out_dtype=torch.bfloat16, out: Optional[torch.Tensor] = None,
+                workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Enqueue the gated projection act(x w_gate^T + b_gate) * (x w_up^T + b_up) of stored matrices in one kernel; activation "silu",
+    "gelu" (by the normal distribution function) or "gelu_tanh"."""
+    return _binding.q8_gated(x, w_gate, w_up, b_gate, b_up, activation, out_dtype, out, workspace, stream)
+
+
+def fh_gated(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, b_gate: Optional[torch.Tensor] = None,
+             b_up: Optional[torch.Tensor] = None, activation: str = "silu", out: Optional[torch.Tensor] = None,
+             workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Enqueue the gated projection act(x w_gate^T + b_gate) * (x w_up^T + b_up) of dense matrices of one dtype (rows contiguous, any row
+    strides); sums in fp32.  Without `workspace` one is allocated where the operands' alignment asks for it."""
+    return _binding.gated(x, w_gate, w_up, b_gate, b_up, activation, out, workspace, stream)
+
+
+def fh_gated_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, b_gate: Optional[torch.Tensor] = None,
+                      b_up: Optional[torch.Tensor] = None, activation: str = "silu", needs_input: bool = True, needs_weight: bool = True,
+                      needs_bias: bool = True, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Enqueue the backward pass of fh_gated from its inputs and its result's gradient; returns (dx, dw_gate, dw_up, db_gate, db_up), None for
+    what is not needed and for the gradient of a bias that is not there."""
+    return _binding.gated_backward(dh, x, w_gate, w_up, b_gate, b_up, activation, needs_input, needs_weight, needs_bias, workspace, stream)

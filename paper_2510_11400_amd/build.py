@@ -19,7 +19,7 @@ LIB = os.path.join(HERE, "libfedhybrid.so")
 BINDING = os.path.join(HERE, "_fh_binding.so")
 SOURCES = ("fh_abi.hip", "fh_compress.hip", "fh_decompress.hip", "fh_classify.hip", "fh_mixed.hip", "fh_sparse.hip",
            "fh_huffman.hip", "fh_chain.hip", "fh_mx_quantize.hip", "fh_mx_matmul.hip", "fh_layer_norm.hip",
-           "fh_mx_layer.hip")
+           "fh_mx_layer.hip", "fh_q8_quantize.hip", "fh_q8_matmul.hip", "fh_gated.hip")
 
 # Strict binary32 semantics on the device: no contraction (the one fused multiply-add
 # of the method is written explicitly), IEEE division, denormals kept.  Packed-fp32

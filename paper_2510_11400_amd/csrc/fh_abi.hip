@@ -249,11 +249,11 @@ const char* fh_status_string(fh_status s)
         case FH_ERR_BAD_ROUND: return "rounding must be FH_ROUND_NEAREST or FH_ROUND_STOCHASTIC";
         case FH_ERR_BAD_NUMEL: return "numel is negative or too large";
         case FH_ERR_BUFFER_TOO_SMALL: return "an output or input buffer capacity is too small";
-        case FH_ERR_ALIGNMENT: return "x, packed and out must be 16-byte aligned, meta 8-byte aligned (microscaled storage 16, plain matrices their elements)";
+        case FH_ERR_ALIGNMENT: return "x, packed and out must be 16-byte aligned, meta 8-byte aligned (microscaled and 8-bit storage 16, plain matrices their elements)";
         case FH_ERR_LAUNCH: return "the HIP runtime refused the kernel launch";
         case FH_ERR_BAD_COUNT: return "item count is negative";
         case FH_ERR_BAD_SHAPE: return "outer / maps must be >= 0, inner / h / w >= 1, channels in 1..16384, raw_channels in 0..channels; rows, cols and row strides within their limits";
-        case FH_ERR_BAD_PARAM: return "k_sigma must be positive, min_outliers at least 1, the pooling window 2, 4 or 8, a norm's eps not negative, a layer's flags among theirs, every reserved field 0";
+        case FH_ERR_BAD_PARAM: return "k_sigma must be positive, min_outliers at least 1, the pooling window 2, 4 or 8, a norm's eps not negative, a layer's flags and activation among theirs, every reserved field 0";
         case FH_ERR_SCRATCH_LIMIT: return "the tensor needs more scratch than the library's static buffer holds";
     }
     return "unknown status";

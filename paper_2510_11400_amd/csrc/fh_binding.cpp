@@ -20,7 +20,7 @@
 namespace {
 
 PyObject* g_error;                       // FedHybridError(status)
-PyObject* g_matrix;                      // MxMatrix(data, rows, cols)
+PyObject *g_matrix, *g_q8_matrix;        // MxMatrix(data, rows, cols), Q8Matrix(data, rows, cols)
 PyObject *g_data, *g_rows, *g_cols, *g_cuda_stream, *g_nearest, *g_stochastic;     // interned names
 
 // The interpreter's lock; autograd's threads come without it.
@@ -226,10 +226,10 @@ struct On {
     static c10::Stream as_recorded(const c10::hip::HIPStream& s) { return c10::Stream::unpack3(s.id(), s.device_index(), c10::DeviceType::CUDA); }
 };
 
-Ref wrapped_matrix(const at::Tensor& data, int64_t rows, int64_t cols)
+Ref wrapped_matrix(const at::Tensor& data, int64_t rows, int64_t cols, PyObject* of = g_matrix)
 {
     Ref d(THPVariable_Wrap(data)), r(PyLong_FromLongLong(rows)), c(PyLong_FromLongLong(cols));
-    PyTypeObject* type = reinterpret_cast<PyTypeObject*>(g_matrix);      // filled here: its __init__ is interpreted, 0.1 us of a call
+    PyTypeObject* type = reinterpret_cast<PyTypeObject*>(of);      // filled here: its __init__ is interpreted, 0.1 us of a call
     Ref m(type->tp_alloc(type, 0));
     if (PyObject_SetAttr(m.p, g_data, d.p) < 0 || PyObject_SetAttr(m.p, g_rows, r.p) < 0 || PyObject_SetAttr(m.p, g_cols, c.p) < 0) throw python_error();
     return m;
@@ -244,10 +244,13 @@ PyObject* tuple(R&&... r)
     return t;
 }
 
-// A stored matrix, MxMatrix in Python.
+// A stored matrix, MxMatrix or Q8Matrix in Python.
 struct Stored { at::Tensor data; int64_t rows, cols; };
-Stored stored(PyObject* o, const char* what)
+Stored stored(PyObject* o, const char* what, PyObject* of = g_matrix)
 {
+    // the two lie differently, and one's bytes are enough for the other's check of sizes
+    if (PyObject_TypeCheck(o, reinterpret_cast<PyTypeObject*>(of == g_matrix ? g_q8_matrix : g_matrix)))
+        raise(PyExc_TypeError, "%s must be stored as %s (got %s)", what, reinterpret_cast<PyTypeObject*>(of)->tp_name, Py_TYPE(o)->tp_name);
     Stored s;
     s.data = tensor(attribute(o, g_data).p, what);
     s.rows = i64(attribute(o, g_rows).p);
@@ -709,16 +712,197 @@ FH_ENTRY(mx_linear, 9)
     return wrap(y);
 FH_EXIT
 
-// (FedHybridError, MxMatrix): the classes that results and errors are of.
-FH_ENTRY(use, 2)
+// ---- 8-bit integer storage, its products, the gated projection ----------------------------------
+int activation_of(PyObject* o)
+{
+    const char* s = PyUnicode_Check(o) ? PyUnicode_AsUTF8(o) : nullptr;
+    if (s) {
+        if (!strcmp(s, "silu")) return FH_SILU;
+        if (!strcmp(s, "gelu")) return FH_GELU;
+        if (!strcmp(s, "gelu_tanh")) return FH_GELU_TANH;
+    }
+    PyErr_Clear();
+    raise(PyExc_ValueError, "activation must be 'silu', 'gelu' or 'gelu_tanh' (got %R)", o);
+}
+// The two biases of a gated projection: of one dtype; either may be undefined.
+struct Biases {
+    at::Tensor gate, up;
+    void *g, *u;
+    int dtype;
+    Biases(PyObject* go, PyObject* uo, int64_t n, c10::Device device) : gate(tensor_or_none(go, "b_gate")), up(tensor_or_none(uo, "b_up"))
+    {
+        if (gate.defined() && up.defined() && gate.scalar_type() != up.scalar_type())
+            raise(PyExc_TypeError, "b_gate and b_up have different dtypes (%s, %s)", c10::toString(gate.scalar_type()), c10::toString(up.scalar_type()));
+        g = vector(gate, n, device, "b_gate");
+        u = vector(up, n, device, "b_up");
+        dtype = gate.defined() ? dtype_code(gate.scalar_type()) : up.defined() ? dtype_code(up.scalar_type()) : FH_F32;
+    }
+};
+// `given`, which has to be rows x cols, or a new matrix.
+Matrix result(PyObject* given, int64_t rows, int64_t cols, at::ScalarType type, c10::Device device, const On& on, const char* what)
+{
+    if (given == Py_None) {
+        const Matrix m = new_matrix(rows, cols, type, device);
+        on.lent(m.t);
+        return m;
+    }
+    const Matrix m = matrix(given, what);
+    if (m.rows != rows || m.cols != cols)
+        raise(PyExc_ValueError, "%s is %lld x %lld, the result %lld x %lld", what, (long long)m.rows, (long long)m.cols, (long long)rows, (long long)cols);
+    on_device(m.t, device, what);
+    return m;
+}
+
+// (x, stream)
+FH_ENTRY(q8_quantize, 2)
+    const Matrix x = matrix(a[0], "x");
+    const On on(a[1], x.device());
+    const at::Tensor data = bytes(fh_q8_bytes(x.rows, x.cols), x.device());
+    on.lent(data);
+    enqueue(x.device(), [&](void* stream) {
+        return fh_q8_quantize(x.data(), (fh_dtype)x.dtype, x.rows, x.cols, x.stride, data.data_ptr(), (size_t)data.numel(), stream);
+    });
+    return wrapped_matrix(data, x.rows, x.cols, g_q8_matrix).take();
+FH_EXIT
+
+// (matrix, out_dtype, out, stream)
+FH_ENTRY(q8_dequantize, 4)
+    const Stored m = stored(a[0], "the stored matrix", g_q8_matrix);
+    const c10::Device device = m.data.device();
+    const On on(a[3], device);
+    const Matrix out = result(a[2], m.rows, m.cols, scalar_type(a[1]), device, on, "out");
+    enqueue(device, [&](void* stream) {
+        return fh_q8_dequantize(m.data.data_ptr(), (size_t)m.data.numel(), m.rows, m.cols, (fh_dtype)out.dtype, out.data(), out.stride, out.bytes(), stream);
+    });
+    return wrap(out.t);
+FH_EXIT
+
+// (a, b, bias, out_dtype, out, workspace, stream)
+FH_ENTRY(q8_matmul, 7)
+    const Stored x = stored(a[0], "a", g_q8_matrix), y = stored(a[1], "b", g_q8_matrix);
+    const at::Tensor bias = tensor_or_none(a[2], "bias");
+    const c10::Device device = x.data.device();
+    if (x.cols != y.cols) raise(PyExc_ValueError, "a has %lld columns, b %lld", (long long)x.cols, (long long)y.cols);
+    on_device(y.data, device, "b");
+    const On on(a[6], device);
+    const Matrix out = result(a[4], x.rows, y.rows, scalar_type(a[3]), device, on, "out");
+    const Work w = work(a[5], fh_q8_matmul_workspace_bytes(x.rows, y.rows, x.cols), device);
+    const fh_q8_product p = {x.data.data_ptr(), (size_t)x.data.numel(), y.data.data_ptr(), (size_t)y.data.numel(), x.rows, y.rows, x.cols,
+                             vector(bias, y.rows, device, "bias"), bias.defined() ? dtype_code(bias.scalar_type()) : FH_F32, out.dtype, out.data(),
+                             out.stride, out.bytes(), w.p, w.n, 0};
+    enqueue(device, [&](void* stream) { return fh_q8_matmul(&p, stream); });
+    return wrap(out.t);
+FH_EXIT
+
+// (x, w_gate, w_up, b_gate, b_up, activation, out_dtype, out, workspace, stream)
+FH_ENTRY(q8_gated, 10)
+    const Stored x = stored(a[0], "x", g_q8_matrix), gate = stored(a[1], "w_gate", g_q8_matrix), up = stored(a[2], "w_up", g_q8_matrix);
+    const c10::Device device = x.data.device();
+    if (gate.rows != up.rows || gate.cols != up.cols)
+        raise(PyExc_ValueError, "w_gate is %lld x %lld, w_up %lld x %lld", (long long)gate.rows, (long long)gate.cols, (long long)up.rows, (long long)up.cols);
+    if (x.cols != gate.cols) raise(PyExc_ValueError, "x has %lld features, the weights take %lld", (long long)x.cols, (long long)gate.cols);
+    on_device(gate.data, device, "w_gate");
+    on_device(up.data, device, "w_up");
+    const Biases bias(a[3], a[4], gate.rows, device);
+    const int activation = activation_of(a[5]);
+    const On on(a[9], device);
+    const Matrix out = result(a[7], x.rows, gate.rows, scalar_type(a[6]), device, on, "out");
+    const Work w = work(a[8], fh_q8_gated_workspace_bytes(x.rows, gate.rows, x.cols), device);
+    const fh_q8_gated_product p = {x.data.data_ptr(), (size_t)x.data.numel(), gate.data.data_ptr(), (size_t)gate.data.numel(), up.data.data_ptr(), (size_t)up.data.numel(),
+                                   x.rows, gate.rows, x.cols, bias.g, bias.u, bias.dtype, out.dtype, activation, 0, out.data(), out.stride, out.bytes(), w.p, w.n, 0};
+    enqueue(device, [&](void* stream) { return fh_q8_gated(&p, stream); });
+    return wrap(out.t);
+FH_EXIT
+
+// What the two calls of the dense projection have in common: everything is of one dtype.
+fh_gated_layer gated_layer(const Matrix& x, const Matrix& gate, const Matrix& up, const Biases& bias, int activation)
+{
+    if (gate.rows != up.rows || gate.cols != up.cols)
+        raise(PyExc_ValueError, "w_gate is %lld x %lld, w_up %lld x %lld", (long long)gate.rows, (long long)gate.cols, (long long)up.rows, (long long)up.cols);
+    if (x.cols != gate.cols) raise(PyExc_ValueError, "x has %lld features, the weights take %lld", (long long)x.cols, (long long)gate.cols);
+    on_device(gate.t, x.device(), "w_gate");
+    on_device(up.t, x.device(), "w_up");
+    if (gate.dtype != x.dtype || up.dtype != x.dtype || ((bias.g || bias.u) && bias.dtype != x.dtype))
+        raise(PyExc_TypeError, "x, the weights and the biases of a gated projection are of one dtype, as x: %s", c10::toString(x.t.scalar_type()));
+    fh_gated_layer l = {};
+    l.tokens = x.rows; l.features = x.cols; l.hidden = gate.rows;
+    l.dtype = x.dtype; l.activation = activation;
+    l.x = x.data(); l.x_stride = x.stride;
+    l.w_gate = gate.data(); l.w_gate_stride = gate.stride;
+    l.w_up = up.data(); l.w_up_stride = up.stride;
+    l.b_gate = bias.g; l.b_up = bias.u;
+    return l;
+}
+
+// (x, w_gate, w_up, b_gate, b_up, activation, out, workspace, stream)
+FH_ENTRY(gated, 9)
+    const Matrix x = matrix(a[0], "x"), gate = matrix(a[1], "w_gate"), up = matrix(a[2], "w_up");
+    const c10::Device device = x.device();
+    const Biases bias(a[3], a[4], gate.rows, device);
+    fh_gated_layer l = gated_layer(x, gate, up, bias, activation_of(a[5]));
+    const On on(a[8], device);
+    const Matrix out = result(a[6], x.rows, gate.rows, x.t.scalar_type(), device, on, "out");
+    if (out.dtype != x.dtype) raise(PyExc_TypeError, "out must have the dtype of x");
+    l.h = out.data(); l.h_stride = out.stride; l.h_cap = out.bytes();
+    const Work w = work(a[7], fh_gated_workspace_bytes(&l, 0), device);
+    l.workspace = w.p; l.workspace_cap = w.n;
+    enqueue(device, [&](void* stream) { return fh_gated(&l, stream); });
+    return wrap(out.t);
+FH_EXIT
+
+// (dh, x, w_gate, w_up, b_gate, b_up, activation, needs_input, needs_weight, needs_bias, workspace, stream)
+//  -> (dx, dw_gate, dw_up, db_gate, db_up)
+FH_ENTRY(gated_backward, 12)
+    const Matrix dh = matrix(a[0], "dh"), x = matrix(a[1], "x"), gate = matrix(a[2], "w_gate"), up = matrix(a[3], "w_up");
+    const c10::Device device = x.device();
+    const Biases bias(a[4], a[5], gate.rows, device);
+    fh_gated_layer l = gated_layer(x, gate, up, bias, activation_of(a[6]));
+    if (dh.rows != x.rows || dh.cols != gate.rows || dh.dtype != x.dtype) raise(PyExc_ValueError, "dh must have the shape and the dtype of the result");
+    on_device(dh.t, device, "dh");
+    const bool input = truth(a[7]), weight = truth(a[8]), biases = truth(a[9]);
+    const On on(a[11], device);
+    const at::ScalarType type = x.t.scalar_type();
+    l.needs = (input ? FH_GATED_NEEDS_INPUT : 0) | (weight ? FH_GATED_NEEDS_WEIGHT : 0);
+    l.dh = dh.data(); l.dh_stride = dh.stride;
+    at::Tensor dx, dw_gate, dw_up, db_gate, db_up;
+    if (input) {
+        dx = new_matrix(x.rows, x.cols, type, device).t;
+        l.dx = dx.data_ptr();
+    }
+    if (weight) {                                                // one behind the other: one product for both
+        Pair p = pair(gate.rows * gate.cols, type, device);
+        dw_gate = p.first.view({gate.rows, gate.cols});
+        dw_up = p.second.view({gate.rows, gate.cols});
+        l.dw_gate = p.first.data_ptr();
+        l.dw_up = p.second.data_ptr();
+    }
+    if (biases && bias.g) {
+        db_gate = values(gate.rows, type, device);
+        l.db_gate = db_gate.data_ptr();
+    }
+    if (biases && bias.u) {
+        db_up = values(gate.rows, type, device);
+        l.db_up = db_up.data_ptr();
+    }
+    for (const at::Tensor* t : {&dx, &dw_gate, &db_gate, &db_up}) on.lent(*t);
+    const Work w = work(a[10], fh_gated_workspace_bytes(&l, 1), device);
+    l.workspace = w.p; l.workspace_cap = w.n;
+    enqueue(device, [&](void* stream) { return fh_gated_backward(&l, stream); });
+    return tuple(Ref(wrap(dx)), Ref(wrap(dw_gate)), Ref(wrap(dw_up)), Ref(wrap(db_gate)), Ref(wrap(db_up)));
+FH_EXIT
+
+// (FedHybridError, MxMatrix, Q8Matrix): the classes that results and errors are of.
+FH_ENTRY(use, 3)
     Py_XSETREF(g_error, Py_NewRef(a[0]));
     Py_XSETREF(g_matrix, Py_NewRef(a[1]));
+    Py_XSETREF(g_q8_matrix, Py_NewRef(a[2]));
     Py_RETURN_NONE;
 FH_EXIT
 
 #define FH_METHOD(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {FH_METHOD(mx_quantize), FH_METHOD(mx_dequantize), FH_METHOD(mx_matmul), FH_METHOD(layer_norm), FH_METHOD(layer_norm_mx),
                            FH_METHOD(layer_norm_backward), FH_METHOD(layer_forward), FH_METHOD(layer_backward), FH_METHOD(mx_linear), FH_METHOD(refuse_tangents),
+                           FH_METHOD(q8_quantize), FH_METHOD(q8_dequantize), FH_METHOD(q8_matmul), FH_METHOD(q8_gated), FH_METHOD(gated), FH_METHOD(gated_backward),
                            FH_METHOD(use), {}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_fh_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,6 +1,6 @@
 // The product of two microscaled matrices: out[i][j] = sum_k A[i][k] B[j][k] + bias[j].
+#include "fh_matrix.hpp"
 #include "fh_mx_plan.hpp"
-#include "fh_norm.hpp"
 
 namespace fh {
 namespace {
@@ -8,7 +8,6 @@ namespace {
 constexpr int64_t kMostSummed = (int64_t)1 << 24;   // a row's codes are addressed with 32 bits
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct ProductArgs {
     const uint8_t *a, *a_scales;       // m rows
@@ -36,28 +35,6 @@ __device__ __forceinline__ f32x16 mx_mfma32(u32x4 a, u32x4 b, uint32_t sa, uint3
 {
     const i32x8 x = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0}, y = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, BYTE, (int)sa, BYTE, (int)sb);
-}
-
-// 16 bytes a lane from a buffer straight into LDS, at `lds` + 16 * lane.  Written out because the compiler would wait for all
-// of them before every later read of LDS, the other stage's too.  No register is written; the caller waits by
-// s_waitcnt vmcnt before the barrier that hands the stage over.
-__device__ __forceinline__ void to_lds(uint32_t lds, u32x4 from, uint32_t offset, uint32_t moved)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 :: "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(from), "s"(__builtin_amdgcn_readfirstlane(moved)) : "memory", "m0");
-}
-__device__ __forceinline__ u32x4 buffer_of(const uint8_t* p, uint32_t bytes)
-{
-    const uint64_t at = (uint64_t)p;
-    return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, bytes, 0x00020000u};
-}
-
-// Tiles in bands of eight columns, so that what an XCD works on at a time shares rows of both operands in its L2.
-__device__ __forceinline__ void in_bands(uint32_t tile, uint32_t m_tiles, uint32_t n_tiles, uint32_t& i, uint32_t& j)
-{
-    const uint32_t band = tile / (8 * m_tiles), first = band * 8, wide = n_tiles - first < 8 ? n_tiles - first : 8, in_band = tile - first * m_tiles;
-    i = in_band / wide;
-    j = first + in_band - i * wide;
 }
 
 // ---- few tiles: the sum split over a workgroup's waves, through LDS --------------------------------
@@ -166,23 +143,6 @@ __global__ __launch_bounds__(WAVES * 64) void mx_waves_kernel(ProductArgs p)
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = sum[e] + (j + e < p.n ? parameter(p.bias, p.bias_dtype, j + e, 0.0f) : 0.0f);
         store4(static_cast<T*>(p.out) + (int64_t)part * p.m * p.n + i * p.stride + j, p.n - j, v);
-    }
-}
-
-// Of 16 bytes of outputs those that are before a row's end.
-template <typename T>
-__device__ __forceinline__ void store_packed(T* p, int n, u32x4 v)
-{
-    constexpr int kRun = 16 / sizeof(T);
-    if (n >= kRun) *reinterpret_cast<u32x4_a2*>(p) = v;
-    else {
-#pragma unroll
-        for (int i = 0; i < kRun; ++i)
-            if (i < n) {
-                const uint32_t w = v[i * (int)sizeof(T) / 4];    // a value of its own: bit_cast of a vector's element takes element 0 whichever is asked for
-                if constexpr (sizeof(T) == 4) p[i] = __builtin_bit_cast(float, w);
-                else p[i].bits = (uint16_t)(w >> (16 * (i & 1)));
-            }
     }
 }
 

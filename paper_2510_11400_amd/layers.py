@@ -10,10 +10,14 @@ the weight's gradient as it is, so nothing is restored.  Behind a layer norm it 
     dW = dy^T x         dy by columns, x by columns (the saved form)
 
 Matrix products are of 4-bit values with binary32 sums; parameters and their gradients keep their own dtype.
+
+The gated projection of a feed-forward block, act(x Wg^T + bg) * (x Wu^T + bu), is dense in training and saves its input alone
+(as autograd saves it, so that SavedActivations compresses it): what has the hidden width is computed again in the
+backward pass.  Frozen, it and the projection behind it work in 8-bit integers with a scale per token and channel.
 """
 from __future__ import annotations
 
-from typing import Optional
+from typing import Optional, Tuple
 
 import torch
 
@@ -72,6 +76,46 @@ def layer_norm_mx_linear(x: torch.Tensor, norm_weight: Optional[torch.Tensor], n
     return _binding.mx_linear(x, norm_weight, norm_bias, weight, bias, eps, rounding, seed, tensor_id)
 
 
+class _Gated(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, b_gate, b_up, activation):
+        m = _rows(x)
+        h = api.fh_gated(m, w_gate, w_up, b_gate, b_up, activation)
+        ctx.activation = activation
+        ctx.save_for_backward(m, w_gate, w_up, b_gate, b_up)
+        return h.view(*x.shape[:-1], h.shape[1])
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dh):
+        m, w_gate, w_up, b_gate, b_up = ctx.saved_tensors
+        x, gate, up, gate_bias, up_bias, _ = ctx.needs_input_grad
+        dx, dw_gate, dw_up, db_gate, db_up = api.fh_gated_backward(_rows(dh), m, w_gate, w_up, b_gate, b_up, ctx.activation, needs_input=x,
+                                                                   needs_weight=gate or up, needs_bias=gate_bias or up_bias)
+        return (dx.view(*dh.shape[:-1], m.shape[1]) if x else None, dw_gate if gate else None, dw_up if up else None,
+                db_gate if gate_bias else None, db_up if up_bias else None, None)
+
+
+def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, b_gate: Optional[torch.Tensor] = None,
+                 b_up: Optional[torch.Tensor] = None, activation: str = "silu") -> torch.Tensor:
+    """act(x w_gate^T + b_gate) * (x w_up^T + b_up) over the last dimension, differentiable; everything of one dtype.  x is saved as autograd saves
+    it (hooks.SavedActivations compresses it), and nothing of the hidden width."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, w_gate, w_up, b_gate, b_up)):
+        return _Gated.apply(x, w_gate, w_up, b_gate, b_up, activation)
+    _binding.refuse_tangents(x, w_gate, w_up, b_gate, b_up)
+    with torch.no_grad():
+        return api.fh_gated(_rows(x), w_gate, w_up, b_gate, b_up, activation).view(*x.shape[:-1], w_gate.shape[0])
+
+
+def q8_linear(x: torch.Tensor, weight: api.Q8Matrix, bias: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x weight^T + bias over the last dimension with x quantised to 8-bit integers, a scale for each token, and a weight that is stored
+    so (api.fh_q8_quantize): two kernels.  For serving: it gives no gradients (tangents are refused)."""
+    _binding.refuse_tangents(x, bias)
+    with torch.no_grad():
+        y = api.fh_q8_matmul(api.fh_q8_quantize(_rows(x)), weight, bias, x.dtype)
+    return y.view(*x.shape[:-1], weight.rows)
+
+
 class LayerNorm(torch.nn.Module):
     """Layer norm over the last dimension."""
 
@@ -120,3 +164,34 @@ class LayerNormMxLinear(torch.nn.Module):
             h, _, _ = api.fh_layer_norm_mx(_rows(x), norm_weight, norm_bias, self.norm.eps, "rows")
             y = api.fh_mx_matmul(h, self._stored, bias, x.dtype)
         return y.view(*x.shape[:-1], self._stored.rows)
+
+
+class GatedLinear(torch.nn.Module):
+    """The gated projection act(gate(x)) * up(x), trained dense; `freeze()` stores the weights once in 8-bit integers for serving.
+
+    A frozen layer runs two kernels for any number of tokens; `q8_linear` is the projection behind it in the same form."""
+
+    def __init__(self, features: int, hidden: int, bias: bool = True, activation: str = "silu", device=None, dtype=None):
+        super().__init__()
+        self.gate = torch.nn.Linear(features, hidden, bias=bias, device=device, dtype=dtype)
+        self.up = torch.nn.Linear(features, hidden, bias=bias, device=device, dtype=dtype)
+        self.activation = activation
+        self._stored: Optional[Tuple[api.Q8Matrix, api.Q8Matrix]] = None
+
+    def freeze(self) -> "GatedLinear":
+        """Store the weights in 8-bit integers; from here on forward() uses these and gives no gradients (tangents are refused).  Call it again
+        after the weights have changed, `thaw()` to train on."""
+        self._stored = api.fh_q8_quantize(self.gate.weight.detach()), api.fh_q8_quantize(self.up.weight.detach())
+        return self
+
+    def thaw(self) -> "GatedLinear":
+        self._stored = None
+        return self
+
+    def forward(self, x: torch.Tensor) -> torch.Tensor:
+        if self._stored is None:
+            return gated_linear(x, self.gate.weight, self.up.weight, self.gate.bias, self.up.bias, self.activation)
+        _binding.refuse_tangents(x, self.gate.bias, self.up.bias)
+        with torch.no_grad():
+            h = api.fh_q8_gated(api.fh_q8_quantize(_rows(x)), *self._stored, self.gate.bias, self.up.bias, self.activation, x.dtype)
+        return h.view(*x.shape[:-1], h.shape[1])
