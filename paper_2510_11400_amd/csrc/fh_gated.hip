@@ -112,7 +112,7 @@ template <> struct OpOf<Bf16> { typedef OfBf16 type; };
 template <Made MADE, typename T>
 hipError_t gated_product(const typename ArgsOf<MADE>::type& p, hipStream_t s)
 {
-    return product_waves<typename OpOf<T>::type, MADE, T, 2, 2, 4>(p, s);
+    return product_of<typename OpOf<T>::type, MADE, T>(p, s);
 }
 
 // The operands of the forward product.
@@ -170,7 +170,7 @@ Backward backward_of(const fh_gated_layer& l)
     Backward b = {};
     b.d_values = padded_bytes(2 * l.hidden, l.dtype) / (int64_t)size;
     b.tokens_padded = padded_bytes(l.tokens, l.dtype) / (int64_t)size;
-    b.tile_rows = 64;
+    b.tile_rows = product_sum_rows(product_plan(l.tokens, 2 * l.hidden, padded_bytes(l.features, l.dtype) / kChunkBytes, l.dtype == FH_F32));
     b.d = aligned((size_t)l.tokens * (size_t)b.d_values * size);
     if (l.needs & FH_GATED_NEEDS_WEIGHT) {
         b.d_turned = aligned((size_t)(2 * l.hidden) * (size_t)b.tokens_padded * size);

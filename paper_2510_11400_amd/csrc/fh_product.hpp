@@ -8,6 +8,7 @@
 
 #include "fh_activation.hpp"
 #include "fh_matrix.hpp"
+#include "fh_product_plan.hpp"
 #include "fh_q8.hpp"
 
 namespace fh {
@@ -113,8 +114,8 @@ __global__ __launch_bounds__(WAVES * 64) void product_waves_kernel(typename Args
     constexpr bool kPair = MADE != Made::linear;
     constexpr int kCols = kPair ? kRowsB / 2 : kRowsB;           // columns of the tile
     constexpr uint32_t kCodes = (kRowsA + kRowsB) * kChunkBytes, kSums = kRowsA * kPad * 4, kArea = kCodes > kSums ? kCodes : kSums;
-    constexpr int kThreads = WAVES * 64, kRuns = kCols / 4, kSteps = kRowsA * kRuns / kThreads;
-    static_assert(kRowsA * kRuns % kThreads == 0 && kThreads % kRuns == 0, "a thread stays with its columns");
+    constexpr int kThreads = WAVES * 64, kRuns = kCols / 4, kSteps = (kRowsA * kRuns + kThreads - 1) / kThreads;
+    static_assert(kThreads % kRuns == 0, "a thread stays with its columns");
     __shared__ __attribute__((aligned(16))) uint8_t s_area[WAVES * kArea];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t i, j;
@@ -205,7 +206,7 @@ __global__ __launch_bounds__(WAVES * 64) void product_waves_kernel(typename Args
     for (int t = 0; t < kSteps; ++t) {
         const int row = (t * kThreads + threadIdx.x) / kRuns;
         const uint32_t i = i0 + row;
-        if (i >= p.m) continue;
+        if (row >= kRowsA || i >= p.m) continue;
         const float mine = scale_of<OP>(p.a, p.m, p.a_pitch, p.chunks, i);
         const Sum4 sum = sum_at(row, col);
         float v[4];
@@ -271,6 +272,356 @@ hipError_t product_waves(typename ArgsOf<MADE>::type p, hipStream_t s)
         p.first = (uint32_t)first;
         return launch(product_waves_kernel<OP, MADE, T, MT, NT, WAVES>, dim3((uint32_t)count), dim3(WAVES * 64), s, p);
     });
+}
+
+// A wave's pairs of sums, (32 MT) rows x 32 columns of each, to what is made of them.  Sixteen rows at a time go through 4 KiB of LDS, so that a lane
+// has four neighbouring columns of both: the formulas, which are long, stand here once for eight passes, and what a row brings (its scale,
+// dh) is read by 64 bytes a pass ahead.
+template <typename OP, Made MADE, typename T, int MT, int NT, typename Args>
+__device__ __forceinline__ void pair_epilogue(const Args& p, const typename OP::Sums (&c)[MT][NT], uint8_t* s_area, uint32_t i0, uint32_t j0, int lane)
+{
+    typedef typename OP::Sum Sum;
+    typedef Sum Sum4 __attribute__((ext_vector_type(4)));
+    const int row16 = lane & 15, upper = lane >> 4 & 1, half = lane >> 5, piece = lane & 7, mine = lane >> 3;
+    const uint32_t col = j0 + piece * 4;
+    const int64_t left = (int64_t)p.n - col;
+    float bias[2][4], scales[2][4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t inside = col + e < p.n ? col + e : p.n - 1;
+        bias[0][e] = parameter(p.bias, p.bias_dtype, inside, 0.0f);
+        bias[1][e] = parameter(p.bias2, p.bias_dtype, inside, 0.0f);
+        scales[0][e] = scale_of<OP>(p.b, p.n, p.b_pitch, p.chunks, inside);
+        scales[1][e] = scale_of<OP>(p.b2, p.n, p.b2_pitch, p.chunks, inside);
+    }
+    struct OfRow { float scale; f32x4 dh; };
+    const auto of_row = [&](int row, OfRow& r) {
+        const uint32_t i = i0 + row;
+        r.scale = OP::kScaled ? scale_of<OP>(p.a, p.m, p.a_pitch, p.chunks, i < p.m ? i : p.m - 1) : 1.0f;
+        if constexpr (MADE == Made::gated_backward) {
+            float dh[4];
+            load4(static_cast<const T*>(p.dh) + (int64_t)i * p.dh_stride + col, i < p.m ? left : 0, dh);
+            r.dh = f32x4{dh[0], dh[1], dh[2], dh[3]};
+        }
+    };
+    float sums[2][4] = {};
+    OfRow next[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) of_row(t * 8 + mine, next[t]);
+#pragma clang loop unroll(disable)
+    for (int pass = 0; pass < 2 * MT; ++pass) {
+#pragma unroll
+        for (int x = 0; x < MT; ++x)
+            if (x == pass >> 1 && upper == (pass & 1)) {
+#pragma unroll
+                for (int y = 0; y < NT; ++y)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        *reinterpret_cast<Sum4*>(s_area + row16 * 256 + ((y * 8 + 2 * e + half) ^ row16) * 16) =
+                            Sum4{c[x][y][4 * e], c[x][y][4 * e + 1], c[x][y][4 * e + 2], c[x][y][4 * e + 3]};
+            }
+        asm volatile("" ::: "memory");                           // a wave's own LDS accesses are in order
+        OfRow now[2];
+        Sum4 sum[2][2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int row = t * 8 + mine;
+            now[t] = next[t];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) sum[t][u] = *reinterpret_cast<const Sum4*>(s_area + row * 256 + ((u * 8 + piece) ^ row) * 16);
+        }
+        asm volatile("" ::: "memory");
+        if (pass + 1 < 2 * MT) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) of_row((pass + 1) * 16 + t * 8 + mine, next[t]);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const uint32_t i = i0 + pass * 16 + t * 8 + mine;
+            float v[4], w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float gate = made_of<OP>(sum[t][0][e], now[t].scale * scales[0][e], bias[0][e]);
+                const float up = made_of<OP>(sum[t][1][e], now[t].scale * scales[1][e], bias[1][e]);
+                if constexpr (MADE == Made::gated) {
+                    v[e] = activated(gate, p.act) * up;
+                } else {
+                    const Activated a = activated_both(gate, p.act);
+                    const bool inside = i < p.m && e < left;     // the others' sums are of no rows
+                    v[e] = inside ? now[t].dh[e] * up * a.slope : 0.0f;
+                    w[e] = inside ? now[t].dh[e] * a.value : 0.0f;
+                    sums[0][e] += v[e];
+                    sums[1][e] += w[e];
+                }
+            }
+            T* to = static_cast<T*>(p.out) + (int64_t)i * p.stride + col;
+            store4(to, i < p.m ? left : 0, v);
+            if constexpr (MADE == Made::gated_backward) store4(to + p.up_at, i < p.m ? left : 0, w);
+        }
+    }
+    if constexpr (MADE == Made::gated_backward) {
+        if (!p.sums || i0 >= p.m) return;
+        // over the eight lanes that have the same columns
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float s = sums[u][e], a, b;
+                s += dpp<0x128>(s);                              // row_ror:8
+                self_swap<16>(s, a, b);
+                s = a + b;
+                self_swap<32>(s, a, b);
+                sums[u][e] = a + b;
+            }
+        if (mine == 0) {
+            float* to = p.sums + (int64_t)(i0 / (MT * 32)) * 2 * p.n + col;
+            store4(to, left, sums[0]);
+            store4(to + p.n, left, sums[1]);
+        }
+    }
+}
+
+// ---- large products: tiles through LDS -----------------------------------------------------------
+// B x B sums of a tile, a chunk at a time; a workgroup of 2 x WN waves, each with B/2 x 64 sums, takes one tile after another.  Two stages of LDS: while one
+// is multiplied the next is on its way, and a stage is handed over before its last quarter, which is in registers by then, so that the matrix
+// unit works across the barrier.  A row's eight pieces of 16 bytes are turned by half the row's number (the loads take them from turned
+// addresses), so that sixteen lanes reading the same piece of sixteen rows meet all 64 banks.
+// The chunks of the next tile follow those of the last without a gap.  A wave's outputs are turned into rows in the part of the free stage that
+// the wave itself loads, so it needs no barrier before it loads there again; that load is sent before the outputs are, because
+// memory operations are counted in their order and the next wait is for the load alone.
+// Of a pair's 64 columns of a wave the first 32 are the gate's and the others the same columns of up, so that both sums of an output are one wave's.
+// Its outputs go through LDS of their own, so that the next load is sent before all of them.
+template <typename OP, Made MADE, typename T, int B, int WN>
+__global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_kernel(typename ArgsOf<MADE>::type p)
+{
+    constexpr bool kPair = MADE != Made::linear;
+    constexpr int kWaves = 2 * WN, kHalf = kWaves / 2, MT = B / 64, NT = 2, kCols = kPair ? B / 2 : B;
+    constexpr uint32_t kStage = 2 * B * kChunkBytes;
+    constexpr int kRun = 16 / sizeof(T), kLanes = 64 / kRun, kRows = 64 / kLanes;
+    constexpr int kStores = kPair ? MT * 4 * (MADE == Made::gated ? 1 : 2) : MT * 32 / kRows;
+    static_assert(kHalf * 64 == B && WN * 64 == B, "a wave loads 64 rows of one operand, and has 64 columns");
+    __shared__ __attribute__((aligned(16))) uint8_t s_stage[2 * kStage + (kPair ? kWaves * 4096 : 0)];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+
+    const uint32_t tiles = p.m_tiles * p.n_tiles, xcd = blockIdx.x & 7;
+    const uint32_t end_tile = run_of(xcd, tiles) + (tiles >> 3) + (xcd < (tiles & 7) ? 1 : 0);
+    const auto corner = [&](uint32_t tile, uint32_t& i0, uint32_t& j0) {
+        in_bands(tile, p.m_tiles, p.n_tiles, i0, j0);
+        i0 *= B;
+        j0 *= kCols;
+    };
+
+    // what is loaded next: a chunk of a tile, in this wave 64 rows of one operand, two times 32 of a buffer each
+    const bool of_b = wave >= kHalf;
+    const int part = wave % kHalf;
+    const uint32_t width = p.chunks * kChunkBytes, end = p.chunks;
+    const uint32_t pitch = of_b ? p.b_pitch : p.a_pitch, pitch2 = kPair && of_b ? p.b2_pitch : pitch;
+    uint32_t next_tile = run_of(blockIdx.x, tiles), next_chunk = 0;
+    u32x4 from, from2;
+    const uint32_t piece_at = ((lane & 7) ^ (lane >> 4)) * 16, at = (lane >> 3) * pitch + piece_at, at2 = (lane >> 3) * pitch2 + piece_at;
+    const auto aim = [&]() {
+        uint32_t i0, j0;
+        corner(next_tile, i0, j0);
+        // rows past the last are past the buffer's end: nothing is read for them, and nothing of theirs is stored
+        const auto rows_of = [&](const uint8_t* base, uint32_t row0, uint32_t all, uint32_t row_pitch) {
+            const uint32_t rows = row0 >= all ? 0u : all - row0 < 32u ? all - row0 : 32u;
+            return buffer_of(base + (int64_t)(rows ? row0 : 0u) * row_pitch, rows ? (rows - 1) * row_pitch + width : 0u);
+        };
+        if (kPair && of_b) {
+            from = rows_of(p.b, j0 + part * 32, p.n, pitch);
+            from2 = rows_of(p.b2, j0 + part * 32, p.n, pitch2);
+        } else {
+            const uint8_t* base = of_b ? p.b : p.a;
+            const uint32_t row0 = (of_b ? j0 : i0) + part * 64, all = of_b ? p.n : p.m;
+            from = rows_of(base, row0, all, pitch);
+            from2 = rows_of(base, row0 + 32, all, pitch);
+        }
+    };
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_stage;
+    const auto load = [&](uint32_t stage) {
+        if (next_tile >= end_tile) return;
+        uint32_t row_at = at, row_at2 = at2;
+        asm("" : "+v"(row_at), "+v"(row_at2));                   // sums made here, not registers kept
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+            to_lds(lds + stage + wave * 8192 + t * 1024, t < 4 ? from : from2, ((t < 4 ? row_at : row_at2) ^ (t & 1) * 64) + t % 4 * 8 * (t < 4 ? pitch : pitch2),
+                   next_chunk * kChunkBytes);
+        if (++next_chunk == end) {
+            next_chunk = 0;
+            next_tile += p.first;
+            if (next_tile < end_tile) aim();
+        }
+    };
+
+    const int h = lane >> 5, r = lane & 31, turned = (h * 4) ^ (lane >> 1 & 7);
+    const uint32_t read_a = (wm * MT * 32 + r) * kChunkBytes, read_b = (B + wn * NT * 32 + r) * kChunkBytes;
+    u32x4 fa[2][MT], fb[2][NT];
+    const auto read = [&](uint32_t stage, int quarter, int to) {
+        const uint8_t* at_piece = s_stage + stage + (uint32_t)(turned ^ quarter) * 16;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) fa[to][t] = *reinterpret_cast<const u32x4*>(at_piece + read_a + t * 4096);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) fb[to][t] = *reinterpret_cast<const u32x4*>(at_piece + read_b + t * 4096);
+    };
+    typename OP::Sums c[MT][NT];
+    // Sums run along b's rows within a lane.
+    const auto multiply = [&](int which) {
+#pragma unroll
+        for (int x = 0; x < MT; ++x)
+#pragma unroll
+            for (int y = 0; y < NT; ++y) c[x][y] = OP::multiply(fb[which][y], fa[which][x], c[x][y]);
+    };
+    uint32_t tile = next_tile, stage = 0;
+    bool behind = false;                                         // outputs were sent after the load that is waited for
+    if (tile >= end_tile) return;
+    aim();
+    load(0);
+    if (next_tile < end_tile) {
+        load(kStage);
+        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");         // the first stage's are older
+    } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if constexpr (!kPair) read(stage, 0, 0);
+    [[maybe_unused]] T* out = static_cast<T*>(p.out);
+#pragma clang loop unroll(disable)
+    for (; tile < end_tile; tile += p.first) {
+        uint32_t i0, j0;
+        corner(tile, i0, j0);
+        float bias_here = 0.0f, scale_here = 0.0f;               // of the wave's column `lane`
+#pragma unroll
+        for (int x = 0; x < MT; ++x)
+#pragma unroll
+            for (int y = 0; y < NT; ++y) c[x][y] = typename OP::Sums{};
+        if constexpr (kPair) read(stage, 0, 0);
+#pragma clang loop unroll(disable)
+        for (uint32_t k = 0; k < end; ++k) {
+            if (!kPair && k + 1 == end) {
+                const uint32_t col = j0 + wn * 64 + lane, inside = col < p.n ? col : p.n - 1;
+                if (p.bias) bias_here = parameter(p.bias, p.bias_dtype, inside, 0.0f);
+                scale_here = scale_of<OP>(p.b, p.n, p.b_pitch, end, inside);
+            }
+            read(stage, 1, 1);
+            multiply(0);
+            read(stage, 2, 0);
+            multiply(1);
+            read(stage, 3, 1);
+            multiply(0);
+            // this wave has read all of this stage, and its part of the next has arrived
+            if (behind) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(kStores) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            behind = false;
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (k + 1 < end) load(stage);
+            stage = kStage - stage;
+            // after the last chunk the next tile's; a pair's epilogue needs the registers and reads them behind it
+            if (!kPair || k + 1 < end) read(stage, 0, 0);
+            multiply(1);
+        }
+        if constexpr (kPair) {
+            load(kStage - stage);
+            pair_epilogue<OP, MADE, T, MT, NT>(p, c, s_stage + 2 * kStage + wave * 4096, i0 + wm * MT * 32, j0 + wn * 32, lane);
+            behind = i0 + B <= p.m && j0 + kCols <= p.n;
+        } else {
+            int l = lane;
+            asm("" : "+v"(l));                                       // what is worked out from it is not kept in registers meanwhile
+            const int mine = l / kLanes, piece = l % kLanes, row32 = l & 31, half = l >> 5;
+            // the sums as values, in place
+            f32x16 v[MT][NT];
+            {
+                float row_scale[MT];
+#pragma unroll
+                for (int x = 0; x < MT; ++x) {
+                    const uint32_t row = i0 + (wm * MT + x) * 32 + row32;
+                    row_scale[x] = OP::kScaled ? scale_of<OP>(p.a, p.m, p.a_pitch, end, row < p.m ? row : p.m - 1) : 1.0f;
+                }
+#pragma unroll
+                for (int y = 0; y < NT; ++y)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int source = (y * 32 + i / 4 * 8 + half * 4 + i % 4) * 4;
+                        const float bias = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(source, __builtin_bit_cast(int, bias_here)));
+                        const float scale = OP::kScaled ? __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(source, __builtin_bit_cast(int, scale_here))) : 1.0f;
+#pragma unroll
+                        for (int x = 0; x < MT; ++x) v[x][y][i] = made_of<OP>(c[x][y][i], row_scale[x] * scale, bias);
+                    }
+            }
+
+            // 32 rows at a time through this wave's 8 KiB of the stage that is free, to runs of 16 bytes a lane
+            constexpr int kPieces = 64 * (int)sizeof(T) / 16;        // of a row
+            const auto turn_of = [](int row) { return kPieces == 16 ? row & 15 : row >> 1 & 7; };
+            uint8_t* s_out = s_stage + (kStage - stage) + wave * 8192;
+            u32x4 made[kStores];
+#pragma unroll
+            for (int x = 0; x < MT; ++x) {
+#pragma unroll
+                for (int y = 0; y < NT; ++y)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const f32x16& o = v[x][y];
+                        if constexpr (sizeof(T) == 2) {              // the upper sixteen rows have the halves of a piece exchanged
+                            const uint32_t at_piece = (uint32_t)((y * 4 + i) ^ turn_of(row32)) * 16 + (uint32_t)(half ^ row32 >> 4) * 8;
+                            *reinterpret_cast<u32x2*>(s_out + row32 * (kPieces * 16) + at_piece) = u32x2{bf16_pair(o[4 * i], o[4 * i + 1]), bf16_pair(o[4 * i + 2], o[4 * i + 3])};
+                        } else {
+                            const uint32_t at_piece = (uint32_t)((y * 8 + 2 * i + half) ^ turn_of(row32)) * 16;
+                            *reinterpret_cast<f32x4*>(s_out + row32 * (kPieces * 16) + at_piece) = f32x4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
+                        }
+                    }
+                asm volatile("" ::: "memory");                       // a wave's own LDS accesses are in order
+#pragma unroll
+                for (int t = 0; t < 32 / kRows; ++t) {
+                    const int from_row = t * kRows + mine;
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(s_out + from_row * (kPieces * 16) + (piece ^ turn_of(from_row)) * 16);
+                    made[x * (32 / kRows) + t] = sizeof(T) == 2 && t * kRows >= 16 ? u32x4{w.z, w.w, w.x, w.y} : w;
+                }
+                asm volatile("" ::: "memory");
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            load(kStage - stage);
+            const uint32_t row = i0 + wm * MT * 32 + mine, col = j0 + wn * 64 + piece * kRun;
+            T* to = out + (int64_t)row * p.stride + col;
+            if (i0 + B <= p.m && j0 + kCols <= p.n) {
+#pragma unroll
+                for (int t = 0; t < kStores; ++t) *reinterpret_cast<u32x4_a2*>(to + (int64_t)(t * kRows) * p.stride) = made[t];
+                behind = true;
+            } else {
+                const int rows = p.m <= row ? 0 : p.m - row < B ? (int)(p.m - row) : B, cols = p.n <= col ? 0 : p.n - col < kRun ? (int)(p.n - col) : kRun;
+#pragma unroll
+                for (int t = 0; t < kStores; ++t) {
+                    int some = t * kRows < rows ? cols : 0;
+                    asm("" : "+v"(some));                            // its masks are not kept in registers either
+                    store_packed(to + (int64_t)(t * kRows) * p.stride, some, made[t]);
+                }
+            }
+        }
+    }
+}
+
+template <typename OP, Made MADE, typename T, int B, int WN>
+hipError_t product_tiles(typename ArgsOf<MADE>::type p, hipStream_t s)
+{
+    constexpr uint32_t kCols = MADE == Made::linear ? B : B / 2;
+    p.m_tiles = (p.m + B - 1) / B;
+    p.n_tiles = (p.n + kCols - 1) / kCols;
+    const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles, held = B > 128 ? 256 : 512;     // what the card holds at a time
+    if (tiles * 8 > INT32_MAX) return hipErrorInvalidValue;
+    const uint32_t grid = (uint32_t)(tiles < held ? tiles : held);
+    p.first = (grid + 7) / 8;
+    return launch(product_tile_kernel<OP, MADE, T, B, WN>, dim3(grid), dim3(2 * WN * 64), s, p);
+}
+
+template <typename OP, Made MADE, typename T>
+hipError_t product_of(const typename ArgsOf<MADE>::type& p, hipStream_t s)
+{
+    switch (product_plan(p.m, MADE == Made::linear ? p.n : 2 * (int64_t)p.n, p.chunks, sizeof(T) == 4 && !OP::kScaled)) {
+        case ProductTile::waves32: return product_waves<OP, MADE, T, 1, 1, 4>(p, s);
+        case ProductTile::waves32_wide: return product_waves<OP, MADE, T, 1, 1, 8>(p, s);
+        case ProductTile::waves64: return product_waves<OP, MADE, T, 2, 2, 4>(p, s);
+        case ProductTile::square128: return product_tiles<OP, MADE, T, 128, 2>(p, s);
+        case ProductTile::square256: break;
+    }
+    return product_tiles<OP, MADE, T, 256, 4>(p, s);
 }
 
 }  // namespace fh

@@ -4,16 +4,10 @@
 namespace fh {
 namespace {
 
-template <Made MADE, typename T>
-hipError_t q8_product_of(const ProductArgs& p, hipStream_t s)
-{
-    return product_waves<OfQ8, MADE, T, 2, 2, 4>(p, s);
-}
-
 template <Made MADE>
 hipError_t q8_product(const ProductArgs& p, int32_t out_dtype, hipStream_t s)
 {
-    return out_dtype == FH_F32 ? q8_product_of<MADE, float>(p, s) : q8_product_of<MADE, Bf16>(p, s);
+    return out_dtype == FH_F32 ? product_of<OfQ8, MADE, float>(p, s) : product_of<OfQ8, MADE, Bf16>(p, s);
 }
 
 bool q8_product_shape_ok(int64_t m, int64_t n, int64_t k) { return q8_shape_ok(m, k) && q8_shape_ok(n, k) && k <= kQ8MostSummed; }
