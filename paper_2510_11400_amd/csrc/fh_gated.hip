@@ -5,7 +5,9 @@
 //        the products behind take it (a relative 2^-9 a value in bf16, as much as the results' own rounding);
 //   dx = D [Wg; Wu]
 //   [dWg; dWu] = D^T x
-// and the biases' gradients are sums of D's columns before that rounding: partial sums by tiles of rows, joined in order.
+// and the biases' gradients are sums of D's columns before that rounding: partial sums by tiles of rows, joined in order.  Operands whose rows are the
+// summed dimension (the weights of dx, D and x of dW) are read as they lie and transposed on their way from LDS to registers; copying them to the other
+// order first took 8192 tokens of 768 -> 2048 in bf16 70 us of 283.  dW has few outputs and a sum over all tokens: several workgroups share a tile's.
 #include "fh_product.hpp"
 
 namespace fh {
@@ -31,28 +33,27 @@ __global__ __launch_bounds__(256) void pack_kernel(const T* x, uint32_t cols, in
         *reinterpret_cast<u32x4*>(out + (int64_t)row * pitch + i * 16) = u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
     }
 }
-// The transposed matrix: out[c][r] = x[r][c], row c from byte c * pitch on; r goes to `padded` with zeros behind `rows`.  Tiles of 64 x 64.
 template <typename T>
-__global__ __launch_bounds__(256) void transpose_kernel(const T* x, uint32_t rows, uint32_t cols, int64_t stride, T* out, int64_t out_stride, uint32_t padded,
-                                                        uint32_t across, uint32_t first)
+__global__ __launch_bounds__(64) void clear_rows_kernel(T* out, uint32_t cols)
 {
-    __shared__ T s_tile[64][65];
-    const uint32_t tile = first + blockIdx.x, r0 = tile / across * 64, c0 = tile % across * 64;
-    for (uint32_t i = threadIdx.x; i < 64 * 64; i += 256) {
-        const uint32_t r = i / 64, c = i % 64;
-        s_tile[r][c] = r0 + r < rows && c0 + c < cols ? x[(int64_t)(r0 + r) * stride + c0 + c] : T{};
-    }
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < 64 * 64; i += 256) {
-        const uint32_t c = i / 64, r = i % 64;
-        if (c0 + c < cols && r0 + r < padded) out[(int64_t)(c0 + c) * out_stride + r0 + r] = s_tile[r][c];
-    }
+    for (uint32_t c = threadIdx.x; c < cols; c += 64) out[(int64_t)blockIdx.x * cols + c] = T{};
 }
-// Columns from..to of every row: zeros.
+// The parts of a shared sum, each `hidden_padded` + hidden rows of cols, added up in their order: the first `hidden` rows and the last.
 template <typename T>
-__global__ __launch_bounds__(64) void clear_columns_kernel(T* out, int64_t stride, uint32_t from, uint32_t to)
+__global__ __launch_bounds__(256) void join_weights_kernel(const float* parts, uint32_t count, uint32_t hidden, uint32_t hidden_padded, uint32_t cols, uint32_t runs, T* gate, T* up)
 {
-    for (uint32_t c = from + threadIdx.x; c < to; c += 64) out[(int64_t)blockIdx.x * stride + c] = T{};
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x, number = at / runs, col = (at - number * runs) * 4;
+    if (number >= 2 * hidden) return;
+    const uint32_t second = number >= hidden, row = second ? number - hidden : number, all = hidden_padded + hidden;
+    const float* from = parts + (int64_t)(second ? hidden_padded + row : row) * cols + col;
+    float v[4] = {};
+    for (uint32_t k = 0; k < count; ++k) {
+        float w[4];
+        load4(from + (int64_t)k * all * cols, (int64_t)cols - col, w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += w[i];
+    }
+    store4((second ? up : gate) + (int64_t)row * cols + col, (int64_t)cols - col, v);
 }
 
 template <typename T>
@@ -64,22 +65,12 @@ hipError_t pack(const void* x, int64_t rows, int64_t cols, int64_t stride, void*
                       (uint32_t)rows, (uint32_t)first);
     });
 }
-template <typename T>
-hipError_t transpose(const void* x, int64_t rows, int64_t cols, int64_t stride, T* out, int64_t out_stride, int64_t padded, hipStream_t s)
-{
-    const int64_t across = (cols + 63) / 64, tiles = (padded + 63) / 64 * across;
-    return in_parts(tiles, 256, [&](int64_t first, int64_t count) {
-        return launch(transpose_kernel<T>, dim3((uint32_t)count), dim3(256), s, static_cast<const T*>(x), (uint32_t)rows, (uint32_t)cols, stride, out, out_stride,
-                      (uint32_t)padded, (uint32_t)across, (uint32_t)first);
-    });
-}
-
-// A matrix as an operand: as it lies, or packed.
+// A matrix as an operand: as it lies, or packed.  As it lies where every row, and its end, is at a multiple of 16 bytes.
 struct Rows { const void* p; int64_t rows, cols, stride; };
 bool lies_well(const Rows& r, int32_t dtype)
 {
     const int64_t size = (int64_t)dtype_size(dtype), pitch = r.stride * size;
-    return is_aligned(r.p, 16) && r.cols * size % kChunkBytes == 0 && (r.rows <= 1 || (pitch % 16 == 0 && pitch <= kMostPitch));
+    return is_aligned(r.p, 16) && r.cols * size % 16 == 0 && (r.rows <= 1 || (pitch % 16 == 0 && pitch <= kMostPitch));
 }
 size_t packed_bytes(const Rows& r, int32_t dtype) { return lies_well(r, dtype) ? 0 : aligned((size_t)r.rows * (size_t)padded_bytes(r.cols, dtype)); }
 
@@ -109,10 +100,20 @@ template <typename T> struct OpOf;
 template <> struct OpOf<float> { typedef OfF32 type; };
 template <> struct OpOf<Bf16> { typedef OfBf16 type; };
 
-template <Made MADE, typename T>
-hipError_t gated_product(const typename ArgsOf<MADE>::type& p, hipStream_t s)
+// The kernel of the products of a layer's pairs of sums.
+ProductTile pair_tile(const fh_gated_layer& l)
 {
-    return product_of<typename OpOf<T>::type, MADE, T>(p, s);
+    return product_tile(l.tokens, 2 * l.hidden, padded_bytes(l.features, l.dtype) / kChunkBytes, l.dtype == FH_F32);
+}
+
+// The chunks of rows of `values`.
+template <typename T>
+void set_summed(ProductArgs& p, int64_t values)
+{
+    const int64_t bytes = values * (int64_t)sizeof(T);
+    p.chunks = p.chunks_each = (uint32_t)((bytes + kChunkBytes - 1) / kChunkBytes);
+    p.tail = (uint32_t)((bytes + 15) / 16 * 16 - (int64_t)(p.chunks - 1) * kChunkBytes);
+    p.parts = 1;
 }
 
 // The operands of the forward product.
@@ -134,7 +135,7 @@ hipError_t forward_operands(const fh_gated_layer& l, ProductArgs& p, Space& spac
     hipError_t e = take(f.x, p.a, p.a_pitch);
     if (e == hipSuccess) e = take(f.gate, p.b, p.b_pitch);
     if (e == hipSuccess) e = take(f.up, p.b2, p.b2_pitch);
-    p.chunks = (uint32_t)(padded_bytes(l.features, l.dtype) / kChunkBytes);
+    set_summed<T>(p, l.features);
     p.m = (uint32_t)l.tokens;
     p.n = (uint32_t)l.hidden;
     p.bias = l.b_gate;
@@ -153,31 +154,30 @@ hipError_t forward_of(const fh_gated_layer& l, hipStream_t s)
     if (e != hipSuccess) return e;
     p.out = l.h;
     p.stride = l.h_stride;
-    return gated_product<Made::gated, T>(p, s);
+    return product_by<typename OpOf<T>::type, Made::gated, T>(pair_tile(l), p, s);
 }
 
 // What the backward call lays out in its workspace.
 struct Backward {
-    int64_t d_values;                  // of a row of D
-    int64_t tokens_padded;             // of a row of D^T and x^T
-    int64_t tile_rows;                 // rows that a partial sum of the biases' gradients stands for
-    size_t d, d_turned, x_turned, w_turned, sums, forward;
-    size_t bytes() const { return d + d_turned + x_turned + w_turned + sums + forward; }
+    int64_t hidden_padded;             // columns of D's halves: whole chunks, so that the products over them have no tails, zeros behind the last
+    int64_t sum_rows;                  // rows that a partial sum of the biases' gradients stands for
+    ProductPlan weights;
+    size_t d, sums, parts, forward;
+    size_t bytes() const { return d + sums + parts + forward; }
 };
 Backward backward_of(const fh_gated_layer& l)
 {
     const size_t size = dtype_size(l.dtype);
     Backward b = {};
-    b.d_values = padded_bytes(2 * l.hidden, l.dtype) / (int64_t)size;
-    b.tokens_padded = padded_bytes(l.tokens, l.dtype) / (int64_t)size;
-    b.tile_rows = product_sum_rows(product_plan(l.tokens, 2 * l.hidden, padded_bytes(l.features, l.dtype) / kChunkBytes, l.dtype == FH_F32));
-    b.d = aligned((size_t)l.tokens * (size_t)b.d_values * size);
+    b.hidden_padded = padded_bytes(l.hidden, l.dtype) / (int64_t)size;
+    b.sum_rows = product_sum_rows(pair_tile(l));
+    b.d = aligned((size_t)l.tokens * (size_t)(2 * b.hidden_padded) * size);
+    if (l.db_gate || l.db_up) b.sums = aligned((size_t)((l.tokens + b.sum_rows - 1) / b.sum_rows) * 2u * (size_t)l.hidden * 4u);
     if (l.needs & FH_GATED_NEEDS_WEIGHT) {
-        b.d_turned = aligned((size_t)(2 * l.hidden) * (size_t)b.tokens_padded * size);
-        b.x_turned = aligned((size_t)l.features * (size_t)b.tokens_padded * size);
+        const int64_t m = b.hidden_padded + l.hidden;
+        b.weights = product_plan(m, l.features, padded_bytes(l.tokens, l.dtype) / kChunkBytes, l.dtype == FH_F32, true);
+        if (b.weights.parts > 1) b.parts = aligned((size_t)b.weights.parts * (size_t)m * (size_t)l.features * 4u);
     }
-    if (l.needs & FH_GATED_NEEDS_INPUT) b.w_turned = aligned((size_t)l.features * (size_t)b.d_values * size);
-    if (l.db_gate || l.db_up) b.sums = aligned((size_t)((l.tokens + b.tile_rows - 1) / b.tile_rows) * 2u * (size_t)l.hidden * 4u);
     b.forward = forward_bytes(l);
     return b;
 }
@@ -188,7 +188,7 @@ hipError_t clear(void* out, int64_t rows, int64_t cols, hipStream_t s)
 {
     if (!out) return hipSuccess;
     return in_parts(rows, 64, [&](int64_t first, int64_t count) {
-        return launch(clear_columns_kernel<T>, dim3((uint32_t)count), dim3(64), s, static_cast<T*>(out) + first * cols, cols, 0u, (uint32_t)cols);
+        return launch(clear_rows_kernel<T>, dim3((uint32_t)count), dim3(64), s, static_cast<T*>(out) + first * cols, (uint32_t)cols);
     });
 }
 
@@ -209,61 +209,74 @@ hipError_t backward_of(const fh_gated_layer& l, hipStream_t s)
     const Backward b = backward_of(l);
     Space space = {static_cast<uint8_t*>(l.workspace)};
     T* d = reinterpret_cast<T*>(space.take(b.d));
-    T* d_turned = reinterpret_cast<T*>(space.take(b.d_turned));
-    T* x_turned = reinterpret_cast<T*>(space.take(b.x_turned));
-    T* w_turned = reinterpret_cast<T*>(space.take(b.w_turned));
     float* sums = reinterpret_cast<float*>(space.take(b.sums));
+    float* parts = reinterpret_cast<float*>(space.take(b.parts));
+    typedef typename OpOf<T>::type Op;
 
     BackwardArgs p = {};
     e = forward_operands<T>(l, p, space, s);
     if (e != hipSuccess) return e;
     p.out = d;
-    p.stride = b.d_values;
+    p.stride = 2 * b.hidden_padded;
     p.dh = l.dh;
     p.dh_stride = l.dh_stride;
-    p.up_at = l.hidden;
+    p.up_at = b.hidden_padded;
     p.sums = b.sums ? sums : nullptr;
-    e = gated_product<Made::gated_backward, T>(p, s);
-    if (e == hipSuccess && b.sums)
-        e = launch_join(sums, (l.tokens + b.tile_rows - 1) / b.tile_rows, l.hidden, 2, l.dtype, l.db_gate, l.db_up, s);
+    e = product_by<Op, Made::gated_backward, T>(pair_tile(l), p, s);
+    if (e == hipSuccess && b.sums) e = launch_join(sums, (l.tokens + b.sum_rows - 1) / b.sum_rows, l.hidden, 2, l.dtype, l.db_gate, l.db_up, s);
 
     if (e == hipSuccess && (l.needs & FH_GATED_NEEDS_INPUT)) {
-        if (b.d_values > 2 * l.hidden)
-            e = in_parts(l.tokens, 64, [&](int64_t first, int64_t count) {
-                return launch(clear_columns_kernel<T>, dim3((uint32_t)count), dim3(64), s, d + first * b.d_values, b.d_values, (uint32_t)(2 * l.hidden), (uint32_t)b.d_values);
-            });
-        if (e == hipSuccess) e = transpose<T>(l.w_gate, l.hidden, l.features, l.w_gate_stride, w_turned, b.d_values, l.hidden, s);
-        if (e == hipSuccess) e = transpose<T>(l.w_up, l.hidden, l.features, l.w_up_stride, w_turned + l.hidden, b.d_values, b.d_values - l.hidden, s);
-        ProductArgs q = {};
+        TurnedArgs q = {};
         q.a = reinterpret_cast<const uint8_t*>(d);
-        q.b = reinterpret_cast<const uint8_t*>(w_turned);
-        q.a_pitch = q.b_pitch = (uint32_t)(b.d_values * size);
-        q.chunks = q.a_pitch / kChunkBytes;
+        q.a_pitch = (uint32_t)(2 * b.hidden_padded * size);
+        set_summed<T>(q, 2 * b.hidden_padded);
+        q.b = p.b;
+        q.b2 = p.b2;
+        q.b_pitch = p.b_pitch;
+        q.b2_pitch = p.b2_pitch;
+        q.summed = (uint32_t)l.hidden;
+        q.split = q.chunks / 2;
         q.m = (uint32_t)l.tokens;
         q.n = (uint32_t)l.features;
         q.out = l.dx;
         q.stride = l.features;
-        if (e == hipSuccess) e = gated_product<Made::linear, T>(q, s);
+        e = product_by<Op, Made::linear, T, Lies::rows, Lies::columns>(product_tile(q.m, q.n, q.chunks, sizeof(T) == 4), q, s);
     }
     if (e == hipSuccess && (l.needs & FH_GATED_NEEDS_WEIGHT)) {
-        e = transpose<T>(d, l.tokens, 2 * l.hidden, b.d_values, d_turned, b.tokens_padded, b.tokens_padded, s);
-        if (e == hipSuccess) e = transpose<T>(l.x, l.tokens, l.features, l.x_stride, x_turned, b.tokens_padded, b.tokens_padded, s);
-        ProductArgs q = {};
-        q.a = reinterpret_cast<const uint8_t*>(d_turned);
-        q.b = reinterpret_cast<const uint8_t*>(x_turned);
-        q.a_pitch = q.b_pitch = (uint32_t)(b.tokens_padded * size);
-        q.chunks = q.a_pitch / kChunkBytes;
+        TurnedArgs q = {};
+        q.a = reinterpret_cast<const uint8_t*>(d);
+        q.a_pitch = (uint32_t)(2 * b.hidden_padded * size);
+        q.b = p.a;
+        q.b_pitch = p.a_pitch;
+        set_summed<T>(q, l.tokens);
+        q.summed = (uint32_t)l.tokens;
+        q.split = q.chunks;
         q.n = (uint32_t)l.features;
         q.stride = l.features;
+        if (b.weights.parts > 1) {
+            q.m = (uint32_t)(b.hidden_padded + l.hidden);
+            q.parts = b.weights.parts;
+            q.chunks_each = b.weights.chunks_each;
+            q.out = parts;
+            e = product_by<Op, Made::linear, float, Lies::columns, Lies::columns>(b.weights.tile, q, s);
+            const int64_t runs = (l.features + 3) / 4;
+            const auto join = [&](int64_t groups) {
+                return launch(join_weights_kernel<T>, dim3((uint32_t)groups), dim3(256), s, parts, q.parts, (uint32_t)l.hidden, (uint32_t)b.hidden_padded, q.n, (uint32_t)runs,
+                              static_cast<T*>(l.dw_gate), static_cast<T*>(l.dw_up));
+            };
+            if (e == hipSuccess) e = join((2 * l.hidden * runs + 255) / 256);
+            return e;
+        }
         // both weights' gradients at once where they lie one behind the other
-        const bool one = static_cast<T*>(l.dw_up) == static_cast<T*>(l.dw_gate) + l.hidden * l.features;
+        const bool one = b.hidden_padded == l.hidden && static_cast<T*>(l.dw_up) == static_cast<T*>(l.dw_gate) + l.hidden * l.features;
         q.m = (uint32_t)(one ? 2 * l.hidden : l.hidden);
         q.out = l.dw_gate;
-        if (e == hipSuccess) e = gated_product<Made::linear, T>(q, s);
-        if (!one) {
-            q.a += l.hidden * (int64_t)q.a_pitch;
+        const ProductTile tile = product_tile(q.m, q.n, q.chunks, sizeof(T) == 4);
+        e = product_by<Op, Made::linear, T, Lies::columns, Lies::columns>(tile, q, s);
+        if (e == hipSuccess && !one) {
+            q.a += b.hidden_padded * size;
             q.out = l.dw_up;
-            if (e == hipSuccess) e = gated_product<Made::linear, T>(q, s);
+            e = product_by<Op, Made::linear, T, Lies::columns, Lies::columns>(tile, q, s);
         }
     }
     return e;

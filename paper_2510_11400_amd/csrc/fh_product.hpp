@@ -21,6 +21,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // The operands' types: lane (r = lane % 32, h = lane / 32) gets the outputs [8 (i/4) + 4 h + i % 4][r], the first index the first operand's row.
 struct OfQ8 {
+    static constexpr uint32_t kSize = 1;
     typedef i32x16 Sums;                                         // whole numbers: exact in any order
     typedef int Sum;
     static constexpr bool kScaled = true;
@@ -30,6 +31,7 @@ struct OfQ8 {
     }
 };
 struct OfBf16 {
+    static constexpr uint32_t kSize = 2;
     typedef f32x16 Sums;
     typedef float Sum;
     static constexpr bool kScaled = false;
@@ -39,6 +41,7 @@ struct OfBf16 {
     }
 };
 struct OfF32 {
+    static constexpr uint32_t kSize = 4;
     typedef f32x16 Sums;
     typedef float Sum;
     static constexpr bool kScaled = false;
@@ -61,24 +64,33 @@ enum class Made : int32_t {
 struct ProductArgs {
     const uint8_t *a, *b, *b2;         // b2: up, where b is the gate
     const void    *bias, *bias2;       // may be null
-    void*          out;
+    void*          out;                // parts > 1: float [parts][m][n]
     int64_t        stride;             // of out, in elements
     uint32_t       a_pitch, b_pitch, b2_pitch;                   // bytes from row to row
     uint32_t       chunks;             // of a row
+    uint32_t       tail;               // bytes of a row's last chunk: a multiple of 16
+    uint32_t       parts, chunks_each; // workgroups that share a tile's sum, chunks of each
     uint32_t       m, n;               // rows of out, columns of out
     uint32_t       m_tiles, n_tiles;
     uint32_t       first;              // workgroup of the launches before this one, or from a workgroup's tile to its next one
     int16_t        bias_dtype, act;
 };
 static_assert(sizeof(ProductArgs) <= 112, "longer arguments are enqueued a microsecond later");
-struct BackwardArgs : ProductArgs {    // out: the gate's gradients, and `up_at` columns further those of up
+struct BackwardArgs : ProductArgs {    // out: the gate's gradients, and `up_at` columns further those of up; zeros from column n to up_at
     const void*    dh;
     int64_t        dh_stride;
     int64_t        up_at;
     float*         sums;               // [m_tiles][2][n] sums of the columns over the tile's rows, or null
 };
-template <Made MADE> struct ArgsOf { typedef ProductArgs type; };
-template <> struct ArgsOf<Made::gated_backward> { typedef BackwardArgs type; };
+struct TurnedArgs : ProductArgs {      // products with an operand that lies by columns: its rows are the summed dimension
+    uint32_t       summed;             // rows of a and b where they lie so
+    uint32_t       split;              // chunks that b has; b2 goes on behind them
+};
+// How an operand lies: its rows by the summed dimension, or the summed dimension's rows by it.
+enum class Lies { rows, columns };
+template <Made MADE, Lies B> struct ArgsOf { typedef ProductArgs type; };
+template <> struct ArgsOf<Made::gated_backward, Lies::rows> { typedef BackwardArgs type; };
+template <> struct ArgsOf<Made::linear, Lies::columns> { typedef TurnedArgs type; };
 
 // A stored matrix in 8-bit integers has its rows' scales behind them.  No chunks: the sums are 0 and there are no scales.
 template <typename OP>
@@ -95,6 +107,57 @@ __device__ __forceinline__ float made_of(typename OP::Sum sum, float scales, flo
     else return sum + bias;
 }
 
+// A buffer that is the same in all lanes, where the compiler has worked it out in vector registers.
+__device__ __forceinline__ u32x4 in_scalars(u32x4 b)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = __builtin_amdgcn_readfirstlane(b[i]);
+    return b;
+}
+
+// An operand that lies by columns, in LDS: the rows of a chunk (64 of bf16, 32 of fp32) one behind the other, COLS columns of each, 128 * COLS bytes as
+// by rows.  In row k the pieces of 16 bytes are turned by turn(k), so that what a wave reads at a time meets all banks: of bf16 four rows
+// of 64 bytes (a transposing read gives a lane four rows of its column), of fp32 one row for each half of the wave.
+template <typename OP, int COLS>
+struct ByColumns {
+    static constexpr uint32_t kRow = COLS * OP::kSize, kPieces = kRow / 16, kRows = kChunkBytes / OP::kSize;   // bytes, pieces of a row; rows of a chunk
+    static __device__ __forceinline__ uint32_t turn(uint32_t k)
+    {
+        if constexpr (OP::kSize == 2) return kPieces >= 16 ? (k & 3) << 2 : kPieces == 8 ? (k & 2) << 1 : 0;
+        else return kPieces >= 16 ? (k >> 4 & 1) << 3 : 0;
+    }
+    // Where a lane's 16 bytes at `at` of the operand's LDS come from: row and byte of the row.
+    static __device__ __forceinline__ uint32_t row_of(uint32_t at) { return at / kRow; }
+    static __device__ __forceinline__ uint32_t byte_of(uint32_t at) { return ((at % kRow / 16) ^ turn(row_of(at))) * 16; }
+    // 16 bytes a lane of 32 columns from `col` on: summed rows (4 h + quarter) of the chunk's eighths.
+    static __device__ __forceinline__ u32x4 read(const uint8_t* s, uint32_t col, int quarter, int lane)
+    {
+        if constexpr (OP::kSize == 2) {
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            const uint32_t i = lane & 15, k = (lane >> 5) * 32 + (i >> 2), piece = (col >> 3) + (lane >> 4 & 1) * 2 + (i >> 1 & 1);
+            const uint8_t* from = s + k * kRow + (piece ^ turn(k)) * 16 + (i & 1) * 8 + quarter * 8 * kRow;
+            const s16x4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)from);
+            const s16x4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(from + 4 * kRow));
+            const u32x2 a = __builtin_bit_cast(u32x2, low), b = __builtin_bit_cast(u32x2, high);
+            return u32x4{a.x, a.y, b.x, b.y};
+        } else {
+            const uint32_t k = (lane >> 5) * 16, c = col + (lane & 31);
+            const uint8_t* from = s + k * kRow + ((c >> 2) ^ turn(k)) * 16 + (c & 3) * 4 + quarter * 4 * kRow;
+            u32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const uint32_t*>(from + e * kRow);
+            return v;
+        }
+    }
+    // The buffer of chunk `chunk` from column `col` on, of `rows` x `cols`, whose last 16 bytes are whole: what is past the rows is read as zeros, past
+    // the columns as zeros or another row's.
+    static __device__ __forceinline__ u32x4 buffer(const uint8_t* p, uint32_t pitch, uint32_t chunk, uint32_t rows, uint32_t col, uint32_t cols)
+    {
+        const uint32_t row = chunk * kRows, left = row >= rows ? 0u : rows - row < kRows ? rows - row : kRows;
+        return in_scalars(buffer_of(p + (int64_t)row * pitch + (int64_t)col * OP::kSize, left ? (left - 1) * pitch + ((cols - col) * OP::kSize + 15) / 16 * 16 : 0u));
+    }
+};
+
 template <typename T> __device__ __forceinline__ void load4(const T* p, int64_t n, float (&v)[4])
 {
     Run<T, 4> r;
@@ -107,64 +170,103 @@ template <typename T> __device__ __forceinline__ void load4(const T* p, int64_t 
 // (32 MT) x (32 NT) sums a workgroup; each wave multiplies every WAVES-th chunk by itself, with an area of LDS of its own and no
 // barrier: a chunk's rows come as whole lines into the area, from there to registers, and while those are multiplied the next chunk's
 // come.  The waves' sums are joined in LDS in the waves' order.
-template <typename OP, Made MADE, typename T, int MT, int NT, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void product_waves_kernel(typename ArgsOf<MADE>::type p)
+template <typename OP, Made MADE, Lies LA, Lies LB, typename T, int MT, int NT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void product_waves_kernel(typename ArgsOf<MADE, LB>::type p)
 {
     constexpr int kRowsA = MT * 32, kRowsB = NT * 32, kPad = kRowsB + 4;
     constexpr bool kPair = MADE != Made::linear;
     constexpr int kCols = kPair ? kRowsB / 2 : kRowsB;           // columns of the tile
     constexpr uint32_t kCodes = (kRowsA + kRowsB) * kChunkBytes, kSums = kRowsA * kPad * 4, kArea = kCodes > kSums ? kCodes : kSums;
     constexpr int kThreads = WAVES * 64, kRuns = kCols / 4, kSteps = (kRowsA * kRuns + kThreads - 1) / kThreads;
+    typedef ByColumns<OP, kRowsA> ColumnsA;
+    typedef ByColumns<OP, kRowsB> ColumnsB;
     static_assert(kThreads % kRuns == 0, "a thread stays with its columns");
     __shared__ __attribute__((aligned(16))) uint8_t s_area[WAVES * kArea];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t number = p.first + blockIdx.x, tiles = p.m_tiles * p.n_tiles, share = p.parts > 1 ? number / tiles : 0;
     uint32_t i, j;
-    in_bands(p.first + blockIdx.x, p.m_tiles, p.n_tiles, i, j);
+    in_bands(number - share * tiles, p.m_tiles, p.n_tiles, i, j);
     const uint32_t i0 = i * kRowsA, j0 = j * kCols;
-    // rows past the last are the last one, so that every address is inside
-    const uint32_t rows_a = p.m - i0 < kRowsA ? p.m - i0 : kRowsA, rows_b = p.n - j0 < kCols ? p.n - j0 : kCols;
-    const uint32_t width = p.chunks * kChunkBytes;
-    const u32x4 from_a = buffer_of(p.a + (int64_t)i0 * p.a_pitch, (rows_a - 1) * p.a_pitch + width);
-    const u32x4 from_b = buffer_of(p.b + (int64_t)j0 * p.b_pitch, (rows_b - 1) * p.b_pitch + width);
-    const u32x4 from_b2 = kPair ? buffer_of(p.b2 + (int64_t)j0 * p.b2_pitch, (rows_b - 1) * p.b2_pitch + width) : from_b;
     const uint32_t piece = ((lane & 7) ^ (lane >> 4)) * 16;      // turned by half the row's number, 4 more for every other eight rows
+    const uint32_t width = (p.chunks - 1) * kChunkBytes + p.tail;
+    // rows past the last are the last one, so that every address is inside; pieces past a row's end are past the buffer's, which reads as zeros
+    u32x4 from_a, from_b, from_b2;
     uint32_t at_a[MT * 4], at_b[NT * 4];
+    if constexpr (LA == Lies::rows) {
+        const uint32_t rows_a = p.m - i0 < kRowsA ? p.m - i0 : kRowsA;
+        from_a = buffer_of(p.a + (int64_t)i0 * p.a_pitch, (rows_a - 1) * p.a_pitch + width);
 #pragma unroll
-    for (int t = 0; t < MT * 4; ++t) {
-        const uint32_t r = t * 8 + (lane >> 3);
-        at_a[t] = (r < rows_a ? r : rows_a - 1) * p.a_pitch + (piece ^ (t & 1) * 64);
+        for (int t = 0; t < MT * 4; ++t) {
+            const uint32_t r = t * 8 + (lane >> 3);
+            at_a[t] = (r < rows_a ? r : rows_a - 1) * p.a_pitch + (piece ^ (t & 1) * 64);
+        }
+    } else {
+#pragma unroll
+        for (int t = 0; t < MT * 4; ++t) at_a[t] = ColumnsA::row_of(t * 1024 + lane * 16) * p.a_pitch + ColumnsA::byte_of(t * 1024 + lane * 16);
     }
+    if constexpr (LB == Lies::rows) {
+        const uint32_t row_b = j0 < p.n ? j0 : p.n - 1, rows_b = p.n - row_b < kCols ? p.n - row_b : kCols;
+        from_b = buffer_of(p.b + (int64_t)row_b * p.b_pitch, (rows_b - 1) * p.b_pitch + width);
+        from_b2 = kPair ? buffer_of(p.b2 + (int64_t)row_b * p.b2_pitch, (rows_b - 1) * p.b2_pitch + width) : from_b;
 #pragma unroll
-    for (int t = 0; t < NT * 4; ++t) {
-        const uint32_t r = (t * 8 + (lane >> 3)) % kCols, pitch = t * 8 < kCols ? p.b_pitch : p.b2_pitch;
-        at_b[t] = (r < rows_b ? r : rows_b - 1) * pitch + (piece ^ (t & 1) * 64);
+        for (int t = 0; t < NT * 4; ++t) {
+            const uint32_t r = (t * 8 + (lane >> 3)) % kCols, pitch = t * 8 < kCols ? p.b_pitch : p.b2_pitch;
+            at_b[t] = (r < rows_b ? r : rows_b - 1) * pitch + (piece ^ (t & 1) * 64);
+        }
     }
     uint8_t* area = s_area + wave * kArea;
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_area + wave * kArea;
+    constexpr uint32_t kNowhere = 1u << 31;                      // past the end of any buffer here
     const auto load = [&](uint32_t chunk) {
+        const bool cut = chunk + 1 == p.chunks && p.tail < kChunkBytes;
+        if constexpr (LA == Lies::rows) {
 #pragma unroll
-        for (int t = 0; t < MT * 4; ++t) to_lds(lds + t * 1024, from_a, at_a[t], chunk * kChunkBytes);
+            for (int t = 0; t < MT * 4; ++t)
+                to_lds(lds + t * 1024, from_a, cut && (piece ^ (t & 1) * 64) >= p.tail ? kNowhere : at_a[t], chunk * kChunkBytes);
+        } else {
+            from_a = ColumnsA::buffer(p.a, p.a_pitch, chunk, p.summed, i0, p.m);
 #pragma unroll
-        for (int t = 0; t < NT * 4; ++t) to_lds(lds + kRowsA * kChunkBytes + t * 1024, t * 8 < kCols ? from_b : from_b2, at_b[t], chunk * kChunkBytes);
+            for (int t = 0; t < MT * 4; ++t) to_lds(lds + t * 1024, from_a, at_a[t], 0);
+        }
+        if constexpr (LB == Lies::rows) {
+#pragma unroll
+            for (int t = 0; t < NT * 4; ++t)
+                to_lds(lds + kRowsA * kChunkBytes + t * 1024, t * 8 < kCols ? from_b : from_b2, cut && (piece ^ (t & 1) * 64) >= p.tail ? kNowhere : at_b[t],
+                       chunk * kChunkBytes);
+        } else {
+            const bool second = chunk >= p.split;
+            const uint32_t pitch = second ? p.b2_pitch : p.b_pitch;
+            from_b = ColumnsB::buffer(second ? p.b2 : p.b, pitch, second ? chunk - p.split : chunk, p.summed, j0, p.n);
+#pragma unroll
+            for (int t = 0; t < NT * 4; ++t)
+                to_lds(lds + kRowsA * kChunkBytes + t * 1024, from_b, ColumnsB::row_of(t * 1024 + lane * 16) * pitch + ColumnsB::byte_of(t * 1024 + lane * 16), 0);
+        }
     };
     const int h = lane >> 5, r = lane & 31, turned = (h * 4) ^ (lane >> 1 & 7);
     typename OP::Sums c[MT][NT] = {};
-    uint32_t k = wave;
-    if (k < p.chunks) load(k);
-    while (k < p.chunks) {
+    uint32_t k = share * p.chunks_each + wave;
+    const uint32_t end = p.chunks - share * p.chunks_each < p.chunks_each ? p.chunks : (share + 1) * p.chunks_each;
+    if (k < end) load(k);
+    while (k < end) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         u32x4 fa[4][MT], fb[4][NT];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const uint8_t* from = area + (uint32_t)(turned ^ q) * 16 + r * kChunkBytes;
 #pragma unroll
-            for (int t = 0; t < NT; ++t) fb[q][t] = *reinterpret_cast<const u32x4*>(from + kRowsA * kChunkBytes + t * 4096);
+            for (int t = 0; t < NT; ++t) {
+                if constexpr (LB == Lies::rows) fb[q][t] = *reinterpret_cast<const u32x4*>(from + kRowsA * kChunkBytes + t * 4096);
+                else fb[q][t] = ColumnsB::read(area + kRowsA * kChunkBytes, t * 32, q, lane);
+            }
 #pragma unroll
-            for (int t = 0; t < MT; ++t) fa[q][t] = *reinterpret_cast<const u32x4*>(from + t * 4096);
+            for (int t = 0; t < MT; ++t) {
+                if constexpr (LA == Lies::rows) fa[q][t] = *reinterpret_cast<const u32x4*>(from + t * 4096);
+                else fa[q][t] = ColumnsA::read(area, t * 32, q, lane);
+            }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the area may be written again
         k += WAVES;
-        if (k < p.chunks) load(k);
+        if (k < end) load(k);
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -213,7 +315,7 @@ __global__ __launch_bounds__(WAVES * 64) void product_waves_kernel(typename Args
         if constexpr (!kPair) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = made_of<OP>(sum[e], mine * scales[e], bias[e]);
-            store4(static_cast<T*>(p.out) + (int64_t)i * p.stride + at, left, v);
+            store4(static_cast<T*>(p.out) + (int64_t)share * p.m * p.n + (int64_t)i * p.stride + at, left, v);
         } else {
             const Sum4 sum2 = sum_at(row, kCols + col);
             float gate[4], up[4];
@@ -232,14 +334,14 @@ __global__ __launch_bounds__(WAVES * 64) void product_waves_kernel(typename Args
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const Activated a = activated_both(gate[e], p.act);
-                    v[e] = dh[e] * up[e] * a.slope;
-                    dup[e] = dh[e] * a.value;
+                    v[e] = e < left ? dh[e] * up[e] * a.slope : 0.0f;
+                    dup[e] = e < left ? dh[e] * a.value : 0.0f;
                     sums[0][e] += v[e];
                     sums[1][e] += dup[e];
                 }
                 T* to = static_cast<T*>(p.out) + (int64_t)i * p.stride + at;
-                store4(to, left, v);
-                store4(to + p.up_at, left, dup);
+                store4(to, p.up_at - at, v);
+                store4(to + p.up_at, p.up_at - at, dup);
             }
         }
     }
@@ -260,17 +362,26 @@ __global__ __launch_bounds__(WAVES * 64) void product_waves_kernel(typename Args
     }
 }
 
-template <typename OP, Made MADE, typename T, int MT, int NT, int WAVES>
-hipError_t product_waves(typename ArgsOf<MADE>::type p, hipStream_t s)
+// The tiles of a product in squares (or halves of them, for a pair) of `side` sums.
+template <Made MADE, typename Args>
+int64_t tiles_of(Args& p, uint32_t side)
 {
-    constexpr uint32_t kCols = NT * (MADE == Made::linear ? 32 : 16);
-    p.m_tiles = (p.m + MT * 32 - 1) / (MT * 32);
-    p.n_tiles = (p.n + kCols - 1) / kCols;
-    const int64_t groups = (int64_t)p.m_tiles * p.n_tiles;
+    const uint32_t cols = MADE == Made::linear ? side : side / 2;
+    uint32_t n = p.n;
+    if constexpr (MADE == Made::gated_backward) n = (uint32_t)p.up_at;   // the zeros behind the last column are written too
+    p.m_tiles = (p.m + side - 1) / side;
+    p.n_tiles = (n + cols - 1) / cols;
+    return (int64_t)p.m_tiles * p.n_tiles;
+}
+template <typename OP, Made MADE, Lies LA, Lies LB, typename T, int MT, int NT, int WAVES>
+hipError_t product_waves(typename ArgsOf<MADE, LB>::type p, hipStream_t s)
+{
+    static_assert(MT == NT, "squares");
+    const int64_t groups = tiles_of<MADE>(p, MT * 32) * p.parts;
     if (groups > INT32_MAX) return hipErrorInvalidValue;
     return in_parts(groups, WAVES * 64, [&](int64_t first, int64_t count) {
         p.first = (uint32_t)first;
-        return launch(product_waves_kernel<OP, MADE, T, MT, NT, WAVES>, dim3((uint32_t)count), dim3(WAVES * 64), s, p);
+        return launch(product_waves_kernel<OP, MADE, LA, LB, T, MT, NT, WAVES>, dim3((uint32_t)count), dim3(WAVES * 64), s, p);
     });
 }
 
@@ -355,8 +466,13 @@ __device__ __forceinline__ void pair_epilogue(const Args& p, const typename OP::
                 }
             }
             T* to = static_cast<T*>(p.out) + (int64_t)i * p.stride + col;
-            store4(to, i < p.m ? left : 0, v);
-            if constexpr (MADE == Made::gated_backward) store4(to + p.up_at, i < p.m ? left : 0, w);
+            if constexpr (MADE == Made::gated) {
+                store4(to, i < p.m ? left : 0, v);
+            } else {
+                const int64_t most = i < p.m ? p.up_at - col : 0;
+                store4(to, most, v);
+                store4(to + p.up_at, most, w);
+            }
         }
     }
     if constexpr (MADE == Made::gated_backward) {
@@ -391,64 +507,107 @@ __device__ __forceinline__ void pair_epilogue(const Args& p, const typename OP::
 // memory operations are counted in their order and the next wait is for the load alone.
 // Of a pair's 64 columns of a wave the first 32 are the gate's and the others the same columns of up, so that both sums of an output are one wave's.
 // Its outputs go through LDS of their own, so that the next load is sent before all of them.
-template <typename OP, Made MADE, typename T, int B, int WN>
-__global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_kernel(typename ArgsOf<MADE>::type p)
+template <typename OP, Made MADE, Lies LA, Lies LB, typename T, int B, int WN>
+__global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_kernel(typename ArgsOf<MADE, LB>::type p)
 {
     constexpr bool kPair = MADE != Made::linear;
     constexpr int kWaves = 2 * WN, kHalf = kWaves / 2, MT = B / 64, NT = 2, kCols = kPair ? B / 2 : B;
     constexpr uint32_t kStage = 2 * B * kChunkBytes;
     constexpr int kRun = 16 / sizeof(T), kLanes = 64 / kRun, kRows = 64 / kLanes;
     constexpr int kStores = kPair ? MT * 4 * (MADE == Made::gated ? 1 : 2) : MT * 32 / kRows;
-    static_assert(kHalf * 64 == B && WN * 64 == B, "a wave loads 64 rows of one operand, and has 64 columns");
+    typedef ByColumns<OP, B> Columns;
+    static_assert(kHalf * 64 == B && WN * 64 == B, "a wave loads an 8 KiB of one operand, and has 64 columns");
     __shared__ __attribute__((aligned(16))) uint8_t s_stage[2 * kStage + (kPair ? kWaves * 4096 : 0)];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
 
-    const uint32_t tiles = p.m_tiles * p.n_tiles, xcd = blockIdx.x & 7;
+    const uint32_t squares = p.m_tiles * p.n_tiles, tiles = squares * p.parts, xcd = blockIdx.x & 7;
     const uint32_t end_tile = run_of(xcd, tiles) + (tiles >> 3) + (xcd < (tiles & 7) ? 1 : 0);
+    const auto share_of = [&](uint32_t tile) { return p.parts > 1 ? tile / squares : 0u; };
     const auto corner = [&](uint32_t tile, uint32_t& i0, uint32_t& j0) {
-        in_bands(tile, p.m_tiles, p.n_tiles, i0, j0);
+        in_bands(tile - share_of(tile) * squares, p.m_tiles, p.n_tiles, i0, j0);
         i0 *= B;
         j0 *= kCols;
     };
+    const auto end_of = [&](uint32_t share) { return p.chunks - share * p.chunks_each < p.chunks_each ? p.chunks : (share + 1) * p.chunks_each; };
 
-    // what is loaded next: a chunk of a tile, in this wave 64 rows of one operand, two times 32 of a buffer each
+    // what is loaded next: a chunk of a tile, in this wave 8 KiB of one operand: by rows 64 of these, two times 32 of a buffer each
     const bool of_b = wave >= kHalf;
     const int part = wave % kHalf;
-    const uint32_t width = p.chunks * kChunkBytes, end = p.chunks;
-    const uint32_t pitch = of_b ? p.b_pitch : p.a_pitch, pitch2 = kPair && of_b ? p.b2_pitch : pitch;
-    uint32_t next_tile = run_of(blockIdx.x, tiles), next_chunk = 0;
-    u32x4 from, from2;
-    const uint32_t piece_at = ((lane & 7) ^ (lane >> 4)) * 16, at = (lane >> 3) * pitch + piece_at, at2 = (lane >> 3) * pitch2 + piece_at;
+    const uint32_t width = (p.chunks - 1) * kChunkBytes + p.tail;
+    uint32_t next_tile = run_of(blockIdx.x, tiles), next_chunk = 0, next_end = 0, next_corner = 0;
+    u32x4 from = {}, from2 = {};
+    const uint32_t piece_at = ((lane & 7) ^ (lane >> 4)) * 16;
     const auto aim = [&]() {
         uint32_t i0, j0;
         corner(next_tile, i0, j0);
-        // rows past the last are past the buffer's end: nothing is read for them, and nothing of theirs is stored
+        next_corner = of_b ? j0 : i0;
+        const uint32_t share = share_of(next_tile);
+        next_chunk = share * p.chunks_each;
+        next_end = end_of(share);
+        // rows past the last are past the buffer's end: zeros are read for them, and nothing of theirs is stored
         const auto rows_of = [&](const uint8_t* base, uint32_t row0, uint32_t all, uint32_t row_pitch) {
             const uint32_t rows = row0 >= all ? 0u : all - row0 < 32u ? all - row0 : 32u;
             return buffer_of(base + (int64_t)(rows ? row0 : 0u) * row_pitch, rows ? (rows - 1) * row_pitch + width : 0u);
         };
-        if (kPair && of_b) {
-            from = rows_of(p.b, j0 + part * 32, p.n, pitch);
-            from2 = rows_of(p.b2, j0 + part * 32, p.n, pitch2);
-        } else {
-            const uint8_t* base = of_b ? p.b : p.a;
-            const uint32_t row0 = (of_b ? j0 : i0) + part * 64, all = of_b ? p.n : p.m;
-            from = rows_of(base, row0, all, pitch);
-            from2 = rows_of(base, row0 + 32, all, pitch);
+        if (of_b ? LB == Lies::rows : LA == Lies::rows) {
+            if (kPair && of_b) {
+                from = rows_of(p.b, j0 + part * 32, p.n, p.b_pitch);
+                from2 = rows_of(p.b2, j0 + part * 32, p.n, p.b2_pitch);
+            } else {
+                const uint8_t* base = of_b ? p.b : p.a;
+                const uint32_t row0 = next_corner + part * 64, all = of_b ? p.n : p.m, pitch = of_b ? p.b_pitch : p.a_pitch;
+                from = rows_of(base, row0, all, pitch);
+                from2 = rows_of(base, row0 + 32, all, pitch);
+            }
         }
     };
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_stage;
-    const auto load = [&](uint32_t stage) {
-        if (next_tile >= end_tile) return;
-        uint32_t row_at = at, row_at2 = at2;
-        asm("" : "+v"(row_at), "+v"(row_at2));                   // sums made here, not registers kept
+    const auto load_rows = [&](uint32_t to) {
+        const uint32_t pitch = of_b ? p.b_pitch : p.a_pitch, pitch2 = kPair && of_b ? p.b2_pitch : pitch;
+        uint32_t l = lane;
+        asm("" : "+v"(l));                                       // offsets made here, not registers kept
+        uint32_t even = piece_at, odd = piece_at ^ 64;
+        constexpr uint32_t kNowhere = 1u << 31;                  // past the end of any buffer here: zeros
+        if (next_chunk + 1 == p.chunks && p.tail < kChunkBytes) {
+            if (even >= p.tail) even = kNowhere;
+            if (odd >= p.tail) odd = kNowhere;
+        }
+        const uint32_t at = (l >> 3) * pitch, at2 = (l >> 3) * pitch2;
 #pragma unroll
         for (int t = 0; t < 8; ++t)
-            to_lds(lds + stage + wave * 8192 + t * 1024, t < 4 ? from : from2, ((t < 4 ? row_at : row_at2) ^ (t & 1) * 64) + t % 4 * 8 * (t < 4 ? pitch : pitch2),
-                   next_chunk * kChunkBytes);
-        if (++next_chunk == end) {
-            next_chunk = 0;
+            to_lds(to + t * 1024, t < 4 ? from : from2, (t & 1 ? odd : even) + (t < 4 ? at : at2) + t % 4 * 8 * (t < 4 ? pitch : pitch2), next_chunk * kChunkBytes);
+    };
+    const auto load_columns = [&](uint32_t to) {
+        const uint8_t* base = p.a;
+        uint32_t pitch = p.a_pitch, chunk = next_chunk, summed = 0;
+        if constexpr (LB == Lies::columns) {
+            summed = p.summed;
+            if (of_b) {
+                const bool second = chunk >= p.split;
+                base = second ? p.b2 : p.b;
+                pitch = second ? p.b2_pitch : p.b_pitch;
+                chunk = second ? chunk - p.split : chunk;
+            }
+        }
+        const u32x4 here = Columns::buffer(base, pitch, chunk, summed, next_corner, of_b ? p.n : p.m);
+        uint32_t at = part * 8192 + lane * 16;
+        asm("" : "+v"(at));
+#pragma unroll
+        for (int t = 0; t < 8; ++t) to_lds(to + t * 1024, here, Columns::row_of(at + t * 1024) * pitch + Columns::byte_of(at + t * 1024), 0);
+    };
+    const auto load = [&](uint32_t stage) {
+        if (next_tile >= end_tile) return;
+        const uint32_t to = lds + stage + wave * 8192;
+        if constexpr (LA == LB) {
+            if constexpr (LA == Lies::rows) load_rows(to);
+            else load_columns(to);
+        } else if (of_b) {
+            load_columns(to);
+        } else {
+            load_rows(to);
+        }
+        if (++next_chunk == next_end) {
             next_tile += p.first;
             if (next_tile < end_tile) aim();
         }
@@ -460,9 +619,15 @@ __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_ker
     const auto read = [&](uint32_t stage, int quarter, int to) {
         const uint8_t* at_piece = s_stage + stage + (uint32_t)(turned ^ quarter) * 16;
 #pragma unroll
-        for (int t = 0; t < MT; ++t) fa[to][t] = *reinterpret_cast<const u32x4*>(at_piece + read_a + t * 4096);
+        for (int t = 0; t < MT; ++t) {
+            if constexpr (LA == Lies::rows) fa[to][t] = *reinterpret_cast<const u32x4*>(at_piece + read_a + t * 4096);
+            else fa[to][t] = Columns::read(s_stage + stage, (wm * MT + t) * 32, quarter, lane);
+        }
 #pragma unroll
-        for (int t = 0; t < NT; ++t) fb[to][t] = *reinterpret_cast<const u32x4*>(at_piece + read_b + t * 4096);
+        for (int t = 0; t < NT; ++t) {
+            if constexpr (LB == Lies::rows) fb[to][t] = *reinterpret_cast<const u32x4*>(at_piece + read_b + t * 4096);
+            else fb[to][t] = Columns::read(s_stage + stage + B * kChunkBytes, (wn * NT + t) * 32, quarter, lane);
+        }
     };
     typename OP::Sums c[MT][NT];
     // Sums run along b's rows within a lane.
@@ -488,6 +653,7 @@ __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_ker
     for (; tile < end_tile; tile += p.first) {
         uint32_t i0, j0;
         corner(tile, i0, j0);
+        const uint32_t share = share_of(tile), begin = share * p.chunks_each, end = end_of(share);
         float bias_here = 0.0f, scale_here = 0.0f;               // of the wave's column `lane`
 #pragma unroll
         for (int x = 0; x < MT; ++x)
@@ -495,11 +661,11 @@ __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_ker
             for (int y = 0; y < NT; ++y) c[x][y] = typename OP::Sums{};
         if constexpr (kPair) read(stage, 0, 0);
 #pragma clang loop unroll(disable)
-        for (uint32_t k = 0; k < end; ++k) {
+        for (uint32_t k = begin; k < end; ++k) {
             if (!kPair && k + 1 == end) {
                 const uint32_t col = j0 + wn * 64 + lane, inside = col < p.n ? col : p.n - 1;
                 if (p.bias) bias_here = parameter(p.bias, p.bias_dtype, inside, 0.0f);
-                scale_here = scale_of<OP>(p.b, p.n, p.b_pitch, end, inside);
+                scale_here = scale_of<OP>(p.b, p.n, p.b_pitch, p.chunks, inside);
             }
             read(stage, 1, 1);
             multiply(0);
@@ -534,7 +700,7 @@ __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_ker
 #pragma unroll
                 for (int x = 0; x < MT; ++x) {
                     const uint32_t row = i0 + (wm * MT + x) * 32 + row32;
-                    row_scale[x] = OP::kScaled ? scale_of<OP>(p.a, p.m, p.a_pitch, end, row < p.m ? row : p.m - 1) : 1.0f;
+                    row_scale[x] = OP::kScaled ? scale_of<OP>(p.a, p.m, p.a_pitch, p.chunks, row < p.m ? row : p.m - 1) : 1.0f;
                 }
 #pragma unroll
                 for (int y = 0; y < NT; ++y)
@@ -545,6 +711,7 @@ __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_ker
                         const float scale = OP::kScaled ? __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(source, __builtin_bit_cast(int, scale_here))) : 1.0f;
 #pragma unroll
                         for (int x = 0; x < MT; ++x) v[x][y][i] = made_of<OP>(c[x][y][i], row_scale[x] * scale, bias);
+                        if (OP::kScaled && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // more values on their way at a time would not fit the registers
                     }
             }
 
@@ -580,7 +747,7 @@ __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_ker
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             load(kStage - stage);
             const uint32_t row = i0 + wm * MT * 32 + mine, col = j0 + wn * 64 + piece * kRun;
-            T* to = out + (int64_t)row * p.stride + col;
+            T* to = out + (int64_t)share * p.m * p.n + (int64_t)row * p.stride + col;
             if (i0 + B <= p.m && j0 + kCols <= p.n) {
 #pragma unroll
                 for (int t = 0; t < kStores; ++t) *reinterpret_cast<u32x4_a2*>(to + (int64_t)(t * kRows) * p.stride) = made[t];
@@ -598,30 +765,27 @@ __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_ker
     }
 }
 
-template <typename OP, Made MADE, typename T, int B, int WN>
-hipError_t product_tiles(typename ArgsOf<MADE>::type p, hipStream_t s)
+template <typename OP, Made MADE, Lies LA, Lies LB, typename T, int B, int WN>
+hipError_t product_tiles(typename ArgsOf<MADE, LB>::type p, hipStream_t s)
 {
-    constexpr uint32_t kCols = MADE == Made::linear ? B : B / 2;
-    p.m_tiles = (p.m + B - 1) / B;
-    p.n_tiles = (p.n + kCols - 1) / kCols;
-    const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles, held = B > 128 ? 256 : 512;     // what the card holds at a time
+    const int64_t tiles = tiles_of<MADE>(p, B) * p.parts, held = B > 128 ? 256 : 512;     // what the card holds at a time
     if (tiles * 8 > INT32_MAX) return hipErrorInvalidValue;
     const uint32_t grid = (uint32_t)(tiles < held ? tiles : held);
     p.first = (grid + 7) / 8;
-    return launch(product_tile_kernel<OP, MADE, T, B, WN>, dim3(grid), dim3(2 * WN * 64), s, p);
+    return launch(product_tile_kernel<OP, MADE, LA, LB, T, B, WN>, dim3(grid), dim3(2 * WN * 64), s, p);
 }
 
-template <typename OP, Made MADE, typename T>
-hipError_t product_of(const typename ArgsOf<MADE>::type& p, hipStream_t s)
+template <typename OP, Made MADE, typename T, Lies LA = Lies::rows, Lies LB = Lies::rows>
+hipError_t product_by(ProductTile tile, const typename ArgsOf<MADE, LB>::type& p, hipStream_t s)
 {
-    switch (product_plan(p.m, MADE == Made::linear ? p.n : 2 * (int64_t)p.n, p.chunks, sizeof(T) == 4 && !OP::kScaled)) {
-        case ProductTile::waves32: return product_waves<OP, MADE, T, 1, 1, 4>(p, s);
-        case ProductTile::waves32_wide: return product_waves<OP, MADE, T, 1, 1, 8>(p, s);
-        case ProductTile::waves64: return product_waves<OP, MADE, T, 2, 2, 4>(p, s);
-        case ProductTile::square128: return product_tiles<OP, MADE, T, 128, 2>(p, s);
+    switch (tile) {
+        case ProductTile::waves32: return product_waves<OP, MADE, LA, LB, T, 1, 1, 4>(p, s);
+        case ProductTile::waves32_wide: return product_waves<OP, MADE, LA, LB, T, 1, 1, 8>(p, s);
+        case ProductTile::waves64: return product_waves<OP, MADE, LA, LB, T, 2, 2, 4>(p, s);
+        case ProductTile::square128: return product_tiles<OP, MADE, LA, LB, T, 128, 2>(p, s);
         case ProductTile::square256: break;
     }
-    return product_tiles<OP, MADE, T, 256, 4>(p, s);
+    return product_tiles<OP, MADE, LA, LB, T, 256, 4>(p, s);
 }
 
 }  // namespace fh

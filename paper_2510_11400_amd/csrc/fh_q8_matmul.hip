@@ -7,7 +7,8 @@ namespace {
 template <Made MADE>
 hipError_t q8_product(const ProductArgs& p, int32_t out_dtype, hipStream_t s)
 {
-    return out_dtype == FH_F32 ? product_of<OfQ8, MADE, float>(p, s) : product_of<OfQ8, MADE, Bf16>(p, s);
+    const ProductTile tile = product_tile(p.m, MADE == Made::linear ? p.n : 2 * (int64_t)p.n, p.chunks, false);
+    return out_dtype == FH_F32 ? product_by<OfQ8, MADE, float>(tile, p, s) : product_by<OfQ8, MADE, Bf16>(tile, p, s);
 }
 
 bool q8_product_shape_ok(int64_t m, int64_t n, int64_t k) { return q8_shape_ok(m, k) && q8_shape_ok(n, k) && k <= kQ8MostSummed; }
@@ -17,7 +18,9 @@ ProductArgs q8_args(const void* a, int64_t m, int64_t n, int64_t k, void* out, i
     ProductArgs p = {};
     p.a = static_cast<const uint8_t*>(a);
     p.a_pitch = p.b_pitch = p.b2_pitch = (uint32_t)(q8_chunks(k) * kQ8Chunk);
-    p.chunks = (uint32_t)q8_chunks(k);
+    p.chunks = p.chunks_each = (uint32_t)q8_chunks(k);
+    p.tail = kChunkBytes;
+    p.parts = 1;
     p.m = (uint32_t)m;
     p.n = (uint32_t)n;
     p.out = out;

@@ -58,7 +58,7 @@ def _check_backward(api, dh, x, wg, wu, bg, bu, act, **kind):
 
 # (tokens, features, hidden)
 SHAPES = [(1, 1, 1), (1, 64, 64), (1, 4096, 1000), (2, 100, 30), (5, 515, 77), (16, 768, 2048), (17, 33, 65), (31, 128, 64), (64, 64, 32), (65, 130, 257), (200, 1000, 513),
-          (333, 515, 1001), (256, 256, 128), (1025, 96, 40), (3000, 64, 300), (2048, 768, 1024)]
+          (333, 515, 1001), (256, 256, 128), (1025, 96, 40), (3000, 64, 300), (2048, 768, 1024), (4096, 520, 1300), (8200, 48, 40), (40, 2000, 1500)]
 
 
 @pytest.mark.parametrize("act", ACTIVATIONS)
@@ -116,6 +116,22 @@ def test_strided_and_unaligned_operands(api, dtype, rows):
         _check_gated(api, *parts, *biases, "silu", out=out[:, 3:3 + f])
         assert bool((out[:, :3] == 7.0).all()) and bool((out[:, 3 + f:] == 7.0).all())
         _check_backward(api, view(dh, rows, f, at, extra), *parts, *biases, "gelu")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("t, k, f, extra", [(2048, 128, 1024, 8), (2100, 200, 1100, 24), (4200, 72, 1000, 40), (1500, 1000, 300, 16), (1030, 24, 2000, 4)])
+def test_strided_operands_of_large_products(api, t, k, f, dtype, extra):
+    """Rows at multiples of 16 bytes that are none of 128, whole chunks and parts of them."""
+    x, wg, wu, bg, bu, dh = _inputs(t, k, f, DTYPES[dtype])
+
+    def view(m, extra):
+        whole = torch.full((m.shape[0], m.shape[1] + extra), float("nan"), device="cuda", dtype=m.dtype)
+        whole[:, :m.shape[1]] = m
+        return whole[:, :m.shape[1]]
+
+    parts = [view(x, extra), view(wg, 2 * extra), view(wu, 0)]
+    _check_gated(api, *parts, bg, bu, "silu")
+    _check_backward(api, view(dh, 3), *parts, bg, bu, "silu")
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
