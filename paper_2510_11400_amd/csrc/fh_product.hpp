@@ -22,6 +22,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 // The operands' types: lane (r = lane % 32, h = lane / 32) gets the outputs [8 (i/4) + 4 h + i % 4][r], the first index the first operand's row.
 struct OfQ8 {
     static constexpr uint32_t kSize = 1;
+    static constexpr int kSteps = 1;                            // matrix instructions of a product of 16 bytes a lane
     typedef i32x16 Sums;                                         // whole numbers: exact in any order
     typedef int Sum;
     static constexpr bool kScaled = true;
@@ -32,6 +33,7 @@ struct OfQ8 {
 };
 struct OfBf16 {
     static constexpr uint32_t kSize = 2;
+    static constexpr int kSteps = 1;                            // matrix instructions of a product of 16 bytes a lane
     typedef f32x16 Sums;
     typedef float Sum;
     static constexpr bool kScaled = false;
@@ -42,6 +44,7 @@ struct OfBf16 {
 };
 struct OfF32 {
     static constexpr uint32_t kSize = 4;
+    static constexpr int kSteps = 4;                            // matrix instructions of a product of 16 bytes a lane
     typedef f32x16 Sums;
     typedef float Sum;
     static constexpr bool kScaled = false;
@@ -120,6 +123,7 @@ __device__ __forceinline__ u32x4 in_scalars(u32x4 b)
 // of 64 bytes (a transposing read gives a lane four rows of its column), of fp32 one row for each half of the wave.
 template <typename OP, int COLS>
 struct ByColumns {
+    static constexpr int kReads = OP::kSize == 2 ? 2 : 4;        // instructions of a read
     static constexpr uint32_t kRow = COLS * OP::kSize, kPieces = kRow / 16, kRows = kChunkBytes / OP::kSize;   // bytes, pieces of a row; rows of a chunk
     static __device__ __forceinline__ uint32_t turn(uint32_t k)
     {
@@ -149,11 +153,11 @@ struct ByColumns {
             return v;
         }
     }
-    // The buffer of chunk `chunk` from column `col` on, of `rows` x `cols`, whose last 16 bytes are whole: what is past the rows is read as zeros, past
-    // the columns as zeros or another row's.
-    static __device__ __forceinline__ u32x4 buffer(const uint8_t* p, uint32_t pitch, uint32_t chunk, uint32_t rows, uint32_t col, uint32_t cols)
+    // The buffer of rows `row` to `end`, of which `rows` exist, from column `col` of `cols` on, whose last 16 bytes are whole: what is past the rows is
+    // read as zeros, past the columns as zeros or another row's.
+    static __device__ __forceinline__ u32x4 buffer(const uint8_t* p, uint32_t pitch, uint32_t row, uint32_t end, uint32_t rows, uint32_t col, uint32_t cols)
     {
-        const uint32_t row = chunk * kRows, left = row >= rows ? 0u : rows - row < kRows ? rows - row : kRows;
+        const uint32_t last = end < rows ? end : rows, left = row >= last ? 0u : last - row;
         return in_scalars(buffer_of(p + (int64_t)row * pitch + (int64_t)col * OP::kSize, left ? (left - 1) * pitch + ((cols - col) * OP::kSize + 15) / 16 * 16 : 0u));
     }
 };
@@ -224,7 +228,7 @@ __global__ __launch_bounds__(WAVES * 64) void product_waves_kernel(typename Args
             for (int t = 0; t < MT * 4; ++t)
                 to_lds(lds + t * 1024, from_a, cut && (piece ^ (t & 1) * 64) >= p.tail ? kNowhere : at_a[t], chunk * kChunkBytes);
         } else {
-            from_a = ColumnsA::buffer(p.a, p.a_pitch, chunk, p.summed, i0, p.m);
+            from_a = ColumnsA::buffer(p.a, p.a_pitch, chunk * ColumnsA::kRows, (chunk + 1) * ColumnsA::kRows, p.summed, i0, p.m);
 #pragma unroll
             for (int t = 0; t < MT * 4; ++t) to_lds(lds + t * 1024, from_a, at_a[t], 0);
         }
@@ -236,7 +240,8 @@ __global__ __launch_bounds__(WAVES * 64) void product_waves_kernel(typename Args
         } else {
             const bool second = chunk >= p.split;
             const uint32_t pitch = second ? p.b2_pitch : p.b_pitch;
-            from_b = ColumnsB::buffer(second ? p.b2 : p.b, pitch, second ? chunk - p.split : chunk, p.summed, j0, p.n);
+            const uint32_t row = (second ? chunk - p.split : chunk) * ColumnsB::kRows;
+            from_b = ColumnsB::buffer(second ? p.b2 : p.b, pitch, row, row + ColumnsB::kRows, p.summed, j0, p.n);
 #pragma unroll
             for (int t = 0; t < NT * 4; ++t)
                 to_lds(lds + kRowsA * kChunkBytes + t * 1024, from_b, ColumnsB::row_of(t * 1024 + lane * 16) * pitch + ColumnsB::byte_of(t * 1024 + lane * 16), 0);
@@ -385,25 +390,27 @@ hipError_t product_waves(typename ArgsOf<MADE, LB>::type p, hipStream_t s)
     });
 }
 
-// A wave's pairs of sums, (32 MT) rows x 32 columns of each, to what is made of them.  Sixteen rows at a time go through 4 KiB of LDS, so that a lane
-// has four neighbouring columns of both: the formulas, which are long, stand here once for eight passes, and what a row brings (its scale,
-// dh) is read by 64 bytes a pass ahead.
+// A wave's (32 MT) x 64 sums to what is made of them.  Sixteen rows at a time go through 4 KiB of LDS, so that a lane has eight of a row: of a linear product
+// neighbours, of a pair four of the gate and the same four of up.  The formulas, which are long, stand here once for eight passes, and what a
+// row brings (its scale, dh) is read a pass ahead.
 template <typename OP, Made MADE, typename T, int MT, int NT, typename Args>
-__device__ __forceinline__ void pair_epilogue(const Args& p, const typename OP::Sums (&c)[MT][NT], uint8_t* s_area, uint32_t i0, uint32_t j0, int lane)
+__device__ __forceinline__ void tile_epilogue(const Args& p, T* out, const typename OP::Sums (&c)[MT][NT], uint8_t* s_area, uint32_t i0, uint32_t j0, int lane)
 {
+    constexpr bool kPair = MADE != Made::linear;
     typedef typename OP::Sum Sum;
     typedef Sum Sum4 __attribute__((ext_vector_type(4)));
     const int row16 = lane & 15, upper = lane >> 4 & 1, half = lane >> 5, piece = lane & 7, mine = lane >> 3;
-    const uint32_t col = j0 + piece * 4;
+    const uint32_t col = j0 + piece * (kPair ? 4 : 8);           // and of the second four
+    const uint32_t col2 = kPair ? col : col + 4;
     const int64_t left = (int64_t)p.n - col;
     float bias[2][4], scales[2][4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const uint32_t inside = col + e < p.n ? col + e : p.n - 1;
+        const uint32_t inside = col + e < p.n ? col + e : p.n - 1, inside2 = col2 + e < p.n ? col2 + e : p.n - 1;
         bias[0][e] = parameter(p.bias, p.bias_dtype, inside, 0.0f);
-        bias[1][e] = parameter(p.bias2, p.bias_dtype, inside, 0.0f);
+        bias[1][e] = parameter(kPair ? p.bias2 : p.bias, p.bias_dtype, inside2, 0.0f);
         scales[0][e] = scale_of<OP>(p.b, p.n, p.b_pitch, p.chunks, inside);
-        scales[1][e] = scale_of<OP>(p.b2, p.n, p.b2_pitch, p.chunks, inside);
+        scales[1][e] = scale_of<OP>(kPair ? p.b2 : p.b, p.n, kPair ? p.b2_pitch : p.b_pitch, p.chunks, inside2);
     }
     struct OfRow { float scale; f32x4 dh; };
     const auto of_row = [&](int row, OfRow& r) {
@@ -439,7 +446,7 @@ __device__ __forceinline__ void pair_epilogue(const Args& p, const typename OP::
             const int row = t * 8 + mine;
             now[t] = next[t];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) sum[t][u] = *reinterpret_cast<const Sum4*>(s_area + row * 256 + ((u * 8 + piece) ^ row) * 16);
+            for (int u = 0; u < 2; ++u) sum[t][u] = *reinterpret_cast<const Sum4*>(s_area + row * 256 + ((kPair ? u * 8 + piece : piece * 2 + u) ^ row) * 16);
         }
         asm volatile("" ::: "memory");
         if (pass + 1 < 2 * MT) {
@@ -452,21 +459,27 @@ __device__ __forceinline__ void pair_epilogue(const Args& p, const typename OP::
             float v[4], w[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float gate = made_of<OP>(sum[t][0][e], now[t].scale * scales[0][e], bias[0][e]);
-                const float up = made_of<OP>(sum[t][1][e], now[t].scale * scales[1][e], bias[1][e]);
-                if constexpr (MADE == Made::gated) {
-                    v[e] = activated(gate, p.act) * up;
+                const float first = made_of<OP>(sum[t][0][e], now[t].scale * scales[0][e], bias[0][e]);
+                const float second = made_of<OP>(sum[t][1][e], now[t].scale * scales[1][e], bias[1][e]);
+                if constexpr (MADE == Made::linear) {
+                    v[e] = first;
+                    w[e] = second;
+                } else if constexpr (MADE == Made::gated) {
+                    v[e] = activated(first, p.act) * second;
                 } else {
-                    const Activated a = activated_both(gate, p.act);
+                    const Activated a = activated_both(first, p.act);
                     const bool inside = i < p.m && e < left;     // the others' sums are of no rows
-                    v[e] = inside ? now[t].dh[e] * up * a.slope : 0.0f;
+                    v[e] = inside ? now[t].dh[e] * second * a.slope : 0.0f;
                     w[e] = inside ? now[t].dh[e] * a.value : 0.0f;
                     sums[0][e] += v[e];
                     sums[1][e] += w[e];
                 }
             }
-            T* to = static_cast<T*>(p.out) + (int64_t)i * p.stride + col;
-            if constexpr (MADE == Made::gated) {
+            T* to = out + (int64_t)i * p.stride + col;
+            if constexpr (MADE == Made::linear) {
+                const float both[8] = {v[0], v[1], v[2], v[3], w[0], w[1], w[2], w[3]};
+                store8(to, i < p.m ? left : 0, both);
+            } else if constexpr (MADE == Made::gated) {
                 store4(to, i < p.m ? left : 0, v);
             } else {
                 const int64_t most = i < p.m ? p.up_at - col : 0;
@@ -502,22 +515,19 @@ __device__ __forceinline__ void pair_epilogue(const Args& p, const typename OP::
 // is multiplied the next is on its way, and a stage is handed over before its last quarter, which is in registers by then, so that the matrix
 // unit works across the barrier.  A row's eight pieces of 16 bytes are turned by half the row's number (the loads take them from turned
 // addresses), so that sixteen lanes reading the same piece of sixteen rows meet all 64 banks.
-// The chunks of the next tile follow those of the last without a gap.  A wave's outputs are turned into rows in the part of the free stage that
-// the wave itself loads, so it needs no barrier before it loads there again; that load is sent before the outputs are, because
-// memory operations are counted in their order and the next wait is for the load alone.
+// The chunks of the next tile follow those of the last without a gap: a tile's outputs go through LDS of their own, and since memory
+// operations are counted in their order and the loads are sent before the outputs are, the next wait is for the loads alone.
 // Of a pair's 64 columns of a wave the first 32 are the gate's and the others the same columns of up, so that both sums of an output are one wave's.
-// Its outputs go through LDS of their own, so that the next load is sent before all of them.
 template <typename OP, Made MADE, Lies LA, Lies LB, typename T, int B, int WN>
 __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_kernel(typename ArgsOf<MADE, LB>::type p)
 {
     constexpr bool kPair = MADE != Made::linear;
     constexpr int kWaves = 2 * WN, kHalf = kWaves / 2, MT = B / 64, NT = 2, kCols = kPair ? B / 2 : B;
     constexpr uint32_t kStage = 2 * B * kChunkBytes;
-    constexpr int kRun = 16 / sizeof(T), kLanes = 64 / kRun, kRows = 64 / kLanes;
-    constexpr int kStores = kPair ? MT * 4 * (MADE == Made::gated ? 1 : 2) : MT * 32 / kRows;
+    constexpr int kStores = MT * 4 * (MADE == Made::gated_backward || (MADE == Made::linear && sizeof(T) == 4) ? 2 : 1);   // of a whole tile, a wave's
     typedef ByColumns<OP, B> Columns;
     static_assert(kHalf * 64 == B && WN * 64 == B, "a wave loads an 8 KiB of one operand, and has 64 columns");
-    __shared__ __attribute__((aligned(16))) uint8_t s_stage[2 * kStage + (kPair ? kWaves * 4096 : 0)];
+    __shared__ __attribute__((aligned(16))) uint8_t s_stage[2 * kStage + kWaves * 4096];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
 
@@ -537,7 +547,6 @@ __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_ker
     const uint32_t width = (p.chunks - 1) * kChunkBytes + p.tail;
     uint32_t next_tile = run_of(blockIdx.x, tiles), next_chunk = 0, next_end = 0, next_corner = 0;
     u32x4 from = {}, from2 = {};
-    const uint32_t piece_at = ((lane & 7) ^ (lane >> 4)) * 16;
     const auto aim = [&]() {
         uint32_t i0, j0;
         corner(next_tile, i0, j0);
@@ -563,54 +572,62 @@ __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_ker
         }
     };
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_stage;
-    const auto load_rows = [&](uint32_t to) {
-        const uint32_t pitch = of_b ? p.b_pitch : p.a_pitch, pitch2 = kPair && of_b ? p.b2_pitch : pitch;
+    // Straight code, whichever way the wave's operand lies: four loads from each of two buffers, neighbours `step` bytes apart, every other one
+    // with its pieces turned another way.  Where no tile is left the buffers are empty.
+    struct Load { u32x4 from[2]; uint32_t at[2][2], step[2], moved, to; };
+    const auto next_load = [&](uint32_t stage) {
+        Load n = {};
+        n.to = lds + stage + wave * 8192;
         uint32_t l = lane;
         asm("" : "+v"(l));                                       // offsets made here, not registers kept
-        uint32_t even = piece_at, odd = piece_at ^ 64;
-        constexpr uint32_t kNowhere = 1u << 31;                  // past the end of any buffer here: zeros
-        if (next_chunk + 1 == p.chunks && p.tail < kChunkBytes) {
-            if (even >= p.tail) even = kNowhere;
-            if (odd >= p.tail) odd = kNowhere;
-        }
-        const uint32_t at = (l >> 3) * pitch, at2 = (l >> 3) * pitch2;
+        if constexpr (LA == Lies::rows || LB == Lies::rows) {
+            constexpr uint32_t kNowhere = 1u << 31;              // past the end of any buffer here: zeros
+            const uint32_t limit = next_chunk + 1 == p.chunks ? p.tail : kChunkBytes, piece = ((l & 7) ^ (l >> 4)) * 16;
+            const uint32_t pitch[2] = {LB == Lies::rows && of_b ? p.b_pitch : p.a_pitch, kPair && of_b ? p.b2_pitch : LB == Lies::rows && of_b ? p.b_pitch : p.a_pitch};
+            n.from[0] = from;
+            n.from[1] = from2;
 #pragma unroll
-        for (int t = 0; t < 8; ++t)
-            to_lds(to + t * 1024, t < 4 ? from : from2, (t & 1 ? odd : even) + (t < 4 ? at : at2) + t % 4 * 8 * (t < 4 ? pitch : pitch2), next_chunk * kChunkBytes);
-    };
-    const auto load_columns = [&](uint32_t to) {
-        const uint8_t* base = p.a;
-        uint32_t pitch = p.a_pitch, chunk = next_chunk, summed = 0;
-        if constexpr (LB == Lies::columns) {
-            summed = p.summed;
-            if (of_b) {
-                const bool second = chunk >= p.split;
-                base = second ? p.b2 : p.b;
-                pitch = second ? p.b2_pitch : p.b_pitch;
-                chunk = second ? chunk - p.split : chunk;
+            for (int u = 0; u < 2; ++u) {
+                n.at[u][0] = (piece < limit ? piece : kNowhere) + (l >> 3) * pitch[u];
+                n.at[u][1] = ((piece ^ 64) < limit ? piece ^ 64 : kNowhere) + (l >> 3) * pitch[u];
+                n.step[u] = 8 * pitch[u];
             }
+            n.moved = next_chunk * kChunkBytes;
         }
-        const u32x4 here = Columns::buffer(base, pitch, chunk, summed, next_corner, of_b ? p.n : p.m);
-        uint32_t at = part * 8192 + lane * 16;
-        asm("" : "+v"(at));
+        if constexpr (LB == Lies::columns) {
+            const bool second = of_b && next_chunk >= p.split, here = LA == Lies::columns || of_b;
+            const uint8_t* base = of_b ? second ? p.b2 : p.b : p.a;
+            const uint32_t pitch = of_b ? second ? p.b2_pitch : p.b_pitch : p.a_pitch, chunk = second ? next_chunk - p.split : next_chunk;
+            const uint32_t summed = next_tile < end_tile ? p.summed : 0u, all = of_b ? p.n : p.m;
 #pragma unroll
-        for (int t = 0; t < 8; ++t) to_lds(to + t * 1024, here, Columns::row_of(at + t * 1024) * pitch + Columns::byte_of(at + t * 1024), 0);
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t place = part * 8192 + u * 4096;
+                const u32x4 buffer = Columns::buffer(base, pitch, chunk * Columns::kRows + Columns::row_of(place), (chunk + 1) * Columns::kRows, summed, next_corner, all);
+                const uint32_t even = Columns::row_of(l * 16) * pitch + Columns::byte_of(place + l * 16);
+                const uint32_t odd = Columns::row_of(l * 16) * pitch + Columns::byte_of(place + 1024 + l * 16);
+                n.from[u] = here ? buffer : n.from[u];
+                n.at[u][0] = here ? even : n.at[u][0];
+                n.at[u][1] = here ? odd : n.at[u][1];
+                n.step[u] = here ? Columns::row_of(1024) * pitch : n.step[u];
+            }
+            n.moved = here ? 0u : n.moved;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) n.from[u] = in_scalars(n.from[u]);
+        return n;
+    };
+    const auto load_piece = [&](const Load& n, int t) { to_lds(n.to + t * 1024, n.from[t / 4], n.at[t / 4][t & 1] + t % 4 * n.step[t / 4], n.moved); };
+    const auto loaded = [&]() {
+        if (++next_chunk != next_end) return;
+        next_tile += p.first;
+        if (next_tile < end_tile) aim();
+        else from = from2 = u32x4{from.x, from.y, 0, from.w};
     };
     const auto load = [&](uint32_t stage) {
-        if (next_tile >= end_tile) return;
-        const uint32_t to = lds + stage + wave * 8192;
-        if constexpr (LA == LB) {
-            if constexpr (LA == Lies::rows) load_rows(to);
-            else load_columns(to);
-        } else if (of_b) {
-            load_columns(to);
-        } else {
-            load_rows(to);
-        }
-        if (++next_chunk == next_end) {
-            next_tile += p.first;
-            if (next_tile < end_tile) aim();
-        }
+        const Load n = next_load(stage);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) load_piece(n, t);
+        loaded();
     };
 
     const int h = lane >> 5, r = lane & 31, turned = (h * 4) ^ (lane >> 1 & 7);
@@ -631,138 +648,75 @@ __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_ker
     };
     typename OP::Sums c[MT][NT];
     // Sums run along b's rows within a lane.
+    const auto product = [&](int which, int number) {
+        const int x = number / NT, y = number % NT;
+        c[x][y] = OP::multiply(fb[which][y], fa[which][x], c[x][y]);
+    };
+    // A quarter's products while the next quarter is read, a read or two to a matrix instruction: left to itself the compiler sends the reads late and waits.
+    constexpr int kReads = MT * (LA == Lies::rows ? 1 : Columns::kReads) + NT * (LB == Lies::rows ? 1 : Columns::kReads), kSteps = MT * NT * OP::kSteps;
     const auto multiply = [&](int which) {
 #pragma unroll
-        for (int x = 0; x < MT; ++x)
+        for (int number = 0; number < MT * NT; ++number) product(which, number);
 #pragma unroll
-            for (int y = 0; y < NT; ++y) c[x][y] = OP::multiply(fb[which][y], fa[which][x], c[x][y]);
+        for (int step = 0; step < kSteps; ++step) {
+            if ((step + 1) * kReads / kSteps > step * kReads / kSteps) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            if ((step + 1) * kReads / kSteps > step * kReads / kSteps + 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
     };
     uint32_t tile = next_tile, stage = 0;
     bool behind = false;                                         // outputs were sent after the load that is waited for
     if (tile >= end_tile) return;
     aim();
     load(0);
-    if (next_tile < end_tile) {
-        load(kStage);
-        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");         // the first stage's are older
-    } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    load(kStage);
+    asm volatile("s_waitcnt vmcnt(8)" ::: "memory");             // the first stage's are older
     __syncthreads();
-    if constexpr (!kPair) read(stage, 0, 0);
-    [[maybe_unused]] T* out = static_cast<T*>(p.out);
 #pragma clang loop unroll(disable)
     for (; tile < end_tile; tile += p.first) {
         uint32_t i0, j0;
         corner(tile, i0, j0);
         const uint32_t share = share_of(tile), begin = share * p.chunks_each, end = end_of(share);
-        float bias_here = 0.0f, scale_here = 0.0f;               // of the wave's column `lane`
 #pragma unroll
         for (int x = 0; x < MT; ++x)
 #pragma unroll
             for (int y = 0; y < NT; ++y) c[x][y] = typename OP::Sums{};
-        if constexpr (kPair) read(stage, 0, 0);
+        read(stage, 0, 0);
 #pragma clang loop unroll(disable)
         for (uint32_t k = begin; k < end; ++k) {
-            if (!kPair && k + 1 == end) {
-                const uint32_t col = j0 + wn * 64 + lane, inside = col < p.n ? col : p.n - 1;
-                if (p.bias) bias_here = parameter(p.bias, p.bias_dtype, inside, 0.0f);
-                scale_here = scale_of<OP>(p.b, p.n, p.b_pitch, p.chunks, inside);
-            }
+            __builtin_amdgcn_sched_barrier(0);
             read(stage, 1, 1);
             multiply(0);
+            __builtin_amdgcn_sched_barrier(0);
             read(stage, 2, 0);
             multiply(1);
+            __builtin_amdgcn_sched_barrier(0);
             read(stage, 3, 1);
             multiply(0);
+            __builtin_amdgcn_sched_barrier(0);
             // this wave has read all of this stage, and its part of the next has arrived
             if (behind) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(kStores) : "memory");
             else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             behind = false;
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            if (k + 1 < end) load(stage);
+            const Load n = next_load(stage);
             stage = kStage - stage;
-            // after the last chunk the next tile's; a pair's epilogue needs the registers and reads them behind it
-            if (!kPair || k + 1 < end) read(stage, 0, 0);
-            multiply(1);
+            read(stage, 0, 0);                                   // after the last chunk the next tile's: read again behind the epilogue, which needs the registers
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                load_piece(n, t);
+#pragma unroll
+                for (int number = t * MT * NT / 8; number < (t + 1) * MT * NT / 8; ++number) product(1, number);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            loaded();
         }
-        if constexpr (kPair) {
-            load(kStage - stage);
-            pair_epilogue<OP, MADE, T, MT, NT>(p, c, s_stage + 2 * kStage + wave * 4096, i0 + wm * MT * 32, j0 + wn * 32, lane);
-            behind = i0 + B <= p.m && j0 + kCols <= p.n;
-        } else {
-            int l = lane;
-            asm("" : "+v"(l));                                       // what is worked out from it is not kept in registers meanwhile
-            const int mine = l / kLanes, piece = l % kLanes, row32 = l & 31, half = l >> 5;
-            // the sums as values, in place
-            f32x16 v[MT][NT];
-            {
-                float row_scale[MT];
-#pragma unroll
-                for (int x = 0; x < MT; ++x) {
-                    const uint32_t row = i0 + (wm * MT + x) * 32 + row32;
-                    row_scale[x] = OP::kScaled ? scale_of<OP>(p.a, p.m, p.a_pitch, p.chunks, row < p.m ? row : p.m - 1) : 1.0f;
-                }
-#pragma unroll
-                for (int y = 0; y < NT; ++y)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int source = (y * 32 + i / 4 * 8 + half * 4 + i % 4) * 4;
-                        const float bias = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(source, __builtin_bit_cast(int, bias_here)));
-                        const float scale = OP::kScaled ? __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(source, __builtin_bit_cast(int, scale_here))) : 1.0f;
-#pragma unroll
-                        for (int x = 0; x < MT; ++x) v[x][y][i] = made_of<OP>(c[x][y][i], row_scale[x] * scale, bias);
-                        if (OP::kScaled && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // more values on their way at a time would not fit the registers
-                    }
-            }
-
-            // 32 rows at a time through this wave's 8 KiB of the stage that is free, to runs of 16 bytes a lane
-            constexpr int kPieces = 64 * (int)sizeof(T) / 16;        // of a row
-            const auto turn_of = [](int row) { return kPieces == 16 ? row & 15 : row >> 1 & 7; };
-            uint8_t* s_out = s_stage + (kStage - stage) + wave * 8192;
-            u32x4 made[kStores];
-#pragma unroll
-            for (int x = 0; x < MT; ++x) {
-#pragma unroll
-                for (int y = 0; y < NT; ++y)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const f32x16& o = v[x][y];
-                        if constexpr (sizeof(T) == 2) {              // the upper sixteen rows have the halves of a piece exchanged
-                            const uint32_t at_piece = (uint32_t)((y * 4 + i) ^ turn_of(row32)) * 16 + (uint32_t)(half ^ row32 >> 4) * 8;
-                            *reinterpret_cast<u32x2*>(s_out + row32 * (kPieces * 16) + at_piece) = u32x2{bf16_pair(o[4 * i], o[4 * i + 1]), bf16_pair(o[4 * i + 2], o[4 * i + 3])};
-                        } else {
-                            const uint32_t at_piece = (uint32_t)((y * 8 + 2 * i + half) ^ turn_of(row32)) * 16;
-                            *reinterpret_cast<f32x4*>(s_out + row32 * (kPieces * 16) + at_piece) = f32x4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]};
-                        }
-                    }
-                asm volatile("" ::: "memory");                       // a wave's own LDS accesses are in order
-#pragma unroll
-                for (int t = 0; t < 32 / kRows; ++t) {
-                    const int from_row = t * kRows + mine;
-                    const u32x4 w = *reinterpret_cast<const u32x4*>(s_out + from_row * (kPieces * 16) + (piece ^ turn_of(from_row)) * 16);
-                    made[x * (32 / kRows) + t] = sizeof(T) == 2 && t * kRows >= 16 ? u32x4{w.z, w.w, w.x, w.y} : w;
-                }
-                asm volatile("" ::: "memory");
-            }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            load(kStage - stage);
-            const uint32_t row = i0 + wm * MT * 32 + mine, col = j0 + wn * 64 + piece * kRun;
-            T* to = out + (int64_t)share * p.m * p.n + (int64_t)row * p.stride + col;
-            if (i0 + B <= p.m && j0 + kCols <= p.n) {
-#pragma unroll
-                for (int t = 0; t < kStores; ++t) *reinterpret_cast<u32x4_a2*>(to + (int64_t)(t * kRows) * p.stride) = made[t];
-                behind = true;
-            } else {
-                const int rows = p.m <= row ? 0 : p.m - row < B ? (int)(p.m - row) : B, cols = p.n <= col ? 0 : p.n - col < kRun ? (int)(p.n - col) : kRun;
-#pragma unroll
-                for (int t = 0; t < kStores; ++t) {
-                    int some = t * kRows < rows ? cols : 0;
-                    asm("" : "+v"(some));                            // its masks are not kept in registers either
-                    store_packed(to + (int64_t)(t * kRows) * p.stride, some, made[t]);
-                }
-            }
-        }
+        tile_epilogue<OP, MADE, T, MT, NT>(p, static_cast<T*>(p.out) + (int64_t)share * p.m * p.n, c, s_stage + 2 * kStage + wave * 4096, i0 + wm * MT * 32, j0 + wn * (kPair ? 32 : 64),
+                                           lane);
+        behind = i0 + B <= p.m && j0 + kCols <= p.n;
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // the empty loads behind the last tile go to LDS too, which is another workgroup's next
 }
 
 template <typename OP, Made MADE, Lies LA, Lies LB, typename T, int B, int WN>
