@@ -79,7 +79,7 @@ Forward forward_rows(const fh_gated_layer& l)
 {
     return {{l.x, l.tokens, l.features, l.x_stride}, {l.w_gate, l.hidden, l.features, l.w_gate_stride}, {l.w_up, l.hidden, l.features, l.w_up_stride}};
 }
-size_t forward_bytes(const fh_gated_layer& l)
+size_t forward_bytes(const fh_gated_layer& l)                    // of the products that want their operands laid out
 {
     const Forward f = forward_rows(l);
     return packed_bytes(f.x, l.dtype) + packed_bytes(f.gate, l.dtype) + packed_bytes(f.up, l.dtype);
@@ -116,6 +116,24 @@ void set_summed(ProductArgs& p, int64_t values)
     p.parts = 1;
 }
 
+template <typename T>
+void set_layer(const fh_gated_layer& l, ProductArgs& p)
+{
+    set_summed<T>(p, l.features);
+    p.m = (uint32_t)l.tokens;
+    p.n = (uint32_t)l.hidden;
+    p.bias = l.b_gate;
+    p.bias2 = l.b_up;
+    p.bias_dtype = (int16_t)l.dtype;
+    p.act = (int16_t)l.activation;
+}
+// Whether a few tokens' forward product takes its operands as they lie, at any alignment; its arguments hold strides in 32 bits.
+bool forward_as_it_lies(const fh_gated_layer& l)
+{
+    const int64_t most = ((int64_t)1 << 32) / (int64_t)dtype_size(l.dtype);
+    return few_rows_dense(l.tokens, l.dtype == FH_F32, forward_bytes(l) > 0) && l.x_stride < most && l.w_gate_stride < most && l.w_up_stride < most;
+}
+
 // The operands of the forward product.
 template <typename T>
 hipError_t forward_operands(const fh_gated_layer& l, ProductArgs& p, Space& space, hipStream_t s)
@@ -135,13 +153,7 @@ hipError_t forward_operands(const fh_gated_layer& l, ProductArgs& p, Space& spac
     hipError_t e = take(f.x, p.a, p.a_pitch);
     if (e == hipSuccess) e = take(f.gate, p.b, p.b_pitch);
     if (e == hipSuccess) e = take(f.up, p.b2, p.b2_pitch);
-    set_summed<T>(p, l.features);
-    p.m = (uint32_t)l.tokens;
-    p.n = (uint32_t)l.hidden;
-    p.bias = l.b_gate;
-    p.bias2 = l.b_up;
-    p.bias_dtype = (int16_t)l.dtype;
-    p.act = (int16_t)l.activation;
+    set_layer<T>(l, p);
     return e;
 }
 
@@ -150,10 +162,23 @@ hipError_t forward_of(const fh_gated_layer& l, hipStream_t s)
 {
     ProductArgs p = {};
     Space space = {static_cast<uint8_t*>(l.workspace)};
-    const hipError_t e = forward_operands<T>(l, p, space, s);
-    if (e != hipSuccess) return e;
     p.out = l.h;
     p.stride = l.h_stride;
+    if (forward_as_it_lies(l)) {
+        const Forward f = forward_rows(l);
+        const auto pitch = [](const Rows& r) { return r.rows <= 1 ? 0u : (uint32_t)(r.stride * (int64_t)sizeof(T)); };
+        p.a = static_cast<const uint8_t*>(f.x.p);
+        p.b = static_cast<const uint8_t*>(f.gate.p);
+        p.b2 = static_cast<const uint8_t*>(f.up.p);
+        p.a_pitch = pitch(f.x);
+        p.b_pitch = pitch(f.gate);
+        p.b2_pitch = pitch(f.up);
+        set_layer<T>(l, p);
+        p.tail = (uint32_t)(l.features * (int64_t)sizeof(T) - (int64_t)(p.chunks - 1) * kChunkBytes);
+        return product_rows<typename OpOf<T>::type, Made::gated, T>(p, s);
+    }
+    const hipError_t e = forward_operands<T>(l, p, space, s);
+    if (e != hipSuccess) return e;
     return product_by<typename OpOf<T>::type, Made::gated, T>(pair_tile(l), p, s);
 }
 
@@ -315,7 +340,7 @@ size_t fh_gated_workspace_bytes(const fh_gated_layer* l, int32_t backward)
 {
     using namespace fh;
     if (check(l) != FH_OK || l->tokens == 0) return 0;
-    return backward ? backward_of(*l).bytes() : forward_bytes(*l);
+    return backward ? backward_of(*l).bytes() : forward_as_it_lies(*l) ? 0 : forward_bytes(*l);
 }
 
 fh_status fh_gated(const fh_gated_layer* l, void* stream)
@@ -329,7 +354,7 @@ fh_status fh_gated(const fh_gated_layer* l, void* stream)
     if (!l->h) return FH_ERR_NULL;
     if (!is_aligned(l->h, dtype_size(l->dtype))) return FH_ERR_ALIGNMENT;
     if (l->h_cap < strided_elements(l->tokens, l->hidden, l->h_stride) * dtype_size(l->dtype)) return FH_ERR_BUFFER_TOO_SMALL;
-    if ((status = check_workspace(*l, forward_bytes(*l))) != FH_OK) return status;
+    if ((status = check_workspace(*l, forward_as_it_lies(*l) ? 0 : forward_bytes(*l))) != FH_OK) return status;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     return (l->dtype == FH_F32 ? forward_of<float>(*l, s) : forward_of<Bf16>(*l, s)) == hipSuccess ? FH_OK : FH_ERR_LAUNCH;
 }

@@ -729,6 +729,149 @@ hipError_t product_tiles(typename ArgsOf<MADE, LB>::type p, hipStream_t s)
     return launch(product_tile_kernel<OP, MADE, LA, LB, T, B, WN>, dim3(grid), dim3(2 * WN * 64), s, p);
 }
 
+// ---- few rows: what counts is how fast the rows of B come ----------------------------------------
+// Up to 16 rows x 16 columns (of a pair both) a workgroup; its waves take 256 bytes of every row in turn, straight from memory to the registers that the
+// 16 x 16 matrix instructions want: lane (r = lane % 16, g = lane / 16) brings 16 bytes of row r, every fourth piece.  The waves' sums are joined in LDS in
+// the waves' order.  Rows may lie at any alignment of their elements: `tail` is exact here.  A pair of 8192 x 4096 in 8 bits comes at 5.2 TB/s, the launch left
+// out; workgroups of 4 and of 16 waves were slower (14.8 us; 17.4 and 17.9).
+template <typename OP> struct Sums16;
+template <> struct Sums16<OfQ8> {
+    typedef i32x4 Sums;
+    static __device__ __forceinline__ Sums multiply(u32x4 a, u32x4 b, Sums c)
+    {
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+    }
+};
+template <> struct Sums16<OfBf16> {
+    typedef f32x4 Sums;
+    static __device__ __forceinline__ Sums multiply(u32x4 a, u32x4 b, Sums c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Sums16<OfF32> {
+    typedef f32x4 Sums;
+    static __device__ __forceinline__ Sums multiply(u32x4 a, u32x4 b, Sums c)
+    {
+        const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], c, 0, 0, 0);
+        return c;
+    }
+};
+// The bytes from `at` on of a row of `width`, zeros behind its end.
+template <typename OP>
+__device__ __forceinline__ u32x4 end_of_row(const uint8_t* row, uint32_t at, uint32_t width)
+{
+    u32x4 v = {};
+    if (at + 16 <= width) return *reinterpret_cast<const u32x4_a2*>(row + at);
+    if constexpr (OP::kSize == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) if (at + 4 * i < width) v[i] = *reinterpret_cast<const uint32_t*>(row + at + 4 * i);
+    } else {                                                     // rows of bytes are whole pieces
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (at + 2 * i < width) v[i / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(row + at + 2 * i) << (16 * (i & 1));
+    }
+    return v;
+}
+template <typename OP, Made MADE, typename T, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void product_rows_kernel(ProductArgs p)
+{
+    constexpr bool kPair = MADE != Made::linear;
+    constexpr int kBoth = kPair ? 2 : 1, kThreads = WAVES * 64, kValues = 256;
+    typedef typename OP::Sum Sum;
+    typedef typename Sums16<OP>::Sums Sums;
+    __shared__ __attribute__((aligned(16))) Sum s_sums[WAVES][kBoth][16][20];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const uint32_t j0 = (p.first + blockIdx.x) * 16, width = p.chunks ? (p.chunks - 1) * kChunkBytes + p.tail : 0u;
+    // rows past the last are the last one
+    const int64_t row = j0 + r < p.n ? j0 + r : p.n - 1;
+    const uint8_t* b[kBoth];
+    b[0] = p.b + row * p.b_pitch + g * 16;
+    if constexpr (kPair) b[1] = p.b2 + row * p.b2_pitch + g * 16;
+    const uint8_t* a = p.a + (int64_t)((uint32_t)r < p.m ? r : p.m - 1) * p.a_pitch + g * 16;
+    // what a thread's output takes beside the sums, on its way meanwhile
+    static_assert(kThreads >= kValues, "an output a thread");
+    const uint32_t out_row = threadIdx.x / 16, out_col = threadIdx.x % 16, i = out_row, j = j0 + out_col;
+    const bool mine = threadIdx.x < kValues && i < p.m && j < p.n;
+    float bias[kBoth], scales[kBoth];
+    if (mine) {
+        const float scale = scale_of<OP>(p.a, p.m, p.a_pitch, p.chunks, i);
+        bias[0] = parameter(p.bias, p.bias_dtype, j, 0.0f);
+        scales[0] = scale_of<OP>(p.b, p.n, p.b_pitch, p.chunks, j) * scale;
+        if constexpr (kPair) {
+            bias[1] = parameter(p.bias2, p.bias_dtype, j, 0.0f);
+            scales[1] = scale_of<OP>(p.b2, p.n, p.b2_pitch, p.chunks, j) * scale;
+        }
+    }
+    Sums c[kBoth] = {};
+    struct Pieces { u32x4 a[4], b[4][kBoth]; };
+    const auto load = [&](uint32_t k, Pieces& q) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int y = 0; y < kBoth; ++y) q.b[t][y] = *reinterpret_cast<const u32x4_a2*>(b[y] + k + t * 64);
+            q.a[t] = *reinterpret_cast<const u32x4_a2*>(a + k + t * 64);
+        }
+    };
+    const auto multiply = [&](const Pieces& q) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int y = 0; y < kBoth; ++y) c[y] = Sums16<OP>::multiply(q.b[t][y], q.a[t], c[y]);
+    };
+    uint32_t k = wave * 256;
+    constexpr uint32_t kStep = WAVES * 256;
+    if (k + 256 <= width) {
+        Pieces now;
+        load(k, now);
+        k += kStep;
+        while (k + 256 <= width) {                               // the next pieces are sent for before these are multiplied
+            Pieces next;
+            load(k, next);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(now);
+            now = next;
+            k += kStep;
+        }
+        multiply(now);
+    }
+    if (k < width) {
+#pragma clang loop unroll(disable)
+        for (uint32_t t = 0; t < 4; ++t) {
+            const uint32_t at = k + t * 64 + g * 16;
+            const u32x4 fa = end_of_row<OP>(a - g * 16, at, width);
+#pragma unroll
+            for (int y = 0; y < kBoth; ++y) c[y] = Sums16<OP>::multiply(end_of_row<OP>(b[y] - g * 16, at, width), fa, c[y]);
+        }
+    }
+    // a lane has columns 4 g .. of row r
+#pragma unroll
+    for (int y = 0; y < kBoth; ++y) *reinterpret_cast<Sums*>(&s_sums[wave][y][r][g * 4]) = c[y];
+    __syncthreads();
+    if (!mine) return;
+    float v[kBoth];
+#pragma unroll
+    for (int y = 0; y < kBoth; ++y) {
+        Sum sum = s_sums[0][y][out_row][out_col];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) sum += s_sums[w][y][out_row][out_col];
+        v[y] = made_of<OP>(sum, scales[y], bias[y]);
+    }
+    if constexpr (kPair) v[0] = activated(v[0], p.act) * v[1];
+    store1(static_cast<T*>(p.out) + (int64_t)i * p.stride + j, v[0]);
+}
+template <typename OP, Made MADE, typename T>
+hipError_t product_rows(ProductArgs p, hipStream_t s)
+{
+    constexpr int kWaves = 8;
+    if (p.m > kMostFewRows) return hipErrorInvalidValue;
+    return in_parts(((int64_t)p.n + 15) / 16, kWaves * 64, [&](int64_t first, int64_t count) {
+        p.first = (uint32_t)first;
+        return launch(product_rows_kernel<OP, MADE, T, kWaves>, dim3((uint32_t)count), dim3(kWaves * 64), s, p);
+    });
+}
+
 template <typename OP, Made MADE, typename T, Lies LA = Lies::rows, Lies LB = Lies::rows>
 hipError_t product_by(ProductTile tile, const typename ArgsOf<MADE, LB>::type& p, hipStream_t s)
 {

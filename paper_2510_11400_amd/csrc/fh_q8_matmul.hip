@@ -7,6 +7,7 @@ namespace {
 template <Made MADE>
 hipError_t q8_product(const ProductArgs& p, int32_t out_dtype, hipStream_t s)
 {
+    if (few_rows_of_bytes(p.m, MADE != Made::linear)) return out_dtype == FH_F32 ? product_rows<OfQ8, MADE, float>(p, s) : product_rows<OfQ8, MADE, Bf16>(p, s);
     const ProductTile tile = product_tile(p.m, MADE == Made::linear ? p.n : 2 * (int64_t)p.n, p.chunks, false);
     return out_dtype == FH_F32 ? product_by<OfQ8, MADE, float>(tile, p, s) : product_by<OfQ8, MADE, Bf16>(tile, p, s);
 }

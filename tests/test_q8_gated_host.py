@@ -100,7 +100,7 @@ def test_q8_gated_refusals():
 
 
 def _layer(**change):
-    a = api.fh_gated_layer(5, 40, 7, 0, 0, 3, 0, FAKE, 41, FAKE, 40, FAKE, 40, FAKE, FAKE, FAKE, 7, BIG, FAKE, 7, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, BIG)
+    a = api.fh_gated_layer(50, 40, 7, 0, 0, 3, 0, FAKE, 41, FAKE, 40, FAKE, 40, FAKE, FAKE, FAKE, 7, BIG, FAKE, 7, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, BIG)
     for name, v in change.items():                               # rows of x at no multiple of 16 bytes: they are packed
         setattr(a, name, v)
     return a
@@ -129,11 +129,11 @@ def test_gated_refusals(backward):
     need = LIB.fh_gated_workspace_bytes(ctypes.byref(_layer()), backward)
     assert need > 0 and status(workspace_cap=need - 1) == 7
     if not backward:                                             # rows as the kernels want them: nothing is laid out again
-        assert LIB.fh_gated_workspace_bytes(ctypes.byref(_layer(x_stride=40)), 0) == 0
+        assert LIB.fh_gated_workspace_bytes(ctypes.byref(_layer(x_stride=40)), 0) == 0 == LIB.fh_gated_workspace_bytes(ctypes.byref(_layer(tokens=5)), 0)
     if backward:
         assert status(needs=0, db_gate=None, db_up=None, dh=None, workspace=None) == 0
     else:
-        assert status(h_cap=5 * 7 * 4 - 1) == 7 and status(tokens=0, x=None, h=None, workspace=None) == 0
+        assert status(h_cap=50 * 7 * 4 - 1) == 7 and status(tokens=0, x=None, h=None, workspace=None) == 0
 
 
 def test_the_workspace_covers_what_the_backward_call_lays_out():
