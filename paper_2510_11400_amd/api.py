@@ -1498,6 +1498,10 @@ class MxLayer:
 
 
 # ---- 8-bit integer storage, its products, the gated projection ----------------------------------------------
+FH_SILU, FH_GELU, FH_GELU_TANH = 0, 1, 2
+FH_GATED_NEEDS_INPUT, FH_GATED_NEEDS_WEIGHT = 1, 2
+
+
 def q8_scales_offset(rows: int, cols: int) -> int:
     """Where the scales begin in a stored matrix."""
     return (cols + 127) // 128 * 128 * rows if 0 <= rows <= _MOST and 0 <= cols <= _MOST else 0

@@ -675,7 +675,7 @@ struct Linear : torch::autograd::Function<Linear> {
 // Forward-mode derivatives: a tangent that went no further would be read as a derivative of zero.
 void no_tangent(const at::Tensor& t, const char* what)
 {
-    if (t.defined() && t._fw_grad(/*level=*/0).defined()) raise(PyExc_NotImplementedError, "%s carries a tangent; the microscaled layers have no forward-mode derivative", what);
+    if (t.defined() && t._fw_grad(/*level=*/0).defined()) raise(PyExc_NotImplementedError, "%s carries a tangent; these layers have no forward-mode derivative", what);
 }
 
 // (tensors): refused where one carries a tangent
@@ -729,7 +729,7 @@ struct Biases {
     at::Tensor gate, up;
     void *g, *u;
     int dtype;
-    Biases(PyObject* go, PyObject* uo, int64_t n, c10::Device device) : gate(tensor_or_none(go, "b_gate")), up(tensor_or_none(uo, "b_up"))
+    Biases(at::Tensor g_, at::Tensor u_, int64_t n, c10::Device device) : gate(std::move(g_)), up(std::move(u_))
     {
         if (gate.defined() && up.defined() && gate.scalar_type() != up.scalar_type())
             raise(PyExc_TypeError, "b_gate and b_up have different dtypes (%s, %s)", c10::toString(gate.scalar_type()), c10::toString(up.scalar_type()));
@@ -803,7 +803,7 @@ FH_ENTRY(q8_gated, 10)
     if (x.cols != gate.cols) raise(PyExc_ValueError, "x has %lld features, the weights take %lld", (long long)x.cols, (long long)gate.cols);
     on_device(gate.data, device, "w_gate");
     on_device(up.data, device, "w_up");
-    const Biases bias(a[3], a[4], gate.rows, device);
+    const Biases bias(tensor_or_none(a[3], "b_gate"), tensor_or_none(a[4], "b_up"), gate.rows, device);
     const int activation = activation_of(a[5]);
     const On on(a[9], device);
     const Matrix out = result(a[7], x.rows, gate.rows, scalar_type(a[6]), device, on, "out");
@@ -834,61 +834,147 @@ fh_gated_layer gated_layer(const Matrix& x, const Matrix& gate, const Matrix& up
     return l;
 }
 
+at::Tensor gated_forward_of(const Matrix& x, const Matrix& gate, const Matrix& up, const Biases& bias, int activation, PyObject* given, PyObject* workspace, const On& on)
+{
+    fh_gated_layer l = gated_layer(x, gate, up, bias, activation);
+    const Matrix out = given ? result(given, x.rows, gate.rows, x.t.scalar_type(), x.device(), on, "out") : new_matrix(x.rows, gate.rows, x.t.scalar_type(), x.device());
+    if (out.dtype != x.dtype) raise(PyExc_TypeError, "out must have the dtype of x");
+    l.h = out.data(); l.h_stride = out.stride; l.h_cap = out.bytes();
+    const Work w = work(workspace, fh_gated_workspace_bytes(&l, 0), x.device());
+    l.workspace = w.p; l.workspace_cap = w.n;
+    enqueue(x.device(), [&](void* stream) { return fh_gated(&l, stream); });
+    return out.t;
+}
+
+struct GatedGradients { at::Tensor dx, dw_gate, dw_up, db_gate, db_up; };
+// What gradients are wanted of.
+struct GatedNeeds { bool input, weight, b_gate, b_up; };
+GatedGradients gated_backward_of(const Matrix& dh, const Matrix& x, const Matrix& gate, const Matrix& up, const Biases& bias, int activation, const GatedNeeds& needs,
+                                 PyObject* workspace)
+{
+    const c10::Device device = x.device();
+    fh_gated_layer l = gated_layer(x, gate, up, bias, activation);
+    if (dh.rows != x.rows || dh.cols != gate.rows || dh.dtype != x.dtype) raise(PyExc_ValueError, "dh must have the shape and the dtype of the result");
+    on_device(dh.t, device, "dh");
+    const at::ScalarType type = x.t.scalar_type();
+    l.needs = (needs.input ? FH_GATED_NEEDS_INPUT : 0) | (needs.weight ? FH_GATED_NEEDS_WEIGHT : 0);
+    l.dh = dh.data(); l.dh_stride = dh.stride;
+    GatedGradients g;
+    if (needs.input) {
+        g.dx = new_matrix(x.rows, x.cols, type, device).t;
+        l.dx = g.dx.data_ptr();
+    }
+    if (needs.weight) {                                          // one behind the other: one product for both
+        Pair p = pair(gate.rows * gate.cols, type, device);
+        g.dw_gate = p.first.view({gate.rows, gate.cols});
+        g.dw_up = p.second.view({gate.rows, gate.cols});
+        l.dw_gate = p.first.data_ptr();
+        l.dw_up = p.second.data_ptr();
+    }
+    if (needs.b_gate && bias.g) {
+        g.db_gate = values(gate.rows, type, device);
+        l.db_gate = g.db_gate.data_ptr();
+    }
+    if (needs.b_up && bias.u) {
+        g.db_up = values(gate.rows, type, device);
+        l.db_up = g.db_up.data_ptr();
+    }
+    const Work w = work(workspace, fh_gated_workspace_bytes(&l, 1), device);
+    l.workspace = w.p; l.workspace_cap = w.n;
+    enqueue(device, [&](void* stream) { return fh_gated_backward(&l, stream); });
+    return g;
+}
+
 // (x, w_gate, w_up, b_gate, b_up, activation, out, workspace, stream)
 FH_ENTRY(gated, 9)
     const Matrix x = matrix(a[0], "x"), gate = matrix(a[1], "w_gate"), up = matrix(a[2], "w_up");
-    const c10::Device device = x.device();
-    const Biases bias(a[3], a[4], gate.rows, device);
-    fh_gated_layer l = gated_layer(x, gate, up, bias, activation_of(a[5]));
-    const On on(a[8], device);
-    const Matrix out = result(a[6], x.rows, gate.rows, x.t.scalar_type(), device, on, "out");
-    if (out.dtype != x.dtype) raise(PyExc_TypeError, "out must have the dtype of x");
-    l.h = out.data(); l.h_stride = out.stride; l.h_cap = out.bytes();
-    const Work w = work(a[7], fh_gated_workspace_bytes(&l, 0), device);
-    l.workspace = w.p; l.workspace_cap = w.n;
-    enqueue(device, [&](void* stream) { return fh_gated(&l, stream); });
-    return wrap(out.t);
+    const Biases bias(tensor_or_none(a[3], "b_gate"), tensor_or_none(a[4], "b_up"), gate.rows, x.device());
+    const int activation = activation_of(a[5]);
+    const On on(a[8], x.device());
+    return wrap(gated_forward_of(x, gate, up, bias, activation, a[6], a[7], on));
 FH_EXIT
 
 // (dh, x, w_gate, w_up, b_gate, b_up, activation, needs_input, needs_weight, needs_bias, workspace, stream)
 //  -> (dx, dw_gate, dw_up, db_gate, db_up)
 FH_ENTRY(gated_backward, 12)
     const Matrix dh = matrix(a[0], "dh"), x = matrix(a[1], "x"), gate = matrix(a[2], "w_gate"), up = matrix(a[3], "w_up");
-    const c10::Device device = x.device();
-    const Biases bias(a[4], a[5], gate.rows, device);
-    fh_gated_layer l = gated_layer(x, gate, up, bias, activation_of(a[6]));
-    if (dh.rows != x.rows || dh.cols != gate.rows || dh.dtype != x.dtype) raise(PyExc_ValueError, "dh must have the shape and the dtype of the result");
-    on_device(dh.t, device, "dh");
-    const bool input = truth(a[7]), weight = truth(a[8]), biases = truth(a[9]);
-    const On on(a[11], device);
-    const at::ScalarType type = x.t.scalar_type();
-    l.needs = (input ? FH_GATED_NEEDS_INPUT : 0) | (weight ? FH_GATED_NEEDS_WEIGHT : 0);
-    l.dh = dh.data(); l.dh_stride = dh.stride;
-    at::Tensor dx, dw_gate, dw_up, db_gate, db_up;
-    if (input) {
-        dx = new_matrix(x.rows, x.cols, type, device).t;
-        l.dx = dx.data_ptr();
+    const Biases bias(tensor_or_none(a[4], "b_gate"), tensor_or_none(a[5], "b_up"), gate.rows, x.device());
+    const int activation = activation_of(a[6]);
+    const GatedNeeds needs = {truth(a[7]), truth(a[8]), truth(a[9]), truth(a[9])};
+    const On on(a[11], x.device());
+    const GatedGradients g = gated_backward_of(dh, x, gate, up, bias, activation, needs, a[10]);
+    for (const at::Tensor* t : {&g.dx, &g.dw_gate, &g.db_gate, &g.db_up}) on.lent(*t);
+    return tuple(Ref(wrap(g.dx)), Ref(wrap(g.dw_gate)), Ref(wrap(g.dw_up)), Ref(wrap(g.db_gate)), Ref(wrap(g.db_up)));
+FH_EXIT
+
+// ---- the same as a step of autograd: what is saved is x and the parameters -----------------------
+struct GatedPass : torch::CustomClassHolder {
+    int activation;
+    bool x, gate, up, b_gate, b_up;                                       // whose gradients are wanted
+    std::vector<int64_t> shape;                                           // of x
+};
+
+struct Gated : torch::autograd::Function<Gated> {
+    using Context = torch::autograd::AutogradContext;
+    static at::Tensor forward(Context* ctx, const at::Tensor& x, const at::Tensor& w_gate, const at::Tensor& w_up, const std::optional<at::Tensor>& b_gate,
+                              const std::optional<at::Tensor>& b_up, const c10::intrusive_ptr<GatedPass>& pass)
+    {
+        const at::Tensor m = rows_of(x);
+        const Matrix rows = matrix(m, "x"), gate = matrix(w_gate, "w_gate"), up = matrix(w_up, "w_up");
+        const Biases bias(b_gate.value_or(at::Tensor()), b_up.value_or(at::Tensor()), gate.rows, rows.device());
+        const On on(Py_None, rows.device());
+        const at::Tensor h = gated_forward_of(rows, gate, up, bias, pass->activation, nullptr, Py_None, on);
+        ctx->save_for_backward({m, w_gate, w_up, b_gate.value_or(at::Tensor()), b_up.value_or(at::Tensor())});
+        ctx->saved_data.emplace("pass", c10::IValue::make_capsule(pass));
+        return shaped(h, x);
     }
-    if (weight) {                                                // one behind the other: one product for both
-        Pair p = pair(gate.rows * gate.cols, type, device);
-        dw_gate = p.first.view({gate.rows, gate.cols});
-        dw_up = p.second.view({gate.rows, gate.cols});
-        l.dw_gate = p.first.data_ptr();
-        l.dw_up = p.second.data_ptr();
+    static torch::autograd::variable_list backward(Context* ctx, const torch::autograd::variable_list& given)
+    {
+        const auto pass = c10::static_intrusive_pointer_cast<GatedPass>(ctx->saved_data.at("pass").toCapsule());
+        const bool again = at::GradMode::is_enabled() && given[0].requires_grad();
+        torch::autograd::variable_list grads(6);
+        {
+            const at::AutoGradMode off(false);
+            const at::Tensor dh = rows_of(given[0]);
+            const auto saved = ctx->get_saved_variables();
+            const Matrix x = matrix(saved[0], "x"), gate = matrix(saved[1], "w_gate"), up = matrix(saved[2], "w_up");
+            const Biases bias(saved[3], saved[4], gate.rows, x.device());
+            const GatedGradients g = gated_backward_of(matrix(dh, "dh"), x, gate, up, bias, pass->activation,
+                                                       {pass->x, pass->gate || pass->up, pass->b_gate, pass->b_up}, Py_None);
+            if (pass->x) grads[0] = g.dx.view(pass->shape);
+            if (pass->gate) grads[1] = g.dw_gate;
+            if (pass->up) grads[2] = g.dw_up;
+            grads[3] = g.db_gate;
+            grads[4] = g.db_up;
+        }
+        if (!again) return grads;
+        for (at::Tensor& g : grads)                                       // leaves of a graph that ends in an error
+            if (g.defined()) g = g.detach().set_requires_grad(true);
+        return torch::autograd::DelayedError("a gated projection is differentiated once", (int64_t)grads.size()).apply(std::move(grads));
     }
-    if (biases && bias.g) {
-        db_gate = values(gate.rows, type, device);
-        l.db_gate = db_gate.data_ptr();
+};
+
+// (x, w_gate, w_up, b_gate, b_up, activation) -> h
+FH_ENTRY(gated_linear, 6)
+    const at::Tensor x = tensor(a[0], "x"), w_gate = tensor(a[1], "w_gate"), w_up = tensor(a[2], "w_up"), b_gate = tensor_or_none(a[3], "b_gate"),
+                     b_up = tensor_or_none(a[4], "b_up");
+    no_tangent(x, "x"); no_tangent(w_gate, "w_gate"); no_tangent(w_up, "w_up"); no_tangent(b_gate, "b_gate"); no_tangent(b_up, "b_up");
+    in_device_memory(x, "x");
+    if (x.dim() == 0) raise(PyExc_ValueError, "x must have a dimension");
+    const auto pass = c10::make_intrusive<GatedPass>();
+    const bool grad = at::GradMode::is_enabled();
+    const auto wanted = [&](const at::Tensor& t) { return grad && t.defined() && t.requires_grad(); };
+    pass->activation = activation_of(a[5]);
+    pass->x = wanted(x); pass->gate = wanted(w_gate); pass->up = wanted(w_up); pass->b_gate = wanted(b_gate); pass->b_up = wanted(b_up);
+    pass->shape = x.sizes().vec();
+    if (pass->x || pass->gate || pass->up || pass->b_gate || pass->b_up) {
+        const auto some = [](const at::Tensor& t) { return t.defined() ? std::optional<at::Tensor>(t) : std::nullopt; };
+        return wrap(Gated::apply(x, w_gate, w_up, some(b_gate), some(b_up), pass));
     }
-    if (biases && bias.u) {
-        db_up = values(gate.rows, type, device);
-        l.db_up = db_up.data_ptr();
-    }
-    for (const at::Tensor* t : {&dx, &dw_gate, &db_gate, &db_up}) on.lent(*t);
-    const Work w = work(a[10], fh_gated_workspace_bytes(&l, 1), device);
-    l.workspace = w.p; l.workspace_cap = w.n;
-    enqueue(device, [&](void* stream) { return fh_gated_backward(&l, stream); });
-    return tuple(Ref(wrap(dx)), Ref(wrap(dw_gate)), Ref(wrap(dw_up)), Ref(wrap(db_gate)), Ref(wrap(db_up)));
+    const Matrix m = matrix(rows_of(x), "x"), gate = matrix(w_gate, "w_gate"), up = matrix(w_up, "w_up");
+    const Biases bias(b_gate, b_up, gate.rows, m.device());
+    const On on(Py_None, m.device());
+    return wrap(shaped(gated_forward_of(m, gate, up, bias, pass->activation, nullptr, Py_None, on), x));
 FH_EXIT
 
 // (FedHybridError, MxMatrix, Q8Matrix): the classes that results and errors are of.
@@ -903,6 +989,7 @@ FH_EXIT
 PyMethodDef g_methods[] = {FH_METHOD(mx_quantize), FH_METHOD(mx_dequantize), FH_METHOD(mx_matmul), FH_METHOD(layer_norm), FH_METHOD(layer_norm_mx),
                            FH_METHOD(layer_norm_backward), FH_METHOD(layer_forward), FH_METHOD(layer_backward), FH_METHOD(mx_linear), FH_METHOD(refuse_tangents),
                            FH_METHOD(q8_quantize), FH_METHOD(q8_dequantize), FH_METHOD(q8_matmul), FH_METHOD(q8_gated), FH_METHOD(gated), FH_METHOD(gated_backward),
+                           FH_METHOD(gated_linear),
                            FH_METHOD(use), {}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_fh_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -21,16 +21,27 @@ int64_t padded_bytes(int64_t cols, int32_t dtype) { return (cols * (int64_t)dtyp
 size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // ---- operands as the products want them ----------------------------------------------------------
-// Rows of any alignment and length to rows of whole chunks, zeros behind their ends.  Sixteen bytes a thread.
+// Rows of any alignment and length to rows of whole chunks, zeros behind their ends: up to three matrices of as many columns, a workgroup a row, sixteen
+// bytes a thread.  (A launch for each took 333 x 515 -> 1001 in fp32, a step, 8 us longer.)
+struct PackArgs {
+    const void* x[3];
+    uint8_t*    out[3];
+    int64_t     stride[3];
+    uint32_t    end[3];                // workgroups of the matrices up to this one
+    uint32_t    cols, pitch, first;
+};
 template <typename T>
-__global__ __launch_bounds__(256) void pack_kernel(const T* x, uint32_t cols, int64_t stride, uint8_t* out, uint32_t pitch, uint32_t rows, uint32_t first)
+__global__ __launch_bounds__(256) void pack_kernel(PackArgs p)
 {
     constexpr int kRun = 16 / sizeof(T);
-    const uint32_t pieces = pitch / 16, row = first + blockIdx.x;
-    for (uint32_t i = threadIdx.x; i < pieces; i += 256) {
+    const uint32_t number = p.first + blockIdx.x, which = (number >= p.end[0]) + (number >= p.end[1]);
+    const uint32_t row = number - (which == 0 ? 0u : which == 1 ? p.end[0] : p.end[1]);
+    const T* x = static_cast<const T*>(which == 0 ? p.x[0] : which == 1 ? p.x[1] : p.x[2]) + (int64_t)row * (which == 0 ? p.stride[0] : which == 1 ? p.stride[1] : p.stride[2]);
+    uint8_t* out = (which == 0 ? p.out[0] : which == 1 ? p.out[1] : p.out[2]) + (int64_t)row * p.pitch;
+    for (uint32_t i = threadIdx.x; i < p.pitch / 16; i += 256) {
         Run<T, kRun> v;
-        v.load(x + (int64_t)row * stride + (int64_t)i * kRun, (int64_t)cols - (int64_t)i * kRun);
-        *reinterpret_cast<u32x4*>(out + (int64_t)row * pitch + i * 16) = u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
+        v.load(x + (int64_t)i * kRun, (int64_t)p.cols - (int64_t)i * kRun);
+        *reinterpret_cast<u32x4*>(out + i * 16) = u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
     }
 }
 template <typename T>
@@ -56,15 +67,6 @@ __global__ __launch_bounds__(256) void join_weights_kernel(const float* parts, u
     store4((second ? up : gate) + (int64_t)row * cols + col, (int64_t)cols - col, v);
 }
 
-template <typename T>
-hipError_t pack(const void* x, int64_t rows, int64_t cols, int64_t stride, void* out, hipStream_t s)
-{
-    const uint32_t pitch = (uint32_t)padded_bytes(cols, sizeof(T) == 4 ? FH_F32 : FH_BF16);
-    return in_parts(rows, 256, [&](int64_t first, int64_t count) {
-        return launch(pack_kernel<T>, dim3((uint32_t)count), dim3(256), s, static_cast<const T*>(x), (uint32_t)cols, stride, static_cast<uint8_t*>(out), pitch,
-                      (uint32_t)rows, (uint32_t)first);
-    });
-}
 // A matrix as an operand: as it lies, or packed.  As it lies where every row, and its end, is at a multiple of 16 bytes.
 struct Rows { const void* p; int64_t rows, cols, stride; };
 bool lies_well(const Rows& r, int32_t dtype)
@@ -139,20 +141,33 @@ template <typename T>
 hipError_t forward_operands(const fh_gated_layer& l, ProductArgs& p, Space& space, hipStream_t s)
 {
     const Forward f = forward_rows(l);
-    const auto take = [&](const Rows& r, const uint8_t*& at, uint32_t& pitch) -> hipError_t {
+    PackArgs q = {};
+    q.cols = (uint32_t)l.features;
+    q.pitch = (uint32_t)padded_bytes(l.features, l.dtype);
+    int count = 0;
+    uint32_t all = 0;
+    const auto take = [&](const Rows& r, const uint8_t*& at, uint32_t& pitch) {
         if (lies_well(r, l.dtype)) {
             at = static_cast<const uint8_t*>(r.p);
             pitch = r.rows <= 1 ? 0u : (uint32_t)(r.stride * (int64_t)sizeof(T));
-            return hipSuccess;
+            return;
         }
         uint8_t* to = space.take(packed_bytes(r, l.dtype));
         at = to;
-        pitch = (uint32_t)padded_bytes(r.cols, l.dtype);
-        return pack<T>(r.p, r.rows, r.cols, r.stride, to, s);
+        pitch = q.pitch;
+        q.x[count] = r.p;
+        q.out[count] = to;
+        q.stride[count] = r.stride;
+        all += (uint32_t)r.rows;
+        for (int i = count++; i < 3; ++i) q.end[i] = all;
     };
-    hipError_t e = take(f.x, p.a, p.a_pitch);
-    if (e == hipSuccess) e = take(f.gate, p.b, p.b_pitch);
-    if (e == hipSuccess) e = take(f.up, p.b2, p.b2_pitch);
+    take(f.x, p.a, p.a_pitch);
+    take(f.gate, p.b, p.b_pitch);
+    take(f.up, p.b2, p.b2_pitch);
+    const hipError_t e = in_parts(all, 256, [&](int64_t first, int64_t some) {
+        q.first = (uint32_t)first;
+        return launch(pack_kernel<T>, dim3((uint32_t)some), dim3(256), s, q);
+    });
     set_layer<T>(l, p);
     return e;
 }
@@ -261,6 +276,7 @@ hipError_t backward_of(const fh_gated_layer& l, hipStream_t s)
         q.b2_pitch = p.b2_pitch;
         q.summed = (uint32_t)l.hidden;
         q.split = q.chunks / 2;
+        q.gap_from = (uint32_t)l.tokens;
         q.m = (uint32_t)l.tokens;
         q.n = (uint32_t)l.features;
         q.out = l.dx;
@@ -279,7 +295,7 @@ hipError_t backward_of(const fh_gated_layer& l, hipStream_t s)
         q.n = (uint32_t)l.features;
         q.stride = l.features;
         if (b.weights.parts > 1) {
-            q.m = (uint32_t)(b.hidden_padded + l.hidden);
+            q.m = q.gap_from = (uint32_t)(b.hidden_padded + l.hidden);
             q.parts = b.weights.parts;
             q.chunks_each = b.weights.chunks_each;
             q.out = parts;
@@ -292,9 +308,11 @@ hipError_t backward_of(const fh_gated_layer& l, hipStream_t s)
             if (e == hipSuccess) e = join((2 * l.hidden * runs + 255) / 256);
             return e;
         }
-        // both weights' gradients at once where they lie one behind the other
-        const bool one = b.hidden_padded == l.hidden && static_cast<T*>(l.dw_up) == static_cast<T*>(l.dw_gate) + l.hidden * l.features;
-        q.m = (uint32_t)(one ? 2 * l.hidden : l.hidden);
+        // both weights' gradients at once where they lie one behind the other: what D has between its halves is left out
+        const bool one = static_cast<T*>(l.dw_up) == static_cast<T*>(l.dw_gate) + l.hidden * l.features;
+        q.m = (uint32_t)(one ? b.hidden_padded + l.hidden : l.hidden);
+        q.gap_from = (uint32_t)l.hidden;
+        q.gap = one ? (uint32_t)(b.hidden_padded - l.hidden) : 0u;
         q.out = l.dw_gate;
         const ProductTile tile = product_tile(q.m, q.n, q.chunks, sizeof(T) == 4);
         e = product_by<Op, Made::linear, T, Lies::columns, Lies::columns>(tile, q, s);

@@ -85,10 +85,27 @@ struct BackwardArgs : ProductArgs {    // out: the gate's gradients, and `up_at`
     int64_t        up_at;
     float*         sums;               // [m_tiles][2][n] sums of the columns over the tile's rows, or null
 };
+struct TurnedArgs;
+template <typename Args> struct has_gap { static constexpr bool value = false; };
+template <> struct has_gap<TurnedArgs> { static constexpr bool value = true; };
 struct TurnedArgs : ProductArgs {      // products with an operand that lies by columns: its rows are the summed dimension
     uint32_t       summed;             // rows of a and b where they lie so
     uint32_t       split;              // chunks that b has; b2 goes on behind them
+    uint32_t       gap_from, gap;      // so many rows of out from there on are left out, those behind them move up
 };
+// The row of out that row i's outputs go to; false where they go nowhere.
+template <typename Args>
+__device__ __forceinline__ bool out_row(const Args& p, uint32_t i, uint32_t& to)
+{
+    to = i;
+    if constexpr (has_gap<Args>::value) {
+        if (i >= p.gap_from) {
+            to = i - p.gap;
+            return i >= p.gap_from + p.gap && i < p.m;
+        }
+    }
+    return i < p.m;
+}
 // How an operand lies: its rows by the summed dimension, or the summed dimension's rows by it.
 enum class Lies { rows, columns };
 template <Made MADE, Lies B> struct ArgsOf { typedef ProductArgs type; };
@@ -320,7 +337,8 @@ __global__ __launch_bounds__(WAVES * 64) void product_waves_kernel(typename Args
         if constexpr (!kPair) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = made_of<OP>(sum[e], mine * scales[e], bias[e]);
-            store4(static_cast<T*>(p.out) + (int64_t)share * p.m * p.n + (int64_t)i * p.stride + at, left, v);
+            uint32_t to;
+            if (out_row(p, i, to)) store4(static_cast<T*>(p.out) + (int64_t)share * p.m * p.n + (int64_t)to * p.stride + at, left, v);
         } else {
             const Sum4 sum2 = sum_at(row, kCols + col);
             float gate[4], up[4];
@@ -475,14 +493,16 @@ __device__ __forceinline__ void tile_epilogue(const Args& p, T* out, const typen
                     sums[1][e] += w[e];
                 }
             }
-            T* to = out + (int64_t)i * p.stride + col;
+            uint32_t row;
+            const bool some = out_row(p, i, row);
+            T* to = out + (int64_t)row * p.stride + col;
             if constexpr (MADE == Made::linear) {
                 const float both[8] = {v[0], v[1], v[2], v[3], w[0], w[1], w[2], w[3]};
-                store8(to, i < p.m ? left : 0, both);
+                store8(to, some ? left : 0, both);
             } else if constexpr (MADE == Made::gated) {
-                store4(to, i < p.m ? left : 0, v);
+                store4(to, some ? left : 0, v);
             } else {
-                const int64_t most = i < p.m ? p.up_at - col : 0;
+                const int64_t most = some ? p.up_at - col : 0;
                 store4(to, most, v);
                 store4(to + p.up_at, most, w);
             }
@@ -715,6 +735,7 @@ __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_ker
         tile_epilogue<OP, MADE, T, MT, NT>(p, static_cast<T*>(p.out) + (int64_t)share * p.m * p.n, c, s_stage + 2 * kStage + wave * 4096, i0 + wm * MT * 32, j0 + wn * (kPair ? 32 : 64),
                                            lane);
         behind = i0 + B <= p.m && j0 + kCols <= p.n;
+        if constexpr (has_gap<typename ArgsOf<MADE, LB>::type>::value) behind = behind && !p.gap;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // the empty loads behind the last tile go to LDS too, which is another workgroup's next
 }

@@ -43,7 +43,8 @@ inline ProductPlan product_plan(int64_t m, int64_t n, int64_t chunks, bool slow,
     ProductPlan best = {ProductTile::waves32, 1, (uint32_t)chunks};
     int64_t least = 0;
     if (chunks == 0) return best;
-    for (const ProductTile t : {ProductTile::waves32, ProductTile::waves32_wide, ProductTile::waves64, ProductTile::square128, ProductTile::square256}) {
+    for (int32_t i = 0; i <= (int32_t)ProductTile::square256; ++i) {
+        const ProductTile t = (ProductTile)i;
         const int64_t side = product_side(t), tiles = ((m + side - 1) / side) * ((n + side - 1) / side);
         // A shared sum's parts, eight chunks of it at least, are written and read once more by a kernel of their own.
         for (int64_t parts = 1; parts == 1 || (shared && parts <= 16 && chunks / parts >= 8 && tiles * (parts - 1) < 512); ++parts) {

@@ -76,35 +76,11 @@ def layer_norm_mx_linear(x: torch.Tensor, norm_weight: Optional[torch.Tensor], n
     return _binding.mx_linear(x, norm_weight, norm_bias, weight, bias, eps, rounding, seed, tensor_id)
 
 
-class _Gated(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, x, w_gate, w_up, b_gate, b_up, activation):
-        m = _rows(x)
-        h = api.fh_gated(m, w_gate, w_up, b_gate, b_up, activation)
-        ctx.activation = activation
-        ctx.save_for_backward(m, w_gate, w_up, b_gate, b_up)
-        return h.view(*x.shape[:-1], h.shape[1])
-
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, dh):
-        m, w_gate, w_up, b_gate, b_up = ctx.saved_tensors
-        x, gate, up, gate_bias, up_bias, _ = ctx.needs_input_grad
-        dx, dw_gate, dw_up, db_gate, db_up = api.fh_gated_backward(_rows(dh), m, w_gate, w_up, b_gate, b_up, ctx.activation, needs_input=x,
-                                                                   needs_weight=gate or up, needs_bias=gate_bias or up_bias)
-        return (dx.view(*dh.shape[:-1], m.shape[1]) if x else None, dw_gate if gate else None, dw_up if up else None,
-                db_gate if gate_bias else None, db_up if up_bias else None, None)
-
-
 def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, b_gate: Optional[torch.Tensor] = None,
                  b_up: Optional[torch.Tensor] = None, activation: str = "silu") -> torch.Tensor:
     """act(x w_gate^T + b_gate) * (x w_up^T + b_up) over the last dimension, differentiable; everything of one dtype.  x is saved as autograd saves
     it (hooks.SavedActivations compresses it), and nothing of the hidden width."""
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, w_gate, w_up, b_gate, b_up)):
-        return _Gated.apply(x, w_gate, w_up, b_gate, b_up, activation)
-    _binding.refuse_tangents(x, w_gate, w_up, b_gate, b_up)
-    with torch.no_grad():
-        return api.fh_gated(_rows(x), w_gate, w_up, b_gate, b_up, activation).view(*x.shape[:-1], w_gate.shape[0])
+    return _binding.gated_linear(x, w_gate, w_up, b_gate, b_up, activation)
 
 
 def q8_linear(x: torch.Tensor, weight: api.Q8Matrix, bias: Optional[torch.Tensor] = None) -> torch.Tensor:

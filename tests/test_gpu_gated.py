@@ -5,6 +5,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 import gated_reference as R  # noqa: E402
+import q8_gated_shapes as S  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -56,14 +57,9 @@ def _check_backward(api, dh, x, wg, wu, bg, bu, act, **kind):
     return got
 
 
-# (tokens, features, hidden)
-SHAPES = [(1, 1, 1), (1, 64, 64), (1, 4096, 1000), (2, 100, 30), (5, 515, 77), (16, 768, 2048), (17, 33, 65), (31, 128, 64), (64, 64, 32), (65, 130, 257), (200, 1000, 513),
-          (333, 515, 1001), (256, 256, 128), (1025, 96, 40), (3000, 64, 300), (2048, 768, 1024), (4096, 520, 1300), (8200, 48, 40), (40, 2000, 1500)]
-
-
 @pytest.mark.parametrize("act", ACTIVATIONS)
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("t, k, f", SHAPES)
+@pytest.mark.parametrize("t, k, f", S.DENSE)
 def test_gated(api, t, k, f, dtype, act):
     x, wg, wu, bg, bu, _ = _inputs(t, k, f, DTYPES[dtype])
     got = _check_gated(api, x, wg, wu, bg, bu, act)
@@ -73,12 +69,44 @@ def test_gated(api, t, k, f, dtype, act):
 
 @pytest.mark.parametrize("act", ACTIVATIONS)
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("t, k, f", SHAPES)
+@pytest.mark.parametrize("t, k, f", S.DENSE)
 def test_backward(api, t, k, f, dtype, act):
     x, wg, wu, bg, bu, dh = _inputs(t, k, f, DTYPES[dtype])
     got = _check_backward(api, dh, x, wg, wu, bg, bu, act)
     again = api.fh_gated_backward(dh, x, wg, wu, bg, bu, act)
     assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+@pytest.mark.parametrize("dtype, t, k, f", S.LARGE)
+def test_large(api, dtype, t, k, f):
+    x, wg, wu, bg, bu, dh = _inputs(t, k, f, DTYPES[dtype])
+    _check_gated(api, x, wg, wu, bg, bu, "gelu")
+    got = _check_backward(api, dh, x, wg, wu, bg, bu, "gelu")
+    again = api.fh_gated_backward(dh, x, wg, wu, bg, bu, "gelu")
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("t, k, f", [(70, 48, 30), (300, 100, 128), (3000, 64, 300)])
+def test_gradients_wherever_the_caller_wants_them(api, dtype, t, k, f):
+    """By the C call the weights' gradients lie apart, in either order, or one behind the other: the same values, and nothing else is written."""
+    import ctypes
+    x, wg, wu, bg, bu, dh = _inputs(t, k, f, DTYPES[dtype])
+    want = api.fh_gated_backward(dh, x, wg, wu, bg, bu, "silu")
+    n = f * k
+    for first, second in ((16, 16 + n), (16, 16 + n + 8), (16 + n + 24, 16)):
+        room = torch.full((2 * n + 64,), 7.0, device="cuda", dtype=x.dtype)
+        l = api.fh_gated_layer(t, k, f, int(dtype == "bf16"), 0, api.FH_GATED_NEEDS_WEIGHT, 0, x.data_ptr(), k, wg.data_ptr(), k, wu.data_ptr(), k, bg.data_ptr(), bu.data_ptr(),
+                               None, f, 0, dh.data_ptr(), f)
+        l.dw_gate, l.dw_up = (room.data_ptr() + at * room.element_size() for at in (first, second))
+        need = api.raw_library().fh_gated_workspace_bytes(ctypes.byref(l), 1)
+        workspace = torch.full((need + 64,), 170, dtype=torch.uint8, device="cuda")
+        l.workspace, l.workspace_cap = workspace.data_ptr(), need
+        assert api.raw_library().fh_gated_backward(ctypes.byref(l), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == 0
+        assert torch.equal(room[first:first + n].view(f, k), want[1]) and torch.equal(room[second:second + n].view(f, k), want[2])
+        room[first:first + n] = 7.0
+        room[second:second + n] = 7.0
+        assert bool((room == 7.0).all()) and bool((workspace[need:] == 170).all())
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -119,7 +147,7 @@ def test_strided_and_unaligned_operands(api, dtype, rows):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("t, k, f, extra", [(2048, 128, 1024, 8), (2100, 200, 1100, 24), (4200, 72, 1000, 40), (1500, 1000, 300, 16), (1030, 24, 2000, 4)])
+@pytest.mark.parametrize("t, k, f, extra", S.STRIDED)
 def test_strided_operands_of_large_products(api, t, k, f, dtype, extra):
     """Rows at multiples of 16 bytes that are none of 128, whole chunks and parts of them."""
     x, wg, wu, bg, bu, dh = _inputs(t, k, f, DTYPES[dtype])

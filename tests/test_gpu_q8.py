@@ -6,6 +6,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 import gated_reference as R  # noqa: E402
+import q8_gated_shapes as S  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -99,12 +100,8 @@ def _pair(api, x):
     return m, (codes, scales)
 
 
-PRODUCTS = [(1, 1, 1), (1, 16, 128), (1, 4096, 4096), (3, 1000, 8192), (5, 100, 40), (16, 2000, 1500), (17, 33, 129), (31, 64, 4096), (64, 64, 64), (65, 130, 257),
-            (197, 1000, 1537), (256, 256, 256), (300, 513, 4100), (1000, 768, 2048), (513, 2049, 640), (8192, 24, 100), (4100, 1030, 96), (2048, 2304, 768)]
-
-
 @pytest.mark.parametrize("out", ["f32", "bf16"])
-@pytest.mark.parametrize("m, n, k", PRODUCTS)
+@pytest.mark.parametrize("m, n, k", S.PRODUCTS)
 def test_products(api, m, n, k, out):
     (a, ra), (b, rb) = _pair(api, _values(m, k, m + k)), _pair(api, _values(n, k, n * 3 + k))
     for bias in (None, torch.randn(n, device="cuda"), torch.randn(n, device="cuda").bfloat16()):
@@ -159,12 +156,8 @@ def test_no_summed_columns(api):
     R.check(h, want, bound)
 
 
-GATED = [(1, 1, 1), (1, 4096, 4096), (2, 100, 300), (7, 1000, 512), (16, 515, 2000), (33, 17, 129), (64, 64, 128), (65, 130, 257), (200, 768, 768), (509, 2731, 1023),
-         (1000, 2048, 768), (4100, 300, 96), (3000, 1500, 640)]
-
-
 @pytest.mark.parametrize("out", ["f32", "bf16"])
-@pytest.mark.parametrize("m, n, k", GATED)
+@pytest.mark.parametrize("m, n, k", S.GATED)
 def test_gated(api, m, n, k, out):
     g = torch.Generator().manual_seed(m + n + k)
     (x, rx), (gate, rg), (up, ru) = _pair(api, _values(m, k, m + k)), *(_pair(api, (torch.randn((n, k), generator=g) / k ** 0.5).cuda()) for _ in range(2))
