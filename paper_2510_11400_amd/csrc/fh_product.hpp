@@ -187,6 +187,16 @@ template <typename T> __device__ __forceinline__ void load4(const T* p, int64_t 
     for (int e = 0; e < 4; ++e) v[e] = r.at(e);
 }
 
+// Four parameters from column `col` of `n` on, zeros where there are none: by one load, of either type.
+__device__ __forceinline__ void parameter4(const void* p, int32_t dtype, int64_t col, int64_t n, float (&v)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = 0.0f;
+    if (!p) return;
+    if (dtype == FH_F32) load4(static_cast<const float*>(p) + col, n - col, v);
+    else load4(static_cast<const Bf16*>(p) + col, n - col, v);
+}
+
 // ---- the sum split over a workgroup's waves, through LDS -----------------------------------------
 // (32 MT) x (32 NT) sums a workgroup; each wave multiplies every WAVES-th chunk by itself, with an area of LDS of its own and no
 // barrier: a chunk's rows come as whole lines into the area, from there to registers, and while those are multiplied the next chunk's
@@ -316,12 +326,12 @@ __global__ __launch_bounds__(WAVES * 64) void product_waves_kernel(typename Args
     const int col = threadIdx.x % kRuns * 4;
     const uint32_t at = j0 + col;
     float bias[4], bias2[4], scales[4], scales2[4];
+    parameter4(p.bias, p.bias_dtype, at, p.n, bias);
+    parameter4(kPair ? p.bias2 : nullptr, p.bias_dtype, at, p.n, bias2);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const bool inside = at + e < p.n;
-        bias[e] = inside ? parameter(p.bias, p.bias_dtype, at + e, 0.0f) : 0.0f;
         scales[e] = inside ? scale_of<OP>(p.b, p.n, p.b_pitch, p.chunks, at + e) : 0.0f;
-        bias2[e] = kPair && inside ? parameter(p.bias2, p.bias_dtype, at + e, 0.0f) : 0.0f;
         scales2[e] = kPair && inside ? scale_of<OP>(p.b2, p.n, p.b2_pitch, p.chunks, at + e) : 0.0f;
     }
     float sums[2][4] = {};
@@ -341,24 +351,25 @@ __global__ __launch_bounds__(WAVES * 64) void product_waves_kernel(typename Args
             if (out_row(p, i, to)) store4(static_cast<T*>(p.out) + (int64_t)share * p.m * p.n + (int64_t)to * p.stride + at, left, v);
         } else {
             const Sum4 sum2 = sum_at(row, kCols + col);
-            float gate[4], up[4];
+            float gate[4], up[4], dup[4], slopes[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 gate[e] = made_of<OP>(sum[e], mine * scales[e], bias[e]);
                 up[e] = made_of<OP>(sum2[e], mine * scales2[e], bias2[e]);
             }
             if constexpr (MADE == Made::gated) {
+                activate(gate, p.act, v);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = activated(gate[e], p.act) * up[e];
+                for (int e = 0; e < 4; ++e) v[e] *= up[e];
                 store4(static_cast<T*>(p.out) + (int64_t)i * p.stride + at, left, v);
             } else {
-                float dh[4], dup[4];
+                float dh[4], act[4];
                 load4(static_cast<const T*>(p.dh) + (int64_t)i * p.dh_stride + at, left, dh);
+                activate(gate, p.act, act, slopes);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const Activated a = activated_both(gate[e], p.act);
-                    v[e] = e < left ? dh[e] * up[e] * a.slope : 0.0f;
-                    dup[e] = e < left ? dh[e] * a.value : 0.0f;
+                    v[e] = e < left ? dh[e] * up[e] * slopes[e] : 0.0f;
+                    dup[e] = e < left ? dh[e] * act[e] : 0.0f;
                     sums[0][e] += v[e];
                     sums[1][e] += dup[e];
                 }
@@ -422,11 +433,11 @@ __device__ __forceinline__ void tile_epilogue(const Args& p, T* out, const typen
     const uint32_t col2 = kPair ? col : col + 4;
     const int64_t left = (int64_t)p.n - col;
     float bias[2][4], scales[2][4];
+    parameter4(p.bias, p.bias_dtype, col, p.n, bias[0]);
+    parameter4(kPair ? p.bias2 : p.bias, p.bias_dtype, col2, p.n, bias[1]);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const uint32_t inside = col + e < p.n ? col + e : p.n - 1, inside2 = col2 + e < p.n ? col2 + e : p.n - 1;
-        bias[0][e] = parameter(p.bias, p.bias_dtype, inside, 0.0f);
-        bias[1][e] = parameter(kPair ? p.bias2 : p.bias, p.bias_dtype, inside2, 0.0f);
         scales[0][e] = scale_of<OP>(p.b, p.n, p.b_pitch, p.chunks, inside);
         scales[1][e] = scale_of<OP>(kPair ? p.b2 : p.b, p.n, kPair ? p.b2_pitch : p.b_pitch, p.chunks, inside2);
     }
@@ -471,24 +482,31 @@ __device__ __forceinline__ void tile_epilogue(const Args& p, T* out, const typen
 #pragma unroll
             for (int t = 0; t < 2; ++t) of_row((pass + 1) * 16 + t * 8 + mine, next[t]);
         }
+        float first[8], second[8], act[8], slopes[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int t = e / 4;
+            first[e] = made_of<OP>(sum[t][0][e % 4], now[t].scale * scales[0][e % 4], bias[0][e % 4]);
+            second[e] = made_of<OP>(sum[t][1][e % 4], now[t].scale * scales[1][e % 4], bias[1][e % 4]);
+        }
+        if constexpr (MADE == Made::gated) activate(first, p.act, act);
+        if constexpr (MADE == Made::gated_backward) activate(first, p.act, act, slopes);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const uint32_t i = i0 + pass * 16 + t * 8 + mine;
             float v[4], w[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float first = made_of<OP>(sum[t][0][e], now[t].scale * scales[0][e], bias[0][e]);
-                const float second = made_of<OP>(sum[t][1][e], now[t].scale * scales[1][e], bias[1][e]);
+                const int at = t * 4 + e;
                 if constexpr (MADE == Made::linear) {
-                    v[e] = first;
-                    w[e] = second;
+                    v[e] = first[at];
+                    w[e] = second[at];
                 } else if constexpr (MADE == Made::gated) {
-                    v[e] = activated(first, p.act) * second;
+                    v[e] = act[at] * second[at];
                 } else {
-                    const Activated a = activated_both(first, p.act);
                     const bool inside = i < p.m && e < left;     // the others' sums are of no rows
-                    v[e] = inside ? now[t].dh[e] * second * a.slope : 0.0f;
-                    w[e] = inside ? now[t].dh[e] * a.value : 0.0f;
+                    v[e] = inside ? now[t].dh[e] * second[at] * slopes[at] : 0.0f;
+                    w[e] = inside ? now[t].dh[e] * act[at] : 0.0f;
                     sums[0][e] += v[e];
                     sums[1][e] += w[e];
                 }
@@ -879,7 +897,12 @@ __global__ __launch_bounds__(WAVES * 64) void product_rows_kernel(ProductArgs p)
         for (int w = 1; w < WAVES; ++w) sum += s_sums[w][y][out_row][out_col];
         v[y] = made_of<OP>(sum, scales[y], bias[y]);
     }
-    if constexpr (kPair) v[0] = activated(v[0], p.act) * v[1];
+    if constexpr (kPair) {
+        const float gate[1] = {v[0]};
+        float act[1];
+        activate(gate, p.act, act);
+        v[0] = act[0] * v[1];
+    }
     store1(static_cast<T*>(p.out) + (int64_t)i * p.stride + j, v[0]);
 }
 template <typename OP, Made MADE, typename T>
