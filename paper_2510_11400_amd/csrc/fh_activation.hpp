@@ -18,7 +18,7 @@ inline bool is_activation(int a) { return a == FH_SILU || a == FH_GELU || a == F
 //               multiplies the error too, within some 1e-6 of its size); the derivative needs the same power.
 // Powers and reciprocals are the hardware's, a unit in the last place off.  The power's argument is rounded, which is |z| units of the power: what g's own
 // rounding costs it too.  An epilogue of 256 x 128 pairs is bound by these instructions: with the library's expf, erfcf and
-// correctly rounded divisions 8192 tokens of 768 -> 2048 took 66 us (silu) and 83 backward.
+// correctly rounded divisions 8192 tokens of 768 -> 2048 took 3 us of 66 longer (silu).
 constexpr float kLog2E = 1.4426950408889634f, kSqrtHalf = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f, kTwoSqrt2OverPi = 1.5957691216057308f,
                 kCubic = 0.044715f;
 
@@ -61,7 +61,8 @@ __device__ __forceinline__ void activate(const float (&g)[N], int act, float (&v
         for (int i = 0; i < N; ++i) {
             const float square = g[i] * g[i], s = sigmoid(kTwoSqrt2OverPi * __builtin_fmaf(kCubic * g[i], square, g[i]));
             values[i] = g[i] * s;
-            if (slopes) slopes[i] = __builtin_fmaf(kTwoSqrt2OverPi * g[i] * __builtin_fmaf(3.0f * kCubic, square, 1.0f) * (1.0f - s), s, s);
+            // g s (1 - s) first: it is 0 where g^3 leaves the range
+            if (slopes) slopes[i] = __builtin_fmaf(g[i] * (s * (1.0f - s)), kTwoSqrt2OverPi * __builtin_fmaf(3.0f * kCubic, square, 1.0f), s);
         }
     }
 }

@@ -149,7 +149,7 @@ hipError_t forward_operands(const fh_gated_layer& l, ProductArgs& p, Space& spac
     const auto take = [&](const Rows& r, const uint8_t*& at, uint32_t& pitch) {
         if (lies_well(r, l.dtype)) {
             at = static_cast<const uint8_t*>(r.p);
-            pitch = r.rows <= 1 ? 0u : (uint32_t)(r.stride * (int64_t)sizeof(T));
+            pitch = (uint32_t)((r.rows <= 1 ? r.cols : r.stride) * (int64_t)sizeof(T));
             return;
         }
         uint8_t* to = space.take(packed_bytes(r, l.dtype));

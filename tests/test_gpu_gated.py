@@ -187,8 +187,8 @@ def test_no_tokens(api, dtype):
 
 @pytest.mark.parametrize("act", ACTIVATIONS)
 def test_activations_over_their_range(api, act):
-    """The gate alone, from -1e4 to 1e4 and around zero: one feature, unit weights, up is 1."""
-    g = torch.cat((torch.linspace(-12, 12, 4001), torch.logspace(-30, 4, 500), -torch.logspace(-30, 4, 500), torch.tensor([0.0, -0.0])))
+    """The gate alone, from -1e18 (whose cube is out of range) to 1e18 and around zero: one feature, unit weights, up is 1."""
+    g = torch.cat((torch.linspace(-12, 12, 4001), torch.logspace(-30, 18, 700), -torch.logspace(-30, 18, 700), torch.tensor([0.0, -0.0])))
     n = g.numel()
     x = torch.ones(1, 1, device="cuda")
     wg, bu = g.view(n, 1).cuda(), torch.ones(n, device="cuda")
@@ -460,3 +460,29 @@ def test_callers_workspaces(api):
         assert all(torch.equal(a, b) for a, b in zip(got, want)) and bool((room[need:] == 170).all())
         with pytest.raises(api.FedHybridError):
             call(room[:need - 1])
+
+
+def test_the_example_runs_and_its_gradients_are_its_layers(api, layers):
+    """Two steps and the served model; a step's gradients are those of the layers' calls on what was restored."""
+    import importlib.util
+    import math
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "gated_layers.py")
+    spec = importlib.util.spec_from_file_location("gated_layers_example", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    first, last, share = example.main(steps=2, tokens=512, features=64, hidden=96, classes=8)
+    assert math.isfinite(first) and math.isfinite(last) and 0.0 <= share <= 1.0
+    torch.manual_seed(1)
+    model = example.Model(64, 96, 8)
+    x = torch.randn(300, 64, device="cuda").bfloat16()
+    y = model(x)
+    dy = torch.randn_like(y)
+    y.backward(dy)
+    m = model.norm(x).detach()
+    parts = [p.detach() for p in (model.gated.gate.weight, model.gated.up.weight, model.gated.gate.bias, model.gated.up.bias)]
+    h = api.fh_gated(m, *parts).requires_grad_()
+    layers.mx_linear(h, model.down.weight.detach(), model.down.bias.detach()).backward(dy)
+    want = api.fh_gated_backward(h.grad, m, *parts)
+    for p, w in zip((model.gated.gate.weight, model.gated.up.weight, model.gated.gate.bias, model.gated.up.bias), want[1:]):
+        assert torch.equal(p.grad, w)
