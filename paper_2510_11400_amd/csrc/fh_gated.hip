@@ -2,7 +2,7 @@
 //
 // Backward, from x, the weights and dh alone, by three products:
 //   D  = [dg | du]: the forward product again, and in its epilogue dg = dh up act'(gate), du = dh act(gate); rounded to the layer's type, in which
-//        the products behind take it (a relative 2^-9 a value in bf16, as much as the results' own rounding);
+//        the products behind take it (up to a relative 2^-8 a value in bf16, as much as the results' own rounding);
 //   dx = D [Wg; Wu]
 //   [dWg; dWu] = D^T x
 // and the biases' gradients are sums of D's columns before that rounding: partial sums by tiles of rows, joined in order.  Operands whose rows are the
@@ -22,7 +22,7 @@ size_t aligned(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // ---- operands as the products want them ----------------------------------------------------------
 // Rows of any alignment and length to rows of whole chunks, zeros behind their ends: up to three matrices of as many columns, a workgroup a row, sixteen
-// bytes a thread.  (A launch for each took 333 x 515 -> 1001 in fp32, a step, 8 us longer.)
+// bytes a thread.  (A launch for each took 333 x 515 -> 1001 in fp32, a step, 8 us longer; this one takes 4.3 us for 9.6 MB read and written.)
 struct PackArgs {
     const void* x[3];
     uint8_t*    out[3];
@@ -49,7 +49,8 @@ __global__ __launch_bounds__(64) void clear_rows_kernel(T* out, uint32_t cols)
 {
     for (uint32_t c = threadIdx.x; c < cols; c += 64) out[(int64_t)blockIdx.x * cols + c] = T{};
 }
-// The parts of a shared sum, each `hidden_padded` + hidden rows of cols, added up in their order: the first `hidden` rows and the last.
+// The parts of a shared sum, each `hidden_padded` + hidden rows of cols, added up in their order: the first `hidden` rows and the last.  Bound by the memory
+// that the parts come from, the memory-side cache as a rule: two parts of 4096 x 768 to bf16 take 6.6 us, 4.8 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void join_weights_kernel(const float* parts, uint32_t count, uint32_t hidden, uint32_t hidden_padded, uint32_t cols, uint32_t runs, T* gate, T* up)
 {
