@@ -565,11 +565,11 @@ template <typename OP, Made MADE, Lies LA, Lies LB, typename T, int B, int WN>
 __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_kernel(typename ArgsOf<MADE, LB>::type p)
 {
     constexpr bool kPair = MADE != Made::linear;
-    constexpr int kWaves = 2 * WN, kHalf = kWaves / 2, MT = B / 64, NT = 2, kCols = kPair ? B / 2 : B;
-    constexpr uint32_t kStage = 2 * B * kChunkBytes;
+    constexpr int kWaves = 2 * WN, MT = B / 64, NT = 2, kCols = kPair ? B / 2 : B;
+    constexpr uint32_t kOfA = B * kChunkBytes, kStage = 2 * kOfA;
     constexpr int kStores = MT * 4 * (MADE == Made::gated_backward || (MADE == Made::linear && sizeof(T) == 4) ? 2 : 1);   // of a whole tile, a wave's
     typedef ByColumns<OP, B> Columns;
-    static_assert(kHalf * 64 == B && WN * 64 == B, "a wave loads 8 KiB of one operand, and has 64 columns");
+    static_assert(kWaves * 32 == B && WN * 64 == B, "a wave loads 32 rows of each operand, and has 64 columns");
     __shared__ __attribute__((aligned(16))) uint8_t s_stage[2 * kStage + kWaves * 4096];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
@@ -584,16 +584,15 @@ __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_ker
     };
     const auto end_of = [&](uint32_t share) { return p.chunks - share * p.chunks_each < p.chunks_each ? p.chunks : (share + 1) * p.chunks_each; };
 
-    // what is loaded next: a chunk of a tile, in this wave 8 KiB of one operand: by rows 64 of these, two times 32 of a buffer each
-    const bool of_b = wave >= kHalf;
-    const int part = wave % kHalf;
+    // what is loaded next: a chunk of a tile, in this wave 4 KiB of each operand: 32 rows, or as much of its columns.  (64 rows of one operand a
+    // wave: products by columns 2.7 % slower, the backward pass of 4096 x 4096 -> 8192 in bf16 1457 us and 1418 on one card; by rows alike within 1 %.)
     const uint32_t width = (p.chunks - 1) * kChunkBytes + p.tail;
-    uint32_t next_tile = run_of(blockIdx.x, tiles), next_chunk = 0, next_end = 0, next_corner = 0;
-    u32x4 from = {}, from2 = {};
+    uint32_t next_tile = run_of(blockIdx.x, tiles), next_chunk = 0, next_end = 0, next_i = 0, next_j = 0;
+    const bool of_up = kPair && (wave & 1);                      // a pair's rows of B are by turns 32 of the gate and 32 of up
+    const uint32_t pitch_b = of_up ? p.b2_pitch : p.b_pitch;
+    u32x4 from_a = {}, from_b = {};
     const auto aim = [&]() {
-        uint32_t i0, j0;
-        corner(next_tile, i0, j0);
-        next_corner = of_b ? j0 : i0;
+        corner(next_tile, next_i, next_j);
         const uint32_t share = share_of(next_tile);
         next_chunk = share * p.chunks_each;
         next_end = end_of(share);
@@ -602,69 +601,58 @@ __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_ker
             const uint32_t rows = row0 >= all ? 0u : all - row0 < 32u ? all - row0 : 32u;
             return buffer_of(base + (int64_t)(rows ? row0 : 0u) * row_pitch, rows ? (rows - 1) * row_pitch + width : 0u);
         };
-        if (of_b ? LB == Lies::rows : LA == Lies::rows) {
-            if (kPair && of_b) {
-                from = rows_of(p.b, j0 + part * 32, p.n, p.b_pitch);
-                from2 = rows_of(p.b2, j0 + part * 32, p.n, p.b2_pitch);
-            } else {
-                const uint8_t* base = of_b ? p.b : p.a;
-                const uint32_t row0 = next_corner + part * 64, all = of_b ? p.n : p.m, pitch = of_b ? p.b_pitch : p.a_pitch;
-                from = rows_of(base, row0, all, pitch);
-                from2 = rows_of(base, row0 + 32, all, pitch);
-            }
-        }
+        if constexpr (LA == Lies::rows) from_a = rows_of(p.a, next_i + wave * 32, p.m, p.a_pitch);
+        if constexpr (LB == Lies::rows) from_b = rows_of(of_up ? p.b2 : p.b, next_j + (kPair ? wave / 2 : wave) * 32, p.n, pitch_b);
     };
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)s_stage;
-    // Straight code, whichever way the wave's operand lies: four loads from each of two buffers, neighbours `step` bytes apart, every other one
-    // with its pieces turned another way.  Where no tile is left the buffers are empty.
-    struct Load { u32x4 from[2]; uint32_t at[2][2], step[2], moved, to; };
+    // Four loads of an operand from one buffer, neighbours `step` bytes apart, every other one with its pieces turned another way.  Where no tile is left
+    // the buffers are empty.
+    struct Loads { u32x4 from; uint32_t at[2], step, moved, to; };
+    const auto next_rows = [&](u32x4 from, uint32_t pitch, uint32_t l) {
+        constexpr uint32_t kNowhere = 1u << 31;                  // past the end of any buffer here: zeros
+        const uint32_t limit = next_chunk + 1 == p.chunks ? p.tail : kChunkBytes, piece = ((l & 7) ^ (l >> 4)) * 16;
+        return Loads{from, {(piece < limit ? piece : kNowhere) + (l >> 3) * pitch, ((piece ^ 64) < limit ? piece ^ 64 : kNowhere) + (l >> 3) * pitch}, 8 * pitch,
+                     next_chunk * kChunkBytes, 0};
+    };
+    const auto next_columns = [&](const uint8_t* base, uint32_t pitch, uint32_t chunk, uint32_t summed, uint32_t col, uint32_t all, uint32_t l) {
+        const uint32_t place = wave * 4096;
+        return Loads{Columns::buffer(base, pitch, chunk * Columns::kRows + Columns::row_of(place), (chunk + 1) * Columns::kRows, summed, col, all),
+                     {Columns::row_of(l * 16) * pitch + Columns::byte_of(place + l * 16), Columns::row_of(l * 16) * pitch + Columns::byte_of(place + 1024 + l * 16)},
+                     Columns::row_of(1024) * pitch, 0, 0};
+    };
+    struct Load { Loads a, b; };
     const auto next_load = [&](uint32_t stage) {
-        Load n = {};
-        n.to = lds + stage + wave * 8192;
+        Load n;
         uint32_t l = lane;
         asm("" : "+v"(l));                                       // offsets made here, not registers kept
-        if constexpr (LA == Lies::rows || LB == Lies::rows) {
-            constexpr uint32_t kNowhere = 1u << 31;              // past the end of any buffer here: zeros
-            const uint32_t limit = next_chunk + 1 == p.chunks ? p.tail : kChunkBytes, piece = ((l & 7) ^ (l >> 4)) * 16;
-            const uint32_t pitch[2] = {LB == Lies::rows && of_b ? p.b_pitch : p.a_pitch, kPair && of_b ? p.b2_pitch : LB == Lies::rows && of_b ? p.b_pitch : p.a_pitch};
-            n.from[0] = from;
-            n.from[1] = from2;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                n.at[u][0] = (piece < limit ? piece : kNowhere) + (l >> 3) * pitch[u];
-                n.at[u][1] = ((piece ^ 64) < limit ? piece ^ 64 : kNowhere) + (l >> 3) * pitch[u];
-                n.step[u] = 8 * pitch[u];
-            }
-            n.moved = next_chunk * kChunkBytes;
+        if constexpr (LA == Lies::rows) n.a = next_rows(from_a, p.a_pitch, l);
+        else n.a = next_columns(p.a, p.a_pitch, next_chunk, next_tile < end_tile ? p.summed : 0u, next_i, p.m, l);
+        if constexpr (LB == Lies::rows) {
+            n.b = next_rows(from_b, pitch_b, l);
+        } else {
+            const bool second = next_chunk >= p.split;
+            n.b = next_columns(second ? p.b2 : p.b, second ? p.b2_pitch : p.b_pitch, second ? next_chunk - p.split : next_chunk, next_tile < end_tile ? p.summed : 0u,
+                               next_j, p.n, l);
         }
-        if constexpr (LB == Lies::columns) {
-            const bool second = of_b && next_chunk >= p.split, here = LA == Lies::columns || of_b;
-            const uint8_t* base = of_b ? second ? p.b2 : p.b : p.a;
-            const uint32_t pitch = of_b ? second ? p.b2_pitch : p.b_pitch : p.a_pitch, chunk = second ? next_chunk - p.split : next_chunk;
-            const uint32_t summed = next_tile < end_tile ? p.summed : 0u, all = of_b ? p.n : p.m;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const uint32_t place = part * 8192 + u * 4096;
-                const u32x4 buffer = Columns::buffer(base, pitch, chunk * Columns::kRows + Columns::row_of(place), (chunk + 1) * Columns::kRows, summed, next_corner, all);
-                const uint32_t even = Columns::row_of(l * 16) * pitch + Columns::byte_of(place + l * 16);
-                const uint32_t odd = Columns::row_of(l * 16) * pitch + Columns::byte_of(place + 1024 + l * 16);
-                n.from[u] = here ? buffer : n.from[u];
-                n.at[u][0] = here ? even : n.at[u][0];
-                n.at[u][1] = here ? odd : n.at[u][1];
-                n.step[u] = here ? Columns::row_of(1024) * pitch : n.step[u];
-            }
-            n.moved = here ? 0u : n.moved;
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) n.from[u] = in_scalars(n.from[u]);
+        n.a.from = in_scalars(n.a.from);
+        n.b.from = in_scalars(n.b.from);
+        n.a.to = lds + stage + wave * 4096;
+        n.b.to = lds + stage + kOfA + wave * 4096;
         return n;
     };
-    const auto load_piece = [&](const Load& n, int t) { to_lds(n.to + t * 1024, n.from[t / 4], n.at[t / 4][t & 1] + t % 4 * n.step[t / 4], n.moved); };
+    const auto load_piece = [&](const Load& n, int t) {
+        const Loads& o = t < 4 ? n.a : n.b;
+        to_lds(o.to + t % 4 * 1024, o.from, o.at[t & 1] + t % 4 * o.step, o.moved);
+    };
     const auto loaded = [&]() {
         if (++next_chunk != next_end) return;
         next_tile += p.first;
-        if (next_tile < end_tile) aim();
-        else from = from2 = u32x4{from.x, from.y, 0, from.w};
+        if (next_tile < end_tile) {
+            aim();
+        } else {
+            from_a = u32x4{from_a.x, from_a.y, 0, from_a.w};
+            from_b = u32x4{from_b.x, from_b.y, 0, from_b.w};
+        }
     };
     const auto load = [&](uint32_t stage) {
         const Load n = next_load(stage);
@@ -674,7 +662,7 @@ __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_ker
     };
 
     const int h = lane >> 5, r = lane & 31, turned = (h * 4) ^ (lane >> 1 & 7);
-    const uint32_t read_a = (wm * MT * 32 + r) * kChunkBytes, read_b = (B + wn * NT * 32 + r) * kChunkBytes;
+    const uint32_t read_a = (wm * MT * 32 + r) * kChunkBytes, read_b = kOfA + (wn * NT * 32 + r) * kChunkBytes;
     u32x4 fa[2][MT], fb[2][NT];
     const auto read = [&](uint32_t stage, int quarter, int to) {
         const uint8_t* at_piece = s_stage + stage + (uint32_t)(turned ^ quarter) * 16;
@@ -686,7 +674,7 @@ __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_ker
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             if constexpr (LB == Lies::rows) fb[to][t] = *reinterpret_cast<const u32x4*>(at_piece + read_b + t * 4096);
-            else fb[to][t] = Columns::read(s_stage + stage + B * kChunkBytes, (wn * NT + t) * 32, quarter, lane);
+            else fb[to][t] = Columns::read(s_stage + stage + kOfA, (wn * NT + t) * 32, quarter, lane);
         }
     };
     typename OP::Sums c[MT][NT];
