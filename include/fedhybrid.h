@@ -647,7 +647,8 @@ fh_status fh_mx_layer_backward(const fh_mx_layer *layer, void *stream);
  *
  * Stored matrices and workspaces are 16-byte aligned, plain matrices and vectors aligned to their
  * elements.  rows, cols <= 2^31 - 256 (products: k <= 2^17 - 1, so that no sum overflows);
- * row_stride <= 2^31.  Nothing is launched where there is no output. */
+ * row_stride <= 2^31.  Nothing is launched where there is no output.  No output may overlap another
+ * pointer's memory; inputs may be the same. */
 typedef enum fh_activation { FH_SILU = 0, FH_GELU = 1, FH_GELU_TANH = 2 } fh_activation;
 size_t    fh_q8_bytes(int64_t rows, int64_t cols);             /* of a stored matrix; 0 for a bad shape */
 size_t    fh_q8_scales_offset(int64_t rows, int64_t cols);
@@ -697,10 +698,11 @@ fh_status fh_q8_gated(const fh_q8_gated_product *product, void *stream);
  * row strides; dx, dw_gate and dw_up are dense.  Everything is of dtype; b_gate and b_up may be NULL.
  * tokens <= 2^21, 1 <= features, hidden <= 2^20, row strides <= 2^31.  tokens = 0 writes zeros to the
  * gradients of the parameters that are asked for.  The sums' order depends on the shapes, the strides and
- * the pointers' alignment alone.  No output may overlap another pointer's memory.
+ * the pointers' alignment alone.  No output may overlap another pointer's memory; inputs may be the same.
  * fh_gated_workspace_bytes: of the forward (backward = 0) or the backward call with this layer; it looks at the
  * shape, the strides, needs, at whether db_gate and db_up are NULL, and at the operands' addresses, not at what
- * is there; 0 for a layer that the call refuses.  The workspace is 16-byte aligned and free again once the call's work has run. */
+ * is there; 0 for no tokens and for a shape, strides of operands, dtype, activation, needs or reserved field that
+ * the call refuses.  The workspace is 16-byte aligned and free again once the call's work has run. */
 #define FH_GATED_NEEDS_INPUT  1
 #define FH_GATED_NEEDS_WEIGHT 2
 typedef struct fh_gated_layer {

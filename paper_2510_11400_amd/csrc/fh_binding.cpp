@@ -10,9 +10,11 @@
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/autograd/variable.h>
 
 #include <ATen/hip/EmptyTensor.h>
 #include <c10/hip/HIPFunctions.h>
+#include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 
 #include "../../include/fedhybrid.h"
@@ -954,6 +956,17 @@ struct Gated : torch::autograd::Function<Gated> {
     }
 };
 
+// A leaf has one node that takes its gradient, of the stream on which it was first used, for as long as any graph of it lives.  A captured backward pass has that
+// stream wait for the captured one; the default stream cannot, and the process ends.
+void no_eager_graph(const at::Tensor& t, const char* what)
+{
+    if (!t.defined() || !t.requires_grad() || !t.is_leaf()) return;
+    const auto node = torch::autograd::impl::try_get_grad_accumulator(t);
+    const auto stream = node ? node->stream() : std::nullopt;
+    if (stream && stream->id() == 0)
+        raise(PyExc_RuntimeError, "%s is part of a graph of autograd from outside of this capture that is still alive; delete what came of it before capturing", what);
+}
+
 // (x, w_gate, w_up, b_gate, b_up, activation) -> h
 FH_ENTRY(gated_linear, 6)
     const at::Tensor x = tensor(a[0], "x"), w_gate = tensor(a[1], "w_gate"), w_up = tensor(a[2], "w_up"), b_gate = tensor_or_none(a[3], "b_gate"),
@@ -969,6 +982,9 @@ FH_ENTRY(gated_linear, 6)
     pass->shape = x.sizes().vec();
     if (pass->x || pass->gate || pass->up || pass->b_gate || pass->b_up) {
         const auto some = [](const at::Tensor& t) { return t.defined() ? std::optional<at::Tensor>(t) : std::nullopt; };
+        if (c10::hip::currentStreamCaptureStatusMayInitCtx() != c10::hip::CaptureStatus::None) {
+            no_eager_graph(x, "x"); no_eager_graph(w_gate, "w_gate"); no_eager_graph(w_up, "w_up"); no_eager_graph(b_gate, "b_gate"); no_eager_graph(b_up, "b_up");
+        }
         return wrap(Gated::apply(x, w_gate, w_up, some(b_gate), some(b_up), pass));
     }
     const Matrix m = matrix(rows_of(x), "x"), gate = matrix(w_gate, "w_gate"), up = matrix(w_up, "w_up");
