@@ -689,7 +689,8 @@ fh_status fh_q8_gated(const fh_q8_gated_product *product, void *stream);
  * gate = x Wg^T + bg,  up = x Wu^T + bu,  h = act(gate) * up, all in binary32, rounded once to dtype.
  * fh_gated writes h.  fh_gated_backward computes from x, the weights, the biases and dh alone (gate and
  * up are computed again; a forward call leaves nothing behind for it)
- *   dgate = dh up act'(gate),  dup = dh act(gate), rounded to dtype for the products that follow:
+ *   dgate = dh up act'(gate),  dup = dh act(gate), rounded to dtype for the products that follow (bf16, with
+ *   tokens * hidden <= 2^19 and tokens * hidden * features <= 2^27: to two such values each, off by 2^-16):
  *   dx = dgate Wg + dup Wu (with FH_GATED_NEEDS_INPUT),
  *   dw_gate = dgate^T x,  dw_up = dup^T x (with FH_GATED_NEEDS_WEIGHT),
  *   db_gate, db_up (each where it is not NULL): sums over the tokens, from before that rounding,

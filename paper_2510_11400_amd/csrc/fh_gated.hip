@@ -2,7 +2,7 @@
 //
 // Backward, from x, the weights and dh alone, by three products:
 //   D  = [dg | du]: the forward product again, and in its epilogue dg = dh up act'(gate), du = dh act(gate); rounded to the layer's type, in which
-//        the products behind take it (up to a relative 2^-8 a value in bf16, as much as the results' own rounding);
+//        the products behind take it (up to a relative 2^-8 a value in bf16, as much as the results' own rounding; small layers keep what it leaves);
 //   dx = D [Wg; Wu]
 //   [dWg; dWu] = D^T x
 // and the biases' gradients are sums of D's columns before that rounding: partial sums by tiles of rows, joined in order.  Operands whose rows are the
@@ -104,9 +104,9 @@ template <> struct OpOf<float> { typedef OfF32 type; };
 template <> struct OpOf<Bf16> { typedef OfBf16 type; };
 
 // The kernel of the products of a layer's pairs of sums.
-ProductTile pair_tile(const fh_gated_layer& l)
+ProductTile pair_tile(const fh_gated_layer& l, ProductTile last = ProductTile::square256)
 {
-    return product_tile(l.tokens, 2 * l.hidden, padded_bytes(l.features, l.dtype) / kChunkBytes, l.dtype == FH_F32);
+    return product_tile(l.tokens, 2 * l.hidden, padded_bytes(l.features, l.dtype) / kChunkBytes, l.dtype == FH_F32, last);
 }
 
 // The chunks of rows of `values`.
@@ -201,6 +201,9 @@ hipError_t forward_of(const fh_gated_layer& l, hipStream_t s)
 // What the backward call lays out in its workspace.
 struct Backward {
     int64_t hidden_padded;             // columns of D's halves: whole chunks, so that the products over them have no tails, zeros behind the last
+    bool rests;                        // D's rows are [dg | du | what their rounding left of each]
+    int64_t d_columns;                 // of a row of D
+    ProductTile pair, last;            // the first product's kernel; the last one that the products may take
     int64_t sum_rows;                  // rows that a partial sum of the biases' gradients stands for
     ProductPlan weights;
     size_t d, sums, parts, forward;
@@ -211,12 +214,16 @@ Backward backward_of(const fh_gated_layer& l)
     const size_t size = dtype_size(l.dtype);
     Backward b = {};
     b.hidden_padded = padded_bytes(l.hidden, l.dtype) / (int64_t)size;
-    b.sum_rows = product_sum_rows(pair_tile(l));
-    b.d = aligned((size_t)l.tokens * (size_t)(2 * b.hidden_padded) * size);
+    b.rests = product_with_rests(l.tokens, l.features, l.hidden, l.dtype == FH_F32);
+    b.last = product_last(b.rests);
+    b.pair = pair_tile(l, b.last);
+    b.sum_rows = product_sum_rows(b.pair);
+    b.d_columns = (b.rests ? 4 : 2) * b.hidden_padded;
+    b.d = aligned((size_t)l.tokens * (size_t)b.d_columns * size);
     if (l.db_gate || l.db_up) b.sums = aligned((size_t)((l.tokens + b.sum_rows - 1) / b.sum_rows) * 2u * (size_t)l.hidden * 4u);
     if (l.needs & FH_GATED_NEEDS_WEIGHT) {
         const int64_t m = b.hidden_padded + l.hidden;
-        b.weights = product_plan(m, l.features, padded_bytes(l.tokens, l.dtype) / kChunkBytes, l.dtype == FH_F32, true);
+        b.weights = product_plan(m, l.features, (b.rests ? 2 : 1) * padded_bytes(l.tokens, l.dtype) / kChunkBytes, l.dtype == FH_F32, true, b.last);
         if (b.weights.parts > 1) b.parts = aligned((size_t)b.weights.parts * (size_t)m * (size_t)l.features * 4u);
     }
     b.forward = forward_bytes(l);
@@ -258,41 +265,47 @@ hipError_t backward_of(const fh_gated_layer& l, hipStream_t s)
     e = forward_operands<T>(l, p, space, s);
     if (e != hipSuccess) return e;
     p.out = d;
-    p.stride = 2 * b.hidden_padded;
+    p.stride = b.d_columns;
     p.dh = l.dh;
     p.dh_stride = l.dh_stride;
     p.up_at = b.hidden_padded;
+    p.rest_at = b.rests ? 2 * b.hidden_padded : 0;
     p.sums = b.sums ? sums : nullptr;
-    e = product_by<Op, Made::gated_backward, T>(pair_tile(l), p, s);
+    e = product_by<Op, Made::gated_backward, T>(b.pair, p, s);
     if (e == hipSuccess && b.sums) e = launch_join(sums, (l.tokens + b.sum_rows - 1) / b.sum_rows, l.hidden, 2, l.dtype, l.db_gate, l.db_up, s);
 
     if (e == hipSuccess && (l.needs & FH_GATED_NEEDS_INPUT)) {
         TurnedArgs q = {};
         q.a = reinterpret_cast<const uint8_t*>(d);
-        q.a_pitch = (uint32_t)(2 * b.hidden_padded * size);
-        set_summed<T>(q, 2 * b.hidden_padded);
+        q.a_pitch = (uint32_t)(b.d_columns * size);
+        set_summed<T>(q, b.d_columns);
         q.b = p.b;
         q.b2 = p.b2;
         q.b_pitch = p.b_pitch;
         q.b2_pitch = p.b2_pitch;
         q.summed = (uint32_t)l.hidden;
-        q.split = q.chunks / 2;
+        q.halves = b.rests;
+        q.rest = (uint32_t)(2 * b.hidden_padded * size);
+        q.split = q.rest / 2 / kChunkBytes;
         q.gap_from = (uint32_t)l.tokens;
         q.m = (uint32_t)l.tokens;
         q.n = (uint32_t)l.features;
         q.out = l.dx;
         q.stride = l.features;
-        e = product_by<Op, Made::linear, T, Lies::rows, Lies::columns>(product_tile(q.m, q.n, q.chunks, sizeof(T) == 4), q, s);
+        e = product_by<Op, Made::linear, T, Lies::rows, Lies::columns>(product_tile(q.m, q.n, q.chunks, sizeof(T) == 4, b.last), q, s);
     }
     if (e == hipSuccess && (l.needs & FH_GATED_NEEDS_WEIGHT)) {
         TurnedArgs q = {};
         q.a = reinterpret_cast<const uint8_t*>(d);
-        q.a_pitch = (uint32_t)(2 * b.hidden_padded * size);
+        q.a_pitch = (uint32_t)(b.d_columns * size);
         q.b = p.a;
         q.b_pitch = p.a_pitch;
         set_summed<T>(q, l.tokens);
         q.summed = (uint32_t)l.tokens;
         q.split = q.chunks;
+        q.halves = b.rests;
+        if (b.rests) q.chunks = q.chunks_each = 2 * q.chunks;
+        q.rest = (uint32_t)(2 * b.hidden_padded * size);
         q.n = (uint32_t)l.features;
         q.stride = l.features;
         if (b.weights.parts > 1) {
@@ -315,7 +328,7 @@ hipError_t backward_of(const fh_gated_layer& l, hipStream_t s)
         q.gap_from = (uint32_t)l.hidden;
         q.gap = one ? (uint32_t)(b.hidden_padded - l.hidden) : 0u;
         q.out = l.dw_gate;
-        const ProductTile tile = product_tile(q.m, q.n, q.chunks, sizeof(T) == 4);
+        const ProductTile tile = b.weights.tile;                 // wherever they lie: the same sums
         e = product_by<Op, Made::linear, T, Lies::columns, Lies::columns>(tile, q, s);
         if (e == hipSuccess && !one) {
             q.a += b.hidden_padded * size;

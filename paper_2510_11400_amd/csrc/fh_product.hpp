@@ -83,6 +83,7 @@ struct BackwardArgs : ProductArgs {    // out: the gate's gradients, and `up_at`
     const void*    dh;
     int64_t        dh_stride;
     int64_t        up_at;
+    int64_t        rest_at;            // columns from a gradient to the rest of its rounding; 0: there are none (tiles through LDS know none)
     float*         sums;               // [m_tiles][2][n] sums of the columns over the tile's rows, or null
 };
 struct TurnedArgs;
@@ -91,6 +92,8 @@ template <> struct has_gap<TurnedArgs> { static constexpr bool value = true; };
 struct TurnedArgs : ProductArgs {      // products with an operand that lies by columns: its rows are the summed dimension
     uint32_t       summed;             // rows of a and b where they lie so
     uint32_t       split;              // chunks that b has; b2 goes on behind them
+    uint32_t       halves;             // 1: every chunk twice in turn, of b the same, of a at a + rest the second time; 0 (in tiles through LDS always): once
+    uint32_t       rest;
     uint32_t       gap_from, gap;      // so many rows of out from there on are left out, those behind them move up
 };
 // The row of out that row i's outputs go to; false where they go nowhere.
@@ -187,6 +190,16 @@ template <typename T> __device__ __forceinline__ void load4(const T* p, int64_t 
     for (int e = 0; e < 4; ++e) v[e] = r.at(e);
 }
 
+// What is left of four values by their rounding to bf16; nothing where the rounded one is no number.
+__device__ __forceinline__ void rests(float (&v)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float rest = v[e] - __builtin_bit_cast(float, bf16_pair(v[e], v[e]) << 16);
+        v[e] = __builtin_fabsf(rest) < __builtin_inff() ? rest : 0.0f;
+    }
+}
+
 // Four parameters from column `col` of `n` on, zeros where there are none: by one load, of either type.
 __device__ __forceinline__ void parameter4(const void* p, int32_t dtype, int64_t col, int64_t n, float (&v)[4])
 {
@@ -252,12 +265,18 @@ __global__ __launch_bounds__(WAVES * 64) void product_waves_kernel(typename Args
     constexpr uint32_t kNowhere = 1u << 31;                      // past the end of any buffer here
     const auto load = [&](uint32_t chunk) {
         const bool cut = chunk + 1 == p.chunks && p.tail < kChunkBytes;
+        uint32_t mine = chunk, rest = 0;                         // chunk of the operands, bytes of a in front of it
+        if constexpr (LB == Lies::columns) {
+            mine = chunk >> p.halves;
+            rest = chunk & p.halves ? p.rest : 0;
+        }
         if constexpr (LA == Lies::rows) {
+            const uint32_t moved = mine * kChunkBytes + rest;
 #pragma unroll
             for (int t = 0; t < MT * 4; ++t)
-                to_lds(lds + t * 1024, from_a, cut && (piece ^ (t & 1) * 64) >= p.tail ? kNowhere : at_a[t], chunk * kChunkBytes);
+                to_lds(lds + t * 1024, from_a, cut && (piece ^ (t & 1) * 64) >= p.tail ? kNowhere : at_a[t], moved);
         } else {
-            from_a = ColumnsA::buffer(p.a, p.a_pitch, chunk * ColumnsA::kRows, (chunk + 1) * ColumnsA::kRows, p.summed, i0, p.m);
+            from_a = ColumnsA::buffer(p.a + rest, p.a_pitch, mine * ColumnsA::kRows, (mine + 1) * ColumnsA::kRows, p.summed, i0, p.m);
 #pragma unroll
             for (int t = 0; t < MT * 4; ++t) to_lds(lds + t * 1024, from_a, at_a[t], 0);
         }
@@ -267,9 +286,9 @@ __global__ __launch_bounds__(WAVES * 64) void product_waves_kernel(typename Args
                 to_lds(lds + kRowsA * kChunkBytes + t * 1024, t * 8 < kCols ? from_b : from_b2, cut && (piece ^ (t & 1) * 64) >= p.tail ? kNowhere : at_b[t],
                        chunk * kChunkBytes);
         } else {
-            const bool second = chunk >= p.split;
+            const bool second = mine >= p.split;
             const uint32_t pitch = second ? p.b2_pitch : p.b_pitch;
-            const uint32_t row = (second ? chunk - p.split : chunk) * ColumnsB::kRows;
+            const uint32_t row = (second ? mine - p.split : mine) * ColumnsB::kRows;
             from_b = ColumnsB::buffer(second ? p.b2 : p.b, pitch, row, row + ColumnsB::kRows, p.summed, j0, p.n);
 #pragma unroll
             for (int t = 0; t < NT * 4; ++t)
@@ -378,6 +397,12 @@ __global__ __launch_bounds__(WAVES * 64) void product_waves_kernel(typename Args
                 T* to = static_cast<T*>(p.out) + (int64_t)i * p.stride + at;
                 store4(to, p.up_at - at, v);
                 store4(to + p.up_at, p.up_at - at, dup);
+                if (sizeof(T) == 2 && p.rest_at) {
+                    rests(v);
+                    rests(dup);
+                    store4(to + p.rest_at, p.up_at - at, v);
+                    store4(to + p.rest_at + p.up_at, p.up_at - at, dup);
+                }
             }
         }
     }

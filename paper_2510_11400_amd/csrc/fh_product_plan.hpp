@@ -37,13 +37,13 @@ inline int64_t product_time(ProductTile t, int64_t tiles, int64_t c, bool slow)
     return (tiles + 255) / 256 * (slow ? 1326 + 718 * c : 1095 + 116 * c);
 }
 
-// m x n sums (a pair's both) over `chunks` chunks.
-inline ProductPlan product_plan(int64_t m, int64_t n, int64_t chunks, bool slow, bool shared)
+// m x n sums (a pair's both) over `chunks` chunks, by a kernel up to `last`.
+inline ProductPlan product_plan(int64_t m, int64_t n, int64_t chunks, bool slow, bool shared, ProductTile last = ProductTile::square256)
 {
     ProductPlan best = {ProductTile::waves32, 1, (uint32_t)chunks};
     int64_t least = 0;
     if (chunks == 0) return best;
-    for (int32_t i = 0; i <= (int32_t)ProductTile::square256; ++i) {
+    for (int32_t i = 0; i <= (int32_t)last; ++i) {
         const ProductTile t = (ProductTile)i;
         const int64_t side = product_side(t), tiles = ((m + side - 1) / side) * ((n + side - 1) / side);
         // A shared sum's parts, eight chunks of it at least, are written and read once more by a kernel of their own.
@@ -56,7 +56,10 @@ inline ProductPlan product_plan(int64_t m, int64_t n, int64_t chunks, bool slow,
     }
     return best;
 }
-inline ProductTile product_tile(int64_t m, int64_t n, int64_t chunks, bool slow) { return product_plan(m, n, chunks, slow, false).tile; }
+inline ProductTile product_tile(int64_t m, int64_t n, int64_t chunks, bool slow, ProductTile last = ProductTile::square256)
+{
+    return product_plan(m, n, chunks, slow, false, last).tile;
+}
 
 // Whether the kernel that is made for few rows takes a product.  In 8 bits 1, 4 and 8 rows of 4096 x 8192 took it 6.2, 6.9 and 7.6 us, the kernels above 6.8, 7.1
 // and 7.0; of 4096 x 4096 4.1, 4.5, 4.8 and 5.1, 5.0, 5.2; pairs of 8192 x 4096 14.8, 15.2, 11.5 and 16.1, 16.1, 12.5; fp32 4 and 16 rows, pairs of 2048 x 1024 and
@@ -65,5 +68,18 @@ inline ProductTile product_tile(int64_t m, int64_t n, int64_t chunks, bool slow)
 constexpr int64_t kMostFewRows = 16;
 inline bool few_rows_of_bytes(int64_t m, bool pair) { return m <= (pair ? 8 : 4); }
 inline bool few_rows_dense(int64_t m, bool slow, bool laid_out) { return m <= kMostFewRows && (slow || laid_out); }
+
+
+// Whether a backward pass keeps what the rounding of [dg | du] to bf16 leaves, as two bf16 values for one (by the kernels up to waves64 alone).  The sums of dx and dW
+// average a rounding's errors where many gradients are summed; where few are, or a few outweigh the others, the results' errors are up to three times those of their own
+// rounding (over 1.5 times in 13 of 100 random layers of 2^14 to 2^18 gradients, 7 and 2 in the next doublings, against 1.4 for large ones).  It costs little there
+// (us; tokens x features x hidden, without and with): 26 x 63 x 49 16.5 and 16.5, 200 x 400 x 300 15 and 17, 333 x 515 x 700 26 and 30, 4096 x 1024 x 64 30 and 34; a layer of
+// 1024 x 512 x 512 would take 25 and 34, of 8 x 4000 x 8192 104 and 173.
+constexpr int64_t kMostWithRests = (int64_t)1 << 19, kMostTermsWithRests = (int64_t)1 << 27;
+inline bool product_with_rests(int64_t tokens, int64_t features, int64_t hidden, bool slow)
+{
+    return !slow && tokens * hidden <= kMostWithRests && tokens * hidden * features <= kMostTermsWithRests;
+}
+inline ProductTile product_last(bool rests) { return rests ? ProductTile::waves64 : ProductTile::square256; }
 
 }  // namespace fh

@@ -87,9 +87,10 @@ def gated(gate, up, act, dtype):
     return h, bound + (HALF[dtype] + 2 * STEP) * (h.abs() + bound)
 
 
-def gated_backward(dh, x, wg, wu, bg, bu, act):
-    """Five (gradient, bound) pairs."""
+def gated_backward(dh, x, wg, wu, bg, bu, act, rests=False):
+    """Five (gradient, bound) pairs; `rests`: the gradients of gate and up are two values of x's type each between the products, twice as many to add."""
     dtype, half = x.dtype, HALF[x.dtype]
+    held, times = (half * half, 2 * (1 + 2 * half)) if rests else (half, 1)      # rests are up to `half` of the values: so much more to add
     g, eg = dense_product(x, wg, bg)
     u, eu = dense_product(x, wu, bu)
     a, slope = activation(g, act)
@@ -103,13 +104,13 @@ def gated_backward(dh, x, wg, wu, bg, bu, act):
     def rounded(y, bound, to=half):
         return y, bound + to * (y.abs() + bound)
 
-    _, edg_r = rounded(dg, edg)                                  # as the products take them
-    _, edu_r = rounded(du, edu)
+    _, edg_r = rounded(dg, edg, held)                            # as the products take them
+    _, edu_r = rounded(du, edu, held)
     dx = mm(dg, wg) + mm(du, wu)
-    ex = mm(edg_r, wg.abs()) + mm(edu_r, wu.abs()) + (2 * n + 2) * 2 * STEP * (mm(dg.abs() + edg_r, wg.abs()) + mm(du.abs() + edu_r, wu.abs()))
+    ex = mm(edg_r, wg.abs()) + mm(edu_r, wu.abs()) + (2 * n * times + 2) * 2 * STEP * (mm(dg.abs() + edg_r, wg.abs()) + mm(du.abs() + edu_r, wu.abs()))
 
     def weight(d, ed):
-        return rounded(mm(d.t(), x), mm(ed.t(), x.abs()) + (t + 2) * 2 * STEP * mm((d.abs() + ed).t(), x.abs()))
+        return rounded(mm(d.t(), x), mm(ed.t(), x.abs()) + (t * times + 2) * 2 * STEP * mm((d.abs() + ed).t(), x.abs()))
 
     def bias(d, ed):
         return rounded(d.sum(0), ed.sum(0) + (t + 2) * STEP * (d.abs() + ed).sum(0))

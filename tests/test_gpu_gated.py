@@ -77,6 +77,31 @@ def test_backward(api, t, k, f, dtype, act):
     assert all(torch.equal(a, b) for a, b in zip(got, again))
 
 
+@pytest.mark.parametrize("act", ACTIVATIONS)
+@pytest.mark.parametrize("t, k, f", S.WITH_RESTS)
+def test_small_backward_passes_keep_the_rests_of_a_rounding(api, t, k, f, act):
+    """Up to 2^19 gradients of the gates and 2^27 products of theirs: the products take each with its rounding's rest.  A bf16 value is off by 2^-8 of it at most, its rest by 2^-8 of that:
+    2^-16 in all, and the sums have twice as many terms."""
+    x, wg, wu, bg, bu, dh = _inputs(t, k, f, torch.bfloat16)
+    want = R.gated_backward(dh, x, wg, wu, bg, bu, act, rests=True)
+    got = api.fh_gated_backward(dh, x, wg, wu, bg, bu, act)
+    for name, y, (w, bound) in zip(("dx", "dw_gate", "dw_up", "db_gate", "db_up"), got, want):
+        R.check(y, w, bound, (name, t, k, f, act))
+
+
+def test_rests_of_what_is_no_number(api):
+    """Gradients beyond bf16's range and NaN: the results that they reach are no numbers, the others are as without them."""
+    x, wg, wu, bg, bu, dh = _inputs(40, 64, 50, torch.bfloat16)
+    want = api.fh_gated_backward(dh, x, wg, wu, bg, bu, "silu")
+    dh[3, 7], dh[20, 0] = float("nan"), float("inf")
+    got = api.fh_gated_backward(dh, x, wg, wu, bg, bu, "silu")
+    rest = [i for i in range(40) if i not in (3, 20)]
+    assert not bool(torch.isfinite(got[0][[3, 20]]).any()) and torch.equal(got[0][rest], want[0][rest])
+    cols = [i for i in range(50) if i not in (0, 7)]
+    for g, w in zip(got[1:], want[1:]):
+        assert not bool(torch.isfinite(g[[0, 7]]).any()) and torch.equal(g[cols], w[cols])
+
+
 @pytest.mark.parametrize("dtype, t, k, f", S.LARGE)
 def test_large(api, dtype, t, k, f):
     x, wg, wu, bg, bu, dh = _inputs(t, k, f, DTYPES[dtype])

@@ -19,7 +19,7 @@ def _program(folder, body):
         pytest.skip("no C++ compiler")
     src, exe = str(folder / "rules.cpp"), str(folder / "rules")
     with open(src, "w") as f:
-        f.write(f'#include "fh_product_plan.hpp"\n#include <cstdio>\nint main()\n{{\n    long long a, b, c, d, e;\n    {body}\n}}\n')
+        f.write(f'#include "fh_product_plan.hpp"\n#include <cstdio>\nint main()\n{{\n    long long a, b, c, d, e, f;\n    {body}\n}}\n')
     subprocess.run([cxx, "-std=c++17", "-I", CSRC, src, "-o", exe], check=True)
     return lambda rows: [tuple(int(v) for v in line.split()) for line in subprocess.run(
         [exe], input="".join(" ".join(map(str, r)) + "\n" for r in rows), text=True, check=True, capture_output=True).stdout.splitlines()]
@@ -27,11 +27,12 @@ def _program(folder, body):
 
 @pytest.fixture(scope="module")
 def plans(tmp_path_factory):
-    """plans(rows of m, n, chunks, fp32, shared) -> (kernel, parts, chunks a part, side, rows of a sum of columns)"""
-    return _program(tmp_path_factory.mktemp("rules"), '''while (std::scanf("%lld %lld %lld %lld %lld", &a, &b, &c, &d, &e) == 5) {
-        const fh::ProductPlan p = fh::product_plan(a, b, c, d != 0, e != 0);
+    """plans(rows of m, n, chunks, fp32, shared, with rests) -> (kernel, parts, chunks a part, side, rows of a sum of columns)"""
+    run = _program(tmp_path_factory.mktemp("rules"), '''while (std::scanf("%lld %lld %lld %lld %lld %lld", &a, &b, &c, &d, &e, &f) == 6) {
+        const fh::ProductPlan p = fh::product_plan(a, b, c, d != 0, e != 0, fh::product_last(f != 0));
         std::printf("%d %u %u %lld %lld\\n", (int)p.tile, p.parts, p.chunks_each, (long long)fh::product_side(p.tile), (long long)fh::product_sum_rows(p.tile));
     }''')
+    return lambda rows: run([(*r, 0) if len(r) == 5 else r for r in rows])
 
 
 @pytest.fixture(scope="module")
@@ -73,3 +74,15 @@ def test_few_rows(few):
     rows = [(m, pair) for m in (1, 4, 5, 8, 9, 16, 17) for pair in (0, 1)]
     for (m, flag), (of_bytes, fp32, bf16) in zip(rows, few(rows)):
         assert of_bytes == (m <= (8 if flag else 4)) and fp32 == (m <= 16) and bf16 == (m <= 16 and flag)
+
+
+def test_rests_are_kept_of_few_gradients_in_bf16(tmp_path, plans):
+    run = _program(tmp_path, 'while (std::scanf("%lld %lld %lld %lld", &a, &b, &c, &d) == 4) std::printf("%d\\n", (int)fh::product_with_rests(a, b, c, d != 0));')
+    rows = [(1, 1, 1, 0), (1, 1, 1, 1), (512, 256, 1024, 0), (512, 257, 1024, 0), (512, 1, 1025, 0), (512, 256, 512, 1), (1 << 21, 1, 1, 0), (1 << 19, 256, 1, 0),
+            (1 << 21, 1 << 20, 1 << 20, 0)]
+    assert [r[0] for r in run(rows)] == [1, 0, 1, 0, 0, 0, 0, 1, 0]
+    shapes = [S.products_of("bf16", *s) for s in S.WITH_RESTS]
+    assert all(p["dx"][5] for p in shapes)
+    taken = {name: {p[0] for p in plans([s[name] for s in shapes])} for name in ("pair", "dx", "dw")}
+    assert taken["pair"] == {0, 1} and taken["dx"] == {0, 1, 2} and taken["dw"] == {0, 1, 2}, taken
+    assert {p[1] > 1 for p in plans([s["dw"] for s in shapes])} == {False, True}
