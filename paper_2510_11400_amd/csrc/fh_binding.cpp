@@ -8,7 +8,7 @@
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
-#include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/autograd/function.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/autograd/variable.h>
 
@@ -633,6 +633,27 @@ struct Pass : torch::CustomClassHolder {                                  // fro
     at::ScalarType p_type;
 };
 
+// What the gradients of a pass come from: it refuses to be differentiated.
+struct Once : torch::autograd::Node {
+    std::string what;
+    Once(std::string w, torch::autograd::edge_list&& next) : Node(std::move(next)), what(std::move(w)) {}
+    torch::autograd::variable_list apply(torch::autograd::variable_list&&) override { throw std::runtime_error(what + " is differentiated once"); }
+};
+// In a backward pass whose graph is kept: its results as what they depend on has them, which is the running node's inputs, whatever is wanted of `given`, the gradient
+// that the pass was given.  Joined to those, the refusal is met by torch.autograd.grad as well, which runs only what lies between.
+void once(const char* what, const at::Tensor& given, torch::autograd::variable_list& grads)
+{
+    if (!at::GradMode::is_enabled()) return;
+    torch::autograd::edge_list next = torch::autograd::get_current_node()->next_edges();
+    next.push_back(torch::autograd::impl::gradient_edge(given));
+    const std::shared_ptr<torch::autograd::Node> node(new Once(what, std::move(next)), torch::autograd::deleteNode);
+    for (at::Tensor& g : grads) {
+        if (!g.defined()) continue;
+        g = g.detach();
+        torch::autograd::create_gradient_edge(g, node);
+    }
+}
+
 struct Linear : torch::autograd::Function<Linear> {
     using Context = torch::autograd::AutogradContext;
     static at::Tensor forward(Context* ctx, const at::Tensor& x, const std::optional<at::Tensor>& norm_weight, const std::optional<at::Tensor>& norm_bias,
@@ -652,7 +673,6 @@ struct Linear : torch::autograd::Function<Linear> {
     static torch::autograd::variable_list backward(Context* ctx, const torch::autograd::variable_list& given)
     {
         const auto pass = c10::static_intrusive_pointer_cast<Pass>(ctx->saved_data.at("pass").toCapsule());
-        const bool again = at::GradMode::is_enabled() && given[0].requires_grad();
         torch::autograd::variable_list grads(6);
         {
             const at::AutoGradMode off(false);
@@ -667,10 +687,8 @@ struct Linear : torch::autograd::Function<Linear> {
             grads[3] = b.dweight;
             grads[4] = b.dbias;
         }
-        if (!again) return grads;
-        for (at::Tensor& g : grads)                                       // leaves of a graph that ends in an error
-            if (g.defined()) g = g.detach().set_requires_grad(true);
-        return torch::autograd::DelayedError("a linear layer in microscaled form is differentiated once", (int64_t)grads.size()).apply(std::move(grads));
+        once("a linear layer in microscaled form", given[0], grads);
+        return grads;
     }
 };
 
@@ -915,27 +933,6 @@ struct GatedPass : torch::CustomClassHolder {
     bool x, gate, up, b_gate, b_up;                                       // whose gradients are wanted
     std::vector<int64_t> shape;                                           // of x
 };
-
-// What the gradients of a pass come from: it refuses to be differentiated.
-struct Once : torch::autograd::Node {
-    std::string what;
-    Once(std::string w, torch::autograd::edge_list&& next) : Node(std::move(next)), what(std::move(w)) {}
-    torch::autograd::variable_list apply(torch::autograd::variable_list&&) override { throw std::runtime_error(what + " is differentiated once"); }
-};
-// In a backward pass whose graph is kept: its results as what they depend on has them, which is the running node's inputs, whatever is wanted of `given`, the gradient
-// that the pass was given.  Joined to those, the refusal is met by torch.autograd.grad as well, which runs only what lies between.
-void once(const char* what, const at::Tensor& given, torch::autograd::variable_list& grads)
-{
-    if (!at::GradMode::is_enabled()) return;
-    torch::autograd::edge_list next = torch::autograd::get_current_node()->next_edges();
-    next.push_back(torch::autograd::impl::gradient_edge(given));
-    const std::shared_ptr<torch::autograd::Node> node(new Once(what, std::move(next)), torch::autograd::deleteNode);
-    for (at::Tensor& g : grads) {
-        if (!g.defined()) continue;
-        g = g.detach();
-        torch::autograd::create_gradient_edge(g, node);
-    }
-}
 
 struct Gated : torch::autograd::Function<Gated> {
     using Context = torch::autograd::AutogradContext;

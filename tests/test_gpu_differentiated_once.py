@@ -22,7 +22,18 @@ def _gated(layers):
     return layer, (layer.gate.weight, layer.up.weight, layer.gate.bias, layer.up.bias)
 
 
-MODULES = {"gated": _gated}
+def _microscaled(layers):
+    layer = torch.nn.Linear(16, 8, device="cuda")
+    layer.forward = lambda x: layers.mx_linear(x, layer.weight, layer.bias)
+    return layer, (layer.weight, layer.bias)
+
+
+def _norm_microscaled(layers):
+    layer = layers.LayerNormMxLinear(16, 8, device="cuda")
+    return layer, (layer.norm.weight, layer.norm.bias, layer.linear.weight, layer.linear.bias)
+
+
+MODULES = {"gated": _gated, "microscaled": _microscaled, "norm and microscaled": _norm_microscaled}
 
 
 def _made(layers, kind):
