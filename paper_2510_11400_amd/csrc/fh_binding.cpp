@@ -643,8 +643,9 @@ struct Once : torch::autograd::Node {
 // that the pass was given.  Joined to those, the refusal is met by torch.autograd.grad as well, which runs only what lies between.
 void once(const char* what, const at::Tensor& given, torch::autograd::variable_list& grads)
 {
-    if (!at::GradMode::is_enabled()) return;
-    torch::autograd::edge_list next = torch::autograd::get_current_node()->next_edges();
+    const auto running = torch::autograd::get_current_node();
+    if (!at::GradMode::is_enabled() || !running) return;
+    torch::autograd::edge_list next = running->next_edges();
     next.push_back(torch::autograd::impl::gradient_edge(given));
     const std::shared_ptr<torch::autograd::Node> node(new Once(what, std::move(next)), torch::autograd::deleteNode);
     for (at::Tensor& g : grads) {
@@ -704,6 +705,22 @@ PyObject* refuse_tangents(PyObject*, PyObject* const* a, Py_ssize_t n)
     HANDLE_TH_ERRORS
     for (Py_ssize_t i = 0; i < n; ++i) no_tangent(tensor_or_none(a[i], "x"), "an input");
     Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
+// (what, dy, gradients): in a backward pass, the gradients as once() has them
+PyObject* differentiated_once(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n < 2) raise(PyExc_TypeError, "a name and a gradient are wanted");
+    const char* what = PyUnicode_AsUTF8(a[0]);
+    if (!what) throw python_error();
+    torch::autograd::variable_list grads;
+    for (Py_ssize_t i = 2; i < n; ++i) grads.push_back(tensor_or_none(a[i], "a gradient"));
+    once(what, tensor(a[1], "dy"), grads);
+    Ref t(PyTuple_New(n - 2));
+    for (Py_ssize_t i = 2; i < n; ++i) PyTuple_SET_ITEM(t.p, i - 2, wrap(grads[i - 2]));
+    return t.take();
     END_HANDLE_TH_ERRORS
 }
 
@@ -1018,7 +1035,7 @@ FH_EXIT
 
 #define FH_METHOD(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {FH_METHOD(mx_quantize), FH_METHOD(mx_dequantize), FH_METHOD(mx_matmul), FH_METHOD(layer_norm), FH_METHOD(layer_norm_mx),
-                           FH_METHOD(layer_norm_backward), FH_METHOD(layer_forward), FH_METHOD(layer_backward), FH_METHOD(mx_linear), FH_METHOD(refuse_tangents),
+                           FH_METHOD(layer_norm_backward), FH_METHOD(layer_forward), FH_METHOD(layer_backward), FH_METHOD(mx_linear), FH_METHOD(refuse_tangents), FH_METHOD(differentiated_once),
                            FH_METHOD(q8_quantize), FH_METHOD(q8_dequantize), FH_METHOD(q8_matmul), FH_METHOD(q8_gated), FH_METHOD(gated), FH_METHOD(gated_backward),
                            FH_METHOD(gated_linear),
                            FH_METHOD(use), {}};

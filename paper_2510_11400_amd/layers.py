@@ -44,14 +44,15 @@ class _LayerNorm(torch.autograd.Function):
         return y.view(x.shape)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        m, mean, rstd, weight = ctx.saved_tensors
-        mean, rstd = mean.view(torch.float32), rstd.view(torch.float32)
-        dx, dw, db = api.fh_layer_norm_backward(_rows(dy), m, mean, rstd, weight, sums=any(ctx.needs_input_grad[1:3]),
-                                                sums_dtype=ctx.sums_dtype)
-        return (dx.view(dy.shape) if ctx.needs_input_grad[0] else None, dw if ctx.needs_input_grad[1] else None,
-                db if ctx.needs_input_grad[2] else None, None)
+        with torch.no_grad():
+            m, mean, rstd, weight = ctx.saved_tensors
+            mean, rstd = mean.view(torch.float32), rstd.view(torch.float32)
+            dx, dw, db = api.fh_layer_norm_backward(_rows(dy), m, mean, rstd, weight, sums=any(ctx.needs_input_grad[1:3]),
+                                                    sums_dtype=ctx.sums_dtype)
+            grads = (dx.view(dy.shape) if ctx.needs_input_grad[0] else None, dw if ctx.needs_input_grad[1] else None,
+                     db if ctx.needs_input_grad[2] else None)
+        return (*_binding.differentiated_once("a layer norm", dy, *grads), None)
 
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5) -> torch.Tensor:

@@ -33,7 +33,12 @@ def _norm_microscaled(layers):
     return layer, (layer.norm.weight, layer.norm.bias, layer.linear.weight, layer.linear.bias)
 
 
-MODULES = {"gated": _gated, "microscaled": _microscaled, "norm and microscaled": _norm_microscaled}
+def _norm(layers):
+    layer = layers.LayerNorm(16, device="cuda")
+    return layer, (layer.weight, layer.bias)
+
+
+MODULES = {"gated": _gated, "microscaled": _microscaled, "norm and microscaled": _norm_microscaled, "norm": _norm}
 
 
 def _made(layers, kind):
