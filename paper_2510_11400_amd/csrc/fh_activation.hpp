@@ -10,29 +10,29 @@ namespace fh {
 
 inline bool is_activation(int a) { return a == FH_SILU || a == FH_GELU || a == FH_GELU_TANH; }
 
-// g times a factor s that goes from 0 to 1, each in a form that loses nothing where s is small:
+// g times a factor s that goes from 0 to 1, each in a form whose error goes by the size of s where that is small:
 //   silu        s = 1/(1 + e^-g)
 //   gelu_tanh   s = (1 + tanh z)/2 = 1/(1 + e^-2z), z = sqrt(2/pi) (g + 0.044715 g^3)
-//   gelu        s = the normal distribution function = erfc(-g/sqrt 2)/2.  For x = |g|/sqrt 2, erfc x = (a1 t + ... + a5 t^5) e^(-x^2), t = 1/(1 + p x)
-//               (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26: within 1.5e-7 of it everywhere, and since the power
-//               multiplies the error too, within some 1e-6 of its size); the derivative needs the same power.
-// Powers and reciprocals are the hardware's, a unit in the last place off.  The power's argument is rounded, which is |z| units of the power: what g's own
-// rounding costs it too.  An epilogue of 256 x 128 pairs is bound by these instructions: with the library's expf, erfcf and
-// correctly rounded divisions 8192 tokens of 768 -> 2048 took 3 us of 66 longer (silu).
-constexpr float kLog2E = 1.4426950408889634f, kSqrtHalf = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f, kTwoSqrt2OverPi = 1.5957691216057308f,
+//   gelu        s = the normal distribution function.  Its tail at x = |g| is e^(-x^2/2) R(x), and R(x), which goes from 1/2 to 1/(sqrt(2 pi) x), is a polynomial in
+//               t = 1/(1 + 0.348 x): a minimax fit weighted for the relative error, 2.7e-7 at most where the power is not 0 yet (x <= 13.4).  A coefficient less leaves 1.9e-6,
+//               one more 4e-8, which the roundings cover.  The derivative needs the same power.
+// Powers and reciprocals are the hardware's, a unit in the last place off.  The power's argument a is rounded, which is two or three half units of the power times |a|: a
+// multiple of what g's own rounding costs it.  Where s is below 2^-126 (g < -87, -10, -13) it is 0.  An epilogue of 256 x 128 pairs is bound by these
+// instructions: with the library's expf, erfcf and correctly rounded divisions 8192 tokens of 768 -> 2048 took 3 us of 66 longer (silu).
+constexpr float kLog2E = 1.4426950408889634f, kInvSqrt2Pi = 0.39894228040143268f, kTwoSqrt2OverPi = 1.5957691216057308f,
                 kCubic = 0.044715f;
 
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -kLog2E)); }
 // s of gelu, and e^(-g^2/2).
 __device__ __forceinline__ float normal_distribution(float g, float& power)
 {
-    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(g), 0.3275911f * kSqrtHalf, 1.0f));
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(g), 0.348f, 1.0f));
     power = __builtin_amdgcn_exp2f(g * g * (-0.5f * kLog2E));
-    float sum = __builtin_fmaf(t, 1.061405429f, -1.453152027f);
-    sum = __builtin_fmaf(t, sum, 1.421413741f);
-    sum = __builtin_fmaf(t, sum, -0.284496736f);
-    sum = __builtin_fmaf(t, sum, 0.254829592f);
-    const float beyond = 0.5f * (t * sum) * power;               // of |g|
+    constexpr float kTail[8] = {-3.38016544e-05f, 0.139593884f, 0.131631389f, 0.15915966f, -0.0252088439f, 0.25113973f, -0.205177411f, 0.0488954782f};
+    float tail = kTail[7];
+#pragma unroll
+    for (int i = 6; i >= 0; --i) tail = __builtin_fmaf(t, tail, kTail[i]);
+    const float beyond = tail * power;                           // |g|
     return g > 0.0f ? 1.0f - beyond : beyond;
 }
 

@@ -6,9 +6,9 @@ Bounds, in half steps of fp32 (2^-24 of the value).  A power of a rounded argume
 instruction; a reciprocal by 2.
   silu        a = g, r = 2; the power, an addition, the reciprocal and the product with g are 6 at most
   gelu_tanh   a = 2 z, r = 8 (the cubic term's constant, two products, the sum, two more constants with their products); the same 6
-  gelu        a = g^2/2, r = 3; beside the power s has t P(t), t = 1/(1 + p |g|).  t is off by 4 (its constant, the sum, the reciprocal), which R(g) = Phi(-g) e^(g^2/2) takes 2.9
-              times at most (at g = 0, where R'/R is 0.8 and p 0.28); eight steps of a polynomial whose terms' magnitudes add up to twice its value at most are 16, its
-              coefficients 2, its fit 2.4; the power's instruction, two products and that with g 5
+  gelu        a = g^2/2, r = 3; beside the power s has a polynomial P(t), t = 1/(1 + p |g|).  t is off by 4 (its constant, the sum, the reciprocal), which R(g) = Phi(-g) e^(g^2/2)
+              takes 2.3 times at most (at g = 0, where R'/R is 0.8 and p 0.348); seven steps of a polynomial whose terms' magnitudes add up to twice its value at most
+              are 14, its coefficients 2, its fit 4.5; the power's instruction, its product and that with g 4
 """
 from __future__ import annotations
 
@@ -38,7 +38,7 @@ def _factors(g, act):
     if act == "silu":
         return 2 * g.abs(), 6.0
     if act == "gelu":
-        return 1.5 * g * g, 37.0
+        return 1.5 * g * g, 34.0
     return 8 * math.sqrt(8.0 / math.pi) * (g + 0.044715 * g ** 3).abs(), 6.0
 
 
@@ -75,18 +75,3 @@ def test_the_slopes_lower_tail(api, act, least):
     power, beside = _factors(g, act)
     bound = STEP * ((power + beside) * s + (2 * (power + beside) + 8.0) * (want - s).abs() + want.abs())
     R.check(got, want, bound, act)
-
-
-@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_gates_up_to_the_end_of_the_range(api, act, dtype):
-    """From 1e6 to 3.4e38 either way: the activation is g or 0, its slope 1 or 0, whatever its powers do on the way."""
-    size = torch.logspace(6, 38.5, 651)
-    parts = _one_feature(torch.cat((size, -size)), 1, DTYPES[dtype])
-    g = parts[1].double().view(1, -1)
-    want = torch.where(g > 0, g, 0.0)
-    assert torch.equal(api.fh_gated(*parts, act).double(), want)
-    dh = torch.ones(1, g.numel(), device="cuda", dtype=DTYPES[dtype])
-    _, dw_gate, dw_up, db_gate, db_up = api.fh_gated_backward(dh, *parts[:3], torch.zeros_like(parts[4]), parts[4], act, needs_input=False)
-    assert torch.equal(db_gate.double(), (g[0] > 0).double()) and torch.equal(dw_gate[:, 0], db_gate)
-    assert torch.equal(db_up.double(), want[0]) and torch.equal(dw_up[:, 0], db_up)
