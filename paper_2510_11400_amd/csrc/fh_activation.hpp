@@ -61,8 +61,8 @@ __device__ __forceinline__ void activate(const float (&g)[N], int act, float (&v
         for (int i = 0; i < N; ++i) {
             const float square = g[i] * g[i], s = sigmoid(kTwoSqrt2OverPi * __builtin_fmaf(kCubic * g[i], square, g[i]));
             values[i] = g[i] * s;
-            // g s (1 - s) first: it is 0 where g^3 leaves the range
-            if (slopes) slopes[i] = __builtin_fmaf(g[i] * (s * (1.0f - s)), kTwoSqrt2OverPi * __builtin_fmaf(3.0f * kCubic, square, 1.0f), s);
+            // z' stays finite where g^2 leaves the range: s (1 - s) is 0 there
+            if (slopes) slopes[i] = __builtin_fmaf(g[i] * (s * (1.0f - s)), kTwoSqrt2OverPi * __builtin_fmaf(3.0f * kCubic, __builtin_fminf(square, 0x1p60f), 1.0f), s);
         }
     }
 }

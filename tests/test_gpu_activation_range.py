@@ -75,3 +75,18 @@ def test_the_slopes_lower_tail(api, act, least):
     power, beside = _factors(g, act)
     bound = STEP * ((power + beside) * s + (2 * (power + beside) + 8.0) * (want - s).abs() + want.abs())
     R.check(got, want, bound, act)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gates_up_to_the_end_of_the_range(api, act, dtype):
+    """From 1e6 to 3.4e38 either way: the activation is g or 0, its slope 1 or 0, whatever its powers do on the way."""
+    size = torch.logspace(6, 38.5, 651)
+    parts = _one_feature(torch.cat((size, -size)), 1, DTYPES[dtype])
+    g = parts[1].double().view(1, -1)
+    want = torch.where(g > 0, g, 0.0)
+    assert torch.equal(api.fh_gated(*parts, act).double(), want)
+    dh = torch.ones(1, g.numel(), device="cuda", dtype=DTYPES[dtype])
+    _, dw_gate, dw_up, db_gate, db_up = api.fh_gated_backward(dh, *parts[:3], torch.zeros_like(parts[4]), parts[4], act, needs_input=False)
+    assert torch.equal(db_gate.double(), (g[0] > 0).double()) and torch.equal(dw_gate[:, 0], db_gate)
+    assert torch.equal(db_up.double(), want[0]) and torch.equal(dw_up[:, 0], db_up)
