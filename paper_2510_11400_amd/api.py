@@ -1544,11 +1544,24 @@ def fh_q8_gated(x: Q8Matrix, w_gate: Q8Matrix, w_up: Q8Matrix, b_gate: Optional[
     return _binding.q8_gated(x, w_gate, w_up, b_gate, b_up, activation, out_dtype, out, workspace, stream)
 
 
+def gated_workspace_bytes(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor) -> int:
+    """Bytes of fh_gated's workspace for these operands: what of them lies at other multiples than of 16 bytes is laid out in it.  Operands of the same shapes, strides
+    and alignment need as many."""
+    return _binding.gated_workspace_bytes(x, w_gate, w_up)
+
+
+def gated_backward_workspace_bytes(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, b_gate: Optional[torch.Tensor] = None,
+                                   b_up: Optional[torch.Tensor] = None, needs_input: bool = True, needs_weight: bool = True,
+                                   needs_bias: bool = True) -> int:
+    """Bytes of fh_gated_backward's workspace for these operands and needs (and for all others of their shapes, strides and alignment)."""
+    return _binding.gated_backward_workspace_bytes(x, w_gate, w_up, b_gate, b_up, needs_input, needs_weight, needs_bias)
+
+
 def fh_gated(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, b_gate: Optional[torch.Tensor] = None,
              b_up: Optional[torch.Tensor] = None, activation: str = "silu", out: Optional[torch.Tensor] = None,
              workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Enqueue the gated projection act(x w_gate^T + b_gate) * (x w_up^T + b_up) of dense matrices of one dtype (rows contiguous, any row
-    strides); sums in fp32.  Without `workspace` one is allocated where the operands' alignment asks for it."""
+    strides); sums in fp32.  Without `workspace` (gated_workspace_bytes) one is allocated where the operands' alignment asks for it."""
     return _binding.gated(x, w_gate, w_up, b_gate, b_up, activation, out, workspace, stream)
 
 
@@ -1556,5 +1569,5 @@ def fh_gated_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w
                       b_up: Optional[torch.Tensor] = None, activation: str = "silu", needs_input: bool = True, needs_weight: bool = True,
                       needs_bias: bool = True, workspace: Optional[torch.Tensor] = None, stream=None):
     """Enqueue the backward pass of fh_gated from its inputs and its result's gradient; returns (dx, dw_gate, dw_up, db_gate, db_up), None for
-    what is not needed and for the gradient of a bias that is not there."""
+    what is not needed and for the gradient of a bias that is not there.  Without `workspace` (gated_backward_workspace_bytes) one is allocated."""
     return _binding.gated_backward(dh, x, w_gate, w_up, b_gate, b_up, activation, needs_input, needs_weight, needs_bias, workspace, stream)

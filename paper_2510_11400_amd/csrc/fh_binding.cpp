@@ -922,6 +922,26 @@ GatedGradients gated_backward_of(const Matrix& dh, const Matrix& x, const Matrix
     return g;
 }
 
+// (x, w_gate, w_up) -> bytes
+FH_ENTRY(gated_workspace_bytes, 3)
+    const Matrix x = matrix(a[0], "x"), gate = matrix(a[1], "w_gate"), up = matrix(a[2], "w_up");
+    const fh_gated_layer l = gated_layer(x, gate, up, Biases(at::Tensor(), at::Tensor(), gate.rows, x.device()), FH_SILU);
+    return PyLong_FromSize_t(fh_gated_workspace_bytes(&l, 0));
+FH_EXIT
+
+// (x, w_gate, w_up, b_gate, b_up, needs_input, needs_weight, needs_bias) -> bytes
+FH_ENTRY(gated_backward_workspace_bytes, 8)
+    const Matrix x = matrix(a[0], "x"), gate = matrix(a[1], "w_gate"), up = matrix(a[2], "w_up");
+    const Biases bias(tensor_or_none(a[3], "b_gate"), tensor_or_none(a[4], "b_up"), gate.rows, x.device());
+    fh_gated_layer l = gated_layer(x, gate, up, bias, FH_SILU);
+    l.needs = (truth(a[5]) ? FH_GATED_NEEDS_INPUT : 0) | (truth(a[6]) ? FH_GATED_NEEDS_WEIGHT : 0);
+    if (truth(a[7])) {                                           // it is looked at whether they are there
+        l.db_gate = bias.g;
+        l.db_up = bias.u;
+    }
+    return PyLong_FromSize_t(fh_gated_workspace_bytes(&l, 1));
+FH_EXIT
+
 // (x, w_gate, w_up, b_gate, b_up, activation, out, workspace, stream)
 FH_ENTRY(gated, 9)
     const Matrix x = matrix(a[0], "x"), gate = matrix(a[1], "w_gate"), up = matrix(a[2], "w_up");
@@ -1037,6 +1057,7 @@ FH_EXIT
 PyMethodDef g_methods[] = {FH_METHOD(mx_quantize), FH_METHOD(mx_dequantize), FH_METHOD(mx_matmul), FH_METHOD(layer_norm), FH_METHOD(layer_norm_mx),
                            FH_METHOD(layer_norm_backward), FH_METHOD(layer_forward), FH_METHOD(layer_backward), FH_METHOD(mx_linear), FH_METHOD(refuse_tangents), FH_METHOD(differentiated_once),
                            FH_METHOD(q8_quantize), FH_METHOD(q8_dequantize), FH_METHOD(q8_matmul), FH_METHOD(q8_gated), FH_METHOD(gated), FH_METHOD(gated_backward),
+                           FH_METHOD(gated_workspace_bytes), FH_METHOD(gated_backward_workspace_bytes),
                            FH_METHOD(gated_linear),
                            FH_METHOD(use), {}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_fh_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
