@@ -885,7 +885,7 @@ at::Tensor gated_forward_of(const Matrix& x, const Matrix& gate, const Matrix& u
 
 struct GatedGradients { at::Tensor dx, dw_gate, dw_up, db_gate, db_up; };
 // What gradients are wanted of.
-struct GatedNeeds { bool input, weight, b_gate, b_up; };
+struct GatedNeeds { bool input, gate, up, b_gate, b_up; };
 GatedGradients gated_backward_of(const Matrix& dh, const Matrix& x, const Matrix& gate, const Matrix& up, const Biases& bias, int activation, const GatedNeeds& needs,
                                  PyObject* workspace)
 {
@@ -894,19 +894,24 @@ GatedGradients gated_backward_of(const Matrix& dh, const Matrix& x, const Matrix
     if (dh.rows != x.rows || dh.cols != gate.rows || dh.dtype != x.dtype) raise(PyExc_ValueError, "dh must have the shape and the dtype of the result");
     on_device(dh.t, device, "dh");
     const at::ScalarType type = x.t.scalar_type();
-    l.needs = (needs.input ? FH_GATED_NEEDS_INPUT : 0) | (needs.weight ? FH_GATED_NEEDS_WEIGHT : 0);
+    l.needs = (needs.input ? FH_GATED_NEEDS_INPUT : 0) | (needs.gate || needs.up ? FH_GATED_NEEDS_WEIGHT : 0);
     l.dh = dh.data(); l.dh_stride = dh.stride;
     GatedGradients g;
     if (needs.input) {
         g.dx = new_matrix(x.rows, x.cols, type, device).t;
         l.dx = g.dx.data_ptr();
     }
-    if (needs.weight) {                                          // one behind the other: one product for both
-        Pair p = pair(gate.rows * gate.cols, type, device);
-        g.dw_gate = p.first.view({gate.rows, gate.cols});
-        g.dw_up = p.second.view({gate.rows, gate.cols});
-        l.dw_gate = p.first.data_ptr();
-        l.dw_up = p.second.data_ptr();
+    if (needs.gate || needs.up) {
+        if (needs.gate && needs.up) {                            // one behind the other: one product for both
+            Pair p = pair(gate.rows * gate.cols, type, device);
+            g.dw_gate = p.first.view({gate.rows, gate.cols});
+            g.dw_up = p.second.view({gate.rows, gate.cols});
+        } else {                                                 // apart: the one that is dropped gives its memory back, and costs a launch more
+            g.dw_gate = new_matrix(gate.rows, gate.cols, type, device).t;
+            g.dw_up = new_matrix(gate.rows, gate.cols, type, device).t;
+        }
+        l.dw_gate = g.dw_gate.data_ptr();
+        l.dw_up = g.dw_up.data_ptr();
     }
     if (needs.b_gate && bias.g) {
         g.db_gate = values(gate.rows, type, device);
@@ -957,7 +962,7 @@ FH_ENTRY(gated_backward, 12)
     const Matrix dh = matrix(a[0], "dh"), x = matrix(a[1], "x"), gate = matrix(a[2], "w_gate"), up = matrix(a[3], "w_up");
     const Biases bias(tensor_or_none(a[4], "b_gate"), tensor_or_none(a[5], "b_up"), gate.rows, x.device());
     const int activation = activation_of(a[6]);
-    const GatedNeeds needs = {truth(a[7]), truth(a[8]), truth(a[9]), truth(a[9])};
+    const GatedNeeds needs = {truth(a[7]), truth(a[8]), truth(a[8]), truth(a[9]), truth(a[9])};
     const On on(a[11], x.device());
     const GatedGradients g = gated_backward_of(dh, x, gate, up, bias, activation, needs, a[10]);
     for (const at::Tensor* t : {&g.dx, &g.dw_gate, &g.db_gate, &g.db_up}) on.lent(*t);
@@ -996,7 +1001,7 @@ struct Gated : torch::autograd::Function<Gated> {
             const Matrix x = matrix(saved[0], "x"), gate = matrix(saved[1], "w_gate"), up = matrix(saved[2], "w_up");
             const Biases bias(saved[3], saved[4], gate.rows, x.device());
             const GatedGradients g = gated_backward_of(matrix(dh, "dh"), x, gate, up, bias, pass->activation,
-                                                       {pass->x, pass->gate || pass->up, pass->b_gate, pass->b_up}, Py_None);
+                                                       {pass->x, pass->gate, pass->up, pass->b_gate, pass->b_up}, Py_None);
             if (pass->x) grads[0] = g.dx.view(pass->shape);
             if (pass->gate) grads[1] = g.dw_gate;
             if (pass->up) grads[2] = g.dw_up;
