@@ -1523,6 +1523,7 @@ def fh_q8_dequantize(m: Q8Matrix, out_dtype=torch.float32, out: Optional[torch.T
 
 
 def q8_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
+    """Bytes of fh_q8_matmul's workspace: none at present, as its product needs nothing laid out."""
     return _lib.fh_q8_matmul_workspace_bytes(m, n, k)
 
 
@@ -1533,6 +1534,7 @@ def fh_q8_matmul(a: Q8Matrix, b: Q8Matrix, bias: Optional[torch.Tensor] = None, 
 
 
 def q8_gated_workspace_bytes(tokens: int, hidden: int, features: int) -> int:
+    """Bytes of fh_q8_gated's workspace: none at present, as q8_matmul_workspace_bytes."""
     return _lib.fh_q8_gated_workspace_bytes(tokens, hidden, features)
 
 

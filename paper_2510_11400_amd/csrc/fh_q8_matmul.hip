@@ -34,6 +34,7 @@ ProductArgs q8_args(const void* a, int64_t m, int64_t n, int64_t k, void* out, i
 
 extern "C" {
 
+// No kernel here lays anything out: a workspace is taken, as by the other products, and left alone.
 size_t fh_q8_matmul_workspace_bytes(int64_t, int64_t, int64_t) { return 0; }
 size_t fh_q8_gated_workspace_bytes(int64_t, int64_t, int64_t) { return 0; }
 
@@ -51,9 +52,6 @@ fh_status fh_q8_matmul(const fh_q8_product* q, void* stream)
         !is_aligned(q->workspace, 16)) return FH_ERR_ALIGNMENT;
     if (q->a_cap < q8_bytes(q->m, q->k) || q->b_cap < q8_bytes(q->n, q->k) || q->out_cap < strided_elements(q->m, q->n, q->stride) * size)
         return FH_ERR_BUFFER_TOO_SMALL;
-    const size_t workspace = fh_q8_matmul_workspace_bytes(q->m, q->n, q->k);
-    if (workspace && !q->workspace) return FH_ERR_NULL;
-    if (q->workspace_cap < workspace) return FH_ERR_BUFFER_TOO_SMALL;
     ProductArgs p = q8_args(q->a, q->m, q->n, q->k, q->out, q->stride);
     p.b = static_cast<const uint8_t*>(q->b);
     p.bias = q->bias;
@@ -75,9 +73,6 @@ fh_status fh_q8_gated(const fh_q8_gated_product* q, void* stream)
         !is_aligned(q->up_bias, bias) || !is_aligned(q->workspace, 16)) return FH_ERR_ALIGNMENT;
     if (q->x_cap < q8_bytes(q->m, q->k) || q->gate_cap < q8_bytes(q->n, q->k) || q->up_cap < q8_bytes(q->n, q->k) ||
         q->out_cap < strided_elements(q->m, q->n, q->stride) * size) return FH_ERR_BUFFER_TOO_SMALL;
-    const size_t workspace = fh_q8_gated_workspace_bytes(q->m, q->n, q->k);
-    if (workspace && !q->workspace) return FH_ERR_NULL;
-    if (q->workspace_cap < workspace) return FH_ERR_BUFFER_TOO_SMALL;
     ProductArgs p = q8_args(q->x, q->m, q->n, q->k, q->out, q->stride);
     p.b = static_cast<const uint8_t*>(q->gate);
     p.b2 = static_cast<const uint8_t*>(q->up);
