@@ -642,7 +642,9 @@ fh_status fh_mx_layer_backward(const fh_mx_layer *layer, void *stream);
  * fh_q8_gated computes out[i][j] = act(gate[i][j]) * up[i][j] of two such products (with their biases)
  * of one x (m x k) and the weights gate and up (n x k each), in one pass.
  *   act (fh_activation): FH_SILU g / (1 + e^-g); FH_GELU g times the normal distribution function at g;
- *   FH_GELU_TANH (g / 2) (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))).
+ *   FH_GELU_TANH (g / 2) (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))).  Each is off by some half units of its
+ *   own value, in the lower tail by up to 2 |g|, 1.5 g^2 and 13 |g + 0.044715 g^3| more; gates below
+ *   some -87, -13 and -10 give 0.
  * k = 0: the products are their biases, or zeros.
  *
  * Stored matrices and workspaces are 16-byte aligned, plain matrices and vectors aligned to their

@@ -13,12 +13,13 @@ inline bool is_activation(int a) { return a == FH_SILU || a == FH_GELU || a == F
 // g times a factor s that goes from 0 to 1, each in a form whose error goes by the size of s where that is small:
 //   silu        s = 1/(1 + e^-g)
 //   gelu_tanh   s = (1 + tanh z)/2 = 1/(1 + e^-2z), z = sqrt(2/pi) (g + 0.044715 g^3)
-//   gelu        s = the normal distribution function.  Its tail at x = |g| is e^(-x^2/2) R(x), and R(x), which goes from 1/2 to 1/(sqrt(2 pi) x), is a polynomial in
-//               t = 1/(1 + 0.348 x): a minimax fit weighted for the relative error, 2.7e-7 at most where the power is not 0 yet (x <= 13.4).  A coefficient less leaves 1.9e-6,
-//               one more 4e-8, which the roundings cover.  The derivative needs the same power.
-// Powers and reciprocals are the hardware's, a unit in the last place off.  The power's argument a is rounded, which is two or three half units of the power times |a|: a
-// multiple of what g's own rounding costs it.  Where s is below 2^-126 (g < -87, -10, -13) it is 0.  An epilogue of 256 x 128 pairs is bound by these
-// instructions: with the library's expf, erfcf and correctly rounded divisions 8192 tokens of 768 -> 2048 took 3 us of 66 longer (silu).
+//   gelu        s = the normal distribution function.  Its tail at x = |g| is e^(-x^2/2) R(x), and R(x), which goes from 1/2 to 1/(sqrt(2 pi) x), is a
+//               polynomial in t = 1/(1 + 0.348 x): a minimax fit weighted for the relative error, 2.7e-7 at most where the power is not 0 yet (x <= 13.4).
+//               A coefficient less leaves 1.9e-6, one more 4e-8, which the roundings cover.  The derivative needs the same power.
+// Powers and reciprocals are the hardware's, a unit in the last place off.  The power's argument a is off by 2, 8 and 3 half units of its own, as many of the
+// power's times |a|: a multiple of what g's own rounding costs it.  Below 2^-126 (g beyond -87, -10, -13) powers and reciprocals are 0 to the hardware.
+// An epilogue of 256 x 128 pairs is bound by these instructions: with the library's expf, erfcf and correctly rounded divisions 8192 tokens of
+// 768 -> 2048 took 3 us of 66 longer (silu).
 constexpr float kLog2E = 1.4426950408889634f, kInvSqrt2Pi = 0.39894228040143268f, kTwoSqrt2OverPi = 1.5957691216057308f,
                 kCubic = 0.044715f;
 

@@ -583,9 +583,10 @@ __device__ __forceinline__ void tile_epilogue(const Args& p, T* out, const typen
 // The chunks of the next tile follow those of the last without a gap: a tile's outputs go through LDS of their own, and since memory
 // operations are counted in their order and the loads are sent before the outputs are, the next wait is for the loads alone.
 // Of a pair's 64 columns of a wave the first 32 are the gate's and the others the same columns of up, so that both sums of an output are one wave's.
-// Measured: 8 bits, 8192 x 8192 x 4096, 240 us, 2.3 POP/s; bf16, pairs of 4096 x 8192 x 4096, 450 us, 1.22 PFLOP/s, and 8192 x 2048 x 768, 56 us.  The large ones
-// are bound by the card's power: the matrix unit is busy 56 to 61 % of the cycles, and the busier it is kept the further the clock falls (1.93 to 1.86 GHz); without
-// the loads 377 of 450 us were left.  In the last a tile has 12 chunks, and the second of two rounds of tiles has nothing to hide its outputs behind.
+// Measured, one call among others (a trace has gaps between them and varies more): 8 bits, 8192 x 8192 x 4096, 240 to 255 us, 2.2 to 2.3 POP/s; bf16, pairs of
+// 4096 x 8192 x 4096, 450 us, 1.22 PFLOP/s, and 8192 x 2048 x 768, 56 us.  The large ones are bound by the card's power: the matrix unit is busy 56 to 61 % of the
+// cycles, and the busier it is kept the further the clock falls (1.93 to 1.86 GHz); without the loads 377 of 450 us were left.  In the last a tile has 12 chunks,
+// and the second of two rounds of tiles has nothing to hide its outputs behind.
 template <typename OP, Made MADE, Lies LA, Lies LB, typename T, int B, int WN>
 __global__ __launch_bounds__(2 * WN * 64, B > 128 ? 1 : 2) void product_tile_kernel(typename ArgsOf<MADE, LB>::type p)
 {

@@ -17,8 +17,10 @@ constexpr int64_t product_side(ProductTile t)
 // The rows that a partial sum of columns stands for: a workgroup's, of the tiles through LDS a wave's.
 constexpr int64_t product_sum_rows(ProductTile t) { return product_side(t) / (t == ProductTile::square128 || t == ProductTile::square256 ? 2 : 1); }
 
-// The expected time in hundredths of a microsecond, from `tiles` of c chunks each: lines through what the kernels measured, the choice by which is within
-// 1 % of the best on average over 55 products of 8-bit integers and bf16, plain and gated, and 4 % of 10 in fp32 (us, in the order above):
+// The expected time in hundredths of a microsecond, from `tiles` of c chunks each: lines through what the kernels measured.  The choice by them is within
+// 1 % of the best on average over 55 products of 8-bit integers and bf16, plain and gated, and 4 % of 10 in fp32; the worst one met took a fifth longer than
+// the best (fp32, pairs of 1748 x 1557 x 690, 103 us and 85: 350 tiles of 128 on 256 units take two rounds where the line counts 1.4).  A time itself may be
+// off by more, most for pairs of few chunks, whose activations no line knows (8 bits, 509 x 2731 x 1023: 9.8 us expected, 14 taken).  Some (us, in the order above):
 //     8-bit  64 x 8192 x 4096    9.3  10.0  10.4  25.2  46.6     1024 x 2048 x 2048   15.0  18.8  11.5  13.8  27.5     4096 x 4096 x 1024  65.0  94.4  51.9  27.1  23.7
 //           512 x 768 x 768      4.1   4.2   5.2   8.3  16.3     2048 x 2048 x 768    15.6  21.6  12.1   9.7  17.1     8192 x 1024 x 8192 283.0 283.9 150.2  71.4  84.1
 //     bf16, pairs of 1024 x 2048 x 768  21.4 28.9 15.0 13.2 25.9    4096 x 2048 x 768   111.1 129.4  66.2  34.8  32.3     256 x 4096 x 4096   49.5  47.5  27.8  47.6  83.6
@@ -72,9 +74,10 @@ inline bool few_rows_dense(int64_t m, bool slow, bool laid_out) { return m <= kM
 
 // Whether a backward pass keeps what the rounding of [dg | du] to bf16 leaves, as two bf16 values for one (by the kernels up to waves64 alone).  The sums of dx and dW
 // average a rounding's errors where many gradients are summed; where few are, or a few outweigh the others, the results' errors are up to three times those of their own
-// rounding (over 1.5 times in 13 of 100 random layers of 2^14 to 2^18 gradients, 7 and 2 in the next doublings, against 1.4 for large ones).  It costs little there
-// (us; tokens x features x hidden, without and with): 26 x 63 x 49 16.5 and 16.5, 200 x 400 x 300 15 and 17, 333 x 515 x 700 26 and 30, 4096 x 1024 x 64 30 and 34; a layer of
-// 1024 x 512 x 512 would take 25 and 34, of 8 x 4000 x 8192 104 and 173.
+// rounding (over 1.5 times in 13 of 100 random layers of 2^14 to 2^18 gradients, 7 and 2 in the next doublings, against 1.4 for large ones).  Within these limits it costs
+// (us; tokens x features x hidden, without and with): 26 x 63 x 49 16.5 and 16.3, 200 x 400 x 300 15.3 and 17.1, 333 x 515 x 700 27 and 30, 4096 x 512 x 64 26.5 and 29,
+// 1024 x 256 x 512 23 and 28.5, 512 x 256 x 1024 24.5 and 32, 16 x 4000 x 2048 38.5 and 55.7; beyond them 4096 x 1024 x 64 would take 30.6 and 33.8, 1024 x 512 x 512
+// 24 and 33.5, 8 x 4000 x 8192 104 and 174.
 constexpr int64_t kMostWithRests = (int64_t)1 << 19, kMostTermsWithRests = (int64_t)1 << 27;
 inline bool product_with_rests(int64_t tokens, int64_t features, int64_t hidden, bool slow)
 {

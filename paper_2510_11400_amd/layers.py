@@ -9,7 +9,8 @@ the weight's gradient as it is, so nothing is restored.  Behind a layer norm it 
     dx = dy W           dy by rows, W by columns             (backward)
     dW = dy^T x         dy by columns, x by columns (the saved form)
 
-Matrix products are of 4-bit values with binary32 sums; parameters and their gradients keep their own dtype.
+Matrix products are of 4-bit values with binary32 sums; parameters and their gradients keep their own dtype.  Every layer here is differentiated once: a
+loss that holds a layer's gradients raises when its own are asked for.
 
 The gated projection of a feed-forward block, act(x Wg^T + bg) * (x Wu^T + bu), is dense in training and saves its input alone
 (as autograd saves it, so that SavedActivations compresses it): what has the hidden width is computed again in the
@@ -80,7 +81,7 @@ def layer_norm_mx_linear(x: torch.Tensor, norm_weight: Optional[torch.Tensor], n
 def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, b_gate: Optional[torch.Tensor] = None,
                  b_up: Optional[torch.Tensor] = None, activation: str = "silu") -> torch.Tensor:
     """act(x w_gate^T + b_gate) * (x w_up^T + b_up) over the last dimension, differentiable; everything of one dtype.  x is saved as autograd saves
-    it (hooks.SavedActivations compresses it), and nothing of the hidden width.  Captured in a graph with gradients wanted, it refuses a leaf that is part of a
+    it (hooks.SavedActivations compresses it), and nothing of the hidden width.  Differentiated once: a loss that holds its gradients is refused.  Captured in a graph with gradients wanted, it refuses a leaf that is part of a
     graph of autograd which was made eagerly on the default stream and is still alive: the backward pass would have that stream wait for the capture."""
     return _binding.gated_linear(x, w_gate, w_up, b_gate, b_up, activation)
 
