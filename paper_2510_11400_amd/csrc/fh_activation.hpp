@@ -14,8 +14,8 @@ inline bool is_activation(int a) { return a == FH_SILU || a == FH_GELU || a == F
 //   silu        s = 1/(1 + e^-g)
 //   gelu_tanh   s = (1 + tanh z)/2 = 1/(1 + e^-2z), z = sqrt(2/pi) (g + 0.044715 g^3)
 //   gelu        s = the normal distribution function.  Its tail at x = |g| is e^(-x^2/2) R(x), and R(x), which goes from 1/2 to 1/(sqrt(2 pi) x), is a
-//               polynomial in t = 1/(1 + 0.348 x): a minimax fit weighted for the relative error, 2.7e-7 at most where the power is not 0 yet (x <= 13.4).
-//               A coefficient less leaves 1.9e-6, one more 4e-8, which the roundings cover.  The derivative needs the same power.
+//               polynomial in t = 1/(1 + 0.348 x): a minimax fit weighted for the relative error, 2.7e-7 at most where the power is not 0 yet (x <= 13.4), 3.2e-7
+//               with its constants in binary32.  A coefficient less leaves 1.9e-6, one more 4e-8, which the roundings cover.  The derivative needs the same power.
 // Powers and reciprocals are the hardware's, a unit in the last place off.  The power's argument a is off by 2, 8 and 3 half units of its own, as many of the
 // power's times |a|: a multiple of what g's own rounding costs it.  Below 2^-126 (g beyond -87, -10, -13) powers and reciprocals are 0 to the hardware.
 // An epilogue of 256 x 128 pairs is bound by these instructions: with the library's expf, erfcf and correctly rounded divisions 8192 tokens of
