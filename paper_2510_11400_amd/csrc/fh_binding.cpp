@@ -1013,15 +1013,17 @@ struct Gated : torch::autograd::Function<Gated> {
     }
 };
 
-// A leaf has one node that takes its gradient, of the stream on which it was first used, for as long as any graph of it lives.  A captured backward pass has that
-// stream wait for the captured one; the default stream cannot, and the process ends.
+// What takes a tensor's gradient is of one stream: of a leaf the one on which it was first used, for as long as any graph of it lives; of another tensor the one on which
+// it was computed.  A captured backward pass has that stream wait for the captured one; the default stream cannot, and the process ends.
 void no_eager_graph(const at::Tensor& t, const char* what)
 {
-    if (!t.defined() || !t.requires_grad() || !t.is_leaf()) return;
-    const auto node = torch::autograd::impl::try_get_grad_accumulator(t);
+    if (!t.defined() || !t.requires_grad()) return;
+    const auto node = t.is_leaf() ? torch::autograd::impl::try_get_grad_accumulator(t) : t.grad_fn();
     const auto stream = node ? node->stream() : std::nullopt;
-    if (stream && stream->id() == 0)
+    if (!stream || stream->id() != 0) return;
+    if (t.is_leaf())
         raise(PyExc_RuntimeError, "%s is part of a graph of autograd from outside of this capture that is still alive; delete what came of it before capturing", what);
+    raise(PyExc_RuntimeError, "%s comes of a graph of autograd from outside of this capture; detach it, or compute it inside", what);
 }
 
 // (x, w_gate, w_up, b_gate, b_up, activation) -> h

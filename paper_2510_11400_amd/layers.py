@@ -81,8 +81,9 @@ def layer_norm_mx_linear(x: torch.Tensor, norm_weight: Optional[torch.Tensor], n
 def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, b_gate: Optional[torch.Tensor] = None,
                  b_up: Optional[torch.Tensor] = None, activation: str = "silu") -> torch.Tensor:
     """act(x w_gate^T + b_gate) * (x w_up^T + b_up) over the last dimension, differentiable; everything of one dtype.  x is saved as autograd saves
-    it (hooks.SavedActivations compresses it), and nothing of the hidden width.  Differentiated once: a loss that holds its gradients is refused.  Captured in a graph with gradients wanted, it refuses a leaf that is part of a
-    graph of autograd which was made eagerly on the default stream and is still alive: the backward pass would have that stream wait for the capture."""
+    it (hooks.SavedActivations compresses it), and nothing of the hidden width.  Differentiated once: a loss that holds its gradients is refused.  Captured in a
+    graph with gradients wanted, it refuses a tensor that wants one and was computed eagerly on the default stream, or is a leaf of a graph of autograd made there that is
+    still alive: the backward pass would have that stream wait for the capture."""
     return _binding.gated_linear(x, w_gate, w_up, b_gate, b_up, activation)
 
 
